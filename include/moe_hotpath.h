@@ -328,6 +328,77 @@ int moe_router_bwd(const moe_bf16* x, const float* Wr, const float* dlogits, int
                    moe_bf16* dx, float* dWr, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * In front of a layer: the residual's addition and the root-mean-square norm, with s = bf16(x + r) and
+ * q[t] = 1 / sqrt(mean over c of s[t, c]^2 + eps):
+ *   sum[t, c] = s[t, c];  y[t, c] = s[t, c] * q[t] * w[c]  (fp32, rounded once);  rstd[t] = q[t] if rstd is not NULL
+ *   x, r, sum, y [T, d] bf16; w [d] fp32; rstd [T] fp32 or NULL.  r may be NULL (the first norm: s = x); sum may then be NULL.
+ *   sum may be x or r, and y too.  d % 8 == 0, d <= 32768; eps >= 0.
+ */
+int moe_add_rms_norm(const moe_bf16* x, const moe_bf16* r, const float* w, int T, int d, float eps,
+                     moe_bf16* sum, moe_bf16* y, float* rstd, void* stream);
+
+/*
+ * The same with y in 8 bits, the input of products in e4m3: each `group` columns of a row share a scale,
+ *   scale[t, i] = max |y| / 448 over the group;  codes[t, c] = e4m3(y[t, c] / scale)  (codes of an all-zero group are zero)
+ *   codes [T, d] bytes (OCP e4m3, nearest even); scale [T, d / group] fp32.  group: 0 (one per row), or a power of two from 8 to 512
+ *   that divides d.  The rest as moe_add_rms_norm.
+ */
+int moe_add_rms_norm_8bit(const moe_bf16* x, const moe_bf16* r, const float* w, int T, int d, float eps, int group,
+                          moe_bf16* sum, uint8_t* codes, float* scale, float* rstd, void* stream);
+
+/*
+ * Derivative of moe_add_rms_norm, from dy and the gradient dsum of the sum itself (NULL: none):
+ *   dx[t, c] = dsum[t, c] + q (dy w - s q^2 mean over c of (dy w s)): the gradient of x and of r alike
+ *   dw[c] = sum over t of dy s q   (fp32, a fixed order)
+ *   dy, dsum, sum, dx [T, d] bf16 (dx may be dy or dsum); w, dw [d] fp32; rstd [T] as the forward call left it.
+ *   ws at least moe_add_rms_norm_bwd_workspace_bytes(T, d).
+ */
+size_t moe_add_rms_norm_bwd_workspace_bytes(int T, int d);
+int moe_add_rms_norm_bwd(const moe_bf16* dy, const moe_bf16* dsum, const moe_bf16* sum, const float* w, const float* rstd,
+                         int T, int d, moe_bf16* dx, float* dw, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Behind the layers: softmax cross entropy of the vocabulary head without the logits in memory.  With z[t] = x[t] . W^T:
+ *   lse[t] = log sum over v of exp(z[t, v]);  loss[t] = lse[t] - z[t, target[t]]
+ * and zeros for a token whose target lies outside [0, V): it counts for nothing, and takes no time in the products.
+ *   x [T, d] bf16; W [V, d] bf16; target [T] int32; loss, lse [T] fp32.  d % 64 == 0; V <= 2^20.
+ *   ws at least moe_head_fwd_workspace_bytes(T, d, V, 0): about T d * 2 + T V * 3 / 16 bytes.
+ * Precondition: the logits are finite.
+ */
+size_t moe_head_fwd_workspace_bytes(int T, int d, int V, int K);
+int moe_head_ce_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, int T, int d, int V,
+                    float* loss, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Its derivative for given dloss [T] fp32 (weights, and the division by a number of tokens, are in it):
+ *   dz[t, v] = dloss[t] (exp(z[t, v] - lse[t]) - [v == target[t]]);  dx = dz . W;  dW = dz^T . x
+ *   dx [T, d], dW [V, d] bf16, overwritten (zeros for a token without a target); loss, lse as the forward call left them.
+ * The logits are formed again, dz is rounded to bf16 in the workspace, a piece of v_piece columns of the vocabulary at a time (a multiple
+ * of 256; 0: as many as keep a piece under 2 GiB).  The workspace is about T d * 2 + T v_piece * 2 bytes and
+ * T d * 4 for each part that dx is summed in.
+ */
+size_t moe_head_bwd_workspace_bytes(int T, int d, int V, int K, int v_piece);
+int moe_head_ce_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, const float* loss, const float* lse, const float* dloss,
+                    int T, int d, int V, int v_piece, moe_bf16* dx, moe_bf16* dW, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Cross entropy together with distillation from a teacher's top logits.  A token's entries are ids[t, j] with teacher[t, j], j < K <= 1024,
+ * those with an id outside [0, V) or a logit of -infinity left out.  With q = softmax over the entries of teacher / temperature:
+ *   kd[t] = sum over the entries of q (log q - log p),  p = softmax over the vocabulary of z / temperature
+ *   lse_t[t] = log sum over v of exp(z[t, v] / temperature)
+ * (zeros for a token without entries), and loss, lse as above, either of the two with or without the other.
+ *   ids [T, K] int32; teacher [T, K] fp32; kd, lse_t [T] fp32; 0 < temperature < infinity.
+ * Backward, for dloss and dkd [T] fp32:  dz += dkd / temperature (p - q) for a token with entries.
+ * Preconditions: a token's valid ids are distinct, their logits not +infinity or NaN.
+ */
+int moe_head_distill_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, const int32_t* ids, const float* teacher,
+                         float temperature, int T, int d, int V, int K, float* loss, float* lse, float* kd, float* lse_t,
+                         void* ws, size_t ws_bytes, void* stream);
+int moe_head_distill_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, const int32_t* ids, const float* teacher,
+                         float temperature, const float* loss, const float* lse, const float* lse_t, const float* dloss, const float* dkd,
+                         int T, int d, int V, int K, int v_piece, moe_bf16* dx, moe_bf16* dW, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Several stages of one layer with one call: the calls above in the layer's order, on buffers that the caller
  * laid out once, so that a small step does not spend its time crossing a language boundary a dozen times.
  * `what` is a sum of MOE_LAYER_ROUTER (moe_router_fwd into logits), MOE_LAYER_FWD (Stages 1-5), MOE_LAYER_BWD

@@ -26,6 +26,9 @@ EXPORTS = [
     "moe_unpermute_combine", "moe_unpermute_combine_bwd", "moe_prof_enable", "moe_prof_count", "moe_prof_read", "moe_prof_mfma_ceiling", "moe_prof_stream_read",
     "moe_router_fwd", "moe_route_bwd", "moe_router_bwd_workspace_bytes", "moe_router_bwd",
     "moe_permute_static_ws_capacity", "moe_permute_static_ws", "moe_layer_run",
+    "moe_add_rms_norm", "moe_add_rms_norm_8bit", "moe_add_rms_norm_bwd_workspace_bytes", "moe_add_rms_norm_bwd",
+    "moe_head_fwd_workspace_bytes", "moe_head_bwd_workspace_bytes", "moe_head_ce_fwd", "moe_head_ce_bwd",
+    "moe_head_distill_fwd", "moe_head_distill_bwd",
 ]
 
 _ERR = {-1: "MOE_ERR_INVALID (bad pointer, alignment or size)", -2: "MOE_ERR_WORKSPACE (workspace too small)",
@@ -64,6 +67,10 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.moe_router_bwd_workspace_bytes.argtypes = [c_int] * 3
     lib.moe_permute_static_ws_capacity.restype = c_sz
     lib.moe_permute_static_ws_capacity.argtypes = []
+    for name, n in (("moe_add_rms_norm_bwd_workspace_bytes", 2), ("moe_head_fwd_workspace_bytes", 4), ("moe_head_bwd_workspace_bytes", 5)):
+        getattr(lib, name).restype = c_sz
+        getattr(lib, name).argtypes = [c_int] * n
+    c_float = ctypes.c_float
     sigs = {
         "moe_route": [vp, c_int, c_int, c_int, c_int, vp, vp, vp],
         "moe_permute": [vp, vp, c_int, c_int, c_int, c_int, c_int, c_int, vp, vp, vp, vp, vp, c_sz, vp],
@@ -84,6 +91,13 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "moe_route_bwd": [vp, vp, vp, c_int, c_int, c_int, c_int, vp, vp],
         "moe_router_bwd": [vp, vp, vp, c_int, c_int, c_int, vp, vp, vp, c_sz, vp],
         "moe_layer_run": [vp, c_int, vp],
+        "moe_add_rms_norm": [vp, vp, vp, c_int, c_int, c_float, vp, vp, vp, vp],
+        "moe_add_rms_norm_8bit": [vp, vp, vp, c_int, c_int, c_float, c_int, vp, vp, vp, vp, vp],
+        "moe_add_rms_norm_bwd": [vp] * 5 + [c_int, c_int, vp, vp, vp, c_sz, vp],
+        "moe_head_ce_fwd": [vp] * 3 + [c_int] * 3 + [vp] * 3 + [c_sz, vp],
+        "moe_head_ce_bwd": [vp] * 6 + [c_int] * 4 + [vp] * 3 + [c_sz, vp],
+        "moe_head_distill_fwd": [vp] * 5 + [c_float] + [c_int] * 4 + [vp] * 5 + [c_sz, vp],
+        "moe_head_distill_bwd": [vp] * 5 + [c_float] + [vp] * 5 + [c_int] * 5 + [vp] * 3 + [c_sz, vp],
         "moe_prof_enable": [c_int],
         "moe_prof_count": [],
         "moe_prof_read": [c_int, ctypes.c_char_p, c_int, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(c_int)],
@@ -399,6 +413,109 @@ def moe_router_bwd(x, Wr, dlogits, dx, dWr, ws) -> None:
     _want(dWr, torch.float32, (E, d), "dWr")
     _check(load().moe_router_bwd(_p(x), _p(Wr), _p(dlogits), T, d, E, _p(dx), _p(dWr), _p(ws),
                                  ws.numel() * ws.element_size(), _stream()), "moe_router_bwd")
+
+
+def moe_add_rms_norm_bwd_workspace_bytes(T: int, d: int) -> int:
+    return int(load().moe_add_rms_norm_bwd_workspace_bytes(T, d))
+
+
+def _norm_args(x, r, w, total, rstd):
+    T, d = x.shape
+    _want(x, BF16, name="x")
+    _want(w, torch.float32, (d,), "w")
+    for t, name in ((r, "r"), (total, "sum")):
+        if t is not None:
+            _want(t, BF16, (T, d), name)
+    if rstd is not None:
+        _want(rstd, torch.float32, (T,), "rstd")
+    return T, d
+
+
+def moe_add_rms_norm(x, r, w, eps: float, sum, y, rstd=None) -> None:
+    """sum = x + r and its root-mean-square norm y; rstd, which the backward needs, may be None, r (and then sum) too."""
+    T, d = _norm_args(x, r, w, sum, rstd)
+    _want(y, BF16, (T, d), "y")
+    _check(load().moe_add_rms_norm(_p(x), _p(r), _p(w), T, d, eps, _p(sum), _p(y), _p(rstd), _stream()), "moe_add_rms_norm")
+
+
+def moe_add_rms_norm_8bit(x, r, w, eps: float, group: int, sum, codes, scale, rstd=None) -> None:
+    """The same with y as e4m3 codes (float8_e4m3fn) and a scale per ``group`` columns (0: per row)."""
+    T, d = _norm_args(x, r, w, sum, rstd)
+    if group < 0 or (group > 0 and d % group):
+        raise MoeError(f"group: {group} does not divide {d} columns")
+    _want(codes, torch.float8_e4m3fn, (T, d), "codes")
+    _want(scale, torch.float32, (T, d // (group or d)), "scale")
+    _check(load().moe_add_rms_norm_8bit(_p(x), _p(r), _p(w), T, d, eps, group, _p(sum), _p(codes), _p(scale), _p(rstd), _stream()),
+           "moe_add_rms_norm_8bit")
+
+
+def moe_add_rms_norm_bwd(dy, dsum, sum, w, rstd, dx, dw, ws) -> None:
+    """dx is the gradient of both x and r; dsum, the gradient of the sum itself, may be None."""
+    T, d = sum.shape
+    for t, name in ((dy, "dy"), (sum, "sum"), (dx, "dx")):
+        _want(t, BF16, (T, d), name)
+    if dsum is not None:
+        _want(dsum, BF16, (T, d), "dsum")
+    _want(w, torch.float32, (d,), "w")
+    _want(rstd, torch.float32, (T,), "rstd")
+    _want(dw, torch.float32, (d,), "dw")
+    _check(load().moe_add_rms_norm_bwd(_p(dy), _p(dsum), _p(sum), _p(w), _p(rstd), T, d, _p(dx), _p(dw), _p(ws),
+                                       ws.numel() * ws.element_size(), _stream()), "moe_add_rms_norm_bwd")
+
+
+def moe_head_fwd_workspace_bytes(T: int, d: int, V: int, K: int = 0) -> int:
+    return int(load().moe_head_fwd_workspace_bytes(T, d, V, K))
+
+
+def moe_head_bwd_workspace_bytes(T: int, d: int, V: int, K: int = 0, v_piece: int = 0) -> int:
+    return int(load().moe_head_bwd_workspace_bytes(T, d, V, K, v_piece))
+
+
+def _head_args(x, W, target, ids=None, teacher=None, rows=()):
+    (T, d), V = x.shape, W.shape[0]
+    _want(x, BF16, name="x")
+    _want(W, BF16, (V, d), "W")
+    _want(target, torch.int32, (T,), "target")
+    if ids is not None:
+        _want(ids, torch.int32, (T, ids.shape[-1]), "ids")
+        _want(teacher, torch.float32, tuple(ids.shape), "teacher")
+    for name, t in rows:
+        _want(t, torch.float32, (T,), name)
+    return T, d, V
+
+
+def moe_head_ce_fwd(x, W, target, loss, lse, ws) -> None:
+    """Cross entropy of the vocabulary head, token by token; a target outside the vocabulary (-100) counts for nothing."""
+    T, d, V = _head_args(x, W, target, rows=(("loss", loss), ("lse", lse)))
+    _check(load().moe_head_ce_fwd(_p(x), _p(W), _p(target), T, d, V, _p(loss), _p(lse), _p(ws), ws.numel() * ws.element_size(),
+                                  _stream()), "moe_head_ce_fwd")
+
+
+def moe_head_ce_bwd(x, W, target, loss, lse, dloss, v_piece: int, dx, dW, ws) -> None:
+    """dx and dW are overwritten; v_piece columns of the vocabulary at a time (0: the library chooses)."""
+    T, d, V = _head_args(x, W, target, rows=(("loss", loss), ("lse", lse), ("dloss", dloss)))
+    _want(dx, BF16, (T, d), "dx")
+    _want(dW, BF16, (V, d), "dW")
+    _check(load().moe_head_ce_bwd(_p(x), _p(W), _p(target), _p(loss), _p(lse), _p(dloss), T, d, V, v_piece, _p(dx), _p(dW), _p(ws),
+                                  ws.numel() * ws.element_size(), _stream()), "moe_head_ce_bwd")
+
+
+def moe_head_distill_fwd(x, W, target, ids, teacher, temperature: float, loss, lse, kd, lse_t, ws) -> None:
+    """Cross entropy, and the divergence from a teacher given by K ids and logits per token (-1: no entry)."""
+    T, d, V = _head_args(x, W, target, ids, teacher, (("loss", loss), ("lse", lse), ("kd", kd), ("lse_t", lse_t)))
+    _check(load().moe_head_distill_fwd(_p(x), _p(W), _p(target), _p(ids), _p(teacher), temperature, T, d, V, ids.shape[1], _p(loss),
+                                       _p(lse), _p(kd), _p(lse_t), _p(ws), ws.numel() * ws.element_size(), _stream()),
+           "moe_head_distill_fwd")
+
+
+def moe_head_distill_bwd(x, W, target, ids, teacher, temperature: float, loss, lse, lse_t, dloss, dkd, v_piece: int, dx, dW, ws) -> None:
+    T, d, V = _head_args(x, W, target, ids, teacher,
+                         (("loss", loss), ("lse", lse), ("lse_t", lse_t), ("dloss", dloss), ("dkd", dkd)))
+    _want(dx, BF16, (T, d), "dx")
+    _want(dW, BF16, (V, d), "dW")
+    _check(load().moe_head_distill_bwd(_p(x), _p(W), _p(target), _p(ids), _p(teacher), temperature, _p(loss), _p(lse), _p(lse_t),
+                                       _p(dloss), _p(dkd), T, d, V, ids.shape[1], v_piece, _p(dx), _p(dW), _p(ws),
+                                       ws.numel() * ws.element_size(), _stream()), "moe_head_distill_bwd")
 
 
 def moe_prof_enable(on: bool) -> None:

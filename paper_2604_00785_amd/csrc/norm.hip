@@ -1,0 +1,333 @@
+// Residual addition and root-mean-square norm in front of a layer, its result in bfloat16 or in 8 bits with scales, and its
+// derivative.  With s = x + r (rounded to bf16: what the residual stream holds is what is normalised), q = 1 / sqrt(mean(s^2) + eps):
+//   y = s q w;      8 bits: scale = max |y| / 448 over each group of columns, codes = y / scale in e4m3
+//   c = mean(dy w s) q^2;   dx = dr = dsum + q (dy w - s c);   dw = sum over rows of dy s q
+// All of it is bound by memory: a row is read once, kept in registers between the sum and its use, and written once.
+#include <climits>
+#include <type_traits>
+#include "common.h"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+
+constexpr int NORM_MAX_D = 32768;
+constexpr float E4M3_MAX = 448.f;
+
+struct NormArgs {
+  const moe_bf16 *x, *r;       // r may be null: s = x
+  const float* w;
+  moe_bf16 *sum, *y;           // sum may be null where r is
+  uint8_t* codes;
+  float *scale, *rstd;         // rstd may be null
+  int T, d, lanes;             // lanes: threads that share a scale (d / 8 or more: the whole row)
+  float eps;
+};
+
+__device__ __forceinline__ void unpack8(const u32x4& p, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[2 * i] = bf16lo(p[i]); v[2 * i + 1] = bf16hi(p[i]); }
+}
+__device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
+  return u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+}
+// Reduction over the TPR threads of a row: inside the waves by lane permutations, across them through LDS.
+template <int TPR, typename Op> __device__ __forceinline__ uint32_t row_reduce(uint32_t v, Op op, uint32_t* part) {
+  v = group_reduce<MOE_WAVE>(v, op);
+  if constexpr (TPR > MOE_WAVE) {
+    __syncthreads();                              // what was there before has been read
+    if (threadIdx.x % MOE_WAVE == 0) part[threadIdx.x / MOE_WAVE] = v;
+    __syncthreads();
+    v = part[0];
+#pragma unroll
+    for (int i = 1; i < TPR / MOE_WAVE; ++i) v = op(v, part[i]);
+  }
+  return v;
+}
+template <int TPR> __device__ __forceinline__ float row_sum(float v, uint32_t* part) {
+  return __uint_as_float(row_reduce<TPR>(__float_as_uint(v), [](uint32_t a, uint32_t b) __attribute__((always_inline)) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }, part));
+}
+// Maximum of absolute values by their bits, which order as the values do and put NaN above everything, so that it is passed on.
+__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+// A row by TPR threads, P pieces of 8 columns each: thread i of the row takes pieces i, i + TPR, ..
+template <int TPR, int P, bool CODES>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_kernel(NormArgs a) {
+  constexpr int ROWS = TPR > 256 ? 1 : 256 / TPR;
+  __shared__ uint32_t part[TPR / MOE_WAVE];
+  const int row = blockIdx.x * ROWS + threadIdx.x / TPR, i0 = threadIdx.x % TPR;
+  if (row >= a.T) return;                         // a whole wave, and only where a row is one
+  const int pieces = a.d / 8;
+  const size_t at = static_cast<size_t>(row) * a.d;
+  float s[P][8];
+  u32x4 xp[P], rp[P];
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const int i = i0 + p * TPR;
+    xp[p] = rp[p] = u32x4{0, 0, 0, 0};
+    if (i < pieces) {
+      xp[p] = *reinterpret_cast<const u32x4*>(a.x + at + 8 * i);
+      if (a.r != nullptr) rp[p] = *reinterpret_cast<const u32x4*>(a.r + at + 8 * i);
+    }
+  }
+  float q = 0.f;
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const int i = i0 + p * TPR;
+    u32x4 total = xp[p];
+    if (a.r != nullptr) {
+      float xv[8], rv[8];
+      unpack8(xp[p], xv);
+      unpack8(rp[p], rv);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) xv[c] += rv[c];
+      total = pack8(xv);
+    }
+    unpack8(total, s[p]);
+    if (i < pieces && a.sum != nullptr) *reinterpret_cast<u32x4*>(a.sum + at + 8 * i) = total;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) q = __builtin_fmaf(s[p][c], s[p][c], q);
+  }
+  q = rsqrtf(row_sum<TPR>(q, part) / static_cast<float>(a.d) + a.eps);
+  if (a.rstd != nullptr && i0 == 0) a.rstd[row] = q;
+  uint32_t top = 0;
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const int i = i0 + p * TPR;
+    if (i < pieces) {
+      const f32x4_t w0 = *reinterpret_cast<const f32x4_t*>(a.w + 8 * i), w1 = *reinterpret_cast<const f32x4_t*>(a.w + 8 * i + 4);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) s[p][c] = s[p][c] * q * (c < 4 ? w0[c] : w1[c - 4]);
+      if constexpr (!CODES) *reinterpret_cast<u32x4*>(a.y + at + 8 * i) = pack8(s[p]);
+    }
+    if constexpr (CODES) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) top = umax(top, __float_as_uint(s[p][c]) & 0x7FFFFFFFu);
+    }
+  }
+  if constexpr (CODES) {
+    const bool whole = a.lanes > MOE_WAVE;        // one scale for the row
+    if (whole) top = row_reduce<TPR>(top, umax, part);
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int i = i0 + p * TPR;
+      uint32_t amax = top;
+      if (!whole) {
+        amax = 0;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) amax = umax(amax, __float_as_uint(s[p][c]) & 0x7FFFFFFFu);
+        if (a.lanes >= 2) amax = umax(amax, dpp_u32<0xB1>(amax));
+        if (a.lanes >= 4) amax = umax(amax, dpp_u32<0x4E>(amax));
+        if (a.lanes >= 8) amax = umax(amax, dpp_u32<0x141>(amax));
+        if (a.lanes >= 16) amax = umax(amax, dpp_u32<0x140>(amax));
+        if (a.lanes >= 32) { const auto e = __builtin_amdgcn_permlane16_swap(amax, amax, false, false); amax = umax(e[0], e[1]); }
+        if (a.lanes >= 64) { const auto e = __builtin_amdgcn_permlane32_swap(amax, amax, false, false); amax = umax(e[0], e[1]); }
+      }
+      if (i >= pieces) continue;
+      const float scale = __uint_as_float(amax) / E4M3_MAX;
+      // (a scale below the smallest normal number has no finite inverse: the largest number instead, which leaves zeros zeros)
+      const float inverse = scale != 0.f ? fminf(1.f / scale, 3.4028235e38f) : 0.f;
+      float v[8];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const float z = s[p][c] * inverse;
+        v[c] = z != z ? z : fminf(fmaxf(z, -E4M3_MAX), E4M3_MAX);
+      }
+      u32x2 o;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        int b = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h], v[4 * h + 1], 0, false);
+        b = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2], v[4 * h + 3], b, true);
+        o[h] = static_cast<uint32_t>(b);
+      }
+      *reinterpret_cast<u32x2*>(a.codes + at + 8 * i) = o;
+      const int groups = whole ? 1 : pieces / a.lanes;
+      if (whole ? i == 0 : i % a.lanes == 0) a.scale[static_cast<size_t>(row) * groups + (whole ? 0 : i / a.lanes)] = scale;
+    }
+  }
+}
+
+struct NormBwdArgs {
+  const moe_bf16 *dy, *dsum, *sum;   // dsum may be null
+  const float *w, *rstd;
+  moe_bf16* dx;
+  float* part;                       // [gridDim.x][d]: a workgroup's share of dw
+  int T, d;
+};
+// The workgroup's rows are blockIdx.x * ROWS + .., in steps of the whole grid; a thread keeps its columns' sums of dw over them.
+template <int TPR, int P>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_bwd_kernel(NormBwdArgs a) {
+  constexpr int ROWS = TPR > 256 ? 1 : 256 / TPR;
+  __shared__ uint32_t part[TPR / MOE_WAVE];
+  __shared__ float share[ROWS > 1 ? (ROWS - 1) * P * 8 * TPR : 1];
+  const int first = blockIdx.x * ROWS + threadIdx.x / TPR, i0 = threadIdx.x % TPR;
+  const int pieces = a.d / 8;
+  float dw[P][8], w[P][8];
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const int i = i0 + p * TPR;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) { dw[p][c] = 0.f; w[p][c] = i < pieces ? a.w[8 * i + c] : 0.f; }
+  }
+  for (int row = first; row < a.T; row += gridDim.x * ROWS) {     // (the same for all threads of a row)
+    const size_t at = static_cast<size_t>(row) * a.d;
+    u32x4 gp[P], sp[P], ap[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int i = i0 + p * TPR;
+      gp[p] = sp[p] = ap[p] = u32x4{0, 0, 0, 0};
+      if (i < pieces) {
+        gp[p] = *reinterpret_cast<const u32x4*>(a.dy + at + 8 * i);
+        sp[p] = *reinterpret_cast<const u32x4*>(a.sum + at + 8 * i);
+        if (a.dsum != nullptr) ap[p] = *reinterpret_cast<const u32x4*>(a.dsum + at + 8 * i);
+      }
+    }
+    const float q = a.rstd[row];
+    float dot = 0.f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      float g[8], s[8];
+      unpack8(gp[p], g);
+      unpack8(sp[p], s);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        dot = __builtin_fmaf(g[c] * w[p][c], s[c], dot);
+        dw[p][c] = __builtin_fmaf(g[c], s[c] * q, dw[p][c]);
+      }
+    }
+    const float k = row_sum<TPR>(dot, part) / static_cast<float>(a.d) * q * q;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int i = i0 + p * TPR;
+      float g[8], s[8], v[8];
+      unpack8(gp[p], g);
+      unpack8(sp[p], s);
+      unpack8(ap[p], v);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) v[c] = __builtin_fmaf(q, __builtin_fmaf(-s[c], k, g[c] * w[p][c]), v[c]);
+      if (i < pieces) *reinterpret_cast<u32x4*>(a.dx + at + 8 * i) = pack8(v);
+    }
+  }
+  // the shares of the workgroup's rows meet in LDS, in the order of the rows
+  if constexpr (ROWS > 1) {
+    const int mine = threadIdx.x / TPR;
+    if (mine > 0) {
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) share[((mine - 1) * P * 8 + p * 8 + c) * TPR + i0] = dw[p][c];
+    }
+    __syncthreads();
+    if (mine > 0) return;
+#pragma unroll
+    for (int m = 0; m < ROWS - 1; ++m)
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) dw[p][c] += share[(m * P * 8 + p * 8 + c) * TPR + i0];
+  }
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const int i = i0 + p * TPR;
+    if (i >= pieces) continue;
+    float* o = a.part + static_cast<size_t>(blockIdx.x) * a.d + 8 * i;
+    *reinterpret_cast<f32x4_t*>(o) = f32x4_t{dw[p][0], dw[p][1], dw[p][2], dw[p][3]};
+    *reinterpret_cast<f32x4_t*>(o + 4) = f32x4_t{dw[p][4], dw[p][5], dw[p][6], dw[p][7]};
+  }
+}
+
+// dw[c] = sum of the n shares, in a fixed order: 8 threads take every eighth share of four columns, then meet in LDS.
+__global__ __launch_bounds__(256) void norm_dw_kernel(const float* __restrict__ part, int n, int d, float* __restrict__ dw) {
+  __shared__ f32x4_t s[8][32];
+  const int c = threadIdx.x % 32, k = threadIdx.x / 32, col = (blockIdx.x * 32 + c) * 4;
+  f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+  if (col < d) {
+#pragma unroll 8
+    for (int i = k; i < n; i += 8) v += *reinterpret_cast<const f32x4_t*>(part + static_cast<size_t>(i) * d + col);
+  }
+  s[k][c] = v;
+  __syncthreads();
+  if (k == 0 && col < d) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) v += s[i][c];
+    *reinterpret_cast<f32x4_t*>(dw + col) = v;
+  }
+}
+
+bool bad_norm_dims(int T, int d) { return T <= 0 || d <= 0 || d % 8 != 0 || d > NORM_MAX_D; }
+int rows_of_group(int d) { return d <= 2048 ? 4 : 1; }
+// Threads of a row: one wave up to 2048 columns (no barrier in the row's sums), 256 up to 8192, else 1024.
+template <typename F> void with_shape(int d, F&& f) {
+  const int pieces = d / 8;
+#define MOE_NORM(TPR) \
+  switch ((pieces + TPR - 1) / TPR) { \
+    case 1: f(std::integral_constant<int, TPR>{}, std::integral_constant<int, 1>{}); break; \
+    case 2: f(std::integral_constant<int, TPR>{}, std::integral_constant<int, 2>{}); break; \
+    case 3: f(std::integral_constant<int, TPR>{}, std::integral_constant<int, 3>{}); break; \
+    default: f(std::integral_constant<int, TPR>{}, std::integral_constant<int, 4>{}); break; \
+  }
+  if (pieces <= 256) { MOE_NORM(64) } else if (pieces <= 1024) { MOE_NORM(256) } else { MOE_NORM(1024) }
+#undef MOE_NORM
+}
+// Workgroups of the backward pass, each with a share of dw: two per compute unit of a whole chip, or as many as there are rows for.
+int norm_bwd_groups(int T, int d) {
+  const int rows = rows_of_group(d), groups = (T - 1) / rows + 1;
+  return groups < 512 ? groups : 512;
+}
+
+template <bool CODES> int launch_norm(const NormArgs& a, const char* name, hipStream_t s) {
+  const dim3 grid((a.T - 1) / rows_of_group(a.d) + 1);
+  with_shape(a.d, [&](auto tpr, auto p) {
+    constexpr int TPR = decltype(tpr)::value, P = decltype(p)::value;
+    MOE_LAUNCH(name, (add_rms_norm_kernel<TPR, P, CODES>), grid, dim3(TPR > 256 ? TPR : 256), 0, s, a);
+  });
+  return moe_check_launch();
+}
+
+}  // namespace
+
+extern "C" int moe_add_rms_norm(const moe_bf16* x, const moe_bf16* r, const float* w, int T, int d, float eps, moe_bf16* sum,
+                                moe_bf16* y, float* rstd, void* stream) {
+  if (!x || !w || !y || (r && !sum) || bad_norm_dims(T, d) || !(eps >= 0.f)) return MOE_ERR_INVALID;
+  const void* ptrs[] = {x, r, w, sum, y, rstd};
+  for (const void* p : ptrs) if (!moe_aligned16(p)) return MOE_ERR_INVALID;
+  const NormArgs a{x, r, w, sum, y, nullptr, nullptr, rstd, T, d, 0, eps};
+  return launch_norm<false>(a, "add_rms_norm", static_cast<hipStream_t>(stream));
+}
+
+extern "C" int moe_add_rms_norm_8bit(const moe_bf16* x, const moe_bf16* r, const float* w, int T, int d, float eps, int group,
+                                     moe_bf16* sum, uint8_t* codes, float* scale, float* rstd, void* stream) {
+  if (!x || !w || !codes || !scale || (r && !sum) || bad_norm_dims(T, d) || !(eps >= 0.f)) return MOE_ERR_INVALID;
+  // a scale's columns are whole pieces of 8, a power of two of them up to a wave, or the row
+  if (group != 0 && (group < 8 || group > 512 || (group & (group - 1)) != 0 || d % group != 0)) return MOE_ERR_INVALID;
+  const void* ptrs[] = {x, r, w, sum, codes, scale, rstd};
+  for (const void* p : ptrs) if (!moe_aligned16(p)) return MOE_ERR_INVALID;
+  const NormArgs a{x, r, w, sum, nullptr, codes, scale, rstd, T, d, group == 0 ? INT_MAX : group / 8, eps};
+  return launch_norm<true>(a, "add_rms_norm_8bit", static_cast<hipStream_t>(stream));
+}
+
+extern "C" size_t moe_add_rms_norm_bwd_workspace_bytes(int T, int d) {
+  if (bad_norm_dims(T, d)) return 0;
+  return static_cast<size_t>(norm_bwd_groups(T, d)) * d * sizeof(float);
+}
+
+extern "C" int moe_add_rms_norm_bwd(const moe_bf16* dy, const moe_bf16* dsum, const moe_bf16* sum, const float* w, const float* rstd,
+                                    int T, int d, moe_bf16* dx, float* dw, void* ws, size_t ws_bytes, void* stream) {
+  if (!dy || !sum || !w || !rstd || !dx || !dw || !ws || bad_norm_dims(T, d)) return MOE_ERR_INVALID;
+  const void* ptrs[] = {dy, dsum, sum, w, rstd, dx, dw, ws};
+  for (const void* p : ptrs) if (!moe_aligned16(p)) return MOE_ERR_INVALID;
+  if (ws_bytes < moe_add_rms_norm_bwd_workspace_bytes(T, d)) return MOE_ERR_WORKSPACE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int groups = norm_bwd_groups(T, d);
+  const NormBwdArgs a{dy, dsum, sum, w, rstd, dx, static_cast<float*>(ws), T, d};
+  with_shape(d, [&](auto tpr, auto p) {
+    constexpr int TPR = decltype(tpr)::value, P = decltype(p)::value;
+    MOE_LAUNCH("add_rms_norm_bwd", (add_rms_norm_bwd_kernel<TPR, P>), dim3(groups), dim3(TPR > 256 ? TPR : 256), 0, s, a);
+  });
+  if (moe_check_launch() != MOE_OK) return MOE_ERR_LAUNCH;
+  MOE_LAUNCH("norm_dw", norm_dw_kernel, dim3((d / 4 + 31) / 32), dim3(256), 0, s, static_cast<const float*>(ws), groups, d, dw);
+  return moe_check_launch();
+}
