@@ -140,20 +140,22 @@ struct GemmArgs {
   int M;
 };
 
-// What the epilogues of the head's products take beside GemmArgs.  Items are the logits that a later kernel needs by themselves: of the
-// target and of the teacher's entries.  They are listed by blocks of 16 rows and, inside a block, by strips of 64 columns.
+// What the epilogues of the head's products take beside GemmArgs.  Items are the logits that count by themselves: of the target and of the
+// teacher's entries.  They are listed by blocks of 16 rows and, inside a block, by strips of 64 columns.
 struct HeadItem { uint32_t at, slot; };   // at: row in the block | column << 4
 struct HeadArgs {
   float* part;                // HEAD_STATS: planes [strips][rows_cap] of maximum, sum and (two) sum at the temperature over HALF columns, without the items
   const f32x4_t* row;         // HEAD_DZ: per row log2(e) lse, factor, and the same at the temperature
   const int32_t* list_start;  // [row block][list_ld]: first item of each strip
   const HeadItem* items;      // [row block][16 slots]
-  float* z_item;              // [row][slots]
-  float c1, c2;               // log2(e), the same over the temperature
+  const f32x4_t* terms;       // HEAD_DZ: as items; the gradient there is t0 + t1 (exp(z / temperature - t2) - 1) + t3 exp(z - lse)
+  float* item;                // [row][slots]: HEAD_STATS: the logit; HEAD_DZ: what the gradient loses when it is rounded
+  float c1, c2, over_tau;     // log2(e), the same over the temperature, 1 / temperature
   int two;                    // both sums, both terms
   int strips, rows_cap, list_ld, slots;
   int col0;                   // vocabulary column of the product's first
   int add;                    // HEAD_DX: onto what is there
+  int lo;                     // HEAD_DZ: what rounding loses is stored too, in as many rows behind the others
 };
 
 // 512 bytes of zeros: what the reduction rows past an expert's end read in the weight-gradient products.
@@ -530,7 +532,8 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
       b_step = 0;
       row_tok = a.row_token + k_lo;
     } else {
-      bbase = reinterpret_cast<const char*>(a.B0 + static_cast<size_t>(k_lo) * a.N + n0);
+      const uint16_t* B = MODE == HEAD_DW && a.row_token[0] != 0 ? a.B1 : a.B0;
+      bbase = reinterpret_cast<const char*>(B + static_cast<size_t>(k_lo) * a.N + n0);
       b_step = static_cast<size_t>(BK) * a.N * 2;
     }
 #pragma unroll
@@ -548,7 +551,9 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
   } else {
     nk = a.K / BK;
     nk_phase = nk;
-    abase = reinterpret_cast<const char*>(a.A0 + static_cast<size_t>(m0) * a.K);
+    // (logits: the tokens' rows side by side, or as they are where all have a loss)
+    const uint16_t* A = is_logits(MODE) && a.row_token[0] != 0 ? a.A1 : a.A0;
+    abase = reinterpret_cast<const char*>(A + static_cast<size_t>(m0) * a.K);
     a_step = BK * 2;
     bool gathered = false;
     if constexpr (MODE == GATE_UP) gathered = a.row_token != nullptr;
@@ -1390,28 +1395,23 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
       auto z_piece = [&](int row, int piece) __attribute__((always_inline)) {
         return reinterpret_cast<float*>(stage + row * (HALF * 4) + ((piece ^ row) << 4));
       };
+      // f(there, row, its place in the lists, its logit's place) for the part's items, 64 at a time
       auto over_items = [&](int part, int lo, int hi, auto&& f) __attribute__((always_inline)) {
-        const HeadItem* it = he->items + static_cast<size_t>((grow0 >> 4) + part) * 16 * he->slots;
-        for (int n = lo + lane; n < hi; n += 64) {
-          const HeadItem x = it[n];
+        const size_t first = static_cast<size_t>((grow0 >> 4) + part) * 16 * he->slots;
+        for (int n0 = lo; n0 < hi; n0 += 64) {
+          const int n = n0 + lane < hi ? n0 + lane : hi - 1;
+          const HeadItem x = he->items[first + n];
           const int row = x.at & 15, c = static_cast<int>(x.at >> 4) - he->col0 - gcol0;
-          f(row, x.slot, z_piece(row, c >> 2) + (c & 3));
+          f(n0 + lane < hi, row, static_cast<size_t>(grow0 + part * 16 + row) * he->slots + x.slot, first + n, z_piece(row, c >> 2) + (c & 3));
         }
       };
-      auto pick = [&](int part, auto& v) __attribute__((always_inline)) {
-        const int lo = wave_lane(item_lo, part), hi = wave_lane(item_hi, part);
-        if (hi <= lo) return;
+      auto put_logits = [&](const auto& v) __attribute__((always_inline)) {
         static_for<NB>([&](auto j) { *reinterpret_cast<f32x4_t*>(z_piece(l16, 4 * decltype(j)::value + lq)) = v[decltype(j)::value]; });
         __builtin_amdgcn_wave_barrier();
-        over_items(part, lo, hi, [&](int row, uint32_t slot, float* z) __attribute__((always_inline)) {
-          he->z_item[static_cast<size_t>(grow0 + part * 16 + row) * he->slots + slot] = *z;
-        });
-        if constexpr (MODE == HEAD_STATS) {
-          __builtin_amdgcn_wave_barrier();
-          over_items(part, lo, hi, [&](int, uint32_t, float* z) __attribute__((always_inline)) { *z = NONE; });
-          __builtin_amdgcn_wave_barrier();
-          static_for<NB>([&](auto j) { v[decltype(j)::value] = *reinterpret_cast<const f32x4_t*>(z_piece(l16, 4 * decltype(j)::value + lq)); });
-        }
+      };
+      auto get_logits = [&](auto& v) __attribute__((always_inline)) {
+        __builtin_amdgcn_wave_barrier();
+        static_for<NB>([&](auto j) { v[decltype(j)::value] = *reinterpret_cast<const f32x4_t*>(z_piece(l16, 4 * decltype(j)::value + lq)); });
         __builtin_amdgcn_wave_barrier();
       };
       auto mask = [&](auto& v, float with) __attribute__((always_inline)) {
@@ -1430,7 +1430,14 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
           if (i * 16 >= rows || left <= 0) return;
           f32x4_t v[NB];
           static_for<NB>([&](auto j) { v[decltype(j)::value] = accq(i_tag, j); });
-          pick(i, v);
+          const int lo = wave_lane(item_lo, i), hi = wave_lane(item_hi, i);
+          if (hi > lo) {
+            put_logits(v);
+            over_items(i, lo, hi, [&](bool there, int, size_t at, size_t, float* z) __attribute__((always_inline)) { if (there) he->item[at] = *z; });
+            __builtin_amdgcn_wave_barrier();
+            over_items(i, lo, hi, [&](bool, int, size_t, size_t, float* z) __attribute__((always_inline)) { *z = NONE; });
+            get_logits(v);
+          }
           mask(v, NONE);
           float m = NONE;
 #pragma unroll
@@ -1457,22 +1464,44 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
       } else {
         const int ld = ae->M;
         const Rsrc oo = rows_of(ae->O0, ld * 2);
+        const bool lows = he->lo != 0;
+        const Rsrc ol = rows_of(ae->O0 + (lows ? static_cast<size_t>(ae->offsets[1]) * ld : 0), ld * 2);
         constexpr int PASSES = 16 * RP / 64;
         u32x4 v4[PASSES];
         const int gc = gcol0 + lane % RP * 8;
         const int off = gc < ld ? (lane / RP * ld + gc) * 2 : PAST;
-        auto store_part = [&](int part) __attribute__((always_inline)) {
+        auto store_part = [&](int part, const f32x4_t (&v)[NB], Rsrc out) __attribute__((always_inline)) {
+          static_for<NB>([&](auto j) { put_quad(l16, decltype(j)::value, v[decltype(j)::value]); });
+          __builtin_amdgcn_wave_barrier();
+          read_staged(v4, stage, IC<RB>{}, IC<PASSES>{}, IC<0>{}, IC<RP>{});
+          __builtin_amdgcn_wave_barrier();
 #pragma unroll
           for (int k = 0; k < PASSES; ++k)
-            __builtin_amdgcn_raw_buffer_store_b128(v4[k], oo, off + (part * 16 + k * (64 / RP)) * ld * 2, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(v4[k], out, off + (part * 16 + k * (64 / RP)) * ld * 2, 0, 0);
         };
+        const auto rounded = [](float x) __attribute__((always_inline)) { return bf16_to_f32(f32_to_bf16(x)); };
         static_for<NB>([&](auto i_tag) {
           constexpr int i = decltype(i_tag)::value;
           if (i * 16 >= rows) return;
-          f32x4_t v[NB];
-          static_for<NB>([&](auto j) { v[decltype(j)::value] = accq(i_tag, j); });
-          pick(i, v);
           const f32x4_t p = rowp[i];
+          f32x4_t v[NB], special[NB];
+          static_for<NB>([&](auto j) { v[decltype(j)::value] = accq(i_tag, j); });
+          const int lo = wave_lane(item_lo, i), hi = wave_lane(item_hi, i);
+          if (hi > lo) {
+            // the gradient at the items replaces their logits; a lane knows it by its bits, which are made to differ from the logit's
+            put_logits(v);
+            over_items(i, lo, hi, [&](bool there, int row, size_t at, size_t n, float* zp) __attribute__((always_inline)) {
+              const f32x4_t t = he->terms[n];
+              const float z = *zp, lse = __shfl(p[0], row);
+              float g = t[0];
+              if (t[1] != 0.f) g = __builtin_fmaf(t[1], expm1f(__builtin_fmaf(z, he->over_tau, -t[2])), g);
+              if (t[3] != 0.f) g = __builtin_fmaf(t[3], __builtin_amdgcn_exp2f(__builtin_fmaf(z, c1, -lse)), g);
+              if (!there) return;
+              he->item[at] = g - rounded(g);
+              *zp = __uint_as_float(__float_as_uint(g) ^ (__float_as_uint(g) == __float_as_uint(z) ? 1u : 0u));
+            });
+            get_logits(special);
+          }
           static_for<NB>([&](auto j_tag) {
             constexpr int j = decltype(j_tag)::value;
 #pragma unroll
@@ -1480,15 +1509,19 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
               const float z = v[j][c];
               float g = __builtin_amdgcn_exp2f(__builtin_fmaf(z, c1, -p[0])) * p[1];
               if (two) g = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(z, c2, -p[2])), p[3], g);
+              if (hi > lo) g = __float_as_uint(special[j][c]) != __float_as_uint(z) ? special[j][c] : g;
               v[j][c] = g;
             }
           });
           mask(v, 0.f);
-          static_for<NB>([&](auto j) { put_quad(l16, decltype(j)::value, v[decltype(j)::value]); });
-          __builtin_amdgcn_wave_barrier();
-          read_staged(v4, stage, IC<RB>{}, IC<PASSES>{}, IC<0>{}, IC<RP>{});
-          __builtin_amdgcn_wave_barrier();
-          store_part(i);
+          store_part(i, v, oo);
+          if (lows) {
+            static_for<NB>([&](auto j) {
+#pragma unroll
+              for (int c = 0; c < 4; ++c) v[decltype(j)::value][c] -= rounded(v[decltype(j)::value][c]);
+            });
+            store_part(i, v, ol);
+          }
         });
       }
     } else if constexpr (MODE == HEAD_DX) {

@@ -16,7 +16,8 @@ namespace {
 
 constexpr int HEAD_MAX_V = 1 << 20, HEAD_MAX_K = 1024;
 constexpr int HEAD_CUS = 256;                       // what the workspace's size is laid out for
-constexpr int SELF_MASK_TOKENS = 4096;
+constexpr int SELF_MASK_TOKENS = 4096, SELF_MASK_LOADS = 8192;   // what a workgroup of head_prep finds out by itself
+constexpr int LOW_TOKENS = 128;                     // up to these, dW takes what rounding dz loses as well: its reduction is padded to 64 rows anyway, and a large product costs no more than writing dW
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct Teacher { const int32_t* ids; const float* logits; float temperature; int K; };
@@ -24,57 +25,76 @@ struct Teacher { const int32_t* ids; const float* logits; float temperature; int
 __device__ __forceinline__ bool entry_there(int id, float l, int V) { return id >= 0 && id < V && l > -__builtin_inff(); }
 __device__ __forceinline__ bool target_there(int y, int V) { return y >= 0 && y < V; }
 
-// Which tokens have a loss, a bit each: a target, or (K > 0) an entry.  A wave takes 64 tokens.
+// Which tokens have a loss, a bit each: a target, or (K > 0) an entry.  A workgroup takes 64 tokens.
 __global__ __launch_bounds__(256) void head_mask_kernel(const int32_t* __restrict__ target, Teacher t, int T, int V, uint64_t* __restrict__ mask) {
-  __shared__ int some[4][MOE_WAVE];
-  const int lane = threadIdx.x % MOE_WAVE, wave = threadIdx.x / MOE_WAVE;
-  const int word = blockIdx.x * 4 + wave, t0 = word * 64;
-  if (t0 >= T) return;
-  some[wave][lane] = t0 + lane < T && target_there(target[t0 + lane], V);
-  __builtin_amdgcn_wave_barrier();
-  const size_t n = static_cast<size_t>(T - t0 < 64 ? T - t0 : 64) * t.K, at = static_cast<size_t>(t0) * t.K;
-#pragma unroll 4
-  for (size_t i = lane; i < n; i += MOE_WAVE)
-    if (entry_there(t.ids[at + i], t.logits[at + i], V)) some[wave][static_cast<int>(i) / t.K] = 1;
-  __builtin_amdgcn_wave_barrier();
-  const uint64_t bits = __ballot(some[wave][lane] != 0);
-  if (lane == 0) mask[word] = bits;
+  __shared__ int some[MOE_WAVE];
+  const int tid = threadIdx.x, t0 = blockIdx.x * 64;
+  if (tid < 64) some[tid] = t0 + tid < T && target_there(target[t0 + tid], V);
+  __syncthreads();
+  const int n = (T - t0 < 64 ? T - t0 : 64) * t.K;
+  const size_t at = static_cast<size_t>(t0) * t.K;
+#pragma unroll 8
+  for (int i = tid; i < n; i += 256)
+    if (entry_there(t.ids[at + i], t.logits[at + i], V)) some[i / t.K] = 1;
+  __syncthreads();
+  if (tid < 64) {
+    const uint64_t bits = __ballot(some[tid] != 0);
+    if (tid == 0) mask[blockIdx.x] = bits;
+  }
 }
+
+// What head_prep leaves for the kernels behind it, as integers: rows of the products from 0 to LIVE; those of dW, with the low parts, from 0
+// to DW_ROWS; whether x itself holds the rows.
+enum { ROWS = 0, LIVE = 1, DW_ROWS = 3, DIRECT = 4, CONTROL_INTS = 5 };
 
 struct HeadPrepArgs {
   const moe_bf16* x;
   const int32_t* target;
   Teacher t;
-  const uint64_t* mask;            // null: up to SELF_MASK_TOKENS tokens, and no teacher
+  const uint64_t* mask;            // null: found here
   int T, d, V, strips;             // strips: of 64 columns
-  int32_t *offsets, *row_token, *token_row;
+  int low;                         // rows of x twice
+  int32_t *control, *row_token, *token_row;
   moe_bf16* xc;
   int32_t* list_start;
   HeadItem* items;
+  f32x4_t* terms;                  // backward, as is what follows
   int32_t* target_slot;
   float *loss, *lse, *kd, *lse_t;  // forward: zeros for tokens without a loss
-  const float *in_loss, *in_lse, *in_lse_t, *dloss, *dkd;   // backward: the rows' factors
+  const float *in_loss, *in_lse, *in_lse_t, *dloss, *dkd;
   f32x4_t* row;
 };
 
-// Workgroup b: rows 16 b to 16 b + 15 of those with a loss, in the order of their tokens; and tokens 16 b to 16 b + 15, if they have none.
+// Workgroup (b, 0): rows 16 b to 16 b + 15 of those with a loss, in the order of their tokens; and tokens 16 b to 16 b + 15, if they have none.
+// Workgroups (b, 1 ..) help with the rows of x.  Sixteen threads share a row's entries.
 __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   extern __shared__ int count[];                     // [strips + 1]
   __shared__ uint64_t own[SELF_MASK_TOKENS / 64];
-  __shared__ int wave_sum[4], s_token[16], s_target[16], s_slot[16], s_taught[16];
+  __shared__ int wave_sum[4], s_token[16], s_target[16], s_slot[16];
   const int tid = threadIdx.x, lane = tid % MOE_WAVE, wave = tid / MOE_WAVE;
   const int words = (a.T + 63) / 64, per = (words + 255) / 256, K = a.t.K, V = a.V, slots = K + 1;
+  const bool lists = blockIdx.y == 0;
   const uint64_t* mask = a.mask;
   if (mask == nullptr) {
+#pragma unroll 4
     for (int w = wave; w < words; w += 4) {
       const int t = w * 64 + lane;
       const uint64_t bits = __ballot(t < a.T && target_there(a.target[t], V));
       if (lane == 0) own[w] = bits;
     }
+    if (K > 0) {
+      __syncthreads();
+#pragma unroll 8
+      for (int i = tid; i < a.T * K; i += 256)
+        if (entry_there(a.t.ids[i], a.t.logits[i], V)) {
+          const int t = i / K;
+          atomicOr(reinterpret_cast<unsigned*>(own) + (t >> 5), 1u << (t & 31));
+        }
+    }
     mask = own;
   }
-  if (tid < 16) { s_token[tid] = -1; s_slot[tid] = K; s_taught[tid] = 0; }
-  for (int i = tid; i <= a.strips; i += 256) count[i] = 0;
+  if (tid < 16) { s_token[tid] = -1; s_target[tid] = -1; s_slot[tid] = K; }
+  if (lists) for (int i = tid; i <= a.strips; i += 256) count[i] = 0;
   __syncthreads();
   // rank of each thread's first token among those with a loss
   const int w0 = tid * per < words ? tid * per : words, w1 = w0 + per < words ? w0 + per : words;
@@ -88,8 +108,13 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   for (int w = 0; w < 4; ++w) { rank += w < wave ? wave_sum[w] : 0; live += wave_sum[w]; }
   rank -= mine;
   const int first = blockIdx.x * 16;
-  if (blockIdx.x == 0 && tid == 0) { a.offsets[0] = 0; a.offsets[1] = live; }
-  if (tid < 16 && first + tid < a.T) {
+  const bool direct = live == a.T && !a.low;
+  if (lists && blockIdx.x == 0 && tid == 0) {
+    a.control[ROWS] = 0; a.control[LIVE] = live;
+    a.control[DW_ROWS - 1] = 0; a.control[DW_ROWS] = a.low ? 2 * live : live;
+    a.control[DIRECT] = direct;
+  }
+  if (lists && tid < 16 && first + tid < a.T) {
     const int t = first + tid;
     if ((mask[t >> 6] >> (t & 63) & 1) == 0) {
       a.token_row[t] = -1;
@@ -100,7 +125,7 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
       }
     }
   }
-  if (first >= live) return;
+  if (first >= live || (direct && !lists)) return;
   for (int w = w0; w < w1 && rank < first + 16; ++w) {
     uint64_t bits = mask[w];
     const int n = __builtin_popcountll(bits);
@@ -109,35 +134,55 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
       if (rank < first || rank >= first + 16) continue;
       const int t = w * 64 + __builtin_ctzll(bits);
       s_token[rank - first] = t;
-      s_target[rank - first] = a.target[t];
-      a.row_token[rank] = t;
-      a.token_row[t] = rank;
+      if (lists) {
+        s_target[rank - first] = a.target[t];
+        a.row_token[rank] = t;
+        a.token_row[t] = rank;
+      }
     }
   }
   __syncthreads();
-  const int n = live - first < 16 ? live - first : 16, pieces = a.d / 8;
-  for (int i = tid; i < n * pieces; i += 256) {
+  const int n = live - first < 16 ? live - first : 16;
+  if (!direct) {
     typedef __attribute__((ext_vector_type(4))) uint32_t u4;
-    const int r = i / pieces, c = (i - r * pieces) * 8;
-    *reinterpret_cast<u4*>(a.xc + static_cast<size_t>(first + r) * a.d + c) = *reinterpret_cast<const u4*>(a.x + static_cast<size_t>(s_token[r]) * a.d + c);
+    const int pieces = a.d / 8, all = n * pieces, step = 256 * gridDim.y;
+    for (int i0 = blockIdx.y * 256 + tid; i0 < all; i0 += 8 * step) {
+      u4 v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int i = i0 + k * step, j = i < all ? i : i0, r = j / pieces;
+        v[k] = *reinterpret_cast<const u4*>(a.x + static_cast<size_t>(s_token[r]) * a.d + (j - r * pieces) * 8);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int i = i0 + k * step;
+        if (i >= all) break;
+        moe_bf16* to = a.xc + static_cast<size_t>(first) * a.d + static_cast<size_t>(i) * 8;
+        *reinterpret_cast<u4*>(to) = v[k];
+        if (a.low) *reinterpret_cast<u4*>(to + static_cast<size_t>(live) * a.d) = v[k];
+      }
+    }
   }
-  auto entry = [&](int i, int& r, int& j, int& id) __attribute__((always_inline)) {
-    r = i / K;
-    j = i - r * K;
-    const size_t at = static_cast<size_t>(s_token[r]) * K + j;
-    id = a.t.ids[at];
-    return entry_there(id, a.t.logits[at], V);
-  };
-  for (int i = tid; i < n * K; i += 256) {
-    int r, j, id;
-    if (!entry(i, r, j, id)) continue;
-    s_taught[r] = 1;
-    if (id == s_target[r]) atomicMin(&s_slot[r], j);     // the target's logit is that of an entry
+  if (!lists) return;
+  const int r = tid >> 4, l16 = tid & 15, y = s_target[r], t = s_token[r];
+  const size_t at = static_cast<size_t>(t < 0 ? 0 : t) * K;
+  const int mine_K = r < n ? K : 0;
+  const float tau = a.t.temperature;
+  float top = -__builtin_inff();
+#pragma unroll 4
+  for (int j = l16; j < mine_K; j += 16) {
+    const int id = a.t.ids[at + j];
+    const float l = a.t.logits[at + j];
+    if (!entry_there(id, l, V)) continue;
+    top = fmaxf(top, l / tau);
+    if (id == y) atomicMin(&s_slot[r], j);               // the target's logit is that of an entry
     atomicAdd(&count[id >> 6], 1);
   }
+  top = group_max<16>(top);
+  const bool taught = top > -__builtin_inff(), has = r < n && target_there(y, V);
   __syncthreads();
-  const bool own_target = tid < n && s_slot[tid] == K && target_there(s_target[tid], V);
-  if (own_target) atomicAdd(&count[s_target[tid] >> 6], 1);
+  const bool own_target = l16 == 0 && has && s_slot[r] == K;
+  if (own_target) atomicAdd(&count[y >> 6], 1);
   __syncthreads();
   // exclusive sums over the strips
   const int chunk = (a.strips + 255) / 256, c0 = tid * chunk, c1 = c0 + chunk < a.strips ? c0 + chunk : a.strips;
@@ -158,61 +203,72 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   }
   if (tid == 255) start[a.strips] = before;
   __syncthreads();
-  HeadItem* items = a.items + static_cast<size_t>(blockIdx.x) * 16 * slots;
-  auto put = [&](int r, int col, int slot) __attribute__((always_inline)) {   // (the order inside a strip does not matter)
-    items[atomicAdd(&count[col >> 6], 1)] = HeadItem{static_cast<uint32_t>(r) | static_cast<uint32_t>(col) << 4, static_cast<uint32_t>(slot)};
+  const size_t list = static_cast<size_t>(blockIdx.x) * 16 * slots;
+  auto put = [&](int col, int slot, const f32x4_t& term) __attribute__((always_inline)) {   // (the order inside a strip does not matter)
+    const int i = atomicAdd(&count[col >> 6], 1);
+    a.items[list + i] = HeadItem{static_cast<uint32_t>(r) | static_cast<uint32_t>(col) << 4, static_cast<uint32_t>(slot)};
+    if (a.terms != nullptr) a.terms[list + i] = term;
   };
-  for (int i = tid; i < n * K; i += 256) {
-    int r, j, id;
-    if (entry(i, r, j, id)) put(r, id, j);
-  }
-  if (own_target) put(tid, s_target[tid], K);
-  if (tid < n) {
-    const int t = s_token[tid];
-    const bool has = target_there(s_target[tid], V), taught = s_taught[tid] != 0;
-    a.target_slot[first + tid] = has ? s_slot[tid] : -1;
-    if (a.row != nullptr) {
-      const float none = __builtin_inff(), tau = a.t.temperature;
-      f32x4_t p = {none, 0.f, none, 0.f};
-      if (has) { p[0] = a.in_lse[t] * LOG2E; p[1] = a.dloss[t]; }
-      if (taught) {
-        const float l = a.in_lse_t[t] * LOG2E, g = a.dkd[t] / tau;
-        if (tau != 1.f) { p[2] = l; p[3] = g; }
-        else { if (!has) p[0] = l; p[1] += g; }                       // one sum serves both
+  // The gradient at the target and at the entries, where it is no plain softmax: p - 1 = exp(-loss) - 1 at the target; p - q = q (exp(log p - log q) - 1)
+  // at an entry.  What does not depend on the logit is put down here.
+  float lq = 0.f, lt = 0.f, gk = 0.f, gl = 0.f, at_target = 0.f;
+  if (a.terms != nullptr && r < n) {
+    if (taught) {
+      float e = 0.f;
+      for (int j = l16; j < mine_K; j += 16) {
+        const float l = a.t.logits[at + j];
+        if (entry_there(a.t.ids[at + j], l, V)) e += expf(l / tau - top);
       }
-      a.row[first + tid] = p;
+      lq = top + logf(group_sum<16>(e));
+      lt = a.in_lse_t[t];
+      gk = a.dkd[t] / tau;
+    }
+    if (has) {
+      gl = a.dloss[t];
+      at_target = expm1f(-a.in_loss[t]) * gl;
+    }
+    if (l16 == 0) {
+      const float none = __builtin_inff();
+      f32x4_t p = {none, 0.f, none, 0.f};
+      if (has) { p[0] = a.in_lse[t] * LOG2E; p[1] = gl; }
+      if (taught) {
+        if (tau != 1.f) { p[2] = lt * LOG2E; p[3] = gk; }
+        else { if (!has) p[0] = lt * LOG2E; p[1] += gk; }             // one exponential serves both
+      }
+      a.row[first + r] = p;
     }
   }
+  for (int j = l16; j < mine_K; j += 16) {
+    const int id = a.t.ids[at + j];
+    const float l = a.t.logits[at + j];
+    if (!entry_there(id, l, V)) continue;
+    const float log_q = l / tau - lq;
+    put(id, j, a.terms == nullptr ? f32x4_t{} : f32x4_t{id == y ? at_target : 0.f, expf(log_q) * gk, lt + log_q, id == y ? 0.f : gl});
+  }
+  if (own_target) put(y, K, f32x4_t{at_target + gk, gk, lt, 0.f});
+  if (l16 == 0 && r < n) a.target_slot[first + r] = has ? s_slot[r] : -1;
 }
 
 __device__ __forceinline__ float wave_sum_of(float v) { return group_sum<MOE_WAVE>(v); }
 __device__ __forceinline__ float wave_max_of(float v) { return group_max<MOE_WAVE>(v); }
 
-// log sum exp of a token's teacher logits over the temperature (all lanes of a wave)
-__device__ __forceinline__ float teacher_lse(const Teacher& t, size_t at, int V, int lane) {
-  float top = -__builtin_inff();
-  for (int j = lane; j < t.K; j += MOE_WAVE) if (entry_there(t.ids[at + j], t.logits[at + j], V)) top = fmaxf(top, t.logits[at + j] / t.temperature);
-  top = wave_max_of(top);
-  float sum = 0.f;
-  for (int j = lane; j < t.K; j += MOE_WAVE)
-    if (entry_there(t.ids[at + j], t.logits[at + j], V)) sum += expf(t.logits[at + j] / t.temperature - top);
-  return top + logf(wave_sum_of(sum));
-}
-
 struct HeadJoinArgs {
   const float* part;
-  const int32_t *offsets, *row_token, *target_slot;
+  const int32_t *control, *row_token, *target_slot;
   const float* z_item;
   Teacher t;
   int strips, rows_cap, V;
   float *loss, *lse, *kd, *lse_t;
   float c1, c2;
 };
-// 16 rows: their strips' maxima and sums joined, then the losses.  Sums of exponentials have the scale 2^E of gemm_tile.h.
-__global__ __launch_bounds__(256) void head_join_kernel(HeadJoinArgs a) {
-  __shared__ float part[16][16][4], joined[16][2];
-  const int tid = threadIdx.x, lane = tid % MOE_WAVE, wave = tid / MOE_WAVE;
-  const int first = blockIdx.x * 16, live = a.offsets[1], K = a.t.K;
+// 16 rows: their strips' maxima and sums joined by 64 threads each, then the losses, a wave for each row with its entries in registers (EPL a
+// lane).  Sums of exponentials have the scale 2^E of gemm_tile.h.
+constexpr int JOIN_THREADS = 1024, JOIN_GROUPS = JOIN_THREADS / 16;
+template <int EPL>
+__global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a) {
+  __shared__ float part[4][JOIN_GROUPS][16];
+  const int tid = threadIdx.x, lane = tid % MOE_WAVE;
+  const int first = blockIdx.x * 16, live = a.control[LIVE], K = a.t.K;
   const bool two = K > 0 && a.t.temperature != 1.f;
   if (first >= live) return;
   constexpr float NONE = -__builtin_inff(), LOW = -3.0e38f;
@@ -221,150 +277,147 @@ __global__ __launch_bounds__(256) void head_join_kernel(HeadJoinArgs a) {
     const size_t plane = static_cast<size_t>(a.strips) * a.rows_cap;
     float e1 = LOW, s1 = 0.f, e2 = LOW, s2 = 0.f;
 #pragma unroll 4
-    for (int s = g; s < a.strips; s += 16) {
+    for (int s = g; s < a.strips; s += JOIN_GROUPS) {
       const float* p = a.part + static_cast<size_t>(s) * a.rows_cap + row;
       const float m = p[0], v1 = p[plane], v2 = two ? p[2 * plane] : 0.f;
       const float f1 = m > NONE ? ceilf(m * a.c1) : LOW, f2 = m > NONE ? ceilf(m * a.c2) : LOW;
       const float n1 = fmaxf(e1, f1), n2 = fmaxf(e2, f2);
-      s1 = s1 * exp2f(e1 - n1) + v1 * exp2f(f1 - n1);
-      s2 = s2 * exp2f(e2 - n2) + v2 * exp2f(f2 - n2);
+      s1 = s1 * __builtin_amdgcn_exp2f(e1 - n1) + v1 * __builtin_amdgcn_exp2f(f1 - n1);
+      s2 = s2 * __builtin_amdgcn_exp2f(e2 - n2) + v2 * __builtin_amdgcn_exp2f(f2 - n2);
       e1 = n1; e2 = n2;
     }
-    part[r][g][0] = e1; part[r][g][1] = s1; part[r][g][2] = e2; part[r][g][3] = s2;
+    part[0][g][r] = e1; part[1][g][r] = s1; part[2][g][r] = e2; part[3][g][r] = s2;
   }
   __syncthreads();
-  if (tid < 32) {
-    const int r = tid % 16, h = tid / 16 * 2;
-    float e = LOW, s = 0.f;
-#pragma unroll
-    for (int g = 0; g < 16; ++g) e = fmaxf(e, part[r][g][h]);
-#pragma unroll
-    for (int g = 0; g < 16; ++g) s += part[r][g][h + 1] * exp2f(part[r][g][h] - e);
-    joined[r][tid / 16] = s > 0.f ? __builtin_fmaf(e, LN2, logf(s)) : NONE;    // log of the sum over the columns that are no item
-  }
-  __syncthreads();
-  for (int r = wave; r < 16 && first + r < live; r += 4) {
-    const int row = first + r, t = a.row_token[row], slot = a.target_slot[row];
-    const float* z = a.z_item + static_cast<size_t>(row) * (K + 1);
-    const float rest1 = joined[r][0], rest2 = two ? joined[r][1] : rest1, tau = a.t.temperature;
-    const size_t at = static_cast<size_t>(t) * K;
-    const float zy = slot >= 0 ? z[slot] : 0.f;
-    float loss = 0.f, lse = 0.f, kd = 0.f, lse_t = 0.f;
-    // loss = log(1 + exp(away)), away = log of the sum over all columns but the target, less the target's logit
-    if (slot >= 0) {
-      float top = rest1;
-      for (int j = lane; j < K; j += MOE_WAVE)
-        if (j != slot && entry_there(a.t.ids[at + j], a.t.logits[at + j], a.V)) top = fmaxf(top, z[j]);
-      top = wave_max_of(top);
-      float sum = 0.f;
-      for (int j = lane; j < K; j += MOE_WAVE)
-        if (j != slot && entry_there(a.t.ids[at + j], a.t.logits[at + j], a.V)) sum += expf(z[j] - top);
-      sum = wave_sum_of(sum);
-      const float away = top > NONE ? top + logf(sum + expf(rest1 - top)) - zy : NONE;
-      loss = fmaxf(away, 0.f) + log1pf(expf(-fabsf(away)));
-      lse = loss + zy;
-    }
-    // With b_j = z_j / tau - log q_j on the entries, b their mean under q, u_j = b_j - b, and R the sum over the columns that are no entry:
-    // kd = log(R e^-b + sum q e^u), where sum q e^u = 1 + sum q (e^u - 1 - u) tells a student that is nearly the teacher from the teacher
-    if (K > 0) {
-      const float lq = teacher_lse(a.t, at, a.V, lane);
-      float mean = 0.f;
-      for (int j = lane; j < K; j += MOE_WAVE) {
-        if (!entry_there(a.t.ids[at + j], a.t.logits[at + j], a.V)) continue;
-        const float log_q = a.t.logits[at + j] / tau - lq;
-        mean += expf(log_q) * (z[j] / tau - log_q);
-      }
-      mean = wave_sum_of(mean);
-      float rest = rest2;
-      if (slot == K) {                                                   // the target is no entry
-        const float b = zy / tau, top = fmaxf(rest, b);
-        rest = top + logf(expf(rest - top) + expf(b - top));
-      }
-      float far = rest - mean, sum = 0.f;
-      for (int j = lane; j < K; j += MOE_WAVE) {
-        if (!entry_there(a.t.ids[at + j], a.t.logits[at + j], a.V)) continue;
-        const float log_q = a.t.logits[at + j] / tau - lq, u = z[j] / tau - log_q - mean;
-        far = fmaxf(far, u);
-        sum += expf(log_q) * (expm1f(fminf(u, 80.f)) - u);
-      }
-      far = wave_max_of(far);
-      sum = wave_sum_of(sum);
-      if (far < 40.f) {
-        kd = log1pf(expf(rest - mean) + sum);
-      } else {                                                           // the same with the largest term in front
-        sum = 0.f;
-        for (int j = lane; j < K; j += MOE_WAVE) {
-          if (!entry_there(a.t.ids[at + j], a.t.logits[at + j], a.V)) continue;
-          sum += expf(z[j] / tau - mean - far);                          // q e^u
-        }
-        kd = far + logf(expf(rest - mean - far) + wave_sum_of(sum));
-      }
-      lse_t = kd + mean;
-      if (!(lq > NONE)) kd = lse_t = 0.f;                                // no entry
-    }
-    if (lane == 0) {
-      a.loss[t] = loss;
-      a.lse[t] = lse;
-      if (K > 0) { a.kd[t] = kd; a.lse_t[t] = lse_t; }
-    }
-  }
-}
-
-struct HeadPatchArgs {
-  const int32_t *offsets, *row_token, *target, *target_slot;
-  const float* z_item;
-  Teacher t;
-  const float *loss, *lse, *lse_t, *dloss, *dkd;
-  moe_bf16* dz;
-  int ld, V, v0, v1;               // columns v0 to v1 are in dz
-};
-// The gradient where it is no plain softmax: at the target and at the entries, from their logits.  p - 1 at the target is exp(-loss) - 1, p - q at an
-// entry q (exp(log p - log q) - 1).  A wave takes a row.
-__global__ __launch_bounds__(256) void head_patch_kernel(HeadPatchArgs a) {
-  const int row = blockIdx.x * 4 + threadIdx.x / MOE_WAVE, lane = threadIdx.x % MOE_WAVE;
-  if (row >= a.offsets[1]) return;
-  const int t = a.row_token[row], slot = a.target_slot[row], K = a.t.K, y = a.target[t];
-  const size_t at = static_cast<size_t>(t) * K;
+  const int r = tid / MOE_WAVE, row = first + r;
+  if (row >= live) return;
+  // log of the sum over the columns that are no item
+  auto joined = [&](int h) __attribute__((always_inline)) {
+    const float e = part[h][lane][r], top = wave_max_of(e), s = wave_sum_of(part[h + 1][lane][r] * __builtin_amdgcn_exp2f(e - top));
+    return s > 0.f ? __builtin_fmaf(top, LN2, logf(s)) : NONE;
+  };
+  const float rest1 = joined(0), rest2 = two ? joined(2) : rest1, tau = a.t.temperature;
+  const int t = a.row_token[row], slot = a.target_slot[row];
   const float* z = a.z_item + static_cast<size_t>(row) * (K + 1);
-  const float tau = a.t.temperature, at_target = slot >= 0 ? expm1f(-a.loss[t]) * a.dloss[t] : 0.f;
-  moe_bf16* out = a.dz + static_cast<size_t>(row) * a.ld;
-  const float lq = K > 0 ? teacher_lse(a.t, at, a.V, lane) : 0.f;
-  const bool taught = K > 0 && lq > -__builtin_inff();
-  const float gk = taught ? a.dkd[t] / tau : 0.f, lt = taught ? a.lse_t[t] : 0.f;
-  for (int j = lane; j < K; j += MOE_WAVE) {
-    const int id = a.t.ids[at + j];
-    if (!entry_there(id, a.t.logits[at + j], a.V) || id < a.v0 || id >= a.v1) continue;
-    const float log_q = a.t.logits[at + j] / tau - lq;
-    float g = expf(log_q) * expm1f(z[j] / tau - lt - log_q) * gk;
-    if (id == y) g += at_target;
-    else if (slot >= 0) g = __builtin_fmaf(expf(z[j] - a.lse[t]), a.dloss[t], g);
-    out[id - a.v0] = f32_to_bf16(g);
+  const size_t at = static_cast<size_t>(t) * K;
+  const float zy = slot >= 0 ? z[slot] : 0.f;
+  bool on[EPL];
+  float zj[EPL], l[EPL];                                 // an entry's logit and, over the temperature, the teacher's
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    const int j = lane + i * MOE_WAVE;
+    on[i] = j < K && entry_there(a.t.ids[at + j], a.t.logits[at + j], a.V);
+    zj[i] = on[i] ? z[j] : 0.f;
+    l[i] = on[i] ? a.t.logits[at + j] / tau : NONE;
   }
-  if (slot == K && lane == 0 && y >= a.v0 && y < a.v1) {
-    float g = at_target;
-    if (taught) g = __builtin_fmaf(expf(z[K] / tau - lt), gk, g);
-    out[y - a.v0] = f32_to_bf16(g);
+  float loss = 0.f, lse = 0.f, kd = 0.f, lse_t = 0.f;
+  // loss = log(1 + exp(away)), away = log of the sum over all columns but the target, less the target's logit
+  if (slot >= 0) {
+    float top = rest1, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) if (on[i] && lane + i * MOE_WAVE != slot) top = fmaxf(top, zj[i]);
+    if (K > 0) top = wave_max_of(top);
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) if (on[i] && lane + i * MOE_WAVE != slot) sum += expf(zj[i] - top);
+    if (K > 0) sum = wave_sum_of(sum);
+    const float away = top > NONE ? top + logf(sum + expf(rest1 - top)) - zy : NONE;
+    loss = fmaxf(away, 0.f) + log1pf(expf(-fabsf(away)));
+    lse = loss + zy;
+  }
+  // With b_j = z_j / tau - log q_j on the entries, b their mean under q, u_j = b_j - b, and R the sum over the columns that are no entry:
+  // kd = log(R e^-b + sum q e^u), where sum q e^u = 1 + sum q (e^u - 1 - u) tells a student that is nearly the teacher from the teacher
+  float top = NONE;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) top = fmaxf(top, l[i]);
+  if (K > 0) top = wave_max_of(top);
+  if (top > NONE) {                                      // there is an entry
+    float sum = 0.f, mean = 0.f;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) sum += on[i] ? expf(l[i] - top) : 0.f;
+    const float lq = top + logf(wave_sum_of(sum));
+    float q[EPL], b[EPL];
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      q[i] = on[i] ? expf(l[i] - lq) : 0.f;
+      b[i] = on[i] ? zj[i] / tau - (l[i] - lq) : 0.f;
+      mean += q[i] * b[i];
+    }
+    mean = wave_sum_of(mean);
+    float rest = rest2;
+    if (slot == K) {                                     // the target is no entry
+      const float zt = zy / tau, m = fmaxf(rest, zt);
+      rest = m + logf(expf(rest - m) + expf(zt - m));
+    }
+    float far = rest - mean;
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      const float u = b[i] - mean;
+      if (on[i]) { far = fmaxf(far, u); sum += q[i] * (expm1f(fminf(u, 80.f)) - u); }
+    }
+    far = wave_max_of(far);
+    sum = wave_sum_of(sum);
+    if (far < 40.f) {
+      kd = log1pf(expf(rest - mean) + sum);
+    } else {                                             // the same with the largest term in front
+      sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) sum += on[i] ? expf(zj[i] / tau - mean - far) : 0.f;      // q e^u
+      kd = far + logf(expf(rest - mean - far) + wave_sum_of(sum));
+    }
+    lse_t = kd + mean;
+  }
+  if (lane == 0) {
+    a.loss[t] = loss;
+    a.lse[t] = lse;
+    if (K > 0) { a.kd[t] = kd; a.lse_t[t] = lse_t; }
   }
 }
 
-// dx of a token: the parts' sums in their order, rounded once; zeros without a loss.
-__global__ __launch_bounds__(256) void head_dx_kernel(const float* __restrict__ part, int parts, const int32_t* __restrict__ token_row, int T, int d,
-                                                      moe_bf16* __restrict__ dx) {
-  const int pieces = d / 8;
+struct HeadDxArgs {
+  const float* part;
+  int parts;
+  const int32_t *token_row, *target_slot, *target;
+  const float* item;               // what dz lost at the items
+  Teacher t;
+  const moe_bf16* W;
+  int T, d, V, all;                // all: of every item, else of the target
+  moe_bf16* dx;
+};
+// dx of a token: the parts' sums in their order and what rounding dz took from them where it is largest, rounded once; zeros without a loss.
+__global__ __launch_bounds__(256) void head_dx_kernel(HeadDxArgs a) {
+  const int pieces = a.d / 8, K = a.t.K;
   const size_t i = static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= static_cast<size_t>(T) * pieces) return;
-  const int t = static_cast<int>(i / pieces), c = static_cast<int>(i - static_cast<size_t>(t) * pieces) * 8, row = token_row[t];
+  if (i >= static_cast<size_t>(a.T) * pieces) return;
+  const int t = static_cast<int>(i / pieces), c = static_cast<int>(i - static_cast<size_t>(t) * pieces) * 8, row = a.token_row[t];
   f32x4_t v[2] = {};
+  typedef __attribute__((ext_vector_type(4))) uint32_t u4;
   if (row >= 0) {
+    auto add = [&](int slot, int id) __attribute__((always_inline)) {
+      const float e = a.item[static_cast<size_t>(row) * (K + 1) + slot];
+      const u4 w = *reinterpret_cast<const u4*>(a.W + static_cast<size_t>(id) * a.d + c);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[k >> 1][2 * (k & 1)] = __builtin_fmaf(e, bf16lo(w[k]), v[k >> 1][2 * (k & 1)]);
+        v[k >> 1][2 * (k & 1) + 1] = __builtin_fmaf(e, bf16hi(w[k]), v[k >> 1][2 * (k & 1) + 1]);
+      }
+    };
+    const int slot = a.target_slot[row];
+    if (slot >= 0) add(slot, a.target[t]);
+    if (a.all) {
+      for (int j = 0; j < K; ++j) {
+        const size_t at = static_cast<size_t>(t) * K + j;
+        if (j != slot && entry_there(a.t.ids[at], a.t.logits[at], a.V)) add(j, a.t.ids[at]);
+      }
+    }
 #pragma unroll 4
-    for (int p = 0; p < parts; ++p) {
-      const float* q = part + (static_cast<size_t>(p) * T + row) * d + c;
+    for (int p = 0; p < a.parts; ++p) {
+      const float* q = a.part + (static_cast<size_t>(p) * a.T + row) * a.d + c;
       v[0] += *reinterpret_cast<const f32x4_t*>(q);
       v[1] += *reinterpret_cast<const f32x4_t*>(q + 4);
     }
   }
-  typedef __attribute__((ext_vector_type(4))) uint32_t u4;
-  *reinterpret_cast<u4*>(dx + static_cast<size_t>(t) * d + c) =
+  *reinterpret_cast<u4*>(a.dx + static_cast<size_t>(t) * a.d + c) =
       u4{pack_bf16(v[0][0], v[0][1]), pack_bf16(v[0][2], v[0][3]), pack_bf16(v[1][0], v[1][1]), pack_bf16(v[1][2], v[1][3])};
 }
 
@@ -416,10 +469,10 @@ int head_edge(int rows, int cols, int depth, double more256, double more128) {
 
 // What the workspace holds, by offset.
 struct HeadLayout {
-  size_t offsets, mask, row_token, token_row, target_slot, xc, list_start, items, z_item, row, big, bytes;
-  int strips64, blocks, slots;
+  size_t control, mask, row_token, token_row, target_slot, xc, list_start, items, terms, item, row, big;   // terms, row: of the backward pass
+  int strips64, blocks, slots, low;
 };
-HeadLayout head_layout(int T, int d, int V, int K) {
+HeadLayout head_layout(int T, int d, int V, int K, bool backward) {
   HeadLayout l{};
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t p = at; at += (bytes + 255) & ~static_cast<size_t>(255); return p; };
@@ -427,21 +480,27 @@ HeadLayout head_layout(int T, int d, int V, int K) {
   l.strips64 = (V + 63) / 64;
   l.blocks = (T + 15) / 16;
   l.slots = K + 1;
-  l.offsets = take(8);
+  l.low = backward && T <= LOW_TOKENS;
+  l.control = take(CONTROL_INTS * 4);
   l.mask = take((n + 63) / 64 * 8);
   l.row_token = take(4 * n);
   l.token_row = take(4 * n);
   l.target_slot = take(4 * n);
-  l.xc = take(2 * n * d);
+  l.xc = take((l.low ? 4 : 2) * n * d);
   l.list_start = take(static_cast<size_t>(l.blocks) * (l.strips64 + 1) * 4);
-  l.items = take(static_cast<size_t>(l.blocks) * 16 * l.slots * sizeof(HeadItem));
-  l.z_item = take(n * l.slots * 4);
-  l.row = take(16 * n);
-  l.big = l.bytes = at;
+  const size_t items = static_cast<size_t>(l.blocks) * 16 * l.slots;
+  l.items = take(items * sizeof(HeadItem));
+  l.item = take(n * l.slots * 4);
+  if (backward) {
+    l.terms = take(items * sizeof(f32x4_t));
+    l.row = take(16 * n);
+  }
+  l.big = at;
   return l;
 }
 size_t head_part_bytes(int T, int V) { return static_cast<size_t>(3) * ((V + 63) / 64) * T * sizeof(float); }
-size_t head_dz_bytes(int T, int piece) { return (static_cast<size_t>(T) * ((piece + 63) & ~63) * 2 + 255) & ~static_cast<size_t>(255); }
+// (a few tokens: what rounding loses lies in as many rows behind the others)
+size_t head_dz_bytes(int T, int piece) { return (static_cast<size_t>(T <= LOW_TOKENS ? 2 * T : T) * ((piece + 63) & ~63) * 2 + 255) & ~static_cast<size_t>(255); }
 
 struct HeadCall {
   const moe_bf16 *x, *W;
@@ -457,13 +516,14 @@ struct HeadCall {
 
 int run_prep(const HeadCall& c, const HeadLayout& l) {
   uint64_t* mask = nullptr;
-  if (c.t.K > 0 || c.T > SELF_MASK_TOKENS) {
+  if (c.T > SELF_MASK_TOKENS || static_cast<long long>(c.T) * (c.t.K + 1) > SELF_MASK_LOADS) {
     mask = reinterpret_cast<uint64_t*>(c.ws + l.mask);
-    MOE_LAUNCH("head_mask", head_mask_kernel, dim3((c.T + 255) / 256), dim3(256), 0, c.s, c.target, c.t, c.T, c.V, mask);
+    MOE_LAUNCH("head_mask", head_mask_kernel, dim3((c.T + 63) / 64), dim3(256), 0, c.s, c.target, c.t, c.T, c.V, mask);
   }
   HeadPrepArgs p{};
   p.x = c.x; p.target = c.target; p.t = c.t; p.mask = mask; p.T = c.T; p.d = c.d; p.V = c.V; p.strips = l.strips64;
-  p.offsets = reinterpret_cast<int32_t*>(c.ws + l.offsets);
+  p.low = l.low;
+  p.control = reinterpret_cast<int32_t*>(c.ws + l.control);
   p.row_token = reinterpret_cast<int32_t*>(c.ws + l.row_token);
   p.token_row = reinterpret_cast<int32_t*>(c.ws + l.token_row);
   p.target_slot = reinterpret_cast<int32_t*>(c.ws + l.target_slot);
@@ -472,23 +532,30 @@ int run_prep(const HeadCall& c, const HeadLayout& l) {
   p.items = reinterpret_cast<HeadItem*>(c.ws + l.items);
   p.loss = c.loss; p.lse = c.lse; p.kd = c.kd; p.lse_t = c.lse_t;
   p.in_loss = c.in_loss; p.in_lse = c.in_lse; p.in_lse_t = c.in_lse_t; p.dloss = c.dloss; p.dkd = c.dkd;
-  p.row = c.dx != nullptr ? reinterpret_cast<f32x4_t*>(c.ws + l.row) : nullptr;
+  if (c.dx != nullptr) {
+    p.terms = reinterpret_cast<f32x4_t*>(c.ws + l.terms);
+    p.row = reinterpret_cast<f32x4_t*>(c.ws + l.row);
+  }
   const int lds = (l.strips64 + 1) * 4;
   static bool configured[MAX_DEVICES] = {};
   if (configure_lds(&head_prep_kernel, (HEAD_MAX_V / 64 + 1) * 4, configured) != MOE_OK) return MOE_ERR_LAUNCH;
-  MOE_LAUNCH("head_prep", head_prep_kernel, dim3(l.blocks), dim3(256), lds, c.s, p);
+  MOE_LAUNCH("head_prep", head_prep_kernel, dim3(l.blocks, (c.d + 1023) / 1024), dim3(256), lds, c.s, p);
   return moe_check_launch();
 }
 
 void fill_head(const HeadCall& c, const HeadLayout& l, GemmArgs& a, HeadArgs& h) {
-  a.offsets = reinterpret_cast<const int32_t*>(c.ws + l.offsets);
+  const int32_t* control = reinterpret_cast<const int32_t*>(c.ws + l.control);
+  a.offsets = control + ROWS;
+  a.row_token = control + DIRECT;
   a.E = 1;
   h.list_start = reinterpret_cast<const int32_t*>(c.ws + l.list_start);
   h.items = reinterpret_cast<const HeadItem*>(c.ws + l.items);
-  h.z_item = reinterpret_cast<float*>(c.ws + l.z_item);
+  h.item = reinterpret_cast<float*>(c.ws + l.item);
+  h.terms = reinterpret_cast<const f32x4_t*>(c.ws + l.terms);
   h.row = reinterpret_cast<const f32x4_t*>(c.ws + l.row);
   h.c1 = LOG2E;
   h.c2 = LOG2E / c.t.temperature;
+  h.over_tau = 1.f / c.t.temperature;
   h.two = c.t.K > 0 && c.t.temperature != 1.f;
   h.rows_cap = c.T;
   h.list_ld = l.strips64 + 1;
@@ -503,31 +570,35 @@ template <int MODE> int launch_head(GemmArgs& a, const HeadArgs& h, int edge, in
 }
 
 int run_head_fwd(const HeadCall& c) {
-  const HeadLayout l = head_layout(c.T, c.d, c.V, c.t.K);
+  const HeadLayout l = head_layout(c.T, c.d, c.V, c.t.K, false);
   int rc = run_prep(c, l);
   if (rc != MOE_OK) return rc;
   GemmArgs a{};
   HeadArgs h{};
   fill_head(c, l, a, h);
-  a.A0 = reinterpret_cast<const uint16_t*>(c.ws + l.xc); a.B0 = c.W; a.K = c.d; a.N = c.V;
+  a.A0 = reinterpret_cast<const uint16_t*>(c.ws + l.xc); a.A1 = c.x; a.B0 = c.W; a.K = c.d; a.N = c.V;
   const int edge = head_edge(c.T, c.V, c.d, 6.0, 3.0);
   h.strips = ceil_div(c.V, edge / 2);
   h.part = reinterpret_cast<float*>(c.ws + l.big);
   if ((rc = launch_head<HEAD_STATS>(a, h, edge, c.T, c.V, "gemm_head_stats", c.s)) != MOE_OK) return rc;
   const HeadJoinArgs j{h.part, a.offsets, reinterpret_cast<const int32_t*>(c.ws + l.row_token), reinterpret_cast<const int32_t*>(c.ws + l.target_slot),
-                       h.z_item, c.t, h.strips, c.T, c.V, c.loss, c.lse, c.kd, c.lse_t, h.c1, h.c2};
-  MOE_LAUNCH("head_join", head_join_kernel, dim3(l.blocks), dim3(256), 0, c.s, j);
+                       h.item, c.t, h.strips, c.T, c.V, c.loss, c.lse, c.kd, c.lse_t, h.c1, h.c2};
+  const dim3 grid(l.blocks), block(JOIN_THREADS);
+  if (c.t.K <= MOE_WAVE) MOE_LAUNCH("head_join", head_join_kernel<1>, grid, block, 0, c.s, j);
+  else if (c.t.K <= 2 * MOE_WAVE) MOE_LAUNCH("head_join", head_join_kernel<2>, grid, block, 0, c.s, j);
+  else MOE_LAUNCH("head_join", head_join_kernel<HEAD_MAX_K / MOE_WAVE>, grid, block, 0, c.s, j);
   return moe_check_launch();
 }
 
 int run_head_bwd(const HeadCall& c, int v_piece) {
-  const HeadLayout l = head_layout(c.T, c.d, c.V, c.t.K);
+  const HeadLayout l = head_layout(c.T, c.d, c.V, c.t.K, true);
   const int piece = head_piece(c.T, c.V, v_piece);
   uint16_t* dz = reinterpret_cast<uint16_t*>(c.ws + l.big);
   float* part = reinterpret_cast<float*>(c.ws + l.big + head_dz_bytes(c.T, piece));
   int rc = run_prep(c, l);
   if (rc != MOE_OK) return rc;
   const HeadShape dxs = head_dx_shape(c.T, c.d, piece);
+  const int dw_rows = l.low ? 2 * c.T : c.T;
   int parts = 0;
   for (int v0 = 0; v0 < c.V; v0 += piece) {
     const int cols = c.V - v0 < piece ? c.V - v0 : piece, ld = (cols + 63) & ~63;
@@ -535,14 +606,11 @@ int run_head_bwd(const HeadCall& c, int v_piece) {
     HeadArgs h{};
     fill_head(c, l, a, h);
     h.col0 = v0;
+    h.lo = l.low;
     const uint16_t* W = c.W + static_cast<size_t>(v0) * c.d;
-    a.A0 = reinterpret_cast<const uint16_t*>(c.ws + l.xc); a.B0 = W; a.O0 = dz; a.K = c.d; a.N = cols; a.M = ld;
+    a.A0 = reinterpret_cast<const uint16_t*>(c.ws + l.xc); a.A1 = c.x; a.B0 = W; a.O0 = dz; a.K = c.d; a.N = cols; a.M = ld;
     rc = launch_head<HEAD_DZ>(a, h, head_edge(c.T, cols, c.d, 6.0, 3.0), c.T, cols, "gemm_head_dz", c.s);
     if (rc != MOE_OK) return rc;
-    const HeadPatchArgs p{a.offsets, reinterpret_cast<const int32_t*>(c.ws + l.row_token), c.target, reinterpret_cast<const int32_t*>(c.ws + l.target_slot),
-                          h.z_item, c.t, c.in_loss, c.in_lse, c.in_lse_t, c.dloss, c.dkd, dz, ld, c.V, v0, v0 + cols};
-    MOE_LAUNCH("head_patch", head_patch_kernel, dim3((c.T + 3) / 4), dim3(256), 0, c.s, p);
-    if ((rc = moe_check_launch()) != MOE_OK) return rc;
     GemmArgs b{};
     b.offsets = a.offsets;
     b.A0 = dz; b.B0 = W; b.O0 = reinterpret_cast<uint16_t*>(part); b.K = ld; b.M = cols; b.N = c.d;
@@ -551,14 +619,15 @@ int run_head_bwd(const HeadCall& c, int v_piece) {
     h.add = v0 > 0;
     if ((rc = launch_head<HEAD_DX>(b, h, dxs.edge, c.T, c.d, "gemm_head_dx", c.s)) != MOE_OK) return rc;
     GemmArgs w{};
-    w.offsets = a.offsets; w.E = 1;
-    w.A0 = dz; w.B0 = a.A0; w.O0 = c.dW + static_cast<size_t>(v0) * c.d; w.M = ld; w.K = cols; w.N = c.d;
-    rc = launch_head<HEAD_DW>(w, h, head_edge(cols, c.d, c.T, 0.8, 1.1), cols, c.d, "gemm_head_dw", c.s);
+    w.offsets = reinterpret_cast<const int32_t*>(c.ws + l.control) + DW_ROWS - 1; w.E = 1; w.row_token = a.row_token;
+    w.A0 = dz; w.B0 = a.A0; w.B1 = a.A1; w.O0 = c.dW + static_cast<size_t>(v0) * c.d; w.M = ld; w.K = cols; w.N = c.d;
+    rc = launch_head<HEAD_DW>(w, h, head_edge(cols, c.d, dw_rows, 0.8, 1.1), cols, c.d, "gemm_head_dw", c.s);
     if (rc != MOE_OK) return rc;
   }
   const size_t n = static_cast<size_t>(c.T) * (c.d / 8);
-  MOE_LAUNCH("head_dx", head_dx_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, c.s, static_cast<const float*>(part), parts,
-             reinterpret_cast<const int32_t*>(c.ws + l.token_row), c.T, c.d, c.dx);
+  const HeadDxArgs x{part, parts, reinterpret_cast<const int32_t*>(c.ws + l.token_row), reinterpret_cast<const int32_t*>(c.ws + l.target_slot), c.target,
+                     reinterpret_cast<const float*>(c.ws + l.item), c.t, c.W, c.T, c.d, c.V, c.T <= LOW_TOKENS, c.dx};
+  MOE_LAUNCH("head_dx", head_dx_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, c.s, x);
   return moe_check_launch();
 }
 
@@ -572,13 +641,13 @@ bool bad_temperature(float t) { return !(t > 0.f) || !(t < __builtin_inff()); }
 
 extern "C" size_t moe_head_fwd_workspace_bytes(int T, int d, int V, int K) {
   if (bad_head_dims(T, d, V, K)) return 0;
-  return head_layout(T, d, V, K).bytes + head_part_bytes(T, V);
+  return head_layout(T, d, V, K, false).big + head_part_bytes(T, V);
 }
 
 extern "C" size_t moe_head_bwd_workspace_bytes(int T, int d, int V, int K, int v_piece) {
   if (bad_head_dims(T, d, V, K) || v_piece < 0 || v_piece % 256 != 0) return 0;
   const int piece = head_piece(T, V, v_piece);
-  return head_layout(T, d, V, K).bytes + head_dz_bytes(T, piece) + static_cast<size_t>(head_dx_shape(T, d, piece).parts) * T * d * sizeof(float);
+  return head_layout(T, d, V, K, true).big + head_dz_bytes(T, piece) + static_cast<size_t>(head_dx_shape(T, d, piece).parts) * T * d * sizeof(float);
 }
 
 extern "C" int moe_head_ce_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, int T, int d, int V, float* loss, float* lse,
