@@ -108,7 +108,7 @@ enum GemmMode { GATE_UP = 0, DOWN = 1, DGRAD_H = 2, DGRAD_X = 3, WGRAD = 4, WGRA
 // row's partial dot product with h = silu(g) u (the gradient of the gate weight).
 // The vocabulary head (head.hip), rows offsets[0] = 0 to offsets[1], one group.  HEAD_STATS, HEAD_DZ: logits A0 . B0^T of which the
 // epilogue makes a row's maximum and sums over the wave's columns, or the logits' gradient (row length M).  HEAD_DX: A0 (row length K) times
-// B0 in E parts of the reduction over its M rows, each part's sums in 32 bits.  HEAD_DW: WGRAD with rows of M elements, K of them wanted.
+// B0 in row_token[0] parts of the reduction over its M rows, each part's sums in 32 bits.  HEAD_DW: WGRAD with rows of M elements, K of them wanted.
 constexpr bool is_logits(int mode) { return mode == HEAD_STATS || mode == HEAD_DZ; }
 constexpr bool is_wgrad(int mode) { return mode == WGRAD || mode == WGRAD_GATHER || mode == WGRAD_GATHER_A || mode == HEAD_DW; }
 constexpr bool is_dgrad_h(int mode) { return mode == DGRAD_H || mode == DGRAD_H_GATE; }
@@ -141,14 +141,16 @@ struct GemmArgs {
 };
 
 // What the epilogues of the head's products take beside GemmArgs.  Items are the logits that count by themselves: of the target and of the
-// teacher's entries.  They are listed by blocks of 16 rows and, inside a block, by strips of 64 columns.
+// teacher's entries.  Without a teacher every row has one item, its target; with one they are listed by blocks of 16 rows and, inside a block,
+// by strips of 64 columns.
 struct HeadItem { uint32_t at, slot; };   // at: row in the block | column << 4
 struct HeadArgs {
   float* part;                // HEAD_STATS: planes [strips][rows_cap] of maximum, sum and (two) sum at the temperature over HALF columns, without the items
   const f32x4_t* row;         // HEAD_DZ: per row log2(e) lse, factor, and the same at the temperature
-  const int32_t* list_start;  // [row block][list_ld]: first item of each strip
+  const int32_t* target;      // [row]
+  const int32_t* list_start;  // [row block][list_ld]: first item of each strip; null: no teacher
   const HeadItem* items;      // [row block][16 slots]
-  const f32x4_t* terms;       // HEAD_DZ: as items; the gradient there is t0 + t1 (exp(z / temperature - t2) - 1) + t3 exp(z - lse)
+  const f32x4_t* terms;       // HEAD_DZ: as items, or [row]; the gradient there is t0 + t1 (exp(z / temperature - t2) - 1) + t3 exp(z - lse)
   float* item;                // [row][slots]: HEAD_STATS: the logit; HEAD_DZ: what the gradient loses when it is rounded
   float c1, c2, over_tau;     // log2(e), the same over the temperature, 1 / temperature
   int two;                    // both sums, both terms
@@ -392,6 +394,9 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
   constexpr bool GATHER_B = (MODE == WGRAD_GATHER);
   constexpr bool GATHER_A = (MODE == WGRAD_GATHER_A);
 
+  // (HEAD_STATS: all M tokens, where none has been left out)
+  auto head_rows = [&]() __attribute__((always_inline)) { return MODE == HEAD_STATS && a.offsets == nullptr ? a.M : a.offsets[1]; };
+
   // ---------------- tile list ---------------------------------------------------
   int total;
   // experts `lane` and `lane + 64`: row range and list position of the first tile, kept for the whole kernel
@@ -404,7 +409,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
   if constexpr (is_wgrad(MODE)) {
     total = a.E * a.m_tiles_cap * a.n_tiles * wpair;
   } else if constexpr (is_logits(MODE) || MODE == HEAD_DX) {
-    total = (a.offsets[1] + S - 1) / S * a.n_tiles * (MODE == HEAD_DX ? a.E : 1);
+    total = (head_rows() + S - 1) / S * a.n_tiles * (MODE == HEAD_DX ? a.row_token[0] : 1);
   } else {
     total = count_row_tiles<S>(a.offsets, a.E, tid0 & 63) * a.n_tiles;
     if constexpr (MODE == GATE_UP || MODE == DOWN) {
@@ -448,7 +453,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
   } else if constexpr (is_logits(MODE)) {
     // Bands of eight row tiles, column tile by column tile: the 32 (or 64) tiles that an XCD works on at a time then share 8 panels of
     // rows and 4 (or 8) of columns; all rows of a column tile in a run would have every XCD fetch all rows in every round.
-    m_end = a.offsets[1];
+    m_end = head_rows();
     rt = (m_end + S - 1) / S;
     const int band = tile / (8 * a.n_tiles), in = tile - band * 8 * a.n_tiles;
     const int high = rt - band * 8 < 8 ? rt - band * 8 : 8;
@@ -457,7 +462,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
     e = 0;
     nt = __builtin_amdgcn_readfirstlane(nt);
   } else if constexpr (MODE == HEAD_DX) {
-    m_end = a.offsets[1];
+    m_end = head_rows();
     rt = (m_end + S - 1) / S;
     e = tile / (rt * a.n_tiles);        // part of the reduction
     const int in = tile - e * rt * a.n_tiles;
@@ -552,7 +557,8 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
     nk = a.K / BK;
     nk_phase = nk;
     // (logits: the tokens' rows side by side, or as they are where all have a loss)
-    const uint16_t* A = is_logits(MODE) && a.row_token[0] != 0 ? a.A1 : a.A0;
+    const uint16_t* A = a.A0;
+    if constexpr (is_logits(MODE)) { if (a.row_token != nullptr && a.row_token[0] != 0) A = a.A1; }
     abase = reinterpret_cast<const char*>(A + static_cast<size_t>(m0) * a.K);
     a_step = BK * 2;
     bool gathered = false;
@@ -572,8 +578,9 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
     if constexpr (MODE == DGRAD_X) { a_phase = (a.A1 - a.A0) * 2; nk *= 2; }
     if constexpr (MODE == HEAD_DX) {
       const int steps = (a.M + BK - 1) / BK;
-      k_lo = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<long long>(steps) * e / a.E)) * BK;
-      k_hi = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<long long>(steps) * (e + 1) / a.E)) * BK;
+      const int parts = a.row_token[0];
+      k_lo = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<long long>(steps) * e / parts)) * BK;
+      k_hi = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<long long>(steps) * (e + 1) / parts)) * BK;
       nk = nk_phase = (k_hi - k_lo) / BK;
       k_hi = k_hi > a.M ? a.M : k_hi;
       abase += static_cast<size_t>(k_lo) * 2;
@@ -1110,12 +1117,17 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
     asm volatile("" ::: "memory");            // requested here, not where they are used
   };
 
-  // The logits' epilogues: first and last item of each of the wave's blocks of 16 rows (in lanes 0 to NB - 1), and HEAD_DZ's factors of the
-  // lane's rows.
-  int item_lo = 0, item_hi = 0;
-  f32x4_t rowp[MODE == HEAD_DZ ? NB : 1];
-  auto fetch_head = [&](const TileState& t) __attribute__((always_inline)) {
+  // The logits' epilogues.  A lane holds up to IT of the items in its wave's piece (place 0 to HALF - 1 of the row | column << 8, or -1), with
+  // their place in HeadArgs::item and (HEAD_DZ) their terms; `many`: there are more, and the parts look them up.
+  // Without a teacher these are the targets of the lane's rows.  Otherwise the bounds of the lists of the wave's blocks (in lanes 0 to NB - 1) are
+  // requested with the tile's first loads, so that one latency, not two in a row, stands behind the main loop.
+  constexpr int IT = HALF / 64;
+  int item_lo = 0, item_hi = 0, list_lo = 0, list_hi = 0, item_at[IT], item_place[IT];
+  bool many = false;
+  f32x4_t item_term[MODE == HEAD_DZ ? IT : 1], rowp[MODE == HEAD_DZ ? NB : 1];
+  auto fetch_lists = [&](const TileState& t) __attribute__((always_inline)) {
     const HeadPtr he = head_args();
+    if (he->list_start == nullptr) return;
     const int first = t.m0 + t.r0, last = t.m_end - 1;
     int b = (first >> 4) + (lane < NB ? lane : NB - 1);
     if (b > last >> 4) b = last >> 4;
@@ -1123,8 +1135,46 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
     if (strip > he->list_ld - 1) strip = he->list_ld - 1;
     if (end > he->list_ld - 1) end = he->list_ld - 1;
     const int32_t* start = he->list_start + static_cast<size_t>(b) * he->list_ld;
-    item_lo = start[strip];
-    item_hi = start[end];
+    list_lo = start[strip];
+    list_hi = start[end];
+    asm volatile("" ::: "memory");            // requested here, not where they are used
+  };
+  auto fetch_items = [&](const TileState& t) __attribute__((always_inline)) {
+    const HeadPtr he = head_args();
+    const int first = t.m0 + t.r0, last = t.m_end - 1, col = he->col0 + t.n0 + wn * HALF;
+    many = false;
+    if (he->list_start == nullptr) {
+#pragma unroll
+      for (int k = 0; k < IT; ++k) {
+        const int r = lane + 64 * k, row = first + r < t.m_wave ? first + r : last;
+        const int c = he->target[row] - col;
+        item_at[k] = first + r < t.m_wave && c >= 0 && c < HALF ? r | c << 8 : -1;
+        item_place[k] = row;
+        if constexpr (MODE == HEAD_DZ) item_term[k] = he->terms[row];
+      }
+    } else {
+      item_lo = list_lo;
+      item_hi = list_hi;
+      const int n = lane < NB && first + lane * 16 < t.m_wave ? item_hi - item_lo : 0, end = wave_incl_scan(n);
+      many = wave_lane(end, 63) > 64 * IT;
+#pragma unroll
+      for (int k = 0; k < IT; ++k) {
+        const int i = lane + 64 * k;
+        int part = 0;
+#pragma unroll
+        for (int p = 0; p < NB - 1; ++p) part += i >= wave_lane(end, p) ? 1 : 0;
+        const int in = i - (__shfl(end, part) - __shfl(n, part)) + __shfl(item_lo, part);
+        item_at[k] = -1;
+        if (i < wave_lane(end, NB - 1)) {
+          const size_t at = static_cast<size_t>((first >> 4) + part) * 16 * he->slots + in;
+          const HeadItem x = he->items[at];
+          const int r = part * 16 + (x.at & 15);
+          item_at[k] = r | (static_cast<int>(x.at >> 4) - col) << 8;
+          item_place[k] = (first + r) * he->slots + static_cast<int>(x.slot);
+          if constexpr (MODE == HEAD_DZ) item_term[k] = he->terms[at];
+        }
+      }
+    }
     if constexpr (MODE == HEAD_DZ) {
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
@@ -1395,15 +1445,35 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
       auto z_piece = [&](int row, int piece) __attribute__((always_inline)) {
         return reinterpret_cast<float*>(stage + row * (HALF * 4) + ((piece ^ row) << 4));
       };
-      // f(there, row, its place in the lists, its logit's place) for the part's items, 64 at a time
-      auto over_items = [&](int part, int lo, int hi, auto&& f) __attribute__((always_inline)) {
+      // f(there, row, place in HeadArgs::item, terms, its logit's place in LDS) for the part's items, a lane each, all lanes together
+      auto over_items = [&](auto part_tag, auto&& f) __attribute__((always_inline)) {
+        constexpr int part = decltype(part_tag)::value;
+        if (!many) {
+#pragma unroll
+          for (int k = 0; k < IT; ++k) {
+            const bool there = item_at[k] >= 0 && (item_at[k] >> 4 & (HALF / 16 - 1)) == part;
+            const int row = there ? item_at[k] & 15 : 0, c = there ? item_at[k] >> 8 : 0;
+            f(there, row, item_place[k], item_term[MODE == HEAD_DZ ? k : 0], z_piece(row, c >> 2) + (c & 3));
+          }
+          return;
+        }
+        const int hi = wave_lane(item_hi, part);
         const size_t first = static_cast<size_t>((grow0 >> 4) + part) * 16 * he->slots;
-        for (int n0 = lo; n0 < hi; n0 += 64) {
+        for (int n0 = wave_lane(item_lo, part); n0 < hi; n0 += 64) {
           const int n = n0 + lane < hi ? n0 + lane : hi - 1;
           const HeadItem x = he->items[first + n];
           const int row = x.at & 15, c = static_cast<int>(x.at >> 4) - he->col0 - gcol0;
-          f(n0 + lane < hi, row, static_cast<size_t>(grow0 + part * 16 + row) * he->slots + x.slot, first + n, z_piece(row, c >> 2) + (c & 3));
+          f(n0 + lane < hi, row, (grow0 + part * 16 + row) * he->slots + static_cast<int>(x.slot), MODE == HEAD_DZ ? he->terms[first + n] : f32x4_t{},
+            z_piece(row, c >> 2) + (c & 3));
         }
+      };
+      auto has_items = [&](auto part_tag) __attribute__((always_inline)) {
+        constexpr int part = decltype(part_tag)::value;
+        if (many) return wave_lane(item_hi, part) > wave_lane(item_lo, part);
+        bool mine = false;
+#pragma unroll
+        for (int k = 0; k < IT; ++k) mine = mine || (item_at[k] >= 0 && (item_at[k] >> 4 & (HALF / 16 - 1)) == part);
+        return __ballot(mine) != 0;
       };
       auto put_logits = [&](const auto& v) __attribute__((always_inline)) {
         static_for<NB>([&](auto j) { *reinterpret_cast<f32x4_t*>(z_piece(l16, 4 * decltype(j)::value + lq)) = v[decltype(j)::value]; });
@@ -1430,12 +1500,11 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
           if (i * 16 >= rows || left <= 0) return;
           f32x4_t v[NB];
           static_for<NB>([&](auto j) { v[decltype(j)::value] = accq(i_tag, j); });
-          const int lo = wave_lane(item_lo, i), hi = wave_lane(item_hi, i);
-          if (hi > lo) {
+          if (has_items(i_tag)) {
             put_logits(v);
-            over_items(i, lo, hi, [&](bool there, int, size_t at, size_t, float* z) __attribute__((always_inline)) { if (there) he->item[at] = *z; });
+            over_items(i_tag, [&](bool there, int, int at, const f32x4_t&, float* z) __attribute__((always_inline)) { if (there) he->item[at] = *z; });
             __builtin_amdgcn_wave_barrier();
-            over_items(i, lo, hi, [&](bool, int, size_t, size_t, float* z) __attribute__((always_inline)) { *z = NONE; });
+            over_items(i_tag, [&](bool there, int, int, const f32x4_t&, float* z) __attribute__((always_inline)) { if (there) *z = NONE; });
             get_logits(v);
           }
           mask(v, NONE);
@@ -1484,14 +1553,16 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
           constexpr int i = decltype(i_tag)::value;
           if (i * 16 >= rows) return;
           const f32x4_t p = rowp[i];
-          f32x4_t v[NB], special[NB];
+          f32x4_t v[NB];
           static_for<NB>([&](auto j) { v[decltype(j)::value] = accq(i_tag, j); });
-          const int lo = wave_lane(item_lo, i), hi = wave_lane(item_hi, i);
-          if (hi > lo) {
+          auto gradient = [&](float z) __attribute__((always_inline)) {
+            const float g = __builtin_amdgcn_exp2f(__builtin_fmaf(z, c1, -p[0])) * p[1];
+            return two ? __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(z, c2, -p[2])), p[3], g) : g;
+          };
+          if (has_items(i_tag)) {
             // the gradient at the items replaces their logits; a lane knows it by its bits, which are made to differ from the logit's
             put_logits(v);
-            over_items(i, lo, hi, [&](bool there, int row, size_t at, size_t n, float* zp) __attribute__((always_inline)) {
-              const f32x4_t t = he->terms[n];
+            over_items(i_tag, [&](bool there, int row, int at, const f32x4_t& t, float* zp) __attribute__((always_inline)) {
               const float z = *zp, lse = __shfl(p[0], row);
               float g = t[0];
               if (t[1] != 0.f) g = __builtin_fmaf(t[1], expm1f(__builtin_fmaf(z, he->over_tau, -t[2])), g);
@@ -1500,19 +1571,21 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
               he->item[at] = g - rounded(g);
               *zp = __uint_as_float(__float_as_uint(g) ^ (__float_as_uint(g) == __float_as_uint(z) ? 1u : 0u));
             });
+            f32x4_t special[NB];
             get_logits(special);
-          }
-          static_for<NB>([&](auto j_tag) {
-            constexpr int j = decltype(j_tag)::value;
+            static_for<NB>([&](auto j_tag) {
+              constexpr int j = decltype(j_tag)::value;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const float z = v[j][c];
-              float g = __builtin_amdgcn_exp2f(__builtin_fmaf(z, c1, -p[0])) * p[1];
-              if (two) g = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(z, c2, -p[2])), p[3], g);
-              if (hi > lo) g = __float_as_uint(special[j][c]) != __float_as_uint(z) ? special[j][c] : g;
-              v[j][c] = g;
-            }
-          });
+              for (int c = 0; c < 4; ++c)
+                v[j][c] = __float_as_uint(special[j][c]) != __float_as_uint(v[j][c]) ? special[j][c] : gradient(v[j][c]);
+            });
+          } else {
+            static_for<NB>([&](auto j_tag) {
+              constexpr int j = decltype(j_tag)::value;
+#pragma unroll
+              for (int c = 0; c < 4; ++c) v[j][c] = gradient(v[j][c]);
+            });
+          }
           mask(v, 0.f);
           store_part(i, v, oo);
           if (lows) {
@@ -1526,7 +1599,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
       }
     } else if constexpr (MODE == HEAD_DX) {
       const HeadPtr he = head_args();
-      float* const out = reinterpret_cast<float*>(ae->O0) + static_cast<size_t>(t.e) * he->rows_cap * ncol;
+      float* const out = reinterpret_cast<float*>(ae->O0) + static_cast<size_t>(t.e) * ae->offsets[1] * ncol;   // as many rows as there are
       const Rsrc oo = rows_of(out, ncol * 4);
       const bool add = he->add != 0;
       static_for<NB>([&](auto i_tag) {
@@ -1601,6 +1674,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
   if (tile < total) {
     TileState cur;
     setup_tile(list_entry(), cur);
+    if constexpr (is_logits(MODE)) fetch_lists(cur);
     first_loads(cur);
     for (;;) {
       last_first_loads(cur);
@@ -1617,7 +1691,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
       if constexpr (MODE == GATE_UP || MODE == DGRAD_H_GATE) {
         if (weighted) fetch_row_weights(cur, a.row_weight);
       }
-      if constexpr (is_logits(MODE)) fetch_head(cur);
+      if constexpr (is_logits(MODE)) fetch_items(cur);
       Finished done{cur.e, cur.m0, cur.n0, cur.r0, cur.m_wave, 0, 4, cur.second};
       tile += gridDim.x;
       const bool more = tile < total;
@@ -1634,11 +1708,15 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
         for (int i = 0; i < NB; ++i) asm volatile("" : "+v"(wv[i]));
       }
       if constexpr (is_logits(MODE)) {
-        asm volatile("" : "+v"(item_lo), "+v"(item_hi));
+#pragma unroll
+        for (int k = 0; k < IT; ++k) asm volatile("" : "+v"(item_at[k]), "+v"(item_place[k]));
         if constexpr (MODE == HEAD_DZ) {
+#pragma unroll
+          for (int k = 0; k < IT; ++k) asm volatile("" : "+v"(item_term[k]));
 #pragma unroll
           for (int i = 0; i < NB; ++i) asm volatile("" : "+v"(rowp[i]));
         }
+        if (more) fetch_lists(cur);
       }
       if (more) first_loads(cur);
       epilogue(done);

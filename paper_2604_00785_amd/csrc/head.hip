@@ -17,6 +17,7 @@ namespace {
 constexpr int HEAD_MAX_V = 1 << 20, HEAD_MAX_K = 1024;
 constexpr int HEAD_CUS = 256;                       // what the workspace's size is laid out for
 constexpr int SELF_MASK_TOKENS = 4096, SELF_MASK_LOADS = 8192;   // what a workgroup of head_prep finds out by itself
+constexpr int ALL_TOKENS = 128;                     // up to these, a forward pass without a teacher takes all tokens for rows
 constexpr int LOW_TOKENS = 128;                     // up to these, dW takes what rounding dz loses as well: its reduction is padded to 64 rows anyway, and a large product costs no more than writing dW
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -45,7 +46,19 @@ __global__ __launch_bounds__(256) void head_mask_kernel(const int32_t* __restric
 
 // What head_prep leaves for the kernels behind it, as integers: rows of the products from 0 to LIVE; those of dW, with the low parts, from 0
 // to DW_ROWS; whether x itself holds the rows.
-enum { ROWS = 0, LIVE = 1, DW_ROWS = 3, DIRECT = 4, CONTROL_INTS = 5 };
+enum { ROWS = 0, LIVE = 1, DW_ROWS = 3, DIRECT = 4, DX_PARTS = 5, CONTROL_INTS = 6 };
+
+// Parts of dx's reduction for `rows` rows, at most `most`: with few tiles a part each to as many compute units as there are.  The time expected of p parts,
+// in K steps of the tile: whole rounds of the chip's places (half of it by the rounds, half by what they hold, since idle units leave the others
+// power), what a tile costs beside its steps, and each part's sums written and read.  Lane p - 1 of a wave weighs p parts.
+struct DxRule { int edge, places, d, steps, most; float fixed; };
+__device__ __forceinline__ int dx_parts(const DxRule& x, int rows, int lane) {
+  const int p = lane + 1;
+  const float tiles = static_cast<float>((rows + x.edge - 1) / x.edge) * ((x.d + x.edge - 1) / x.edge) * p, rounds = tiles / x.places;
+  const float time = 0.5f * (rounds + fmaxf(1.f, floorf(rounds + 0.95f))) * (x.fixed + static_cast<float>(x.steps) / p) + p * (static_cast<float>(rows) * x.d / 4.0e6f);
+  const uint32_t key = p <= x.most && (p == 1 || x.steps / p >= 4) ? __float_as_uint(time) & ~63u | static_cast<uint32_t>(lane) : ~0u;
+  return 1 + (group_reduce<MOE_WAVE>(key, [](uint32_t u, uint32_t v) __attribute__((always_inline)) { return u < v ? u : v; }) & 63u);
+}
 
 struct HeadPrepArgs {
   const moe_bf16* x;
@@ -54,6 +67,9 @@ struct HeadPrepArgs {
   const uint64_t* mask;            // null: found here
   int T, d, V, strips;             // strips: of 64 columns
   int low;                         // rows of x twice
+  DxRule dx;
+  long long dx_room;               // rows that the parts' sums have room for, together
+  int32_t* target_row;             // the rows' targets
   int32_t *control, *row_token, *token_row;
   moe_bf16* xc;
   int32_t* list_start;
@@ -94,7 +110,7 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     mask = own;
   }
   if (tid < 16) { s_token[tid] = -1; s_target[tid] = -1; s_slot[tid] = K; }
-  if (lists) for (int i = tid; i <= a.strips; i += 256) count[i] = 0;
+  if (lists && K > 0) for (int i = tid; i <= a.strips; i += 256) count[i] = 0;
   __syncthreads();
   // rank of each thread's first token among those with a loss
   const int w0 = tid * per < words ? tid * per : words, w1 = w0 + per < words ? w0 + per : words;
@@ -113,6 +129,13 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     a.control[ROWS] = 0; a.control[LIVE] = live;
     a.control[DW_ROWS - 1] = 0; a.control[DW_ROWS] = a.low ? 2 * live : live;
     a.control[DIRECT] = direct;
+  }
+  if (lists && blockIdx.x == 0 && wave == 0 && a.row != nullptr) {
+    DxRule x = a.dx;
+    const long long room = live > 0 ? a.dx_room / live : 1;
+    x.most = room < 64 ? static_cast<int>(room) : 64;
+    const int parts = dx_parts(x, live > 0 ? live : 1, lane);
+    if (lane == 0) a.control[DX_PARTS] = parts;
   }
   if (lists && tid < 16 && first + tid < a.T) {
     const int t = first + tid;
@@ -168,6 +191,17 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   const size_t at = static_cast<size_t>(t < 0 ? 0 : t) * K;
   const int mine_K = r < n ? K : 0;
   const float tau = a.t.temperature;
+  if (K == 0) {                                          // every row has a target, its only item
+    if (l16 == 0 && r < n) {
+      a.target_row[first + r] = y;
+      if (a.row != nullptr) {
+        const float gl = a.dloss[t];
+        a.row[first + r] = f32x4_t{a.in_lse[t] * LOG2E, gl, 0.f, 0.f};
+        a.terms[first + r] = f32x4_t{expm1f(-a.in_loss[t]) * gl, 0.f, 0.f, 0.f};
+      }
+    }
+    return;
+  }
   float top = -__builtin_inff();
 #pragma unroll 4
   for (int j = l16; j < mine_K; j += 16) {
@@ -254,7 +288,8 @@ __device__ __forceinline__ float wave_max_of(float v) { return group_max<MOE_WAV
 
 struct HeadJoinArgs {
   const float* part;
-  const int32_t *control, *row_token, *target_slot;
+  const int32_t *control, *row_token, *target_slot, *target;   // control null: rows are tokens, all T of them
+  int T;
   const float* z_item;
   Teacher t;
   int strips, rows_cap, V;
@@ -268,7 +303,7 @@ template <int EPL>
 __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a) {
   __shared__ float part[4][JOIN_GROUPS][16];
   const int tid = threadIdx.x, lane = tid % MOE_WAVE;
-  const int first = blockIdx.x * 16, live = a.control[LIVE], K = a.t.K;
+  const int first = blockIdx.x * 16, live = a.control != nullptr ? a.control[LIVE] : a.T, K = a.t.K;
   const bool two = K > 0 && a.t.temperature != 1.f;
   if (first >= live) return;
   constexpr float NONE = -__builtin_inff(), LOW = -3.0e38f;
@@ -297,7 +332,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
     return s > 0.f ? __builtin_fmaf(top, LN2, logf(s)) : NONE;
   };
   const float rest1 = joined(0), rest2 = two ? joined(2) : rest1, tau = a.t.temperature;
-  const int t = a.row_token[row], slot = a.target_slot[row];
+  const int t = a.control != nullptr ? a.row_token[row] : row;
+  const int slot = K > 0 ? a.target_slot[row] : target_there(a.target[t], a.V) ? 0 : -1;
   const float* z = a.z_item + static_cast<size_t>(row) * (K + 1);
   const size_t at = static_cast<size_t>(t) * K;
   const float zy = slot >= 0 ? z[slot] : 0.f;
@@ -376,7 +412,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
 
 struct HeadDxArgs {
   const float* part;
-  int parts;
+  const int32_t* control;
   const int32_t *token_row, *target_slot, *target;
   const float* item;               // what dz lost at the items
   Teacher t;
@@ -402,7 +438,7 @@ __global__ __launch_bounds__(256) void head_dx_kernel(HeadDxArgs a) {
         v[k >> 1][2 * (k & 1) + 1] = __builtin_fmaf(e, bf16hi(w[k]), v[k >> 1][2 * (k & 1) + 1]);
       }
     };
-    const int slot = a.target_slot[row];
+    const int slot = K > 0 ? a.target_slot[row] : 0, parts = a.control[DX_PARTS], live = a.control[LIVE];
     if (slot >= 0) add(slot, a.target[t]);
     if (a.all) {
       for (int j = 0; j < K; ++j) {
@@ -411,8 +447,8 @@ __global__ __launch_bounds__(256) void head_dx_kernel(HeadDxArgs a) {
       }
     }
 #pragma unroll 4
-    for (int p = 0; p < a.parts; ++p) {
-      const float* q = a.part + (static_cast<size_t>(p) * a.T + row) * a.d + c;
+    for (int p = 0; p < parts; ++p) {
+      const float* q = a.part + (static_cast<size_t>(p) * live + row) * a.d + c;
       v[0] += *reinterpret_cast<const f32x4_t*>(q);
       v[1] += *reinterpret_cast<const f32x4_t*>(q + 4);
     }
@@ -447,11 +483,11 @@ template <int S> void head_parts(int T, int d, int cols, double& best, HeadShape
   const double tiles = static_cast<double>(ceil_div(T, S)) * ceil_div(d, S);
   const int steps = ceil_div(cols, BK);
   for (int p = 1; p <= 64 && (p == 1 || steps / p >= 4); ++p) {
-    // each part's sums are written and read: T d 8 bytes at some 4 bytes per compute unit and cycle
-    const double time = head_time<S>(tiles * p, static_cast<double>(steps) / p, TileCost<S>::FIXED) + p * (static_cast<double>(T) * d / 4.0e6);
+    const double time = head_time<S>(tiles * p, static_cast<double>(steps) / p, TileCost<S>::FIXED) + p * (static_cast<double>(T) * d / 4.0e6);   // as dx_parts
     if (time < best) { best = time; shape = {S, p}; }
   }
 }
+// The edge for all T tokens; the parts are chosen again for those that have a loss, in the room that this number leaves.
 HeadShape head_dx_shape(int T, int d, int cols) {
   HeadShape shape{128, 1};
   double best = 1e300;
@@ -469,7 +505,7 @@ int head_edge(int rows, int cols, int depth, double more256, double more128) {
 
 // What the workspace holds, by offset.
 struct HeadLayout {
-  size_t control, mask, row_token, token_row, target_slot, xc, list_start, items, terms, item, row, big;   // terms, row: of the backward pass
+  size_t control, mask, row_token, token_row, target_row, target_slot, xc, list_start, items, terms, item, row, big;   // terms, row: of the backward pass
   int strips64, blocks, slots, low;
 };
 HeadLayout head_layout(int T, int d, int V, int K, bool backward) {
@@ -485,11 +521,14 @@ HeadLayout head_layout(int T, int d, int V, int K, bool backward) {
   l.mask = take((n + 63) / 64 * 8);
   l.row_token = take(4 * n);
   l.token_row = take(4 * n);
+  l.target_row = take(4 * n);
   l.target_slot = take(4 * n);
   l.xc = take((l.low ? 4 : 2) * n * d);
-  l.list_start = take(static_cast<size_t>(l.blocks) * (l.strips64 + 1) * 4);
   const size_t items = static_cast<size_t>(l.blocks) * 16 * l.slots;
-  l.items = take(items * sizeof(HeadItem));
+  if (K > 0) {
+    l.list_start = take(static_cast<size_t>(l.blocks) * (l.strips64 + 1) * 4);
+    l.items = take(items * sizeof(HeadItem));
+  }
   l.item = take(n * l.slots * 4);
   if (backward) {
     l.terms = take(items * sizeof(f32x4_t));
@@ -514,7 +553,7 @@ struct HeadCall {
   hipStream_t s;
 };
 
-int run_prep(const HeadCall& c, const HeadLayout& l) {
+int run_prep(const HeadCall& c, const HeadLayout& l, const DxRule& dx, long long dx_room) {
   uint64_t* mask = nullptr;
   if (c.T > SELF_MASK_TOKENS || static_cast<long long>(c.T) * (c.t.K + 1) > SELF_MASK_LOADS) {
     mask = reinterpret_cast<uint64_t*>(c.ws + l.mask);
@@ -523,6 +562,8 @@ int run_prep(const HeadCall& c, const HeadLayout& l) {
   HeadPrepArgs p{};
   p.x = c.x; p.target = c.target; p.t = c.t; p.mask = mask; p.T = c.T; p.d = c.d; p.V = c.V; p.strips = l.strips64;
   p.low = l.low;
+  p.dx = dx; p.dx_room = dx_room;
+  p.target_row = reinterpret_cast<int32_t*>(c.ws + l.target_row);
   p.control = reinterpret_cast<int32_t*>(c.ws + l.control);
   p.row_token = reinterpret_cast<int32_t*>(c.ws + l.row_token);
   p.token_row = reinterpret_cast<int32_t*>(c.ws + l.token_row);
@@ -548,7 +589,8 @@ void fill_head(const HeadCall& c, const HeadLayout& l, GemmArgs& a, HeadArgs& h)
   a.offsets = control + ROWS;
   a.row_token = control + DIRECT;
   a.E = 1;
-  h.list_start = reinterpret_cast<const int32_t*>(c.ws + l.list_start);
+  h.target = reinterpret_cast<const int32_t*>(c.ws + l.target_row);
+  h.list_start = c.t.K > 0 ? reinterpret_cast<const int32_t*>(c.ws + l.list_start) : nullptr;
   h.items = reinterpret_cast<const HeadItem*>(c.ws + l.items);
   h.item = reinterpret_cast<float*>(c.ws + l.item);
   h.terms = reinterpret_cast<const f32x4_t*>(c.ws + l.terms);
@@ -564,25 +606,38 @@ void fill_head(const HeadCall& c, const HeadLayout& l, GemmArgs& a, HeadArgs& h)
 template <int MODE> int launch_head(GemmArgs& a, const HeadArgs& h, int edge, int rows, int cols, const char* name, hipStream_t s) {
   a.n_tiles = ceil_div(cols, edge);
   a.m_tiles_cap = ceil_div(rows, edge);
-  const long long tiles = static_cast<long long>(a.n_tiles) * a.m_tiles_cap * a.E;
+  const long long tiles = static_cast<long long>(a.n_tiles) * a.m_tiles_cap * (MODE == HEAD_DX ? 64 : 1);
   if (tiles > 0x7FFFFFFFll / 2) return MOE_ERR_INVALID;
   return edge == 128 ? launch_gemm_head<MODE, 128>(a, h, tiles, s, name) : launch_gemm_head<MODE, 256>(a, h, tiles, s, name);
 }
+// For tests: the edge of a launch's tiles on entry (0: the rule decides), the one that it ran with on return.
+int settle_edge(int* edge, int rule) {
+  if (edge == nullptr) return rule;
+  return *edge = *edge == 0 ? rule : *edge;
+}
 
-int run_head_fwd(const HeadCall& c) {
+int run_head_fwd(const HeadCall& c, int* edges) {
   const HeadLayout l = head_layout(c.T, c.d, c.V, c.t.K, false);
-  int rc = run_prep(c, l);
-  if (rc != MOE_OK) return rc;
   GemmArgs a{};
   HeadArgs h{};
   fill_head(c, l, a, h);
   a.A0 = reinterpret_cast<const uint16_t*>(c.ws + l.xc); a.A1 = c.x; a.B0 = c.W; a.K = c.d; a.N = c.V;
-  const int edge = head_edge(c.T, c.V, c.d, 6.0, 3.0);
+  // A few tokens cost the same with or without a loss, one pass over W: no kernel in front finds those that have one.
+  const bool all = c.t.K == 0 && c.T <= ALL_TOKENS;
+  int rc = MOE_OK;
+  if (all) {
+    a.offsets = nullptr; a.row_token = nullptr; a.A0 = c.x; a.M = c.T;
+    h.target = c.target;
+  } else if ((rc = run_prep(c, l, DxRule{}, 0)) != MOE_OK) {
+    return rc;
+  }
+  const int edge = settle_edge(edges, head_edge(c.T, c.V, c.d, 6.0, 3.0));
   h.strips = ceil_div(c.V, edge / 2);
   h.part = reinterpret_cast<float*>(c.ws + l.big);
   if ((rc = launch_head<HEAD_STATS>(a, h, edge, c.T, c.V, "gemm_head_stats", c.s)) != MOE_OK) return rc;
-  const HeadJoinArgs j{h.part, a.offsets, reinterpret_cast<const int32_t*>(c.ws + l.row_token), reinterpret_cast<const int32_t*>(c.ws + l.target_slot),
-                       h.item, c.t, h.strips, c.T, c.V, c.loss, c.lse, c.kd, c.lse_t, h.c1, h.c2};
+  const HeadJoinArgs j{h.part, all ? nullptr : reinterpret_cast<const int32_t*>(c.ws + l.control), reinterpret_cast<const int32_t*>(c.ws + l.row_token),
+                       reinterpret_cast<const int32_t*>(c.ws + l.target_slot), c.target, c.T, h.item, c.t, h.strips, c.T, c.V, c.loss, c.lse, c.kd, c.lse_t,
+                       h.c1, h.c2};
   const dim3 grid(l.blocks), block(JOIN_THREADS);
   if (c.t.K <= MOE_WAVE) MOE_LAUNCH("head_join", head_join_kernel<1>, grid, block, 0, c.s, j);
   else if (c.t.K <= 2 * MOE_WAVE) MOE_LAUNCH("head_join", head_join_kernel<2>, grid, block, 0, c.s, j);
@@ -590,16 +645,20 @@ int run_head_fwd(const HeadCall& c) {
   return moe_check_launch();
 }
 
-int run_head_bwd(const HeadCall& c, int v_piece) {
+int run_head_bwd(const HeadCall& c, int v_piece, int* edges) {
   const HeadLayout l = head_layout(c.T, c.d, c.V, c.t.K, true);
   const int piece = head_piece(c.T, c.V, v_piece);
   uint16_t* dz = reinterpret_cast<uint16_t*>(c.ws + l.big);
   float* part = reinterpret_cast<float*>(c.ws + l.big + head_dz_bytes(c.T, piece));
-  int rc = run_prep(c, l);
-  if (rc != MOE_OK) return rc;
   const HeadShape dxs = head_dx_shape(c.T, c.d, piece);
+  const int dx_edge = settle_edge(edges != nullptr ? edges + 1 : nullptr, dxs.edge);
+  // (the parts are those of all pieces: no more than the smallest, the last, has steps for)
+  const int last = c.V - (c.V - 1) / piece * piece;
+  const DxRule rule{dx_edge, HEAD_CUS * 256 / dx_edge, c.d, ceil_div(last, BK), 0, static_cast<float>(dx_edge == 256 ? TileCost<256>::FIXED : TileCost<128>::FIXED)};
+  int rc = run_prep(c, l, rule, static_cast<long long>(dxs.parts) * c.T);
+  if (rc != MOE_OK) return rc;
+  const int32_t* control = reinterpret_cast<const int32_t*>(c.ws + l.control);
   const int dw_rows = l.low ? 2 * c.T : c.T;
-  int parts = 0;
   for (int v0 = 0; v0 < c.V; v0 += piece) {
     const int cols = c.V - v0 < piece ? c.V - v0 : piece, ld = (cols + 63) & ~63;
     GemmArgs a{};
@@ -609,23 +668,21 @@ int run_head_bwd(const HeadCall& c, int v_piece) {
     h.lo = l.low;
     const uint16_t* W = c.W + static_cast<size_t>(v0) * c.d;
     a.A0 = reinterpret_cast<const uint16_t*>(c.ws + l.xc); a.A1 = c.x; a.B0 = W; a.O0 = dz; a.K = c.d; a.N = cols; a.M = ld;
-    rc = launch_head<HEAD_DZ>(a, h, head_edge(c.T, cols, c.d, 6.0, 3.0), c.T, cols, "gemm_head_dz", c.s);
+    rc = launch_head<HEAD_DZ>(a, h, settle_edge(edges, head_edge(c.T, cols, c.d, 6.0, 3.0)), c.T, cols, "gemm_head_dz", c.s);
     if (rc != MOE_OK) return rc;
     GemmArgs b{};
-    b.offsets = a.offsets;
+    b.offsets = a.offsets; b.row_token = control + DX_PARTS;
     b.A0 = dz; b.B0 = W; b.O0 = reinterpret_cast<uint16_t*>(part); b.K = ld; b.M = cols; b.N = c.d;
-    b.E = dxs.parts < ld / 64 ? dxs.parts : ld / 64;
-    if (v0 == 0) parts = b.E;
     h.add = v0 > 0;
-    if ((rc = launch_head<HEAD_DX>(b, h, dxs.edge, c.T, c.d, "gemm_head_dx", c.s)) != MOE_OK) return rc;
+    if ((rc = launch_head<HEAD_DX>(b, h, dx_edge, c.T, c.d, "gemm_head_dx", c.s)) != MOE_OK) return rc;
     GemmArgs w{};
-    w.offsets = reinterpret_cast<const int32_t*>(c.ws + l.control) + DW_ROWS - 1; w.E = 1; w.row_token = a.row_token;
+    w.offsets = control + DW_ROWS - 1; w.E = 1; w.row_token = a.row_token;
     w.A0 = dz; w.B0 = a.A0; w.B1 = a.A1; w.O0 = c.dW + static_cast<size_t>(v0) * c.d; w.M = ld; w.K = cols; w.N = c.d;
-    rc = launch_head<HEAD_DW>(w, h, head_edge(cols, c.d, dw_rows, 0.8, 1.1), cols, c.d, "gemm_head_dw", c.s);
+    rc = launch_head<HEAD_DW>(w, h, settle_edge(edges != nullptr ? edges + 2 : nullptr, head_edge(cols, c.d, dw_rows, 0.8, 1.1)), cols, c.d, "gemm_head_dw", c.s);
     if (rc != MOE_OK) return rc;
   }
   const size_t n = static_cast<size_t>(c.T) * (c.d / 8);
-  const HeadDxArgs x{part, parts, reinterpret_cast<const int32_t*>(c.ws + l.token_row), reinterpret_cast<const int32_t*>(c.ws + l.target_slot), c.target,
+  const HeadDxArgs x{part, control, reinterpret_cast<const int32_t*>(c.ws + l.token_row), reinterpret_cast<const int32_t*>(c.ws + l.target_slot), c.target,
                      reinterpret_cast<const float*>(c.ws + l.item), c.t, c.W, c.T, c.d, c.V, c.T <= LOW_TOKENS, c.dx};
   MOE_LAUNCH("head_dx", head_dx_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, c.s, x);
   return moe_check_launch();
@@ -650,52 +707,61 @@ extern "C" size_t moe_head_bwd_workspace_bytes(int T, int d, int V, int K, int v
   return head_layout(T, d, V, K, true).big + head_dz_bytes(T, piece) + static_cast<size_t>(head_dx_shape(T, d, piece).parts) * T * d * sizeof(float);
 }
 
-extern "C" int moe_head_ce_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, int T, int d, int V, float* loss, float* lse,
-                               void* ws, size_t ws_bytes, void* stream) {
-  if (bad_head_dims(T, d, V, 0) || bad_ptrs({x, W, target, loss, lse, ws})) return MOE_ERR_INVALID;
-  if (ws_bytes < moe_head_fwd_workspace_bytes(T, d, V, 0)) return MOE_ERR_WORKSPACE;
-  HeadCall c{};
-  c.x = x; c.W = W; c.target = target; c.t = {nullptr, nullptr, 1.f, 0}; c.T = T; c.d = d; c.V = V; c.loss = loss; c.lse = lse;
-  c.ws = static_cast<char*>(ws); c.s = static_cast<hipStream_t>(stream);
-  return run_head_fwd(c);
+// Both losses, or (ids null, K 0) the cross entropy alone: what the calls of moe_hotpath.h come to.  edges, for tests: as in gemm.h, of the
+// logits' launch, then (backward) of dx and dW.
+namespace {
+bool bad_edge_list(const int* edges, int n) {
+  for (int i = 0; edges != nullptr && i < n; ++i) if (edges[i] != 0 && edges[i] != 128 && edges[i] != 256) return true;
+  return false;
 }
-
-extern "C" int moe_head_ce_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, const float* loss, const float* lse,
-                               const float* dloss, int T, int d, int V, int v_piece, moe_bf16* dx, moe_bf16* dW, void* ws, size_t ws_bytes,
-                               void* stream) {
-  if (bad_head_dims(T, d, V, 0) || v_piece < 0 || v_piece % 256 != 0) return MOE_ERR_INVALID;
-  if (bad_ptrs({x, W, target, loss, lse, dloss, dx, dW, ws})) return MOE_ERR_INVALID;
-  if (ws_bytes < moe_head_bwd_workspace_bytes(T, d, V, 0, v_piece)) return MOE_ERR_WORKSPACE;
-  HeadCall c{};
-  c.x = x; c.W = W; c.target = target; c.t = {nullptr, nullptr, 1.f, 0}; c.T = T; c.d = d; c.V = V;
-  c.in_loss = loss; c.in_lse = lse; c.dloss = dloss; c.dx = dx; c.dW = dW;
-  c.ws = static_cast<char*>(ws); c.s = static_cast<hipStream_t>(stream);
-  return run_head_bwd(c, v_piece);
-}
-
-extern "C" int moe_head_distill_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, const int32_t* ids, const float* teacher,
-                                    float temperature, int T, int d, int V, int K, float* loss, float* lse, float* kd, float* lse_t, void* ws,
-                                    size_t ws_bytes, void* stream) {
-  if (bad_head_dims(T, d, V, K) || K == 0 || bad_temperature(temperature)) return MOE_ERR_INVALID;
-  if (bad_ptrs({x, W, target, ids, teacher, loss, lse, kd, lse_t, ws})) return MOE_ERR_INVALID;
+}  // namespace
+extern "C" int moe_head_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, const int32_t* ids, const float* teacher, float temperature,
+                            int T, int d, int V, int K, float* loss, float* lse, float* kd, float* lse_t, void* ws, size_t ws_bytes, void* stream,
+                            int* edges) {
+  if (bad_head_dims(T, d, V, K) || bad_temperature(temperature) || bad_edge_list(edges, 1)) return MOE_ERR_INVALID;
+  if (bad_ptrs({x, W, target, loss, lse, ws}) || (K > 0 && bad_ptrs({ids, teacher, kd, lse_t}))) return MOE_ERR_INVALID;
   if (ws_bytes < moe_head_fwd_workspace_bytes(T, d, V, K)) return MOE_ERR_WORKSPACE;
   HeadCall c{};
   c.x = x; c.W = W; c.target = target; c.t = {ids, teacher, temperature, K}; c.T = T; c.d = d; c.V = V;
   c.loss = loss; c.lse = lse; c.kd = kd; c.lse_t = lse_t;
   c.ws = static_cast<char*>(ws); c.s = static_cast<hipStream_t>(stream);
-  return run_head_fwd(c);
+  return run_head_fwd(c, edges);
+}
+extern "C" int moe_head_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, const int32_t* ids, const float* teacher, float temperature,
+                            const float* loss, const float* lse, const float* lse_t, const float* dloss, const float* dkd, int T, int d, int V, int K,
+                            int v_piece, moe_bf16* dx, moe_bf16* dW, void* ws, size_t ws_bytes, void* stream, int* edges) {
+  if (bad_head_dims(T, d, V, K) || bad_temperature(temperature) || v_piece < 0 || v_piece % 256 != 0 || bad_edge_list(edges, 3)) return MOE_ERR_INVALID;
+  if (bad_ptrs({x, W, target, loss, lse, dloss, dx, dW, ws}) || (K > 0 && bad_ptrs({ids, teacher, lse_t, dkd}))) return MOE_ERR_INVALID;
+  if (ws_bytes < moe_head_bwd_workspace_bytes(T, d, V, K, v_piece)) return MOE_ERR_WORKSPACE;
+  HeadCall c{};
+  c.x = x; c.W = W; c.target = target; c.t = {ids, teacher, temperature, K}; c.T = T; c.d = d; c.V = V;
+  c.in_loss = loss; c.in_lse = lse; c.in_lse_t = lse_t; c.dloss = dloss; c.dkd = dkd; c.dx = dx; c.dW = dW;
+  c.ws = static_cast<char*>(ws); c.s = static_cast<hipStream_t>(stream);
+  return run_head_bwd(c, v_piece, edges);
+}
+
+extern "C" int moe_head_ce_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, int T, int d, int V, float* loss, float* lse,
+                               void* ws, size_t ws_bytes, void* stream) {
+  return moe_head_fwd(x, W, target, nullptr, nullptr, 1.f, T, d, V, 0, loss, lse, nullptr, nullptr, ws, ws_bytes, stream, nullptr);
+}
+
+extern "C" int moe_head_ce_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, const float* loss, const float* lse,
+                               const float* dloss, int T, int d, int V, int v_piece, moe_bf16* dx, moe_bf16* dW, void* ws, size_t ws_bytes,
+                               void* stream) {
+  return moe_head_bwd(x, W, target, nullptr, nullptr, 1.f, loss, lse, nullptr, dloss, nullptr, T, d, V, 0, v_piece, dx, dW, ws, ws_bytes, stream, nullptr);
+}
+
+extern "C" int moe_head_distill_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, const int32_t* ids, const float* teacher,
+                                    float temperature, int T, int d, int V, int K, float* loss, float* lse, float* kd, float* lse_t, void* ws,
+                                    size_t ws_bytes, void* stream) {
+  if (K <= 0) return MOE_ERR_INVALID;
+  return moe_head_fwd(x, W, target, ids, teacher, temperature, T, d, V, K, loss, lse, kd, lse_t, ws, ws_bytes, stream, nullptr);
 }
 
 extern "C" int moe_head_distill_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, const int32_t* ids, const float* teacher,
                                     float temperature, const float* loss, const float* lse, const float* lse_t, const float* dloss,
                                     const float* dkd, int T, int d, int V, int K, int v_piece, moe_bf16* dx, moe_bf16* dW, void* ws,
                                     size_t ws_bytes, void* stream) {
-  if (bad_head_dims(T, d, V, K) || K == 0 || bad_temperature(temperature) || v_piece < 0 || v_piece % 256 != 0) return MOE_ERR_INVALID;
-  if (bad_ptrs({x, W, target, ids, teacher, loss, lse, lse_t, dloss, dkd, dx, dW, ws})) return MOE_ERR_INVALID;
-  if (ws_bytes < moe_head_bwd_workspace_bytes(T, d, V, K, v_piece)) return MOE_ERR_WORKSPACE;
-  HeadCall c{};
-  c.x = x; c.W = W; c.target = target; c.t = {ids, teacher, temperature, K}; c.T = T; c.d = d; c.V = V;
-  c.in_loss = loss; c.in_lse = lse; c.in_lse_t = lse_t; c.dloss = dloss; c.dkd = dkd; c.dx = dx; c.dW = dW;
-  c.ws = static_cast<char*>(ws); c.s = static_cast<hipStream_t>(stream);
-  return run_head_bwd(c, v_piece);
+  if (K <= 0) return MOE_ERR_INVALID;
+  return moe_head_bwd(x, W, target, ids, teacher, temperature, loss, lse, lse_t, dloss, dkd, T, d, V, K, v_piece, dx, dW, ws, ws_bytes, stream, nullptr);
 }

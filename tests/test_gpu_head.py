@@ -64,6 +64,30 @@ def run(a, tau=1.0, v_piece=0, train=True, junk=0xAB):
     return out
 
 
+def run_at_edge(a, edge, tau=1.0, v_piece=0):
+    """Both directions with the tiles of every product at one edge, whatever the rule would take."""
+    import ctypes
+    lib = B.load()
+    P, I, F = ctypes.c_void_p, ctypes.c_int, ctypes.c_float
+    lib.moe_head_fwd.argtypes = [P] * 5 + [F] + [I] * 4 + [P] * 5 + [ctypes.c_size_t, P, P]
+    lib.moe_head_bwd.argtypes = [P] * 5 + [F] + [P] * 5 + [I] * 5 + [P] * 3 + [ctypes.c_size_t, P, P]
+    t = {k: v.to(DEV) for k, v in a.items()}
+    (T, d), V, K = a["x"].shape, a["W"].shape[0], a["ids"].shape[1] if "ids" in a else 0
+    n = max(B.moe_head_fwd_workspace_bytes(T, d, V, K), B.moe_head_bwd_workspace_bytes(T, d, V, K, v_piece))
+    ws = torch.full((n,), 0xAB, dtype=torch.uint8, device=DEV)
+    out = {k: torch.full((T,), 7.0, device=DEV) for k in ["loss", "lse"] + (["kd", "lse_t"] if K else [])}
+    out.update(dx=torch.empty(T, d, dtype=BF, device=DEV), dW=torch.empty(V, d, dtype=BF, device=DEV))
+    p = lambda o, k: o[k].data_ptr() if k in o else None  # noqa: E731
+    head = [p(t, "x"), p(t, "W"), p(t, "target"), p(t, "ids"), p(t, "teacher"), tau]
+    stream = torch.cuda.current_stream().cuda_stream
+    fwd, bwd = (ctypes.c_int * 1)(edge), (ctypes.c_int * 3)(edge, edge, edge)
+    assert lib.moe_head_fwd(*head, T, d, V, K, *[p(out, k) for k in ("loss", "lse", "kd", "lse_t")], ws.data_ptr(), n, stream, ctypes.addressof(fwd)) == 0
+    assert lib.moe_head_bwd(*head, *[p(out, k) for k in ("loss", "lse", "lse_t")], p(t, "dloss"), p(t, "dkd"), T, d, V, K, v_piece, p(out, "dx"),
+                            p(out, "dW"), ws.data_ptr(), n, stream, ctypes.addressof(bwd)) == 0
+    assert list(fwd) == [edge] and list(bwd) == [edge] * 3
+    return out
+
+
 def compare(a, got, tau=1.0):
     train = "dx" in got
     want, bound = R.head(a["x"], a["W"], a["target"], a.get("ids"), a.get("teacher"), tau, a["dloss"] if train else None, a.get("dkd"))
@@ -105,6 +129,21 @@ def test_distillation(T, d, V, K, tau):
     print("distillation", T, d, V, K, tau, flush=True)
     a = make(T, d, V, K, masked=0.2 if T > 2 else 0.0)
     compare(a, run(a, tau), tau)
+
+
+@pytest.mark.parametrize("edge", [128, 256])
+@pytest.mark.parametrize("T,d,V,K,masked", [(1, 64, 1, 0, 0), (1, 192, 700, 0, 0), (17, 128, 129, 20, 0.2), (64, 64, 257, 0, 0), (65, 128, 5000, 3, 0), (128, 256, 640, 0, 0.5),
+                                            (129, 64, 1031, 64, 0), (250, 128, 300, 100, 0.1), (256, 64, 256, 0, 0), (300, 320, 513, 33, 0.3), (600, 64, 3001, 0, 0.6),
+                                            (520, 64, 200, 128, 0)])
+def test_both_tile_edges(T, d, V, K, masked, edge):
+    print("edge", edge, T, d, V, K, masked, flush=True)
+    a = make(T, d, V, K, masked=masked, seed=15)
+    if masked:
+        a["target"][0] = 0                               # not all without a loss
+    tau = 1.3 if K % 2 else 1.0
+    compare(a, run_at_edge(a, edge, tau), tau)
+    if V > 512:
+        compare(a, run_at_edge(a, edge, tau, v_piece=512), tau)
 
 
 def test_targets_and_entries_come_and_go_apart():
