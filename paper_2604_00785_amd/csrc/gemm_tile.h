@@ -108,7 +108,8 @@ enum GemmMode { GATE_UP = 0, DOWN = 1, DGRAD_H = 2, DGRAD_X = 3, WGRAD = 4, WGRA
 // row's partial dot product with h = silu(g) u (the gradient of the gate weight).
 // The vocabulary head (head.hip), rows offsets[0] = 0 to offsets[1], one group.  HEAD_STATS, HEAD_DZ: logits A0 . B0^T of which the
 // epilogue makes a row's maximum and sums over the wave's columns, or the logits' gradient (row length M).  HEAD_DX: A0 (row length K) times
-// B0 in row_token[0] parts of the reduction over its M rows, each part's sums in 32 bits.  HEAD_DW: WGRAD with rows of M elements, K of them wanted.
+// B0 in row_token[0] parts of the reduction over its M rows, each part's sums in 32 bits.  HEAD_DW: WGRAD with rows of M elements, K of them
+// wanted, in E parts of the reduction; with more than one O1 takes each part's sums in 32 bits.
 constexpr bool is_logits(int mode) { return mode == HEAD_STATS || mode == HEAD_DZ; }
 constexpr bool is_wgrad(int mode) { return mode == WGRAD || mode == WGRAD_GATHER || mode == WGRAD_GATHER_A || mode == HEAD_DW; }
 constexpr bool is_dgrad_h(int mode) { return mode == DGRAD_H || mode == DGRAD_H_GATE; }
@@ -370,7 +371,7 @@ struct TileState {
   int tokn[Tile<S>::NL];        // gathered operand: tokens of the lane's reduction rows of a coming step
   const char* sa_next;          // scalar bases of the next A / B tile to load (LOAD_BIAS low)
   const char* sb_next;
-  const char* sa_phase1;        // DGRAD_X: bases of the second K phase
+  const char* sa_phase1;        // DGRAD_X, and logits of few rows: bases of the second K phase
   const char* sb_phase1;
   size_t a_step, b_step;        // bytes per step
   const int32_t* row_tok;       // gathered operand: token of the expert's first reduction row onwards
@@ -455,7 +456,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
     // rows and 4 (or 8) of columns; all rows of a column tile in a run would have every XCD fetch all rows in every round.
     m_end = head_rows();
     rt = (m_end + S - 1) / S;
-    const int band = tile / (8 * a.n_tiles), in = tile - band * 8 * a.n_tiles;
+        const int band = tile / (8 * a.n_tiles), in = tile - band * 8 * a.n_tiles;
     const int high = rt - band * 8 < 8 ? rt - band * 8 : 8;
     nt = in / high;
     m0 = (band * 8 + in - nt * high) * S;
@@ -519,8 +520,15 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
   int nk, nk_phase;                     // steps in total / in the first K phase
 
   if constexpr (is_wgrad(MODE)) {
-    k_lo = __builtin_amdgcn_readfirstlane(a.offsets[e]);
-    k_hi = __builtin_amdgcn_readfirstlane(a.offsets[e + 1]);
+    if constexpr (MODE == HEAD_DW) {
+      const int all = a.offsets[1], steps = (all + BK - 1) / BK;
+      k_lo = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<long long>(steps) * e / a.E)) * BK;
+      k_hi = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<long long>(steps) * (e + 1) / a.E)) * BK;
+      k_hi = k_hi > all ? all : k_hi;
+    } else {
+      k_lo = __builtin_amdgcn_readfirstlane(a.offsets[e]);
+      k_hi = __builtin_amdgcn_readfirstlane(a.offsets[e + 1]);
+    }
     nk = (k_hi - k_lo + BK - 1) / BK;
     nk_phase = nk;
     if constexpr (GATHER_A) {
@@ -627,6 +635,17 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
   t.sb_phase1 = nullptr;
   if constexpr (MODE == DGRAD_X) { t.sa_phase1 = scalarize(abase + a_phase - LOAD_BIAS); t.sb_phase1 = scalarize(bbase + b_phase - LOAD_BIAS); }
   t.a_step = a_step; t.b_step = b_step; t.k_lo = k_lo; t.k_hi = k_hi; t.row_tok = row_tok; t.nk = nk; t.nk_phase = nk_phase;
+  if constexpr (is_logits(MODE)) {
+    // A tile with few rows waits for memory.  Where weight rows are multiples of 4096 bytes, tiles that run in step read the same few bytes of each,
+    // which lie in a fraction of the channels: they begin their reductions at different steps (57 tokens of d 4096, V 32003: 63 -> 48.5 us; with many
+    // rows it costs 1 %).
+    if (t.few) {
+      const int rot = __builtin_amdgcn_readfirstlane(nt * 3 % nk);
+      t.sa_phase1 = t.sa_next; t.sb_phase1 = t.sb_next;
+      t.sa_next += rot * BK * 2; t.sb_next += rot * BK * 2;
+      t.nk_phase = nk - rot;
+    }
+  }
   t.last_partial = (is_wgrad(MODE) || MODE == HEAD_DX) && ((k_hi - k_lo) % BK) != 0;
   // The last three steps of a tile are copies of their own: the last step that loads (it loads the tile's last
   // step, the one that may be partial in a weight gradient), the step that only awaits, and the last one.
@@ -676,13 +695,13 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
   };
   auto a_end = [&](TileState& t, int kt) __attribute__((always_inline)) {
     t.sa_next += t.a_step;
-    if constexpr (MODE == DGRAD_X) {
+    if constexpr (MODE == DGRAD_X || is_logits(MODE)) {
       if (kt + 1 == t.nk_phase) t.sa_next = t.sa_phase1;
     }
   };
   auto b_end = [&](TileState& t, int kt) __attribute__((always_inline)) {
     t.sb_next += t.b_step;
-    if constexpr (MODE == DGRAD_X) {
+    if constexpr (MODE == DGRAD_X || is_logits(MODE)) {
       if (kt + 1 == t.nk_phase) t.sb_next = t.sb_phase1;
     }
   };
@@ -1539,11 +1558,13 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
         u32x4 v4[PASSES];
         const int gc = gcol0 + lane % RP * 8;
         const int off = gc < ld ? (lane / RP * ld + gc) * 2 : PAST;
-        auto store_part = [&](int part, const f32x4_t (&v)[NB], Rsrc out) __attribute__((always_inline)) {
+        auto stage_part = [&](const f32x4_t (&v)[NB]) __attribute__((always_inline)) {
           static_for<NB>([&](auto j) { put_quad(l16, decltype(j)::value, v[decltype(j)::value]); });
           __builtin_amdgcn_wave_barrier();
           read_staged(v4, stage, IC<RB>{}, IC<PASSES>{}, IC<0>{}, IC<RP>{});
           __builtin_amdgcn_wave_barrier();
+        };
+        auto store_part = [&](int part, Rsrc out) __attribute__((always_inline)) {
 #pragma unroll
           for (int k = 0; k < PASSES; ++k)
             __builtin_amdgcn_raw_buffer_store_b128(v4[k], out, off + (part * 16 + k * (64 / RP)) * ld * 2, 0, 0);
@@ -1587,21 +1608,26 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
             });
           }
           mask(v, 0.f);
-          store_part(i, v, oo);
+          if constexpr (i > 0) { if (!lows) store_part(i - 1, oo); }     // behind the arithmetic of the part after it, as above
+          stage_part(v);
           if (lows) {
+            store_part(i, oo);
             static_for<NB>([&](auto j) {
 #pragma unroll
               for (int c = 0; c < 4; ++c) v[decltype(j)::value][c] -= rounded(v[decltype(j)::value][c]);
             });
-            store_part(i, v, ol);
+            stage_part(v);
+            store_part(i, ol);
           }
         });
+        if (!lows && rows > 0) store_part((rows - 1) >> 4, oo);
       }
-    } else if constexpr (MODE == HEAD_DX) {
-      const HeadPtr he = head_args();
-      float* const out = reinterpret_cast<float*>(ae->O0) + static_cast<size_t>(t.e) * ae->offsets[1] * ncol;   // as many rows as there are
+    } else if (MODE == HEAD_DX || (MODE == HEAD_DW && ae->E > 1)) {
+      // a part's sums in 32 bits, behind those of the parts before it
+      float* const out = reinterpret_cast<float*>(MODE == HEAD_DX ? ae->O0 : ae->O1) + static_cast<size_t>(t.e) * (MODE == HEAD_DX ? ae->offsets[1] : ae->K) * ncol;
       const Rsrc oo = rows_of(out, ncol * 4);
-      const bool add = he->add != 0;
+      bool add = false;
+      if constexpr (MODE == HEAD_DX) add = head_args()->add != 0;
       static_for<NB>([&](auto i_tag) {
         constexpr int i = decltype(i_tag)::value;
         if (i * 16 >= rows) return;
@@ -1616,7 +1642,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
       });
     } else {
       uint16_t* out = t.second ? ae->O1 : ae->O0;
-      if constexpr (is_wgrad(MODE)) out += static_cast<size_t>(t.e) * ae->M * ncol;
+      if constexpr (is_wgrad(MODE) && MODE != HEAD_DW) out += static_cast<size_t>(t.e) * ae->M * ncol;
       const Rsrc oo = rows_of(out, ncol * 2);
       constexpr int PASSES = 32 * RP / 64;
       u32x4 v[PASSES];

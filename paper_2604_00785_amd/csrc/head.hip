@@ -51,11 +51,11 @@ enum { ROWS = 0, LIVE = 1, DW_ROWS = 3, DIRECT = 4, DX_PARTS = 5, CONTROL_INTS =
 // Parts of dx's reduction for `rows` rows, at most `most`: with few tiles a part each to as many compute units as there are.  The time expected of p parts,
 // in K steps of the tile: whole rounds of the chip's places (half of it by the rounds, half by what they hold, since idle units leave the others
 // power), what a tile costs beside its steps, and each part's sums written and read.  Lane p - 1 of a wave weighs p parts.
-struct DxRule { int edge, places, d, steps, most; float fixed; };
+struct DxRule { int edge, places, d, steps, most; float fixed, step; };
 __device__ __forceinline__ int dx_parts(const DxRule& x, int rows, int lane) {
   const int p = lane + 1;
   const float tiles = static_cast<float>((rows + x.edge - 1) / x.edge) * ((x.d + x.edge - 1) / x.edge) * p, rounds = tiles / x.places;
-  const float time = 0.5f * (rounds + fmaxf(1.f, floorf(rounds + 0.95f))) * (x.fixed + static_cast<float>(x.steps) / p) + p * (static_cast<float>(rows) * x.d / 4.0e6f);
+  const float time = 0.5f * (rounds + fmaxf(1.f, floorf(rounds + 0.95f))) * (x.fixed + x.step * x.steps / p) + p * (static_cast<float>(rows) * x.d / 1.0e6f);
   const uint32_t key = p <= x.most && (p == 1 || x.steps / p >= 4) ? __float_as_uint(time) & ~63u | static_cast<uint32_t>(lane) : ~0u;
   return 1 + (group_reduce<MOE_WAVE>(key, [](uint32_t u, uint32_t v) __attribute__((always_inline)) { return u < v ? u : v; }) & 63u);
 }
@@ -92,11 +92,17 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   const bool lists = blockIdx.y == 0;
   const uint64_t* mask = a.mask;
   if (mask == nullptr) {
-#pragma unroll 4
-    for (int w = wave; w < words; w += 4) {
-      const int t = w * 64 + lane;
-      const uint64_t bits = __ballot(t < a.T && target_there(a.target[t], V));
-      if (lane == 0) own[w] = bits;
+    constexpr int WORDS = SELF_MASK_TOKENS / 256;        // of a wave, requested together
+    int y[WORDS];
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      const int t = (wave + 4 * i) * 64 + lane;
+      y[i] = t < a.T ? a.target[t] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      const uint64_t bits = __ballot(target_there(y[i], V));
+      if (lane == 0) own[wave + 4 * i] = bits;
     }
     if (K > 0) {
       __syncthreads();
@@ -166,6 +172,13 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   }
   __syncthreads();
   const int n = live - first < 16 ? live - first : 16;
+  const int r = tid >> 4, l16 = tid & 15, y = s_target[r], t = s_token[r];
+  const bool has = r < n && target_there(y, V);
+  float in_loss = 0.f, in_lse = 0.f, in_lse_t = 0.f, gl = 0.f, in_dkd = 0.f;      // requested ahead of the rows
+  if (a.row != nullptr && lists && r < n) {
+    in_loss = a.in_loss[t]; in_lse = a.in_lse[t]; gl = has ? a.dloss[t] : 0.f;
+    if (K > 0) { in_lse_t = a.in_lse_t[t]; in_dkd = a.dkd[t]; }
+  }
   if (!direct) {
     typedef __attribute__((ext_vector_type(4))) uint32_t u4;
     const int pieces = a.d / 8, all = n * pieces, step = 256 * gridDim.y;
@@ -173,8 +186,8 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
       u4 v[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const int i = i0 + k * step, j = i < all ? i : i0, r = j / pieces;
-        v[k] = *reinterpret_cast<const u4*>(a.x + static_cast<size_t>(s_token[r]) * a.d + (j - r * pieces) * 8);
+        const int i = i0 + k * step, j = i < all ? i : i0, row = j / pieces;
+        v[k] = *reinterpret_cast<const u4*>(a.x + static_cast<size_t>(s_token[row]) * a.d + (j - row * pieces) * 8);
       }
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -187,7 +200,6 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     }
   }
   if (!lists) return;
-  const int r = tid >> 4, l16 = tid & 15, y = s_target[r], t = s_token[r];
   const size_t at = static_cast<size_t>(t < 0 ? 0 : t) * K;
   const int mine_K = r < n ? K : 0;
   const float tau = a.t.temperature;
@@ -195,9 +207,8 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     if (l16 == 0 && r < n) {
       a.target_row[first + r] = y;
       if (a.row != nullptr) {
-        const float gl = a.dloss[t];
-        a.row[first + r] = f32x4_t{a.in_lse[t] * LOG2E, gl, 0.f, 0.f};
-        a.terms[first + r] = f32x4_t{expm1f(-a.in_loss[t]) * gl, 0.f, 0.f, 0.f};
+        a.row[first + r] = f32x4_t{in_lse * LOG2E, gl, 0.f, 0.f};
+        a.terms[first + r] = f32x4_t{expm1f(-in_loss) * gl, 0.f, 0.f, 0.f};
       }
     }
     return;
@@ -213,7 +224,7 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     atomicAdd(&count[id >> 6], 1);
   }
   top = group_max<16>(top);
-  const bool taught = top > -__builtin_inff(), has = r < n && target_there(y, V);
+  const bool taught = top > -__builtin_inff();
   __syncthreads();
   const bool own_target = l16 == 0 && has && s_slot[r] == K;
   if (own_target) atomicAdd(&count[y >> 6], 1);
@@ -245,7 +256,7 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   };
   // The gradient at the target and at the entries, where it is no plain softmax: p - 1 = exp(-loss) - 1 at the target; p - q = q (exp(log p - log q) - 1)
   // at an entry.  What does not depend on the logit is put down here.
-  float lq = 0.f, lt = 0.f, gk = 0.f, gl = 0.f, at_target = 0.f;
+  float lq = 0.f, lt = 0.f, gk = 0.f, at_target = 0.f;
   if (a.terms != nullptr && r < n) {
     if (taught) {
       float e = 0.f;
@@ -254,17 +265,14 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
         if (entry_there(a.t.ids[at + j], l, V)) e += expf(l / tau - top);
       }
       lq = top + logf(group_sum<16>(e));
-      lt = a.in_lse_t[t];
-      gk = a.dkd[t] / tau;
+      lt = in_lse_t;
+      gk = in_dkd / tau;
     }
-    if (has) {
-      gl = a.dloss[t];
-      at_target = expm1f(-a.in_loss[t]) * gl;
-    }
+    if (has) at_target = expm1f(-in_loss) * gl;
     if (l16 == 0) {
       const float none = __builtin_inff();
       f32x4_t p = {none, 0.f, none, 0.f};
-      if (has) { p[0] = a.in_lse[t] * LOG2E; p[1] = gl; }
+      if (has) { p[0] = in_lse * LOG2E; p[1] = gl; }
       if (taught) {
         if (tau != 1.f) { p[2] = lt * LOG2E; p[3] = gk; }
         else { if (!has) p[0] = lt * LOG2E; p[1] += gk; }             // one exponential serves both
@@ -410,6 +418,11 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
   }
 }
 
+__device__ __forceinline__ void store8(moe_bf16* to, const f32x4_t (&v)[2]) {
+  typedef __attribute__((ext_vector_type(4))) uint32_t u4;
+  *reinterpret_cast<u4*>(to) = u4{pack_bf16(v[0][0], v[0][1]), pack_bf16(v[0][2], v[0][3]), pack_bf16(v[1][0], v[1][1]), pack_bf16(v[1][2], v[1][3])};
+}
+
 struct HeadDxArgs {
   const float* part;
   const int32_t* control;
@@ -419,10 +432,27 @@ struct HeadDxArgs {
   const moe_bf16* W;
   int T, d, V, all;                // all: of every item, else of the target
   moe_bf16* dx;
+  const float* dw_part;            // dW's sums, [dw_parts][V][d], if they are in parts
+  int dw_parts, dx_groups;         // workgroups from dx_groups on are for them
+  moe_bf16* dW;
 };
-// dx of a token: the parts' sums in their order and what rounding dz took from them where it is largest, rounded once; zeros without a loss.
+// dx of a token: the parts' sums in their order and what rounding dz took from them where it is largest, rounded once; zeros without a loss.  And dW
+// likewise, where its reduction over the tokens is in parts.
 __global__ __launch_bounds__(256) void head_dx_kernel(HeadDxArgs a) {
   const int pieces = a.d / 8, K = a.t.K;
+  if (static_cast<int>(blockIdx.x) >= a.dx_groups) {
+    const size_t i = static_cast<size_t>(blockIdx.x - a.dx_groups) * 256 + threadIdx.x, n = static_cast<size_t>(a.V) * pieces;
+    if (i >= n) return;
+    f32x4_t v[2] = {};
+#pragma unroll 4
+    for (int p = 0; p < a.dw_parts; ++p) {
+      const float* q = a.dw_part + (p * n + i) * 8;
+      v[0] += *reinterpret_cast<const f32x4_t*>(q);
+      v[1] += *reinterpret_cast<const f32x4_t*>(q + 4);
+    }
+    store8(a.dW + i * 8, v);
+    return;
+  }
   const size_t i = static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x;
   if (i >= static_cast<size_t>(a.T) * pieces) return;
   const int t = static_cast<int>(i / pieces), c = static_cast<int>(i - static_cast<size_t>(t) * pieces) * 8, row = a.token_row[t];
@@ -453,8 +483,7 @@ __global__ __launch_bounds__(256) void head_dx_kernel(HeadDxArgs a) {
       v[1] += *reinterpret_cast<const f32x4_t*>(q + 4);
     }
   }
-  *reinterpret_cast<u4*>(a.dx + static_cast<size_t>(t) * a.d + c) =
-      u4{pack_bf16(v[0][0], v[0][1]), pack_bf16(v[0][2], v[0][3]), pack_bf16(v[1][0], v[1][1]), pack_bf16(v[1][2], v[1][3])};
+  store8(a.dx + static_cast<size_t>(t) * a.d + c, v);
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------------------
@@ -479,20 +508,33 @@ template <int S> double head_time(double tiles, double steps, double fixed) {
   return (0.5 * rounds + 0.5 * (whole < 1.0 ? 1.0 : whole)) * each;
 }
 struct HeadShape { int edge, parts; };
-template <int S> void head_parts(int T, int d, int cols, double& best, HeadShape& shape) {
-  const double tiles = static_cast<double>(ceil_div(T, S)) * ceil_div(d, S);
-  const int steps = ceil_div(cols, BK);
+template <int S> void head_parts(int rows, int d, int depth, double more, double& best, HeadShape& shape) {
+  const double tiles = static_cast<double>(ceil_div(rows, S)) * ceil_div(d, S);
+  const int steps = ceil_div(depth, BK);
   for (int p = 1; p <= 64 && (p == 1 || steps / p >= 4); ++p) {
-    const double time = head_time<S>(tiles * p, static_cast<double>(steps) / p, TileCost<S>::FIXED) + p * (static_cast<double>(T) * d / 4.0e6);   // as dx_parts
+    const double time = head_time<S>(tiles * p, static_cast<double>(steps) / p, TileCost<S>::FIXED + more) + p * (static_cast<double>(rows) * d / 1.0e6);   // as dx_parts
     if (time < best) { best = time; shape = {S, p}; }
   }
 }
-// The edge for all T tokens; the parts are chosen again for those that have a loss, in the room that this number leaves.
+// dx: the edge for all T tokens; the parts are chosen again for those that have a loss, in the room that this number leaves.
 HeadShape head_dx_shape(int T, int d, int cols) {
   HeadShape shape{128, 1};
   double best = 1e300;
-  head_parts<256>(T, d, cols, best, shape);
-  head_parts<128>(T, d, cols, best, shape);
+  head_parts<256>(T, d, cols, 0.0, best, shape);
+  head_parts<128>(T, d, cols, 0.0, best, shape);
+  return shape;
+}
+// dW of `cols` columns of the vocabulary.  One part needs no sums beside it: where the reduction is in parts it has to be worth more than they cost.
+HeadShape head_dw_shape(int cols, int d, int rows, bool whole) {
+  HeadShape shape{128, 1};
+  double best = 1e300;
+  head_parts<256>(cols, d, rows, 0.8, best, shape);
+  head_parts<128>(cols, d, rows, 1.1, best, shape);
+  if (!whole || shape.parts == 1) {
+    const double one256 = head_time<256>(static_cast<double>(ceil_div(cols, 256)) * ceil_div(d, 256), ceil_div(rows, BK), TileCost<256>::FIXED + 0.8);
+    const double one128 = head_time<128>(static_cast<double>(ceil_div(cols, 128)) * ceil_div(d, 128), ceil_div(rows, BK), TileCost<128>::FIXED + 1.1);
+    shape = {one128 < one256 ? 128 : 256, 1};
+  }
   return shape;
 }
 template <int S> double head_plain_time(int rows, int cols, int depth, double fixed) {
@@ -606,7 +648,7 @@ void fill_head(const HeadCall& c, const HeadLayout& l, GemmArgs& a, HeadArgs& h)
 template <int MODE> int launch_head(GemmArgs& a, const HeadArgs& h, int edge, int rows, int cols, const char* name, hipStream_t s) {
   a.n_tiles = ceil_div(cols, edge);
   a.m_tiles_cap = ceil_div(rows, edge);
-  const long long tiles = static_cast<long long>(a.n_tiles) * a.m_tiles_cap * (MODE == HEAD_DX ? 64 : 1);
+  const long long tiles = static_cast<long long>(a.n_tiles) * a.m_tiles_cap * (MODE == HEAD_DX ? 64 : a.E);
   if (tiles > 0x7FFFFFFFll / 2) return MOE_ERR_INVALID;
   return edge == 128 ? launch_gemm_head<MODE, 128>(a, h, tiles, s, name) : launch_gemm_head<MODE, 256>(a, h, tiles, s, name);
 }
@@ -654,11 +696,14 @@ int run_head_bwd(const HeadCall& c, int v_piece, int* edges) {
   const int dx_edge = settle_edge(edges != nullptr ? edges + 1 : nullptr, dxs.edge);
   // (the parts are those of all pieces: no more than the smallest, the last, has steps for)
   const int last = c.V - (c.V - 1) / piece * piece;
-  const DxRule rule{dx_edge, HEAD_CUS * 256 / dx_edge, c.d, ceil_div(last, BK), 0, static_cast<float>(dx_edge == 256 ? TileCost<256>::FIXED : TileCost<128>::FIXED)};
+  const bool large = dx_edge == 256;
+  const DxRule rule{dx_edge, HEAD_CUS * 256 / dx_edge, c.d, ceil_div(last, BK), 0, static_cast<float>(large ? TileCost<256>::FIXED : TileCost<128>::FIXED),
+                    static_cast<float>(large ? TileCost<256>::STEP : TileCost<128>::STEP)};
   int rc = run_prep(c, l, rule, static_cast<long long>(dxs.parts) * c.T);
   if (rc != MOE_OK) return rc;
   const int32_t* control = reinterpret_cast<const int32_t*>(c.ws + l.control);
-  const int dw_rows = l.low ? 2 * c.T : c.T;
+  const HeadShape dws = head_dw_shape(piece, c.d, l.low ? 2 * c.T : c.T, piece >= c.V);
+  float* dw_part = part + static_cast<size_t>(dxs.parts) * c.T * c.d;
   for (int v0 = 0; v0 < c.V; v0 += piece) {
     const int cols = c.V - v0 < piece ? c.V - v0 : piece, ld = (cols + 63) & ~63;
     GemmArgs a{};
@@ -676,15 +721,17 @@ int run_head_bwd(const HeadCall& c, int v_piece, int* edges) {
     h.add = v0 > 0;
     if ((rc = launch_head<HEAD_DX>(b, h, dx_edge, c.T, c.d, "gemm_head_dx", c.s)) != MOE_OK) return rc;
     GemmArgs w{};
-    w.offsets = control + DW_ROWS - 1; w.E = 1; w.row_token = a.row_token;
+    w.offsets = control + DW_ROWS - 1; w.E = dws.parts; w.row_token = a.row_token; w.O1 = reinterpret_cast<uint16_t*>(dw_part);
     w.A0 = dz; w.B0 = a.A0; w.B1 = a.A1; w.O0 = c.dW + static_cast<size_t>(v0) * c.d; w.M = ld; w.K = cols; w.N = c.d;
-    rc = launch_head<HEAD_DW>(w, h, settle_edge(edges != nullptr ? edges + 2 : nullptr, head_edge(cols, c.d, dw_rows, 0.8, 1.1)), cols, c.d, "gemm_head_dw", c.s);
+    rc = launch_head<HEAD_DW>(w, h, settle_edge(edges != nullptr ? edges + 2 : nullptr, dws.edge), cols, c.d, "gemm_head_dw", c.s);
     if (rc != MOE_OK) return rc;
   }
   const size_t n = static_cast<size_t>(c.T) * (c.d / 8);
   const HeadDxArgs x{part, control, reinterpret_cast<const int32_t*>(c.ws + l.token_row), reinterpret_cast<const int32_t*>(c.ws + l.target_slot), c.target,
-                     reinterpret_cast<const float*>(c.ws + l.item), c.t, c.W, c.T, c.d, c.V, c.T <= LOW_TOKENS, c.dx};
-  MOE_LAUNCH("head_dx", head_dx_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, c.s, x);
+                     reinterpret_cast<const float*>(c.ws + l.item), c.t, c.W, c.T, c.d, c.V, c.T <= LOW_TOKENS, c.dx,
+                     dw_part, dws.parts, static_cast<int>((n + 255) / 256), c.dW};
+  const size_t groups = x.dx_groups + (dws.parts > 1 ? (static_cast<size_t>(c.V) * (c.d / 8) + 255) / 256 : 0);
+  MOE_LAUNCH("head_dx", head_dx_kernel, dim3(static_cast<unsigned>(groups)), dim3(256), 0, c.s, x);
   return moe_check_launch();
 }
 
@@ -704,7 +751,9 @@ extern "C" size_t moe_head_fwd_workspace_bytes(int T, int d, int V, int K) {
 extern "C" size_t moe_head_bwd_workspace_bytes(int T, int d, int V, int K, int v_piece) {
   if (bad_head_dims(T, d, V, K) || v_piece < 0 || v_piece % 256 != 0) return 0;
   const int piece = head_piece(T, V, v_piece);
-  return head_layout(T, d, V, K, true).big + head_dz_bytes(T, piece) + static_cast<size_t>(head_dx_shape(T, d, piece).parts) * T * d * sizeof(float);
+  const int dw_parts = head_dw_shape(piece, d, T <= LOW_TOKENS ? 2 * T : T, piece >= V).parts;
+  return head_layout(T, d, V, K, true).big + head_dz_bytes(T, piece) +
+         (static_cast<size_t>(head_dx_shape(T, d, piece).parts) * T + (dw_parts > 1 ? static_cast<size_t>(dw_parts) * V : 0)) * d * sizeof(float);
 }
 
 // Both losses, or (ids null, K 0) the cross entropy alone: what the calls of moe_hotpath.h come to.  edges, for tests: as in gemm.h, of the
