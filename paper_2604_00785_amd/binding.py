@@ -123,18 +123,18 @@ def _p(t: Optional[torch.Tensor]):
         return None
     if not t.is_cuda or not t.is_contiguous():
         raise MoeError("tensors must be contiguous device tensors")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _stream():
     # the current stream's handle without building a Stream object around it (0.2 us instead of 2.7 us per call)
-    return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _want(t: torch.Tensor, dtype, shape=None, name="tensor"):
     if t.dtype != dtype:
         raise MoeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise MoeError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
 
 

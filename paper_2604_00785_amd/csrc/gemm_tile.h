@@ -636,10 +636,10 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
   if constexpr (MODE == DGRAD_X) { t.sa_phase1 = scalarize(abase + a_phase - LOAD_BIAS); t.sb_phase1 = scalarize(bbase + b_phase - LOAD_BIAS); }
   t.a_step = a_step; t.b_step = b_step; t.k_lo = k_lo; t.k_hi = k_hi; t.row_tok = row_tok; t.nk = nk; t.nk_phase = nk_phase;
   if constexpr (is_logits(MODE)) {
-    // A tile with few rows waits for memory.  Where weight rows are multiples of 4096 bytes, tiles that run in step read the same few bytes of each,
-    // which lie in a fraction of the channels: they begin their reductions at different steps (57 tokens of d 4096, V 32003: 63 -> 48.5 us; with many
-    // rows it costs 1 %).
-    if (t.few) {
+    // With one or two row tiles the product waits for memory.  Where weight rows are multiples of 4096 bytes, tiles that run in step read the same
+    // few bytes of each, which lie in a fraction of the channels: they begin their reductions at different steps (57 tokens of d 4096, V 32003: 63 -> 48.5 us;
+    // 200 of d 2048, V 50304: 59.6 -> 55; other rows as before; with many row tiles it costs 1 %).
+    if (rt <= 2) {
       const int rot = __builtin_amdgcn_readfirstlane(nt * 3 % nk);
       t.sa_phase1 = t.sa_next; t.sb_phase1 = t.sb_next;
       t.sa_next += rot * BK * 2; t.sb_next += rot * BK * 2;
@@ -1246,7 +1246,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
     // PASSES staged passes of 64 / PIECES rows of RB bytes each (16-byte pieces swizzled by row & (RB / 16 - 1), region at
     // `base`), the PIECES pieces from PIECE0 on of each row: read into registers, and stored from there (first row
     // `first`, counted from the wave's first) to columns col0 + 8 piece.  NT: the output is not read again soon (g and u: not
-    // before the backward pass; dWg and dWu: not by this layer at all), so its stores are marked non-temporal and leave
+    // before the backward pass; dWg, dWu and the head's dW: not by this layer at all), so its stores are marked non-temporal and leave
     // the caches to what the next kernels read (measured: 0.4-0.6 % of the step, most of it in the kernels that follow).
     auto read_staged = [&](u32x4* v, const char* base, auto rb_tag, auto passes_tag, auto piece0_tag, auto pieces_tag)
         __attribute__((always_inline)) {
@@ -1648,7 +1648,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
       u32x4 v[PASSES];
       // parts of 32 rows
       auto store_part = [&](int part) __attribute__((always_inline)) {
-        store_rows(IC<(MODE == WGRAD_GATHER) ? 1 : 0>{}, v, oo, part * 32, IC<PASSES>{}, IC<RP>{});
+        store_rows(IC<(MODE == WGRAD_GATHER || MODE == HEAD_DW) ? 1 : 0>{}, v, oo, part * 32, IC<PASSES>{}, IC<RP>{});
       };
       auto parts = [&](auto ragged_tag) __attribute__((always_inline)) {
       constexpr bool RAGGED = decltype(ragged_tag)::value != 0;

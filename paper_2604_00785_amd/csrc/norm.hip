@@ -32,9 +32,14 @@ __device__ __forceinline__ void unpack8(const u32x4& p, float (&v)[8]) {
 __device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
   return u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
 }
+// Rows are read once and long after they were written, or by nobody else soon: non-temporal loads leave the caches to what is
+// written.  One pass over other rows each time, us, ordinary -> non-temporal: 8192 x 2048 forward 30.7 -> 28.2 (4.8 TB/s), 8 bits 31.9 -> 27.4,
+// backward 36.5 -> 34.1; 4001 x 4096 28.3 -> 24.8 (5.3 TB/s), 26.3 -> 24.3, 34.7 -> 31.9.
+__device__ __forceinline__ u32x4 load8(const moe_bf16* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
+
 // Reduction over the TPR threads of a row: inside the waves by lane permutations, across them through LDS.
 template <int TPR, typename Op> __device__ __forceinline__ uint32_t row_reduce(uint32_t v, Op op, uint32_t* part) {
-  v = group_reduce<MOE_WAVE>(v, op);
+  v = group_reduce<TPR < MOE_WAVE ? TPR : MOE_WAVE>(v, op);
   if constexpr (TPR > MOE_WAVE) {
     __syncthreads();                              // what was there before has been read
     if (threadIdx.x % MOE_WAVE == 0) part[threadIdx.x / MOE_WAVE] = v;
@@ -57,9 +62,9 @@ __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b 
 template <int TPR, int P, bool CODES>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_kernel(NormArgs a) {
   constexpr int ROWS = TPR > 256 ? 1 : 256 / TPR;
-  __shared__ uint32_t part[TPR / MOE_WAVE];
+  __shared__ uint32_t part[TPR > MOE_WAVE ? TPR / MOE_WAVE : 1];
   const int row = blockIdx.x * ROWS + threadIdx.x / TPR, i0 = threadIdx.x % TPR;
-  if (row >= a.T) return;                         // a whole wave, and only where a row is one
+  if (row >= a.T) return;                         // all of a row's threads, and only where no barrier follows
   const int pieces = a.d / 8;
   const size_t at = static_cast<size_t>(row) * a.d;
   float s[P][8];
@@ -69,8 +74,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_kernel(Nor
     const int i = i0 + p * TPR;
     xp[p] = rp[p] = u32x4{0, 0, 0, 0};
     if (i < pieces) {
-      xp[p] = *reinterpret_cast<const u32x4*>(a.x + at + 8 * i);
-      if (a.r != nullptr) rp[p] = *reinterpret_cast<const u32x4*>(a.r + at + 8 * i);
+      xp[p] = load8(a.x + at + 8 * i);
+      if (a.r != nullptr) rp[p] = load8(a.r + at + 8 * i);
     }
   }
   float q = 0.f;
@@ -109,7 +114,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_kernel(Nor
     }
   }
   if constexpr (CODES) {
-    const bool whole = a.lanes > MOE_WAVE;        // one scale for the row
+    const bool whole = a.lanes >= pieces;         // one scale for the row
     if (whole) top = row_reduce<TPR>(top, umax, part);
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -161,7 +166,7 @@ struct NormBwdArgs {
 template <int TPR, int P>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_bwd_kernel(NormBwdArgs a) {
   constexpr int ROWS = TPR > 256 ? 1 : 256 / TPR;
-  __shared__ uint32_t part[TPR / MOE_WAVE];
+  __shared__ uint32_t part[TPR > MOE_WAVE ? TPR / MOE_WAVE : 1];
   __shared__ float share[ROWS > 1 ? (ROWS - 1) * P * 8 * TPR : 1];
   const int first = blockIdx.x * ROWS + threadIdx.x / TPR, i0 = threadIdx.x % TPR;
   const int pieces = a.d / 8;
@@ -172,20 +177,30 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_bwd_kernel
 #pragma unroll
     for (int c = 0; c < 8; ++c) { dw[p][c] = 0.f; w[p][c] = i < pieces ? a.w[8 * i + c] : 0.f; }
   }
-  for (int row = first; row < a.T; row += gridDim.x * ROWS) {     // (the same for all threads of a row)
-    const size_t at = static_cast<size_t>(row) * a.d;
-    u32x4 gp[P], sp[P], ap[P];
+  // the next row's pieces are requested before this row's are used
+  struct Row { u32x4 g[P], s[P], a[P]; float q; };
+  auto load = [&](int row, Row& x) __attribute__((always_inline)) {
+    const size_t at = static_cast<size_t>(row < a.T ? row : a.T - 1) * a.d;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int i = i0 + p * TPR;
-      gp[p] = sp[p] = ap[p] = u32x4{0, 0, 0, 0};
+      x.g[p] = x.s[p] = x.a[p] = u32x4{0, 0, 0, 0};
       if (i < pieces) {
-        gp[p] = *reinterpret_cast<const u32x4*>(a.dy + at + 8 * i);
-        sp[p] = *reinterpret_cast<const u32x4*>(a.sum + at + 8 * i);
-        if (a.dsum != nullptr) ap[p] = *reinterpret_cast<const u32x4*>(a.dsum + at + 8 * i);
+        x.g[p] = load8(a.dy + at + 8 * i);
+        x.s[p] = load8(a.sum + at + 8 * i);
+        if (a.dsum != nullptr) x.a[p] = load8(a.dsum + at + 8 * i);
       }
     }
-    const float q = a.rstd[row];
+    x.q = a.rstd[row < a.T ? row : a.T - 1];
+  };
+  const int step = gridDim.x * ROWS;
+  Row now, next;
+  load(first, now);
+  for (int row = first; row < a.T; row += step, now = next) {     // (the same for all threads of a row)
+    if (row + step < a.T) load(row + step, next);
+    const size_t at = static_cast<size_t>(row) * a.d;
+    const u32x4 (&gp)[P] = now.g, (&sp)[P] = now.s, (&ap)[P] = now.a;
+    const float q = now.q;
     float dot = 0.f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -239,27 +254,27 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_bwd_kernel
   }
 }
 
-// dw[c] = sum of the n shares, in a fixed order: 8 threads take every eighth share of four columns, then meet in LDS.
+// dw[c] = sum of the n shares, in a fixed order: 32 threads take every 32nd share of four columns, then meet in LDS.
 __global__ __launch_bounds__(256) void norm_dw_kernel(const float* __restrict__ part, int n, int d, float* __restrict__ dw) {
-  __shared__ f32x4_t s[8][32];
-  const int c = threadIdx.x % 32, k = threadIdx.x / 32, col = (blockIdx.x * 32 + c) * 4;
+  __shared__ f32x4_t s[32][8];
+  const int c = threadIdx.x % 8, k = threadIdx.x / 8, col = (blockIdx.x * 8 + c) * 4;
   f32x4_t v = {0.f, 0.f, 0.f, 0.f};
   if (col < d) {
-#pragma unroll 8
-    for (int i = k; i < n; i += 8) v += *reinterpret_cast<const f32x4_t*>(part + static_cast<size_t>(i) * d + col);
+#pragma unroll 16
+    for (int i = k; i < n; i += 32) v += *reinterpret_cast<const f32x4_t*>(part + static_cast<size_t>(i) * d + col);
   }
   s[k][c] = v;
   __syncthreads();
   if (k == 0 && col < d) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) v += s[i][c];
+    for (int i = 1; i < 32; ++i) v += s[i][c];
     *reinterpret_cast<f32x4_t*>(dw + col) = v;
   }
 }
 
 bool bad_norm_dims(int T, int d) { return T <= 0 || d <= 0 || d % 8 != 0 || d > NORM_MAX_D; }
-int rows_of_group(int d) { return d <= 2048 ? 4 : 1; }
-// Threads of a row: one wave up to 2048 columns (no barrier in the row's sums), 256 up to 8192, else 1024.
+int rows_of_group(int d) { return d <= 256 ? 16 : d <= 2048 ? 4 : 1; }
+// Threads of a row: 16 up to 256 columns, one wave up to 2048 (no barrier in the row's sums), 256 up to 8192, else 1024.
 template <typename F> void with_shape(int d, F&& f) {
   const int pieces = d / 8;
 #define MOE_NORM(TPR) \
@@ -269,13 +284,14 @@ template <typename F> void with_shape(int d, F&& f) {
     case 3: f(std::integral_constant<int, TPR>{}, std::integral_constant<int, 3>{}); break; \
     default: f(std::integral_constant<int, TPR>{}, std::integral_constant<int, 4>{}); break; \
   }
-  if (pieces <= 256) { MOE_NORM(64) } else if (pieces <= 1024) { MOE_NORM(256) } else { MOE_NORM(1024) }
+  if (pieces <= 32) { MOE_NORM(16) } else if (pieces <= 256) { MOE_NORM(64) } else if (pieces <= 1024) { MOE_NORM(256) } else { MOE_NORM(1024) }
 #undef MOE_NORM
 }
-// Workgroups of the backward pass, each with a share of dw: two per compute unit of a whole chip, or as many as there are rows for.
+// Workgroups of the backward pass, each with a share of dw: two per compute unit of a whole chip, one where a share is long, or as many as there are
+// rows for.  us with 256 / 512 / 1024: 8192 x 2048 34.1 / 33.4 / 39.9, 4001 x 4096 34.8 / 30.4 / 35.0, 2000 x 8192 36.0 / 40.7 / 51.5, 16384 x 136 13.3 / 11.9 / 15.0.
 int norm_bwd_groups(int T, int d) {
-  const int rows = rows_of_group(d), groups = (T - 1) / rows + 1;
-  return groups < 512 ? groups : 512;
+  const int rows = rows_of_group(d), groups = (T - 1) / rows + 1, most = d <= 4096 ? 512 : 256;
+  return groups < most ? groups : most;
 }
 
 template <bool CODES> int launch_norm(const NormArgs& a, const char* name, hipStream_t s) {
@@ -328,6 +344,6 @@ extern "C" int moe_add_rms_norm_bwd(const moe_bf16* dy, const moe_bf16* dsum, co
     MOE_LAUNCH("add_rms_norm_bwd", (add_rms_norm_bwd_kernel<TPR, P>), dim3(groups), dim3(TPR > 256 ? TPR : 256), 0, s, a);
   });
   if (moe_check_launch() != MOE_OK) return MOE_ERR_LAUNCH;
-  MOE_LAUNCH("norm_dw", norm_dw_kernel, dim3((d / 4 + 31) / 32), dim3(256), 0, s, static_cast<const float*>(ws), groups, d, dw);
+  MOE_LAUNCH("norm_dw", norm_dw_kernel, dim3((d / 4 + 7) / 8), dim3(256), 0, s, static_cast<const float*>(ws), groups, d, dw);
   return moe_check_launch();
 }
