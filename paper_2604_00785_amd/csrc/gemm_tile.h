@@ -146,7 +146,7 @@ struct GemmArgs {
 // by strips of 64 columns.
 struct HeadItem { uint32_t at, slot; };   // at: row in the block | column << 4
 struct HeadArgs {
-  float* part;                // HEAD_STATS: planes [strips][rows_cap] of maximum, sum and (two) sum at the temperature over HALF columns, without the items
+  float* part;                // HEAD_STATS: [row block][strips of HALF columns][2 or (two) 3][16 rows]: maximum, sum and sum at the temperature, without the items
   const f32x4_t* row;         // HEAD_DZ: per row log2(e) lse, factor, and the same at the temperature
   const int32_t* target;      // [row]
   const int32_t* list_start;  // [row block][list_ld]: first item of each strip; null: no teacher
@@ -155,7 +155,7 @@ struct HeadArgs {
   float* item;                // [row][slots]: HEAD_STATS: the logit; HEAD_DZ: what the gradient loses when it is rounded
   float c1, c2, over_tau;     // log2(e), the same over the temperature, 1 / temperature
   int two;                    // both sums, both terms
-  int strips, rows_cap, list_ld, slots;
+  int strips, list_ld, slots;
   int col0;                   // vocabulary column of the product's first
   int add;                    // HEAD_DX: onto what is there
   int lo;                     // HEAD_DZ: what rounding loses is stored too, in as many rows behind the others
@@ -1512,8 +1512,9 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
         });
       };
       if constexpr (MODE == HEAD_STATS) {
-        const size_t plane = static_cast<size_t>(he->strips) * he->rows_cap;
-        float* const out = he->part + static_cast<size_t>(gcol0 / HALF) * he->rows_cap + grow0 + l16 + lq * plane;
+        const int planes = two ? 3 : 2;
+        const size_t block = static_cast<size_t>(he->strips) * planes * 16;
+        float* const out = he->part + (grow0 >> 4) * block + gcol0 / HALF * planes * 16 + lane;
         static_for<NB>([&](auto i_tag) {
           constexpr int i = decltype(i_tag)::value;
           if (i * 16 >= rows || left <= 0) return;
@@ -1547,7 +1548,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
               for (int c = 0; c < 4; ++c) s2 += __builtin_amdgcn_exp2f(__builtin_fmaf(v[j][c], c2, -e2));
             s2 = quads_reduce(s2, add);
           }
-          if (lq < (two ? 3 : 2) && i * 16 + l16 < rows) out[i * 16] = lq == 0 ? m : lq == 1 ? s1 : s2;
+          if (lq < planes && i * 16 + l16 < rows) out[i * block] = lq == 0 ? m : lq == 1 ? s1 : s2;
         });
       } else {
         const int ld = ae->M;

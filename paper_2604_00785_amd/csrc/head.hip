@@ -89,7 +89,7 @@ struct HeadPrepArgs {
 __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   extern __shared__ int count[];                     // [strips + 1]
   __shared__ uint64_t own[SELF_MASK_TOKENS / 64];
-  __shared__ int wave_sum[4], s_token[16], s_target[16], s_slot[16];
+  __shared__ int wave_sum[4], s_token[16], s_slot[16];
   const int tid = threadIdx.x, lane = tid % MOE_WAVE, wave = tid / MOE_WAVE;
   const int words = (a.T + 63) / 64, per = (words + 255) / 256, K = a.t.K, V = a.V, slots = K + 1;
   const bool lists = blockIdx.y == 0;
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     }
     mask = own;
   }
-  if (tid < 16) { s_token[tid] = -1; s_target[tid] = -1; s_slot[tid] = K; }
+  if (tid < 16) { s_token[tid] = -1; s_slot[tid] = K; }
   if (lists && K > 0) for (int i = tid; i <= a.strips; i += 256) count[i] = 0;
   __syncthreads();
   // rank of each thread's first token among those with a loss
@@ -158,24 +158,24 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     }
   }
   if (first >= live || (direct && !lists)) return;
-  for (int w = w0; w < w1 && rank < first + 16; ++w) {
-    uint64_t bits = mask[w];
-    const int n = __builtin_popcountll(bits);
-    if (rank + n <= first) { rank += n; continue; }
-    for (; bits != 0; bits &= bits - 1, ++rank) {
-      if (rank < first || rank >= first + 16) continue;
-      const int t = w * 64 + __builtin_ctzll(bits);
-      s_token[rank - first] = t;
-      if (lists) {
-        s_target[rank - first] = a.target[t];
-        a.row_token[rank] = t;
-        a.token_row[t] = rank;
-      }
+  // the words that hold ranks first to first + 15, a bit a lane
+  for (uint64_t hit = __ballot(mine > 0 && rank < first + 16 && rank + mine > first); hit != 0; hit &= hit - 1) {
+    const int l = __builtin_ctzll(hit), from = (wave * MOE_WAVE + l) * per, to = from + per < words ? from + per : words;
+    int at = wave_lane(rank, l);
+    for (int w = from; w < to; ++w) {
+      const uint64_t bits = mask[w];
+      const int rk = at + __builtin_popcountll(bits & ((1ull << lane) - 1));
+      if ((bits >> lane & 1) != 0 && rk >= first && rk < first + 16) s_token[rk - first] = w * 64 + lane;
+      at += __builtin_popcountll(bits);
     }
   }
   __syncthreads();
   const int n = live - first < 16 ? live - first : 16;
-  const int r = tid >> 4, l16 = tid & 15, y = s_target[r], t = s_token[r];
+  const int r = tid >> 4, l16 = tid & 15, t = s_token[r], y = r < n ? a.target[t] : -1;
+  if (lists && l16 == 0 && r < n) {
+    a.row_token[first + r] = t;
+    a.token_row[t] = first + r;
+  }
   const bool has = r < n && target_there(y, V);
   float in_loss = 0.f, in_lse = 0.f, in_lse_t = 0.f, gl = 0.f, in_dkd = 0.f;      // requested ahead of the rows
   if (a.row != nullptr && lists && r < n) {
@@ -303,51 +303,28 @@ struct HeadJoinArgs {
   int T;
   const float* z_item;
   Teacher t;
-  int strips, rows_cap, V;
+  int strips, V;
   float *loss, *lse, *kd, *lse_t;
   float c1, c2;
 };
-// 16 rows: their strips' maxima and sums joined by 64 threads each, then the losses, a wave for each row with its entries in registers (EPL a
-// lane).  Sums of exponentials have the scale 2^E of gemm_tile.h.
-constexpr int JOIN_THREADS = 1024, JOIN_GROUPS = JOIN_THREADS / 16;
+// 16 rows: their strips' maxima and sums joined by 256 threads to four rows, then the losses, a wave for each row with its entries in registers
+// (EPL a lane).  Sums of exponentials have the scale 2^E of gemm_tile.h.
+constexpr int JOIN_THREADS = 1024, JOIN_GROUPS = JOIN_THREADS / 4;
 template <int EPL>
 __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a) {
-  __shared__ float part[4][JOIN_GROUPS][16];
+  __shared__ float part[4][16][JOIN_GROUPS + 1];
   const int tid = threadIdx.x, lane = tid % MOE_WAVE;
   const int first = blockIdx.x * 16, live = a.control != nullptr ? a.control[LIVE] : a.T, K = a.t.K;
   const bool two = K > 0 && a.t.temperature != 1.f;
   if (first >= live) return;
   constexpr float NONE = -__builtin_inff(), LOW = -3.0e38f;
-  {
-    const int r = tid % 16, g = tid / 16, row = first + r < live ? first + r : live - 1;
-    const size_t plane = static_cast<size_t>(a.strips) * a.rows_cap;
-    float e1 = LOW, s1 = 0.f, e2 = LOW, s2 = 0.f;
-#pragma unroll 4
-    for (int s = g; s < a.strips; s += JOIN_GROUPS) {
-      const float* p = a.part + static_cast<size_t>(s) * a.rows_cap + row;
-      const float m = p[0], v1 = p[plane], v2 = two ? p[2 * plane] : 0.f;
-      const float f1 = m > NONE ? ceilf(m * a.c1) : LOW, f2 = m > NONE ? ceilf(m * a.c2) : LOW;
-      const float n1 = fmaxf(e1, f1), n2 = fmaxf(e2, f2);
-      s1 = s1 * __builtin_amdgcn_exp2f(e1 - n1) + v1 * __builtin_amdgcn_exp2f(f1 - n1);
-      s2 = s2 * __builtin_amdgcn_exp2f(e2 - n2) + v2 * __builtin_amdgcn_exp2f(f2 - n2);
-      e1 = n1; e2 = n2;
-    }
-    part[0][g][r] = e1; part[1][g][r] = s1; part[2][g][r] = e2; part[3][g][r] = s2;
-  }
-  __syncthreads();
-  const int r = tid / MOE_WAVE, row = first + r;
-  if (row >= live) return;
-  // log of the sum over the columns that are no item
-  auto joined = [&](int h) __attribute__((always_inline)) {
-    const float e = part[h][lane][r], top = wave_max_of(e), s = wave_sum_of(part[h + 1][lane][r] * __builtin_amdgcn_exp2f(e - top));
-    return s > 0.f ? __builtin_fmaf(top, LN2, logf(s)) : NONE;
-  };
-  const float rest1 = joined(0), rest2 = two ? joined(2) : rest1, tau = a.t.temperature;
+  // what belongs to the wave's row is requested first
+  const int r = tid / MOE_WAVE, row = first + r < live ? first + r : live - 1;
   const int t = a.control != nullptr ? a.row_token[row] : row;
   const int slot = K > 0 ? a.target_slot[row] : target_there(a.target[t], a.V) ? 0 : -1;
   const float* z = a.z_item + static_cast<size_t>(row) * (K + 1);
   const size_t at = static_cast<size_t>(t) * K;
-  const float zy = slot >= 0 ? z[slot] : 0.f;
+  const float zy = slot >= 0 ? z[slot] : 0.f, tau = a.t.temperature;
   bool on[EPL];
   float zj[EPL], l[EPL];                                 // an entry's logit and, over the temperature, the teacher's
 #pragma unroll
@@ -357,6 +334,50 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
     zj[i] = on[i] ? z[j] : 0.f;
     l[i] = on[i] ? a.t.logits[at + j] / tau : NONE;
   }
+  {
+    const int quad = tid % 4, g = tid / 4;
+    const int planes = two ? 3 : 2;
+    const float* base = a.part + static_cast<size_t>(blockIdx.x) * a.strips * planes * 16 + quad * 4;
+    float e1[4], s1[4], e2[4], s2[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { e1[i] = e2[i] = LOW; s1[i] = s2[i] = 0.f; }
+#pragma unroll 2
+    for (int s = g; s < a.strips; s += JOIN_GROUPS) {
+      const float* p = base + s * planes * 16;
+      const f32x4_t m = *reinterpret_cast<const f32x4_t*>(p), v1 = *reinterpret_cast<const f32x4_t*>(p + 16);
+      const f32x4_t v2 = two ? *reinterpret_cast<const f32x4_t*>(p + 32) : f32x4_t{};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float f1 = m[i] > NONE ? ceilf(m[i] * a.c1) : LOW, n1 = fmaxf(e1[i], f1);
+        s1[i] = s1[i] * __builtin_amdgcn_exp2f(e1[i] - n1) + v1[i] * __builtin_amdgcn_exp2f(f1 - n1);
+        e1[i] = n1;
+        if (two) {
+          const float f2 = m[i] > NONE ? ceilf(m[i] * a.c2) : LOW, n2 = fmaxf(e2[i], f2);
+          s2[i] = s2[i] * __builtin_amdgcn_exp2f(e2[i] - n2) + v2[i] * __builtin_amdgcn_exp2f(f2 - n2);
+          e2[i] = n2;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      part[0][quad * 4 + i][g] = e1[i]; part[1][quad * 4 + i][g] = s1[i];
+      if (two) { part[2][quad * 4 + i][g] = e2[i]; part[3][quad * 4 + i][g] = s2[i]; }
+    }
+  }
+  __syncthreads();
+  if (first + r >= live) return;
+  // log of the sum over the columns that are no item
+  auto joined = [&](int h) __attribute__((always_inline)) {
+    float e[JOIN_GROUPS / MOE_WAVE], top = LOW, s = 0.f;
+#pragma unroll
+    for (int i = 0; i < JOIN_GROUPS / MOE_WAVE; ++i) { e[i] = part[h][r][lane + i * MOE_WAVE]; top = fmaxf(top, e[i]); }
+    top = wave_max_of(top);
+#pragma unroll
+    for (int i = 0; i < JOIN_GROUPS / MOE_WAVE; ++i) s += part[h + 1][r][lane + i * MOE_WAVE] * __builtin_amdgcn_exp2f(e[i] - top);
+    s = wave_sum_of(s);
+    return s > 0.f ? __builtin_fmaf(top, LN2, logf(s)) : NONE;
+  };
+  const float rest1 = joined(0), rest2 = two ? joined(2) : rest1;
   float loss = 0.f, lse = 0.f, kd = 0.f, lse_t = 0.f;
   // loss = log(1 + exp(away)), away = log of the sum over all columns but the target, less the target's logit
   if (slot >= 0) {
@@ -585,7 +606,7 @@ HeadLayout head_layout(int T, int d, int V, int K, bool backward) {
   l.big = at;
   return l;
 }
-size_t head_part_bytes(int T, int V) { return static_cast<size_t>(3) * ((V + 63) / 64) * T * sizeof(float); }
+size_t head_part_bytes(int T, int V) { return static_cast<size_t>(3) * ((V + 63) / 64) * ((T + 15) & ~15) * sizeof(float); }
 // (a few tokens: what rounding loses lies in as many rows behind the others)
 size_t head_dz_bytes(int T, int piece) { return (static_cast<size_t>(T <= LOW_TOKENS ? 2 * T : T) * ((piece + 63) & ~63) * 2 + 255) & ~static_cast<size_t>(255); }
 
@@ -647,7 +668,6 @@ void fill_head(const HeadCall& c, const HeadLayout& l, GemmArgs& a, HeadArgs& h)
   h.c2 = LOG2E / c.t.temperature;
   h.over_tau = 1.f / c.t.temperature;
   h.two = c.t.K > 0 && c.t.temperature != 1.f;
-  h.rows_cap = c.T;
   h.list_ld = l.strips64 + 1;
   h.slots = l.slots;
 }
@@ -684,7 +704,7 @@ int run_head_fwd(const HeadCall& c, int* edges) {
   h.part = reinterpret_cast<float*>(c.ws + l.big);
   if ((rc = launch_head<HEAD_STATS>(a, h, edge, c.T, c.V, "gemm_head_stats", c.s)) != MOE_OK) return rc;
   const HeadJoinArgs j{h.part, all ? nullptr : reinterpret_cast<const int32_t*>(c.ws + l.control), reinterpret_cast<const int32_t*>(c.ws + l.row_token),
-                       reinterpret_cast<const int32_t*>(c.ws + l.target_slot), c.target, c.T, h.item, c.t, h.strips, c.T, c.V, c.loss, c.lse, c.kd, c.lse_t,
+                       reinterpret_cast<const int32_t*>(c.ws + l.target_slot), c.target, c.T, h.item, c.t, h.strips, c.V, c.loss, c.lse, c.kd, c.lse_t,
                        h.c1, h.c2};
   const dim3 grid(l.blocks), block(JOIN_THREADS);
   if (c.t.K <= MOE_WAVE) MOE_LAUNCH("head_join", head_join_kernel<1>, grid, block, 0, c.s, j);
