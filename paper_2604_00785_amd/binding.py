@@ -518,6 +518,42 @@ def moe_head_distill_bwd(x, W, target, ids, teacher, temperature: float, loss, l
                                        ws.numel() * ws.element_size(), _stream()), "moe_head_distill_bwd")
 
 
+class HeadBuffers:
+    """The vocabulary head's results and workspace for one shape, allocated once.
+
+    K entries of a teacher per token (0: cross entropy alone); ``train=False`` leaves out what only the backward
+    needs.  The calls enqueue on the current stream and do not synchronise.
+    """
+
+    def __init__(self, T: int, d: int, V: int, K: int = 0, v_piece: int = 0, train: bool = True, device="cuda:0"):
+        dev = torch.device(device)
+        row = lambda: torch.zeros(T, dtype=torch.float32, device=dev)  # noqa: E731
+        self.v_piece = v_piece
+        self.loss, self.lse = row(), row()
+        self.kd, self.lse_t = (row(), row()) if K else (None, None)
+        nbytes = moe_head_fwd_workspace_bytes(T, d, V, K)
+        if train:
+            self.dx = torch.zeros(T, d, dtype=BF16, device=dev)
+            self.dW = torch.zeros(V, d, dtype=BF16, device=dev)
+            nbytes = max(nbytes, moe_head_bwd_workspace_bytes(T, d, V, K, v_piece))
+        if nbytes == 0:
+            raise MoeError(f"no head of {T} tokens, d {d}, {V} columns, {K} entries, pieces of {v_piece}")
+        self.ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+
+    def run_fwd(self, x, W, target, ids=None, teacher=None, temperature: float = 1.0) -> None:
+        if ids is None:
+            moe_head_ce_fwd(x, W, target, self.loss, self.lse, self.ws)
+        else:
+            moe_head_distill_fwd(x, W, target, ids, teacher, temperature, self.loss, self.lse, self.kd, self.lse_t, self.ws)
+
+    def run_bwd(self, x, W, target, dloss, ids=None, teacher=None, temperature: float = 1.0, dkd=None) -> None:
+        if ids is None:
+            moe_head_ce_bwd(x, W, target, self.loss, self.lse, dloss, self.v_piece, self.dx, self.dW, self.ws)
+        else:
+            moe_head_distill_bwd(x, W, target, ids, teacher, temperature, self.loss, self.lse, self.lse_t, dloss, dkd,
+                                 self.v_piece, self.dx, self.dW, self.ws)
+
+
 def moe_prof_enable(on: bool) -> None:
     _check(load().moe_prof_enable(1 if on else 0), "moe_prof_enable")
 

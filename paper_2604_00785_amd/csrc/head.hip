@@ -29,22 +29,28 @@ struct Teacher { const int32_t* ids; const float* logits; float temperature; int
 __device__ __forceinline__ bool entry_there(int id, float l, int V) { return id >= 0 && id < V && l > -__builtin_inff(); }
 __device__ __forceinline__ bool target_there(int y, int V) { return y >= 0 && y < V; }
 
-// Which tokens have a loss, a bit each: a target, or (K > 0) an entry.  A workgroup takes 64 tokens.
-__global__ __launch_bounds__(256) void head_mask_kernel(const int32_t* __restrict__ target, Teacher t, int T, int V, uint64_t* __restrict__ mask) {
-  __shared__ int some[MOE_WAVE];
-  const int tid = threadIdx.x, t0 = blockIdx.x * 64;
-  if (tid < 64) some[tid] = t0 + tid < T && target_there(target[t0 + tid], V);
-  __syncthreads();
-  const int n = (T - t0 < 64 ? T - t0 : 64) * t.K;
-  const size_t at = static_cast<size_t>(t0) * t.K;
-#pragma unroll 8
-  for (int i = tid; i < n; i += 256)
-    if (entry_there(t.ids[at + i], t.logits[at + i], V)) some[i / t.K] = 1;
-  __syncthreads();
-  if (tid < 64) {
-    const uint64_t bits = __ballot(some[tid] != 0);
-    if (tid == 0) mask[blockIdx.x] = bits;
+// Which tokens have a loss, a bit each: a target, or (K > 0) an entry.  A workgroup takes 16 tokens, sixteen threads each.
+__global__ __launch_bounds__(256) void head_mask_kernel(const int32_t* __restrict__ target, Teacher t, int T, int V, uint16_t* __restrict__ mask) {
+  __shared__ uint32_t bits[4];
+  const int tid = threadIdx.x, l16 = tid & 15, token = blockIdx.x * 16 + (tid >> 4);
+  bool some = false;
+  if (token < T) {
+    some = l16 == 0 && target_there(target[token], V);
+    const size_t at = static_cast<size_t>(token) * t.K;
+#pragma unroll 4
+    for (int j = l16; j < t.K; j += 16) {
+      const int id = t.ids[at + j];
+      const float l = t.logits[at + j];
+      some = some || entry_there(id, l, V);
+    }
   }
+  const uint64_t any = __ballot(some);
+  uint32_t four = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) four |= (any >> (16 * k) & 0xFFFFu) != 0 ? 1u << k : 0u;
+  if (tid % MOE_WAVE == 0) bits[tid / MOE_WAVE] = four;
+  __syncthreads();
+  if (tid == 0) mask[blockIdx.x] = static_cast<uint16_t>(bits[0] | bits[1] << 4 | bits[2] << 8 | bits[3] << 12);
 }
 
 // What head_prep leaves for the kernels behind it, as integers: rows of the products from 0 to LIVE; those of dW, with the low parts, from 0
@@ -564,12 +570,16 @@ HeadShape head_dw_shape(int cols, int d, int rows, bool whole) {
   }
   return shape;
 }
-template <int S> double head_plain_time(int rows, int cols, int depth, double fixed) {
-  return head_time<S>(static_cast<double>(ceil_div(rows, S)) * ceil_div(cols, S), ceil_div(depth, BK), fixed);
-}
-int head_edge(int rows, int cols, int depth, double more256, double more128) {
-  return head_plain_time<128>(rows, cols, depth, TileCost<128>::FIXED + more128) <
-                 head_plain_time<256>(rows, cols, depth, TileCost<256>::FIXED + more256) ? 128 : 256;
+// The logits' products.  Their epilogues take the vector unit, which a tile of 256 leaves idle matrix cores beside and two of 128 share a compute unit for:
+// so narrow rows take 128 (more: what the epilogue of a tile of 256 costs beside that of a plain product, 3.0 at 128; K steps of 1.4 us).  256 / 128 in us,
+// sums (gradient): 3799 tokens, d 256, V 50524 169 / 160 (215 / 191); 1597, 64, 25439 34 / 29 (48 / 37); 3372, 576, 43471 202 / 197 (239 / 217);
+// 1420, 3968, 58453 516 / 728 (541 / 749); 8192, 2048, 50304 1201 / 1535 (1331 / 1736).
+int logits_edge(int rows, int cols, int d, double more) {
+  const auto time = [&](auto edge, double fixed) {
+    constexpr int S = decltype(edge)::value;
+    return head_time<S>(static_cast<double>(ceil_div(rows, S)) * ceil_div(cols, S), ceil_div(d, BK), fixed);
+  };
+  return time(IC<128>{}, TileCost<128>::FIXED + 3.0) < time(IC<256>{}, TileCost<256>::FIXED + more) ? 128 : 256;
 }
 
 // What the workspace holds, by offset.
@@ -626,7 +636,8 @@ int run_prep(const HeadCall& c, const HeadLayout& l, const DxRule& dx, long long
   uint64_t* mask = nullptr;
   if (c.T > SELF_MASK_TOKENS || static_cast<long long>(c.T) * (c.t.K + 1) > SELF_MASK_LOADS) {
     mask = reinterpret_cast<uint64_t*>(c.ws + l.mask);
-    MOE_LAUNCH("head_mask", head_mask_kernel, dim3((c.T + 63) / 64), dim3(256), 0, c.s, c.target, c.t, c.T, c.V, mask);
+    MOE_LAUNCH("head_mask", head_mask_kernel, dim3((c.T + 63) / 64 * 4), dim3(256), 0, c.s, c.target, c.t, c.T, c.V,
+               reinterpret_cast<uint16_t*>(mask));
   }
   HeadPrepArgs p{};
   p.x = c.x; p.target = c.target; p.t = c.t; p.mask = mask; p.T = c.T; p.d = c.d; p.V = c.V; p.strips = l.strips64;
@@ -699,7 +710,7 @@ int run_head_fwd(const HeadCall& c, int* edges) {
   } else if ((rc = run_prep(c, l, DxRule{}, 0)) != MOE_OK) {
     return rc;
   }
-  const int edge = settle_edge(edges, head_edge(c.T, c.V, c.d, 6.0, 3.0));
+  const int edge = settle_edge(edges, logits_edge(c.T, c.V, c.d, 9.5));
   h.strips = ceil_div(c.V, edge / 2);
   h.part = reinterpret_cast<float*>(c.ws + l.big);
   if ((rc = launch_head<HEAD_STATS>(a, h, edge, c.T, c.V, "gemm_head_stats", c.s)) != MOE_OK) return rc;
@@ -739,7 +750,7 @@ int run_head_bwd(const HeadCall& c, int v_piece, int* edges) {
     h.lo = l.low;
     const uint16_t* W = c.W + static_cast<size_t>(v0) * c.d;
     a.A0 = reinterpret_cast<const uint16_t*>(c.ws + l.xc); a.A1 = c.x; a.B0 = W; a.O0 = dz; a.K = c.d; a.N = cols; a.M = ld;
-    rc = launch_head<HEAD_DZ>(a, h, settle_edge(edges, head_edge(c.T, cols, c.d, 6.0, 3.0)), c.T, cols, "gemm_head_dz", c.s);
+    rc = launch_head<HEAD_DZ>(a, h, settle_edge(edges, logits_edge(c.T, cols, c.d, 10.8)), c.T, cols, "gemm_head_dz", c.s);
     if (rc != MOE_OK) return rc;
     GemmArgs b{};
     b.offsets = a.offsets; b.row_token = control + DX_PARTS;

@@ -290,3 +290,57 @@ def test_gradients_may_be_negative_zero_or_large():
     a["dkd"][::2] = 0
     a["dloss"][1::3] *= -3e4
     compare(a, run(a, 1.5), 1.5)
+
+
+@pytest.mark.parametrize("T,K", [(60, 0), (60, 7), (500, 0), (500, 7)])
+def test_nothing_of_a_token_without_a_loss_is_looked_at(T, K):
+    """NaN wherever a masked token or an entry that does not count has a number."""
+    a = make(T, 64, 300, K, masked=0.4, seed=16)
+    out = a["target"] < 0
+    a["target"][0], out[0] = 5, False
+    clean = compare(a, run(a, 1.5), 1.5)
+    nan = float("nan")
+    a["x"][out] = nan
+    a["dloss"][out] = nan
+    if K:
+        a["dkd"][out] = nan
+        a["teacher"][a["ids"] < 0] = nan
+    got = run(a, 1.5)
+    a["x"][out] = 0
+    a["dloss"][out] = 0
+    if K:
+        a["dkd"][out] = 0
+        a["teacher"][a["ids"] < 0] = 0
+    compare(a, got, 1.5)
+    assert torch.equal(clean["loss"], R.head(a["x"], a["W"], a["target"])[0]["loss"])
+
+
+def test_offsets_past_32_bits():
+    """A gradient of the logits of 5.8 GB (and 2.9e9 elements), checked at tokens and columns from all over it."""
+    T, d, V = 72000, 64, 40001
+    g = torch.Generator(device=DEV).manual_seed(17)
+    x = torch.randn(T, d, generator=g, device=DEV).bfloat16()
+    W = (0.1 * torch.randn(V, d, generator=g, device=DEV)).bfloat16()
+    target = torch.randint(0, V, (T,), generator=g, device=DEV).int()
+    dloss = torch.rand(T, generator=g, device=DEV) / T
+    loss, lse = torch.empty(T, device=DEV), torch.empty(T, device=DEV)
+    dx, dW = torch.empty(T, d, dtype=BF, device=DEV), torch.empty(V, d, dtype=BF, device=DEV)
+    piece = (V + 255) // 256 * 256
+    ws = torch.empty(max(B.moe_head_fwd_workspace_bytes(T, d, V), B.moe_head_bwd_workspace_bytes(T, d, V, 0, piece)), dtype=torch.uint8, device=DEV)
+    assert T * piece * 2 > 2 ** 32 and ws.numel() > T * piece * 2
+    B.moe_head_ce_fwd(x, W, target, loss, lse, ws)
+    B.moe_head_ce_bwd(x, W, target, loss, lse, dloss, piece, dx, dW, ws)
+    rows = torch.cat([torch.arange(0, T, 1999), torch.tensor([T - 1])])
+    few = {"x": x[rows.to(DEV)].cpu(), "W": W.cpu(), "target": target[rows.to(DEV)].cpu(), "dloss": dloss[rows.to(DEV)].cpu()}
+    want, bound = R.head(few["x"], few["W"], few["target"], dloss=few["dloss"])
+    for k, v in (("loss", loss), ("lse", lse), ("dx", dx)):
+        R.check(v[rows.to(DEV)], want[k], bound[k], k)
+    # columns: the gradient over all tokens, in 64 bits, with the log of the sums checked above
+    cols = torch.cat([torch.arange(0, V, 4003), torch.tensor([V - 1])]).to(DEV)
+    z = x.double() @ W[cols].double().t()
+    dz = (z - lse.double()[:, None]).exp() - (target[:, None] == cols[None, :]).double()
+    dz *= dloss.double()[:, None]
+    ref = dz.t() @ x.double()
+    # (the factor of dz's rounding, its exponential's and the sum's: T terms)
+    off = (R.HALF16 + 2.0 ** -16 + T * R.HALF32) * (dz.abs().t() @ x.double().abs()) + R.HALF16 * ref.abs()
+    R.check(dW[cols], ref.cpu(), off.cpu(), "dW")
