@@ -135,7 +135,7 @@ struct GemmArgs {
   int N;                // output columns (per half for GATE_UP)
   int n_tiles;          // column tiles
   int m_tiles_cap;      // upper bound on row tiles (row-grouped products); row tiles of one dW (WGRAD)
-  int stream_rows;      // GATE_UP, DOWN: nothing is done where there are at most this many rows (0: always): a launch of
+  int stream_rows;      // HEAD_DX: not zero = onto the sums that are there.  GATE_UP, DOWN: nothing is done where there are at most this many rows (0: always): a launch of
                         // the streaming kernel in front has done it
   // WGRAD: out[e][M][N] = sum over the expert's rows of A[r][M] * B[r][N]
   int M;
@@ -157,7 +157,6 @@ struct HeadArgs {
   int two;                    // both sums, both terms
   int strips, list_ld, slots;
   int col0;                   // vocabulary column of the product's first
-  int add;                    // HEAD_DX: onto what is there
   int lo;                     // HEAD_DZ: what rounding loses is stored too, in as many rows behind the others
 };
 
@@ -377,11 +376,15 @@ struct TileState {
   const int32_t* row_tok;       // gathered operand: token of the expert's first reduction row onwards
 };
 
+// How dW's tiles are dealt behind dx's (see head_deal): `extra` tiles of this workgroup's own, from `first` on in steps of `by`, then
+// those behind the first `skipped`, in turn with all workgroups.
+struct Deal { int extra, first, by, skipped; };
+
 // One product's tile list, walked by this workgroup from list position first_tile in steps of
 // gridDim.x.  Returns the position at which the workgroup left the list, counted from its end:
 // where it enters a list that follows in the same launch.
 template <int MODE, int S, int ARG>
-__device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile) {
+__device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile, Deal deal = {}) {
   using TL = Tile<S>;
   using TileState = TileState<S>;
   constexpr int NL = TL::NL, NB = TL::NB, HALF = TL::HALF, TILE_BYTES = TL::BYTES;
@@ -1627,8 +1630,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
       // a part's sums in 32 bits, behind those of the parts before it
       float* const out = reinterpret_cast<float*>(MODE == HEAD_DX ? ae->O0 : ae->O1) + static_cast<size_t>(t.e) * (MODE == HEAD_DX ? ae->offsets[1] : ae->K) * ncol;
       const Rsrc oo = rows_of(out, ncol * 4);
-      bool add = false;
-      if constexpr (MODE == HEAD_DX) add = head_args()->add != 0;
+      const bool add = MODE == HEAD_DX && ae->stream_rows != 0;
       static_for<NB>([&](auto i_tag) {
         constexpr int i = decltype(i_tag)::value;
         if (i * 16 >= rows) return;
@@ -1694,8 +1696,9 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
   const int run = static_cast<int>(gridDim.x >> 3);
   const int whole_runs = total / run;
   int block = first_tile / run, place = first_tile - block * run;
+  if constexpr (MODE == HEAD_DW) tile = deal.extra > 0 ? deal.first : deal.skipped + first_tile;
   auto list_entry = [&]() __attribute__((always_inline)) {
-    if (block >= whole_runs) return tile;
+    if (MODE == HEAD_DW || block >= whole_runs) return tile;
     return (mix ? ((block & 1) ? whole_runs - 1 - (block >> 1) : (block >> 1)) : block) * run + place;
   };
   if (tile < total) {
@@ -1720,7 +1723,14 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile)
       }
       if constexpr (is_logits(MODE)) fetch_items(cur);
       Finished done{cur.e, cur.m0, cur.n0, cur.r0, cur.m_wave, 0, 4, cur.second};
-      tile += gridDim.x;
+      if constexpr (MODE == HEAD_DW) {
+        if (deal.extra > 1) tile += deal.by;
+        else if (deal.extra == 1) tile = deal.skipped + first_tile;
+        else tile += gridDim.x;
+        deal.extra -= deal.extra > 0;
+      } else {
+        tile += gridDim.x;
+      }
       const bool more = tile < total;
       if (more) {
         block += 8;
@@ -1766,6 +1776,46 @@ __device__ __forceinline__ int first_list_position() {
 template <int MODE, int S>
 __global__ __launch_bounds__(GEMM_THREADS, Tile<S>::PER_CU) void grouped_gemm_kernel(GemmArgs a) {
   gemm_tile_list<MODE, S, 0>(a, first_list_position());
+}
+
+// The constants of the model of a tile's time (see below, where tile edges are chosen).
+template <int S> struct TileCost;
+template <> struct TileCost<256> { static constexpr double FIXED = 5.2, WGRAD = 6.0, STEP = 1.0, SWIGLU_BWD = 16.0, RAGGED = 0.5; };
+template <> struct TileCost<128> { static constexpr double FIXED = 2.7, WGRAD = 3.8, STEP = 0.75, SWIGLU_BWD = 9.0, RAGGED = 0.8; };
+
+// dx and dW of the head in one launch.  dx has few tiles with long reductions: in the last round of them `idle` workgroups have none, and take
+// as many tiles of dW as fit into that time; the rest is dealt to all in turn, to those first that have waited.
+struct HeadDeal { int idle, extra; };
+__host__ __device__ __forceinline__ HeadDeal head_deal(int dx_tiles, float dx_each, int dw_tiles, float dw_each, int places) {
+  const int rest = dx_tiles % places;
+  if (rest == 0) return {places, 0};
+  const int idle = places - rest, fit = static_cast<int>(dx_each / dw_each), most = dw_tiles / idle;
+  return {idle, fit < most ? fit : most};
+}
+template <int S> __host__ __device__ __forceinline__ float head_dx_each(int steps, int parts) {
+  return static_cast<float>(TileCost<S>::FIXED) + static_cast<float>(TileCost<S>::STEP) * static_cast<float>(steps) / static_cast<float>(parts);
+}
+template <int S> __host__ __device__ __forceinline__ float head_dw_each(int steps, int parts) {
+  return static_cast<float>(TileCost<S>::WGRAD) + 1.1f * static_cast<float>(TileCost<S>::STEP) * static_cast<float>(steps) / static_cast<float>(parts);
+}
+// How long the two take together, in the model's units: half the workgroup that ends last, half the mean (idle units leave the others power).
+__host__ __device__ __forceinline__ float head_bwd_time(int dx_tiles, float dx_each, int dw_tiles, float dw_each, int places) {
+  const HeadDeal deal = head_deal(dx_tiles, dx_each, dw_tiles, dw_each, places);
+  const int rounds = dx_tiles / places, left = dw_tiles - deal.idle * deal.extra, whole = left / places, rest = left - whole * places;
+  float last = rounds * dx_each + (deal.extra + whole + (rest > 0 ? 1 : 0)) * dw_each;
+  if (dx_tiles > rounds * places) {
+    const float busy = (rounds + 1) * dx_each + (whole + (rest > deal.idle ? 1 : 0)) * dw_each;
+    last = busy > last ? busy : last;
+  }
+  return 0.5f * (last + (dx_tiles * dx_each + dw_tiles * dw_each) / places);
+}
+template <int S>
+__global__ __launch_bounds__(GEMM_THREADS, Tile<S>::PER_CU) void grouped_gemm_head_bwd_kernel(GemmArgs a, GemmArgs b) {
+  const int next = gemm_tile_list<HEAD_DX, S, 0>(a, first_list_position());
+  const int parts = a.row_token[0], dx_tiles = (a.offsets[1] + S - 1) / S * a.n_tiles * parts, dw_tiles = b.E * b.m_tiles_cap * b.n_tiles;
+  const HeadDeal d = head_deal(dx_tiles, head_dx_each<S>((a.M + BK - 1) / BK, parts), dw_tiles, head_dw_each<S>((b.offsets[1] + BK - 1) / BK, b.E), gridDim.x);
+  const int extra = __builtin_amdgcn_readfirstlane(d.extra);
+  gemm_tile_list<HEAD_DW, S, 1>(b, next, Deal{next < d.idle ? extra : 0, next, d.idle, d.idle * extra});
 }
 
 template <int MODE, int S>
@@ -1846,6 +1896,15 @@ int launch_gemm_head(const GemmArgs& a, const HeadArgs& h, long long max_tiles, 
   return moe_check_launch();
 }
 
+template <int S>
+int launch_gemm_head_bwd(const GemmArgs& a, const GemmArgs& b, long long max_tiles, hipStream_t s, const char* name) {
+  const dim3 grid(persistent_grid<S>(max_tiles));
+  static bool configured[MAX_DEVICES] = {};
+  if (configure_lds(&grouped_gemm_head_bwd_kernel<S>, Tile<S>::LDS, configured) != MOE_OK) return MOE_ERR_LAUNCH;
+  MOE_LAUNCH(name, (grouped_gemm_head_bwd_kernel<S>), grid, dim3(GEMM_THREADS), Tile<S>::LDS, s, a, b);
+  return moe_check_launch();
+}
+
 template <int MODE_A, int MODE_B, int S>
 int launch_gemm_pair(const GemmArgs& a, const GemmArgs& b, long long max_tiles, hipStream_t s, const char* name) {
   const dim3 grid(persistent_grid<S>(max_tiles));
@@ -1895,9 +1954,6 @@ long long count_tiles(GemmArgs& a, int R_cap) {
 //   1500 tokens, d 2048, f 1024, 64 experts, 8             156 / 166    72 / 84    165 / 196   312 / 361
 //   2048 tokens of the same layer                          163 / 204    91 / 110   222 / 245   350 / 422
 //   8192 tokens of the same layer                          470 / 646   263 / 324   557 / 683   876 / 1214
-template <int S> struct TileCost;
-template <> struct TileCost<256> { static constexpr double FIXED = 5.2, WGRAD = 6.0, STEP = 1.0, SWIGLU_BWD = 16.0, RAGGED = 0.5; };
-template <> struct TileCost<128> { static constexpr double FIXED = 2.7, WGRAD = 3.8, STEP = 0.75, SWIGLU_BWD = 9.0, RAGGED = 0.8; };
 struct ListCost { double tiles, each; };
 // rows: routed rows to expect
 template <int MODE, int S>

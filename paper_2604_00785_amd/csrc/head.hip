@@ -57,15 +57,18 @@ __global__ __launch_bounds__(256) void head_mask_kernel(const int32_t* __restric
 // to DW_ROWS; whether x itself holds the rows.
 enum { ROWS = 0, LIVE = 1, DW_ROWS = 3, DIRECT = 4, DX_PARTS = 5, CONTROL_INTS = 6 };
 
-// Parts of dx's reduction for `rows` rows, at most `most`: with few tiles a part each to as many compute units as there are.  The time expected of p parts,
-// in K steps of the tile: whole rounds of the chip's places (half of it by the rounds, half by what they hold, since idle units leave the others
-// power), what a tile costs beside its steps, and each part's sums written and read.  Lane p - 1 of a wave weighs p parts.
-struct DxRule { int edge, places, d, steps, most; float fixed, step; };
-__device__ __forceinline__ int dx_parts(const DxRule& x, int rows, int lane) {
+// Parts of dx's reduction for `rows` rows, at most `most`: the number with which dx and dW together take least time (head_bwd_time), each part's sums
+// being written and read besides (8 bytes an element, 7 MB in the model's unit of time).  Lane p - 1 of a wave weighs p parts.
+struct BwdRule { int edge, places, d, steps, most, dw_tiles, dw_parts, low; };
+template <int S> __device__ __forceinline__ float bwd_time_of(const BwdRule& x, int rows, int p) {
+  const int tiles = (rows + S - 1) / S * ((x.d + S - 1) / S) * p;
+  return head_bwd_time(tiles, head_dx_each<S>(x.steps, p), x.dw_tiles, head_dw_each<S>(((x.low ? 2 : 1) * rows + BK - 1) / BK, x.dw_parts), x.places) +
+         p * (static_cast<float>(rows) * x.d / 1.0e6f);
+}
+__device__ __forceinline__ int dx_parts(const BwdRule& x, int rows, int lane) {
   const int p = lane + 1;
-  const float tiles = static_cast<float>((rows + x.edge - 1) / x.edge) * ((x.d + x.edge - 1) / x.edge) * p, rounds = tiles / x.places;
-  const float time = 0.5f * (rounds + fmaxf(1.f, floorf(rounds + 0.95f))) * (x.fixed + x.step * x.steps / p) + p * (static_cast<float>(rows) * x.d / 1.0e6f);
-  const uint32_t key = p <= x.most && (p == 1 || x.steps / p >= 4) ? __float_as_uint(time) & ~63u | static_cast<uint32_t>(lane) : ~0u;
+  const float time = x.edge == 256 ? bwd_time_of<256>(x, rows, p) : bwd_time_of<128>(x, rows, p);
+  const uint32_t key = p <= x.most && (p == 1 || x.steps / p >= 4) ? (__float_as_uint(time) & ~63u) | static_cast<uint32_t>(lane) : ~0u;
   return 1 + (group_reduce<MOE_WAVE>(key, [](uint32_t u, uint32_t v) __attribute__((always_inline)) { return u < v ? u : v; }) & 63u);
 }
 
@@ -76,7 +79,7 @@ struct HeadPrepArgs {
   const uint64_t* mask;            // null: found here
   int T, d, V, strips;             // strips: of 64 columns
   int low;                         // rows of x twice
-  DxRule dx;
+  BwdRule dx;
   long long dx_room;               // rows that the parts' sums have room for, together
   int32_t* target_row;             // the rows' targets
   int32_t *control, *row_token, *token_row;
@@ -146,7 +149,7 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     a.control[DIRECT] = direct;
   }
   if (lists && blockIdx.x == 0 && wave == 0 && a.row != nullptr) {
-    DxRule x = a.dx;
+    BwdRule x = a.dx;
     const long long room = live > 0 ? a.dx_room / live : 1;
     x.most = room < 64 ? static_cast<int>(room) : 64;
     const int parts = dx_parts(x, live > 0 ? live : 1, lane);
@@ -540,34 +543,29 @@ template <int S> double head_time(double tiles, double steps, double fixed) {
   const double each = fixed + TileCost<S>::STEP * steps;
   return (0.5 * rounds + 0.5 * (whole < 1.0 ? 1.0 : whole)) * each;
 }
-struct HeadShape { int edge, parts; };
-template <int S> void head_parts(int rows, int d, int depth, double more, double& best, HeadShape& shape) {
-  const double tiles = static_cast<double>(ceil_div(rows, S)) * ceil_div(d, S);
-  const int steps = ceil_div(depth, BK);
-  for (int p = 1; p <= 64 && (p == 1 || steps / p >= 4); ++p) {
-    const double time = head_time<S>(tiles * p, static_cast<double>(steps) / p, TileCost<S>::FIXED + more) + p * (static_cast<double>(rows) * d / 1.0e6);   // as dx_parts
-    if (time < best) { best = time; shape = {S, p}; }
+// The backward products of `cols` columns: their tiles' edge and the parts of either reduction, dW's in more than one only where its tiles do not fill the
+// chip, and not in pieces of the vocabulary (`whole`), whose sums would have to be rounded one by one.  The parts of dx are those for all T
+// tokens; they are chosen again for the tokens that have a loss, in the room that these leave.
+struct BwdShape { int edge, dx_parts, dw_parts; };
+template <int S> void weigh_bwd(int T, int d, int cols, int depth, bool whole, double& best, BwdShape& shape) {
+  const int places = HEAD_CUS * Tile<S>::PER_CU, wide = ceil_div(d, S), steps = ceil_div(cols, BK), dw_steps = ceil_div(depth, BK);
+  const long long dx_tiles = static_cast<long long>(ceil_div(T, S)) * wide, dw_tiles = static_cast<long long>(ceil_div(cols, S)) * wide;
+  int q = 1;
+  if (whole) while (dw_tiles * (q + 1) <= places && dw_steps / (q + 1) >= 4) ++q;
+  constexpr int some[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 56, 64};
+  for (int p : some) {
+    if (p > 1 && (steps / p < 4 || dx_tiles * p > 8ll * places)) break;
+    const double time = head_bwd_time(static_cast<int>(dx_tiles * p), head_dx_each<S>(steps, p), static_cast<int>(dw_tiles * q), head_dw_each<S>(dw_steps, q), places) +
+                        (static_cast<double>(p) * T + (q > 1 ? static_cast<double>(q) * cols : 0.0)) * d / 1.0e6;
+    if (time < best) { best = time; shape = {S, p, q}; }
   }
 }
-// dx: the edge for all T tokens; the parts are chosen again for those that have a loss, in the room that this number leaves.
-HeadShape head_dx_shape(int T, int d, int cols) {
-  HeadShape shape{128, 1};
+BwdShape head_bwd_shape(int T, int d, int cols, bool whole) {
+  BwdShape shape{128, 1, 1};
   double best = 1e300;
-  head_parts<256>(T, d, cols, 0.0, best, shape);
-  head_parts<128>(T, d, cols, 0.0, best, shape);
-  return shape;
-}
-// dW of `cols` columns of the vocabulary.  One part needs no sums beside it: where the reduction is in parts it has to be worth more than they cost.
-HeadShape head_dw_shape(int cols, int d, int rows, bool whole) {
-  HeadShape shape{128, 1};
-  double best = 1e300;
-  head_parts<256>(cols, d, rows, 0.8, best, shape);
-  head_parts<128>(cols, d, rows, 1.1, best, shape);
-  if (!whole || shape.parts == 1) {
-    const double one256 = head_time<256>(static_cast<double>(ceil_div(cols, 256)) * ceil_div(d, 256), ceil_div(rows, BK), TileCost<256>::FIXED + 0.8);
-    const double one128 = head_time<128>(static_cast<double>(ceil_div(cols, 128)) * ceil_div(d, 128), ceil_div(rows, BK), TileCost<128>::FIXED + 1.1);
-    shape = {one128 < one256 ? 128 : 256, 1};
-  }
+  const int depth = T <= LOW_TOKENS ? 2 * T : T;
+  weigh_bwd<256>(T, d, cols, depth, whole, best, shape);
+  weigh_bwd<128>(T, d, cols, depth, whole, best, shape);
   return shape;
 }
 // The logits' products.  Their epilogues take the vector unit, which a tile of 256 leaves idle matrix cores beside and two of 128 share a compute unit for:
@@ -632,7 +630,7 @@ struct HeadCall {
   hipStream_t s;
 };
 
-int run_prep(const HeadCall& c, const HeadLayout& l, const DxRule& dx, long long dx_room) {
+int run_prep(const HeadCall& c, const HeadLayout& l, const BwdRule& dx, long long dx_room) {
   uint64_t* mask = nullptr;
   if (c.T > SELF_MASK_TOKENS || static_cast<long long>(c.T) * (c.t.K + 1) > SELF_MASK_LOADS) {
     mask = reinterpret_cast<uint64_t*>(c.ws + l.mask);
@@ -682,11 +680,11 @@ void fill_head(const HeadCall& c, const HeadLayout& l, GemmArgs& a, HeadArgs& h)
   h.list_ld = l.strips64 + 1;
   h.slots = l.slots;
 }
-template <int MODE> int launch_head(GemmArgs& a, const HeadArgs& h, int edge, int rows, int cols, const char* name, hipStream_t s) {
-  a.n_tiles = ceil_div(cols, edge);
-  a.m_tiles_cap = ceil_div(rows, edge);
-  const long long tiles = static_cast<long long>(a.n_tiles) * a.m_tiles_cap * (MODE == HEAD_DX ? 64 : a.E);
-  if (tiles > 0x7FFFFFFFll / 2) return MOE_ERR_INVALID;
+bool too_many(long long tiles) { return tiles > 0x7FFFFFFFll / 2; }
+template <int MODE> int launch_logits(GemmArgs& a, const HeadArgs& h, int edge, int rows, const char* name, hipStream_t s) {
+  a.n_tiles = ceil_div(a.N, edge);
+  const long long tiles = static_cast<long long>(a.n_tiles) * ceil_div(rows, edge);
+  if (too_many(tiles)) return MOE_ERR_INVALID;
   return edge == 128 ? launch_gemm_head<MODE, 128>(a, h, tiles, s, name) : launch_gemm_head<MODE, 256>(a, h, tiles, s, name);
 }
 // For tests: the edge of a launch's tiles on entry (0: the rule decides), the one that it ran with on return.
@@ -707,13 +705,13 @@ int run_head_fwd(const HeadCall& c, int* edges) {
   if (all) {
     a.offsets = nullptr; a.row_token = nullptr; a.A0 = c.x; a.M = c.T;
     h.target = c.target;
-  } else if ((rc = run_prep(c, l, DxRule{}, 0)) != MOE_OK) {
+  } else if ((rc = run_prep(c, l, BwdRule{}, 0)) != MOE_OK) {
     return rc;
   }
   const int edge = settle_edge(edges, logits_edge(c.T, c.V, c.d, 9.5));
   h.strips = ceil_div(c.V, edge / 2);
   h.part = reinterpret_cast<float*>(c.ws + l.big);
-  if ((rc = launch_head<HEAD_STATS>(a, h, edge, c.T, c.V, "gemm_head_stats", c.s)) != MOE_OK) return rc;
+  if ((rc = launch_logits<HEAD_STATS>(a, h, edge, c.T, "gemm_head_stats", c.s)) != MOE_OK) return rc;
   const HeadJoinArgs j{h.part, all ? nullptr : reinterpret_cast<const int32_t*>(c.ws + l.control), reinterpret_cast<const int32_t*>(c.ws + l.row_token),
                        reinterpret_cast<const int32_t*>(c.ws + l.target_slot), c.target, c.T, h.item, c.t, h.strips, c.V, c.loss, c.lse, c.kd, c.lse_t,
                        h.c1, h.c2};
@@ -726,21 +724,20 @@ int run_head_fwd(const HeadCall& c, int* edges) {
 
 int run_head_bwd(const HeadCall& c, int v_piece, int* edges) {
   const HeadLayout l = head_layout(c.T, c.d, c.V, c.t.K, true);
-  const int piece = head_piece(c.T, c.V, v_piece);
+  const int piece = head_piece(c.T, c.V, v_piece), wanted = edges != nullptr ? edges[1] : 0;
   uint16_t* dz = reinterpret_cast<uint16_t*>(c.ws + l.big);
   float* part = reinterpret_cast<float*>(c.ws + l.big + head_dz_bytes(c.T, piece));
-  const HeadShape dxs = head_dx_shape(c.T, c.d, piece);
-  const int dx_edge = settle_edge(edges != nullptr ? edges + 1 : nullptr, dxs.edge);
+  BwdShape shape = head_bwd_shape(c.T, c.d, piece, piece >= c.V);
+  float* dw_part = part + static_cast<size_t>(shape.dx_parts) * c.T * c.d;
+  if (wanted != 0) shape.edge = wanted;
+  if (edges != nullptr) edges[1] = shape.edge;
+  const int places = HEAD_CUS * 256 / shape.edge, wide = ceil_div(c.d, shape.edge);
   // (the parts are those of all pieces: no more than the smallest, the last, has steps for)
   const int last = c.V - (c.V - 1) / piece * piece;
-  const bool large = dx_edge == 256;
-  const DxRule rule{dx_edge, HEAD_CUS * 256 / dx_edge, c.d, ceil_div(last, BK), 0, static_cast<float>(large ? TileCost<256>::FIXED : TileCost<128>::FIXED),
-                    static_cast<float>(large ? TileCost<256>::STEP : TileCost<128>::STEP)};
-  int rc = run_prep(c, l, rule, static_cast<long long>(dxs.parts) * c.T);
+  const BwdRule rule{shape.edge, places, c.d, ceil_div(last, BK), 0, ceil_div(last, shape.edge) * wide * shape.dw_parts, shape.dw_parts, l.low};
+  int rc = run_prep(c, l, rule, static_cast<long long>(shape.dx_parts) * c.T);
   if (rc != MOE_OK) return rc;
   const int32_t* control = reinterpret_cast<const int32_t*>(c.ws + l.control);
-  const HeadShape dws = head_dw_shape(piece, c.d, l.low ? 2 * c.T : c.T, piece >= c.V);
-  float* dw_part = part + static_cast<size_t>(dxs.parts) * c.T * c.d;
   for (int v0 = 0; v0 < c.V; v0 += piece) {
     const int cols = c.V - v0 < piece ? c.V - v0 : piece, ld = (cols + 63) & ~63;
     GemmArgs a{};
@@ -750,24 +747,26 @@ int run_head_bwd(const HeadCall& c, int v_piece, int* edges) {
     h.lo = l.low;
     const uint16_t* W = c.W + static_cast<size_t>(v0) * c.d;
     a.A0 = reinterpret_cast<const uint16_t*>(c.ws + l.xc); a.A1 = c.x; a.B0 = W; a.O0 = dz; a.K = c.d; a.N = cols; a.M = ld;
-    rc = launch_head<HEAD_DZ>(a, h, settle_edge(edges, logits_edge(c.T, cols, c.d, 10.8)), c.T, cols, "gemm_head_dz", c.s);
+    rc = launch_logits<HEAD_DZ>(a, h, settle_edge(edges, logits_edge(c.T, cols, c.d, 10.8)), c.T, "gemm_head_dz", c.s);
     if (rc != MOE_OK) return rc;
     GemmArgs b{};
-    b.offsets = a.offsets; b.row_token = control + DX_PARTS;
+    b.offsets = a.offsets; b.row_token = control + DX_PARTS; b.stream_rows = v0 > 0;
     b.A0 = dz; b.B0 = W; b.O0 = reinterpret_cast<uint16_t*>(part); b.K = ld; b.M = cols; b.N = c.d;
-    h.add = v0 > 0;
-    if ((rc = launch_head<HEAD_DX>(b, h, dx_edge, c.T, c.d, "gemm_head_dx", c.s)) != MOE_OK) return rc;
     GemmArgs w{};
-    w.offsets = control + DW_ROWS - 1; w.E = dws.parts; w.row_token = a.row_token; w.O1 = reinterpret_cast<uint16_t*>(dw_part);
+    w.offsets = control + DW_ROWS - 1; w.E = shape.dw_parts; w.row_token = a.row_token; w.O1 = reinterpret_cast<uint16_t*>(dw_part);
     w.A0 = dz; w.B0 = a.A0; w.B1 = a.A1; w.O0 = c.dW + static_cast<size_t>(v0) * c.d; w.M = ld; w.K = cols; w.N = c.d;
-    rc = launch_head<HEAD_DW>(w, h, settle_edge(edges != nullptr ? edges + 2 : nullptr, dws.edge), cols, c.d, "gemm_head_dw", c.s);
+    b.n_tiles = w.n_tiles = wide;
+    w.m_tiles_cap = ceil_div(cols, shape.edge);
+    const long long dw_tiles = static_cast<long long>(wide) * w.m_tiles_cap * w.E, tiles = dw_tiles + 64ll * ceil_div(c.T, shape.edge) * wide;
+    if (too_many(tiles)) return MOE_ERR_INVALID;
+    rc = shape.edge == 128 ? launch_gemm_head_bwd<128>(b, w, tiles, c.s, "gemm_head_dx+dw") : launch_gemm_head_bwd<256>(b, w, tiles, c.s, "gemm_head_dx+dw");
     if (rc != MOE_OK) return rc;
   }
   const size_t n = static_cast<size_t>(c.T) * (c.d / 8);
   const HeadDxArgs x{part, control, reinterpret_cast<const int32_t*>(c.ws + l.token_row), reinterpret_cast<const int32_t*>(c.ws + l.target_slot), c.target,
                      reinterpret_cast<const float*>(c.ws + l.item), c.t, c.W, c.T, c.d, c.V, c.T <= LOW_TOKENS, c.dx,
-                     dw_part, dws.parts, static_cast<int>((n + 255) / 256), c.dW};
-  const size_t groups = x.dx_groups + (dws.parts > 1 ? (static_cast<size_t>(c.V) * (c.d / 8) + 255) / 256 : 0);
+                     dw_part, shape.dw_parts, static_cast<int>((n + 255) / 256), c.dW};
+  const size_t groups = x.dx_groups + (shape.dw_parts > 1 ? (static_cast<size_t>(c.V) * (c.d / 8) + 255) / 256 : 0);
   MOE_LAUNCH("head_dx", head_dx_kernel, dim3(static_cast<unsigned>(groups)), dim3(256), 0, c.s, x);
   return moe_check_launch();
 }
@@ -788,13 +787,13 @@ extern "C" size_t moe_head_fwd_workspace_bytes(int T, int d, int V, int K) {
 extern "C" size_t moe_head_bwd_workspace_bytes(int T, int d, int V, int K, int v_piece) {
   if (bad_head_dims(T, d, V, K) || v_piece < 0 || v_piece % 256 != 0) return 0;
   const int piece = head_piece(T, V, v_piece);
-  const int dw_parts = head_dw_shape(piece, d, T <= LOW_TOKENS ? 2 * T : T, piece >= V).parts;
+  const BwdShape shape = head_bwd_shape(T, d, piece, piece >= V);
   return head_layout(T, d, V, K, true).big + head_dz_bytes(T, piece) +
-         (static_cast<size_t>(head_dx_shape(T, d, piece).parts) * T + (dw_parts > 1 ? static_cast<size_t>(dw_parts) * V : 0)) * d * sizeof(float);
+         (static_cast<size_t>(shape.dx_parts) * T + (shape.dw_parts > 1 ? static_cast<size_t>(shape.dw_parts) * V : 0)) * d * sizeof(float);
 }
 
 // Both losses, or (ids null, K 0) the cross entropy alone: what the calls of moe_hotpath.h come to.  edges, for tests: as in gemm.h, of the
-// logits' launch, then (backward) of dx and dW.
+// logits' launch, then (backward) of dx and dW together.
 namespace {
 bool bad_edge_list(const int* edges, int n) {
   for (int i = 0; edges != nullptr && i < n; ++i) if (edges[i] != 0 && edges[i] != 128 && edges[i] != 256) return true;
@@ -816,7 +815,7 @@ extern "C" int moe_head_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t*
 extern "C" int moe_head_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, const int32_t* ids, const float* teacher, float temperature,
                             const float* loss, const float* lse, const float* lse_t, const float* dloss, const float* dkd, int T, int d, int V, int K,
                             int v_piece, moe_bf16* dx, moe_bf16* dW, void* ws, size_t ws_bytes, void* stream, int* edges) {
-  if (bad_head_dims(T, d, V, K) || bad_temperature(temperature) || v_piece < 0 || v_piece % 256 != 0 || bad_edge_list(edges, 3)) return MOE_ERR_INVALID;
+  if (bad_head_dims(T, d, V, K) || bad_temperature(temperature) || v_piece < 0 || v_piece % 256 != 0 || bad_edge_list(edges, 2)) return MOE_ERR_INVALID;
   if (bad_ptrs({x, W, target, loss, lse, dloss, dx, dW, ws}) || (K > 0 && bad_ptrs({ids, teacher, lse_t, dkd}))) return MOE_ERR_INVALID;
   if (ws_bytes < moe_head_bwd_workspace_bytes(T, d, V, K, v_piece)) return MOE_ERR_WORKSPACE;
   HeadCall c{};
