@@ -16,7 +16,9 @@ namespace {
 
 constexpr int HEAD_MAX_V = 1 << 20, HEAD_MAX_K = 1024;
 constexpr int HEAD_CUS = 256;                       // what the workspace's size is laid out for
-constexpr int SELF_MASK_TOKENS = 4096, SELF_MASK_LOADS = 8192;   // what a workgroup of head_prep finds out by itself
+// Without a teacher each workgroup of head_prep finds out by itself which of up to so many tokens have a target; entries are looked through by a
+// kernel in front (300 tokens, 20 entries each, d 704, V 14000: training step 103 -> 90 us against doing the same with those)
+constexpr int SELF_MASK_TOKENS = 4096;
 constexpr int ALL_TOKENS = 256;                     // up to these, a forward pass without a teacher takes all tokens for rows
 // Up to these many tokens dW takes what rounding dz loses as well (and dx what it loses at the teacher's entries).  The rounding of a token's gradient
 // at its target is one number for a whole row of dW: over many tokens such errors average out to the size of dW's own rounding, over a few they need
@@ -76,7 +78,7 @@ struct HeadPrepArgs {
   const moe_bf16* x;
   const int32_t* target;
   Teacher t;
-  const uint64_t* mask;            // null: found here
+  const uint64_t* mask;            // null: found here (no teacher)
   int T, d, V, strips;             // strips: of 64 columns
   int low;                         // rows of x twice
   BwdRule dx;
@@ -115,15 +117,6 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     for (int i = 0; i < WORDS; ++i) {
       const uint64_t bits = __ballot(target_there(y[i], V));
       if (lane == 0) own[wave + 4 * i] = bits;
-    }
-    if (K > 0) {
-      __syncthreads();
-#pragma unroll 8
-      for (int i = tid; i < a.T * K; i += 256)
-        if (entry_there(a.t.ids[i], a.t.logits[i], V)) {
-          const int t = i / K;
-          atomicOr(reinterpret_cast<unsigned*>(own) + (t >> 5), 1u << (t & 31));
-        }
     }
     mask = own;
   }
@@ -632,7 +625,7 @@ struct HeadCall {
 
 int run_prep(const HeadCall& c, const HeadLayout& l, const BwdRule& dx, long long dx_room) {
   uint64_t* mask = nullptr;
-  if (c.T > SELF_MASK_TOKENS || static_cast<long long>(c.T) * (c.t.K + 1) > SELF_MASK_LOADS) {
+  if (c.t.K > 0 || c.T > SELF_MASK_TOKENS) {
     mask = reinterpret_cast<uint64_t*>(c.ws + l.mask);
     MOE_LAUNCH("head_mask", head_mask_kernel, dim3((c.T + 63) / 64 * 4), dim3(256), 0, c.s, c.target, c.t, c.T, c.V,
                reinterpret_cast<uint16_t*>(mask));
