@@ -456,62 +456,81 @@ struct HeadDxArgs {
   const float* item;               // what dz lost at the items
   Teacher t;
   const moe_bf16* W;
-  int T, d, V, all;                // all: of every item, else of the target
+  int T, d, V;
   moe_bf16* dx;
   const float* dw_part;            // dW's sums, [dw_parts][V][d], if they are in parts
   int dw_parts, dx_groups;         // workgroups from dx_groups on are for them
   moe_bf16* dW;
 };
-// dx of a token: the parts' sums in their order and what rounding dz took from them where it is largest, rounded once; zeros without a loss.  And dW
+// v += e W[id, c .. c + 7]
+__device__ __forceinline__ void add_row(const HeadDxArgs& a, float e, int id, int c, f32x4_t (&v)[2]) {
+  typedef __attribute__((ext_vector_type(4))) uint32_t u4;
+  const u4 w = *reinterpret_cast<const u4*>(a.W + static_cast<size_t>(id) * a.d + c);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    v[k >> 1][2 * (k & 1)] = __builtin_fmaf(e, bf16lo(w[k]), v[k >> 1][2 * (k & 1)]);
+    v[k >> 1][2 * (k & 1) + 1] = __builtin_fmaf(e, bf16hi(w[k]), v[k >> 1][2 * (k & 1) + 1]);
+  }
+}
+__device__ __forceinline__ void add_parts(const float* part, size_t stride, int parts, f32x4_t (&v)[2]) {
+#pragma unroll 4
+  for (int p = 0; p < parts; ++p) {
+    v[0] += *reinterpret_cast<const f32x4_t*>(part + p * stride);
+    v[1] += *reinterpret_cast<const f32x4_t*>(part + p * stride + 4);
+  }
+}
+__device__ __forceinline__ void head_dw_sum(const HeadDxArgs& a) {
+  const size_t i = static_cast<size_t>(blockIdx.x - a.dx_groups) * 256 + threadIdx.x, n = static_cast<size_t>(a.V) * (a.d / 8);
+  if (i >= n) return;
+  f32x4_t v[2] = {};
+  add_parts(a.dw_part + i * 8, n * 8, a.dw_parts, v);
+  store8(a.dW + i * 8, v);
+}
+// dx of a token: the parts' sums in their order and what rounding dz took from them at the target, rounded once; zeros without a loss.  And dW
 // likewise, where its reduction over the tokens is in parts.
 __global__ __launch_bounds__(256) void head_dx_kernel(HeadDxArgs a) {
+  if (static_cast<int>(blockIdx.x) >= a.dx_groups) { head_dw_sum(a); return; }
   const int pieces = a.d / 8, K = a.t.K;
-  if (static_cast<int>(blockIdx.x) >= a.dx_groups) {
-    const size_t i = static_cast<size_t>(blockIdx.x - a.dx_groups) * 256 + threadIdx.x, n = static_cast<size_t>(a.V) * pieces;
-    if (i >= n) return;
-    f32x4_t v[2] = {};
-#pragma unroll 4
-    for (int p = 0; p < a.dw_parts; ++p) {
-      const float* q = a.dw_part + (p * n + i) * 8;
-      v[0] += *reinterpret_cast<const f32x4_t*>(q);
-      v[1] += *reinterpret_cast<const f32x4_t*>(q + 4);
-    }
-    store8(a.dW + i * 8, v);
-    return;
-  }
   const size_t i = static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x;
   if (i >= static_cast<size_t>(a.T) * pieces) return;
   const int t = static_cast<int>(i / pieces), c = static_cast<int>(i - static_cast<size_t>(t) * pieces) * 8, row = a.token_row[t];
   f32x4_t v[2] = {};
-  typedef __attribute__((ext_vector_type(4))) uint32_t u4;
   if (row >= 0) {
-    auto add = [&](float e, int id) __attribute__((always_inline)) {
-      const u4 w = *reinterpret_cast<const u4*>(a.W + static_cast<size_t>(id) * a.d + c);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        v[k >> 1][2 * (k & 1)] = __builtin_fmaf(e, bf16lo(w[k]), v[k >> 1][2 * (k & 1)]);
-        v[k >> 1][2 * (k & 1) + 1] = __builtin_fmaf(e, bf16hi(w[k]), v[k >> 1][2 * (k & 1) + 1]);
-      }
-    };
-    const int slot = K > 0 ? a.target_slot[row] : 0, parts = a.control[DX_PARTS], live = a.control[LIVE];
+    const int slot = K > 0 ? a.target_slot[row] : 0, live = a.control[LIVE];
+    if (slot >= 0) add_row(a, a.item[static_cast<size_t>(row) * (K + 1) + slot], a.target[t], c, v);
+    add_parts(a.part + static_cast<size_t>(row) * a.d + c, static_cast<size_t>(live) * a.d, a.control[DX_PARTS], v);
+  }
+  store8(a.dx + static_cast<size_t>(t) * a.d + c, v);
+}
+// The same for a few tokens with a teacher, with what rounding took at the entries too: a workgroup has 256 columns of a token, eight threads share the
+// items of eight columns.
+constexpr int FEW_PIECES = 32, FEW_SHARES = 256 / FEW_PIECES;
+__global__ __launch_bounds__(256) void head_dx_few_kernel(HeadDxArgs a) {
+  __shared__ f32x4_t sums[FEW_SHARES][FEW_PIECES][2];
+  if (static_cast<int>(blockIdx.x) >= a.dx_groups) { head_dw_sum(a); return; }
+  const int wide = (a.d / 8 + FEW_PIECES - 1) / FEW_PIECES, t = blockIdx.x / wide, K = a.t.K;
+  const int share = threadIdx.x / FEW_PIECES, piece = threadIdx.x % FEW_PIECES, c = ((blockIdx.x - t * wide) * FEW_PIECES + piece) * 8;
+  const int row = a.token_row[t];
+  f32x4_t v[2] = {};
+  if (row >= 0 && c < a.d) {
     const float* item = a.item + static_cast<size_t>(row) * (K + 1);
-    if (slot >= 0) add(item[slot], a.target[t]);
-    if (a.all) {
-#pragma unroll 8
-      for (int j = 0; j < K; ++j) {
-        const size_t at = static_cast<size_t>(t) * K + j;
-        const int id = a.t.ids[at];
-        const bool on = j != slot && entry_there(id, a.t.logits[at], a.V);
-        add(on ? item[j] : 0.f, on ? id : 0);
-      }
-    }
+    const size_t at = static_cast<size_t>(t) * K;
+    if (share == 0 && a.target_slot[row] == K) add_row(a, item[K], a.target[t], c, v);     // (a target that is an entry is among them)
 #pragma unroll 4
-    for (int p = 0; p < parts; ++p) {
-      const float* q = a.part + (static_cast<size_t>(p) * live + row) * a.d + c;
-      v[0] += *reinterpret_cast<const f32x4_t*>(q);
-      v[1] += *reinterpret_cast<const f32x4_t*>(q + 4);
+    for (int j = share; j < K; j += FEW_SHARES) {
+      const int id = a.t.ids[at + j];
+      const float l = a.t.logits[at + j], e = item[j];
+      const bool on = entry_there(id, l, a.V);
+      add_row(a, on ? e : 0.f, on ? id : 0, c, v);
     }
   }
+  sums[share][piece][0] = v[0];
+  sums[share][piece][1] = v[1];
+  __syncthreads();
+  if (share != 0 || c >= a.d) return;
+#pragma unroll
+  for (int i = 1; i < FEW_SHARES; ++i) { v[0] += sums[i][piece][0]; v[1] += sums[i][piece][1]; }
+  if (row >= 0) add_parts(a.part + static_cast<size_t>(row) * a.d + c, static_cast<size_t>(a.control[LIVE]) * a.d, a.control[DX_PARTS], v);
   store8(a.dx + static_cast<size_t>(t) * a.d + c, v);
 }
 
@@ -557,7 +576,9 @@ BwdShape head_bwd_shape(int T, int d, int cols, bool whole) {
   BwdShape shape{128, 1, 1};
   double best = 1e300;
   const int depth = T <= LOW_TOKENS ? 2 * T : T;
-  weigh_bwd<256>(T, d, cols, depth, whole, best, shape);
+  // One reduction step of dW, all of it waiting for memory: two workgroups on a compute unit wait better.  256 / 128 in us: 10 tokens, d 2048, V 50304 110 / 94;
+  // 8, 2880, 35317 117 / 96; 1, 832, 61930 62 / 50; 22, 1216, 178071 248 / 257.  (100, 2048, 50304: 119 / 118, as the model has it.)
+  if (depth > 64) weigh_bwd<256>(T, d, cols, depth, whole, best, shape);
   weigh_bwd<128>(T, d, cols, depth, whole, best, shape);
   return shape;
 }
@@ -755,12 +776,13 @@ int run_head_bwd(const HeadCall& c, int v_piece, int* edges) {
     rc = shape.edge == 128 ? launch_gemm_head_bwd<128>(b, w, tiles, c.s, "gemm_head_dx+dw") : launch_gemm_head_bwd<256>(b, w, tiles, c.s, "gemm_head_dx+dw");
     if (rc != MOE_OK) return rc;
   }
-  const size_t n = static_cast<size_t>(c.T) * (c.d / 8);
+  const bool few = c.t.K > 0 && c.T <= LOW_TOKENS;
+  const size_t dx_groups = few ? static_cast<size_t>(c.T) * ceil_div(c.d / 8, FEW_PIECES) : (static_cast<size_t>(c.T) * (c.d / 8) + 255) / 256;
   const HeadDxArgs x{part, control, reinterpret_cast<const int32_t*>(c.ws + l.token_row), reinterpret_cast<const int32_t*>(c.ws + l.target_slot), c.target,
-                     reinterpret_cast<const float*>(c.ws + l.item), c.t, c.W, c.T, c.d, c.V, c.T <= LOW_TOKENS, c.dx,
-                     dw_part, shape.dw_parts, static_cast<int>((n + 255) / 256), c.dW};
-  const size_t groups = x.dx_groups + (shape.dw_parts > 1 ? (static_cast<size_t>(c.V) * (c.d / 8) + 255) / 256 : 0);
-  MOE_LAUNCH("head_dx", head_dx_kernel, dim3(static_cast<unsigned>(groups)), dim3(256), 0, c.s, x);
+                     reinterpret_cast<const float*>(c.ws + l.item), c.t, c.W, c.T, c.d, c.V, c.dx, dw_part, shape.dw_parts, static_cast<int>(dx_groups), c.dW};
+  const dim3 groups(static_cast<unsigned>(dx_groups + (shape.dw_parts > 1 ? (static_cast<size_t>(c.V) * (c.d / 8) + 255) / 256 : 0)));
+  if (few) MOE_LAUNCH("head_dx", head_dx_few_kernel, groups, dim3(256), 0, c.s, x);
+  else MOE_LAUNCH("head_dx", head_dx_kernel, groups, dim3(256), 0, c.s, x);
   return moe_check_launch();
 }
 

@@ -291,6 +291,7 @@ template <typename F> void with_shape(int d, F&& f) {
 // rows for.  us with 256 / 512 / 1024: 8192 x 2048 34.1 / 33.4 / 39.9, 4001 x 4096 34.8 / 30.4 / 35.0, 2000 x 8192 36.0 / 40.7 / 51.5, 16384 x 136 13.3 / 11.9 / 15.0.
 int norm_bwd_groups(int T, int d) {
   const int rows = rows_of_group(d), groups = (T - 1) / rows + 1, most = d <= 4096 ? 512 : 256;
+  if (groups <= 4) return 1;                      // its share is dw: a few more rows in turn take less than another launch
   return groups < most ? groups : most;
 }
 
@@ -338,12 +339,13 @@ extern "C" int moe_add_rms_norm_bwd(const moe_bf16* dy, const moe_bf16* dsum, co
   if (ws_bytes < moe_add_rms_norm_bwd_workspace_bytes(T, d)) return MOE_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int groups = norm_bwd_groups(T, d);
-  const NormBwdArgs a{dy, dsum, sum, w, rstd, dx, static_cast<float*>(ws), T, d};
+  const NormBwdArgs a{dy, dsum, sum, w, rstd, dx, groups == 1 ? dw : static_cast<float*>(ws), T, d};
   with_shape(d, [&](auto tpr, auto p) {
     constexpr int TPR = decltype(tpr)::value, P = decltype(p)::value;
     MOE_LAUNCH("add_rms_norm_bwd", (add_rms_norm_bwd_kernel<TPR, P>), dim3(groups), dim3(TPR > 256 ? TPR : 256), 0, s, a);
   });
   if (moe_check_launch() != MOE_OK) return MOE_ERR_LAUNCH;
+  if (groups == 1) return MOE_OK;
   MOE_LAUNCH("norm_dw", norm_dw_kernel, dim3((d / 4 + 7) / 8), dim3(256), 0, s, static_cast<const float*>(ws), groups, d, dw);
   return moe_check_launch();
 }
