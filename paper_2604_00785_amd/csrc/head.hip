@@ -19,7 +19,10 @@ constexpr int HEAD_CUS = 256;                       // what the workspace's size
 // Without a teacher each workgroup of head_prep finds out by itself which of up to so many tokens have a target; entries are looked through by a
 // kernel in front (300 tokens, 20 entries each, d 704, V 14000: training step 103 -> 90 us against doing the same with those)
 constexpr int SELF_MASK_TOKENS = 4096;
-constexpr int ALL_TOKENS = 256;                     // up to these, a forward pass without a teacher takes all tokens for rows
+// Up to these many tokens all are taken for rows, with a loss or not, as the products are one pass over W in any case: a forward pass without a
+// teacher then needs no kernel in front (ALL_TOKENS), and with one nothing has to be known of all tokens before the rows are laid out
+// (ALL_TAUGHT: 40 tokens, 22 entries each, 21.6 -> 19.2 us; beyond, masked tokens cost more than the kernel: 256, 30 % of them masked, 257 -> 270).
+constexpr int ALL_TOKENS = 256, ALL_TAUGHT = 128;
 // Up to these many tokens dW takes what rounding dz loses as well (and dx what it loses at the teacher's entries).  The rounding of a token's gradient
 // at its target is one number for a whole row of dW: over many tokens such errors average out to the size of dW's own rounding, over a few they need
 // not.  Up to 32 tokens it costs nothing, the reduction is padded to 64 rows; 40 of d 2048, V 50304: dW 60 -> 71 us of 238; 100 tokens: 69 -> 93.
@@ -78,7 +81,8 @@ struct HeadPrepArgs {
   const moe_bf16* x;
   const int32_t* target;
   Teacher t;
-  const uint64_t* mask;            // null: found here (no teacher)
+  const uint64_t* mask;            // null: found here (no teacher), or all
+  int all;                         // every token is a row (with a teacher); rows without a loss are zeros
   int T, d, V, strips;             // strips: of 64 columns
   int low;                         // rows of x twice
   BwdRule dx;
@@ -100,12 +104,12 @@ struct HeadPrepArgs {
 __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   extern __shared__ int count[];                     // [strips + 1]
   __shared__ uint64_t own[SELF_MASK_TOKENS / 64];
-  __shared__ int wave_sum[4], s_token[16], s_slot[16];
+  __shared__ int wave_sum[4], s_token[16], s_slot[16], s_zero[16];
   const int tid = threadIdx.x, lane = tid % MOE_WAVE, wave = tid / MOE_WAVE;
   const int words = (a.T + 63) / 64, per = (words + 255) / 256, K = a.t.K, V = a.V, slots = K + 1;
   const bool lists = blockIdx.y == 0;
   const uint64_t* mask = a.mask;
-  if (mask == nullptr) {
+  if (mask == nullptr && !a.all) {
     constexpr int WORDS = SELF_MASK_TOKENS / 256;        // of a wave, requested together
     int y[WORDS];
 #pragma unroll
@@ -120,13 +124,13 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     }
     mask = own;
   }
-  if (tid < 16) { s_token[tid] = -1; s_slot[tid] = K; }
+  if (tid < 16) { s_token[tid] = a.all && static_cast<int>(blockIdx.x) * 16 + tid < a.T ? blockIdx.x * 16 + tid : -1; s_slot[tid] = K; }
   if (lists && K > 0) for (int i = tid; i <= a.strips; i += 256) count[i] = 0;
   __syncthreads();
   // rank of each thread's first token among those with a loss
   const int w0 = tid * per < words ? tid * per : words, w1 = w0 + per < words ? w0 + per : words;
   int mine = 0;
-  for (int w = w0; w < w1; ++w) mine += __builtin_popcountll(mask[w]);
+  if (!a.all) for (int w = w0; w < w1; ++w) mine += __builtin_popcountll(mask[w]);
   int rank = wave_incl_scan(mine);
   if (lane == 63) wave_sum[wave] = rank;
   __syncthreads();
@@ -134,8 +138,9 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
 #pragma unroll
   for (int w = 0; w < 4; ++w) { rank += w < wave ? wave_sum[w] : 0; live += wave_sum[w]; }
   rank -= mine;
+  if (a.all) live = a.T;
   const int first = blockIdx.x * 16;
-  const bool direct = live == a.T && !a.low;
+  const bool direct = a.all ? a.row == nullptr : live == a.T && !a.low;
   if (lists && blockIdx.x == 0 && tid == 0) {
     a.control[ROWS] = 0; a.control[LIVE] = live;
     a.control[DW_ROWS - 1] = 0; a.control[DW_ROWS] = a.low ? 2 * live : live;
@@ -148,7 +153,7 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     const int parts = dx_parts(x, live > 0 ? live : 1, lane);
     if (lane == 0) a.control[DX_PARTS] = parts;
   }
-  if (lists && tid < 16 && first + tid < a.T) {
+  if (lists && !a.all && tid < 16 && first + tid < a.T) {
     const int t = first + tid;
     if ((mask[t >> 6] >> (t & 63) & 1) == 0) {
       a.token_row[t] = -1;
@@ -184,6 +189,17 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     in_loss = a.in_loss[t]; in_lse = a.in_lse[t]; gl = has ? a.dloss[t] : 0.f;
     if (K > 0) { in_lse_t = a.in_lse_t[t]; in_dkd = a.dkd[t]; }
   }
+  if (a.all && !direct) {                                // (not the numbers of a token that counts for nothing)
+    bool some = has;
+    for (int j = l16; j < (r < n ? K : 0); j += 16) {
+      const int id = a.t.ids[static_cast<size_t>(t) * K + j];
+      const float l = a.t.logits[static_cast<size_t>(t) * K + j];
+      some = some || entry_there(id, l, V);
+    }
+    const uint64_t any = __ballot(some);
+    if (l16 == 0) s_zero[r] = (any >> (lane & 48) & 0xFFFFu) == 0;
+    __syncthreads();
+  }
   if (!direct) {
     typedef __attribute__((ext_vector_type(4))) uint32_t u4;
     const int pieces = a.d / 8, all = n * pieces, step = 256 * gridDim.y;
@@ -193,6 +209,7 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
       for (int k = 0; k < 8; ++k) {
         const int i = i0 + k * step, j = i < all ? i : i0, row = j / pieces;
         v[k] = *reinterpret_cast<const u4*>(a.x + static_cast<size_t>(s_token[row]) * a.d + (j - row * pieces) * 8);
+        if (a.all && s_zero[row]) v[k] = u4{0, 0, 0, 0};
       }
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -646,7 +663,8 @@ struct HeadCall {
 
 int run_prep(const HeadCall& c, const HeadLayout& l, const BwdRule& dx, long long dx_room) {
   uint64_t* mask = nullptr;
-  if (c.t.K > 0 || c.T > SELF_MASK_TOKENS) {
+  const bool all = c.t.K > 0 && c.T <= ALL_TAUGHT;
+  if (!all && (c.t.K > 0 || c.T > SELF_MASK_TOKENS)) {
     mask = reinterpret_cast<uint64_t*>(c.ws + l.mask);
     MOE_LAUNCH("head_mask", head_mask_kernel, dim3((c.T + 63) / 64 * 4), dim3(256), 0, c.s, c.target, c.t, c.T, c.V,
                reinterpret_cast<uint16_t*>(mask));
@@ -654,6 +672,7 @@ int run_prep(const HeadCall& c, const HeadLayout& l, const BwdRule& dx, long lon
   HeadPrepArgs p{};
   p.x = c.x; p.target = c.target; p.t = c.t; p.mask = mask; p.T = c.T; p.d = c.d; p.V = c.V; p.strips = l.strips64;
   p.low = l.low;
+  p.all = all;
   p.dx = dx; p.dx_room = dx_room;
   p.target_row = reinterpret_cast<int32_t*>(c.ws + l.target_row);
   p.control = reinterpret_cast<int32_t*>(c.ws + l.control);
@@ -713,7 +732,6 @@ int run_head_fwd(const HeadCall& c, int* edges) {
   HeadArgs h{};
   fill_head(c, l, a, h);
   a.A0 = reinterpret_cast<const uint16_t*>(c.ws + l.xc); a.A1 = c.x; a.B0 = c.W; a.K = c.d; a.N = c.V;
-  // A few tokens cost the same with or without a loss, one pass over W: no kernel in front finds those that have one.
   const bool all = c.t.K == 0 && c.T <= ALL_TOKENS;
   int rc = MOE_OK;
   if (all) {
