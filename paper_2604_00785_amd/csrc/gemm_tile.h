@@ -397,9 +397,15 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
   constexpr bool B_KN = (is_wgrad(MODE) || is_dgrad_h(MODE) || MODE == DGRAD_X || MODE == HEAD_DX);  // stored [k][n]
   constexpr bool GATHER_B = (MODE == WGRAD_GATHER);
   constexpr bool GATHER_A = (MODE == WGRAD_GATHER_A);
+  constexpr bool IS_HEAD = is_logits(MODE) || MODE == HEAD_DX || MODE == HEAD_DW;
 
-  // (HEAD_STATS: all M tokens, where none has been left out)
-  auto head_rows = [&]() __attribute__((always_inline)) { return MODE == HEAD_STATS && a.offsets == nullptr ? a.M : a.offsets[1]; };
+  // What the head's products read on the device is read once: their rows (HEAD_STATS without offsets: all M tokens), whether x itself holds them, the
+  // parts of dx.  (For every tile: a latency between the tiles, which counts where they have one or two steps.)
+  int head_rows = 0, head_flag = 0;
+  if constexpr (IS_HEAD) {
+    head_rows = __builtin_amdgcn_readfirstlane(MODE == HEAD_STATS && a.offsets == nullptr ? a.M : a.offsets[1]);
+    head_flag = __builtin_amdgcn_readfirstlane(a.row_token == nullptr ? 0 : a.row_token[0]);
+  }
 
   // ---------------- tile list ---------------------------------------------------
   int total;
@@ -413,7 +419,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
   if constexpr (is_wgrad(MODE)) {
     total = a.E * a.m_tiles_cap * a.n_tiles * wpair;
   } else if constexpr (is_logits(MODE) || MODE == HEAD_DX) {
-    total = (head_rows() + S - 1) / S * a.n_tiles * (MODE == HEAD_DX ? a.row_token[0] : 1);
+    total = (head_rows + S - 1) / S * a.n_tiles * (MODE == HEAD_DX ? head_flag : 1);
   } else {
     total = count_row_tiles<S>(a.offsets, a.E, tid0 & 63) * a.n_tiles;
     if constexpr (MODE == GATE_UP || MODE == DOWN) {
@@ -457,7 +463,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
   } else if constexpr (is_logits(MODE)) {
     // Bands of eight row tiles, column tile by column tile: the 32 (or 64) tiles that an XCD works on at a time then share 8 panels of
     // rows and 4 (or 8) of columns; all rows of a column tile in a run would have every XCD fetch all rows in every round.
-    m_end = head_rows();
+    m_end = head_rows;
     rt = (m_end + S - 1) / S;
         const int band = tile / (8 * a.n_tiles), in = tile - band * 8 * a.n_tiles;
     const int high = rt - band * 8 < 8 ? rt - band * 8 : 8;
@@ -466,7 +472,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
     e = 0;
     nt = __builtin_amdgcn_readfirstlane(nt);
   } else if constexpr (MODE == HEAD_DX) {
-    m_end = head_rows();
+    m_end = head_rows;
     rt = (m_end + S - 1) / S;
     e = tile / (rt * a.n_tiles);        // part of the reduction
     const int in = tile - e * rt * a.n_tiles;
@@ -524,7 +530,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
 
   if constexpr (is_wgrad(MODE)) {
     if constexpr (MODE == HEAD_DW) {
-      const int all = a.offsets[1], steps = (all + BK - 1) / BK;
+      const int all = head_rows, steps = (all + BK - 1) / BK;
       k_lo = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<long long>(steps) * e / a.E)) * BK;
       k_hi = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<long long>(steps) * (e + 1) / a.E)) * BK;
       k_hi = k_hi > all ? all : k_hi;
@@ -548,7 +554,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
       b_step = 0;
       row_tok = a.row_token + k_lo;
     } else {
-      const uint16_t* B = MODE == HEAD_DW && a.row_token[0] != 0 ? a.B1 : a.B0;
+      const uint16_t* B = MODE == HEAD_DW && head_flag != 0 ? a.B1 : a.B0;
       bbase = reinterpret_cast<const char*>(B + static_cast<size_t>(k_lo) * a.N + n0);
       b_step = static_cast<size_t>(BK) * a.N * 2;
     }
@@ -569,7 +575,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
     nk_phase = nk;
     // (logits: the tokens' rows side by side, or as they are where all have a loss)
     const uint16_t* A = a.A0;
-    if constexpr (is_logits(MODE)) { if (a.row_token != nullptr && a.row_token[0] != 0) A = a.A1; }
+    if constexpr (is_logits(MODE)) { if (head_flag != 0) A = a.A1; }
     abase = reinterpret_cast<const char*>(A + static_cast<size_t>(m0) * a.K);
     a_step = BK * 2;
     bool gathered = false;
@@ -589,7 +595,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
     if constexpr (MODE == DGRAD_X) { a_phase = (a.A1 - a.A0) * 2; nk *= 2; }
     if constexpr (MODE == HEAD_DX) {
       const int steps = (a.M + BK - 1) / BK;
-      const int parts = a.row_token[0];
+      const int parts = head_flag;
       k_lo = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<long long>(steps) * e / parts)) * BK;
       k_hi = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<long long>(steps) * (e + 1) / parts)) * BK;
       nk = nk_phase = (k_hi - k_lo) / BK;
@@ -1143,14 +1149,37 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
   // their place in HeadArgs::item and (HEAD_DZ) their terms; `many`: there are more, and the parts look them up.
   // Without a teacher these are the targets of the lane's rows.  Otherwise the bounds of the lists of the wave's blocks (in lanes 0 to NB - 1) are
   // requested with the tile's first loads, so that one latency, not two in a row, stands behind the main loop.
+  // (What a lane of a tile of 128 needs of its rows comes with them; a tile of 256 has no registers for that.)
   constexpr int IT = HALF / 64;
+  constexpr bool EARLY = S == 128;
+  int early_target[IT] = {};
+  f32x4_t early_term[IT] = {}, early_row[NB] = {};
   int item_lo = 0, item_hi = 0, list_lo = 0, list_hi = 0, item_at[IT], item_place[IT];
   bool many = false;
-  f32x4_t item_term[MODE == HEAD_DZ ? IT : 1], rowp[MODE == HEAD_DZ ? NB : 1];
+  f32x4_t item_term[MODE == HEAD_DZ ? IT : 1], rowp[NB];
+  auto fetch_rows = [&](const TileState& t, f32x4_t (&to)[NB]) __attribute__((always_inline)) {
+    const HeadPtr he = head_args();
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      int r = t.m0 + t.r0 + i * 16 + (lane & 15);
+      if (r > t.m_end - 1) r = t.m_end - 1;
+      to[i] = he->row[r];
+    }
+  };
   auto fetch_lists = [&](const TileState& t) __attribute__((always_inline)) {
     const HeadPtr he = head_args();
-    if (he->list_start == nullptr) return;
     const int first = t.m0 + t.r0, last = t.m_end - 1;
+    if constexpr (EARLY && MODE == HEAD_DZ) fetch_rows(t, early_row);
+    if (he->list_start == nullptr) {
+#pragma unroll
+      for (int k = 0; k < IT; ++k) {
+        const int r = first + lane + 64 * k, row = r < t.m_wave ? r : last;
+        early_target[k] = he->target[row];
+        if constexpr (EARLY && MODE == HEAD_DZ) early_term[k] = he->terms[row];
+      }
+      asm volatile("" ::: "memory");
+      return;
+    }
     int b = (first >> 4) + (lane < NB ? lane : NB - 1);
     if (b > last >> 4) b = last >> 4;
     int strip = (he->col0 + t.n0 + wn * HALF) >> 6, end = strip + HALF / 64;
@@ -1169,10 +1198,10 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
 #pragma unroll
       for (int k = 0; k < IT; ++k) {
         const int r = lane + 64 * k, row = first + r < t.m_wave ? first + r : last;
-        const int c = he->target[row] - col;
+        const int c = early_target[k] - col;
         item_at[k] = first + r < t.m_wave && c >= 0 && c < HALF ? r | c << 8 : -1;
         item_place[k] = row;
-        if constexpr (MODE == HEAD_DZ) item_term[k] = he->terms[row];
+        if constexpr (MODE == HEAD_DZ) item_term[k] = EARLY ? early_term[k] : he->terms[row];
       }
     } else {
       item_lo = list_lo;
@@ -1198,11 +1227,11 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
       }
     }
     if constexpr (MODE == HEAD_DZ) {
+      if constexpr (EARLY) {
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        int r = first + i * 16 + (lane & 15);
-        if (r > last) r = last;
-        rowp[i] = he->row[r];
+        for (int i = 0; i < NB; ++i) rowp[i] = early_row[i];
+      } else {
+        fetch_rows(t, rowp);
       }
     }
     asm volatile("" ::: "memory");            // requested here, not where they are used
