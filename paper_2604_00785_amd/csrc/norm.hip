@@ -1,6 +1,6 @@
 // Residual addition and root-mean-square norm in front of a layer, its result in bfloat16 or in 8 bits with scales, and its
 // derivative.  With s = x + r (rounded to bf16: what the residual stream holds is what is normalised), q = 1 / sqrt(mean(s^2) + eps):
-//   y = s q w;      8 bits: scale = max |y| / 448 over each group of columns, codes = y / scale in e4m3
+//   y = s q w;      8 bits: scale = max |y| / 448 over each group of columns, codes = y / scale = 448 s w / max |s w| in e4m3
 //   c = mean(dy w s) q^2;   dx = dr = dsum + q (dy w - s c);   dw = sum over rows of dy s q
 // All of it is bound by memory: a row is read once, kept in registers between the sum and its use, and written once.
 #include <climits>
@@ -98,59 +98,97 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_kernel(Nor
   }
   q = rsqrtf(row_sum<TPR>(q, part) / static_cast<float>(a.d) + a.eps);
   if (a.rstd != nullptr && i0 == 0) a.rstd[row] = q;
-  uint32_t top = 0;
+  if constexpr (!CODES) {
 #pragma unroll
-  for (int p = 0; p < P; ++p) {
-    const int i = i0 + p * TPR;
-    if (i < pieces) {
+    for (int p = 0; p < P; ++p) {
+      const int i = i0 + p * TPR;
+      if (i >= pieces) continue;
       const f32x4_t w0 = *reinterpret_cast<const f32x4_t*>(a.w + 8 * i), w1 = *reinterpret_cast<const f32x4_t*>(a.w + 8 * i + 4);
 #pragma unroll
       for (int c = 0; c < 8; ++c) s[p][c] = s[p][c] * q * (c < 4 ? w0[c] : w1[c - 4]);
-      if constexpr (!CODES) *reinterpret_cast<u32x4*>(a.y + at + 8 * i) = pack8(s[p]);
+      *reinterpret_cast<u32x4*>(a.y + at + 8 * i) = pack8(s[p]);
     }
-    if constexpr (CODES) {
-#pragma unroll
-      for (int c = 0; c < 8; ++c) top = umax(top, __float_as_uint(s[p][c]) & 0x7FFFFFFFu);
-    }
-  }
-  if constexpr (CODES) {
+  } else {
+    // A code is a step of 2^-4: a quotient next to a border goes to the wrong side when its own roundings add up.  So it is formed from the exact
+    // product s w (v and low), the exact largest one (m and off) and 448 over that in two parts (factor and rest), rounded once.  It does not depend
+    // on q, which only says whether there is a number at all.  (None of 16 million codes of 4001 x 4096 differ from 64 bits', 5 to 16 do if y itself is divided by
+    // its scale.)
+    float w[P][8];
+    uint32_t top = 0;
     const bool whole = a.lanes >= pieces;         // one scale for the row
-    if (whole) top = row_reduce<TPR>(top, umax, part);
+    const auto amax_of = [&](int p, uint32_t most) __attribute__((always_inline)) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) most = umax(most, __float_as_uint(s[p][c] * w[p][c]) & 0x7FFFFFFFu);
+      return most;
+    };
+    // how far the largest product is above its rounding m: no other one is
+    const auto above = [&](int p, float m, float most) __attribute__((always_inline)) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) most = fmaxf(most, __builtin_fmaf(fabsf(s[p][c]), fabsf(w[p][c]), -m));
+      return most;
+    };
+    const auto larger = [](uint32_t u, uint32_t v) __attribute__((always_inline)) {
+      return __float_as_uint(fmaxf(__uint_as_float(u), __uint_as_float(v)));
+    };
+    // over the threads that share a scale
+    const auto shared = [&](uint32_t v, auto op) __attribute__((always_inline)) {
+      if (a.lanes >= 2) v = op(v, dpp_u32<0xB1>(v));
+      if (a.lanes >= 4) v = op(v, dpp_u32<0x4E>(v));
+      if (a.lanes >= 8) v = op(v, dpp_u32<0x141>(v));
+      if (a.lanes >= 16) v = op(v, dpp_u32<0x140>(v));
+      if (a.lanes >= 32) { const auto e = __builtin_amdgcn_permlane16_swap(v, v, false, false); v = op(e[0], e[1]); }
+      if (a.lanes >= 64) { const auto e = __builtin_amdgcn_permlane32_swap(v, v, false, false); v = op(e[0], e[1]); }
+      return v;
+    };
+    constexpr float LEAST = -3.4028235e38f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int i = i0 + p * TPR;
+      f32x4_t w0{}, w1{};
+      if (i < pieces) { w0 = *reinterpret_cast<const f32x4_t*>(a.w + 8 * i); w1 = *reinterpret_cast<const f32x4_t*>(a.w + 8 * i + 4); }
+#pragma unroll
+      for (int c = 0; c < 8; ++c) w[p][c] = c < 4 ? w0[c] : w1[c - 4];
+    }
+    float row_above = LEAST;
+    if (whole) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) top = amax_of(p, top);
+      top = row_reduce<TPR>(top, umax, part);
+#pragma unroll
+      for (int p = 0; p < P; ++p) row_above = above(p, __uint_as_float(top), row_above);
+      row_above = __uint_as_float(row_reduce<TPR>(__float_as_uint(row_above), larger, part));
+    }
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int i = i0 + p * TPR;
       uint32_t amax = top;
+      float off = row_above;
       if (!whole) {
-        amax = 0;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) amax = umax(amax, __float_as_uint(s[p][c]) & 0x7FFFFFFFu);
-        if (a.lanes >= 2) amax = umax(amax, dpp_u32<0xB1>(amax));
-        if (a.lanes >= 4) amax = umax(amax, dpp_u32<0x4E>(amax));
-        if (a.lanes >= 8) amax = umax(amax, dpp_u32<0x141>(amax));
-        if (a.lanes >= 16) amax = umax(amax, dpp_u32<0x140>(amax));
-        if (a.lanes >= 32) { const auto e = __builtin_amdgcn_permlane16_swap(amax, amax, false, false); amax = umax(e[0], e[1]); }
-        if (a.lanes >= 64) { const auto e = __builtin_amdgcn_permlane32_swap(amax, amax, false, false); amax = umax(e[0], e[1]); }
+        amax = shared(amax_of(p, 0), umax);
+        off = __uint_as_float(shared(__float_as_uint(above(p, __uint_as_float(amax), LEAST)), larger));
       }
       if (i >= pieces) continue;
-      const float scale = __uint_as_float(amax) / E4M3_MAX;
-      // (a scale below the smallest normal number has no finite inverse: the largest number instead, which leaves zeros zeros)
-      const float inverse = scale != 0.f ? fminf(1.f / scale, 3.4028235e38f) : 0.f;
-      float v[8];
+      const float m = __uint_as_float(amax);
+      // (far from the ends of the range only; where 448 / m is not finite the largest number instead, which leaves zeros zeros)
+      const bool fine = m > 0x1p-100f && m < 0x1p100f;
+      const float factor = m != 0.f ? fminf(E4M3_MAX / m, 3.4028235e38f) : 0.f, nothing = 0.f * q;
+      const float rest = fine ? (__builtin_fmaf(-factor, m, E4M3_MAX) - factor * off) * (factor * (1.f / E4M3_MAX)) : 0.f, low_factor = fine ? factor : 0.f;
+      float z[8];
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
-        const float z = s[p][c] * inverse;
-        v[c] = z != z ? z : fminf(fmaxf(z, -E4M3_MAX), E4M3_MAX);
+        const float v = __builtin_fmaf(s[p][c], w[p][c], nothing), low = __builtin_fmaf(s[p][c], w[p][c], -v);
+        z[c] = __builtin_fmaf(v, factor, __builtin_fmaf(v, rest, low * low_factor));      // at most 448 and a bit, which rounds to 448
       }
       u32x2 o;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        int b = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h], v[4 * h + 1], 0, false);
-        b = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2], v[4 * h + 3], b, true);
+        int b = __builtin_amdgcn_cvt_pk_fp8_f32(z[4 * h], z[4 * h + 1], 0, false);
+        b = __builtin_amdgcn_cvt_pk_fp8_f32(z[4 * h + 2], z[4 * h + 3], b, true);
         o[h] = static_cast<uint32_t>(b);
       }
       *reinterpret_cast<u32x2*>(a.codes + at + 8 * i) = o;
       const int groups = whole ? 1 : pieces / a.lanes;
-      if (whole ? i == 0 : i % a.lanes == 0) a.scale[static_cast<size_t>(row) * groups + (whole ? 0 : i / a.lanes)] = scale;
+      if (whole ? i == 0 : i % a.lanes == 0) a.scale[static_cast<size_t>(row) * groups + (whole ? 0 : i / a.lanes)] = m * q * (1.f / E4M3_MAX);
     }
   }
 }

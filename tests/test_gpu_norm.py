@@ -143,3 +143,20 @@ def test_values_that_are_not_finite():
     codes, scale = torch.empty(4, 512, dtype=torch.float8_e4m3fn, device=DEV), torch.empty(4, 4, device=DEV)
     B.moe_add_rms_norm_8bit(dev(a["x"]), dev(a["r"]), dev(a["w"]), EPS, 128, total, codes, scale)
     assert bool(torch.isnan(scale[1]).all()) and bool(torch.isnan(codes[1].float()).all()) and bool(torch.isfinite(scale[0]).all())
+
+
+@pytest.mark.parametrize("d,group", [(1024, 64), (512, 0), (4096, 128)])
+def test_codes_are_those_of_64_bits(d, group):
+    """Every code is the nearest to the quotient in 64 bits, borders included but for the last bit of a 32-bit number."""
+    T = 500
+    a = make(T, d, 6)
+    _, y, _ = R.norm(a["x"], a["r"], a["w"], EPS)
+    total, codes = torch.empty(T, d, dtype=BF, device=DEV), torch.empty(T, d, dtype=torch.float8_e4m3fn, device=DEV)
+    scale = torch.empty(T, d // (group or d), device=DEV)
+    B.moe_add_rms_norm_8bit(dev(a["x"]), dev(a["r"]), dev(a["w"]), EPS, group, total, codes, scale)
+    q = y.view(T, d // (group or d), -1)
+    q = (q / (q.abs().amax(2, keepdim=True) / 448.0)).view(T, d)
+    got = codes.float().cpu().to(R.F64)
+    # the codes of the quotient one 32-bit rounding to either side
+    low, high = ((q * (1 + sign * 2 * R.HALF32)).float().to(torch.float8_e4m3fn).to(R.F64) for sign in (-1, 1))
+    assert bool(((got == low) | (got == high)).all())
