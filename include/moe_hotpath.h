@@ -20,6 +20,9 @@
  * plain sum and needs no backward pass of its own).  Stage 1's Router layer and the derivatives of Stage 1:
  * moe_router_fwd, moe_route_bwd, moe_router_bwd.
  *
+ * In front of the layer and behind it: moe_add_rms_norm (_8bit, _bwd), the residual's addition and the norm; moe_head_ce_fwd / _bwd and
+ * moe_head_distill_fwd / _bwd, the vocabulary head's losses without its logits.
+ *
  * Conventions, valid for every function below
  * -------------------------------------------
  * - Every pointer except `stream` is a DEVICE pointer to memory the caller owns,

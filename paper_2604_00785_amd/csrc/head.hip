@@ -7,6 +7,10 @@
 // rounded to bf16 (the products read it as their operand; half a step is 2^-9 of each element, against the 2^-9 of dx and dW themselves), then
 // the two products.  What bounds it is the matrix pipe: four products of 2 T V d operations, one of them for the logits a second time.
 //
+// us, with the library's products for the same sizes (no losses in them): 8192 tokens, d 2048, V 50304: logits and sums 1220 (1350), logits and gradient 1330,
+// dx and dW 2110 (1220 + 1610); all of the training step 4720.  The chip is at its power limit there (clock 1.7 to 1.96 GHz, matrix pipe busy 0.61 to 0.82).
+// One token: 39 for 206 MB of weights (5.2 TB/s), 57 tokens of d 4096, V 32003 46 for 262 MB (5.7 TB/s).
+//
 // Tokens without a loss are left out of all products: a first kernel finds the others, copies their rows of x side by side, and lists by blocks of
 // 16 rows and strips of 64 columns which logits count by themselves.
 #include <initializer_list>

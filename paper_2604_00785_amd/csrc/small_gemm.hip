@@ -1,6 +1,6 @@
 // Grouped products for experts with few rows (a decoding step, a short prompt): what bounds them is the one pass
 // over the weights of the experts that have rows, 2 bytes for at most 2 * 16 operations.  The tiled kernel of
-// grouped_gemm.hip, made for many rows, has one workgroup per compute unit and spends as long between its tiles as
+// gemm_tile.h, made for many rows, has one workgroup per compute unit and spends as long between its tiles as
 // they take to stream here; with one token its eight experts are 64 tiles for 256 compute units.
 //
 // Here a workgroup owns 64 weight rows (32 of Wg and the same 32 of Wu, or 64 of Wd) of one expert and up to 16 activation
@@ -85,7 +85,7 @@ __device__ __forceinline__ bool st_find_tile(const int32_t* __restrict__ offsets
 // A wave's own ring in LDS: RING pieces of FR fragments of 16 weight rows and 8 XL activation rows, 128 bytes each.
 template <int FR, int XL> constexpr int st_piece_bytes() { return (2 * FR + XL) * 1024; }
 typedef const __attribute__((address_space(3))) bf16x8_t* LdsFrag;
-// The 16-byte piece `logical` of a row lies at physical piece (logical + row) mod 8, as in the tiles of grouped_gemm.hip; the lane's
+// The 16-byte piece `logical` of a row lies at physical piece (logical + row) mod 8, as in the tiles of gemm_tile.h; the lane's
 // share of it in a load that fills 8 rows: row lane / 8, physical piece lane % 8.
 __device__ __forceinline__ uint32_t st_lane_piece(int lane) { return static_cast<uint32_t>(((lane & 7) - (lane >> 3)) & 7) * 16u; }
 
