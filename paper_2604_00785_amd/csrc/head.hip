@@ -68,15 +68,15 @@ enum { ROWS = 0, LIVE = 1, DW_ROWS = 3, DIRECT = 4, DX_PARTS = 5, CONTROL_INTS =
 
 // Parts of dx's reduction for `rows` rows, at most `most`: the number with which dx and dW together take least time (head_bwd_time), each part's sums
 // being written and read besides (8 bytes an element, 7 MB in the model's unit of time).  Lane p - 1 of a wave weighs p parts.
-struct BwdRule { int edge, places, d, steps, most, dw_tiles, dw_parts, low; };
-template <int S> __device__ __forceinline__ float bwd_time_of(const BwdRule& x, int rows, int p) {
-  const int tiles = (rows + S - 1) / S * ((x.d + S - 1) / S) * p;
-  return head_bwd_time(tiles, head_dx_each<S>(x.steps, p), x.dw_tiles, head_dw_each<S>(((x.low ? 2 : 1) * rows + BK - 1) / BK, x.dw_parts), x.places) +
+struct BwdRule { int edge, places, d, steps, most, dw_tiles, dw_parts, low; float fixed, wgrad, step; };
+__device__ __forceinline__ float bwd_time_of(const BwdRule& x, int rows, int p) {
+  const int tiles = (rows + x.edge - 1) / x.edge * ((x.d + x.edge - 1) / x.edge) * p;
+  return head_bwd_time(tiles, x.fixed + x.step * x.steps / p, x.dw_tiles, x.wgrad + 1.1f * x.step * (((x.low ? 2 : 1) * rows + BK - 1) / BK) / x.dw_parts, x.places) +
          p * (static_cast<float>(rows) * x.d / 1.0e6f);
 }
 __device__ __forceinline__ int dx_parts(const BwdRule& x, int rows, int lane) {
   const int p = lane + 1;
-  const float time = x.edge == 256 ? bwd_time_of<256>(x, rows, p) : bwd_time_of<128>(x, rows, p);
+  const float time = bwd_time_of(x, rows, p);
   const uint32_t key = p <= x.most && (p == 1 || x.steps / p >= 4) ? (__float_as_uint(time) & ~63u) | static_cast<uint32_t>(lane) : ~0u;
   return 1 + (group_reduce<MOE_WAVE>(key, [](uint32_t u, uint32_t v) __attribute__((always_inline)) { return u < v ? u : v; }) & 63u);
 }
@@ -104,7 +104,8 @@ struct HeadPrepArgs {
 };
 
 // Workgroup (b, 0): rows 16 b to 16 b + 15 of those with a loss, in the order of their tokens; and tokens 16 b to 16 b + 15, if they have none.
-// Workgroups (b, 1 ..) help with the rows of x.  Sixteen threads share a row's entries.
+// Workgroups (b, 1 ..) help with the rows of x.  Sixteen threads share a row and its entries.  A workgroup behind those of the rows writes down what is
+// found for all.  (The kernel is one chain of a few us, and short code is part of that: it is fetched cold.)
 __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   extern __shared__ int count[];                     // [strips + 1]
   __shared__ uint64_t own[SELF_MASK_TOKENS / 64];
@@ -145,17 +146,22 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   if (a.all) live = a.T;
   const int first = blockIdx.x * 16;
   const bool direct = a.all ? a.row == nullptr : live == a.T && !a.low;
-  if (lists && blockIdx.x == 0 && tid == 0) {
-    a.control[ROWS] = 0; a.control[LIVE] = live;
-    a.control[DW_ROWS - 1] = 0; a.control[DW_ROWS] = a.low ? 2 * live : live;
-    a.control[DIRECT] = direct;
-  }
-  if (lists && blockIdx.x == 0 && wave == 0 && a.row != nullptr) {
-    BwdRule x = a.dx;
-    const long long room = live > 0 ? a.dx_room / live : 1;
-    x.most = room < 64 ? static_cast<int>(room) : 64;
-    const int parts = dx_parts(x, live > 0 ? live : 1, lane);
-    if (lane == 0) a.control[DX_PARTS] = parts;
+  if (blockIdx.x == gridDim.x - 1) {
+    if (!lists || wave != 0) return;
+    int parts = 1;
+    if (a.row != nullptr) {
+      BwdRule x = a.dx;
+      const long long room = live > 0 ? a.dx_room / live : 1;
+      x.most = room < 64 ? static_cast<int>(room) : 64;
+      parts = dx_parts(x, live > 0 ? live : 1, lane);
+    }
+    if (lane == 0) {
+      a.control[ROWS] = 0; a.control[LIVE] = live;
+      a.control[DW_ROWS - 1] = 0; a.control[DW_ROWS] = a.low ? 2 * live : live;
+      a.control[DIRECT] = direct;
+      a.control[DX_PARTS] = parts;
+    }
+    return;
   }
   if (lists && !a.all && tid < 16 && first + tid < a.T) {
     const int t = first + tid;
@@ -204,31 +210,31 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     if (l16 == 0) s_zero[r] = (any >> (lane & 48) & 0xFFFFu) == 0;
     __syncthreads();
   }
-  if (!direct) {
+  if (!direct && r < n) {
     typedef __attribute__((ext_vector_type(4))) uint32_t u4;
-    const int pieces = a.d / 8, all = n * pieces, step = 256 * gridDim.y;
-    for (int i0 = blockIdx.y * 256 + tid; i0 < all; i0 += 8 * step) {
+    const bool zero = a.all && s_zero[r];
+    const int pieces = a.d / 8, step = 16 * gridDim.y;
+    const u4* from = reinterpret_cast<const u4*>(a.x + static_cast<size_t>(t) * a.d);
+    u4* to = reinterpret_cast<u4*>(a.xc + static_cast<size_t>(first + r) * a.d);
+    u4* again = a.low ? reinterpret_cast<u4*>(a.xc + static_cast<size_t>(live + first + r) * a.d) : to;
+    for (int p0 = l16 + 16 * blockIdx.y; p0 < pieces; p0 += 8 * step) {
       u4 v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int i = i0 + k * step, j = i < all ? i : i0, row = j / pieces;
-        v[k] = *reinterpret_cast<const u4*>(a.x + static_cast<size_t>(s_token[row]) * a.d + (j - row * pieces) * 8);
-        if (a.all && s_zero[row]) v[k] = u4{0, 0, 0, 0};
-      }
+      for (int k = 0; k < 8; ++k) v[k] = from[p0 + k * step < pieces ? p0 + k * step : p0];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const int i = i0 + k * step;
-        if (i >= all) break;
-        moe_bf16* to = a.xc + static_cast<size_t>(first) * a.d + static_cast<size_t>(i) * 8;
-        *reinterpret_cast<u4*>(to) = v[k];
-        if (a.low) *reinterpret_cast<u4*>(to + static_cast<size_t>(live) * a.d) = v[k];
+        const int p = p0 + k * step;
+        if (p >= pieces) break;
+        if (zero) v[k] = u4{0, 0, 0, 0};
+        to[p] = v[k];
+        if (a.low) again[p] = v[k];
       }
     }
   }
   if (!lists) return;
   const size_t at = static_cast<size_t>(t < 0 ? 0 : t) * K;
   const int mine_K = r < n ? K : 0;
-  const float tau = a.t.temperature;
+  const float tau = a.t.temperature, over_tau = 1.f / tau;
   if (K == 0) {                                          // every row has a target, its only item
     if (l16 == 0 && r < n) {
       a.target_row[first + r] = y;
@@ -240,12 +246,12 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     return;
   }
   float top = -__builtin_inff();
-#pragma unroll 4
+#pragma unroll 2
   for (int j = l16; j < mine_K; j += 16) {
     const int id = a.t.ids[at + j];
     const float l = a.t.logits[at + j];
     if (!entry_there(id, l, V)) continue;
-    top = fmaxf(top, l / tau);
+    top = fmaxf(top, l * over_tau);
     if (id == y) atomicMin(&s_slot[r], j);               // the target's logit is that of an entry
     atomicAdd(&count[id >> 6], 1);
   }
@@ -288,7 +294,7 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
       float e = 0.f;
       for (int j = l16; j < mine_K; j += 16) {
         const float l = a.t.logits[at + j];
-        if (entry_there(a.t.ids[at + j], l, V)) e += expf(l / tau - top);
+        if (entry_there(a.t.ids[at + j], l, V)) e += expf(l * over_tau - top);
       }
       lq = top + logf(group_sum<16>(e));
       lt = in_lse_t;
@@ -310,7 +316,7 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     const int id = a.t.ids[at + j];
     const float l = a.t.logits[at + j];
     if (!entry_there(id, l, V)) continue;
-    const float log_q = l / tau - lq;
+    const float log_q = l * over_tau - lq;
     put(id, j, a.terms == nullptr ? f32x4_t{} : f32x4_t{id == y ? at_target : 0.f, expf(log_q) * gk, lt + log_q, id == y ? 0.f : gl});
   }
   if (own_target) put(y, K, f32x4_t{at_target + gk, gk, lt, 0.f});
@@ -722,7 +728,7 @@ int run_prep(const HeadCall& c, const HeadLayout& l, const BwdRule& dx, long lon
   const int lds = (l.strips64 + 1) * 4;
   static bool configured[MAX_DEVICES] = {};
   if (configure_lds(&head_prep_kernel, (HEAD_MAX_V / 64 + 1) * 4, configured) != MOE_OK) return MOE_ERR_LAUNCH;
-  MOE_LAUNCH("head_prep", head_prep_kernel, dim3(l.blocks, (c.d + 1023) / 1024), dim3(256), lds, c.s, p);
+  MOE_LAUNCH("head_prep", head_prep_kernel, dim3(l.blocks + 1, (c.d + 1023) / 1024), dim3(256), lds, c.s, p);
   return moe_check_launch();
 }
 
@@ -797,7 +803,10 @@ int run_head_bwd(const HeadCall& c, int v_piece, int* edges) {
   const int places = HEAD_CUS * 256 / shape.edge, wide = ceil_div(c.d, shape.edge);
   // (the parts are those of all pieces: no more than the smallest, the last, has steps for)
   const int last = c.V - (c.V - 1) / piece * piece;
-  const BwdRule rule{shape.edge, places, c.d, ceil_div(last, BK), 0, ceil_div(last, shape.edge) * wide * shape.dw_parts, shape.dw_parts, l.low};
+  const BwdRule rule{shape.edge, places, c.d, ceil_div(last, BK), 0, ceil_div(last, shape.edge) * wide * shape.dw_parts, shape.dw_parts, l.low,
+                     static_cast<float>(shape.edge == 256 ? TileCost<256>::FIXED : TileCost<128>::FIXED),
+                     static_cast<float>(shape.edge == 256 ? TileCost<256>::WGRAD : TileCost<128>::WGRAD),
+                     static_cast<float>(shape.edge == 256 ? TileCost<256>::STEP : TileCost<128>::STEP)};
   int rc = run_prep(c, l, rule, static_cast<long long>(shape.dx_parts) * c.T);
   if (rc != MOE_OK) return rc;
   const int32_t* control = reinterpret_cast<const int32_t*>(c.ws + l.control);
