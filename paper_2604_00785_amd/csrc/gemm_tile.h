@@ -1526,14 +1526,16 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
         for (int k = 0; k < IT; ++k) mine = mine || (item_at[k] >= 0 && (item_at[k] >> 4 & (HALF / 16 - 1)) == part);
         return __ballot(mine) != 0;
       };
+      // (a wave's LDS operations are carried out in order; the compiler is not to change theirs)
+      auto in_order = []() __attribute__((always_inline)) { __builtin_amdgcn_wave_barrier(); asm volatile("" ::: "memory"); };
       auto put_logits = [&](const auto& v) __attribute__((always_inline)) {
         static_for<NB>([&](auto j) { *reinterpret_cast<f32x4_t*>(z_piece(l16, 4 * decltype(j)::value + lq)) = v[decltype(j)::value]; });
-        __builtin_amdgcn_wave_barrier();
+        in_order();
       };
       auto get_logits = [&](auto& v) __attribute__((always_inline)) {
-        __builtin_amdgcn_wave_barrier();
+        in_order();
         static_for<NB>([&](auto j) { v[decltype(j)::value] = *reinterpret_cast<const f32x4_t*>(z_piece(l16, 4 * decltype(j)::value + lq)); });
-        __builtin_amdgcn_wave_barrier();
+        in_order();
       };
       auto mask = [&](auto& v, float with) __attribute__((always_inline)) {
         if (left >= HALF) return;
@@ -1555,7 +1557,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
           if (has_items(i_tag)) {
             put_logits(v);
             over_items(i_tag, [&](bool there, int, int at, const f32x4_t&, float* z) __attribute__((always_inline)) { if (there) he->item[at] = *z; });
-            __builtin_amdgcn_wave_barrier();
+            in_order();
             over_items(i_tag, [&](bool there, int, int, const f32x4_t&, float* z) __attribute__((always_inline)) { if (there) *z = NONE; });
             get_logits(v);
           }
@@ -1593,9 +1595,9 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
         const int off = gc < ld ? (lane / RP * ld + gc) * 2 : PAST;
         auto stage_part = [&](const f32x4_t (&v)[NB]) __attribute__((always_inline)) {
           static_for<NB>([&](auto j) { put_quad(l16, decltype(j)::value, v[decltype(j)::value]); });
-          __builtin_amdgcn_wave_barrier();
+          in_order();
           read_staged(v4, stage, IC<RB>{}, IC<PASSES>{}, IC<0>{}, IC<RP>{});
-          __builtin_amdgcn_wave_barrier();
+          in_order();
         };
         auto store_part = [&](int part, Rsrc out) __attribute__((always_inline)) {
 #pragma unroll

@@ -235,12 +235,15 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   const size_t at = static_cast<size_t>(t < 0 ? 0 : t) * K;
   const int mine_K = r < n ? K : 0;
   const float tau = a.t.temperature, over_tau = 1.f / tau;
+  // The gradient at the target and at the entries, where it is no plain softmax: p - 1 = exp(-loss) - 1 at the target; p - q = q (exp(log p - log q) - 1)
+  // at an entry.  What does not depend on the logit is put down here (q by the hardware's exponential: 1e-6 of what is rounded to 2^-8).
+  const float at_target = has && a.row != nullptr ? expm1f(-in_loss) * gl : 0.f;
   if (K == 0) {                                          // every row has a target, its only item
     if (l16 == 0 && r < n) {
       a.target_row[first + r] = y;
       if (a.row != nullptr) {
         a.row[first + r] = f32x4_t{in_lse * LOG2E, gl, 0.f, 0.f};
-        a.terms[first + r] = f32x4_t{expm1f(-in_loss) * gl, 0.f, 0.f, 0.f};
+        a.terms[first + r] = f32x4_t{at_target, 0.f, 0.f, 0.f};
       }
     }
     return;
@@ -286,21 +289,18 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     a.items[list + i] = HeadItem{static_cast<uint32_t>(r) | static_cast<uint32_t>(col) << 4, static_cast<uint32_t>(slot)};
     if (a.terms != nullptr) a.terms[list + i] = term;
   };
-  // The gradient at the target and at the entries, where it is no plain softmax: p - 1 = exp(-loss) - 1 at the target; p - q = q (exp(log p - log q) - 1)
-  // at an entry.  What does not depend on the logit is put down here.
-  float lq = 0.f, lt = 0.f, gk = 0.f, at_target = 0.f;
+  float lq = 0.f, lt = 0.f, gk = 0.f;
   if (a.terms != nullptr && r < n) {
     if (taught) {
       float e = 0.f;
       for (int j = l16; j < mine_K; j += 16) {
         const float l = a.t.logits[at + j];
-        if (entry_there(a.t.ids[at + j], l, V)) e += expf(l * over_tau - top);
+        if (entry_there(a.t.ids[at + j], l, V)) e += __builtin_amdgcn_exp2f((l * over_tau - top) * LOG2E);
       }
       lq = top + logf(group_sum<16>(e));
       lt = in_lse_t;
-      gk = in_dkd / tau;
+      gk = in_dkd * over_tau;
     }
-    if (has) at_target = expm1f(-in_loss) * gl;
     if (l16 == 0) {
       const float none = __builtin_inff();
       f32x4_t p = {none, 0.f, none, 0.f};
@@ -317,7 +317,7 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     const float l = a.t.logits[at + j];
     if (!entry_there(id, l, V)) continue;
     const float log_q = l * over_tau - lq;
-    put(id, j, a.terms == nullptr ? f32x4_t{} : f32x4_t{id == y ? at_target : 0.f, expf(log_q) * gk, lt + log_q, id == y ? 0.f : gl});
+    put(id, j, a.terms == nullptr ? f32x4_t{} : f32x4_t{id == y ? at_target : 0.f, __builtin_amdgcn_exp2f(log_q * LOG2E) * gk, lt + log_q, id == y ? 0.f : gl});
   }
   if (own_target) put(y, K, f32x4_t{at_target + gk, gk, lt, 0.f});
   if (l16 == 0 && r < n) a.target_slot[first + r] = has ? s_slot[r] : -1;
