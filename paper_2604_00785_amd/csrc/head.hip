@@ -359,7 +359,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
   // at most instead of 1.5e-6; 0.9 us of 45).
   double zy = 0.0;
   if (slot >= 0) {
-    if (a.control != nullptr || a.T > 16) {
+    if (a.T > 16) {
       zy = z[slot];
     } else {
       const moe_bf16 *xr = a.x + static_cast<size_t>(t) * a.d, *wr = a.W + static_cast<size_t>(a.target[t]) * a.d;
@@ -429,21 +429,24 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
     s = wave_sum_of(s);
     return s > 0.f ? static_cast<float>(static_cast<double>(top) * 0.693147180559945309 - from + static_cast<double>(logf(s))) : NONE;
   };
-  // (without a teacher the difference to the target's logit is all that is needed)
-  const float rest1 = joined(0, K == 0 ? zy : 0.0), rest2 = two ? joined(2, 0.0) : rest1;
+  const float rest1 = joined(0, zy), rest2 = two ? joined(2, 0.0) : static_cast<float>(rest1 + zy);     // rest1: less the target's logit
   float loss = 0.f, lse = 0.f, kd = 0.f, lse_t = 0.f;
   // loss = log(1 + exp(away)), away = log of the sum over all columns but the target, less the target's logit
   if (slot >= 0) {
     float away = rest1;
     if (K > 0) {
-      float top = rest1, sum = 0.f;
+      float top = rest1, sum = 0.f, far[EPL];
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) if (on[i] && lane + i * MOE_WAVE != slot) top = fmaxf(top, zj[i]);
+      for (int i = 0; i < EPL; ++i) {
+        far[i] = on[i] && lane + i * MOE_WAVE != slot ? static_cast<float>(zj[i] - zy) : NONE;
+        top = fmaxf(top, far[i]);
+      }
       top = wave_max_of(top);
+      if (top > NONE) {
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) if (on[i] && lane + i * MOE_WAVE != slot) sum += expf(zj[i] - top);
-      sum = wave_sum_of(sum);
-      away = top > NONE ? top + logf(sum + expf(rest1 - top)) - static_cast<float>(zy) : NONE;
+        for (int i = 0; i < EPL; ++i) sum += expf(far[i] - top);
+        away = top + logf(wave_sum_of(sum) + expf(rest1 - top));
+      }
     }
     loss = fmaxf(away, 0.f) + log1pf(expf(-fabsf(away)));
     lse = static_cast<float>(loss + zy);
