@@ -157,7 +157,7 @@ struct HeadArgs {
   int two;                    // both sums, both terms
   int strips, list_ld, slots;
   int col0;                   // vocabulary column of the product's first
-  int lo;                     // HEAD_DZ: what rounding loses is stored too, in as many rows behind the others
+  int lo;                     // HEAD_DZ: up to so many rows what rounding loses is stored too, in as many rows behind the others
 };
 
 // 512 bytes of zeros: what the reduction rows past an expert's end read in the weight-gradient products.
@@ -1587,8 +1587,9 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
       } else {
         const int ld = ae->M;
         const Rsrc oo = rows_of(ae->O0, ld * 2);
-        const bool lows = he->lo != 0;
-        const Rsrc ol = rows_of(ae->O0 + (lows ? static_cast<size_t>(ae->offsets[1]) * ld : 0), ld * 2);
+        const int all_rows = ae->offsets[1];
+        const bool lows = all_rows <= he->lo;
+        const Rsrc ol = rows_of(ae->O0 + (lows ? static_cast<size_t>(all_rows) * ld : 0), ld * 2);
         constexpr int PASSES = 16 * RP / 64;
         u32x4 v4[PASSES];
         const int gc = gcol0 + lane % RP * 8;

@@ -27,10 +27,12 @@ constexpr int SELF_MASK_TOKENS = 4096;
 // teacher then needs no kernel in front (ALL_TOKENS), and with one nothing has to be known of all tokens before the rows are laid out
 // (ALL_TAUGHT: 40 tokens, 22 entries each, 21.6 -> 19.2 us; beyond, masked tokens cost more than the kernel: 256, 30 % of them masked, 257 -> 270).
 constexpr int ALL_TOKENS = 256, ALL_TAUGHT = 128;
-// Up to these many tokens dW takes what rounding dz loses as well (and dx what it loses at the teacher's entries).  The rounding of a token's gradient
-// at its target is one number for a whole row of dW: over many tokens such errors average out to the size of dW's own rounding, over a few they need
-// not.  Up to 32 tokens it costs nothing, the reduction is padded to 64 rows; 40 of d 2048, V 50304: dW 60 -> 71 us of 238; 100 tokens: 69 -> 93.
-constexpr int LOW_TOKENS = 64;
+// Up to these many tokens with a loss dW takes what rounding dz loses as well, as further rows of its reduction (and of up to these many tokens dx what
+// it loses at the teacher's entries).  The rounding of a token's gradient at its target is one number for a whole row of dW: over many tokens such
+// errors average out to the size of dW's own rounding, over a few they need not (84 tokens, 80 % of them masked: 0.0027 of dW's norm, 0.0017 with it).
+// Training steps without / with, us: 100 tokens of d 2048, V 50304 216 / 222; 128, 1088, 32003 99 / 105; 90, 320, 500 37 / 39; up to 32 the same, as the
+// reduction is padded to 64 rows.
+constexpr int LOW_TOKENS = 128;
 constexpr float LOG2E = 1.4426950408889634f;
 
 struct Teacher { const int32_t* ids; const float* logits; float temperature; int K; };
@@ -88,7 +90,7 @@ struct HeadPrepArgs {
   const uint64_t* mask;            // null: found here (no teacher), or all
   int all;                         // every token is a row (with a teacher); rows without a loss are zeros
   int T, d, V, strips;             // strips: of 64 columns
-  int low;                         // rows of x twice
+  int low;                         // up to so many rows: rows of x twice
   BwdRule dx;
   long long dx_room;               // rows that the parts' sums have room for, together
   int32_t* target_row;             // the rows' targets
@@ -145,19 +147,20 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   rank -= mine;
   if (a.all) live = a.T;
   const int first = blockIdx.x * 16;
-  const bool direct = a.all ? a.row == nullptr : live == a.T && !a.low;
+  const bool low = live <= a.low, direct = a.all ? a.row == nullptr : live == a.T && !low;
   if (blockIdx.x == gridDim.x - 1) {
     if (!lists || wave != 0) return;
     int parts = 1;
     if (a.row != nullptr) {
       BwdRule x = a.dx;
+      x.low = low;
       const long long room = live > 0 ? a.dx_room / live : 1;
       x.most = room < 64 ? static_cast<int>(room) : 64;
       parts = dx_parts(x, live > 0 ? live : 1, lane);
     }
     if (lane == 0) {
       a.control[ROWS] = 0; a.control[LIVE] = live;
-      a.control[DW_ROWS - 1] = 0; a.control[DW_ROWS] = a.low ? 2 * live : live;
+      a.control[DW_ROWS - 1] = 0; a.control[DW_ROWS] = low ? 2 * live : live;
       a.control[DIRECT] = direct;
       a.control[DX_PARTS] = parts;
     }
@@ -216,7 +219,7 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     const int pieces = a.d / 8, step = 16 * gridDim.y;
     const u4* from = reinterpret_cast<const u4*>(a.x + static_cast<size_t>(t) * a.d);
     u4* to = reinterpret_cast<u4*>(a.xc + static_cast<size_t>(first + r) * a.d);
-    u4* again = a.low ? reinterpret_cast<u4*>(a.xc + static_cast<size_t>(live + first + r) * a.d) : to;
+    u4* again = low ? reinterpret_cast<u4*>(a.xc + static_cast<size_t>(live + first + r) * a.d) : to;
     for (int p0 = l16 + 16 * blockIdx.y; p0 < pieces; p0 += 8 * step) {
       u4 v[8];
 #pragma unroll
@@ -227,7 +230,7 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
         if (p >= pieces) break;
         if (zero) v[k] = u4{0, 0, 0, 0};
         to[p] = v[k];
-        if (a.low) again[p] = v[k];
+        if (low) again[p] = v[k];
       }
     }
   }
@@ -656,6 +659,8 @@ struct HeadLayout {
   size_t control, mask, row_token, token_row, target_row, target_slot, xc, list_start, items, terms, item, row, big;   // terms, row: of the backward pass
   int strips64, blocks, slots, low;
 };
+// Rows of dz, and of x beside it: those of all tokens, or twice as many as take what rounding loses.
+int head_dz_rows(int T) { return T <= LOW_TOKENS ? 2 * T : T < 2 * LOW_TOKENS ? 2 * LOW_TOKENS : T; }
 HeadLayout head_layout(int T, int d, int V, int K, bool backward) {
   HeadLayout l{};
   size_t at = 0;
@@ -664,14 +669,14 @@ HeadLayout head_layout(int T, int d, int V, int K, bool backward) {
   l.strips64 = (V + 63) / 64;
   l.blocks = (T + 15) / 16;
   l.slots = K + 1;
-  l.low = backward && T <= LOW_TOKENS;
+  l.low = backward ? LOW_TOKENS : 0;
   l.control = take(CONTROL_INTS * 4);
   l.mask = take((n + 63) / 64 * 8);
   l.row_token = take(4 * n);
   l.token_row = take(4 * n);
   l.target_row = take(4 * n);
   l.target_slot = take(4 * n);
-  l.xc = take((l.low ? 4 : 2) * n * d);
+  l.xc = take(2 * static_cast<size_t>(backward ? head_dz_rows(T) : T) * d);
   const size_t items = static_cast<size_t>(l.blocks) * 16 * l.slots;
   if (K > 0) {
     l.list_start = take(static_cast<size_t>(l.blocks) * (l.strips64 + 1) * 4);
@@ -686,8 +691,7 @@ HeadLayout head_layout(int T, int d, int V, int K, bool backward) {
   return l;
 }
 size_t head_part_bytes(int T, int V) { return static_cast<size_t>(3) * ((V + 63) / 64) * ((T + 15) & ~15) * sizeof(float); }
-// (a few tokens: what rounding loses lies in as many rows behind the others)
-size_t head_dz_bytes(int T, int piece) { return (static_cast<size_t>(T <= LOW_TOKENS ? 2 * T : T) * ((piece + 63) & ~63) * 2 + 255) & ~static_cast<size_t>(255); }
+size_t head_dz_bytes(int T, int piece) { return (static_cast<size_t>(head_dz_rows(T)) * ((piece + 63) & ~63) * 2 + 255) & ~static_cast<size_t>(255); }
 
 struct HeadCall {
   const moe_bf16 *x, *W;
@@ -806,7 +810,7 @@ int run_head_bwd(const HeadCall& c, int v_piece, int* edges) {
   const int places = HEAD_CUS * 256 / shape.edge, wide = ceil_div(c.d, shape.edge);
   // (the parts are those of all pieces: no more than the smallest, the last, has steps for)
   const int last = c.V - (c.V - 1) / piece * piece;
-  const BwdRule rule{shape.edge, places, c.d, ceil_div(last, BK), 0, ceil_div(last, shape.edge) * wide * shape.dw_parts, shape.dw_parts, l.low,
+  const BwdRule rule{shape.edge, places, c.d, ceil_div(last, BK), 0, ceil_div(last, shape.edge) * wide * shape.dw_parts, shape.dw_parts, 0,
                      static_cast<float>(shape.edge == 256 ? TileCost<256>::FIXED : TileCost<128>::FIXED),
                      static_cast<float>(shape.edge == 256 ? TileCost<256>::WGRAD : TileCost<128>::WGRAD),
                      static_cast<float>(shape.edge == 256 ? TileCost<256>::STEP : TileCost<128>::STEP)};

@@ -315,6 +315,20 @@ def test_nothing_of_a_token_without_a_loss_is_looked_at(T, K):
     assert torch.equal(clean["loss"], R.head(a["x"], a["W"], a["target"])[0]["loss"])
 
 
+@pytest.mark.parametrize("T,masked", [(64, 0.0), (65, 0.0), (128, 0.0), (200, 0.6), (255, 0.55), (600, 0.85)])
+@pytest.mark.parametrize("K", [0, 9])
+def test_weight_gradient_of_few_tokens_is_rounded_once(T, masked, K):
+    """With up to 128 losses, what rounding the logits' gradient loses goes into dW as well: 2 terms leave 2^-18 of it, the logits' errors some 1e-5,
+    and what remains is the rounding of dW itself, 2^-9 / sqrt(3) and more of its norm: a twentieth of that is left for all else."""
+    a = make(T, 256, 3000, K, masked, seed=5)
+    assert int((a["target"] >= 0).sum()) <= 128
+    got = run(a)
+    want, _ = R.head(a["x"], a["W"], a["target"], a.get("ids"), a.get("teacher"), 1.0, a["dloss"], a.get("dkd"))
+    once = float((want["dW"].bfloat16().double() - want["dW"]).norm())
+    off = float((got["dW"].cpu().double() - want["dW"]).norm())
+    assert off <= 1.05 * once, (off, once)
+
+
 def test_offsets_past_32_bits():
     """A gradient of the logits of 5.8 GB (and 2.9e9 elements), checked at tokens and columns from all over it."""
     T, d, V = 72000, 64, 40001
