@@ -381,13 +381,13 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
   }
   const float tau = a.t.temperature;
   bool on[EPL];
-  float zj[EPL], l[EPL];                                 // an entry's logit and, over the temperature, the teacher's
+  float zj[EPL], l[EPL];                                 // an entry's logit and the teacher's
 #pragma unroll
   for (int i = 0; i < EPL; ++i) {
     const int j = lane + i * MOE_WAVE;
     on[i] = j < K && entry_there(a.t.ids[at + j], a.t.logits[at + j], a.V);
     zj[i] = on[i] ? z[j] : 0.f;
-    l[i] = on[i] ? a.t.logits[at + j] / tau : NONE;
+    l[i] = on[i] ? a.t.logits[at + j] : NONE;
   }
   {
     const int quad = tid % 4, g = tid / 4;
@@ -454,8 +454,10 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
     loss = fmaxf(away, 0.f) + log1pf(expf(-fabsf(away)));
     lse = static_cast<float>(loss + zy);
   }
-  // With b_j = z_j / tau - log q_j on the entries, b their mean under q, u_j = b_j - b, and R the sum over the columns that are no entry:
-  // kd = log(R e^-b + sum q e^u), where sum q e^u = 1 + sum q (e^u - 1 - u) tells a student that is nearly the teacher from the teacher
+  // With b_j = z_j / tau - log q_j on the entries, b their mean under q, t_j = z_j / tau - b, u_j = t_j - log q_j, and R the sum over the columns that
+  // are no entry: kd = log(R e^-b + sum e^t), where sum e^t = 1 + sum q (e^u - 1 - u) tells a student that is nearly the teacher from the teacher.
+  // Logits are taken from their largest before they are divided: the type's lowest value is a logit like others, whatever the temperature.  An entry
+  // that is next to nothing to the teacher has a u that says nothing of its e^t = q e^u, which is then formed by itself; q = 0 leaves e^t alone.
   float top = NONE;
 #pragma unroll
   for (int i = 0; i < EPL; ++i) top = fmaxf(top, l[i]);
@@ -463,14 +465,16 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
   if (top > NONE) {                                      // there is an entry
     float sum = 0.f, mean = 0.f;
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) sum += on[i] ? expf(l[i] - top) : 0.f;
-    const float lq = top + logf(wave_sum_of(sum));
-    float q[EPL], b[EPL];
+    for (int i = 0; i < EPL; ++i) {
+      l[i] = (l[i] - top) / tau;
+      sum += on[i] ? expf(l[i]) : 0.f;
+    }
+    const float log_sum = logf(wave_sum_of(sum));
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
-      q[i] = on[i] ? expf(l[i] - lq) : 0.f;
-      b[i] = on[i] ? zj[i] / tau - (l[i] - lq) : 0.f;
-      mean += q[i] * b[i];
+      l[i] -= log_sum;                                   // log q
+      const float q = on[i] ? expf(l[i]) : 0.f;
+      if (q != 0.f) mean += q * (zj[i] / tau - l[i]);
     }
     mean = wave_sum_of(mean);
     float rest = rest2;
@@ -482,8 +486,10 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
     sum = 0.f;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
-      const float u = b[i] - mean;
-      if (on[i]) { far = fmaxf(far, u); sum += q[i] * (expm1f(fminf(u, 80.f)) - u); }
+      const float e = zj[i] / tau - mean, u = e - l[i], q = expf(l[i]);
+      if (!on[i]) continue;
+      far = fmaxf(far, e);
+      sum += u < 20.f ? q * (expm1f(u) - u) : expf(e) - (q != 0.f ? q * (1.f + u) : 0.f);
     }
     far = wave_max_of(far);
     sum = wave_sum_of(sum);
@@ -492,7 +498,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
     } else {                                             // the same with the largest term in front
       sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) sum += on[i] ? expf(zj[i] / tau - mean - far) : 0.f;      // q e^u
+      for (int i = 0; i < EPL; ++i) sum += on[i] ? expf(zj[i] / tau - mean - far) : 0.f;
       kd = far + logf(expf(rest - mean - far) + wave_sum_of(sum));
     }
     lse_t = kd + mean;
