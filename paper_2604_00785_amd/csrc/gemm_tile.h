@@ -151,7 +151,8 @@ struct HeadArgs {
   const int32_t* target;      // [row]
   const int32_t* list_start;  // [row block][list_ld]: first item of each strip; null: no teacher
   const HeadItem* items;      // [row block][16 slots]
-  const f32x4_t* terms;       // HEAD_DZ: as items, or [row]; the gradient there is t0 + t1 (exp(z / temperature - t2) - 1) + t3 exp(z - lse)
+  const f32x4_t* terms;       // HEAD_DZ: as items, or [row]; the gradient there is t0 + t1 (exp(z / temperature - t2) - 1) + t3 exp(z - lse); with `two` and
+                              // t1 = 0 it is t0 + the row's term at the temperature + t3 exp(z - lse)
   float* item;                // [row][slots]: HEAD_STATS: the logit; HEAD_DZ: what the gradient loses when it is rounded
   float c1, c2, over_tau;     // log2(e), the same over the temperature, 1 / temperature
   int two;                    // both sums, both terms
@@ -1621,8 +1622,10 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
             put_logits(v);
             over_items(i_tag, [&](bool there, int row, int at, const f32x4_t& t, float* zp) __attribute__((always_inline)) {
               const float z = *zp, lse = __shfl(p[0], row);
-              float g = t[0];
+              float g = t[0], lse_t = 0.f, of_p = 0.f;
+              if (two) { lse_t = __shfl(p[2], row); of_p = __shfl(p[3], row); }
               if (t[1] != 0.f) g = __builtin_fmaf(t[1], expm1f(__builtin_fmaf(z, he->over_tau, -t[2])), g);
+              else if (two) g = __builtin_fmaf(of_p, __builtin_amdgcn_exp2f(__builtin_fmaf(z, c2, -lse_t)), g);
               if (t[3] != 0.f) g = __builtin_fmaf(t[3], __builtin_amdgcn_exp2f(__builtin_fmaf(z, c1, -lse)), g);
               if (!there) return;
               he->item[at] = g - rounded(g);

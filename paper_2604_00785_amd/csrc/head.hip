@@ -237,9 +237,12 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   if (!lists) return;
   const size_t at = static_cast<size_t>(t < 0 ? 0 : t) * K;
   const int mine_K = r < n ? K : 0;
-  const float tau = a.t.temperature, over_tau = 1.f / tau;
+  const float tau = a.t.temperature;
   // The gradient at the target and at the entries, where it is no plain softmax: p - 1 = exp(-loss) - 1 at the target; p - q = q (exp(log p - log q) - 1)
-  // at an entry.  What does not depend on the logit is put down here (q by the hardware's exponential: 1e-6 of what is rounded to 2^-8).
+  // at an entry.  What does not depend on the logit is put down here (q by the hardware's exponential: 1e-6 of what is rounded to 2^-8).  Where q is small
+  // (below e^-20), q times a number is no way to p: by and by it has few bits, then none.  There the entry's p comes from the row's factors, like any other
+  // column's, and q alone stands in its terms; what the difference of the two loses is 1e-6 of e^-20 at most.
+  constexpr float SMALL_LOG_Q = -20.f;
   const float at_target = has && a.row != nullptr ? expm1f(-in_loss) * gl : 0.f;
   if (K == 0) {                                          // every row has a target, its only item
     if (l16 == 0 && r < n) {
@@ -257,7 +260,7 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     const int id = a.t.ids[at + j];
     const float l = a.t.logits[at + j];
     if (!entry_there(id, l, V)) continue;
-    top = fmaxf(top, l * over_tau);
+    top = fmaxf(top, l);
     if (id == y) atomicMin(&s_slot[r], j);               // the target's logit is that of an entry
     atomicAdd(&count[id >> 6], 1);
   }
@@ -298,11 +301,11 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
       float e = 0.f;
       for (int j = l16; j < mine_K; j += 16) {
         const float l = a.t.logits[at + j];
-        if (entry_there(a.t.ids[at + j], l, V)) e += __builtin_amdgcn_exp2f((l * over_tau - top) * LOG2E);
+        if (entry_there(a.t.ids[at + j], l, V)) e += __builtin_amdgcn_exp2f((l - top) / tau * LOG2E);
       }
-      lq = top + logf(group_sum<16>(e));
+      lq = logf(group_sum<16>(e));
       lt = in_lse_t;
-      gk = in_dkd * over_tau;
+      gk = in_dkd / tau;
     }
     if (l16 == 0) {
       const float none = __builtin_inff();
@@ -319,8 +322,17 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     const int id = a.t.ids[at + j];
     const float l = a.t.logits[at + j];
     if (!entry_there(id, l, V)) continue;
-    const float log_q = l * over_tau - lq;
-    put(id, j, a.terms == nullptr ? f32x4_t{} : f32x4_t{id == y ? at_target : 0.f, __builtin_amdgcn_exp2f(log_q * LOG2E) * gk, lt + log_q, id == y ? 0.f : gl});
+    f32x4_t term = {};
+    if (a.terms != nullptr) {
+      const float log_q = (l - top) / tau - lq, of_q = __builtin_amdgcn_exp2f(log_q * LOG2E) * gk;
+      term = f32x4_t{id == y ? at_target : 0.f, of_q, lt + log_q, id == y ? 0.f : gl};
+      if (log_q < SMALL_LOG_Q) {
+        term[0] -= of_q;
+        term[1] = term[2] = 0.f;
+        if (tau == 1.f) term[3] += gk;                   // (exp(z - lse) is p; otherwise the epilogue adds gk p where term[1] is zero)
+      }
+    }
+    put(id, j, term);
   }
   if (own_target) put(y, K, f32x4_t{at_target + gk, gk, lt, 0.f});
   if (l16 == 0 && r < n) a.target_slot[first + r] = has ? s_slot[r] : -1;

@@ -85,3 +85,37 @@ def test_losses_of_logits_that_fall_evenly(spread, tau):
     want, bound = reference(a, tau)
     for k in ("loss", "lse", "kd", "lse_t"):
         R.check(got[k], want[k], bound[k], k)
+
+
+@pytest.mark.parametrize("T,d,V,K", SHAPES)
+@pytest.mark.parametrize("tau", [0.1, 0.5, 1.0, 4.0])
+@pytest.mark.parametrize("gap", [15.0, 19.0, 21.0, 60.0, 86.0, 90.0, 1e4, 3.4e38])
+def test_gradients_of_a_teacher_that_spreads_widely(T, d, V, K, tau, gap):
+    """What the student gives to an entry that is nothing to the teacher is what it has to unlearn: the whole of p is left of p - q."""
+    print("gradient of a wide teacher", T, d, V, K, tau, gap, flush=True)
+    a = wide(T, d, V, K, gap, seed=23)
+    for v_piece in (0, 256):
+        got = run(a, tau, v_piece=v_piece)
+        want, bound = reference(a, tau)
+        for k in got:
+            R.check(got[k], want[k], bound[k], k)
+
+
+@pytest.mark.parametrize("tau", [0.25, 1.0, 2.0])
+@pytest.mark.parametrize("target", ["all", "half", "none"])
+def test_gradients_on_either_side_of_the_least_q(tau, target):
+    """Entries with log q from 0 to -40 in small steps, the student's p near q, far above and far below; with and without a target, which is an entry in some rows."""
+    T, d, V, K = 60, 64, 400, 60
+    a = make(T, d, V, K, seed=24)
+    a["ids"] = torch.stack([torch.randperm(V, generator=torch.Generator().manual_seed(t))[:K] for t in range(T)]).int()
+    z = (a["x"].float() @ a["W"].float().t()).gather(1, a["ids"].long())
+    fall = torch.linspace(0, -40 * tau, K)
+    a["teacher"] = torch.where(torch.arange(T)[:, None] % 3 == 0, z + fall, fall.expand(T, K)).contiguous()
+    a["target"][::4] = a["ids"][::4, 7]
+    a["target"][1::4] = a["ids"][1::4, K - 3]
+    if target != "all":
+        a["target"][(torch.arange(T) % 2 == 1) | (target == "none")] = -100
+    got = run(a, tau)
+    want, bound = reference(a, tau)
+    for k in got:
+        R.check(got[k], want[k], bound[k], k)
