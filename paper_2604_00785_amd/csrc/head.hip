@@ -334,7 +334,7 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     }
     put(id, j, term);
   }
-  if (own_target) put(y, K, f32x4_t{at_target + gk, gk, lt, 0.f});
+  if (own_target) put(y, K, f32x4_t{at_target, 0.f, 0.f, tau == 1.f ? gk : 0.f});      // (and gk p, as below the least q)
   if (l16 == 0 && r < n) a.target_slot[first + r] = has ? s_slot[r] : -1;
 }
 

@@ -44,7 +44,7 @@ def reference(a, tau):
     z = a["x"].to(R.F64) @ a["W"].to(R.F64).t() / tau
     log_p = torch.log_softmax(z, 1).gather(1, torch.where(there, a["ids"], 0).long())
     log_q = torch.log_softmax(l, 1)
-    q = torch.where(there, log_q.exp(), 0.0)
+    q = torch.where(there, log_q.exp(), 0.0)              # (rows without entries are zeros)
     far = torch.where(q > 0, (1 + (log_p - log_q).abs() + want["kd"][:, None]) * (8 * (l - top).abs() + 8 * log_q.abs() + 16), 0.0)
     # as in R.head: the logits' errors and the sums over the columns, then sums over K entries
     Wd, xd = a["W"].to(R.F64), a["x"].to(R.F64)
@@ -115,6 +115,28 @@ def test_gradients_on_either_side_of_the_least_q(tau, target):
     a["target"][1::4] = a["ids"][1::4, K - 3]
     if target != "all":
         a["target"][(torch.arange(T) % 2 == 1) | (target == "none")] = -100
+    got = run(a, tau)
+    want, bound = reference(a, tau)
+    for k in got:
+        R.check(got[k], want[k], bound[k], k)
+
+
+@pytest.mark.parametrize("T", [1, 200])
+@pytest.mark.parametrize("tau", [0.7, 1.0, 3.0])
+@pytest.mark.parametrize("weight", [0.0, 1e-9])
+@pytest.mark.parametrize("far", [2.0, 4.0, 8.0])
+def test_gradient_at_a_target_that_only_the_distillation_trains(T, tau, weight, far):
+    """A target that is no entry and counts (next to) nothing by itself has dkd / temperature p, however small p is.  One token has a loss, so
+    that nothing else stands in its target's row of dW."""
+    d, V, K = 128, 2000, 8
+    a = make(T, d, V, K, seed=25, known=0.0)
+    for t in range(T):                                    # an entry is likely, the target unlikely
+        a["ids"][t] = (int(a["target"][t]) + 1 + torch.arange(K) * 3) % V
+    lift = far / (0.05 ** 2 * d)
+    a["x"] = (a["x"].float() + lift * (a["W"][a["ids"][:, 0].long()].float() - a["W"][a["target"].long()].float())).bfloat16()
+    a["dloss"] *= weight
+    a["target"][:T - 1] = -100
+    a["ids"][:T - 1] = -1
     got = run(a, tau)
     want, bound = reference(a, tau)
     for k in got:
