@@ -433,7 +433,9 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
   }
   __syncthreads();
   if (first + r >= live) return;
-  // log of the sum over the columns that are no item, less `from`
+  // log of the sum over the columns that are no item, less `from`.  A sum is zero where there are no such columns (or all are -infinity); one that is NaN
+  // stays NaN, and so does what an item that is NaN or infinite makes of a row without others.
+  const double lost = zy < static_cast<double>(__builtin_inff()) ? 0.0 : static_cast<double>(__builtin_nanf(""));
   auto joined = [&](int h, double from) __attribute__((always_inline)) {
     float e[JOIN_GROUPS / MOE_WAVE], top = LOW, s = 0.f;
 #pragma unroll
@@ -442,7 +444,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
 #pragma unroll
     for (int i = 0; i < JOIN_GROUPS / MOE_WAVE; ++i) s += part[h + 1][r][lane + i * MOE_WAVE] * __builtin_amdgcn_exp2f(e[i] - top);
     s = wave_sum_of(s);
-    return s > 0.f ? static_cast<float>(static_cast<double>(top) * 0.693147180559945309 - from + static_cast<double>(logf(s))) : NONE;
+    return static_cast<float>((s == 0.f ? static_cast<double>(NONE) : static_cast<double>(top) * 0.693147180559945309 - from + static_cast<double>(logf(s))) + lost);
   };
   const float rest1 = joined(0, zy), rest2 = two ? joined(2, 0.0) : static_cast<float>(rest1 + zy);     // rest1: less the target's logit
   float loss = 0.f, lse = 0.f, kd = 0.f, lse_t = 0.f;
@@ -456,12 +458,10 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
         far[i] = on[i] && lane + i * MOE_WAVE != slot ? static_cast<float>(zj[i] - zy) : NONE;
         top = fmaxf(top, far[i]);
       }
-      top = wave_max_of(top);
-      if (top > NONE) {
+      top = fmaxf(wave_max_of(top), LOW);                // (a maximum passes over NaN, the sum does not; no other column at all: log 0)
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) sum += expf(far[i] - top);
-        away = top + logf(wave_sum_of(sum) + expf(rest1 - top));
-      }
+      for (int i = 0; i < EPL; ++i) sum += expf(far[i] - top);
+      away = top + logf(wave_sum_of(sum) + expf(rest1 - top));
     }
     loss = fmaxf(away, 0.f) + log1pf(expf(-fabsf(away)));
     lse = static_cast<float>(loss + zy);

@@ -1,0 +1,67 @@
+"""Logits that are not finite: what is not a number is not a loss of nothing."""
+import pytest
+import torch
+
+from test_gpu_head import make, run
+
+pytestmark = pytest.mark.gpu
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.mark.parametrize("T", [5, 40, 300])              # all tokens are rows; the same with more than one block; rows found first (with a teacher)
+@pytest.mark.parametrize("K", [0, 6, 300])
+@pytest.mark.parametrize("tau", [1.0, 1.5])
+@pytest.mark.parametrize("value", [NAN, INF, -INF])
+def test_a_token_that_is_not_finite(T, K, tau, value):
+    """One number of a token's x makes its logits NaN or infinite, of either sign: its losses and gradient are NaN, as is dW, and the other tokens' are what they were."""
+    if K == 0 and tau != 1.0:
+        pytest.skip("no teacher, no temperature")
+    a = make(T, 64, 400, K, seed=31)
+    clean = run(a, tau)
+    t = 3 if T < 20 else T - 2
+    a["x"][t, 17] = value
+    got = run(a, tau)
+    for k in clean:
+        if k == "dW":
+            assert bool(torch.isnan(got[k]).any(1).all())
+            continue
+        one = torch.arange(T, device=got[k].device) == t
+        assert bool(torch.isnan(got[k][one]).all()), (k, got[k][one])
+        assert torch.equal(got[k][~one], clean[k][~one]), k
+
+
+@pytest.mark.parametrize("T", [5, 300])
+@pytest.mark.parametrize("K", [0, 6])
+@pytest.mark.parametrize("row", ["target", "entry", "other"])
+@pytest.mark.parametrize("value", [NAN, INF])
+def test_a_column_that_is_not_finite(T, K, row, value):
+    """A row of W that makes one logit of every token NaN or +infinity: the target's, an entry's or one that does not count by itself."""
+    if K == 0 and row == "entry":
+        pytest.skip("no entries")
+    a = make(T, 64, 400, K, seed=32)
+    a["x"][:, 5] = 1.0                                   # (an infinity of its own sign)
+    v = {"target": 7, "entry": 8, "other": 9}[row]
+    a["target"][:] = 7
+    if K:
+        a["ids"] = torch.where((a["ids"] >= 7) & (a["ids"] < 10), 0 * a["ids"] - 1, a["ids"])
+        a["ids"][:, 0] = 8
+    a["W"][v, 5] = value
+    got = run(a, 1.5, train=False)
+    for k, x in got.items():
+        assert bool(torch.isnan(x).all()), (k, x)
+
+
+def test_nothing_but_the_target_and_entries():
+    """Every column is an item, so that no sum over the others is there to carry a NaN."""
+    a = make(3, 64, 4, 3, seed=33)
+    a["target"][:] = torch.tensor([3, 3, 0])
+    a["ids"] = torch.tensor([[0, 1, 2], [0, 1, 2], [1, 2, 3]]).int()
+    a["x"][0, 0] = NAN
+    a["x"][1, 0] = INF
+    got = run(a, 1.5, train=False)
+    for k, x in got.items():
+        assert bool(torch.isnan(x[:2]).all()) and bool(torch.isfinite(x[2])), (k, x)
+    one = make(2, 64, 1, 0, seed=34)
+    one["x"][0, 0] = NAN
+    got = run(one, train=False)
+    assert bool(torch.isnan(got["loss"][0])) and float(got["loss"][1]) == 0.0
