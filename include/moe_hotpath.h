@@ -366,7 +366,8 @@ int moe_add_rms_norm_bwd(const moe_bf16* dy, const moe_bf16* dsum, const moe_bf1
  * and zeros for a token whose target lies outside [0, V): it counts for nothing, and takes no time in the products.
  *   x [T, d] bf16; W [V, d] bf16; target [T] int32; loss, lse [T] fp32.  d % 64 == 0; V <= 2^20.
  *   ws at least moe_head_fwd_workspace_bytes(T, d, V, 0): about T d * 2 + T V * 3 / 16 bytes.
- * A token with a logit that is NaN or infinite has NaN for its losses and its dx, and makes all of dW NaN.
+ * A token with a logit that is NaN or infinite has NaN for its losses and its dx, and makes all of dW NaN.  So has one whose logits (for kd: over the
+ * temperature) are 2^30 or larger; up to 2^29 the losses are right.
  */
 size_t moe_head_fwd_workspace_bytes(int T, int d, int V, int K);
 int moe_head_ce_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, int T, int d, int V,

@@ -434,7 +434,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
   __syncthreads();
   if (first + r >= live) return;
   // log of the sum over the columns that are no item, less `from`.  A sum is zero where there are no such columns (or all are -infinity); one that is NaN
-  // stays NaN, and so does what an item that is NaN or infinite makes of a row without others.
+  // stays NaN, and so does what an item that is NaN or infinite makes of a row without others.  Where a scale 2^E has E of 2^30 or more, the product that
+  // E is rounded up from is off by 64 or more, which sums of powers do not bear for long (2^31: zero or infinity): NaN as well.
   const double lost = zy < static_cast<double>(__builtin_inff()) ? 0.0 : static_cast<double>(__builtin_nanf(""));
   auto joined = [&](int h, double from) __attribute__((always_inline)) {
     float e[JOIN_GROUPS / MOE_WAVE], top = LOW, s = 0.f;
@@ -444,7 +445,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
 #pragma unroll
     for (int i = 0; i < JOIN_GROUPS / MOE_WAVE; ++i) s += part[h + 1][r][lane + i * MOE_WAVE] * __builtin_amdgcn_exp2f(e[i] - top);
     s = wave_sum_of(s);
-    return static_cast<float>((s == 0.f ? static_cast<double>(NONE) : static_cast<double>(top) * 0.693147180559945309 - from + static_cast<double>(logf(s))) + lost);
+    const float log_s = fabsf(top) < 0x1p30f ? logf(s) : __builtin_nanf("");
+    return static_cast<float>((s == 0.f && top == LOW ? static_cast<double>(NONE) : static_cast<double>(top) * 0.693147180559945309 - from + static_cast<double>(log_s)) + lost);
   };
   const float rest1 = joined(0, zy), rest2 = two ? joined(2, 0.0) : static_cast<float>(rest1 + zy);     // rest1: less the target's logit
   float loss = 0.f, lse = 0.f, kd = 0.f, lse_t = 0.f;

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import head_reference as R
 from test_gpu_head import make, run
 
 pytestmark = pytest.mark.gpu
@@ -65,3 +66,40 @@ def test_nothing_but_the_target_and_entries():
     one["x"][0, 0] = NAN
     got = run(one, train=False)
     assert bool(torch.isnan(got["loss"][0])) and float(got["loss"][1]) == 0.0
+
+
+@pytest.mark.parametrize("T,K", [(5, 0), (40, 0), (300, 0), (40, 6)])
+def test_logits_past_the_range(T, K):
+    """Losses are right for logits up to 2^29 of either sign, and NaN from 2^30 on: never a number that says nothing."""
+    a = make(T, 64, 400, K, seed=35)
+    x = a["x"].float()
+    high = float((x @ a["W"].float().t()).abs().max())
+    for bits in (20, 27, 29):
+        a["x"] = (x * (0.95 * 2.0 ** bits / high)).bfloat16()
+        got = run(a, train=False)
+        want, bound = R.head(a["x"], a["W"], a["target"], a.get("ids"), a.get("teacher"))
+        # (that loss, log(1 + sum exp), is made for those near zero and overflows from 709 on; the difference does not, and has 64 bits enough here)
+        z = a["x"].to(R.F64) @ a["W"].to(R.F64).t()
+        want["loss"] = torch.logsumexp(z, 1) - z.gather(1, a["target"][:, None].long())[:, 0]
+        for k in got:
+            R.check(got[k], want[k], bound[k], k)
+    # all columns nearly alike: each token's logits are nearly one number, of either sign
+    g = torch.Generator().manual_seed(1)
+    w = torch.randn(64, generator=g)
+    a["W"] = (w + 0.01 * torch.randn(400, 64, generator=g)).bfloat16()
+    sign = torch.where(torch.arange(T)[:, None] % 2 == 0, 1.0, -1.0)
+    for bits in (30, 31, 33, 40, 100):
+        a["x"] = (sign * w * (1.1 * 2.0 ** bits / float(w.square().sum()))).bfloat16()
+        assert float((a["x"].float() @ a["W"].float().t()).abs().amin()) > 2.0 ** bits
+        for k, v in run(a, train=False).items():
+            assert bool(torch.isnan(v).all()), (bits, k)
+
+
+@pytest.mark.parametrize("T", [5, 40, 300])
+def test_temperatures_past_the_range(T):
+    """The same with the logits over the temperature: the divergence alone is lost."""
+    a = make(T, 64, 400, 6, seed=36)
+    clean = run(a, train=False)
+    got = run(a, 1e-12, train=False)
+    assert torch.equal(got["loss"], clean["loss"]) and torch.equal(got["lse"], clean["lse"])
+    assert bool(torch.isnan(got["kd"]).all()) and bool(torch.isnan(got["lse_t"]).all())
