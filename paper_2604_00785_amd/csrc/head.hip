@@ -430,11 +430,12 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
   }
   __syncthreads();
   if (first + r >= live) return;
-  // log of the sum over the columns that are no item, less `from`.  A sum is zero where there are no such columns (or all are -infinity); one that is NaN
+  // log of the sum over the columns that are no item, less `from`.  The exponents are products with LOG2E as 32 bits have it, so its inverse leads back from them (with log 2
+  // a loss would have 1.3e-8 of the logits' size in it; kd, whose terms are differences in 32 bits, does not notice).  A sum is zero where there are no such columns (or all are -infinity); one that is NaN
   // stays NaN, and so does what an item that is NaN or infinite makes of a row without others.  Where a scale 2^E has E of 2^30 or more, the product that
   // E is rounded up from is off by 64 or more, which sums of powers do not bear for long (2^31: zero or infinity): NaN as well.
   const double lost = zy < static_cast<double>(__builtin_inff()) ? 0.0 : static_cast<double>(__builtin_nanf(""));
-  auto joined = [&](int h, double from) __attribute__((always_inline)) {
+  auto joined = [&](int h, double from, double unit) __attribute__((always_inline)) {
     float e[JOIN_GROUPS / MOE_WAVE], top = LOW, s = 0.f;
 #pragma unroll
     for (int i = 0; i < JOIN_GROUPS / MOE_WAVE; ++i) { e[i] = part[h][r][lane + i * MOE_WAVE]; top = fmaxf(top, e[i]); }
@@ -443,9 +444,9 @@ __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(HeadJoinArgs a)
     for (int i = 0; i < JOIN_GROUPS / MOE_WAVE; ++i) s += part[h + 1][r][lane + i * MOE_WAVE] * __builtin_amdgcn_exp2f(e[i] - top);
     s = wave_sum_of(s);
     const float log_s = fabsf(top) < 0x1p30f ? logf(s) : __builtin_nanf("");
-    return static_cast<float>((s == 0.f && top == LOW ? static_cast<double>(NONE) : static_cast<double>(top) * 0.693147180559945309 - from + static_cast<double>(log_s)) + lost);
+    return static_cast<float>((s == 0.f && top == LOW ? static_cast<double>(NONE) : static_cast<double>(top) * unit - from + static_cast<double>(log_s)) + lost);
   };
-  const float rest1 = joined(0, zy), rest2 = two ? joined(2, 0.0) : static_cast<float>(rest1 + zy);     // rest1: less the target's logit
+  const float rest1 = joined(0, zy, 1.0 / static_cast<double>(LOG2E)), rest2 = two ? joined(2, 0.0, 0.693147180559945309) : static_cast<float>(rest1 + zy);     // rest1: less the target's logit
   float loss = 0.f, lse = 0.f, kd = 0.f, lse_t = 0.f;
   // loss = log(1 + exp(away)), away = log of the sum over all columns but the target, less the target's logit
   if (slot >= 0) {

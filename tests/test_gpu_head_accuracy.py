@@ -39,3 +39,11 @@ def test_the_targets_own_logit(T, masked, K):
         a["ids"] = torch.where(a["ids"] >= 0, a["ids"] + 400, -1)                     # (no targets among them)
     off, bound = losses(a, run(a, train=False))
     assert float(off.square().mean().sqrt()) <= bound, (float(off.mean()), float(off.square().mean().sqrt()), bound)
+
+
+@pytest.mark.parametrize("high", [2000.0, -2000.0])
+def test_the_unit_of_the_exponents(high):
+    """log2(e) has a rounding of its own, which logits of 2000 make visible; one common to all is not part of a loss."""
+    a = alike(16, 64, 60000, high)
+    off, bound = losses(a, run(a, train=False))
+    assert float(off.square().mean().sqrt()) <= bound, (float(off.mean()), float(off.square().mean().sqrt()), bound)
