@@ -33,8 +33,8 @@ __device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
   return u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
 }
 // Rows are read once and long after they were written, or by nobody else soon: non-temporal loads leave the caches to what is
-// written.  One pass over other rows each time, us, ordinary -> non-temporal: 8192 x 2048 forward 30.7 -> 28.2 (4.8 TB/s), 8 bits 31.9 -> 27.4,
-// backward 36.5 -> 34.1; 4001 x 4096 28.3 -> 24.8 (5.3 TB/s), 26.3 -> 24.3, 34.7 -> 31.9.
+// written.  One pass over other rows each time, us, ordinary -> non-temporal: 8192 x 2048 forward 30.7 -> 28.2 (4.8 TB/s), 8 bits 31.9 -> 27.4;
+// 4001 x 4096 28.3 -> 24.8 (5.3 TB/s), 26.3 -> 24.3; the backward's rows take 2 to 3 us of some 30 less too.
 __device__ __forceinline__ u32x4 load8(const moe_bf16* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
 
 // Reduction over the TPR threads of a row: inside the waves by lane permutations, across them through LDS.
@@ -206,16 +206,36 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_bwd_kernel
   constexpr int ROWS = TPR > 256 ? 1 : 256 / TPR;
   __shared__ uint32_t part[TPR > MOE_WAVE ? TPR / MOE_WAVE : 1];
   __shared__ float share[ROWS > 1 ? (ROWS - 1) * P * 8 * TPR : 1];
-  const int first = blockIdx.x * ROWS + threadIdx.x / TPR, i0 = threadIdx.x % TPR;
+  const int first = ROWS == 1 ? blockIdx.x : blockIdx.x * ROWS + threadIdx.x / TPR, i0 = ROWS == 1 ? threadIdx.x : threadIdx.x % TPR;
   const int pieces = a.d / 8;
-  float dw[P][8], w[P][8];
+  // The next row's pieces are requested before this row's are used, but for rows of 1024 threads, which have 128 registers each: those are for this row, and each
+  // thread keeps its weights in LDS (and forms dw with dx, when the row's sum has come).  All in registers, with the next row, went to memory and back, us:
+  // 1000 x 16384 47.6 -> 34.2, 500 x 32768 120 -> 38.5, 4000 x 32768 861 -> 211 (5.0 TB/s).
+  constexpr bool AHEAD = TPR < 1024;
+  __shared__ f32x4_t own_w[AHEAD ? 1 : P * 2 * TPR];
+  float dw[P][8];
+  f32x4_t kept[P][2];
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     const int i = i0 + p * TPR;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) { dw[p][c] = 0.f; w[p][c] = i < pieces ? a.w[8 * i + c] : 0.f; }
+    for (int c = 0; c < 8; ++c) dw[p][c] = 0.f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      kept[p][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      if (i < pieces) kept[p][h] = *reinterpret_cast<const f32x4_t*>(a.w + 8 * i + 4 * h);
+      if constexpr (!AHEAD) own_w[(2 * p + h) * TPR + i0] = kept[p][h];
+    }
   }
-  // the next row's pieces are requested before this row's are used
+  auto weights = [&](int p, float (&v)[8]) __attribute__((always_inline)) {
+    if constexpr (!AHEAD) {
+      asm volatile("" ::: "memory");                      // (read here, not in front of the rows or of the pieces before)
+      kept[p][0] = own_w[2 * p * TPR + i0];
+      kept[p][1] = own_w[(2 * p + 1) * TPR + i0];
+    }
+#pragma unroll
+    for (int c = 0; c < 8; ++c) v[c] = kept[p][c / 4][c % 4];
+  };
   struct Row { u32x4 g[P], s[P], a[P]; float q; };
   auto load = [&](int row, Row& x) __attribute__((always_inline)) {
     const size_t at = static_cast<size_t>(row < a.T ? row : a.T - 1) * a.d;
@@ -233,36 +253,48 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_bwd_kernel
   };
   const int step = gridDim.x * ROWS;
   Row now, next;
-  load(first, now);
-  for (int row = first; row < a.T; row += step, now = next) {     // (the same for all threads of a row)
-    if (row + step < a.T) load(row + step, next);
+  if constexpr (AHEAD) load(first, now);
+  for (int row = first; row < a.T; row += step) {                 // (the same for all threads of a row)
+    if constexpr (!AHEAD) load(row, now);
+    else if (row + step < a.T) load(row + step, next);
     const size_t at = static_cast<size_t>(row) * a.d;
     const u32x4 (&gp)[P] = now.g, (&sp)[P] = now.s, (&ap)[P] = now.a;
+    auto unpacked_here = [&](int p) __attribute__((always_inline)) {
+      if constexpr (!AHEAD) asm volatile("" : "+v"(now.g[p]), "+v"(now.s[p]), "+v"(now.a[p]));
+    };
     const float q = now.q;
     float dot = 0.f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      float g[8], s[8];
+      float g[8], s[8], w[8];
+      unpacked_here(p);
       unpack8(gp[p], g);
       unpack8(sp[p], s);
+      weights(p, w);
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
-        dot = __builtin_fmaf(g[c] * w[p][c], s[c], dot);
-        dw[p][c] = __builtin_fmaf(g[c], s[c] * q, dw[p][c]);
+        dot = __builtin_fmaf(g[c] * w[c], s[c], dot);
+        if constexpr (AHEAD) dw[p][c] = __builtin_fmaf(g[c], s[c] * q, dw[p][c]);
       }
     }
     const float k = row_sum<TPR>(dot, part) / static_cast<float>(a.d) * q * q;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int i = i0 + p * TPR;
-      float g[8], s[8], v[8];
+      float g[8], s[8], w[8], v[8];
+      unpacked_here(p);                                   // (again, not kept over the row's sum)
       unpack8(gp[p], g);
       unpack8(sp[p], s);
       unpack8(ap[p], v);
+      weights(p, w);
 #pragma unroll
-      for (int c = 0; c < 8; ++c) v[c] = __builtin_fmaf(q, __builtin_fmaf(-s[c], k, g[c] * w[p][c]), v[c]);
+      for (int c = 0; c < 8; ++c) {
+        v[c] = __builtin_fmaf(q, __builtin_fmaf(-s[c], k, g[c] * w[c]), v[c]);
+        if constexpr (!AHEAD) dw[p][c] = __builtin_fmaf(g[c], s[c] * q, dw[p][c]);
+      }
       if (i < pieces) *reinterpret_cast<u32x4*>(a.dx + at + 8 * i) = pack8(v);
     }
+    if constexpr (AHEAD) now = next;
   }
   // the shares of the workgroup's rows meet in LDS, in the order of the rows
   if constexpr (ROWS > 1) {
@@ -326,7 +358,8 @@ template <typename F> void with_shape(int d, F&& f) {
 #undef MOE_NORM
 }
 // Workgroups of the backward pass, each with a share of dw: two per compute unit of a whole chip, one where a share is long, or as many as there are
-// rows for.  us with 256 / 512 / 1024: 8192 x 2048 34.1 / 33.4 / 39.9, 4001 x 4096 34.8 / 30.4 / 35.0, 2000 x 8192 36.0 / 40.7 / 51.5, 16384 x 136 13.3 / 11.9 / 15.0.
+// rows for.  us with 256 / 512 / 1024: 8192 x 2048 32.8 / 29.8 / 34.3, 4001 x 4096 34.5 / 29.4 / 32.0, 2000 x 8192 34.6 / 33.3 / 41.0, 1500 x 12288 37.9 / 42.2 / 51.3,
+// 500 x 32768 38.8 / 52.1 / 52.3, 16384 x 136 13.1 / 11.2 / 14.1.
 int norm_bwd_groups(int T, int d) {
   const int rows = rows_of_group(d), groups = (T - 1) / rows + 1, most = d <= 4096 ? 512 : 256;
   if (groups <= 4) return 1;                      // its share is dw: a few more rows in turn take less than another launch
