@@ -132,6 +132,8 @@ def _stream():
 
 
 def _want(t: torch.Tensor, dtype, shape=None, name="tensor"):
+    if t is None:
+        raise MoeError(f"{name} is missing")
     if t.dtype != dtype:
         raise MoeError(f"{name}: expected {dtype}, got {t.dtype}")
     if shape is not None and t.shape != shape:
@@ -471,29 +473,34 @@ def moe_head_bwd_workspace_bytes(T: int, d: int, V: int, K: int = 0, v_piece: in
     return int(load().moe_head_bwd_workspace_bytes(T, d, V, K, v_piece))
 
 
-def _head_args(x, W, target, ids=None, teacher=None, rows=()):
+def _head_args(x, W, target, rows):
     (T, d), V = x.shape, W.shape[0]
     _want(x, BF16, name="x")
     _want(W, BF16, (V, d), "W")
     _want(target, torch.int32, (T,), "target")
-    if ids is not None:
-        _want(ids, torch.int32, (T, ids.shape[-1]), "ids")
-        _want(teacher, torch.float32, tuple(ids.shape), "teacher")
     for name, t in rows:
         _want(t, torch.float32, (T,), name)
     return T, d, V
 
 
+def _teacher_args(T, ids, teacher):
+    _want(ids, torch.int32, name="ids")
+    K = ids.shape[-1]
+    _want(ids, torch.int32, (T, K), "ids")
+    _want(teacher, torch.float32, (T, K), "teacher")
+    return K
+
+
 def moe_head_ce_fwd(x, W, target, loss, lse, ws) -> None:
     """Cross entropy of the vocabulary head, token by token; a target outside the vocabulary (-100) counts for nothing."""
-    T, d, V = _head_args(x, W, target, rows=(("loss", loss), ("lse", lse)))
+    T, d, V = _head_args(x, W, target, (("loss", loss), ("lse", lse)))
     _check(load().moe_head_ce_fwd(_p(x), _p(W), _p(target), T, d, V, _p(loss), _p(lse), _p(ws), ws.numel() * ws.element_size(),
                                   _stream()), "moe_head_ce_fwd")
 
 
 def moe_head_ce_bwd(x, W, target, loss, lse, dloss, v_piece: int, dx, dW, ws) -> None:
     """dx and dW are overwritten; v_piece columns of the vocabulary at a time (0: the library chooses)."""
-    T, d, V = _head_args(x, W, target, rows=(("loss", loss), ("lse", lse), ("dloss", dloss)))
+    T, d, V = _head_args(x, W, target, (("loss", loss), ("lse", lse), ("dloss", dloss)))
     _want(dx, BF16, (T, d), "dx")
     _want(dW, BF16, (V, d), "dW")
     _check(load().moe_head_ce_bwd(_p(x), _p(W), _p(target), _p(loss), _p(lse), _p(dloss), T, d, V, v_piece, _p(dx), _p(dW), _p(ws),
@@ -502,19 +509,20 @@ def moe_head_ce_bwd(x, W, target, loss, lse, dloss, v_piece: int, dx, dW, ws) ->
 
 def moe_head_distill_fwd(x, W, target, ids, teacher, temperature: float, loss, lse, kd, lse_t, ws) -> None:
     """Cross entropy, and the divergence from a teacher given by K ids and logits per token (-1: no entry)."""
-    T, d, V = _head_args(x, W, target, ids, teacher, (("loss", loss), ("lse", lse), ("kd", kd), ("lse_t", lse_t)))
-    _check(load().moe_head_distill_fwd(_p(x), _p(W), _p(target), _p(ids), _p(teacher), temperature, T, d, V, ids.shape[1], _p(loss),
+    T, d, V = _head_args(x, W, target, (("loss", loss), ("lse", lse), ("kd", kd), ("lse_t", lse_t)))
+    K = _teacher_args(T, ids, teacher)
+    _check(load().moe_head_distill_fwd(_p(x), _p(W), _p(target), _p(ids), _p(teacher), temperature, T, d, V, K, _p(loss),
                                        _p(lse), _p(kd), _p(lse_t), _p(ws), ws.numel() * ws.element_size(), _stream()),
            "moe_head_distill_fwd")
 
 
 def moe_head_distill_bwd(x, W, target, ids, teacher, temperature: float, loss, lse, lse_t, dloss, dkd, v_piece: int, dx, dW, ws) -> None:
-    T, d, V = _head_args(x, W, target, ids, teacher,
-                         (("loss", loss), ("lse", lse), ("lse_t", lse_t), ("dloss", dloss), ("dkd", dkd)))
+    T, d, V = _head_args(x, W, target, (("loss", loss), ("lse", lse), ("lse_t", lse_t), ("dloss", dloss), ("dkd", dkd)))
+    K = _teacher_args(T, ids, teacher)
     _want(dx, BF16, (T, d), "dx")
     _want(dW, BF16, (V, d), "dW")
     _check(load().moe_head_distill_bwd(_p(x), _p(W), _p(target), _p(ids), _p(teacher), temperature, _p(loss), _p(lse), _p(lse_t),
-                                       _p(dloss), _p(dkd), T, d, V, ids.shape[1], v_piece, _p(dx), _p(dW), _p(ws),
+                                       _p(dloss), _p(dkd), T, d, V, K, v_piece, _p(dx), _p(dW), _p(ws),
                                        ws.numel() * ws.element_size(), _stream()), "moe_head_distill_bwd")
 
 
@@ -528,7 +536,7 @@ class HeadBuffers:
     def __init__(self, T: int, d: int, V: int, K: int = 0, v_piece: int = 0, train: bool = True, device="cuda:0"):
         dev = torch.device(device)
         row = lambda: torch.zeros(T, dtype=torch.float32, device=dev)  # noqa: E731
-        self.v_piece = v_piece
+        self.v_piece, self.train = v_piece, train
         self.loss, self.lse = row(), row()
         self.kd, self.lse_t = (row(), row()) if K else (None, None)
         nbytes = moe_head_fwd_workspace_bytes(T, d, V, K)
@@ -540,13 +548,21 @@ class HeadBuffers:
             raise MoeError(f"no head of {T} tokens, d {d}, {V} columns, {K} entries, pieces of {v_piece}")
         self.ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
 
+    def _fits(self, ids) -> None:
+        if ids is not None and self.kd is None:
+            raise MoeError("a teacher on buffers made without entries (K = 0)")
+
     def run_fwd(self, x, W, target, ids=None, teacher=None, temperature: float = 1.0) -> None:
+        self._fits(ids)
         if ids is None:
             moe_head_ce_fwd(x, W, target, self.loss, self.lse, self.ws)
         else:
             moe_head_distill_fwd(x, W, target, ids, teacher, temperature, self.loss, self.lse, self.kd, self.lse_t, self.ws)
 
     def run_bwd(self, x, W, target, dloss, ids=None, teacher=None, temperature: float = 1.0, dkd=None) -> None:
+        if not self.train:
+            raise MoeError("a backward pass on buffers made with train=False")
+        self._fits(ids)
         if ids is None:
             moe_head_ce_bwd(x, W, target, self.loss, self.lse, dloss, self.v_piece, self.dx, self.dW, self.ws)
         else:
