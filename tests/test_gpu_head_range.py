@@ -103,3 +103,21 @@ def test_temperatures_past_the_range(T):
     got = run(a, 1e-12, train=False)
     assert torch.equal(got["loss"], clean["loss"]) and torch.equal(got["lse"], clean["lse"])
     assert bool(torch.isnan(got["kd"]).all()) and bool(torch.isnan(got["lse_t"]).all())
+
+
+@pytest.mark.parametrize("T,K", [(60, 0), (60, 7), (200, 7), (500, 0), (500, 7), (4500, 0)])
+def test_what_stands_in_masked_places_leaves_no_trace(T, K):
+    """NaN, infinities and huge numbers wherever a token without a loss or an entry that does not count has one: the same bits as with ordinary numbers there."""
+    a = make(T, 64, 300, K, masked=0.4, seed=37)
+    out = a["target"] < 0
+    clean = run(a, 1.5)
+    for value in (NAN, INF, 3e38):
+        b = dict(a)
+        b["x"], b["dloss"] = a["x"].clone(), a["dloss"].clone()
+        b["x"][out], b["dloss"][out] = value, value
+        if K:
+            b["dkd"], b["teacher"] = a["dkd"].clone(), a["teacher"].clone()
+            b["dkd"][out] = value
+            b["teacher"][a["ids"] < 0] = value
+        for k, v in run(b, 1.5).items():
+            assert torch.equal(v, clean[k]), (value, k)
