@@ -335,7 +335,8 @@ int moe_router_bwd(const moe_bf16* x, const float* Wr, const float* dlogits, int
  * q[t] = 1 / sqrt(mean over c of s[t, c]^2 + eps):
  *   sum[t, c] = s[t, c];  y[t, c] = s[t, c] * q[t] * w[c]  (fp32, rounded once);  rstd[t] = q[t] if rstd is not NULL
  *   x, r, sum, y [T, d] bf16; w [d] fp32; rstd [T] fp32 or NULL.  r may be NULL (the first norm: s = x); sum may then be NULL.
- *   sum may be x or r, and y too.  d % 8 == 0, d <= 32768; eps >= 0.
+ *   sum may be x or r, and y too.  d % 8 == 0, d <= 32768; eps >= 0 (0: a row of zeros has no norm, its y is NaN).
+ *   A row whose squares sum up to more than fp32 holds (values of 1e19) counts as infinite: q = 0.
  */
 int moe_add_rms_norm(const moe_bf16* x, const moe_bf16* r, const float* w, int T, int d, float eps,
                      moe_bf16* sum, moe_bf16* y, float* rstd, void* stream);
@@ -363,7 +364,8 @@ int moe_add_rms_norm_bwd(const moe_bf16* dy, const moe_bf16* dsum, const moe_bf1
 /*
  * Behind the layers: softmax cross entropy of the vocabulary head without the logits in memory.  With z[t] = x[t] . W^T:
  *   lse[t] = log sum over v of exp(z[t, v]);  loss[t] = lse[t] - z[t, target[t]]
- * and zeros for a token whose target lies outside [0, V): it counts for nothing, and takes no time in the products.
+ * and zeros for a token whose target lies outside [0, V): it counts for nothing, and takes no time in the products (but in a forward pass of up to 256
+ * tokens, one pass over W in any case, or with a teacher in any pass of up to 128).  z[t, target[t]] is summed in 64 bits.
  *   x [T, d] bf16; W [V, d] bf16; target [T] int32; loss, lse [T] fp32.  d % 64 == 0; V <= 2^20.
  *   ws at least moe_head_fwd_workspace_bytes(T, d, V, 0): about T d * 2 + T V * 3 / 16 bytes.
  * A token with a logit that is NaN or infinite has NaN for its losses and its dx, and makes all of dW NaN.  So has one whose logits (for kd: over the
@@ -393,7 +395,8 @@ int moe_head_ce_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target,
  * (zeros for a token without entries), and loss, lse as above, either of the two with or without the other.
  *   ids [T, K] int32; teacher [T, K] fp32; kd, lse_t [T] fp32; 0 < temperature < infinity.
  * Backward, for dloss and dkd [T] fp32:  dz += dkd / temperature (p - q) for a token with entries.
- * Preconditions: a token's valid ids are distinct, their logits not +infinity or NaN.
+ * Entries may lie as far below each other as fp32 goes: one with q = 0 still has its p in kd and the gradient.
+ * Preconditions: a token's valid ids are distinct, their logits not +infinity.  (One that is NaN is left out.)
  */
 int moe_head_distill_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, const int32_t* ids, const float* teacher,
                          float temperature, int T, int d, int V, int K, float* loss, float* lse, float* kd, float* lse_t,

@@ -466,7 +466,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
     // rows and 4 (or 8) of columns; all rows of a column tile in a run would have every XCD fetch all rows in every round.
     m_end = head_rows;
     rt = (m_end + S - 1) / S;
-        const int band = tile / (8 * a.n_tiles), in = tile - band * 8 * a.n_tiles;
+    const int band = tile / (8 * a.n_tiles), in = tile - band * 8 * a.n_tiles;
     const int high = rt - band * 8 < 8 ? rt - band * 8 : 8;
     nt = in / high;
     m0 = (band * 8 + in - nt * high) * S;

@@ -5,11 +5,13 @@
 // The logits are never in memory.  Forward: the product's epilogue leaves a row's maximum and sum of exponentials for every strip of columns, and
 // the logits that count by themselves (target, entries); a last kernel joins them.  Backward: the logits once more, their gradient
 // rounded to bf16 (the products read it as their operand; half a step is 2^-9 of each element, against the 2^-9 of dx and dW themselves), then
-// the two products.  What bounds it is the matrix pipe: four products of 2 T V d operations, one of them for the logits a second time.
+// the two products.  What bounds it is the matrix pipe: four products of 2 T V d operations, one of them for the logits a second time, as the two calls share no memory
+// but the losses.  dx and dW are 0.0023 of their norm from 64 bits, 0.0017 of it their own rounding and as much that of dz: products of 32-bit
+// operands take eight times as long (the plain form), dz in two parts would, by count, take 45 % longer.
 //
-// us, with the library's products for the same sizes (no losses in them): 8192 tokens, d 2048, V 50304: logits and sums 1220 (1350), logits and gradient 1330,
-// dx and dW 2110 (1220 + 1610); all of the training step 4720.  The chip is at its power limit there (clock 1.7 to 1.96 GHz, matrix pipe busy 0.61 to 0.82).
-// One token: 39 for 206 MB of weights (5.2 TB/s), 57 tokens of d 4096, V 32003 46 for 262 MB (5.7 TB/s).
+// us, with the library's products for the same sizes (no losses in them): 8192 tokens, d 2048, V 50304: logits and sums 1220 to 1260 (1350), logits and gradient 1330 to 1390,
+// dx and dW 2110 to 2180 (1220 + 1610); all of the training step 4720 to 4940, by card.  The chip is at its power limit there (clock 1.7 to 1.96 GHz, matrix pipe busy 0.61 to 0.82).
+// One token: 40 for 206 MB of weights (5.2 TB/s), 57 tokens of d 4096, V 32003 46 for 262 MB (5.7 TB/s).
 //
 // Tokens without a loss are left out of all products: a first kernel finds the others, copies their rows of x side by side, and lists by blocks of
 // 16 rows and strips of 64 columns which logits count by themselves.

@@ -10,13 +10,10 @@ INF, NAN = float("inf"), float("nan")
 
 
 @pytest.mark.parametrize("T", [5, 40, 300])              # all tokens are rows; the same with more than one block; rows found first (with a teacher)
-@pytest.mark.parametrize("K", [0, 6, 300])
-@pytest.mark.parametrize("tau", [1.0, 1.5])
+@pytest.mark.parametrize("K,tau", [(0, 1.0), (6, 1.0), (6, 1.5), (300, 1.0), (300, 1.5)])
 @pytest.mark.parametrize("value", [NAN, INF, -INF])
 def test_a_token_that_is_not_finite(T, K, tau, value):
     """One number of a token's x makes its logits NaN or infinite, of either sign: its losses and gradient are NaN, as is dW, and the other tokens' are what they were."""
-    if K == 0 and tau != 1.0:
-        pytest.skip("no teacher, no temperature")
     a = make(T, 64, 400, K, seed=31)
     clean = run(a, tau)
     t = 3 if T < 20 else T - 2
@@ -32,13 +29,10 @@ def test_a_token_that_is_not_finite(T, K, tau, value):
 
 
 @pytest.mark.parametrize("T", [5, 300])
-@pytest.mark.parametrize("K", [0, 6])
-@pytest.mark.parametrize("row", ["target", "entry", "other"])
+@pytest.mark.parametrize("K,row", [(0, "target"), (0, "other"), (6, "target"), (6, "entry"), (6, "other")])
 @pytest.mark.parametrize("value", [NAN, INF])
 def test_a_column_that_is_not_finite(T, K, row, value):
     """A row of W that makes one logit of every token NaN or +infinity: the target's, an entry's or one that does not count by itself."""
-    if K == 0 and row == "entry":
-        pytest.skip("no entries")
     a = make(T, 64, 400, K, seed=32)
     a["x"][:, 5] = 1.0                                   # (an infinity of its own sign)
     v = {"target": 7, "entry": 8, "other": 9}[row]
