@@ -4,7 +4,7 @@
 //   dx = dz W;   dW = dz^T x
 // The logits are never in memory.  Forward: the product's epilogue leaves a row's maximum and sum of exponentials for every strip of columns, and
 // the logits that count by themselves (target, entries); a last kernel joins them.  Backward: the logits once more, their gradient
-// rounded to bf16 (the products read it as their operand; half a step is 2^-9 of each element, against the 2^-9 of dx and dW themselves), then
+// rounded to bf16 (the products read it as their operand; half a step is at most 2^-8 of each element, as it is of those of dx and dW themselves), then
 // the two products.  What bounds it is the matrix pipe: four products of 2 T V d operations, one of them for the logits a second time, as the two calls share no memory
 // but the losses.  dx and dW are 0.0023 of their norm from 64 bits, 0.0017 of it their own rounding and as much that of dz: products of 32-bit
 // operands take eight times as long (the plain form), dz in two parts would, by count, take 45 % longer.
