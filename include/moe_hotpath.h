@@ -22,6 +22,7 @@
  *
  * In front of the layer and behind it: moe_add_rms_norm (_8bit, _bwd), the residual's addition and the norm; moe_head_ce_fwd / _bwd and
  * moe_head_distill_fwd / _bwd, the vocabulary head's losses without its logits.
+ * In front of attention: moe_qk_norm_rope (_bwd), norms of queries and keys with the rotation.  Behind a backward pass: moe_grad_norm, moe_grad_clip.
  *
  * Conventions, valid for every function below
  * -------------------------------------------
@@ -404,6 +405,49 @@ int moe_head_distill_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* ta
 int moe_head_distill_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, const int32_t* ids, const float* teacher,
                          float temperature, const float* loss, const float* lse, const float* lse_t, const float* dloss, const float* dkd,
                          int T, int d, int V, int K, int v_piece, moe_bf16* dx, moe_bf16* dW, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Between a block's projections and its attention: the norm of every head's queries and keys, and the rotation by position, in one pass.  For a head's
+ * row x of D columns:  v = x w / sqrt(mean(x^2) + eps);  then R of its columns are turned, pair i by the angle pos[t] freq[i] (formed in 64 bits):
+ *   (a, b) -> (a cos - b sin, a sin + b cos),  the pairs being (2 i, 2 i + 1) if `pairs` is not 0, else (i, i + R / 2);  columns from R on stay.
+ *   q, qo [T, Hq, D], k, ko [T, Hk, D] bf16, each with its own distance `ld` from a token to the next in elements (a multiple of 8, at least H D: queries and
+ *   keys may be columns of a wider matrix); wq, wk [D] fp32; pos [T] int32 of any value; freq [R / 2] fp32 (may be NULL for R = 0).
+ *   D % 8 == 0, D <= 512; R % 16 == 0, 0 <= R <= D; Hq, Hk <= 4096; T <= 2^30.  qo may be q and ko may be k (with the same ld); no other overlap.
+ */
+int moe_qk_norm_rope(const moe_bf16* q, long long q_ld, const moe_bf16* k, long long k_ld, const float* wq, const float* wk, const int32_t* pos,
+                     const float* freq, int pairs, float eps, int T, int Hq, int Hk, int D, int R, moe_bf16* qo, long long qo_ld,
+                     moe_bf16* ko, long long ko_ld, void* stream);
+
+/*
+ * Its derivative, from the gradients dqo, dko of what it gave and the q, k that it was given (root and rotation are formed again):
+ *   dv = dqo turned back;  dq = r (dv w - q r^2 mean(dv w q)), r = 1 / sqrt(mean(q^2) + eps);  dwq = sum over tokens and heads of dv q r  (fp32, a fixed order)
+ * and likewise for k.  dq may be dqo or q, dk may be dko or k (with the same ld).  ws at least moe_qk_norm_rope_bwd_workspace_bytes(T, Hq, Hk, D).
+ */
+size_t moe_qk_norm_rope_bwd_workspace_bytes(int T, int Hq, int Hk, int D);
+int moe_qk_norm_rope_bwd(const moe_bf16* dqo, long long dqo_ld, const moe_bf16* dko, long long dko_ld, const moe_bf16* q, long long q_ld,
+                         const moe_bf16* k, long long k_ld, const float* wq, const float* wk, const int32_t* pos, const float* freq, int pairs,
+                         float eps, int T, int Hq, int Hk, int D, int R, moe_bf16* dq, long long dq_ld, moe_bf16* dk, long long dk_ld,
+                         float* dwq, float* dwk, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Behind a backward pass: the norm of all gradients of a model together, and their scaling to a largest norm.
+ *   norm[0] = sqrt(sum over all tensors of g^2)  (summed in 64 bits in a fixed order, then rounded to fp32)
+ *   moe_grad_clip: out = g min(1, largest / (norm + 1e-6)), rounded once; the norm is that of the 64-bit sum.  A norm of infinity makes finite gradients 0, one
+ *   of NaN makes all of them NaN.
+ * `grads` is a HOST array of n <= 2^20 tensors; it is read before the call returns, so a captured call keeps the addresses that it was given.  A tensor is dense, at any
+ * multiple of its elements' size, and may have no elements (its pointers are then not looked at).  out may be in: nothing is written where the norm is no
+ * larger than `largest`.  An output that overlaps another tensor's input or output is refused.  moe_grad_norm does not look at `out`.
+ *   norm [1] fp32; 0 < largest < infinity.  ws at least moe_grad_norm_workspace_bytes(n).
+ */
+enum { MOE_TYPE_BF16 = 0, MOE_TYPE_F32 = 1 };
+typedef struct moe_grad {
+  const void* in;
+  void* out;
+  int64_t count, type;
+} moe_grad;
+size_t moe_grad_norm_workspace_bytes(int n);
+int moe_grad_norm(const moe_grad* grads, int n, float* norm, void* ws, size_t ws_bytes, void* stream);
+int moe_grad_clip(const moe_grad* grads, int n, double largest, float* norm, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Several stages of one layer with one call: the calls above in the layer's order, on buffers that the caller

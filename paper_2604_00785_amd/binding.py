@@ -7,6 +7,7 @@ raised.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 import struct
@@ -29,6 +30,8 @@ EXPORTS = [
     "moe_add_rms_norm", "moe_add_rms_norm_8bit", "moe_add_rms_norm_bwd_workspace_bytes", "moe_add_rms_norm_bwd",
     "moe_head_fwd_workspace_bytes", "moe_head_bwd_workspace_bytes", "moe_head_ce_fwd", "moe_head_ce_bwd",
     "moe_head_distill_fwd", "moe_head_distill_bwd",
+    "moe_qk_norm_rope", "moe_qk_norm_rope_bwd_workspace_bytes", "moe_qk_norm_rope_bwd",
+    "moe_grad_norm_workspace_bytes", "moe_grad_norm", "moe_grad_clip",
 ]
 
 _ERR = {-1: "MOE_ERR_INVALID (bad pointer, alignment or size)", -2: "MOE_ERR_WORKSPACE (workspace too small)",
@@ -67,10 +70,11 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.moe_router_bwd_workspace_bytes.argtypes = [c_int] * 3
     lib.moe_permute_static_ws_capacity.restype = c_sz
     lib.moe_permute_static_ws_capacity.argtypes = []
-    for name, n in (("moe_add_rms_norm_bwd_workspace_bytes", 2), ("moe_head_fwd_workspace_bytes", 4), ("moe_head_bwd_workspace_bytes", 5)):
+    for name, n in (("moe_add_rms_norm_bwd_workspace_bytes", 2), ("moe_head_fwd_workspace_bytes", 4), ("moe_head_bwd_workspace_bytes", 5),
+                    ("moe_qk_norm_rope_bwd_workspace_bytes", 4), ("moe_grad_norm_workspace_bytes", 1)):
         getattr(lib, name).restype = c_sz
         getattr(lib, name).argtypes = [c_int] * n
-    c_float = ctypes.c_float
+    c_float, ll = ctypes.c_float, ctypes.c_longlong
     sigs = {
         "moe_route": [vp, c_int, c_int, c_int, c_int, vp, vp, vp],
         "moe_permute": [vp, vp, c_int, c_int, c_int, c_int, c_int, c_int, vp, vp, vp, vp, vp, c_sz, vp],
@@ -98,6 +102,10 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "moe_head_ce_bwd": [vp] * 6 + [c_int] * 4 + [vp] * 3 + [c_sz, vp],
         "moe_head_distill_fwd": [vp] * 5 + [c_float] + [c_int] * 4 + [vp] * 5 + [c_sz, vp],
         "moe_head_distill_bwd": [vp] * 5 + [c_float] + [vp] * 5 + [c_int] * 5 + [vp] * 3 + [c_sz, vp],
+        "moe_qk_norm_rope": [vp, ll] * 2 + [vp] * 4 + [c_int, c_float] + [c_int] * 5 + [vp, ll] * 2 + [vp],
+        "moe_qk_norm_rope_bwd": [vp, ll] * 4 + [vp] * 4 + [c_int, c_float] + [c_int] * 5 + [vp, ll] * 2 + [vp] * 3 + [c_sz, vp],
+        "moe_grad_norm": [vp, c_int, vp, vp, c_sz, vp],
+        "moe_grad_clip": [vp, c_int, ctypes.c_double, vp, vp, c_sz, vp],
         "moe_prof_enable": [c_int],
         "moe_prof_count": [],
         "moe_prof_read": [c_int, ctypes.c_char_p, c_int, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(c_int)],
@@ -524,6 +532,113 @@ def moe_head_distill_bwd(x, W, target, ids, teacher, temperature: float, loss, l
     _check(load().moe_head_distill_bwd(_p(x), _p(W), _p(target), _p(ids), _p(teacher), temperature, _p(loss), _p(lse), _p(lse_t),
                                        _p(dloss), _p(dkd), T, d, V, K, v_piece, _p(dx), _p(dW), _p(ws),
                                        ws.numel() * ws.element_size(), _stream()), "moe_head_distill_bwd")
+
+
+def _here(t, dtype, shape, name):
+    """The address of a dense tensor on the current device, whose stream the call is enqueued on."""
+    _want(t, dtype, shape, name)
+    return _where(t, name)
+
+
+def _where(t, name):
+    if t is None:
+        raise MoeError(f"{name} is missing")
+    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice() or not t.is_contiguous():
+        raise MoeError(f"{name}: tensors must be contiguous device tensors, on the current device")
+    return t.data_ptr()
+
+
+def _space(ws):
+    return _where(ws, "ws"), ws.numel() * ws.element_size()
+
+
+def _heads(t, T, H, D, name):
+    """Address and distance between tokens of [T, H, D]: a token's heads lie side by side, tokens may be rows of something wider."""
+    _want(t, BF16, (T, H, D), name)
+    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+        raise MoeError(f"{name}: tensors must be device tensors, on the current device")
+    by_token, by_head, by_column = t.stride()
+    if (D > 1 and by_column != 1) or (H > 1 and by_head != D):
+        raise MoeError(f"{name}: a token's heads must lie side by side, strides are {t.stride()}")
+    return t.data_ptr(), by_token if T > 1 else H * D
+
+
+def _qk_args(q, k, wq, wk, pos, freq):
+    for t, name in ((q, "q"), (k, "k")):
+        if t is None or t.dim() != 3:
+            raise MoeError(f"{name}: expected [tokens, heads, columns]")
+    (T, Hq, D), Hk = q.shape, k.shape[1]
+    R = 0
+    if freq is not None:
+        _want(freq, torch.float32, (freq.numel(),), "freq")
+        R = 2 * freq.numel()
+    return T, Hq, Hk, D, R, (_here(wq, torch.float32, (D,), "wq"), _here(wk, torch.float32, (D,), "wk"), _here(pos, torch.int32, (T,), "pos"),
+                             _where(freq, "freq") if R else None)
+
+
+def moe_qk_norm_rope(q, k, wq, wk, pos, freq, pairs: bool, eps: float, qo, ko) -> None:
+    """Norm of every head's queries and keys and their rotation by ``pos[t] * freq[i]``; ``pairs``: neighbours are turned, else halves.
+
+    ``freq`` has an entry for each pair of rotated columns (None: none is rotated).  qo may be q and ko may be k."""
+    T, Hq, Hk, D, R, w = _qk_args(q, k, wq, wk, pos, freq)
+    _check(load().moe_qk_norm_rope(*_heads(q, T, Hq, D, "q"), *_heads(k, T, Hk, D, "k"), *w, 1 if pairs else 0, eps, T, Hq, Hk, D, R,
+                                   *_heads(qo, T, Hq, D, "qo"), *_heads(ko, T, Hk, D, "ko"), _stream()), "moe_qk_norm_rope")
+
+
+def moe_qk_norm_rope_bwd_workspace_bytes(T: int, Hq: int, Hk: int, D: int) -> int:
+    return int(load().moe_qk_norm_rope_bwd_workspace_bytes(T, Hq, Hk, D))
+
+
+def moe_qk_norm_rope_bwd(dqo, dko, q, k, wq, wk, pos, freq, pairs: bool, eps: float, dq, dk, dwq, dwk, ws) -> None:
+    """From the gradients of what ``moe_qk_norm_rope`` gave for q and k.  dq may be dqo or q, dk may be dko or k."""
+    T, Hq, Hk, D, R, w = _qk_args(q, k, wq, wk, pos, freq)
+    _check(load().moe_qk_norm_rope_bwd(*_heads(dqo, T, Hq, D, "dqo"), *_heads(dko, T, Hk, D, "dko"), *_heads(q, T, Hq, D, "q"),
+                                       *_heads(k, T, Hk, D, "k"), *w, 1 if pairs else 0, eps, T, Hq, Hk, D, R, *_heads(dq, T, Hq, D, "dq"),
+                                       *_heads(dk, T, Hk, D, "dk"), _here(dwq, torch.float32, (D,), "dwq"), _here(dwk, torch.float32, (D,), "dwk"),
+                                       *_space(ws), _stream()), "moe_qk_norm_rope_bwd")
+
+
+_GRAD_TYPES = {BF16: 0, torch.float32: 1}
+
+
+def _grad_table(grads, outs):
+    """struct moe_grad of each tensor; the table is read before the call returns."""
+    if len(grads) == 0:
+        raise MoeError("grads: no tensors")
+    table = array.array("q")
+    for n, ts in (("grads", grads), ("outs", outs)):
+        dev = torch._C._cuda_getDevice() if ts[0].is_cuda else 0
+        for i, t in enumerate(ts):
+            if t.get_device() != dev or not t.is_contiguous():
+                raise MoeError(f"{n}[{i}]: tensors must be contiguous device tensors, on the current device")
+    for i, (g, o) in enumerate(zip(grads, outs)):
+        kind = _GRAD_TYPES.get(g.dtype)
+        if kind is None:
+            raise MoeError(f"grads[{i}]: expected bfloat16 or float32, got {g.dtype}")
+        if o is not g and (o.dtype is not g.dtype or o.shape != g.shape):
+            _want(o, g.dtype, g.shape, f"outs[{i}]")
+        table.extend((g.data_ptr(), o.data_ptr(), g.numel(), kind))
+    return table, table.buffer_info()[0], len(grads)
+
+
+def moe_grad_norm_workspace_bytes(n: int) -> int:
+    """For n tensors."""
+    return int(load().moe_grad_norm_workspace_bytes(n))
+
+
+def moe_grad_norm(grads, norm, ws) -> None:
+    """norm[0]: the norm of all these tensors (bfloat16 and float32) together."""
+    table, at, n = _grad_table(grads, grads)
+    _check(load().moe_grad_norm(at, n, _here(norm, torch.float32, (1,), "norm"), *_space(ws), _stream()), "moe_grad_norm")
+
+
+def moe_grad_clip(grads, largest: float, norm, outs, ws) -> None:
+    """The norm, and ``outs[i] = grads[i] * min(1, largest / (norm + 1e-6))``; outs None: in place."""
+    outs = grads if outs is None else outs
+    if len(outs) != len(grads):
+        raise MoeError(f"{len(grads)} gradients, {len(outs)} outs")
+    table, at, n = _grad_table(grads, outs)
+    _check(load().moe_grad_clip(at, n, largest, _here(norm, torch.float32, (1,), "norm"), *_space(ws), _stream()), "moe_grad_clip")
 
 
 class HeadBuffers:

@@ -1,0 +1,101 @@
+"""What the norms of queries and keys and the gradients' norm refuse before anything reaches a device."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2604_00785_amd import binding as B
+
+INVALID, WORKSPACE = -1, -2
+N, P, Q = None, ctypes.c_void_p(4096), ctypes.c_void_p(4104)      # never followed: a call that is refused reads nothing
+BIG = 1 << 40
+
+
+def qk_args(bwd):
+    """Names and values of a call that would go through."""
+    d = {}
+    if bwd:
+        d.update(dqo=P, dqo_ld=128, dko=P, dko_ld=64)
+    d.update(q=P, q_ld=128, k=P, k_ld=64, wq=P, wk=P, pos=P, freq=P, pairs=0, eps=1e-5, T=4, Hq=2, Hk=1, D=64, R=32)
+    d.update(dict(dq=P, dq_ld=128, dk=P, dk_ld=64, dwq=P, dwk=P, ws=P, n=BIG) if bwd else dict(qo=P, qo_ld=128, ko=P, ko_ld=64))
+    return d
+
+
+@pytest.mark.parametrize("bwd", [False, True])
+def test_qk_refusals(bwd):
+    lib = B.load()
+    fn = lib.moe_qk_norm_rope_bwd if bwd else lib.moe_qk_norm_rope
+    ok = qk_args(bwd)
+    bad = [(n, v) for n, p in ok.items() if p is P for v in (N, Q)]
+    bad += [(n, v) for n in ok if n.endswith("_ld") for v in (56, 0, -128, 132, (1 << 32) + 8)]
+    bad += [("T", 0), ("T", -1), ("T", (1 << 30) + 1), ("Hq", 0), ("Hk", 0), ("Hq", 4097), ("Hk", -1), ("D", 0), ("D", 60), ("D", 520), ("R", -16), ("R", 8),
+            ("R", 80), ("eps", -1e-5), ("eps", float("nan"))]
+    for name, value in bad:
+        assert fn(*dict(ok, **{name: value}).values(), N) == INVALID, (name, value)
+    # in place only with the rows where they are (here all tensors have one address)
+    for name in ("dq_ld", "dk_ld") if bwd else ("qo_ld", "ko_ld"):
+        assert fn(*dict(ok, **{name: 256}).values(), N) == INVALID, name
+    if bwd:
+        n = B.moe_qk_norm_rope_bwd_workspace_bytes(4, 2, 1, 64)
+        assert n > 0 and fn(*dict(ok, n=n - 1).values(), N) == WORKSPACE
+        for T, Hq, Hk, D in ((0, 2, 1, 64), (4, 0, 1, 64), (4, 2, 0, 64), (4, 2, 1, 60), (4, 2, 1, 1024)):
+            assert B.moe_qk_norm_rope_bwd_workspace_bytes(T, Hq, Hk, D) == 0
+        assert B.moe_qk_norm_rope_bwd_workspace_bytes(1 << 20, 32, 8, 128) <= 1 << 20           # shares do not grow with the tokens
+
+
+class Grad(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64), ("type", ctypes.c_int64)]
+
+
+def table(*rows):
+    return (Grad * len(rows))(*[Grad(*r) for r in rows])
+
+
+def test_grad_refusals():
+    lib = B.load()
+    ok = table((4096, 4096, 10, 0), (8192, 16384, 10, 1))
+    for call in (lambda g, n, norm, ws, b: lib.moe_grad_norm(g, n, norm, ws, b, N), lambda g, n, norm, ws, b: lib.moe_grad_clip(g, n, 1.0, norm, ws, b, N)):
+        for args in ((N, 2, P, P, BIG), (ok, 0, P, P, BIG), (ok, -1, P, P, BIG), (ok, (1 << 20) + 1, P, P, BIG), (ok, 2, N, P, BIG), (ok, 2, Q, P, BIG), (ok, 2, P, N, BIG),
+                     (ok, 2, P, Q, BIG)):
+            assert call(*args) == INVALID, args
+        assert call(ok, 2, P, P, B.moe_grad_norm_workspace_bytes(2) - 1) == WORKSPACE
+        for row in ((4096, 4096, 10, 2), (4096, 4096, 10, -1), (4096, 4096, -1, 0), (4096, 4096, (1 << 40) + 1, 0), (0, 4096, 10, 0), (4097, 4096, 10, 0),
+                    (4098, 4096, 10, 1)):
+            assert call(table((1 << 20, 1 << 20, 5, 0), row), 2, P, P, BIG) == INVALID, row
+    for largest in (0.0, -1.0, float("inf"), float("nan")):
+        assert lib.moe_grad_clip(ok, 2, largest, P, P, BIG, N) == INVALID
+    for row in ((4096, 0, 10, 0), (4096, 4097, 10, 0), (4096, 4098, 10, 1)):
+        assert lib.moe_grad_clip(table(row), 1, 1.0, P, P, BIG, N) == INVALID, row
+    assert B.moe_grad_norm_workspace_bytes(0) == 0 and B.moe_grad_norm_workspace_bytes(-3) == 0 and B.moe_grad_norm_workspace_bytes((1 << 20) + 1) == 0
+
+
+@pytest.mark.parametrize("more", [0, 300])
+def test_clipping_refuses_outputs_over_other_tensors(more):
+    """The same tensor twice, an output over another's input, over another's output, over its own input at another place."""
+    lib = B.load()
+    rest = [((1 << 30) + 4096 * i, (1 << 31) + 4096 * i, 100, 0) for i in range(more)]
+    for rows in ([(4096, 4096, 10, 0), (4096, 4096, 10, 0)], [(4096, 8192, 10, 0), (4112, 8200, 2, 1)], [(4096, 8192, 10, 0), (8210, 16384, 3, 0)],
+                 [(4096, 4100, 10, 0)], [(4096, 4092, 10, 1)], [(4096, 8192, 1000, 0), (4100, 4100, 1, 0)], [(4100, 4100, 1, 1), (4096, 16384, 8, 0)]):
+        assert lib.moe_grad_clip(table(*rest, *rows), more + len(rows), 1.0, P, P, BIG, N) == INVALID, rows
+
+
+def test_binding_refuses_types_shapes_and_host_tensors():
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    q, k, w, pos, freq, ws = bf(4, 2, 64), bf(4, 1, 64), torch.zeros(64), torch.zeros(4, dtype=torch.int32), torch.zeros(16), torch.zeros(1 << 20, dtype=torch.uint8)
+    one = torch.zeros(1)
+    calls = [
+        ("device", lambda: B.moe_qk_norm_rope(q, k, w, w, pos, freq, False, 1e-5, q, k)),               # on the host
+        ("wq", lambda: B.moe_qk_norm_rope(q, k, bf(64), w, pos, freq, False, 1e-5, q, k)),
+        ("q", lambda: B.moe_qk_norm_rope(q[0], k, w, w, pos, freq, False, 1e-5, q, k)),
+        ("k", lambda: B.moe_qk_norm_rope(q, None, w, w, pos, freq, False, 1e-5, q, k)),
+        ("freq", lambda: B.moe_qk_norm_rope(q, k, w, w, pos, freq.double(), False, 1e-5, q, k)),
+        ("freq", lambda: B.moe_qk_norm_rope(q, k, w, w, pos, freq.view(2, 8), False, 1e-5, q, k)),
+        ("grads", lambda: B.moe_grad_norm([q], one, ws)),                                                # on the host
+        ("grads", lambda: B.moe_grad_clip([q, q.half()], 1.0, one, None, ws)),
+        ("outs", lambda: B.moe_grad_clip([q, k], 1.0, one, [q], ws)),
+        ("no tensors", lambda: B.moe_grad_norm([], one, ws)),
+    ]
+    for n, (what, call) in enumerate(calls):
+        with pytest.raises(B.MoeError, match=what):
+            call()
+            raise AssertionError(n)
