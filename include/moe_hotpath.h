@@ -22,6 +22,7 @@
  *
  * In front of the layer and behind it: moe_add_rms_norm (_8bit, _bwd), the residual's addition and the norm; moe_head_ce_fwd / _bwd and
  * moe_head_distill_fwd / _bwd, the vocabulary head's losses without its logits.
+ * moe_head_score_fwd / _bwd, log probabilities of given tokens with entropies and the likeliest alternatives.
  * In front of attention: moe_qk_norm_rope (_bwd), norms of queries and keys with the rotation.  Behind a backward pass: moe_grad_norm, moe_grad_clip.
  *
  * Conventions, valid for every function below
@@ -405,6 +406,30 @@ int moe_head_distill_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* ta
 int moe_head_distill_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, const int32_t* ids, const float* teacher,
                          float temperature, const float* loss, const float* lse, const float* lse_t, const float* dloss, const float* dkd,
                          int T, int d, int V, int K, int v_piece, moe_bf16* dx, moe_bf16* dW, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * What the head says of given tokens, at a temperature: with s = x[t] . W^T / temperature and p = softmax(s) over the vocabulary,
+ *   lse[t] = log sum over v of exp(s[v]);  logp[t] = s[target[t]] - lse[t];  entropy[t] = -sum over v of p log p
+ *   ids[t, 0 .. K), top[t, 0 .. K): the K columns of largest s, largest first, of equal ones the lower column first, and their log p.
+ * A token whose target lies outside [0, V) counts for nothing: zeros, and ids of -1; beyond 256 tokens it takes no time in the products.
+ *   x [T, d], W [V, d] bf16; target, ids int32; the rest fp32.  d % 64 == 0; V <= 2^20; 0 <= K <= 64 and K <= V (0: ids, top may be NULL); 0 < temperature < infinity.
+ * Logits are compared in 64 bits among the K + 8 that are largest by the matrix product in 32 (its error is about 1e-6 of |x| |W row|).
+ * Log probabilities and entropies are sums of positive terms: they keep their digits next to zero.  Logits that are NaN or infinite, or 2^30 and more over the
+ * temperature, give NaN.  ws at least moe_head_score_fwd_workspace_bytes(T, d, V, K): about T d * 2 + T V * 5 / 8 bytes.
+ */
+size_t moe_head_score_fwd_workspace_bytes(int T, int d, int V, int K);
+int moe_head_score_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, int T, int d, int V, int K,
+                       float* logp, float* entropy, float* lse, int32_t* ids, float* top, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Its derivative for given dlogp and dentropy [T] fp32 (NULL: zeros), with logp, entropy and lse as the forward call left them:
+ *   dz[t, v] = (dlogp ([v == target] - p) - dentropy p (log p + entropy)) / temperature;  dx = dz . W;  dW = dz^T . x
+ * Sizes, pieces of the vocabulary, workspace and rounding as moe_head_ce_bwd.
+ */
+size_t moe_head_score_bwd_workspace_bytes(int T, int d, int V, int v_piece);
+int moe_head_score_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, const float* logp, const float* entropy,
+                       const float* lse, const float* dlogp, const float* dentropy, int T, int d, int V, int v_piece, moe_bf16* dx, moe_bf16* dW,
+                       void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Between a block's projections and its attention: the norm of every head's queries and keys, and the rotation by position, in one pass.  For a head's

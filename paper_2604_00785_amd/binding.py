@@ -30,6 +30,7 @@ EXPORTS = [
     "moe_add_rms_norm", "moe_add_rms_norm_8bit", "moe_add_rms_norm_bwd_workspace_bytes", "moe_add_rms_norm_bwd",
     "moe_head_fwd_workspace_bytes", "moe_head_bwd_workspace_bytes", "moe_head_ce_fwd", "moe_head_ce_bwd",
     "moe_head_distill_fwd", "moe_head_distill_bwd",
+    "moe_head_score_fwd_workspace_bytes", "moe_head_score_fwd", "moe_head_score_bwd_workspace_bytes", "moe_head_score_bwd",
     "moe_qk_norm_rope", "moe_qk_norm_rope_bwd_workspace_bytes", "moe_qk_norm_rope_bwd",
     "moe_grad_norm_workspace_bytes", "moe_grad_norm", "moe_grad_clip",
 ]
@@ -71,7 +72,8 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.moe_permute_static_ws_capacity.restype = c_sz
     lib.moe_permute_static_ws_capacity.argtypes = []
     for name, n in (("moe_add_rms_norm_bwd_workspace_bytes", 2), ("moe_head_fwd_workspace_bytes", 4), ("moe_head_bwd_workspace_bytes", 5),
-                    ("moe_qk_norm_rope_bwd_workspace_bytes", 4), ("moe_grad_norm_workspace_bytes", 1)):
+                    ("moe_qk_norm_rope_bwd_workspace_bytes", 4), ("moe_grad_norm_workspace_bytes", 1),
+                    ("moe_head_score_fwd_workspace_bytes", 4), ("moe_head_score_bwd_workspace_bytes", 4)):
         getattr(lib, name).restype = c_sz
         getattr(lib, name).argtypes = [c_int] * n
     c_float, ll = ctypes.c_float, ctypes.c_longlong
@@ -102,6 +104,8 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "moe_head_ce_bwd": [vp] * 6 + [c_int] * 4 + [vp] * 3 + [c_sz, vp],
         "moe_head_distill_fwd": [vp] * 5 + [c_float] + [c_int] * 4 + [vp] * 5 + [c_sz, vp],
         "moe_head_distill_bwd": [vp] * 5 + [c_float] + [vp] * 5 + [c_int] * 5 + [vp] * 3 + [c_sz, vp],
+        "moe_head_score_fwd": [vp] * 3 + [c_float] + [c_int] * 4 + [vp] * 6 + [c_sz, vp],
+        "moe_head_score_bwd": [vp] * 3 + [c_float] + [vp] * 5 + [c_int] * 4 + [vp] * 3 + [c_sz, vp],
         "moe_qk_norm_rope": [vp, ll] * 2 + [vp] * 4 + [c_int, c_float] + [c_int] * 5 + [vp, ll] * 2 + [vp],
         "moe_qk_norm_rope_bwd": [vp, ll] * 4 + [vp] * 4 + [c_int, c_float] + [c_int] * 5 + [vp, ll] * 2 + [vp] * 3 + [c_sz, vp],
         "moe_grad_norm": [vp, c_int, vp, vp, c_sz, vp],
@@ -550,6 +554,42 @@ def _where(t, name):
 
 def _space(ws):
     return _where(ws, "ws"), ws.numel() * ws.element_size()
+
+
+def moe_head_score_fwd_workspace_bytes(T: int, d: int, V: int, K: int = 0) -> int:
+    return int(load().moe_head_score_fwd_workspace_bytes(T, d, V, K))
+
+
+def moe_head_score_bwd_workspace_bytes(T: int, d: int, V: int, v_piece: int = 0) -> int:
+    return int(load().moe_head_score_bwd_workspace_bytes(T, d, V, v_piece))
+
+
+def _score_args(x, W, target):
+    if x is None or W is None or x.dim() != 2 or W.dim() != 2:
+        raise MoeError("x, W: expected [tokens, columns] and [vocabulary, columns]")
+    (T, d), V = x.shape, W.shape[0]
+    return T, d, V, (_here(x, BF16, (T, d), "x"), _here(W, BF16, (V, d), "W"), _here(target, torch.int32, (T,), "target"))
+
+
+def moe_head_score_fwd(x, W, target, temperature: float, logp, entropy, lse, ids, top, ws) -> None:
+    """Log probability of each target at a temperature, entropy of each token's distribution, and as many of its likeliest
+    alternatives as ids and top have columns (None: none); a target outside the vocabulary (-100) counts for nothing."""
+    T, d, V, given = _score_args(x, W, target)
+    K, lists = 0, (None, None)
+    if ids is not None or top is not None:
+        K = ids.shape[-1] if ids is not None else top.shape[-1]
+        lists = (_here(ids, torch.int32, (T, K), "ids"), _here(top, torch.float32, (T, K), "top"))
+    _check(load().moe_head_score_fwd(*given, temperature, T, d, V, K, *(_here(t, torch.float32, (T,), n) for t, n in ((logp, "logp"), (entropy, "entropy"), (lse, "lse"))),
+                                     *lists, *_space(ws), _stream()), "moe_head_score_fwd")
+
+
+def moe_head_score_bwd(x, W, target, temperature: float, logp, entropy, lse, dlogp, dentropy, v_piece: int, dx, dW, ws) -> None:
+    """From the gradients of log probabilities and (unless None) entropies; dx and dW are overwritten."""
+    T, d, V, given = _score_args(x, W, target)
+    rows = [(logp, "logp"), (entropy, "entropy"), (lse, "lse"), (dlogp, "dlogp")]
+    _check(load().moe_head_score_bwd(*given, temperature, *(_here(t, torch.float32, (T,), n) for t, n in rows),
+                                     None if dentropy is None else _here(dentropy, torch.float32, (T,), "dentropy"), T, d, V, v_piece,
+                                     _here(dx, BF16, (T, d), "dx"), _here(dW, BF16, (V, d), "dW"), *_space(ws), _stream()), "moe_head_score_bwd")
 
 
 def _heads(t, T, H, D, name):

@@ -59,6 +59,7 @@
 #include "common.h"
 #include "dma.h"
 #include "gemm.h"
+#include "head_score.h"
 
 namespace {
 
@@ -101,7 +102,7 @@ template <int N, typename F> __device__ __forceinline__ void static_for(F&& f) {
 }
 
 enum GemmMode { GATE_UP = 0, DOWN = 1, DGRAD_H = 2, DGRAD_X = 3, WGRAD = 4, WGRAD_GATHER = 5, DGRAD_H_GATE = 6,
-                WGRAD_GATHER_A = 7, HEAD_STATS = 8, HEAD_DZ = 9, HEAD_DX = 10, HEAD_DW = 11 };
+                WGRAD_GATHER_A = 7, HEAD_STATS = 8, HEAD_DZ = 9, HEAD_DX = 10, HEAD_DW = 11, HEAD_TOP = 12, HEAD_SCORE_DZ = 13 };
 // WGRAD_GATHER / WGRAD_GATHER_A: a weight gradient whose B / A operand rows are token rows found through
 // row_token.  DGRAD_H_GATE: DGRAD_H for a forward pass that folded the gate weight into h: its A rows are
 // rows of dout found through row_token, its epilogue scales by the row's gate weight and also emits the
@@ -109,8 +110,11 @@ enum GemmMode { GATE_UP = 0, DOWN = 1, DGRAD_H = 2, DGRAD_X = 3, WGRAD = 4, WGRA
 // The vocabulary head (head.hip), rows offsets[0] = 0 to offsets[1], one group.  HEAD_STATS, HEAD_DZ: logits A0 . B0^T of which the
 // epilogue makes a row's maximum and sums over the wave's columns, or the logits' gradient (row length M).  HEAD_DX: A0 (row length K) times
 // B0 in row_token[0] parts of the reduction over its M rows, each part's sums in 32 bits.  HEAD_DW: WGRAD with rows of M elements, K of them
-// wanted, in E parts of the reduction; with more than one O1 takes each part's sums in 32 bits.
-constexpr bool is_logits(int mode) { return mode == HEAD_STATS || mode == HEAD_DZ; }
+// wanted, in E parts of the reduction; with more than one O1 takes each part's sums in 32 bits.  HEAD_TOP: HEAD_STATS of all logits, which leaves the largest of every
+// few columns apart.  HEAD_SCORE_DZ: HEAD_DZ with the gradient of the entropy.
+constexpr bool is_logits(int mode) { return mode == HEAD_STATS || mode == HEAD_DZ || mode == HEAD_TOP || mode == HEAD_SCORE_DZ; }
+constexpr bool is_head_dz(int mode) { return mode == HEAD_DZ || mode == HEAD_SCORE_DZ; }
+constexpr bool is_head_fwd(int mode) { return mode == HEAD_STATS || mode == HEAD_TOP; }
 constexpr bool is_wgrad(int mode) { return mode == WGRAD || mode == WGRAD_GATHER || mode == WGRAD_GATHER_A || mode == HEAD_DW; }
 constexpr bool is_dgrad_h(int mode) { return mode == DGRAD_H || mode == DGRAD_H_GATE; }
 
@@ -146,8 +150,8 @@ struct GemmArgs {
 // by strips of 64 columns.
 struct HeadItem { uint32_t at, slot; };   // at: row in the block | column << 4
 struct HeadArgs {
-  float* part;                // HEAD_STATS: [row block][strips of HALF columns][2 or (two) 3][16 rows]: maximum, sum and sum at the temperature, without the items
-  const f32x4_t* row;         // HEAD_DZ: per row log2(e) lse, factor, and the same at the temperature
+  float* part;                // HEAD_TOP: HeadStrip [row block][strips of HALF columns][16 rows].  HEAD_STATS: [row block][strips of HALF columns][2 or (two) 3][16 rows]: maximum, sum and sum at the temperature, without the items
+  const f32x4_t* row;         // HEAD_DZ: per row log2(e) lse, factor, and the same at the temperature.  HEAD_SCORE_DZ: l, u, v of 2^t (u + v t), t = c1 z - l
   const int32_t* target;      // [row]
   const int32_t* list_start;  // [row block][list_ld]: first item of each strip; null: no teacher
   const HeadItem* items;      // [row block][16 slots]
@@ -404,7 +408,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
   // parts of dx.  (For every tile: a latency between the tiles, which counts where they have one or two steps.)
   int head_rows = 0, head_flag = 0;
   if constexpr (IS_HEAD) {
-    head_rows = __builtin_amdgcn_readfirstlane(MODE == HEAD_STATS && a.offsets == nullptr ? a.M : a.offsets[1]);
+    head_rows = __builtin_amdgcn_readfirstlane(is_head_fwd(MODE) && a.offsets == nullptr ? a.M : a.offsets[1]);
     head_flag = __builtin_amdgcn_readfirstlane(a.row_token == nullptr ? 0 : a.row_token[0]);
   }
 
@@ -1157,7 +1161,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
   f32x4_t early_term[IT] = {}, early_row[NB] = {};
   int item_lo = 0, item_hi = 0, list_lo = 0, list_hi = 0, item_at[IT], item_place[IT];
   bool many = false;
-  f32x4_t item_term[MODE == HEAD_DZ ? IT : 1], rowp[NB];
+  f32x4_t item_term[is_head_dz(MODE) ? IT : 1], rowp[NB];
   auto fetch_rows = [&](const TileState& t, f32x4_t (&to)[NB]) __attribute__((always_inline)) {
     const HeadPtr he = head_args();
 #pragma unroll
@@ -1170,13 +1174,13 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
   auto fetch_lists = [&](const TileState& t) __attribute__((always_inline)) {
     const HeadPtr he = head_args();
     const int first = t.m0 + t.r0, last = t.m_end - 1;
-    if constexpr (EARLY && MODE == HEAD_DZ) fetch_rows(t, early_row);
+    if constexpr (EARLY && is_head_dz(MODE)) fetch_rows(t, early_row);
     if (he->list_start == nullptr) {
 #pragma unroll
       for (int k = 0; k < IT; ++k) {
         const int r = first + lane + 64 * k, row = r < t.m_wave ? r : last;
         early_target[k] = he->target[row];
-        if constexpr (EARLY && MODE == HEAD_DZ) early_term[k] = he->terms[row];
+        if constexpr (EARLY && is_head_dz(MODE)) early_term[k] = he->terms[row];
       }
       asm volatile("" ::: "memory");
       return;
@@ -1202,7 +1206,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
         const int c = early_target[k] - col;
         item_at[k] = first + r < t.m_wave && c >= 0 && c < HALF ? r | c << 8 : -1;
         item_place[k] = row;
-        if constexpr (MODE == HEAD_DZ) item_term[k] = EARLY ? early_term[k] : he->terms[row];
+        if constexpr (is_head_dz(MODE)) item_term[k] = EARLY ? early_term[k] : he->terms[row];
       }
     } else {
       item_lo = list_lo;
@@ -1223,11 +1227,11 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
           const int r = part * 16 + (x.at & 15);
           item_at[k] = r | (static_cast<int>(x.at >> 4) - col) << 8;
           item_place[k] = (first + r) * he->slots + static_cast<int>(x.slot);
-          if constexpr (MODE == HEAD_DZ) item_term[k] = he->terms[at];
+          if constexpr (is_head_dz(MODE)) item_term[k] = he->terms[at];
         }
       }
     }
-    if constexpr (MODE == HEAD_DZ) {
+    if constexpr (is_head_dz(MODE)) {
       if constexpr (EARLY) {
 #pragma unroll
         for (int i = 0; i < NB; ++i) rowp[i] = early_row[i];
@@ -1505,7 +1509,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
           for (int k = 0; k < IT; ++k) {
             const bool there = item_at[k] >= 0 && (item_at[k] >> 4 & (HALF / 16 - 1)) == part;
             const int row = there ? item_at[k] & 15 : 0, c = there ? item_at[k] >> 8 : 0;
-            f(there, row, item_place[k], item_term[MODE == HEAD_DZ ? k : 0], z_piece(row, c >> 2) + (c & 3));
+            f(there, row, item_place[k], item_term[is_head_dz(MODE) ? k : 0], z_piece(row, c >> 2) + (c & 3));
           }
           return;
         }
@@ -1515,7 +1519,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
           const int n = n0 + lane < hi ? n0 + lane : hi - 1;
           const HeadItem x = he->items[first + n];
           const int row = x.at & 15, c = static_cast<int>(x.at >> 4) - he->col0 - gcol0;
-          f(n0 + lane < hi, row, (grow0 + part * 16 + row) * he->slots + static_cast<int>(x.slot), MODE == HEAD_DZ ? he->terms[first + n] : f32x4_t{},
+          f(n0 + lane < hi, row, (grow0 + part * 16 + row) * he->slots + static_cast<int>(x.slot), is_head_dz(MODE) ? he->terms[first + n] : f32x4_t{},
             z_piece(row, c >> 2) + (c & 3));
         }
       };
@@ -1585,6 +1589,55 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
           }
           if (lq < planes && i * 16 + l16 < rows) out[i * block] = lq == 0 ? m : lq == 1 ? s1 : s2;
         });
+      } else if constexpr (MODE == HEAD_TOP) {
+        HeadStrip* const out = reinterpret_cast<HeadStrip*>(he->part) + ((grow0 >> 4) * static_cast<size_t>(he->strips) + gcol0 / HALF) * 16 + l16;
+        static_for<NB>([&](auto i_tag) {
+          constexpr int i = decltype(i_tag)::value;
+          if (i * 16 >= rows || left <= 0) return;
+          f32x4_t v[NB];
+          static_for<NB>([&](auto j) { v[decltype(j)::value] = accq(i_tag, j); });
+          mask(v, NONE);
+          // One element after the other meets the largest so far: the smaller of the two takes its place among the others.  (These maxima and minima pass NaN on.)
+          float m = v[0][0];
+          int place = 0;
+          v[0][0] = NONE;
+          float next = NONE;
+#pragma unroll
+          for (int k = 1; k < 4 * NB; ++k) {
+            const float x = v[k / 4][k % 4];
+            place = x > m ? k : place;
+            const float less = __builtin_elementwise_minimum(m, x);
+            m = __builtin_elementwise_maximum(m, x);
+            v[k / 4][k % 4] = less;
+            next = fmaxf(next, less);
+          }
+          const float whole = quads_reduce(m, [](float x, float y) __attribute__((always_inline)) { return __builtin_elementwise_maximum(x, y); });
+          const float e1 = whole > NONE ? ceilf(whole * c1) : 0.f;
+          float sum = 0.f, moment = 0.f;
+#pragma unroll
+          for (int k = 1; k < 4 * NB; ++k) {
+            // (2^-1000 is 0, and 0 times -1000 too)
+            const float t = __builtin_elementwise_maximum(__builtin_fmaf(v[k / 4][k % 4], c1, -e1), -1000.f), e = __builtin_amdgcn_exp2f(t);
+            sum += e;
+            moment = __builtin_fmaf(e, t, moment);
+          }
+          const auto add = [](float x, float y) __attribute__((always_inline)) { return x + y; };
+          sum = quads_reduce(sum, add);
+          moment = quads_reduce(moment, add);
+          if (i * 16 + l16 < rows) {
+            HeadStrip* const o = out + static_cast<size_t>(i) * he->strips * 16;
+            constexpr uint32_t LOW = 4 * NB - 1;
+            u32x2 w;
+            w.x = __float_as_uint(m);
+            w.y = (ordered_u32(__float_as_uint(next)) & ~LOW) | static_cast<uint32_t>(place);
+            *reinterpret_cast<u32x2*>(&o->lane[lq]) = w;
+            if (lq == 0) {
+              w.x = __float_as_uint(sum);
+              w.y = __float_as_uint(moment);
+              *reinterpret_cast<u32x2*>(&o->sum) = w;
+            }
+          }
+        });
       } else {
         const int ld = ae->M;
         const Rsrc oo = rows_of(ae->O0, ld * 2);
@@ -1614,7 +1667,9 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
           f32x4_t v[NB];
           static_for<NB>([&](auto j) { v[decltype(j)::value] = accq(i_tag, j); });
           auto gradient = [&](float z) __attribute__((always_inline)) {
-            const float g = __builtin_amdgcn_exp2f(__builtin_fmaf(z, c1, -p[0])) * p[1];
+            const float t = __builtin_fmaf(z, c1, -p[0]);
+            if constexpr (MODE == HEAD_SCORE_DZ) return __builtin_amdgcn_exp2f(t) * __builtin_fmaf(p[2], t, p[1]);
+            const float g = __builtin_amdgcn_exp2f(t) * p[1];
             return two ? __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(z, c2, -p[2])), p[3], g) : g;
           };
           if (has_items(i_tag)) {
@@ -1739,7 +1794,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
   if (tile < total) {
     TileState cur;
     setup_tile(list_entry(), cur);
-    if constexpr (is_logits(MODE)) fetch_lists(cur);
+    if constexpr (is_logits(MODE) && MODE != HEAD_TOP) fetch_lists(cur);
     first_loads(cur);
     for (;;) {
       last_first_loads(cur);
@@ -1756,7 +1811,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
       if constexpr (MODE == GATE_UP || MODE == DGRAD_H_GATE) {
         if (weighted) fetch_row_weights(cur, a.row_weight);
       }
-      if constexpr (is_logits(MODE)) fetch_items(cur);
+      if constexpr (is_logits(MODE) && MODE != HEAD_TOP) fetch_items(cur);
       Finished done{cur.e, cur.m0, cur.n0, cur.r0, cur.m_wave, 0, 4, cur.second};
       if constexpr (MODE == HEAD_DW) {
         if (deal.extra > 1) tile += deal.by;
@@ -1779,10 +1834,10 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
 #pragma unroll
         for (int i = 0; i < NB; ++i) asm volatile("" : "+v"(wv[i]));
       }
-      if constexpr (is_logits(MODE)) {
+      if constexpr (is_logits(MODE) && MODE != HEAD_TOP) {
 #pragma unroll
         for (int k = 0; k < IT; ++k) asm volatile("" : "+v"(item_at[k]), "+v"(item_place[k]));
-        if constexpr (MODE == HEAD_DZ) {
+        if constexpr (is_head_dz(MODE)) {
 #pragma unroll
           for (int k = 0; k < IT; ++k) asm volatile("" : "+v"(item_term[k]));
 #pragma unroll

@@ -17,6 +17,7 @@
 // 16 rows and strips of 64 columns which logits count by themselves.
 #include <initializer_list>
 #include "gemm_tile.h"
+#include "head_score.h"
 
 namespace {
 
@@ -105,6 +106,9 @@ struct HeadPrepArgs {
   float *loss, *lse, *kd, *lse_t;  // forward: zeros for tokens without a loss
   const float *in_loss, *in_lse, *in_lse_t, *dloss, *dkd;
   f32x4_t* row;
+  // log probabilities with entropies, instead of losses (in_loss, dloss: log probability and its gradient); dentropy may be null
+  const float *in_entropy, *dentropy;
+  float over_tau;
 };
 
 // Workgroup (b, 0): rows 16 b to 16 b + 15 of those with a loss, in the order of their tokens; and tokens 16 b to 16 b + 15, if they have none.
@@ -249,7 +253,12 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   if (K == 0) {                                          // every row has a target, its only item
     if (l16 == 0 && r < n) {
       a.target_row[first + r] = y;
-      if (a.row != nullptr) {
+      if (a.in_entropy != nullptr) {
+        // dz = -p (u + v (log p + entropy)) / temperature, and at the target u (1 - p) in place of -u p
+        const float entropy = a.in_entropy[t], u = gl * a.over_tau, v = a.dentropy != nullptr ? a.dentropy[t] * a.over_tau : 0.f;
+        a.row[first + r] = f32x4_t{in_lse * LOG2E, -__builtin_fmaf(v, entropy, u), v * -0.693147180559945309f, 0.f};
+        a.terms[first + r] = f32x4_t{-__builtin_fmaf(expm1f(in_loss), u, expf(in_loss) * v * (in_loss + entropy)), 0.f, 0.f, 0.f};
+      } else if (a.row != nullptr) {
         a.row[first + r] = f32x4_t{in_lse * LOG2E, gl, 0.f, 0.f};
         a.terms[first + r] = f32x4_t{at_target, 0.f, 0.f, 0.f};
       }
@@ -723,6 +732,13 @@ struct HeadCall {
   moe_bf16 *dx, *dW;
   char* ws;
   hipStream_t s;
+  // log probabilities (loss, in_loss, dloss) at a temperature with entropies, and K alternatives
+  bool score;
+  float tau;
+  int K;
+  float *entropy, *top;
+  int32_t* ids;
+  const float *in_entropy, *dentropy;
 };
 
 int run_prep(const HeadCall& c, const HeadLayout& l, const BwdRule& dx, long long dx_room) {
@@ -748,6 +764,10 @@ int run_prep(const HeadCall& c, const HeadLayout& l, const BwdRule& dx, long lon
   p.items = reinterpret_cast<HeadItem*>(c.ws + l.items);
   p.loss = c.loss; p.lse = c.lse; p.kd = c.kd; p.lse_t = c.lse_t;
   p.in_loss = c.in_loss; p.in_lse = c.in_lse; p.in_lse_t = c.in_lse_t; p.dloss = c.dloss; p.dkd = c.dkd;
+  if (c.score) {
+    p.loss = nullptr;                                      // the join takes all tokens
+    p.in_entropy = c.in_entropy; p.dentropy = c.dentropy; p.over_tau = 1.f / c.tau;
+  }
   if (c.dx != nullptr) {
     p.terms = reinterpret_cast<f32x4_t*>(c.ws + l.terms);
     p.row = reinterpret_cast<f32x4_t*>(c.ws + l.row);
@@ -770,7 +790,7 @@ void fill_head(const HeadCall& c, const HeadLayout& l, GemmArgs& a, HeadArgs& h)
   h.item = reinterpret_cast<float*>(c.ws + l.item);
   h.terms = reinterpret_cast<const f32x4_t*>(c.ws + l.terms);
   h.row = reinterpret_cast<const f32x4_t*>(c.ws + l.row);
-  h.c1 = LOG2E;
+  h.c1 = c.score ? LOG2E / c.tau : LOG2E;
   h.c2 = LOG2E / c.t.temperature;
   h.over_tau = 1.f / c.t.temperature;
   h.two = c.t.K > 0 && c.t.temperature != 1.f;
@@ -818,6 +838,30 @@ int run_head_fwd(const HeadCall& c, int* edges) {
   return moe_check_launch();
 }
 
+size_t score_part_bytes(int T, int V) { return static_cast<size_t>((V + 63) / 64) * ((T + 15) & ~15) * sizeof(HeadStrip); }
+int run_score_fwd(const HeadCall& c, int* edges) {
+  const HeadLayout l = head_layout(c.T, c.d, c.V, 0, false);
+  GemmArgs a{};
+  HeadArgs h{};
+  fill_head(c, l, a, h);
+  a.A0 = reinterpret_cast<const uint16_t*>(c.ws + l.xc); a.A1 = c.x; a.B0 = c.W; a.K = c.d; a.N = c.V;
+  const bool all = c.T <= ALL_TOKENS;
+  int rc = MOE_OK;
+  if (all) {
+    a.offsets = nullptr; a.row_token = nullptr; a.A0 = c.x; a.M = c.T;
+  } else if ((rc = run_prep(c, l, BwdRule{}, 0)) != MOE_OK) {
+    return rc;
+  }
+  const int edge = settle_edge(edges, logits_edge(c.T, c.V, c.d, 9.5));
+  h.strips = ceil_div(c.V, edge / 2);
+  h.part = reinterpret_cast<float*>(c.ws + l.big);
+  if ((rc = launch_logits<HEAD_TOP>(a, h, edge, c.T, "gemm_head_top", c.s)) != MOE_OK) return rc;
+  const ScoreJoinArgs j{reinterpret_cast<const HeadStrip*>(h.part), all ? nullptr : reinterpret_cast<const int32_t*>(c.ws + l.control),
+                        reinterpret_cast<const int32_t*>(c.ws + l.token_row), c.target, c.x, c.W, c.T, c.d, c.V, c.K, h.strips, h.c1, 1.0 / c.tau,
+                        c.loss, c.entropy, c.lse, c.ids, c.top};
+  return moe_head_score_join(j, edge, c.s);
+}
+
 int run_head_bwd(const HeadCall& c, int v_piece, int* edges) {
   const HeadLayout l = head_layout(c.T, c.d, c.V, c.t.K, true);
   const int piece = head_piece(c.T, c.V, v_piece), wanted = edges != nullptr ? edges[1] : 0;
@@ -846,7 +890,8 @@ int run_head_bwd(const HeadCall& c, int v_piece, int* edges) {
     h.lo = l.low;
     const uint16_t* W = c.W + static_cast<size_t>(v0) * c.d;
     a.A0 = reinterpret_cast<const uint16_t*>(c.ws + l.xc); a.A1 = c.x; a.B0 = W; a.O0 = dz; a.K = c.d; a.N = cols; a.M = ld;
-    rc = launch_logits<HEAD_DZ>(a, h, settle_edge(edges, logits_edge(c.T, cols, c.d, 10.8)), c.T, "gemm_head_dz", c.s);
+    const int edge = settle_edge(edges, logits_edge(c.T, cols, c.d, 10.8));
+    rc = c.score ? launch_logits<HEAD_SCORE_DZ>(a, h, edge, c.T, "gemm_head_score_dz", c.s) : launch_logits<HEAD_DZ>(a, h, edge, c.T, "gemm_head_dz", c.s);
     if (rc != MOE_OK) return rc;
     GemmArgs b{};
     b.offsets = a.offsets; b.row_token = control + DX_PARTS; b.stream_rows = v0 > 0;
@@ -949,4 +994,50 @@ extern "C" int moe_head_distill_bwd(const moe_bf16* x, const moe_bf16* W, const 
                                     size_t ws_bytes, void* stream) {
   if (K <= 0) return MOE_ERR_INVALID;
   return moe_head_bwd(x, W, target, ids, teacher, temperature, loss, lse, lse_t, dloss, dkd, T, d, V, K, v_piece, dx, dW, ws, ws_bytes, stream, nullptr);
+}
+
+// Log probabilities, entropies and alternatives.  edges, for tests: as above.
+namespace {
+bool bad_score(int T, int d, int V, int K) { return bad_head_dims(T, d, V, 0) || K < 0 || K > SCORE_MAX_K || K > V; }
+}  // namespace
+extern "C" size_t moe_head_score_fwd_workspace_bytes(int T, int d, int V, int K) {
+  if (bad_score(T, d, V, K)) return 0;
+  return head_layout(T, d, V, 0, false).big + score_part_bytes(T, V);
+}
+extern "C" size_t moe_head_score_bwd_workspace_bytes(int T, int d, int V, int v_piece) { return moe_head_bwd_workspace_bytes(T, d, V, 0, v_piece); }
+
+extern "C" int moe_head_score_fwd_edges(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, int T, int d, int V, int K,
+                                        float* logp, float* entropy, float* lse, int32_t* ids, float* top, void* ws, size_t ws_bytes, void* stream,
+                                        int* edges) {
+  if (bad_score(T, d, V, K) || bad_temperature(temperature) || bad_edge_list(edges, 1)) return MOE_ERR_INVALID;
+  if (bad_ptrs({x, W, target, logp, entropy, lse, ws}) || (K > 0 && bad_ptrs({ids, top}))) return MOE_ERR_INVALID;
+  if (ws_bytes < moe_head_score_fwd_workspace_bytes(T, d, V, K)) return MOE_ERR_WORKSPACE;
+  HeadCall c{};
+  c.x = x; c.W = W; c.target = target; c.t.temperature = 1.f; c.T = T; c.d = d; c.V = V;
+  c.score = true; c.tau = temperature; c.K = K;
+  c.loss = logp; c.entropy = entropy; c.lse = lse; c.ids = ids; c.top = top;
+  c.ws = static_cast<char*>(ws); c.s = static_cast<hipStream_t>(stream);
+  return run_score_fwd(c, edges);
+}
+extern "C" int moe_head_score_bwd_edges(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, const float* logp,
+                                        const float* entropy, const float* lse, const float* dlogp, const float* dentropy, int T, int d, int V, int v_piece,
+                                        moe_bf16* dx, moe_bf16* dW, void* ws, size_t ws_bytes, void* stream, int* edges) {
+  if (bad_head_dims(T, d, V, 0) || bad_temperature(temperature) || v_piece < 0 || v_piece % 256 != 0 || bad_edge_list(edges, 2)) return MOE_ERR_INVALID;
+  if (bad_ptrs({x, W, target, logp, entropy, lse, dlogp, dx, dW, ws}) || !moe_aligned16(dentropy)) return MOE_ERR_INVALID;
+  if (ws_bytes < moe_head_score_bwd_workspace_bytes(T, d, V, v_piece)) return MOE_ERR_WORKSPACE;
+  HeadCall c{};
+  c.x = x; c.W = W; c.target = target; c.t.temperature = 1.f; c.T = T; c.d = d; c.V = V;
+  c.score = true; c.tau = temperature;
+  c.in_loss = logp; c.in_lse = lse; c.in_entropy = entropy; c.dloss = dlogp; c.dentropy = dentropy; c.dx = dx; c.dW = dW;
+  c.ws = static_cast<char*>(ws); c.s = static_cast<hipStream_t>(stream);
+  return run_head_bwd(c, v_piece, edges);
+}
+extern "C" int moe_head_score_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, int T, int d, int V, int K, float* logp,
+                                  float* entropy, float* lse, int32_t* ids, float* top, void* ws, size_t ws_bytes, void* stream) {
+  return moe_head_score_fwd_edges(x, W, target, temperature, T, d, V, K, logp, entropy, lse, ids, top, ws, ws_bytes, stream, nullptr);
+}
+extern "C" int moe_head_score_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, const float* logp, const float* entropy,
+                                  const float* lse, const float* dlogp, const float* dentropy, int T, int d, int V, int v_piece, moe_bf16* dx, moe_bf16* dW,
+                                  void* ws, size_t ws_bytes, void* stream) {
+  return moe_head_score_bwd_edges(x, W, target, temperature, logp, entropy, lse, dlogp, dentropy, T, d, V, v_piece, dx, dW, ws, ws_bytes, stream, nullptr);
 }

@@ -1,0 +1,28 @@
+// What the products of the vocabulary head leave for its scores, and the kernel that joins it.
+#pragma once
+#include "common.h"
+
+// HEAD_TOP: what a row has in a wave's HALF columns.  A lane's HALF / 4 of them (16 j + 4 l + c for lane l of four) have their largest logit apart; the others' sums, of all
+// four lanes together, are relative to 2^E, E the row's largest logit here in units of log2 rounded up, as in HEAD_STATS: sum = sum 2^t, moment = sum t 2^t, t <= 0.
+// next: the second largest of the lane's columns rounded up, as an integer in the order of the numbers, whose low bits are the largest one's place (4 j + c).
+struct HeadTop { float top; uint32_t next; };
+struct HeadStrip { HeadTop lane[4]; float sum, moment; };
+__host__ __device__ __forceinline__ uint32_t ordered_u32(uint32_t bits) { return bits ^ ((bits >> 31) != 0 ? 0xFFFFFFFFu : 0x80000000u); }
+
+constexpr int SCORE_MAX_K = 64, SCORE_SPARE = 8;
+constexpr int score_wanted(int K) { return K > 0 ? K + SCORE_SPARE : 1; }       // logits that are formed anew
+
+struct ScoreJoinArgs {
+  const HeadStrip* part;
+  const int32_t *control, *token_row, *target;     // control null: rows are tokens
+  const moe_bf16 *x, *W;
+  int T, d, V, K, strips;
+  float c1;                                        // log2(e) over the temperature
+  double over_tau;
+  float *logp, *entropy, *lse;
+  int32_t* ids;
+  float* top;
+};
+
+// edge: of the tiles that the strips are from (HALF = edge / 2)
+int moe_head_score_join(const ScoreJoinArgs& a, int edge, hipStream_t s);

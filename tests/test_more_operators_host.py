@@ -1,4 +1,4 @@
-"""What the norms of queries and keys and the gradients' norm refuse before anything reaches a device."""
+"""What the head's scores, the norms of queries and keys and the gradients' norm refuse before anything reaches a device."""
 import ctypes
 
 import pytest
@@ -99,3 +99,45 @@ def test_binding_refuses_types_shapes_and_host_tensors():
         with pytest.raises(B.MoeError, match=what):
             call()
             raise AssertionError(n)
+
+
+def score_args(bwd):
+    d = dict(x=P, W=P, target=P, temperature=1.0)
+    if bwd:
+        d.update(logp=P, entropy=P, lse=P, dlogp=P, dentropy=P, T=4, d=64, V=100, v_piece=0, dx=P, dW=P, ws=P, n=BIG)
+    else:
+        d.update(T=4, d=64, V=100, K=5, logp=P, entropy=P, lse=P, ids=P, top=P, ws=P, n=BIG)
+    return d
+
+
+@pytest.mark.parametrize("bwd", [False, True])
+def test_score_refusals(bwd):
+    lib = B.load()
+    fn = lib.moe_head_score_bwd if bwd else lib.moe_head_score_fwd
+    ok = score_args(bwd)
+    bad = [(n, v) for n, p in ok.items() if p is P for v in (N, Q) if (n, v) != ("dentropy", N)]
+    bad += [("T", 0), ("T", -2), ("T", (1 << 26) + 1), ("d", 0), ("d", 32), ("d", 100), ("V", 0), ("V", (1 << 20) + 1)]
+    bad += [("temperature", v) for v in (0.0, -1.0, float("inf"), float("nan"))]
+    bad += [("v_piece", v) for v in (-256, 1, 300)] if bwd else [("K", -1), ("K", 65), ("V", 4)]
+    for name, value in bad:
+        assert fn(*dict(ok, **{name: value}).values(), N) == INVALID, (name, value)
+    assert fn(*dict(ok, n=100).values(), N) == WORKSPACE
+    if bwd:
+        assert B.moe_head_score_bwd_workspace_bytes(4, 64, 100, 300) == 0 and B.moe_head_score_bwd_workspace_bytes(4, 60, 100) == 0
+    else:
+        for T, d, V, K in ((0, 64, 100, 5), (4, 60, 100, 5), (4, 64, 0, 0), (4, 64, 100, 65), (4, 64, 4, 5), (4, 64, 100, -1)):
+            assert B.moe_head_score_fwd_workspace_bytes(T, d, V, K) == 0
+        assert B.moe_head_score_fwd_workspace_bytes(8192, 2048, 50304, 20) < 8192 * 50304           # far from the logits (2 bytes each)
+
+
+def test_scores_in_the_binding():
+    bf, f32 = lambda *s: torch.zeros(*s, dtype=torch.bfloat16), lambda *s: torch.zeros(*s)  # noqa: E731
+    x, W, y, r, ids, ws = bf(4, 64), bf(100, 64), torch.zeros(4, dtype=torch.int32), f32(4), torch.zeros(4, 5, dtype=torch.int32), torch.zeros(1 << 20, dtype=torch.uint8)
+    for what, call in [
+        ("device", lambda: B.moe_head_score_fwd(x, W, y, 1.0, r, r, r, ids, f32(4, 5), ws)),             # on the host
+        ("x", lambda: B.moe_head_score_fwd(f32(4, 64), W, y, 1.0, r, r, r, ids, f32(4, 5), ws)),
+        ("x, W", lambda: B.moe_head_score_fwd(None, W, y, 1.0, r, r, r, ids, f32(4, 5), ws)),
+        ("x, W", lambda: B.moe_head_score_bwd(x, W[0], y, 1.0, r, r, r, r, r, 0, x, W, ws)),
+    ]:
+        with pytest.raises(B.MoeError, match=what):
+            call()
