@@ -150,7 +150,7 @@ struct GemmArgs {
 // by strips of 64 columns.
 struct HeadItem { uint32_t at, slot; };   // at: row in the block | column << 4
 struct HeadArgs {
-  float* part;                // HEAD_TOP: HeadStrip [row block][strips of HALF columns][16 rows].  HEAD_STATS: [row block][strips of HALF columns][2 or (two) 3][16 rows]: maximum, sum and sum at the temperature, without the items
+  float* part;                // HEAD_TOP: HeadStrip [row][strips of HALF columns].  HEAD_STATS: [row block][strips of HALF columns][2 or (two) 3][16 rows]: maximum, sum and sum at the temperature, without the items
   const f32x4_t* row;         // HEAD_DZ: per row log2(e) lse, factor, and the same at the temperature.  HEAD_SCORE_DZ: l, u, v of 2^t (u + v t), t = c1 z - l
   const int32_t* target;      // [row]
   const int32_t* list_start;  // [row block][list_ld]: first item of each strip; null: no teacher
@@ -1590,7 +1590,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
           if (lq < planes && i * 16 + l16 < rows) out[i * block] = lq == 0 ? m : lq == 1 ? s1 : s2;
         });
       } else if constexpr (MODE == HEAD_TOP) {
-        HeadStrip* const out = reinterpret_cast<HeadStrip*>(he->part) + ((grow0 >> 4) * static_cast<size_t>(he->strips) + gcol0 / HALF) * 16 + l16;
+        HeadStrip* const out = reinterpret_cast<HeadStrip*>(he->part) + static_cast<size_t>(grow0 + l16) * he->strips + gcol0 / HALF;
         static_for<NB>([&](auto i_tag) {
           constexpr int i = decltype(i_tag)::value;
           if (i * 16 >= rows || left <= 0) return;
@@ -1625,7 +1625,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
           sum = quads_reduce(sum, add);
           moment = quads_reduce(moment, add);
           if (i * 16 + l16 < rows) {
-            HeadStrip* const o = out + static_cast<size_t>(i) * he->strips * 16;
+            HeadStrip* const o = out + static_cast<size_t>(i * 16) * he->strips;
             constexpr uint32_t LOW = 4 * NB - 1;
             u32x2 w;
             w.x = __float_as_uint(m);

@@ -4,6 +4,7 @@
 // size have a norm; each workgroup leaves its sum, and whoever needs the norm adds these up in one order: no atomics, the same bits every time.
 #include <algorithm>
 #include <new>
+#include <type_traits>
 #include "common.h"
 
 namespace {
@@ -12,29 +13,30 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 // (tensors may begin anywhere in a buffer of many: at multiples of their elements' size)
 typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t u32x4_any;
 
-// What a launch knows of its tensors comes with its arguments, so that nothing has to be copied to the device first, in a graph or out of it.
-constexpr int TENSORS = 120;                        // of a launch: 4 KB of arguments
-constexpr int GRAD_GROUPS = 1024;                   // workgroups of a launch at most, each with its sum
+// What a launch knows of its tensors comes with its arguments, so that nothing has to be copied to the device first, in a graph or out of it: at most 4 KB of them, and
+// less where there are few.  A tensor's chunks are CHUNK bytes each but for the last.
+constexpr int GRAD_THREADS = 256, GRAD_GROUPS = 2048;   // workgroups of a launch at most, each with its sum
+constexpr int FEW_TENSORS = 24, NORM_TENSORS = 240, CLIP_TENSORS = 160;
 constexpr int MAX_TENSORS = 1 << 20;
-struct GradTable {
-  const void* in[TENSORS];
-  void* out[TENSORS];
-  uint64_t count[TENSORS];                          // elements, and in the lowest bit whether they have 32 bits
-  uint32_t first[TENSORS + 1];                      // first chunk
-  uint32_t n;
+template <int CAP, bool CLIP> struct GradTable {
+  const void* in[CAP];
+  void* out[CLIP ? CAP : 1];
+  uint32_t first[CAP + 1];                          // first chunk
+  uint32_t last[CAP];                               // elements of the last chunk, and in the lowest bit whether they have 32 bits
+  uint32_t n, each, more;                           // chunks of a workgroup: each, and one more for the first `more` of them
 };
-static_assert(sizeof(GradTable) <= 3900, "kernel arguments");
+static_assert(sizeof(GradTable<NORM_TENSORS, false>) <= 3968 && sizeof(GradTable<CLIP_TENSORS, true>) <= 3968, "kernel arguments");
 
-__device__ __forceinline__ void add_squares(const u32x4& v, bool f32, double& s) {
+template <bool F32> __device__ __forceinline__ void add_squares(const u32x4& v, double (&s)[2]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (f32) {
+    if constexpr (F32) {
       const double a = static_cast<double>(__uint_as_float(v[i]));
-      s = __builtin_fma(a, a, s);
+      s[i & 1] = __builtin_fma(a, a, s[i & 1]);
     } else {
       const double a = static_cast<double>(bf16lo(v[i])), b = static_cast<double>(bf16hi(v[i]));
-      s = __builtin_fma(a, a, s);
-      s = __builtin_fma(b, b, s);
+      s[0] = __builtin_fma(a, a, s[0]);
+      s[1] = __builtin_fma(b, b, s[1]);
     }
   }
 }
@@ -51,103 +53,153 @@ __device__ __forceinline__ double group_total(double v, double (&part)[4]) {
   return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// f(tensor, is 32 bits, first piece of 16 bytes, pieces of the tensor, its elements, whether this is its last chunk) for the workgroup's chunks, a run of them: of
-// 256 U pieces each.
-template <int U, typename F> __device__ __forceinline__ void over_chunks(const GradTable& t, uint32_t total, bool backwards, F&& f) {
-  const uint32_t b = backwards ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
-  const uint32_t c0 = static_cast<uint32_t>(static_cast<uint64_t>(total) * b / gridDim.x), c1 = static_cast<uint32_t>(static_cast<uint64_t>(total) * (b + 1) / gridDim.x);
+// A thread's pieces of a chunk: U of 16 bytes, 256 apart.
+template <int U> __device__ __forceinline__ void load_chunk(const u32x4_any* p, u32x4 (&v)[U]) {
+#pragma unroll
+  for (int u = 0; u < U; ++u) v[u] = p[u * GRAD_THREADS + threadIdx.x];
+}
+// whole(type, tensor, first chunk, chunks) for the workgroup's runs of whole chunks of one tensor, from the last to the first if `backwards`;
+// rest(type, tensor, chunk, elements) for a tensor's last chunk, which may be a whole one.
+template <int CAP, bool CLIP, typename Whole, typename Rest>
+__device__ __forceinline__ void over_chunks(const GradTable<CAP, CLIP>& t, bool backwards, Whole&& whole, Rest&& rest) {
+  const uint32_t b = blockIdx.x, c0 = b * t.each + (b < t.more ? b : t.more), c1 = c0 + t.each + (b < t.more ? 1 : 0);
   if (c0 >= c1) return;
-  uint32_t e = 0;                                   // the last tensor whose first chunk is not behind c0
-  for (uint32_t step = 64; step > 0; step /= 2)
-    if (e + step < t.n && t.first[e + step] <= c0) e += step;
-  for (uint32_t c = c0; c < c1; ++e) {
-    const uint32_t first = t.first[e], end = t.first[e + 1], to = end < c1 ? end : c1;
-    const bool f32 = (t.count[e] & 1) != 0;
-    const uint64_t count = t.count[e] >> 1, pieces = count / (f32 ? 4 : 8);
-    for (; c < to; ++c) f(e, f32, static_cast<uint64_t>(c - first) * (256 * U), pieces, count, c + 1 == end);
+  const auto tensor_of = [&](uint32_t c) __attribute__((always_inline)) {   // the last whose first chunk is not behind c
+    uint32_t e = 0;
+#pragma unroll
+    for (uint32_t step = 128; step > 0; step /= 2)
+      if (e + step < t.n && t.first[e + step] <= c) e += step;
+    return e;
+  };
+  const auto part = [&](uint32_t e) __attribute__((always_inline)) {
+    const uint32_t first = t.first[e], end = t.first[e + 1], from = c0 > first ? c0 : first, to = c1 < end ? c1 : end, last = t.last[e];
+    const bool ends = to == end;
+    const uint32_t n = to - from - (ends ? 1 : 0);
+    if ((last & 1) != 0) {
+      if (backwards && ends) rest(std::true_type{}, e, end - 1 - first, last >> 1);
+      if (n > 0) whole(std::true_type{}, e, from - first, n);
+      if (!backwards && ends) rest(std::true_type{}, e, end - 1 - first, last >> 1);
+    } else {
+      if (backwards && ends) rest(std::false_type{}, e, end - 1 - first, last >> 1);
+      if (n > 0) whole(std::false_type{}, e, from - first, n);
+      if (!backwards && ends) rest(std::false_type{}, e, end - 1 - first, last >> 1);
+    }
+  };
+  if (!backwards) {
+    for (uint32_t e = tensor_of(c0); e < t.n && t.first[e] < c1; ++e) part(e);
+  } else {
+    for (uint32_t e = tensor_of(c1 - 1) + 1; e-- > 0 && t.first[e + 1] > c0;) part(e);
   }
 }
 
-template <int U> __global__ __launch_bounds__(256) void grad_norm_kernel(GradTable t, double* __restrict__ sums) {
+template <int U, int CAP> __global__ __launch_bounds__(GRAD_THREADS) void grad_norm_kernel(GradTable<CAP, false> t, double* __restrict__ sums) {
   __shared__ double part[4];
-  double s = 0.0;
-  over_chunks<U>(t, t.first[t.n], false, [&](uint32_t e, bool f32, uint64_t p0, uint64_t pieces, uint64_t count, bool last) __attribute__((always_inline)) {
-    const u32x4_any* in = static_cast<const u32x4_any*>(t.in[e]);
+  double s[2] = {0.0, 0.0};
+  over_chunks(t, false, [&](auto f32, uint32_t e, uint32_t c, uint32_t n) __attribute__((always_inline)) {
+    constexpr bool F32 = decltype(f32)::value;
+    const u32x4_any* p = static_cast<const u32x4_any*>(t.in[e]) + static_cast<size_t>(c) * (GRAD_THREADS * U);
+    u32x4 v[U], w[U];
+    load_chunk<U>(p, v);
+    for (; n > 1; --n) {                            // the next chunk is requested before this one is used
+      p += GRAD_THREADS * U;
+      load_chunk<U>(p, w);
+#pragma unroll
+      for (int u = 0; u < U; ++u) add_squares<F32>(v[u], s);
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = w[u];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) add_squares<F32>(v[u], s);
+  }, [&](auto f32, uint32_t e, uint32_t c, uint32_t count) __attribute__((always_inline)) {
+    constexpr bool F32 = decltype(f32)::value;
+    constexpr uint32_t PER = F32 ? 4 : 8;
+    const u32x4_any* p = static_cast<const u32x4_any*>(t.in[e]) + static_cast<size_t>(c) * (GRAD_THREADS * U);
+    const uint32_t pieces = count / PER;
     u32x4 v[U];
-    if (p0 + 256 * U <= pieces) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = in[p0 + u * 256 + threadIdx.x];
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const uint64_t p = p0 + u * 256 + threadIdx.x;
-        v[u] = u32x4{0, 0, 0, 0};
-        if (p < pieces) v[u] = in[p];
-      }
+    for (int u = 0; u < U; ++u) {
+      v[u] = u32x4{0, 0, 0, 0};
+      if (u * GRAD_THREADS + threadIdx.x < pieces) v[u] = p[u * GRAD_THREADS + threadIdx.x];
+    }
+    if (threadIdx.x < count % PER) {
+      const uint32_t at = pieces * PER + threadIdx.x;
+      const double a = F32 ? reinterpret_cast<const float*>(p)[at] : bf16_to_f32(reinterpret_cast<const uint16_t*>(p)[at]);
+      s[0] = __builtin_fma(a, a, s[0]);
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u) add_squares(v[u], f32, s);
-    const uint64_t at = pieces * (f32 ? 4 : 8) + threadIdx.x;
-    if (last && at < count) {
-      const float a = f32 ? static_cast<const float*>(t.in[e])[at] : bf16_to_f32(static_cast<const uint16_t*>(t.in[e])[at]);
-      s = __builtin_fma(static_cast<double>(a), static_cast<double>(a), s);
-    }
+    for (int u = 0; u < U; ++u) add_squares<F32>(v[u], s);
   });
-  s = group_total(s, part);
-  if (threadIdx.x == 0) sums[blockIdx.x] = s;
+  const double total = group_total(s[0] + s[1], part);
+  if (threadIdx.x == 0) sums[blockIdx.x] = total;
 }
 
 // sqrt of the workgroups' sums, in every thread of a workgroup of 256
 __device__ __forceinline__ double norm_of(const double* sums, int n, double (&part)[4]) {
   double s = 0.0;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < n; i += 256) s += sums[i];
+#pragma unroll 8
+  for (int i = threadIdx.x; i < n; i += GRAD_THREADS) s += sums[i];
   return sqrt(group_total(s, part));
 }
-__global__ __launch_bounds__(256) void grad_norm_finish_kernel(const double* __restrict__ sums, int n, float* __restrict__ norm) {
+__global__ __launch_bounds__(GRAD_THREADS) void grad_norm_finish_kernel(const double* __restrict__ sums, int n, float* __restrict__ norm) {
   __shared__ double part[4];
   const double v = norm_of(sums, n, part);
   if (threadIdx.x == 0) norm[0] = static_cast<float>(v);
 }
 
-// Backwards through the chunks, so that what the norm has read last, and the caches still hold, is read first.
-template <int U> __global__ __launch_bounds__(256) void grad_clip_kernel(GradTable t, const double* __restrict__ sums, int n, double largest, float* __restrict__ norm) {
+// Each workgroup goes backwards through the chunks that it had for the norm: what was read last, and the caches still hold, is read first.
+template <int U, int CAP> __global__ __launch_bounds__(GRAD_THREADS) void grad_clip_kernel(GradTable<CAP, true> t, const double* __restrict__ sums, int n_sums, double largest,
+                                                                                           float* __restrict__ norm) {
   __shared__ double part[4];
-  const double v = norm_of(sums, n, part), ratio = largest / (v + 1e-6);
+  const double v = norm_of(sums, n_sums, part), ratio = largest / (v + 1e-6);
   if (norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) norm[0] = static_cast<float>(v);
   // As m 2^e with m in [1/2, 1): a scale may lie below what 32 bits hold where the gradients are as large.  (NaN stays NaN.)
-  int e = 0;
-  const float m = ratio >= 1.0 ? 1.f : static_cast<float>(frexp(ratio, &e));
-  if (ratio >= 1.0) e = 0;
-  const auto scaled1 = [&](float x) __attribute__((always_inline)) { return __builtin_amdgcn_ldexpf(x * m, e); };
-  const bool same = m == 1.f && e == 0;
-  over_chunks<U>(t, t.first[t.n], true, [&](uint32_t which, bool f32, uint64_t p0, uint64_t pieces, uint64_t count, bool last) __attribute__((always_inline)) {
-    if (same && t.in[which] == t.out[which]) return;
-    const u32x4_any* in = static_cast<const u32x4_any*>(t.in[which]);
-    u32x4_any* out = static_cast<u32x4_any*>(t.out[which]);
-    auto scaled = [&](u32x4 x) __attribute__((always_inline)) {
+  int exponent = 0;
+  const float m = ratio >= 1.0 ? 1.f : static_cast<float>(frexp(ratio, &exponent));
+  if (ratio >= 1.0) exponent = 0;
+  const bool same = m == 1.f && exponent == 0;
+  const auto scaled = [&](float x) __attribute__((always_inline)) { return __builtin_amdgcn_ldexpf(x * m, exponent); };
+  const auto scaled4 = [&](auto f32, u32x4 x) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        x[i] = f32 ? __float_as_uint(scaled1(__uint_as_float(x[i]))) : pack_bf16(scaled1(bf16lo(x[i])), scaled1(bf16hi(x[i])));
-      return x;
-    };
-    u32x4 v[U];
-    if (p0 + 256 * U <= pieces) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = in[p0 + u * 256 + threadIdx.x];
-#pragma unroll
-      for (int u = 0; u < U; ++u) out[p0 + u * 256 + threadIdx.x] = scaled(v[u]);
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const uint64_t p = p0 + u * 256 + threadIdx.x;
-        if (p < pieces) out[p] = scaled(in[p]);
-      }
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (decltype(f32)::value) x[i] = __float_as_uint(scaled(__uint_as_float(x[i])));
+      else x[i] = pack_bf16(scaled(bf16lo(x[i])), scaled(bf16hi(x[i])));
     }
-    const uint64_t at = pieces * (f32 ? 4 : 8) + threadIdx.x;
-    if (last && at < count) {
-      if (f32) static_cast<float*>(t.out[which])[at] = scaled1(static_cast<const float*>(t.in[which])[at]);
-      else static_cast<uint16_t*>(t.out[which])[at] = f32_to_bf16(scaled1(bf16_to_f32(static_cast<const uint16_t*>(t.in[which])[at])));
+    return x;
+  };
+  over_chunks(t, true, [&](auto f32, uint32_t e, uint32_t c, uint32_t n) __attribute__((always_inline)) {
+    if (same && t.in[e] == t.out[e]) return;
+    constexpr int CHUNK = GRAD_THREADS * U;
+    const u32x4_any* p = static_cast<const u32x4_any*>(t.in[e]) + (static_cast<size_t>(c) + n - 1) * CHUNK;
+    u32x4_any* o = static_cast<u32x4_any*>(t.out[e]) + (static_cast<size_t>(c) + n - 1) * CHUNK;
+    u32x4 v[U], w[U];
+    load_chunk<U>(p, v);
+    const auto put = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) o[u * GRAD_THREADS + threadIdx.x] = scaled4(f32, v[u]);
+    };
+    for (; n > 1; --n) {
+      p -= CHUNK;
+      load_chunk<U>(p, w);
+      put();
+      o -= CHUNK;
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = w[u];
+    }
+    put();
+  }, [&](auto f32, uint32_t e, uint32_t c, uint32_t count) __attribute__((always_inline)) {
+    if (same && t.in[e] == t.out[e]) return;
+    constexpr bool F32 = decltype(f32)::value;
+    constexpr uint32_t PER = F32 ? 4 : 8;
+    const u32x4_any* p = static_cast<const u32x4_any*>(t.in[e]) + static_cast<size_t>(c) * (GRAD_THREADS * U);
+    u32x4_any* o = static_cast<u32x4_any*>(t.out[e]) + static_cast<size_t>(c) * (GRAD_THREADS * U);
+    const uint32_t pieces = count / PER;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (u * GRAD_THREADS + threadIdx.x < pieces) o[u * GRAD_THREADS + threadIdx.x] = scaled4(f32, p[u * GRAD_THREADS + threadIdx.x]);
+    if (threadIdx.x < count % PER) {
+      const uint32_t at = pieces * PER + threadIdx.x;
+      if constexpr (F32) reinterpret_cast<float*>(o)[at] = scaled(reinterpret_cast<const float*>(p)[at]);
+      else reinterpret_cast<uint16_t*>(o)[at] = f32_to_bf16(scaled(bf16_to_f32(reinterpret_cast<const uint16_t*>(p)[at])));
     }
   });
 }
@@ -192,29 +244,56 @@ int overlap(const moe_grad* g, int n) {
 }
 // Pieces of 16 bytes that a thread takes of a chunk: four, or one where there would be too few chunks for all compute units.
 constexpr int WIDE = 4;
-constexpr long long FEW_PIECES = 2ll * GRAD_GROUPS * 256 * WIDE;
+constexpr long long FEW_PIECES = 1ll * GRAD_GROUPS * GRAD_THREADS * WIDE;
 
-// f(table, chunks) for the tensors, as many at a time as a table holds
-template <typename F> int over_tables(const moe_grad* g, int n, int u, F&& f) {
-  GradTable t;
-  t.n = 0;
-  unsigned long long chunks = 0;
-  for (int i = 0; i <= n; ++i) {
-    if (i == n || t.n == TENSORS) {
-      t.first[t.n] = static_cast<uint32_t>(chunks);
-      if (t.n > 0 && f(t, static_cast<long long>(chunks)) != MOE_OK) return MOE_ERR_LAUNCH;
-      t.n = 0;
-      chunks = 0;
+int tables_for(int n, int cap) { return (n + cap - 1) / cap; }
+int groups_for(unsigned long long chunks) { return chunks < GRAD_GROUPS ? static_cast<int>(chunks > 0 ? chunks : 1) : GRAD_GROUPS; }
+// f(table, chunks) for all tensors, CAP of them at a time or, if that takes several tables, as many in each
+template <int U, int CAP, bool CLIP, typename F> int over_tables(const moe_grad* g, int n, F&& f) {
+  const int tables = tables_for(n, CAP), each = (n + tables - 1) / tables;
+  GradTable<CAP, CLIP> t;
+  for (int at = 0; at < n; at += each) {
+    unsigned long long chunks = 0;
+    t.n = 0;
+    for (int i = at; i < n && i < at + each; ++i) {
+      if (g[i].count == 0) continue;
+      const unsigned long long count = g[i].count, chunk = static_cast<unsigned long long>(GRAD_THREADS) * U * (16 / bytes_of(g[i])), c = (count + chunk - 1) / chunk;
+      t.in[t.n] = g[i].in;
+      if constexpr (CLIP) t.out[t.n] = g[i].out;
+      t.last[t.n] = static_cast<uint32_t>(count - (c - 1) * chunk) << 1 | (g[i].type == MOE_TYPE_F32 ? 1 : 0);
+      t.first[t.n++] = static_cast<uint32_t>(chunks);
+      chunks += c;
     }
-    if (i == n || g[i].count == 0) continue;
-    const unsigned long long count = g[i].count, pieces = count / (16 / bytes_of(g[i])), c = (pieces + 256 * u - 1) / (256 * u);
-    t.in[t.n] = g[i].in;
-    t.out[t.n] = g[i].out;
-    t.count[t.n] = count << 1 | (g[i].type == MOE_TYPE_F32 ? 1 : 0);
-    t.first[t.n++] = static_cast<uint32_t>(chunks);
-    chunks += c > 0 ? c : 1;
+    t.first[t.n] = static_cast<uint32_t>(chunks);
+    const unsigned long long groups = groups_for(chunks);
+    t.each = static_cast<uint32_t>(chunks / groups);
+    t.more = static_cast<uint32_t>(chunks % groups);
+    if (f(t, static_cast<int>(groups)) != MOE_OK) return MOE_ERR_LAUNCH;
   }
   return MOE_OK;
+}
+struct GradCall {
+  const moe_grad* g;
+  int n;
+  double* sums;
+  double largest;
+  float* norm;
+  hipStream_t s;
+};
+template <int U, int CAP> int launch_norms(const GradCall& c, int& parts) {
+  return over_tables<U, CAP, false>(c.g, c.n, [&](const GradTable<CAP, false>& t, int groups) {
+    MOE_LAUNCH("grad_norm", (grad_norm_kernel<U, CAP>), dim3(groups), dim3(GRAD_THREADS), 0, c.s, t, c.sums + parts);
+    parts += groups;
+    return moe_check_launch();
+  });
+}
+template <int U, int CAP> int launch_clips(const GradCall& c, int parts) {
+  float* norm = c.norm;                              // the first launch writes it
+  return over_tables<U, CAP, true>(c.g, c.n, [&](const GradTable<CAP, true>& t, int groups) {
+    MOE_LAUNCH("grad_clip", (grad_clip_kernel<U, CAP>), dim3(groups), dim3(GRAD_THREADS), 0, c.s, t, c.sums, parts, c.largest, norm);
+    norm = nullptr;
+    return moe_check_launch();
+  });
 }
 int run_grads(const moe_grad* g, int n, bool clip, double largest, float* norm, void* ws, size_t ws_bytes, hipStream_t s) {
   if (bad_grads(g, n, clip) || norm == nullptr || !moe_aligned16(norm) || ws == nullptr || !moe_aligned16(ws)) return MOE_ERR_INVALID;
@@ -223,30 +302,16 @@ int run_grads(const moe_grad* g, int n, bool clip, double largest, float* norm, 
   for (int i = 0; i < n; ++i) pieces += static_cast<unsigned long long>(g[i].count) / (16 / bytes_of(g[i])) + 1;
   if (pieces > 1ull << 40) return MOE_ERR_INVALID;   // chunks are counted in 32 bits
   if (clip && overlap(g, n) != MOE_OK) return MOE_ERR_INVALID;
-  const bool wide = pieces >= FEW_PIECES;
-  double* const sums = static_cast<double*>(ws);
+  const bool wide = pieces >= FEW_PIECES, few = n <= FEW_TENSORS;
+  const GradCall c{g, n, static_cast<double*>(ws), largest, norm, s};
   int parts = 0;
-  auto groups = [](long long chunks) { return static_cast<int>(chunks < GRAD_GROUPS ? chunks : GRAD_GROUPS); };
-  int rc = over_tables(g, n, wide ? WIDE : 1, [&](const GradTable& t, long long chunks) {
-    const dim3 grid(groups(chunks));
-    if (wide) MOE_LAUNCH("grad_norm", grad_norm_kernel<WIDE>, grid, dim3(256), 0, s, t, sums + parts);
-    else MOE_LAUNCH("grad_norm", grad_norm_kernel<1>, grid, dim3(256), 0, s, t, sums + parts);
-    parts += grid.x;
-    return moe_check_launch();
-  });
+  int rc = wide ? (few ? launch_norms<WIDE, FEW_TENSORS>(c, parts) : launch_norms<WIDE, NORM_TENSORS>(c, parts))
+                : (few ? launch_norms<1, FEW_TENSORS>(c, parts) : launch_norms<1, NORM_TENSORS>(c, parts));
   if (rc != MOE_OK) return rc;
-  float* left = norm;                                // the first launch that knows the norm writes it
-  if (clip) {
-    rc = over_tables(g, n, wide ? WIDE : 1, [&](const GradTable& t, long long chunks) {
-      const dim3 grid(groups(chunks));
-      if (wide) MOE_LAUNCH("grad_clip", grad_clip_kernel<WIDE>, grid, dim3(256), 0, s, t, sums, parts, largest, left);
-      else MOE_LAUNCH("grad_clip", grad_clip_kernel<1>, grid, dim3(256), 0, s, t, sums, parts, largest, left);
-      left = nullptr;
-      return moe_check_launch();
-    });
-  }
-  if (rc != MOE_OK || left == nullptr) return rc;
-  MOE_LAUNCH("grad_norm_finish", grad_norm_finish_kernel, dim3(1), dim3(256), 0, s, sums, parts, norm);
+  if (clip)
+    return wide ? (few ? launch_clips<WIDE, FEW_TENSORS>(c, parts) : launch_clips<WIDE, CLIP_TENSORS>(c, parts))
+                : (few ? launch_clips<1, FEW_TENSORS>(c, parts) : launch_clips<1, CLIP_TENSORS>(c, parts));
+  MOE_LAUNCH("grad_norm_finish", grad_norm_finish_kernel, dim3(1), dim3(GRAD_THREADS), 0, s, c.sums, parts, norm);
   return moe_check_launch();
 }
 
@@ -254,7 +319,7 @@ int run_grads(const moe_grad* g, int n, bool clip, double largest, float* norm, 
 
 extern "C" size_t moe_grad_norm_workspace_bytes(int n) {
   if (n <= 0 || n > MAX_TENSORS) return 0;
-  return static_cast<size_t>((n + TENSORS - 1) / TENSORS) * GRAD_GROUPS * sizeof(double);
+  return static_cast<size_t>(tables_for(n, n <= FEW_TENSORS ? FEW_TENSORS : NORM_TENSORS)) * GRAD_GROUPS * sizeof(double);
 }
 
 extern "C" int moe_grad_norm(const moe_grad* grads, int n, float* norm, void* ws, size_t ws_bytes, void* stream) {

@@ -13,48 +13,63 @@
 
 namespace {
 
-constexpr int SCORE_THREADS = 256, SCORE_CANDIDATES = 512;
+constexpr int SCORE_CANDIDATES = 512, SCORE_FEW = 256;
 
 __device__ __forceinline__ float from_ordered(uint32_t k) { return __uint_as_float(k ^ ((k >> 31) != 0 ? 0x80000000u : 0xFFFFFFFFu)); }
 // Sums of 2^t and t 2^t relative to 2^e, e a whole number.
 struct ScoreSum {
   float e = -3.0e38f, sum = 0.f, moment = 0.f;
-  __device__ __forceinline__ void add(float E, float s, float m) {
-    const float n = fmaxf(e, E), f = __builtin_amdgcn_exp2f(e - n), g = __builtin_amdgcn_exp2f(E - n);
-    moment = f * __builtin_fmaf(sum, e - n, moment) + g * __builtin_fmaf(s, E - n, m);
-    sum = f * sum + g * s;
+  __device__ __forceinline__ void raise(float n) {                        // n >= e
+    const float f = __builtin_amdgcn_exp2f(e - n);
+    moment = f * __builtin_fmaf(sum, e - n, moment);
+    sum *= f;
     e = n;
   }
-  __device__ __forceinline__ void add_logit(float z, float c1) {
-    const float E = ceilf(z * c1), t = __builtin_fmaf(z, c1, -E), s = __builtin_amdgcn_exp2f(t);
-    add(E, s, s * t);
+  __device__ __forceinline__ void add(float E, float s, float m) {        // E <= e
+    const float g = __builtin_amdgcn_exp2f(E - e);
+    sum = __builtin_fmaf(g, s, sum);
+    moment = __builtin_fmaf(g, __builtin_fmaf(s, E - e, m), moment);
+  }
+  __device__ __forceinline__ void add_logit(float z, float c1) {          // z c1 <= e
+    const float t = __builtin_fmaf(z, c1, -e), s = __builtin_amdgcn_exp2f(t);
+    sum += s;
+    moment = __builtin_fmaf(s, t, moment);
   }
 };
 
-// Logits of up to four columns in 64 bits, by a wave.
-__device__ __forceinline__ void exact_logits(const moe_bf16* x, const moe_bf16* W, int d, const int (&col)[4], double (&z)[4]) {
+// Logits of N columns in 64 bits, by a wave; AHEAD pieces of each row requested together.
+template <int N, int AHEAD> __device__ __forceinline__ void exact_logits(const moe_bf16* x, const moe_bf16* W, int d, const int (&col)[N], double (&z)[N]) {
   typedef __attribute__((ext_vector_type(4))) uint32_t u4;
+  constexpr int STEP = MOE_WAVE * 8;
   const int lane = threadIdx.x % MOE_WAVE;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) z[k] = 0.0;
-#pragma unroll 2
-  for (int c = lane * 8; c < d; c += MOE_WAVE * 8) {
-    u4 w[4];
-    const u4 p = *reinterpret_cast<const u4*>(x + c);
+  for (int k = 0; k < N; ++k) z[k] = 0.0;
+  for (int c0 = lane * 8; c0 < d; c0 += AHEAD * STEP) {
+    u4 p[AHEAD], w[AHEAD][N];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const u4*>(W + static_cast<size_t>(col[k]) * d + c);
+    for (int u = 0; u < AHEAD; ++u) {
+      const int c = c0 + u * STEP < d ? c0 + u * STEP : c0;
+      p[u] = *reinterpret_cast<const u4*>(x + c);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float lo = bf16lo(p[i]), hi = bf16hi(p[i]);
+      for (int k = 0; k < N; ++k) w[u][k] = *reinterpret_cast<const u4*>(W + static_cast<size_t>(col[k]) * d + c);
+    }
+    asm volatile("" ::: "memory");
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        z[k] += static_cast<double>(lo * bf16lo(w[k][i]));
-        z[k] += static_cast<double>(hi * bf16hi(w[k][i]));
+    for (int u = 0; u < AHEAD; ++u) {
+      if (c0 + u * STEP >= d) break;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const double lo = bf16lo(p[u][i]), hi = bf16hi(p[u][i]);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          z[k] = __builtin_fma(lo, static_cast<double>(bf16lo(w[u][k][i])), z[k]);
+          z[k] = __builtin_fma(hi, static_cast<double>(bf16hi(w[u][k][i])), z[k]);
+        }
       }
     }
   }
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
+  for (int k = 0; k < N; ++k)
 #pragma unroll
     for (int i = 1; i < MOE_WAVE; i *= 2) z[k] += __shfl_xor(z[k], i);
 }
@@ -63,25 +78,48 @@ __device__ __forceinline__ int64_t ordered_i64(double v) {
   return b >= 0 ? b : b ^ 0x7FFFFFFFFFFFFFFFll;
 }
 
-// A workgroup for each token.  HALF: columns of a strip.
-template <int HALF>
-__global__ __launch_bounds__(SCORE_THREADS) void head_score_join_kernel(ScoreJoinArgs a) {
+// Maximum over groups of G threads (a power of two up to a wave), in all of them.
+template <int G> __device__ __forceinline__ uint64_t group_most(uint64_t v) {
+#pragma unroll
+  for (int i = 1; i < G; i *= 2) {
+    const uint64_t o = __shfl_xor(v, i);
+    v = o > v ? o : v;
+  }
+  return v;
+}
+
+// put(i, number of k with above(k, i)) for i and k below n, sixteen threads to an i.
+template <int THREADS, typename Above, typename Put> __device__ __forceinline__ void ranked(int n, Above&& above, Put&& put) {
+  const int l16 = threadIdx.x % 16;
+  for (int i = threadIdx.x / 16; i - static_cast<int>(threadIdx.x / 16) < n; i += THREADS / 16) {
+    uint32_t count = 0;
+    if (i < n) for (int k = l16; k < n; k += 16) count += above(k, i) ? 1 : 0;
+    count = group_reduce<16>(count, [](uint32_t u, uint32_t v) __attribute__((always_inline)) { return u + v; });
+    if (i < n && l16 == 0) put(i, static_cast<int>(count));
+  }
+}
+
+// A workgroup of THREADS for each token.  HALF: columns of a strip; LIST: with alternatives.
+template <int HALF, int THREADS, bool LIST>
+__global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs a) {
+  constexpr int GROUPS = 256, WAVES = THREADS / MOE_WAVE, AT_ONCE = THREADS > 256 ? 4 : 8, STEP = THREADS / 4;
   extern __shared__ double exact[];
-  __shared__ uint64_t keys[SCORE_THREADS], found[SCORE_CANDIDATES], chosen[score_wanted(SCORE_MAX_K)], s_top, s_least;
-  __shared__ uint32_t found_next[SCORE_CANDIDATES], chosen_next[score_wanted(SCORE_MAX_K)];
-  __shared__ float part[4][3];
-  __shared__ int s_found, s_columns;
+  __shared__ uint64_t keys[LIST ? GROUPS : WAVES], found[LIST ? SCORE_CANDIDATES : 1], chosen[score_wanted(LIST ? SCORE_MAX_K : 0)], s_top, s_least;
+  __shared__ uint32_t found_next[LIST ? SCORE_CANDIDATES : 1], chosen_next[score_wanted(LIST ? SCORE_MAX_K : 0)];
+  __shared__ float part[WAVES][3];
+  __shared__ int s_found, s_columns, s_top_at;
   constexpr uint32_t LOW = HALF / 4 - 1;
   constexpr uint32_t NONE = 0xFF800000u, LEAST = 0x00800000u;             // -infinity; the order of the lowest number
-  const int tid = threadIdx.x, lane = tid % MOE_WAVE, wave = tid / MOE_WAVE, lq = tid & 3, t = blockIdx.x, K = a.K, wanted = score_wanted(K);
+  const int tid = threadIdx.x, lane = tid % MOE_WAVE, wave = tid / MOE_WAVE, lq = tid & 3, K = LIST ? a.K : 0, wanted = score_wanted(K);
+  const int t = blockIdx.x;
   const int y = a.target[t];
   if (y < 0 || y >= a.V) {
     if (tid == 0) { a.logp[t] = 0.f; a.entropy[t] = 0.f; a.lse[t] = 0.f; }
-    for (int k = tid; k < K; k += SCORE_THREADS) { a.ids[static_cast<size_t>(t) * K + k] = -1; a.top[static_cast<size_t>(t) * K + k] = 0.f; }
+    for (int k = tid; k < K; k += THREADS) { a.ids[static_cast<size_t>(t) * K + k] = -1; a.top[static_cast<size_t>(t) * K + k] = 0.f; }
     return;
   }
   const int row = a.control != nullptr ? a.token_row[t] : t;
-  const HeadStrip* const strip = a.part + static_cast<size_t>(row >> 4) * a.strips * 16 + (row & 15);
+  const HeadStrip* const strip = a.part + static_cast<size_t>(row) * a.strips;
   const float c1 = a.c1;
   int32_t* const columns = reinterpret_cast<int32_t*>(exact + wanted * (HALF / 4) + 1);
 
@@ -90,60 +128,114 @@ __global__ __launch_bounds__(SCORE_THREADS) void head_score_join_kernel(ScoreJoi
     const int place = static_cast<int>(x.next & LOW), col = s * HALF + 16 * (place >> 2) + 4 * lq + (place & 3);
     return __float_as_uint(x.top) == NONE ? 0 : static_cast<uint64_t>(ordered_u32(__float_as_uint(x.top))) << 32 | ~static_cast<uint32_t>(col);
   };
+  const auto load = [&](int s0, HeadTop (&x)[AT_ONCE]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int s = s0 + i * STEP;
+      x[i] = HeadTop{-__builtin_inff(), 0};
+      if (s < a.strips) x[i] = strip[s].lane[lq];
+    }
+  };
+  // All logits but a thread's largest are summed up at once; the largest of all is left out.  (A sum's NaN reaches all that is made of it.)
+  constexpr bool KEEP = LIST && THREADS > 256;
+  HeadTop kept[KEEP ? AT_ONCE : 1];                                       // of the first round
   uint64_t best = 0;
   ScoreSum total;
-#pragma unroll 4
-  for (int s = tid >> 2; s < a.strips; s += SCORE_THREADS / 4) {
-    const HeadTop x = strip[static_cast<size_t>(s) * 16].lane[lq];
-    float sum = 0.f, moment = 0.f;
-    if (lq == 0) { sum = strip[static_cast<size_t>(s) * 16].sum; moment = strip[static_cast<size_t>(s) * 16].moment; }
-    float whole = x.top;
-    whole = __builtin_elementwise_maximum(whole, __uint_as_float(dpp_u32<0xB1>(__float_as_uint(whole))));
-    whole = __builtin_elementwise_maximum(whole, __uint_as_float(dpp_u32<0x4E>(__float_as_uint(whole))));
-    if (lq == 0 && !(__float_as_uint(whole) == NONE)) total.add(whole == whole ? ceilf(whole * c1) : whole, sum, moment);
-    const uint64_t key = key_of(x, s), less = key < best ? key : best;
-    best = key < best ? best : key;
-    if (less != 0) total.add_logit(from_ordered(static_cast<uint32_t>(less >> 32)), c1);
+  for (int s0 = tid >> 2; s0 < a.strips; s0 += AT_ONCE * STEP) {
+    HeadTop x[AT_ONCE];
+    float sum[AT_ONCE], moment[AT_ONCE], E[AT_ONCE], most = total.e;
+    load(s0, x);
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      sum[i] = moment[i] = 0.f;
+      if (lq == 0 && s0 + i * STEP < a.strips) {
+        const HeadStrip* const at = strip + s0 + i * STEP;
+        sum[i] = at->sum;
+        moment[i] = at->moment;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      if constexpr (KEEP) { if (s0 == tid >> 2) kept[i] = x[i]; }
+      float whole = x[i].top;
+      whole = __builtin_elementwise_maximum(whole, __uint_as_float(dpp_u32<0xB1>(__float_as_uint(whole))));
+      whole = __builtin_elementwise_maximum(whole, __uint_as_float(dpp_u32<0x4E>(__float_as_uint(whole))));
+      E[i] = __float_as_uint(whole) == NONE ? total.e : ceilf(whole * c1);
+      most = fmaxf(most, E[i]);
+    }
+    total.raise(fmaxf(most, -3.0e38f));
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      total.add(__float_as_uint(x[i].top) == NONE && sum[i] == 0.f ? total.e : E[i], sum[i], moment[i]);
+      const uint64_t key = key_of(x[i], s0 + i * STEP), less = key < best ? key : best;
+      best = key < best ? best : key;
+      if (less != 0) total.add_logit(from_ordered(static_cast<uint32_t>(less >> 32)), c1);
+    }
   }
-  keys[tid] = best;
-  if (tid == 0) { s_top = s_least = 0; s_found = s_columns = 0; }
-  __syncthreads();
-  int rank = 0;
-#pragma unroll 8
-  for (int i = 0; i < SCORE_THREADS; ++i) rank += keys[i] > best;
-  if (rank == 0 && best != 0) s_top = best;
-  if (rank == wanted - 1 && best != 0) s_least = best;
-  if (rank != 0 && best != 0) total.add_logit(from_ordered(static_cast<uint32_t>(best >> 32)), c1);
+  if (tid == 0) { s_top = s_least = 0; s_found = s_columns = 0; s_top_at = 0; }
+  if constexpr (!LIST) {
+    const uint64_t most = group_most<MOE_WAVE>(best);
+    if (lane == 0) keys[wave] = most;
+    __syncthreads();
+    uint64_t whole = keys[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) whole = keys[w] > whole ? keys[w] : whole;
+    if (tid == 0) s_top = whole;
+    if (best != whole && best != 0) total.add_logit(from_ordered(static_cast<uint32_t>(best >> 32)), c1);
+  } else {
+    // The largest of every few threads, and of these the one that `wanted` - 1 are above: no smaller logit is among the `wanted` largest.
+    const bool coarse = wanted <= 32;                                     // 64 groups are enough
+    constexpr int FINE = THREADS / GROUPS;
+    uint64_t mine = group_most<FINE>(best);
+    if (coarse) mine = group_most<FINE * 4>(mine);
+    const int size = coarse ? FINE * 4 : FINE, groups = THREADS / size;
+    if (tid % size == 0) keys[tid / size] = mine;
+    __syncthreads();
+    ranked<THREADS>(groups, [&](int k, int i) __attribute__((always_inline)) { return keys[k] > keys[i]; }, [&](int i, int above) __attribute__((always_inline)) {
+      if (above == 0 && keys[i] != 0) s_top = keys[i];
+      if (above == wanted - 1 && keys[i] != 0) s_least = keys[i];
+    });
+    __syncthreads();
+    if (best != s_top && best != 0) total.add_logit(from_ordered(static_cast<uint32_t>(best >> 32)), c1);
+  }
   {
-    const float e = group_max<MOE_WAVE>(total.e), f = __builtin_amdgcn_exp2f(total.e - e);
-    const float moment = group_sum<MOE_WAVE>(f * __builtin_fmaf(total.sum, total.e - e, total.moment)), sum = group_sum<MOE_WAVE>(f * total.sum);
+    const float e = group_max<MOE_WAVE>(total.e);
+    total.raise(e);
+    const float moment = group_sum<MOE_WAVE>(total.moment), sum = group_sum<MOE_WAVE>(total.sum);
     if (lane == 0) { part[wave][0] = e; part[wave][1] = sum; part[wave][2] = moment; }
   }
   __syncthreads();
-  ScoreSum all;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) all.add(part[w][0], part[w][1], part[w][2]);
   const uint64_t top_key = s_top, least = s_least;
-  int n = top_key != 0 ? 1 : 0;                                           // lanes of the product whose columns are looked at
-  if (K == 0) {
-    if (tid == 0) { chosen[0] = top_key; chosen_next[0] = 0; }
+  const int top_col = static_cast<int>(~static_cast<uint32_t>(top_key));
+  int m = top_key != 0 ? 1 : 0;                                           // columns whose logits are formed anew, beside the target
+  if constexpr (!LIST) {
+    if (tid == 0) { columns[0] = m != 0 ? top_col : y; columns[1] = y; }
+    __syncthreads();
+    if (m == 0) m = 1;
   } else {
-    for (int s = tid >> 2; s < a.strips; s += SCORE_THREADS / 4) {
-      const HeadTop x = strip[static_cast<size_t>(s) * 16].lane[lq];
+    int n;                                                                // lanes of the product whose columns are looked at
+    const auto look = [&](const HeadTop& x, int s) __attribute__((always_inline)) {
       const uint64_t key = key_of(x, s);
-      if (key == 0 || key < least) continue;
+      if (key == 0 || key < least) return;
       const int at = atomicAdd(&s_found, 1);
       if (at < SCORE_CANDIDATES) { found[at] = key; found_next[at] = x.next | LOW; }
+    };
+    if constexpr (KEEP) {
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) if ((tid >> 2) + i * STEP < a.strips) look(kept[i], (tid >> 2) + i * STEP);
+    }
+    for (int s0 = (tid >> 2) + (KEEP ? AT_ONCE * STEP : 0); s0 < a.strips; s0 += AT_ONCE * STEP) {
+      HeadTop x[AT_ONCE];
+      load(s0, x);
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) look(x[i], s0 + i * STEP);
     }
     __syncthreads();
     n = s_found;
     if (n <= SCORE_CANDIDATES) {
-      for (int i = tid; i < n; i += SCORE_THREADS) {
-        const uint64_t mine = found[i];
-        int above = 0;
-        for (int k = 0; k < n; ++k) above += found[k] > mine;
-        if (above < wanted) { chosen[above] = mine; chosen_next[above] = found_next[i]; }
-      }
+      ranked<THREADS>(n, [&](int k, int i) __attribute__((always_inline)) { return found[k] > found[i]; }, [&](int i, int above) __attribute__((always_inline)) {
+        if (above < wanted) { chosen[above] = found[i]; chosen_next[above] = found_next[i]; }
+      });
       n = n < wanted ? n : wanted;
     } else {
       // (large logits in few threads' strips: one after the other)
@@ -151,50 +243,60 @@ __global__ __launch_bounds__(SCORE_THREADS) void head_score_join_kernel(ScoreJoi
       for (uint64_t last = ~0ull; n < wanted; ++n) {
         uint64_t most = 0;
         uint32_t next = 0;
-        for (int s = tid >> 2; s < a.strips; s += SCORE_THREADS / 4) {
-          const HeadTop x = strip[static_cast<size_t>(s) * 16].lane[lq];
+        for (int s = tid >> 2; s < a.strips; s += STEP) {
+          const HeadTop x = strip[s].lane[lq];
           const uint64_t key = key_of(x, s);
           if (key < last && key > most) { most = key; next = x.next | LOW; }
         }
+        const uint64_t of_wave = group_most<MOE_WAVE>(most);
         __syncthreads();
-        keys[tid] = most;
+        if (lane == 0) keys[wave] = of_wave;
         __syncthreads();
         uint64_t whole = 0;
-        for (int i = 0; i < SCORE_THREADS; ++i) whole = keys[i] > whole ? keys[i] : whole;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) whole = keys[w] > whole ? keys[w] : whole;
         if (whole == 0) break;
         if (most == whole) { chosen[n] = most; chosen_next[n] = next; }
         last = whole;
       }
     }
+    __syncthreads();
+    // the columns to look at: those, and all of a lane whose second largest may be among the `wanted` largest
+    const uint32_t border = n == wanted ? static_cast<uint32_t>(chosen[n - 1] >> 32) : 0;
+    for (int i = tid; i < n * (HALF / 4); i += THREADS) {
+      const int which = i / (HALF / 4), place = i % (HALF / 4), own = static_cast<int>(~static_cast<uint32_t>(chosen[which]));
+      const int col = own / HALF * HALF + 16 * (place >> 2) + (own & 12) + (place & 3);
+      const uint32_t next = chosen_next[which];
+      if (col == own || (next >= LEAST && next >= border && col < a.V)) {
+        const int at = atomicAdd(&s_columns, 1);
+        columns[at] = col;
+        if (col == top_col) s_top_at = at;
+      }
+    }
+    __syncthreads();
+    m = s_columns;
+    if (tid == 0) columns[m] = y;
+    __syncthreads();
   }
-  __syncthreads();
-  // the columns to look at: those, and all of a lane whose second largest may be among the `wanted` largest
-  const uint32_t border = n == wanted ? static_cast<uint32_t>(chosen[n - 1] >> 32) : 0;
-  for (int i = tid; i < n * (HALF / 4); i += SCORE_THREADS) {
-    const int which = i / (HALF / 4), place = i % (HALF / 4), own = static_cast<int>(~static_cast<uint32_t>(chosen[which]));
-    const int col = own / HALF * HALF + 16 * (place >> 2) + (own & 12) + (place & 3);
-    const uint32_t next = chosen_next[which];
-    if (col == own || (K > 0 && next >= LEAST && next >= border && col < a.V)) columns[atomicAdd(&s_columns, 1)] = col;
-  }
-  __syncthreads();
-  const int m = s_columns;
-  if (tid == 0) columns[m] = y;
-  __syncthreads();
-  for (int i = wave * 4; i <= m; i += 16) {
-    int col[4];
-    double z[4];
+  constexpr int N = !LIST || THREADS > 256 ? 2 : 4, AHEAD = N == 2 ? 4 : 2;
+  for (int i = wave * N; i <= m; i += WAVES * N) {
+    int col[N];
+    double z[N];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) col[k] = __builtin_amdgcn_readfirstlane(columns[i + k <= m ? i + k : m]);
-    exact_logits(a.x + static_cast<size_t>(t) * a.d, a.W, a.d, col, z);
+    for (int k = 0; k < N; ++k) col[k] = __builtin_amdgcn_readfirstlane(columns[i + k <= m ? i + k : m]);
+    exact_logits<N, AHEAD>(a.x + static_cast<size_t>(t) * a.d, a.W, a.d, col, z);
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int k = 0; k < N; ++k)
       if (lane == 0 && i + k <= m) exact[i + k] = z[k];
   }
   __syncthreads();
+  ScoreSum all;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) all.e = fmaxf(all.e, part[w][0]);
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) all.add(part[w][0], part[w][1], part[w][2]);
   // the largest logit by the product is what the sums leave out: the formulas hold whether it is the largest in 64 bits or next to it
-  const int top_col = static_cast<int>(~static_cast<uint32_t>(top_key));
-  double z_top = 0.0;
-  for (int i = 0; i < m; ++i) z_top = columns[i] == top_col ? exact[i] : z_top;
+  const double z_top = exact[s_top_at];
   const double from = static_cast<double>(all.e) - z_top * static_cast<double>(c1);
   // (NaN where a logit is no number or infinite, and where a scale of 2^30 or more leaves its exponent without digits)
   const bool alone = all.e == -3.0e38f;                                    // no other column
@@ -209,30 +311,35 @@ __global__ __launch_bounds__(SCORE_THREADS) void head_score_join_kernel(ScoreJoi
     a.entropy[t] = static_cast<float>(log_1R) + Q / (1.f + R);
     a.lse[t] = static_cast<float>(z_top * a.over_tau + log_1R);
   }
-  if (K == 0) return;
-  for (int k = m + tid; k < K; k += SCORE_THREADS) {                       // (logits of -infinity)
+  if constexpr (!LIST) return;
+  for (int k = m + tid; k < K; k += THREADS) {                       // (logits of -infinity)
     a.ids[static_cast<size_t>(t) * K + k] = -1;
     a.top[static_cast<size_t>(t) * K + k] = __builtin_nanf("");
   }
-  for (int i = tid; i < m; i += SCORE_THREADS) {
-    const int64_t mine = ordered_i64(exact[i]);
-    const int col = columns[i];
-    int above = 0;
-    for (int k = 0; k < m; ++k) {
-      const int64_t other = ordered_i64(exact[k]);
-      above += other > mine || (other == mine && columns[k] < col);
-    }
-    if (above >= K) continue;
-    a.ids[static_cast<size_t>(t) * K + above] = col;
-    a.top[static_cast<size_t>(t) * K + above] = col == top_col ? -static_cast<float>(log_1R) : static_cast<float>((exact[i] - z_top) * a.over_tau - log_1R);
-  }
+  ranked<THREADS>(m, [&](int k, int i) __attribute__((always_inline)) {
+    const int64_t one = ordered_i64(exact[k]), two = ordered_i64(exact[i]);
+    return one > two || (one == two && columns[k] < columns[i]);
+  }, [&](int i, int above) __attribute__((always_inline)) {
+    if (above >= K) return;
+    a.ids[static_cast<size_t>(t) * K + above] = columns[i];
+    a.top[static_cast<size_t>(t) * K + above] = columns[i] == top_col ? -static_cast<float>(log_1R) : static_cast<float>((exact[i] - z_top) * a.over_tau - log_1R);
+  });
+}
+
+template <int HALF, int THREADS, bool LIST> void launch_join(const ScoreJoinArgs& a, hipStream_t s) {
+  const int lds = LIST ? (score_wanted(a.K) * (HALF / 4) + 1) * 12 : (HALF / 4 + 2) * 12;
+  MOE_LAUNCH("head_score_join", (head_score_join_kernel<HALF, THREADS, LIST>), dim3(a.T), dim3(THREADS), lds, s, a);
+}
+template <int HALF> void launch_join_of(const ScoreJoinArgs& a, hipStream_t s) {
+  if (a.K == 0) launch_join<HALF, 256, false>(a, s);
+  else if (a.T <= SCORE_FEW) launch_join<HALF, 1024, true>(a, s);
+  else launch_join<HALF, 256, true>(a, s);
 }
 
 }  // namespace
 
 int moe_head_score_join(const ScoreJoinArgs& a, int edge, hipStream_t s) {
-  const int lds = (score_wanted(a.K) * (edge / 8) + 1) * 12;
-  if (edge == 128) MOE_LAUNCH("head_score_join", head_score_join_kernel<64>, dim3(a.T), dim3(SCORE_THREADS), lds, s, a);
-  else MOE_LAUNCH("head_score_join", head_score_join_kernel<128>, dim3(a.T), dim3(SCORE_THREADS), lds, s, a);
+  if (edge == 128) launch_join_of<64>(a, s);
+  else launch_join_of<128>(a, s);
   return moe_check_launch();
 }
