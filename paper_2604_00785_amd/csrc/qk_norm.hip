@@ -4,6 +4,7 @@
 // Bound by memory: every element is read once and written once.  A thread has 16 columns of a head, both of every pair among them, so that nothing passes between
 // threads but a row's sums; a few threads share a head, and a workgroup's threads take the heads of one or a few tokens, whose angles are formed once, in 64 bits
 // (a position of 10^6 times a frequency in 32 bits is off by 0.06), and kept in LDS.
+#include <initializer_list>
 #include <type_traits>
 #include "common.h"
 
@@ -11,7 +12,7 @@ namespace {
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
-constexpr int QK_MAX_D = 512, QK_THREADS = 256, QK_AHEAD = 4;
+constexpr int QK_MAX_D = 512, QK_THREADS = 256;
 
 struct QkSide {
   const moe_bf16 *x, *dy;              // dy: of the backward pass
@@ -39,6 +40,7 @@ __device__ __forceinline__ void unpack16(const u32x4& a, const u32x4& b, float (
 __device__ __forceinline__ u32x4 pack_half(const float (&v)[16], int at) {
   return u32x4{pack_bf16(v[at], v[at + 1]), pack_bf16(v[at + 2], v[at + 3]), pack_bf16(v[at + 4], v[at + 5]), pack_bf16(v[at + 6], v[at + 7])};
 }
+__device__ __forceinline__ u32x4 load8(const moe_bf16* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
 // Where a thread's two pieces of 8 columns begin.  Rotated pieces first: as halves i and i + R / 16, as neighbours 2 i and 2 i + 1; then the others, two and two.
 struct Place { int a, b; bool turned, has_a, has_b; };
 __device__ __forceinline__ Place place_of(int i, int D, int R, bool pairs) {
@@ -46,35 +48,28 @@ __device__ __forceinline__ Place place_of(int i, int D, int R, bool pairs) {
   const int a = turned && !pairs ? i : 2 * i, b = turned && !pairs ? i + R / 16 : 2 * i + 1;
   return {8 * a, 8 * b, turned, 8 * a < D, 8 * b < D};
 }
-// The thread's pairs turned by its angles (sin negative: back).  Neighbours: pair j is (2 j, 2 j + 1) of the 16; halves: (j, j + 8).
-__device__ __forceinline__ void turn(float (&v)[16], const float (&c)[8], const float (&s)[8], bool pairs, float sign) {
-  if (pairs) {
+// The thread's pairs turned by its angles (sign -1: back).  Neighbours: pair j is (2 j, 2 j + 1) of the 16; halves: (j, j + 8).
+template <bool PAIRS> __device__ __forceinline__ void turn(float (&v)[16], const float (&c)[8], const float (&s)[8], float sign) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float a = v[2 * j], b = v[2 * j + 1], sn = sign * s[j];
-      v[2 * j] = __builtin_fmaf(a, c[j], -(b * sn));
-      v[2 * j + 1] = __builtin_fmaf(a, sn, b * c[j]);
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float a = v[j], b = v[j + 8], sn = sign * s[j];
-      v[j] = __builtin_fmaf(a, c[j], -(b * sn));
-      v[j + 8] = __builtin_fmaf(a, sn, b * c[j]);
-    }
+  for (int j = 0; j < 8; ++j) {
+    constexpr int NEXT = PAIRS ? 1 : 8;
+    const int at = PAIRS ? 2 * j : j;
+    const float a = v[at], b = v[at + NEXT], sn = sign * s[j];
+    v[at] = __builtin_fmaf(a, c[j], -(b * sn));
+    v[at + NEXT] = __builtin_fmaf(a, sn, b * c[j]);
   }
 }
 
 // TPR threads to a head, N tokens to a workgroup at a time.
-template <int TPR, int N, bool BWD>
+template <int TPR, int N, bool PAIRS, bool BWD>
 __global__ __launch_bounds__(QK_THREADS) void qk_norm_kernel(QkArgs a) {
   constexpr int GROUPS = QK_THREADS / TPR, EACH = GROUPS / N;           // groups of threads, those of a token
+  constexpr int AHEAD = BWD ? 2 : 4;                                    // heads requested together
   static_assert(EACH >= 1, "a group for each token");
   __shared__ float angle[2][N][QK_MAX_D / 2];
   __shared__ float share[BWD ? GROUPS * TPR * 17 : 1];
   const int tid = threadIdx.x, i = tid % TPR, group = tid / TPR, slot = group / EACH, mine = group % EACH;
-  const bool pairs = a.pairs != 0;
-  const Place at = place_of(i, a.D, a.R, pairs);
+  const Place at = place_of(i, a.D, a.R, PAIRS);
   const float over_D = 1.f / static_cast<float>(a.D);
   float dw[2][16];
   if constexpr (BWD) {
@@ -83,26 +78,26 @@ __global__ __launch_bounds__(QK_THREADS) void qk_norm_kernel(QkArgs a) {
   }
   const int blocks = (a.T + N - 1) / N;
   for (int block = blockIdx.x; block < blocks; block += gridDim.x) {
-    const int half = a.R / 2;
+    const int half = a.R / 2, t = block * N + slot;
     if (BWD) __syncthreads();                                            // the angles of the tokens before have been read
     for (int j = tid; j < N * half; j += QK_THREADS) {
-      const int n = j / half, f = j - n * half, t = block * N + n;
+      const int n = j / half, f = j - n * half, token = block * N + n;
       float s = 0.f, c = 1.f;
-      if (t < a.T) {
-        const double turns = static_cast<double>(a.pos[t]) * static_cast<double>(a.freq[f]) * 0.15915494309189533577;
+      if (token < a.T) {
+        const double turns = static_cast<double>(a.pos[token]) * static_cast<double>(a.freq[f]) * 0.15915494309189533577;
         sincospif(static_cast<float>(2.0 * (turns - floor(turns))), &s, &c);
       }
       angle[0][n][f] = c;
       angle[1][n][f] = s;
     }
     __syncthreads();
-    const int t = block * N + slot;
     float c[8], s[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       c[j] = at.turned ? angle[0][slot][8 * i + j] : 1.f;
       s[j] = at.turned ? angle[1][slot][8 * i + j] : 0.f;
     }
+    // (Addresses are a base of the workgroup's tokens and 32 bits of a thread's own: qk_tokens() sees to it that these suffice.)
     auto side = [&](const QkSide& x, auto which) __attribute__((always_inline)) {
       constexpr int W = decltype(which)::value;
       float w[16];
@@ -118,29 +113,31 @@ __global__ __launch_bounds__(QK_THREADS) void qk_norm_kernel(QkArgs a) {
           for (int l = 0; l < 4; ++l) w[8 * h + j + l] = v[l];
         }
       }
-      const moe_bf16* const xr = x.x + t * x.x_ld;
-      const moe_bf16* const gr = BWD ? x.dy + t * x.dy_ld : nullptr;
-      moe_bf16* const yr = x.out + t * x.out_ld;
-      for (int h0 = mine; h0 < x.H; h0 += QK_AHEAD * EACH) {
-        u32x4 xa[QK_AHEAD], xb[QK_AHEAD], ga[QK_AHEAD], gb[QK_AHEAD];
+      const moe_bf16* const xs = x.x + static_cast<long long>(block) * N * x.x_ld;
+      const moe_bf16* const gs = BWD ? x.dy + static_cast<long long>(block) * N * x.dy_ld : nullptr;
+      moe_bf16* const ys = x.out + static_cast<long long>(block) * N * x.out_ld;
+      const uint32_t x0 = slot * static_cast<uint32_t>(x.x_ld), g0 = slot * static_cast<uint32_t>(x.dy_ld), y0 = slot * static_cast<uint32_t>(x.out_ld);
+      for (int h0 = mine; h0 < x.H; h0 += AHEAD * EACH) {
+        u32x4 xa[AHEAD], xb[AHEAD], ga[AHEAD], gb[AHEAD];
 #pragma unroll
-        for (int u = 0; u < QK_AHEAD; ++u) {
+        for (int u = 0; u < AHEAD; ++u) {
           const int h = h0 + u * EACH;
           xa[u] = xb[u] = ga[u] = gb[u] = u32x4{0, 0, 0, 0};
           if (h >= x.H) continue;
-          const size_t head = static_cast<size_t>(h) * a.D;
-          if (at.has_a) xa[u] = *reinterpret_cast<const u32x4*>(xr + head + at.a);
-          if (at.has_b) xb[u] = *reinterpret_cast<const u32x4*>(xr + head + at.b);
+          const uint32_t head = static_cast<uint32_t>(h * a.D);
+          if (at.has_a) xa[u] = load8(xs + (x0 + head + at.a));
+          if (at.has_b) xb[u] = load8(xs + (x0 + head + at.b));
           if constexpr (BWD) {
-            if (at.has_a) ga[u] = *reinterpret_cast<const u32x4*>(gr + head + at.a);
-            if (at.has_b) gb[u] = *reinterpret_cast<const u32x4*>(gr + head + at.b);
+            if (at.has_a) ga[u] = load8(gs + (g0 + head + at.a));
+            if (at.has_b) gb[u] = load8(gs + (g0 + head + at.b));
           }
         }
 #pragma unroll
-        for (int u = 0; u < QK_AHEAD; ++u) {
+        for (int u = 0; u < AHEAD; ++u) {
+          __builtin_amdgcn_sched_barrier(0);                             // (one head's numbers in registers at a time)
           const int h = h0 + u * EACH;
           if (h >= x.H) continue;                                        // (the same for all threads of a head)
-          const size_t head = static_cast<size_t>(h) * a.D;
+          const uint32_t head = static_cast<uint32_t>(h * a.D);
           float v[16], sum = 0.f;
           unpack16(xa[u], xb[u], v);
 #pragma unroll
@@ -149,11 +146,11 @@ __global__ __launch_bounds__(QK_THREADS) void qk_norm_kernel(QkArgs a) {
           if constexpr (!BWD) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) v[j] = v[j] * r * w[j];
-            turn(v, c, s, pairs, 1.f);
+            turn<PAIRS>(v, c, s, 1.f);
           } else {
             float g[16], dot = 0.f;
             unpack16(ga[u], gb[u], g);
-            turn(g, c, s, pairs, -1.f);
+            turn<PAIRS>(g, c, s, -1.f);
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
               dw[W][j] = __builtin_fmaf(g[j], v[j] * r, dw[W][j]);
@@ -164,8 +161,8 @@ __global__ __launch_bounds__(QK_THREADS) void qk_norm_kernel(QkArgs a) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) v[j] = r * __builtin_fmaf(-v[j], k, g[j]);
           }
-          if (at.has_a) *reinterpret_cast<u32x4*>(yr + head + at.a) = pack_half(v, 0);
-          if (at.has_b) *reinterpret_cast<u32x4*>(yr + head + at.b) = pack_half(v, 8);
+          if (at.has_a) *reinterpret_cast<u32x4*>(ys + (y0 + head + at.a)) = pack_half(v, 0);
+          if (at.has_b) *reinterpret_cast<u32x4*>(ys + (y0 + head + at.b)) = pack_half(v, 8);
         }
       }
     };
@@ -184,7 +181,7 @@ __global__ __launch_bounds__(QK_THREADS) void qk_norm_kernel(QkArgs a) {
       __syncthreads();
       for (int c = tid; c < TPR * 16; c += QK_THREADS) {
         const int owner = c / 16, j = c % 16;
-        const Place o = place_of(owner, a.D, a.R, pairs);
+        const Place o = place_of(owner, a.D, a.R, PAIRS);
         const int col = j < 8 ? o.a + j : o.b + j - 8;
         if (!(j < 8 ? o.has_a : o.has_b)) continue;
         float v = 0.f;
@@ -236,20 +233,28 @@ template <typename F> void with_threads(int D, F&& f) {
   else f(std::integral_constant<int, 32>{});
 }
 constexpr int QK_TOKENS = 4, QK_MANY = 2048;      // tokens to a workgroup, where there are as many tokens
+constexpr long long QK_NEAR = 1ll << 28;          // elements from a token to the next at most, where a workgroup has several
+int qk_tokens(const QkArgs& a) {
+  for (const QkSide* s : {&a.q, &a.k})
+    for (long long ld : {s->x_ld, s->out_ld, s->dy_ld}) if (ld > QK_NEAR) return 1;
+  return a.T >= QK_MANY ? QK_TOKENS : 1;
+}
 // Workgroups of the backward pass, each with a share of dw.
-int qk_bwd_groups(int T) {
-  const int groups = T >= QK_MANY ? (T + QK_TOKENS - 1) / QK_TOKENS : T;
-  return groups < 512 ? groups : 512;
+int qk_bwd_groups(int T, int tokens) {
+  const int groups = (T + tokens - 1) / tokens;
+  return groups < 1024 ? groups : 1024;
 }
 template <bool BWD> int launch_qk(const QkArgs& a, const char* name, hipStream_t s) {
+  const int tokens = qk_tokens(a);
+  const dim3 grid(BWD ? qk_bwd_groups(a.T, tokens) : (a.T + tokens - 1) / tokens);
   with_threads(a.D, [&](auto tpr) {
     constexpr int TPR = decltype(tpr)::value;
-    if (a.T >= QK_MANY) {
-      const dim3 grid(BWD ? qk_bwd_groups(a.T) : (a.T + QK_TOKENS - 1) / QK_TOKENS);
-      MOE_LAUNCH(name, (qk_norm_kernel<TPR, QK_TOKENS, BWD>), grid, dim3(QK_THREADS), 0, s, a);
+    if (tokens == QK_TOKENS) {
+      if (a.pairs) MOE_LAUNCH(name, (qk_norm_kernel<TPR, QK_TOKENS, true, BWD>), grid, dim3(QK_THREADS), 0, s, a);
+      else MOE_LAUNCH(name, (qk_norm_kernel<TPR, QK_TOKENS, false, BWD>), grid, dim3(QK_THREADS), 0, s, a);
     } else {
-      const dim3 grid(BWD ? qk_bwd_groups(a.T) : a.T);
-      MOE_LAUNCH(name, (qk_norm_kernel<TPR, 1, BWD>), grid, dim3(QK_THREADS), 0, s, a);
+      if (a.pairs) MOE_LAUNCH(name, (qk_norm_kernel<TPR, 1, true, BWD>), grid, dim3(QK_THREADS), 0, s, a);
+      else MOE_LAUNCH(name, (qk_norm_kernel<TPR, 1, false, BWD>), grid, dim3(QK_THREADS), 0, s, a);
     }
   });
   return moe_check_launch();
@@ -267,7 +272,7 @@ extern "C" int moe_qk_norm_rope(const moe_bf16* q, long long q_ld, const moe_bf1
 
 extern "C" size_t moe_qk_norm_rope_bwd_workspace_bytes(int T, int Hq, int Hk, int D) {
   if (bad_qk_dims(T, Hq, Hk, D)) return 0;
-  return static_cast<size_t>(qk_bwd_groups(T)) * 2 * D * sizeof(float);
+  return static_cast<size_t>(T < 1024 ? T : 1024) * 2 * D * sizeof(float);
 }
 
 extern "C" int moe_qk_norm_rope_bwd(const moe_bf16* dqo, long long dqo_ld, const moe_bf16* dko, long long dko_ld, const moe_bf16* q, long long q_ld,
@@ -279,6 +284,6 @@ extern "C" int moe_qk_norm_rope_bwd(const moe_bf16* dqo, long long dqo_ld, const
   if (ws_bytes < moe_qk_norm_rope_bwd_workspace_bytes(T, Hq, Hk, D)) return MOE_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (launch_qk<true>(a, "qk_norm_rope_bwd", s) != MOE_OK) return MOE_ERR_LAUNCH;
-  MOE_LAUNCH("qk_dw", qk_dw_kernel, dim3(2 * D / 8), dim3(256), 0, s, static_cast<const float*>(ws), qk_bwd_groups(T), D, dwq, dwk);
+  MOE_LAUNCH("qk_dw", qk_dw_kernel, dim3(2 * D / 8), dim3(256), 0, s, static_cast<const float*>(ws), qk_bwd_groups(T, qk_tokens(a)), D, dwq, dwk);
   return moe_check_launch();
 }
