@@ -538,22 +538,31 @@ def moe_head_distill_bwd(x, W, target, ids, teacher, temperature: float, loss, l
                                        ws.numel() * ws.element_size(), _stream()), "moe_head_distill_bwd")
 
 
-def _here(t, dtype, shape, name):
-    """The address of a dense tensor on the current device, whose stream the call is enqueued on."""
-    _want(t, dtype, shape, name)
-    return _where(t, name)
-
-
-def _where(t, name):
+# The calls below take the device of their first tensor, which has to be the current one: their kernels go to its current stream.
+def _device_of(t, name) -> int:
     if t is None:
         raise MoeError(f"{name} is missing")
-    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice() or not t.is_contiguous():
+    at = t.get_device()                       # -1: on the host
+    if at < 0 or at != torch._C._cuda_getDevice():
+        raise MoeError(f"{name}: tensors must be device tensors, on the current device")
+    return at
+
+
+def _here(t, dtype, shape, name, dev):
+    """The address of a dense tensor on that device."""
+    if t is None or t.dtype is not dtype or t.shape != shape:
+        _want(t, dtype, shape, name)
+    if t.get_device() != dev or not t.is_contiguous():
         raise MoeError(f"{name}: tensors must be contiguous device tensors, on the current device")
     return t.data_ptr()
 
 
-def _space(ws):
-    return _where(ws, "ws"), ws.numel() * ws.element_size()
+def _space(ws, dev):
+    if ws is None:
+        raise MoeError("ws is missing")
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise MoeError("ws: tensors must be contiguous device tensors, on the current device")
+    return ws.data_ptr(), ws.nbytes
 
 
 def moe_head_score_fwd_workspace_bytes(T: int, d: int, V: int, K: int = 0) -> int:
@@ -567,39 +576,49 @@ def moe_head_score_bwd_workspace_bytes(T: int, d: int, V: int, v_piece: int = 0)
 def _score_args(x, W, target):
     if x is None or W is None or x.dim() != 2 or W.dim() != 2:
         raise MoeError("x, W: expected [tokens, columns] and [vocabulary, columns]")
+    dev = _device_of(x, "x")
     (T, d), V = x.shape, W.shape[0]
-    return T, d, V, (_here(x, BF16, (T, d), "x"), _here(W, BF16, (V, d), "W"), _here(target, torch.int32, (T,), "target"))
+    return dev, T, d, V, _here(x, BF16, (T, d), "x", dev), _here(W, BF16, (V, d), "W", dev), _here(target, torch.int32, (T,), "target", dev)
 
 
 def moe_head_score_fwd(x, W, target, temperature: float, logp, entropy, lse, ids, top, ws) -> None:
     """Log probability of each target at a temperature, entropy of each token's distribution, and as many of its likeliest
     alternatives as ids and top have columns (None: none); a target outside the vocabulary (-100) counts for nothing."""
-    T, d, V, given = _score_args(x, W, target)
-    K, lists = 0, (None, None)
+    dev, T, d, V, *given = _score_args(x, W, target)
+    K, lists, f32 = 0, (None, None), torch.float32
     if ids is not None or top is not None:
         K = ids.shape[-1] if ids is not None else top.shape[-1]
-        lists = (_here(ids, torch.int32, (T, K), "ids"), _here(top, torch.float32, (T, K), "top"))
-    _check(load().moe_head_score_fwd(*given, temperature, T, d, V, K, *(_here(t, torch.float32, (T,), n) for t, n in ((logp, "logp"), (entropy, "entropy"), (lse, "lse"))),
-                                     *lists, *_space(ws), _stream()), "moe_head_score_fwd")
+        lists = _here(ids, torch.int32, (T, K), "ids", dev), _here(top, f32, (T, K), "top", dev)
+    rows = (T,)
+    rc = load().moe_head_score_fwd(*given, temperature, T, d, V, K, _here(logp, f32, rows, "logp", dev), _here(entropy, f32, rows, "entropy", dev),
+                                   _here(lse, f32, rows, "lse", dev), *lists, *_space(ws, dev), _stream())
+    if rc != 0:
+        _check(rc, "moe_head_score_fwd")
 
 
 def moe_head_score_bwd(x, W, target, temperature: float, logp, entropy, lse, dlogp, dentropy, v_piece: int, dx, dW, ws) -> None:
     """From the gradients of log probabilities and (unless None) entropies; dx and dW are overwritten."""
-    T, d, V, given = _score_args(x, W, target)
-    rows = [(logp, "logp"), (entropy, "entropy"), (lse, "lse"), (dlogp, "dlogp")]
-    _check(load().moe_head_score_bwd(*given, temperature, *(_here(t, torch.float32, (T,), n) for t, n in rows),
-                                     None if dentropy is None else _here(dentropy, torch.float32, (T,), "dentropy"), T, d, V, v_piece,
-                                     _here(dx, BF16, (T, d), "dx"), _here(dW, BF16, (V, d), "dW"), *_space(ws), _stream()), "moe_head_score_bwd")
+    dev, T, d, V, *given = _score_args(x, W, target)
+    f32, rows = torch.float32, (T,)
+    rc = load().moe_head_score_bwd(*given, temperature, _here(logp, f32, rows, "logp", dev), _here(entropy, f32, rows, "entropy", dev),
+                                   _here(lse, f32, rows, "lse", dev), _here(dlogp, f32, rows, "dlogp", dev),
+                                   None if dentropy is None else _here(dentropy, f32, rows, "dentropy", dev), T, d, V, v_piece,
+                                   _here(dx, BF16, (T, d), "dx", dev), _here(dW, BF16, (V, d), "dW", dev), *_space(ws, dev), _stream())
+    if rc != 0:
+        _check(rc, "moe_head_score_bwd")
 
 
-def _heads(t, T, H, D, name):
+def _heads(t, shape, name, dev):
     """Address and distance between tokens of [T, H, D]: a token's heads lie side by side, tokens may be rows of something wider."""
-    _want(t, BF16, (T, H, D), name)
-    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+    if t is None or t.dtype is not BF16 or t.shape != shape:
+        _want(t, BF16, shape, name)
+    if t.get_device() != dev:
         raise MoeError(f"{name}: tensors must be device tensors, on the current device")
+    T, H, D = shape
     by_token, by_head, by_column = t.stride()
-    if (D > 1 and by_column != 1) or (H > 1 and by_head != D):
-        raise MoeError(f"{name}: a token's heads must lie side by side, strides are {t.stride()}")
+    if by_column != 1 or by_head != D:
+        if (D > 1 and by_column != 1) or (H > 1 and by_head != D):
+            raise MoeError(f"{name}: a token's heads must lie side by side, strides are {t.stride()}")
     return t.data_ptr(), by_token if T > 1 else H * D
 
 
@@ -607,22 +626,29 @@ def _qk_args(q, k, wq, wk, pos, freq):
     for t, name in ((q, "q"), (k, "k")):
         if t is None or t.dim() != 3:
             raise MoeError(f"{name}: expected [tokens, heads, columns]")
-    (T, Hq, D), Hk = q.shape, k.shape[1]
-    R = 0
+    q_shape = T, _, D = q.shape
+    k_shape = T, k.shape[1], D
+    R, freq_at = 0, None
     if freq is not None:
-        _want(freq, torch.float32, (freq.numel(),), "freq")
-        R = 2 * freq.numel()
-    return T, Hq, Hk, D, R, (_here(wq, torch.float32, (D,), "wq"), _here(wk, torch.float32, (D,), "wk"), _here(pos, torch.int32, (T,), "pos"),
-                             _where(freq, "freq") if R else None)
+        R = 2 * freq.shape[0] if freq.dim() == 1 else -1
+        if freq.dtype is not torch.float32 or R < 0:
+            raise MoeError(f"freq: expected float32 [pairs], got {freq.dtype} {tuple(freq.shape)}")
+    dev = _device_of(q, "q")
+    if R:
+        freq_at = _here(freq, torch.float32, freq.shape, "freq", dev)
+    return dev, q_shape, k_shape, R, (_here(wq, torch.float32, (D,), "wq", dev), _here(wk, torch.float32, (D,), "wk", dev),
+                                      _here(pos, torch.int32, (T,), "pos", dev), freq_at)
 
 
 def moe_qk_norm_rope(q, k, wq, wk, pos, freq, pairs: bool, eps: float, qo, ko) -> None:
     """Norm of every head's queries and keys and their rotation by ``pos[t] * freq[i]``; ``pairs``: neighbours are turned, else halves.
 
     ``freq`` has an entry for each pair of rotated columns (None: none is rotated).  qo may be q and ko may be k."""
-    T, Hq, Hk, D, R, w = _qk_args(q, k, wq, wk, pos, freq)
-    _check(load().moe_qk_norm_rope(*_heads(q, T, Hq, D, "q"), *_heads(k, T, Hk, D, "k"), *w, 1 if pairs else 0, eps, T, Hq, Hk, D, R,
-                                   *_heads(qo, T, Hq, D, "qo"), *_heads(ko, T, Hk, D, "ko"), _stream()), "moe_qk_norm_rope")
+    dev, qs, ks, R, w = _qk_args(q, k, wq, wk, pos, freq)
+    rc = load().moe_qk_norm_rope(*_heads(q, qs, "q", dev), *_heads(k, ks, "k", dev), *w, 1 if pairs else 0, eps, qs[0], qs[1], ks[1], qs[2], R,
+                                 *_heads(qo, qs, "qo", dev), *_heads(ko, ks, "ko", dev), _stream())
+    if rc != 0:
+        _check(rc, "moe_qk_norm_rope")
 
 
 def moe_qk_norm_rope_bwd_workspace_bytes(T: int, Hq: int, Hk: int, D: int) -> int:
@@ -631,34 +657,43 @@ def moe_qk_norm_rope_bwd_workspace_bytes(T: int, Hq: int, Hk: int, D: int) -> in
 
 def moe_qk_norm_rope_bwd(dqo, dko, q, k, wq, wk, pos, freq, pairs: bool, eps: float, dq, dk, dwq, dwk, ws) -> None:
     """From the gradients of what ``moe_qk_norm_rope`` gave for q and k.  dq may be dqo or q, dk may be dko or k."""
-    T, Hq, Hk, D, R, w = _qk_args(q, k, wq, wk, pos, freq)
-    _check(load().moe_qk_norm_rope_bwd(*_heads(dqo, T, Hq, D, "dqo"), *_heads(dko, T, Hk, D, "dko"), *_heads(q, T, Hq, D, "q"),
-                                       *_heads(k, T, Hk, D, "k"), *w, 1 if pairs else 0, eps, T, Hq, Hk, D, R, *_heads(dq, T, Hq, D, "dq"),
-                                       *_heads(dk, T, Hk, D, "dk"), _here(dwq, torch.float32, (D,), "dwq"), _here(dwk, torch.float32, (D,), "dwk"),
-                                       *_space(ws), _stream()), "moe_qk_norm_rope_bwd")
+    dev, qs, ks, R, w = _qk_args(q, k, wq, wk, pos, freq)
+    D = qs[2]
+    rc = load().moe_qk_norm_rope_bwd(*_heads(dqo, qs, "dqo", dev), *_heads(dko, ks, "dko", dev), *_heads(q, qs, "q", dev), *_heads(k, ks, "k", dev), *w,
+                                     1 if pairs else 0, eps, qs[0], qs[1], ks[1], D, R, *_heads(dq, qs, "dq", dev), *_heads(dk, ks, "dk", dev),
+                                     _here(dwq, torch.float32, (D,), "dwq", dev), _here(dwk, torch.float32, (D,), "dwk", dev), *_space(ws, dev), _stream())
+    if rc != 0:
+        _check(rc, "moe_qk_norm_rope_bwd")
 
 
 _GRAD_TYPES = {BF16: 0, torch.float32: 1}
+_dtype, _shape, _device = torch.Tensor.dtype.__get__, torch.Tensor.shape.__get__, torch.Tensor.get_device
 
 
 def _grad_table(grads, outs):
-    """struct moe_grad of each tensor; the table is read before the call returns."""
-    if len(grads) == 0:
+    """(struct moe_grad of each tensor, their device); the table is read before the call returns.  (Looked at attribute by attribute, all tensors at once: half the time
+    of tensor by tensor.)"""
+    n = len(grads)
+    if n == 0:
         raise MoeError("grads: no tensors")
-    table = array.array("q")
-    for n, ts in (("grads", grads), ("outs", outs)):
-        dev = torch._C._cuda_getDevice() if ts[0].is_cuda else 0
-        for i, t in enumerate(ts):
-            if t.get_device() != dev or not t.is_contiguous():
-                raise MoeError(f"{n}[{i}]: tensors must be contiguous device tensors, on the current device")
-    for i, (g, o) in enumerate(zip(grads, outs)):
-        kind = _GRAD_TYPES.get(g.dtype)
-        if kind is None:
-            raise MoeError(f"grads[{i}]: expected bfloat16 or float32, got {g.dtype}")
-        if o is not g and (o.dtype is not g.dtype or o.shape != g.shape):
-            _want(o, g.dtype, g.shape, f"outs[{i}]")
-        table.extend((g.data_ptr(), o.data_ptr(), g.numel(), kind))
-    return table, table.buffer_info()[0], len(grads)
+    dev = _device_of(grads[0], "grads[0]")
+    types, shapes = [*map(_dtype, grads)], [*map(_shape, grads)]
+    kinds = [*map(_GRAD_TYPES.get, types)]
+    if None in kinds:
+        raise MoeError(f"grads[{kinds.index(None)}]: expected bfloat16 or float32, got {types[kinds.index(None)]}")
+    same = outs is grads
+    if not same and ([*map(_dtype, outs)] != types or [*map(_shape, outs)] != shapes):
+        for i, o in enumerate(outs):
+            _want(o, types[i], shapes[i], f"outs[{i}]")
+    for name, ts in (("grads", grads),) if same else (("grads", grads), ("outs", outs)):
+        if {*map(_device, ts)} != {dev} or not all(map(torch.Tensor.is_contiguous, ts)):
+            raise MoeError(f"{name}: tensors must be contiguous device tensors, on the current device")
+    table = array.array("q", bytes(32 * n))
+    table[0::4] = ins = array.array("q", map(torch.Tensor.data_ptr, grads))
+    table[1::4] = ins if same else array.array("q", map(torch.Tensor.data_ptr, outs))
+    table[2::4] = array.array("q", map(torch.Tensor.numel, grads))
+    table[3::4] = array.array("q", kinds)
+    return table, dev
 
 
 def moe_grad_norm_workspace_bytes(n: int) -> int:
@@ -668,8 +703,10 @@ def moe_grad_norm_workspace_bytes(n: int) -> int:
 
 def moe_grad_norm(grads, norm, ws) -> None:
     """norm[0]: the norm of all these tensors (bfloat16 and float32) together."""
-    table, at, n = _grad_table(grads, grads)
-    _check(load().moe_grad_norm(at, n, _here(norm, torch.float32, (1,), "norm"), *_space(ws), _stream()), "moe_grad_norm")
+    table, dev = _grad_table(grads, grads)
+    rc = load().moe_grad_norm(table.buffer_info()[0], len(grads), _here(norm, torch.float32, (1,), "norm", dev), *_space(ws, dev), _stream())
+    if rc != 0:
+        _check(rc, "moe_grad_norm")
 
 
 def moe_grad_clip(grads, largest: float, norm, outs, ws) -> None:
@@ -677,8 +714,10 @@ def moe_grad_clip(grads, largest: float, norm, outs, ws) -> None:
     outs = grads if outs is None else outs
     if len(outs) != len(grads):
         raise MoeError(f"{len(grads)} gradients, {len(outs)} outs")
-    table, at, n = _grad_table(grads, outs)
-    _check(load().moe_grad_clip(at, n, largest, _here(norm, torch.float32, (1,), "norm"), *_space(ws), _stream()), "moe_grad_clip")
+    table, dev = _grad_table(grads, outs)
+    rc = load().moe_grad_clip(table.buffer_info()[0], len(grads), largest, _here(norm, torch.float32, (1,), "norm", dev), *_space(ws, dev), _stream())
+    if rc != 0:
+        _check(rc, "moe_grad_clip")
 
 
 class HeadBuffers:
