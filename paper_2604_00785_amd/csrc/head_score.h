@@ -9,7 +9,7 @@ struct HeadTop { float top; uint32_t next; };
 struct HeadStrip { HeadTop lane[4]; float sum, moment; };
 __host__ __device__ __forceinline__ uint32_t ordered_u32(uint32_t bits) { return bits ^ ((bits >> 31) != 0 ? 0xFFFFFFFFu : 0x80000000u); }
 
-constexpr int SCORE_MAX_K = 64, SCORE_SPARE = 8;
+constexpr int SCORE_MAX_K = 64, SCORE_SPARE = 4;
 constexpr int score_wanted(int K) { return K > 0 ? K + SCORE_SPARE : 1; }       // logits that are formed anew
 
 struct ScoreJoinArgs {
