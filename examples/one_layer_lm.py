@@ -79,9 +79,11 @@ class OneLayerLM:
         return -self.scores.loss
 
     def top_logits(self, tokens, entries):
+        """The largest logits of every token, as a teacher gives them."""
         self.forward(tokens)
-        top = (self.n2.float() @ self.p["W"].float().t()).topk(entries, 1)
-        return top.indices.int(), top.values.contiguous()
+        s = B.ScoreBuffers(self.T, self.d, self.V, entries, train=False, device=self.device)
+        s.run_fwd(self.n2, self.p["W"], torch.zeros(self.T, dtype=torch.int32, device=self.device))
+        return s.ids, s.top + s.lse[:, None]
 
 
 class Adam:
@@ -114,8 +116,16 @@ def language(V, seed=0, device="cuda:0"):
     return walk
 
 
-def train(model, walk, steps, lr=3e-3, teacher=None, entries=0, temperature=1.0):
-    """The mean loss (with a teacher: divergence) of every step, on the host."""
+def limited(grads, largest):
+    """Gradients scaled in place to a largest norm; the norm that they had, on the device."""
+    ts = list(grads.values())
+    norm = torch.empty(1, dtype=torch.float32, device=ts[0].device)
+    B.moe_grad_clip(ts, largest, norm, None, torch.empty(B.moe_grad_norm_workspace_bytes(len(ts)), dtype=torch.uint8, device=ts[0].device))
+    return norm
+
+
+def train(model, walk, steps, lr=3e-3, teacher=None, entries=0, temperature=1.0, largest=None):
+    """The mean loss (with a teacher: divergence) of every step, on the host; largest: what the gradients' norm is limited to."""
     adam, curve = Adam(model.p, lr), []
     for n in range(steps):
         tokens, target = walk(model.T, 100 + n)
@@ -126,7 +136,10 @@ def train(model, walk, steps, lr=3e-3, teacher=None, entries=0, temperature=1.0)
             ids[target < 0] = -1                                   # nothing is learnt from prompts
             target = torch.full_like(target, -100)                 # the teacher alone is learnt from
             more = (ids, logits, temperature)
-        adam.step(model.p, model.train_step(tokens, target, weight, *more))
+        grads = model.train_step(tokens, target, weight, *more)
+        if largest is not None:
+            limited(grads, largest)
+        adam.step(model.p, grads)
         curve.append(float(((model.head.loss if teacher is None else model.head.kd) * weight).sum()))
     return curve
 

@@ -764,6 +764,35 @@ class HeadBuffers:
                                  self.v_piece, self.dx, self.dW, self.ws)
 
 
+class ScoreBuffers:
+    """The head's scores (log probabilities, entropies, K alternatives a token) and their gradients for one shape, allocated once.
+
+    ``train=False`` leaves out what only the backward needs.  The calls enqueue on the current stream and do not synchronise.
+    """
+
+    def __init__(self, T: int, d: int, V: int, K: int = 0, v_piece: int = 0, train: bool = True, device="cuda:0"):
+        dev = torch.device(device)
+        row = lambda: torch.zeros(T, dtype=torch.float32, device=dev)  # noqa: E731
+        nbytes = moe_head_score_fwd_workspace_bytes(T, d, V, K)
+        back = moe_head_score_bwd_workspace_bytes(T, d, V, v_piece) if train else 1
+        if nbytes == 0 or back == 0:
+            raise MoeError(f"no scores of {T} tokens, d {d}, {V} columns, {K} alternatives, pieces of {v_piece}")
+        self.v_piece, self.train = v_piece, train
+        self.logp, self.entropy, self.lse = row(), row(), row()
+        self.ids, self.top = (torch.zeros(T, K, dtype=torch.int32, device=dev), torch.zeros(T, K, dtype=torch.float32, device=dev)) if K else (None, None)
+        if train:
+            self.dx, self.dW = torch.zeros(T, d, dtype=BF16, device=dev), torch.zeros(V, d, dtype=BF16, device=dev)
+        self.ws = torch.empty(max(nbytes, back), dtype=torch.uint8, device=dev)
+
+    def run_fwd(self, x, W, target, temperature: float = 1.0) -> None:
+        moe_head_score_fwd(x, W, target, temperature, self.logp, self.entropy, self.lse, self.ids, self.top, self.ws)
+
+    def run_bwd(self, x, W, target, dlogp, dentropy=None, temperature: float = 1.0) -> None:
+        if not self.train:
+            raise MoeError("a backward pass on buffers made with train=False")
+        moe_head_score_bwd(x, W, target, temperature, self.logp, self.entropy, self.lse, dlogp, dentropy, self.v_piece, self.dx, self.dW, self.ws)
+
+
 def moe_prof_enable(on: bool) -> None:
     _check(load().moe_prof_enable(1 if on else 0), "moe_prof_enable")
 
