@@ -200,13 +200,16 @@ bool bad_grads(const moe_grad* g, int n, bool clip) {
   }
   return false;
 }
-// Whether some output lies over an input other than its own, or over another output: what is there would depend on who comes first.
+// Whether some output lies over an input other than its own, or over another output (the norm and the workspace are such): what is there would depend on who comes first.
 struct Range { uintptr_t from, to; bool out; };
-int overlap(const moe_grad* g, int n) {
-  Range few[2 * 256];
-  Range* r = n <= 256 ? few : new (std::nothrow) Range[2 * static_cast<size_t>(n)];
+int overlap(const moe_grad* g, int n, const float* norm, const void* ws, size_t ws_bytes) {
+  Range few[2 * 256 + 2];
+  Range* r = n <= 256 ? few : new (std::nothrow) Range[2 * static_cast<size_t>(n) + 2];
   if (r == nullptr) return MOE_ERR_INVALID;
-  int m = 0;
+  const uintptr_t at[2] = {reinterpret_cast<uintptr_t>(norm), reinterpret_cast<uintptr_t>(ws)};
+  r[0] = {at[0], at[0] + sizeof(float), true};
+  r[1] = {at[1], at[1] + ws_bytes, true};
+  int m = 2;
   for (int i = 0; i < n; ++i) {
     if (g[i].count == 0) continue;
     const uintptr_t in = reinterpret_cast<uintptr_t>(g[i].in), out = reinterpret_cast<uintptr_t>(g[i].out), bytes = static_cast<uintptr_t>(g[i].count) * bytes_of(g[i]);
@@ -283,7 +286,7 @@ int run_grads(const moe_grad* g, int n, bool clip, double largest, float* norm, 
   unsigned long long pieces = 0;
   for (int i = 0; i < n; ++i) pieces += static_cast<unsigned long long>(g[i].count) / (16 / bytes_of(g[i])) + 1;
   if (pieces > 1ull << 40) return MOE_ERR_INVALID;   // chunks are counted in 32 bits
-  if (clip && overlap(g, n) != MOE_OK) return MOE_ERR_INVALID;
+  if (clip && overlap(g, n, norm, ws, moe_grad_norm_workspace_bytes(n)) != MOE_OK) return MOE_ERR_INVALID;
   const bool wide = pieces >= FEW_PIECES, few = n <= FEW_TENSORS;
   const GradCall c{g, n, static_cast<double*>(ws), largest, norm, s};
   int parts = 0;

@@ -14,6 +14,7 @@
 namespace {
 
 constexpr int SCORE_CANDIDATES = 512, SCORE_FEW = 256;
+constexpr int SCORE_ROW = 1 << 20;                 // workgroups of a row of the grid (a launch may have 2^32 threads in a row)
 
 __device__ __forceinline__ float from_ordered(uint32_t k) { return __uint_as_float(k ^ ((k >> 31) != 0 ? 0x80000000u : 0xFFFFFFFFu)); }
 // Sums of 2^t and t 2^t relative to 2^e, e a whole number.
@@ -111,7 +112,8 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
   constexpr uint32_t LOW = HALF / 4 - 1;
   constexpr uint32_t NONE = 0xFF800000u, LEAST = 0x00800000u;             // -infinity; the order of the lowest number
   const int tid = threadIdx.x, lane = tid % MOE_WAVE, wave = tid / MOE_WAVE, lq = tid & 3, K = LIST ? a.K : 0, wanted = score_wanted(K);
-  const int t = blockIdx.x;
+  const int t = blockIdx.y * SCORE_ROW + blockIdx.x;
+  if (t >= a.T) return;
   const int y = a.target[t];
   if (y < 0 || y >= a.V) {
     if (tid == 0) { a.logp[t] = 0.f; a.entropy[t] = 0.f; a.lse[t] = 0.f; }
@@ -328,7 +330,7 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
 
 template <int HALF, int THREADS, bool LIST> void launch_join(const ScoreJoinArgs& a, hipStream_t s) {
   const int lds = LIST ? (score_wanted(a.K) * (HALF / 4) + 1) * 12 : (HALF / 4 + 2) * 12;
-  MOE_LAUNCH("head_score_join", (head_score_join_kernel<HALF, THREADS, LIST>), dim3(a.T), dim3(THREADS), lds, s, a);
+  MOE_LAUNCH("head_score_join", (head_score_join_kernel<HALF, THREADS, LIST>), dim3(a.T < SCORE_ROW ? a.T : SCORE_ROW, (a.T + SCORE_ROW - 1) / SCORE_ROW), dim3(THREADS), lds, s, a);
 }
 template <int HALF> void launch_join_of(const ScoreJoinArgs& a, hipStream_t s) {
   if (a.K == 0) launch_join<HALF, 256, false>(a, s);

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(QK_THREADS) void qk_norm_kernel(QkArgs a) {
   const int blocks = (a.T + N - 1) / N;
   for (int block = blockIdx.x; block < blocks; block += gridDim.x) {
     const int half = a.R / 2, t = block * N + slot;
-    if (BWD) __syncthreads();                                            // the angles of the tokens before have been read
+    if (block != static_cast<int>(blockIdx.x)) __syncthreads();          // the angles of the tokens before have been read
     for (int j = tid; j < N * half; j += QK_THREADS) {
       const int n = j / half, f = j - n * half, token = block * N + n;
       float s = 0.f, c = 1.f;
@@ -233,6 +233,7 @@ template <typename F> void with_threads(int D, F&& f) {
   else f(std::integral_constant<int, 32>{});
 }
 constexpr int QK_TOKENS = 4, QK_MANY = 2048;      // tokens to a workgroup, where there are as many tokens
+constexpr int QK_MOST = 1 << 20;                  // workgroups of a launch (it may have 2^32 threads)
 constexpr long long QK_NEAR = 1ll << 28;          // elements from a token to the next at most, where a workgroup has several
 int qk_tokens(const QkArgs& a) {
   for (const QkSide* s : {&a.q, &a.k})
@@ -246,7 +247,8 @@ int qk_bwd_groups(int T, int tokens) {
 }
 template <bool BWD> int launch_qk(const QkArgs& a, const char* name, hipStream_t s) {
   const int tokens = qk_tokens(a);
-  const dim3 grid(BWD ? qk_bwd_groups(a.T, tokens) : (a.T + tokens - 1) / tokens);
+  const int blocks = (a.T + tokens - 1) / tokens;
+  const dim3 grid(BWD ? qk_bwd_groups(a.T, tokens) : blocks < QK_MOST ? blocks : QK_MOST);
   with_threads(a.D, [&](auto tpr) {
     constexpr int TPR = decltype(tpr)::value;
     if (tokens == QK_TOKENS) {

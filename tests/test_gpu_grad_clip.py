@@ -97,6 +97,21 @@ def test_slices_at_any_place():
         assert bool((outs[t].cpu()[~covered[t]] == 7.0).all())
 
 
+def test_large_slices_at_any_place():
+    """The same where a thread takes several pieces: slices of 20 million elements that begin at odd places."""
+    g = torch.Generator(device=DEV).manual_seed(4)
+    flat = torch.randn(20_000_011, generator=g, device=DEV).to(BF)
+    out = torch.full((20_000_020,), 7.0, dtype=BF, device=DEV)
+    cuts = [1, 3, 4_000_002, 4_000_003, 11_111_112, 20_000_008]
+    grads, to = [flat[a:b] for a, b in zip(cuts, cuts[1:])], [out[a + 5:b + 5] for a, b in zip(cuts, cuts[1:])]
+    norm, _ = clip(grads, 0.25, to)
+    want = R.grad_norm([flat[1:20_000_008].cpu()])
+    close(norm, want)
+    scaled = flat[1:20_000_008].double() * (0.25 / (want + 1e-6))
+    assert float(((out[6:20_000_013].double() - scaled).abs() - scaled.abs() * (R.HALF16 + 3 * R.HALF32) - R.LEAST16).max()) <= 0
+    assert bool((out[:6] == 7.0).all()) and bool((out[20_000_013:] == 7.0).all())
+
+
 def test_ends_of_the_range():
     # squares that 32 bits do not hold, large and small
     for size in (1e30, 1e-30):

@@ -292,3 +292,14 @@ def test_offsets_past_32_bits():
     lse = [math.log(V - 4 + sum(math.exp(s * 4 * v) for v in (3.0, 2.0, 1.0, 2.5))) for s in (1, -1)]
     for t, s in ((0, 1), (1, -1)):
         assert abs(float(got["lse"][t]) - lse[t]) < 1e-4 and abs(float(got["logp"][t]) - (s * 12.0 - lse[t])) < 1e-4
+
+
+def test_more_tokens_than_a_row_of_the_grid_has_workgroups():
+    T, d, V = (1 << 20) + 3, 64, 3
+    g = torch.Generator(device=DEV).manual_seed(15)
+    x, W = torch.randn(T, d, generator=g, device=DEV).bfloat16(), (0.1 * torch.randn(V, d, generator=g, device=DEV)).bfloat16()
+    target = (torch.arange(T, device=DEV) % 4 - 1).int()
+    got = forward(x, W, target, 2)
+    for at in (slice(0, 400), slice(T - 400, T)):
+        want, bound = R.score(x[at].cpu(), W.cpu(), target[at].cpu(), 2)
+        R.check_all({n: v[at] for n, v in got.items()}, want, bound)

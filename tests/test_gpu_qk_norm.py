@@ -159,6 +159,22 @@ def test_offsets_past_32_bits():
     R.check(kv, *R.qk_norm(k, wk, pos, freq, False, EPS), "k")
 
 
+def test_more_tokens_than_a_launch_has_workgroups_for():
+    """A token's rows are those of the token alone: the last of 2^22 and some are the same in a small call."""
+    T, D = (4 << 20) + 37, 8
+    g = torch.Generator(device=DEV).manual_seed(9)
+    q, k = (torch.randn(T, 1, D, generator=g, device=DEV).bfloat16() for _ in range(2))
+    w, pos = torch.rand(D, generator=g, device=DEV), torch.arange(T, dtype=torch.int32, device=DEV)
+    # (no rotated columns, so that a large call and a small one differ in nothing but their workgroups)
+    qo, ko = run(q, k, w, w, pos, None, False)
+    for at in (slice(T - 50, T), slice(0, 50), slice(T // 2, T // 2 + 50)):
+        a, b = run(q[at].clone(), k[at].clone(), w, w, pos[at].clone(), None, False)
+        assert torch.equal(a, qo[at]) and torch.equal(b, ko[at])
+    dq, dk, dwq, dwk = run_bwd(qo, ko, q, k, w, w, pos, None, False)
+    da, db, _, _ = run_bwd(qo[-50:].clone(), ko[-50:].clone(), q[-50:].clone(), k[-50:].clone(), w, w, pos[-50:].clone(), None, False)
+    assert torch.equal(da, dq[-50:]) and torch.equal(db, dk[-50:])
+
+
 @pytest.mark.parametrize("T", [50, 2500])
 def test_in_a_graph_and_on_another_stream(T):
     q, k, wq, wk, pos, freq, dqo, dko = inputs(T, 4, 2, 128, 128, seed=8)

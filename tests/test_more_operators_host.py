@@ -53,7 +53,7 @@ def table(*rows):
 
 def test_grad_refusals():
     lib = B.load()
-    ok = table((4096, 4096, 10, 0), (8192, 16384, 10, 1))
+    ok = table((1 << 20, 1 << 20, 10, 0), (2 << 20, 3 << 20, 10, 1))
     for call in (lambda g, n, norm, ws, b: lib.moe_grad_norm(g, n, norm, ws, b, N), lambda g, n, norm, ws, b: lib.moe_grad_clip(g, n, 1.0, norm, ws, b, N)):
         for args in ((N, 2, P, P, BIG), (ok, 0, P, P, BIG), (ok, -1, P, P, BIG), (ok, (1 << 20) + 1, P, P, BIG), (ok, 2, N, P, BIG), (ok, 2, Q, P, BIG), (ok, 2, P, N, BIG),
                      (ok, 2, P, Q, BIG)):
@@ -74,9 +74,14 @@ def test_clipping_refuses_outputs_over_other_tensors(more):
     """The same tensor twice, an output over another's input, over another's output, over its own input at another place."""
     lib = B.load()
     rest = [((1 << 30) + 4096 * i, (1 << 31) + 4096 * i, 100, 0) for i in range(more)]
+    far, further = ctypes.c_void_p(1 << 40), ctypes.c_void_p(1 << 41)
     for rows in ([(4096, 4096, 10, 0), (4096, 4096, 10, 0)], [(4096, 8192, 10, 0), (4112, 8200, 2, 1)], [(4096, 8192, 10, 0), (8210, 16384, 3, 0)],
                  [(4096, 4100, 10, 0)], [(4096, 4092, 10, 1)], [(4096, 8192, 1000, 0), (4100, 4100, 1, 0)], [(4100, 4100, 1, 1), (4096, 16384, 8, 0)]):
-        assert lib.moe_grad_clip(table(*rest, *rows), more + len(rows), 1.0, P, P, BIG, N) == INVALID, rows
+        assert lib.moe_grad_clip(table(*rest, *rows), more + len(rows), 1.0, far, further, BIG, N) == INVALID, rows
+    # the norm or the workspace over a tensor, or over each other
+    for norm, ws, rows in ((4096, 8192, [(4090, 4090, 10, 0)]), (4096, 8192, [(4096, 1 << 20, 1, 1)]), (1 << 40, 4096, [(1 << 20, 4096 + 1024 * 8 - 2, 1, 0)]),
+                           (1 << 40, 4096, [(4096, 1 << 20, 1, 0)]), (4096 + 16, 4096, [(1 << 20, 1 << 21, 1, 0)])):
+        assert lib.moe_grad_clip(table(*rest, *rows), more + len(rows), 1.0, ctypes.c_void_p(norm), ctypes.c_void_p(ws), BIG, N) == INVALID, (norm, ws, rows)
 
 
 def test_binding_refuses_types_shapes_and_host_tensors():
