@@ -150,7 +150,7 @@ struct GemmArgs {
 // by strips of 64 columns.
 struct HeadItem { uint32_t at, slot; };   // at: row in the block | column << 4
 struct HeadArgs {
-  float* part;                // HEAD_TOP: HeadStrip [row][strips of HALF columns].  HEAD_STATS: [row block][strips of HALF columns][2 or (two) 3][16 rows]: maximum, sum and sum at the temperature, without the items
+  float* part;                // HEAD_TOP: HeadStrip, or (two 0) HeadBest, [row][strips of HALF columns].  HEAD_STATS: [row block][strips of HALF columns][2 or (two) 3][16 rows]: maximum, sum and sum at the temperature, without the items
   const f32x4_t* row;         // HEAD_DZ: per row log2(e) lse, factor, and the same at the temperature.  HEAD_SCORE_DZ: l, u, v of 2^t (u + v t), t = c1 z - l
   const int32_t* target;      // [row]
   const int32_t* list_start;  // [row block][list_ld]: first item of each strip; null: no teacher
@@ -1590,7 +1590,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
           if (lq < planes && i * 16 + l16 < rows) out[i * block] = lq == 0 ? m : lq == 1 ? s1 : s2;
         });
       } else if constexpr (MODE == HEAD_TOP) {
-        HeadStrip* const out = reinterpret_cast<HeadStrip*>(he->part) + static_cast<size_t>(grow0 + l16) * he->strips + gcol0 / HALF;
+        const size_t out = static_cast<size_t>(grow0 + l16) * he->strips + gcol0 / HALF;
         static_for<NB>([&](auto i_tag) {
           constexpr int i = decltype(i_tag)::value;
           if (i * 16 >= rows || left <= 0) return;
@@ -1622,10 +1622,27 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
             moment = __builtin_fmaf(e, t, moment);
           }
           const auto add = [](float x, float y) __attribute__((always_inline)) { return x + y; };
+          if (!two) {
+            // the first of the four lanes' largest stays apart, the others join the sums
+            const float column = static_cast<float>(16 * (place >> 2) + 4 * lq + (place & 3));
+            const float first = quads_reduce(m == whole ? column : static_cast<float>(HALF), [](float x, float y) __attribute__((always_inline)) { return fminf(x, y); });
+            const float t = __builtin_elementwise_maximum(__builtin_fmaf(m, c1, -e1), -1000.f), e = __builtin_amdgcn_exp2f(t);
+            if (column != first) {
+              sum += e;
+              moment = __builtin_fmaf(e, t, moment);
+            }
+            sum = quads_reduce(sum, add);
+            moment = quads_reduce(moment, add);
+            if (lq == 0 && i * 16 + l16 < rows) {
+              const u32x4 w = {__float_as_uint(whole), static_cast<uint32_t>(first) & (HALF - 1), __float_as_uint(sum), __float_as_uint(moment)};
+              *reinterpret_cast<u32x4*>(reinterpret_cast<HeadBest*>(he->part) + out + static_cast<size_t>(i * 16) * he->strips) = w;
+            }
+            return;
+          }
           sum = quads_reduce(sum, add);
           moment = quads_reduce(moment, add);
           if (i * 16 + l16 < rows) {
-            HeadStrip* const o = out + static_cast<size_t>(i * 16) * he->strips;
+            HeadStrip* const o = reinterpret_cast<HeadStrip*>(he->part) + out + static_cast<size_t>(i * 16) * he->strips;
             constexpr uint32_t LOW = 4 * NB - 1;
             u32x2 w;
             w.x = __float_as_uint(m);

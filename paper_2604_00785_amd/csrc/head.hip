@@ -854,9 +854,10 @@ int run_score_fwd(const HeadCall& c, int* edges) {
   }
   const int edge = settle_edge(edges, logits_edge(c.T, c.V, c.d, 9.5));
   h.strips = ceil_div(c.V, edge / 2);
+  h.two = c.K > 0;
   h.part = reinterpret_cast<float*>(c.ws + l.big);
   if ((rc = launch_logits<HEAD_TOP>(a, h, edge, c.T, "gemm_head_top", c.s)) != MOE_OK) return rc;
-  const ScoreJoinArgs j{reinterpret_cast<const HeadStrip*>(h.part), all ? nullptr : reinterpret_cast<const int32_t*>(c.ws + l.control),
+  const ScoreJoinArgs j{h.part, all ? nullptr : reinterpret_cast<const int32_t*>(c.ws + l.control),
                         reinterpret_cast<const int32_t*>(c.ws + l.token_row), c.target, c.x, c.W, c.T, c.d, c.V, c.K, h.strips, h.c1, 1.0 / c.tau,
                         c.loss, c.entropy, c.lse, c.ids, c.top};
   return moe_head_score_join(j, edge, c.s);

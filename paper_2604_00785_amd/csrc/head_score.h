@@ -7,13 +7,15 @@
 // next: the second largest of the lane's columns rounded up, as an integer in the order of the numbers, whose low bits are the largest one's place (4 j + c).
 struct HeadTop { float top; uint32_t next; };
 struct HeadStrip { HeadTop lane[4]; float sum, moment; };
+// The same where no alternatives are wanted: the strip's largest logit, its column in the strip, and the sums of all others.
+struct HeadBest { float top; uint32_t column; float sum, moment; };
 __host__ __device__ __forceinline__ uint32_t ordered_u32(uint32_t bits) { return bits ^ ((bits >> 31) != 0 ? 0xFFFFFFFFu : 0x80000000u); }
 
 constexpr int SCORE_MAX_K = 64, SCORE_SPARE = 4;
 constexpr int score_wanted(int K) { return K > 0 ? K + SCORE_SPARE : 1; }       // logits that are formed anew
 
 struct ScoreJoinArgs {
-  const HeadStrip* part;
+  const void* part;                                // HeadStrip, or (K 0) HeadBest [row][strips]
   const int32_t *control, *token_row, *target;     // control null: rows are tokens
   const moe_bf16 *x, *W;
   int T, d, V, K, strips;

@@ -89,6 +89,80 @@ template <int G> __device__ __forceinline__ uint64_t group_most(uint64_t v) {
   return v;
 }
 
+constexpr uint32_t NONE = 0xFF800000u;              // -infinity
+// What the sums over all columns but the largest come to.  The largest by the product is what they leave out: the formulas hold whether it is the largest in 64 bits
+// or next to it.  NaN where a logit is no number or infinite, and where a scale of 2^30 or more leaves its exponent without digits.
+struct ScoreResult { double log_1R; float entropy; };
+__device__ __forceinline__ ScoreResult result_of(const ScoreSum& all, bool there, double z_top, float c1) {
+  const double from = static_cast<double>(all.e) - z_top * static_cast<double>(c1);
+  const bool alone = all.e == -3.0e38f;                                    // no other column
+  const bool fine = there && fabs(z_top * static_cast<double>(c1)) < 0x1p30 && (alone || fabsf(all.e) < 0x1p30f);
+  const double whole = fmax(rint(from), -10000.0);
+  const float scale = fine ? __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(static_cast<float>(from - whole)), static_cast<int>(whole)) : __builtin_nanf("");
+  const float R = alone ? 0.f : all.sum * scale;
+  const float Q = alone ? 0.f : -0.693147180559945309f * scale * __builtin_fmaf(static_cast<float>(from), all.sum, all.moment);
+  const float log_1R = fine ? log1pf(R) : __builtin_nanf("");
+  return {static_cast<double>(log_1R), log_1R + Q / (1.f + R)};
+}
+__device__ __forceinline__ void put_scores(const ScoreJoinArgs& a, int t, const ScoreResult& r, bool at_top, double z, double z_top) {
+  a.logp[t] = at_top ? -static_cast<float>(r.log_1R) : static_cast<float>((z - z_top) * a.over_tau - r.log_1R);
+  a.entropy[t] = r.entropy;
+  a.lse[t] = static_cast<float>(z_top * a.over_tau + r.log_1R);
+}
+
+// Without alternatives: a wave for each token.  HALF: columns of a strip.
+template <int HALF> __global__ __launch_bounds__(256) void head_score_kernel(ScoreJoinArgs a) {
+  constexpr int AT_ONCE = 4;
+  typedef __attribute__((ext_vector_type(4))) uint32_t u4;
+  const int lane = threadIdx.x % MOE_WAVE, t = __builtin_amdgcn_readfirstlane((blockIdx.y * SCORE_ROW + blockIdx.x) * 4 + threadIdx.x / MOE_WAVE);
+  if (t >= a.T) return;
+  const int y = a.target[t];
+  if (y < 0 || y >= a.V) {
+    if (lane == 0) { a.logp[t] = 0.f; a.entropy[t] = 0.f; a.lse[t] = 0.f; }
+    return;
+  }
+  const int row = a.control != nullptr ? a.token_row[t] : t;
+  const u4* const strip = static_cast<const u4*>(a.part) + static_cast<size_t>(row) * a.strips;
+  const float c1 = a.c1;
+  uint64_t best = 0;
+  ScoreSum total;
+  for (int s0 = lane; s0 < a.strips; s0 += AT_ONCE * MOE_WAVE) {
+    u4 x[AT_ONCE];
+    float E[AT_ONCE], most = total.e;
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int s = s0 + i * MOE_WAVE;
+      x[i] = u4{NONE, 0, 0, 0};
+      if (s < a.strips) x[i] = strip[s];
+    }
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      E[i] = x[i][0] == NONE ? total.e : ceilf(__uint_as_float(x[i][0]) * c1);
+      most = fmaxf(most, E[i]);
+    }
+    total.raise(most);
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const float sum = __uint_as_float(x[i][2]);
+      total.add(x[i][0] == NONE && sum == 0.f ? total.e : E[i], sum, __uint_as_float(x[i][3]));
+      const int col = (s0 + i * MOE_WAVE) * HALF + static_cast<int>(x[i][1]);
+      const uint64_t key = x[i][0] == NONE ? 0 : static_cast<uint64_t>(ordered_u32(x[i][0])) << 32 | ~static_cast<uint32_t>(col), less = key < best ? key : best;
+      best = key < best ? best : key;
+      if (less != 0) total.add_logit(from_ordered(static_cast<uint32_t>(less >> 32)), c1);
+    }
+  }
+  const uint64_t top_key = group_most<MOE_WAVE>(best);
+  if (best != top_key && best != 0) total.add_logit(from_ordered(static_cast<uint32_t>(best >> 32)), c1);
+  total.raise(group_max<MOE_WAVE>(total.e));
+  total.sum = group_sum<MOE_WAVE>(total.sum);
+  total.moment = group_sum<MOE_WAVE>(total.moment);
+  const int top_col = top_key != 0 ? static_cast<int>(~__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(top_key))) : y;
+  const int col[2] = {top_col, y};
+  double z[2];
+  exact_logits<2, 4>(a.x + static_cast<size_t>(t) * a.d, a.W, a.d, col, z);
+  if (lane == 0) put_scores(a, t, result_of(total, top_key != 0, z[0], c1), y == top_col, z[1], z[0]);
+}
+
 // put(i, number of k with above(k, i)) for i and k below n, sixteen threads to an i.
 template <int THREADS, typename Above, typename Put> __device__ __forceinline__ void ranked(int n, Above&& above, Put&& put) {
   const int l16 = threadIdx.x % 16;
@@ -100,18 +174,18 @@ template <int THREADS, typename Above, typename Put> __device__ __forceinline__ 
   }
 }
 
-// A workgroup of THREADS for each token.  HALF: columns of a strip; LIST: with alternatives.
-template <int HALF, int THREADS, bool LIST>
+// With alternatives: a workgroup of THREADS for each token.  HALF: columns of a strip.
+template <int HALF, int THREADS>
 __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs a) {
   constexpr int GROUPS = 256, WAVES = THREADS / MOE_WAVE, AT_ONCE = THREADS > 256 ? 4 : 8, STEP = THREADS / 4;
   extern __shared__ double exact[];
-  __shared__ uint64_t keys[LIST ? GROUPS : WAVES], found[LIST ? SCORE_CANDIDATES : 1], chosen[score_wanted(LIST ? SCORE_MAX_K : 0)], s_top, s_least;
-  __shared__ uint32_t found_next[LIST ? SCORE_CANDIDATES : 1], chosen_next[score_wanted(LIST ? SCORE_MAX_K : 0)];
+  __shared__ uint64_t keys[GROUPS], found[SCORE_CANDIDATES], chosen[score_wanted(SCORE_MAX_K)], s_top, s_least;
+  __shared__ uint32_t found_next[SCORE_CANDIDATES], chosen_next[score_wanted(SCORE_MAX_K)];
   __shared__ float part[WAVES][3];
   __shared__ int s_found, s_columns, s_top_at;
   constexpr uint32_t LOW = HALF / 4 - 1;
-  constexpr uint32_t NONE = 0xFF800000u, LEAST = 0x00800000u;             // -infinity; the order of the lowest number
-  const int tid = threadIdx.x, lane = tid % MOE_WAVE, wave = tid / MOE_WAVE, lq = tid & 3, K = LIST ? a.K : 0, wanted = score_wanted(K);
+  constexpr uint32_t LEAST = 0x00800000u;                                 // the order of the lowest number
+  const int tid = threadIdx.x, lane = tid % MOE_WAVE, wave = tid / MOE_WAVE, lq = tid & 3, K = a.K, wanted = score_wanted(K);
   const int t = blockIdx.y * SCORE_ROW + blockIdx.x;
   if (t >= a.T) return;
   const int y = a.target[t];
@@ -121,7 +195,7 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
     return;
   }
   const int row = a.control != nullptr ? a.token_row[t] : t;
-  const HeadStrip* const strip = a.part + static_cast<size_t>(row) * a.strips;
+  const HeadStrip* const strip = static_cast<const HeadStrip*>(a.part) + static_cast<size_t>(row) * a.strips;
   const float c1 = a.c1;
   int32_t* const columns = reinterpret_cast<int32_t*>(exact + wanted * (HALF / 4) + 1);
 
@@ -139,7 +213,7 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
     }
   };
   // All logits but a thread's largest are summed up at once; the largest of all is left out.  (A sum's NaN reaches all that is made of it.)
-  constexpr bool KEEP = LIST && THREADS > 256;
+  constexpr bool KEEP = THREADS > 256;
   HeadTop kept[KEEP ? AT_ONCE : 1];                                       // of the first round
   uint64_t best = 0;
   ScoreSum total;
@@ -175,16 +249,7 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
     }
   }
   if (tid == 0) { s_top = s_least = 0; s_found = s_columns = 0; s_top_at = 0; }
-  if constexpr (!LIST) {
-    const uint64_t most = group_most<MOE_WAVE>(best);
-    if (lane == 0) keys[wave] = most;
-    __syncthreads();
-    uint64_t whole = keys[0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) whole = keys[w] > whole ? keys[w] : whole;
-    if (tid == 0) s_top = whole;
-    if (best != whole && best != 0) total.add_logit(from_ordered(static_cast<uint32_t>(best >> 32)), c1);
-  } else {
+  {
     // The largest of every few threads, and of these the one that `wanted` - 1 are above: no smaller logit is among the `wanted` largest.
     const bool coarse = wanted <= 32;                                     // 64 groups are enough
     constexpr int FINE = THREADS / GROUPS;
@@ -209,12 +274,8 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
   __syncthreads();
   const uint64_t top_key = s_top, least = s_least;
   const int top_col = static_cast<int>(~static_cast<uint32_t>(top_key));
-  int m = top_key != 0 ? 1 : 0;                                           // columns whose logits are formed anew, beside the target
-  if constexpr (!LIST) {
-    if (tid == 0) { columns[0] = m != 0 ? top_col : y; columns[1] = y; }
-    __syncthreads();
-    if (m == 0) m = 1;
-  } else {
+  int m;                                                                  // columns whose logits are formed anew, beside the target
+  {
     int n;                                                                // lanes of the product whose columns are looked at
     const auto look = [&](const HeadTop& x, int s) __attribute__((always_inline)) {
       const uint64_t key = key_of(x, s);
@@ -280,7 +341,7 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
     if (tid == 0) columns[m] = y;
     __syncthreads();
   }
-  constexpr int N = !LIST || THREADS > 256 ? 2 : 4, AHEAD = N == 2 ? 4 : 2;
+  constexpr int N = THREADS > 256 ? 2 : 4, AHEAD = N == 2 ? 4 : 2;
   for (int i = wave * N; i <= m; i += WAVES * N) {
     int col[N];
     double z[N];
@@ -297,23 +358,9 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
   for (int w = 0; w < WAVES; ++w) all.e = fmaxf(all.e, part[w][0]);
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) all.add(part[w][0], part[w][1], part[w][2]);
-  // the largest logit by the product is what the sums leave out: the formulas hold whether it is the largest in 64 bits or next to it
   const double z_top = exact[s_top_at];
-  const double from = static_cast<double>(all.e) - z_top * static_cast<double>(c1);
-  // (NaN where a logit is no number or infinite, and where a scale of 2^30 or more leaves its exponent without digits)
-  const bool alone = all.e == -3.0e38f;                                    // no other column
-  const bool fine = top_key != 0 && fabs(z_top * static_cast<double>(c1)) < 0x1p30 && (alone || fabsf(all.e) < 0x1p30f);
-  const double whole = fmax(rint(from), -10000.0);
-  const float scale = fine ? __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(static_cast<float>(from - whole)), static_cast<int>(whole)) : __builtin_nanf("");
-  const float R = alone ? 0.f : all.sum * scale;
-  const float Q = alone ? 0.f : -0.693147180559945309f * scale * __builtin_fmaf(static_cast<float>(from), all.sum, all.moment);
-  const double log_1R = static_cast<double>(fine ? log1pf(R) : __builtin_nanf(""));
-  if (tid == 0) {
-    a.logp[t] = y == top_col ? -static_cast<float>(log_1R) : static_cast<float>((exact[m] - z_top) * a.over_tau - log_1R);
-    a.entropy[t] = static_cast<float>(log_1R) + Q / (1.f + R);
-    a.lse[t] = static_cast<float>(z_top * a.over_tau + log_1R);
-  }
-  if constexpr (!LIST) return;
+  const ScoreResult r = result_of(all, top_key != 0, z_top, c1);
+  if (tid == 0) put_scores(a, t, r, y == top_col, exact[m], z_top);
   for (int k = m + tid; k < K; k += THREADS) {                       // (logits of -infinity)
     a.ids[static_cast<size_t>(t) * K + k] = -1;
     a.top[static_cast<size_t>(t) * K + k] = __builtin_nanf("");
@@ -324,24 +371,26 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
   }, [&](int i, int above) __attribute__((always_inline)) {
     if (above >= K) return;
     a.ids[static_cast<size_t>(t) * K + above] = columns[i];
-    a.top[static_cast<size_t>(t) * K + above] = columns[i] == top_col ? -static_cast<float>(log_1R) : static_cast<float>((exact[i] - z_top) * a.over_tau - log_1R);
+    a.top[static_cast<size_t>(t) * K + above] = columns[i] == top_col ? -static_cast<float>(r.log_1R) : static_cast<float>((exact[i] - z_top) * a.over_tau - r.log_1R);
   });
 }
 
-template <int HALF, int THREADS, bool LIST> void launch_join(const ScoreJoinArgs& a, hipStream_t s) {
-  const int lds = LIST ? (score_wanted(a.K) * (HALF / 4) + 1) * 12 : (HALF / 4 + 2) * 12;
-  MOE_LAUNCH("head_score_join", (head_score_join_kernel<HALF, THREADS, LIST>), dim3(a.T < SCORE_ROW ? a.T : SCORE_ROW, (a.T + SCORE_ROW - 1) / SCORE_ROW), dim3(THREADS), lds, s, a);
-}
-template <int HALF> void launch_join_of(const ScoreJoinArgs& a, hipStream_t s) {
-  if (a.K == 0) launch_join<HALF, 256, false>(a, s);
-  else if (a.T <= SCORE_FEW) launch_join<HALF, 1024, true>(a, s);
-  else launch_join<HALF, 256, true>(a, s);
+template <int HALF> void launch_join(const ScoreJoinArgs& a, hipStream_t s) {
+  const auto rows = [](int n) { return dim3(n < SCORE_ROW ? n : SCORE_ROW, (n + SCORE_ROW - 1) / SCORE_ROW); };
+  if (a.K == 0) {
+    MOE_LAUNCH("head_score", (head_score_kernel<HALF>), rows((a.T + 3) / 4), dim3(256), 0, s, a);
+    return;
+  }
+  const int lds = (score_wanted(a.K) * (HALF / 4) + 1) * 12;
+  const dim3 grid = rows(a.T);
+  if (a.T <= SCORE_FEW) MOE_LAUNCH("head_score_join", (head_score_join_kernel<HALF, 1024>), grid, dim3(1024), lds, s, a);
+  else MOE_LAUNCH("head_score_join", (head_score_join_kernel<HALF, 256>), grid, dim3(256), lds, s, a);
 }
 
 }  // namespace
 
 int moe_head_score_join(const ScoreJoinArgs& a, int edge, hipStream_t s) {
-  if (edge == 128) launch_join_of<64>(a, s);
-  else launch_join_of<128>(a, s);
+  if (edge == 128) launch_join<64>(a, s);
+  else launch_join<128>(a, s);
   return moe_check_launch();
 }
