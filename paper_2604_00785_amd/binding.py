@@ -667,7 +667,7 @@ def moe_qk_norm_rope_bwd(dqo, dko, q, k, wq, wk, pos, freq, pairs: bool, eps: fl
 
 
 _GRAD_TYPES = {BF16: 0, torch.float32: 1}
-_dtype, _shape, _device = torch.Tensor.dtype.__get__, torch.Tensor.shape.__get__, torch.Tensor.get_device
+_dtype, _numel, _device = torch.Tensor.dtype.__get__, torch.Tensor.numel, torch.Tensor.get_device
 
 
 def _grad_table(grads, outs):
@@ -677,21 +677,22 @@ def _grad_table(grads, outs):
     if n == 0:
         raise MoeError("grads: no tensors")
     dev = _device_of(grads[0], "grads[0]")
-    types, shapes = [*map(_dtype, grads)], [*map(_shape, grads)]
+    types, counts = [*map(_dtype, grads)], [*map(_numel, grads)]
     kinds = [*map(_GRAD_TYPES.get, types)]
     if None in kinds:
         raise MoeError(f"grads[{kinds.index(None)}]: expected bfloat16 or float32, got {types[kinds.index(None)]}")
     same = outs is grads
-    if not same and ([*map(_dtype, outs)] != types or [*map(_shape, outs)] != shapes):
+    if not same and ([*map(_dtype, outs)] != types or [*map(_numel, outs)] != counts):
         for i, o in enumerate(outs):
-            _want(o, types[i], shapes[i], f"outs[{i}]")
+            if o.dtype is not types[i] or o.numel() != counts[i]:
+                raise MoeError(f"outs[{i}]: expected {counts[i]} elements of {types[i]}, got {o.numel()} of {o.dtype}")
     for name, ts in (("grads", grads),) if same else (("grads", grads), ("outs", outs)):
         if {*map(_device, ts)} != {dev} or not all(map(torch.Tensor.is_contiguous, ts)):
             raise MoeError(f"{name}: tensors must be contiguous device tensors, on the current device")
     table = array.array("q", bytes(32 * n))
     table[0::4] = ins = array.array("q", map(torch.Tensor.data_ptr, grads))
     table[1::4] = ins if same else array.array("q", map(torch.Tensor.data_ptr, outs))
-    table[2::4] = array.array("q", map(torch.Tensor.numel, grads))
+    table[2::4] = array.array("q", counts)
     table[3::4] = array.array("q", kinds)
     return table, dev
 

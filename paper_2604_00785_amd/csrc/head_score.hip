@@ -110,11 +110,14 @@ __device__ __forceinline__ void put_scores(const ScoreJoinArgs& a, int t, const 
   a.lse[t] = static_cast<float>(z_top * a.over_tau + r.log_1R);
 }
 
-// Without alternatives: a wave for each token.  HALF: columns of a strip.
-template <int HALF> __global__ __launch_bounds__(256) void head_score_kernel(ScoreJoinArgs a) {
-  constexpr int AT_ONCE = 4;
+// Without alternatives: a wave for each token, or (FEW) four.  HALF: columns of a strip.
+template <int HALF, bool FEW> __global__ __launch_bounds__(256) void head_score_kernel(ScoreJoinArgs a) {
+  constexpr int AT_ONCE = 4, STEP = FEW ? 4 * MOE_WAVE : MOE_WAVE;
   typedef __attribute__((ext_vector_type(4))) uint32_t u4;
-  const int lane = threadIdx.x % MOE_WAVE, t = __builtin_amdgcn_readfirstlane((blockIdx.y * SCORE_ROW + blockIdx.x) * 4 + threadIdx.x / MOE_WAVE);
+  __shared__ uint64_t tops[FEW ? 4 : 1];
+  __shared__ float parts[FEW ? 4 : 1][3];
+  const int lane = threadIdx.x % MOE_WAVE, wave = threadIdx.x / MOE_WAVE, group = blockIdx.y * SCORE_ROW + blockIdx.x;
+  const int t = __builtin_amdgcn_readfirstlane(FEW ? group : group * 4 + wave);
   if (t >= a.T) return;
   const int y = a.target[t];
   if (y < 0 || y >= a.V) {
@@ -126,12 +129,12 @@ template <int HALF> __global__ __launch_bounds__(256) void head_score_kernel(Sco
   const float c1 = a.c1;
   uint64_t best = 0;
   ScoreSum total;
-  for (int s0 = lane; s0 < a.strips; s0 += AT_ONCE * MOE_WAVE) {
+  for (int s0 = FEW ? threadIdx.x : lane; s0 < a.strips; s0 += AT_ONCE * STEP) {
     u4 x[AT_ONCE];
     float E[AT_ONCE], most = total.e;
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
-      const int s = s0 + i * MOE_WAVE;
+      const int s = s0 + i * STEP;
       x[i] = u4{NONE, 0, 0, 0};
       if (s < a.strips) x[i] = strip[s];
     }
@@ -145,17 +148,33 @@ template <int HALF> __global__ __launch_bounds__(256) void head_score_kernel(Sco
     for (int i = 0; i < AT_ONCE; ++i) {
       const float sum = __uint_as_float(x[i][2]);
       total.add(x[i][0] == NONE && sum == 0.f ? total.e : E[i], sum, __uint_as_float(x[i][3]));
-      const int col = (s0 + i * MOE_WAVE) * HALF + static_cast<int>(x[i][1]);
+      const int col = (s0 + i * STEP) * HALF + static_cast<int>(x[i][1]);
       const uint64_t key = x[i][0] == NONE ? 0 : static_cast<uint64_t>(ordered_u32(x[i][0])) << 32 | ~static_cast<uint32_t>(col), less = key < best ? key : best;
       best = key < best ? best : key;
       if (less != 0) total.add_logit(from_ordered(static_cast<uint32_t>(less >> 32)), c1);
     }
   }
-  const uint64_t top_key = group_most<MOE_WAVE>(best);
+  uint64_t top_key = group_most<MOE_WAVE>(best);
+  if constexpr (FEW) {
+    if (lane == 0) tops[wave] = top_key;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top_key = tops[w] > top_key ? tops[w] : top_key;
+  }
   if (best != top_key && best != 0) total.add_logit(from_ordered(static_cast<uint32_t>(best >> 32)), c1);
   total.raise(group_max<MOE_WAVE>(total.e));
   total.sum = group_sum<MOE_WAVE>(total.sum);
   total.moment = group_sum<MOE_WAVE>(total.moment);
+  if constexpr (FEW) {
+    if (lane == 0) { parts[wave][0] = total.e; parts[wave][1] = total.sum; parts[wave][2] = total.moment; }
+    __syncthreads();
+    if (wave != 0) return;
+    total = ScoreSum{};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) total.e = fmaxf(total.e, parts[w][0]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) total.add(parts[w][0], parts[w][1], parts[w][2]);
+  }
   const int top_col = top_key != 0 ? static_cast<int>(~__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(top_key))) : y;
   const int col[2] = {top_col, y};
   double z[2];
@@ -378,7 +397,8 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
 template <int HALF> void launch_join(const ScoreJoinArgs& a, hipStream_t s) {
   const auto rows = [](int n) { return dim3(n < SCORE_ROW ? n : SCORE_ROW, (n + SCORE_ROW - 1) / SCORE_ROW); };
   if (a.K == 0) {
-    MOE_LAUNCH("head_score", (head_score_kernel<HALF>), rows((a.T + 3) / 4), dim3(256), 0, s, a);
+    if (a.T <= SCORE_FEW) MOE_LAUNCH("head_score", (head_score_kernel<HALF, true>), dim3(a.T), dim3(256), 0, s, a);
+    else MOE_LAUNCH("head_score", (head_score_kernel<HALF, false>), rows((a.T + 3) / 4), dim3(256), 0, s, a);
     return;
   }
   const int lds = (score_wanted(a.K) * (HALF / 4) + 1) * 12;
