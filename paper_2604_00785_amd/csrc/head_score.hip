@@ -202,6 +202,7 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
   __shared__ uint32_t found_next[SCORE_CANDIDATES], chosen_next[score_wanted(SCORE_MAX_K)];
   __shared__ float part[WAVES][3];
   __shared__ int s_found, s_columns, s_top_at;
+  __shared__ uint32_t s_border;
   constexpr uint32_t LOW = HALF / 4 - 1;
   constexpr uint32_t LEAST = 0x00800000u;                                 // the order of the lowest number
   const int tid = threadIdx.x, lane = tid % MOE_WAVE, wave = tid / MOE_WAVE, lq = tid & 3, K = a.K, wanted = score_wanted(K);
@@ -267,7 +268,7 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
       if (less != 0) total.add_logit(from_ordered(static_cast<uint32_t>(less >> 32)), c1);
     }
   }
-  if (tid == 0) { s_top = s_least = 0; s_found = s_columns = 0; s_top_at = 0; }
+  if (tid == 0) { s_top = s_least = 0; s_found = s_columns = 0; s_top_at = 0; s_border = 0; }
   {
     // The largest of every few threads, and of these the one that `wanted` - 1 are above: no smaller logit is among the `wanted` largest.
     const bool coarse = wanted <= 32;                                     // 64 groups are enough
@@ -343,13 +344,23 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
       }
     }
     __syncthreads();
-    // the columns to look at: those, and all of a lane whose second largest may be among the `wanted` largest
-    const uint32_t border = n == wanted ? static_cast<uint32_t>(chosen[n - 1] >> 32) : 0;
+    // No logit below the `wanted`-th of the largest and second largest of these lanes is among the `wanted` largest of all.  The columns to look at: the lanes' largest down
+    // to that, and all of a lane whose second largest may be as large (it is known but for its low bits).
+    const auto value = [&](int i) __attribute__((always_inline)) { return i < n ? static_cast<uint32_t>(chosen[i] >> 32) : chosen_next[i - n] & ~LOW; };
+    uint32_t border = n == wanted ? value(n - 1) : 0;
+    // (Finding it costs as much as looking at one lane more: where there are few lanes.)
+    if (__syncthreads_count(tid < n && chosen_next[tid] >= LEAST && chosen_next[tid] >= border) > 1) {
+      ranked<THREADS>(2 * n, [&](int k, int i) __attribute__((always_inline)) { return value(k) > value(i) || (value(k) == value(i) && k < i); },
+                      [&](int i, int above) __attribute__((always_inline)) { if (above == wanted - 1) s_border = value(i); });
+      __syncthreads();
+      border = s_border > border ? s_border : border;
+    }
     for (int i = tid; i < n * (HALF / 4); i += THREADS) {
       const int which = i / (HALF / 4), place = i % (HALF / 4), own = static_cast<int>(~static_cast<uint32_t>(chosen[which]));
       const int col = own / HALF * HALF + 16 * (place >> 2) + (own & 12) + (place & 3);
       const uint32_t next = chosen_next[which];
-      if (col == own || (next >= LEAST && next >= border && col < a.V)) {
+      const bool all_of_it = next >= LEAST && next >= border;
+      if (col == own ? own == top_col || static_cast<uint32_t>(chosen[which] >> 32) >= border : all_of_it && col < a.V) {
         const int at = atomicAdd(&s_columns, 1);
         columns[at] = col;
         if (col == top_col) s_top_at = at;
