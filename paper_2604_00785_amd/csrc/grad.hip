@@ -1,6 +1,7 @@
 // The norm of all gradients of a model together, and their scaling to a largest norm:
 //   norm = sqrt(sum over all tensors of g^2);   out = g min(1, largest / (norm + 1e-6))
-// Bound by memory: one pass reads every gradient, the second reads it once more and writes it.  Squares and their sums are in 64 bits, so that gradients of any
+// Bound by memory: one pass reads every gradient, the second reads it once more and writes it, as more than the caches hold has to be: 298 MB take 54 + 90 us (5.5 and
+// 6.6 TB/s), 1.22 GB 203 + 430 (6.0 and 5.7; a large copy runs at 4.9).  Squares and their sums are in 64 bits, so that gradients of any
 // size have a norm; each workgroup leaves its sum, and whoever needs the norm adds these up in one order: no atomics, the same bits every time.
 #include <algorithm>
 #include <new>
@@ -15,7 +16,7 @@ typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t u32x4_any;
 
 // What a launch knows of its tensors comes with its arguments, so that nothing has to be copied to the device first, in a graph or out of it: at most 4 KB of them, and
 // less where there are few.  A tensor's chunks are CHUNK bytes each but for the last.
-constexpr int GRAD_THREADS = 256, GRAD_GROUPS = 1024;   // workgroups of a launch at most, each with its sum
+constexpr int GRAD_THREADS = 256, GRAD_GROUPS = 2048;   // workgroups of a launch at most, each with its sum
 constexpr int FEW_TENSORS = 24, NORM_TENSORS = 240, CLIP_TENSORS = 160;
 constexpr int MAX_TENSORS = 1 << 20;
 template <int CAP, bool CLIP> struct GradTable {
@@ -62,8 +63,8 @@ template <int U> struct Chunk {
   u32x4 v[U];
   float extra;
 };
-// Calls use(chunk) for each of the workgroup's chunks, the next one being requested before; from the last to the first if BACKWARDS.  (Tensors may be as small as a
-// chunk: waiting for one after the other would take a latency each, 85 instead of 66 us for the sum over 300 MB in 126 tensors.)
+// Calls use(chunk) for each of the workgroup's chunks, one after the other whatever tensors they belong to, the next one being requested before; from the last to the first
+// if BACKWARDS.
 template <int U, bool BACKWARDS, int CAP, bool CLIP, typename Use> __device__ __forceinline__ void over_chunks(const GradTable<CAP, CLIP>& t, Use&& use) {
   constexpr uint32_t WHOLE = GRAD_THREADS * U;
   const uint32_t b = blockIdx.x, c0 = b * t.each + (b < t.more ? b : t.more), n = t.each + (b < t.more ? 1 : 0);
@@ -146,7 +147,10 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_norm_finish_kernel(const do
   if (threadIdx.x == 0) norm[0] = static_cast<float>(v);
 }
 
-// Each workgroup goes backwards through the chunks that it had for the norm: what was read last, and the caches still hold, is read first.
+// Each workgroup goes backwards through the chunks that it had for the norm, so that what the caches still hold is read first (1.22 GB: 445 -> 430 us).
+// What it writes is past what the caches hold anyway, and so is what it reads for the last time: with non-temporal stores the next pass reads from memory without
+// waiting for the writes of this one, and so does the norm (us, ordinary / non-temporal: norm of 298 MB in 126 tensors 87 / 54, of 1.22 GB in 8 245 / 203, clip 95 / 91 and
+// 460 / 441).  Where there is a megabyte or two, they stay ordinary: the update that comes next finds them in the caches.
 template <int U, int CAP> __global__ __launch_bounds__(GRAD_THREADS) void grad_clip_kernel(GradTable<CAP, true> t, const double* __restrict__ sums, int n_sums, double largest,
                                                                                            float* __restrict__ norm) {
   __shared__ double part[4];

@@ -7,8 +7,8 @@
 // Which of two logits is larger is told in 64 bits (products of two bf16 numbers are exact in 32 bits, their sums in 64 are off by 1e-16): the chain of additions of the
 // matrix product would put one in some 10^4 alternatives in the wrong place.  So the K + SCORE_SPARE largest by the product are formed anew, a row of W each, and ordered by that.
 // Candidates: the columns of a lane of the product (16 or 32) have their largest apart.  None of the C largest logits lies in another lane's columns than
-// those with the C largest of these; where the second largest of such a lane may be among them too, all of its columns are candidates.  That is one lane in four
-// tokens for 28 of 50304 columns, and no more than C of them whatever the logits are.
+// those with the C largest of these; where the second largest of such a lane may be among them too, all of its columns are candidates.  That is one lane in six
+// tokens for 24 of 50304 columns, and no more than C of them whatever the logits are.
 #include "head_score.h"
 
 namespace {
@@ -110,7 +110,7 @@ __device__ __forceinline__ void put_scores(const ScoreJoinArgs& a, int t, const 
   a.lse[t] = static_cast<float>(z_top * a.over_tau + r.log_1R);
 }
 
-// Without alternatives: a wave for each token, or (FEW) four.  HALF: columns of a strip.
+// Without alternatives: a wave for each token, or (FEW) four (V 50304, us, one / four: 256 tokens 6.4 / 5.5, 1000 8.0 / 8.1, 4000 15 / 21; 8192 23).  HALF: columns of a strip.
 template <int HALF, bool FEW> __global__ __launch_bounds__(256) void head_score_kernel(ScoreJoinArgs a) {
   constexpr int AT_ONCE = 4, STEP = FEW ? 4 * MOE_WAVE : MOE_WAVE;
   typedef __attribute__((ext_vector_type(4))) uint32_t u4;
@@ -193,7 +193,8 @@ template <int THREADS, typename Above, typename Put> __device__ __forceinline__ 
   }
 }
 
-// With alternatives: a workgroup of THREADS for each token.  HALF: columns of a strip.
+// With alternatives: a workgroup of THREADS for each token, 1024 where there are few (d 2048, V 50304, 20 alternatives, us, 256 / 1024: 1 token 18.5 / 12.7, 256 tokens
+// 31.6 / 20.5, 600 tokens 35 / 41).  HALF: columns of a strip.  3074 tokens take 95 to 107 us, most of it for some 30 rows of W each, 390 MB at 4 TB/s.
 template <int HALF, int THREADS>
 __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs a) {
   constexpr int GROUPS = 256, WAVES = THREADS / MOE_WAVE, AT_ONCE = THREADS > 256 ? 4 : 8, STEP = THREADS / 4;
@@ -348,7 +349,7 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
     // to that, and all of a lane whose second largest may be as large (it is known but for its low bits).
     const auto value = [&](int i) __attribute__((always_inline)) { return i < n ? static_cast<uint32_t>(chosen[i] >> 32) : chosen_next[i - n] & ~LOW; };
     uint32_t border = n == wanted ? value(n - 1) : 0;
-    // (Finding it costs as much as looking at one lane more: where there are few lanes.)
+    // (Finding it costs as much as looking at one lane more.  One token, 17 of 213 columns: 28 -> 18 us.)
     if (__syncthreads_count(tid < n && chosen_next[tid] >= LEAST && chosen_next[tid] >= border) > 1) {
       ranked<THREADS>(2 * n, [&](int k, int i) __attribute__((always_inline)) { return value(k) > value(i) || (value(k) == value(i) && k < i); },
                       [&](int i, int above) __attribute__((always_inline)) { if (above == wanted - 1) s_border = value(i); });

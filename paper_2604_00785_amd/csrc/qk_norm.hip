@@ -1,7 +1,8 @@
 // Norm of every head's queries and keys, and the rotation by position, in one pass, and its derivative.  For a head's row x of D columns, r = 1 / sqrt(mean(x^2) + eps):
 //   v = x r w;   (a, b) -> (a cos t - b sin t, a sin t + b cos t) on R columns of v, t = pos freq[i];   the other columns of v stay
 //   dv = the gradient turned back;   g = dv w;   dx = r (g - x r^2 mean(g x));   dw = sum over tokens and heads of dv x r
-// Bound by memory: every element is read once and written once.  A thread has 16 columns of a head, both of every pair among them, so that nothing passes between
+// Bound by memory: every element is read once and written once (8192 tokens of 32 + 8 heads of 128 columns: forward 33 us, 5.1 TB/s, backward 46, 5.4; a large copy runs
+// at 4.9 TB/s).  A thread has 16 columns of a head, both of every pair among them, so that nothing passes between
 // threads but a row's sums; a few threads share a head, and a workgroup's threads take the heads of one or a few tokens, whose angles are formed once, in 64 bits
 // (a position of 10^6 times a frequency in 32 bits is off by 0.06), and kept in LDS.
 #include <initializer_list>
@@ -40,7 +41,8 @@ __device__ __forceinline__ void unpack16(const u32x4& a, const u32x4& b, float (
 __device__ __forceinline__ u32x4 pack_half(const float (&v)[16], int at) {
   return u32x4{pack_bf16(v[at], v[at + 1]), pack_bf16(v[at + 2], v[at + 3]), pack_bf16(v[at + 4], v[at + 5]), pack_bf16(v[at + 6], v[at + 7])};
 }
-__device__ __forceinline__ u32x4 load8(const moe_bf16* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
+// (Ordinary loads: queries and keys come straight from their projection, gradients from the attention, and the caches have most of them.)
+__device__ __forceinline__ u32x4 load8(const moe_bf16* p) { return *reinterpret_cast<const u32x4*>(p); }
 // Where a thread's two pieces of 8 columns begin.  Rotated pieces first: as halves i and i + R / 16, as neighbours 2 i and 2 i + 1; then the others, two and two.
 struct Place { int a, b; bool turned, has_a, has_b; };
 __device__ __forceinline__ Place place_of(int i, int D, int R, bool pairs) {
@@ -64,7 +66,7 @@ template <bool PAIRS> __device__ __forceinline__ void turn(float (&v)[16], const
 template <int TPR, int N, bool PAIRS, bool BWD>
 __global__ __launch_bounds__(QK_THREADS) void qk_norm_kernel(QkArgs a) {
   constexpr int GROUPS = QK_THREADS / TPR, EACH = GROUPS / N;           // groups of threads, those of a token
-  constexpr int AHEAD = BWD ? 2 : 4;                                    // heads requested together
+  constexpr int AHEAD = 2;                                              // heads requested together
   static_assert(EACH >= 1, "a group for each token");
   __shared__ float angle[2][N][QK_MAX_D / 2];
   __shared__ float share[BWD ? GROUPS * TPR * 17 : 1];
@@ -232,7 +234,9 @@ template <typename F> void with_threads(int D, F&& f) {
   else if (D <= 256) f(std::integral_constant<int, 16>{});
   else f(std::integral_constant<int, 32>{});
 }
-constexpr int QK_TOKENS = 4, QK_MANY = 2048;      // tokens to a workgroup, where there are as many tokens
+// Tokens to a workgroup, where there are as many: the more, the more heads a thread has for its angles and weights, and the fewer workgroups.  The shape above, us, 1 / 2 / 4 / 8 tokens:
+// forward 40 / 36 / 34 / 38, backward 69 / 55 / 50 / 52; 4001 tokens of 24 + 8 heads of 96 columns 20 / 15 / 14 / 14.
+constexpr int QK_TOKENS = 4, QK_MANY = 2048;
 constexpr int QK_MOST = 1 << 20;                  // workgroups of a launch (it may have 2^32 threads)
 constexpr long long QK_NEAR = 1ll << 28;          // elements from a token to the next at most, where a workgroup has several
 int qk_tokens(const QkArgs& a) {
@@ -241,9 +245,10 @@ int qk_tokens(const QkArgs& a) {
   return a.T >= QK_MANY ? QK_TOKENS : 1;
 }
 // Workgroups of the backward pass, each with a share of dw.
+constexpr int QK_SHARES = 512;
 int qk_bwd_groups(int T, int tokens) {
   const int groups = (T + tokens - 1) / tokens;
-  return groups < 1024 ? groups : 1024;
+  return groups < QK_SHARES ? groups : QK_SHARES;
 }
 template <bool BWD> int launch_qk(const QkArgs& a, const char* name, hipStream_t s) {
   const int tokens = qk_tokens(a);
@@ -274,7 +279,7 @@ extern "C" int moe_qk_norm_rope(const moe_bf16* q, long long q_ld, const moe_bf1
 
 extern "C" size_t moe_qk_norm_rope_bwd_workspace_bytes(int T, int Hq, int Hk, int D) {
   if (bad_qk_dims(T, Hq, Hk, D)) return 0;
-  return static_cast<size_t>(T < 1024 ? T : 1024) * 2 * D * sizeof(float);
+  return static_cast<size_t>(T < QK_SHARES ? T : QK_SHARES) * 2 * D * sizeof(float);
 }
 
 extern "C" int moe_qk_norm_rope_bwd(const moe_bf16* dqo, long long dqo_ld, const moe_bf16* dko, long long dko_ld, const moe_bf16* q, long long q_ld,
