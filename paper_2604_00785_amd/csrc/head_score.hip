@@ -9,6 +9,7 @@
 // Candidates: the columns of a lane of the product (16 or 32) have their largest apart.  None of the C largest logits lies in another lane's columns than
 // those with the C largest of these; where the second largest of such a lane may be among them too, all of its columns are candidates.  That is one lane in six
 // tokens for 24 of 50304 columns, and no more than C of them whatever the logits are.
+#include <type_traits>
 #include "head_score.h"
 
 namespace {
@@ -38,21 +39,22 @@ struct ScoreSum {
   }
 };
 
-// Logits of N columns in 64 bits, by a wave; AHEAD pieces of each row requested together.
-template <int N, int AHEAD> __device__ __forceinline__ void exact_logits(const moe_bf16* x, const moe_bf16* W, int d, const int (&col)[N], double (&z)[N]) {
+// Logits of N columns in 64 bits by each LANES lanes of a wave; AHEAD pieces of each row requested together.
+template <int LANES, int N, int AHEAD>
+__device__ __forceinline__ void exact_logits(const moe_bf16* x, const moe_bf16* W, int d, const int (&col)[N], double (&z)[N]) {
   typedef __attribute__((ext_vector_type(4))) uint32_t u4;
-  constexpr int STEP = MOE_WAVE * 8;
-  const int lane = threadIdx.x % MOE_WAVE;
+  constexpr int STEP = LANES * 8;
+  const moe_bf16* row[N];
 #pragma unroll
-  for (int k = 0; k < N; ++k) z[k] = 0.0;
-  for (int c0 = lane * 8; c0 < d; c0 += AHEAD * STEP) {
+  for (int k = 0; k < N; ++k) { z[k] = 0.0; row[k] = W + static_cast<size_t>(col[k]) * d; }
+  for (int c0 = threadIdx.x % LANES * 8; c0 < d; c0 += AHEAD * STEP) {
     u4 p[AHEAD], w[AHEAD][N];
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       const int c = c0 + u * STEP < d ? c0 + u * STEP : c0;
       p[u] = *reinterpret_cast<const u4*>(x + c);
 #pragma unroll
-      for (int k = 0; k < N; ++k) w[u][k] = *reinterpret_cast<const u4*>(W + static_cast<size_t>(col[k]) * d + c);
+      for (int k = 0; k < N; ++k) w[u][k] = *reinterpret_cast<const u4*>(row[k] + c);
     }
     asm volatile("" ::: "memory");
 #pragma unroll
@@ -70,9 +72,18 @@ template <int N, int AHEAD> __device__ __forceinline__ void exact_logits(const m
     }
   }
 #pragma unroll
-  for (int k = 0; k < N; ++k)
+  for (int k = 0; k < N; ++k) {
+    const auto from = [&](auto ctrl) __attribute__((always_inline)) {
+      const uint64_t b = __builtin_bit_cast(uint64_t, z[k]);
+      return __builtin_bit_cast(double, static_cast<uint64_t>(dpp_u32<decltype(ctrl)::value>(static_cast<uint32_t>(b >> 32))) << 32 | dpp_u32<decltype(ctrl)::value>(static_cast<uint32_t>(b)));
+    };
+    z[k] += from(std::integral_constant<int, 0xB1>{});                     // (the steps of group_reduce)
+    z[k] += from(std::integral_constant<int, 0x4E>{});
+    z[k] += from(std::integral_constant<int, 0x141>{});
+    z[k] += from(std::integral_constant<int, 0x140>{});
 #pragma unroll
-    for (int i = 1; i < MOE_WAVE; i *= 2) z[k] += __shfl_xor(z[k], i);
+    for (int i = 16; i < LANES; i *= 2) z[k] += __shfl_xor(z[k], i);
+  }
 }
 __device__ __forceinline__ int64_t ordered_i64(double v) {
   const int64_t b = __builtin_bit_cast(int64_t, v == 0.0 ? 0.0 : v);          // (-0 and +0 are equal)
@@ -178,7 +189,7 @@ template <int HALF, bool FEW> __global__ __launch_bounds__(256) void head_score_
   const int top_col = top_key != 0 ? static_cast<int>(~__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(top_key))) : y;
   const int col[2] = {top_col, y};
   double z[2];
-  exact_logits<2, 4>(a.x + static_cast<size_t>(t) * a.d, a.W, a.d, col, z);
+  exact_logits<MOE_WAVE, 2, 4>(a.x + static_cast<size_t>(t) * a.d, a.W, a.d, col, z);
   if (lane == 0) put_scores(a, t, result_of(total, top_key != 0, z[0], c1), y == top_col, z[1], z[0]);
 }
 
@@ -372,17 +383,25 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
     if (tid == 0) columns[m] = y;
     __syncthreads();
   }
-  constexpr int N = THREADS > 256 ? 2 : 4, AHEAD = N == 2 ? 4 : 2;
-  for (int i = wave * N; i <= m; i += WAVES * N) {
-    int col[N];
-    double z[N];
+  // Sixteen lanes take a row of W, or, where there are few tokens and long rows, a wave: one latency then instead of several.
+  const moe_bf16* const x_row = a.x + static_cast<size_t>(t) * a.d;
+  const auto form = [&](auto lanes, auto at_once, auto ahead) __attribute__((always_inline)) {
+    constexpr int LANES = decltype(lanes)::value, N = decltype(at_once)::value, SETS = THREADS / LANES;
+    const int set = tid / LANES;
+    for (int i = 0; i + wave * (MOE_WAVE / LANES) <= m; i += SETS * N) {
+      int col[N];
+      double z[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) col[k] = __builtin_amdgcn_readfirstlane(columns[i + k <= m ? i + k : m]);
-    exact_logits<N, AHEAD>(a.x + static_cast<size_t>(t) * a.d, a.W, a.d, col, z);
+      for (int k = 0; k < N; ++k) col[k] = columns[i + k * SETS + set < m ? i + k * SETS + set : m];
+      exact_logits<LANES, N, decltype(ahead)::value>(x_row, a.W, a.d, col, z);
 #pragma unroll
-    for (int k = 0; k < N; ++k)
-      if (lane == 0 && i + k <= m) exact[i + k] = z[k];
-  }
+      for (int k = 0; k < N; ++k)
+        if (tid % LANES == 0 && i + k * SETS + set <= m) exact[i + k * SETS + set] = z[k];
+    }
+  };
+  constexpr bool FEW = THREADS > 256;
+  if (FEW && a.d > 512) form(std::integral_constant<int, MOE_WAVE>{}, std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
+  else form(std::integral_constant<int, 16>{}, std::integral_constant<int, FEW ? 1 : 2>{}, std::integral_constant<int, 4>{});
   __syncthreads();
   ScoreSum all;
 #pragma unroll
