@@ -150,7 +150,7 @@ struct GemmArgs {
 // by strips of 64 columns.
 struct HeadItem { uint32_t at, slot; };   // at: row in the block | column << 4
 struct HeadArgs {
-  float* part;                // HEAD_TOP: HeadStrip, or (two 0) HeadBest, [row][strips of HALF columns].  HEAD_STATS: [row block][strips of HALF columns][2 or (two) 3][16 rows]: maximum, sum and sum at the temperature, without the items
+  float* part;                // HEAD_TOP: HeadStrip, or (two 0) HeadBest, [row][strips of HALF columns], or (two 2) the logits, [row][slots].  HEAD_STATS: [row block][strips of HALF columns][2 or (two) 3][16 rows]: maximum, sum and sum at the temperature, without the items
   const f32x4_t* row;         // HEAD_DZ: per row log2(e) lse, factor, and the same at the temperature.  HEAD_SCORE_DZ: l, u, v of 2^t (u + v t), t = c1 z - l
   const int32_t* target;      // [row]
   const int32_t* list_start;  // [row block][list_ld]: first item of each strip; null: no teacher
@@ -1596,6 +1596,15 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
           if (i * 16 >= rows || left <= 0) return;
           f32x4_t v[NB];
           static_for<NB>([&](auto j) { v[decltype(j)::value] = accq(i_tag, j); });
+          if (he->two == 2) {
+            float* const o = he->part + static_cast<size_t>(grow0 + i * 16 + l16) * he->slots + gcol0 + 4 * lq;
+            if (i * 16 + l16 < rows) {
+              static_for<NB>([&](auto j) {
+                if (16 * decltype(j)::value + 4 * lq < left) *reinterpret_cast<f32x4_t*>(o + 16 * decltype(j)::value) = v[decltype(j)::value];
+              });
+            }
+            return;
+          }
           mask(v, NONE);
           // One element after the other meets the largest so far: the smaller of the two takes its place among the others.  (These maxima and minima pass NaN on.)
           float m = v[0][0];

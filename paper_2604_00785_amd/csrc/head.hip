@@ -838,7 +838,9 @@ int run_head_fwd(const HeadCall& c, int* edges) {
   return moe_check_launch();
 }
 
-size_t score_part_bytes(int T, int V) { return static_cast<size_t>((V + 63) / 64) * ((T + 15) & ~15) * sizeof(HeadStrip); }
+size_t score_part_bytes(int T, int d, int V, int K) {
+  return static_cast<size_t>((T + 15) & ~15) * (score_whole(d, V, K) ? score_ld(V) * sizeof(float) : static_cast<size_t>((V + 63) / 64) * sizeof(HeadStrip));
+}
 int run_score_fwd(const HeadCall& c, int* edges) {
   const HeadLayout l = head_layout(c.T, c.d, c.V, 0, false);
   GemmArgs a{};
@@ -854,7 +856,8 @@ int run_score_fwd(const HeadCall& c, int* edges) {
   }
   const int edge = settle_edge(edges, logits_edge(c.T, c.V, c.d, 9.5));
   h.strips = ceil_div(c.V, edge / 2);
-  h.two = c.K > 0;
+  h.two = c.K == 0 ? 0 : score_whole(c.d, c.V, c.K) ? 2 : 1;
+  h.slots = score_ld(c.V);
   h.part = reinterpret_cast<float*>(c.ws + l.big);
   if ((rc = launch_logits<HEAD_TOP>(a, h, edge, c.T, "gemm_head_top", c.s)) != MOE_OK) return rc;
   const ScoreJoinArgs j{h.part, all ? nullptr : reinterpret_cast<const int32_t*>(c.ws + l.control),
@@ -1003,7 +1006,7 @@ bool bad_score(int T, int d, int V, int K) { return bad_head_dims(T, d, V, 0) ||
 }  // namespace
 extern "C" size_t moe_head_score_fwd_workspace_bytes(int T, int d, int V, int K) {
   if (bad_score(T, d, V, K)) return 0;
-  return head_layout(T, d, V, 0, false).big + score_part_bytes(T, V);
+  return head_layout(T, d, V, 0, false).big + score_part_bytes(T, d, V, K);
 }
 extern "C" size_t moe_head_score_bwd_workspace_bytes(int T, int d, int V, int v_piece) { return moe_head_bwd_workspace_bytes(T, d, V, 0, v_piece); }
 

@@ -204,6 +204,158 @@ template <int THREADS, typename Above, typename Put> __device__ __forceinline__ 
   }
 }
 
+// The logits of columns[0 .. m], in 64 bits.  Sixteen lanes take a row of W, or, where there are few tokens and long rows, a wave: one latency then instead of several.
+template <int THREADS> __device__ __forceinline__ void form_exact(const moe_bf16* x, const moe_bf16* W, int d, const int32_t* columns, double* exact, int m) {
+  const int tid = threadIdx.x, wave = tid / MOE_WAVE;
+  const auto form = [&](auto lanes, auto at_once, auto ahead) __attribute__((always_inline)) {
+    constexpr int LANES = decltype(lanes)::value, N = decltype(at_once)::value, SETS = THREADS / LANES;
+    const int set = tid / LANES;
+    for (int i = 0; i + wave * (MOE_WAVE / LANES) <= m; i += SETS * N) {
+      int col[N];
+      double z[N];
+#pragma unroll
+      for (int k = 0; k < N; ++k) col[k] = columns[i + k * SETS + set < m ? i + k * SETS + set : m];
+      exact_logits<LANES, N, decltype(ahead)::value>(x, W, d, col, z);
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (tid % LANES == 0 && i + k * SETS + set <= m) exact[i + k * SETS + set] = z[k];
+    }
+  };
+  constexpr bool FEW = THREADS > 256;
+  if (FEW && d > 512) form(std::integral_constant<int, MOE_WAVE>{}, std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
+  else form(std::integral_constant<int, 16>{}, std::integral_constant<int, FEW ? 1 : 2>{}, std::integral_constant<int, 4>{});
+}
+// The K largest of m of these, in the order of their logits, of equal ones the lower column first.
+template <int THREADS>
+__device__ __forceinline__ void put_alternatives(const ScoreJoinArgs& a, int t, const ScoreResult& r, const int32_t* columns, const double* exact, int m, int top_col, double z_top) {
+  const size_t out = static_cast<size_t>(t) * a.K;
+  for (int k = m + threadIdx.x; k < a.K; k += THREADS) {                   // (logits of -infinity)
+    a.ids[out + k] = -1;
+    a.top[out + k] = __builtin_nanf("");
+  }
+  ranked<THREADS>(m, [&](int k, int i) __attribute__((always_inline)) {
+    const int64_t one = ordered_i64(exact[k]), two = ordered_i64(exact[i]);
+    return one > two || (one == two && columns[k] < columns[i]);
+  }, [&](int i, int above) __attribute__((always_inline)) {
+    if (above >= a.K) return;
+    a.ids[out + above] = columns[i];
+    a.top[out + above] = columns[i] == top_col ? -static_cast<float>(r.log_1R) : static_cast<float>((exact[i] - z_top) * a.over_tau - r.log_1R);
+  });
+}
+
+// With alternatives, from the logits themselves: a thread has PIECES times four of them in registers.
+template <int THREADS, int PIECES> __global__ __launch_bounds__(THREADS) void head_score_whole_kernel(ScoreJoinArgs a) {
+  // Groups of threads have 4, 8 or 16 columns side by side, and there are at least as many groups as logits are wanted; where fewer of them have any, all columns are candidates.
+  constexpr int WAVES = THREADS / MOE_WAVE, SIZE = THREADS == 64 ? 1 : THREADS == 256 ? 2 : 4, GROUPS = THREADS / SIZE, WANTED = score_wanted(SCORE_MAX_K);
+  constexpr int CANDIDATES = WANTED * SIZE * 4;
+  __shared__ uint64_t keys[GROUPS], found[CANDIDATES], s_top, s_least;
+  __shared__ double exact[WANTED + 1];
+  __shared__ int32_t columns[WANTED + 1];
+  __shared__ float part[WAVES][2];
+  __shared__ int s_found;
+  const int tid = threadIdx.x, lane = tid % MOE_WAVE, wave = tid / MOE_WAVE, K = a.K, wanted = score_wanted(K);
+  const int t = blockIdx.y * SCORE_ROW + blockIdx.x;
+  if (t >= a.T) return;
+  const int y = a.target[t];
+  if (y < 0 || y >= a.V) {
+    if (tid == 0) { a.logp[t] = 0.f; a.entropy[t] = 0.f; a.lse[t] = 0.f; }
+    for (int k = tid; k < K; k += THREADS) { a.ids[static_cast<size_t>(t) * K + k] = -1; a.top[static_cast<size_t>(t) * K + k] = 0.f; }
+    return;
+  }
+  const int row = a.control != nullptr ? a.token_row[t] : t, ld = score_ld(a.V);
+  const float* const z_row = static_cast<const float*>(a.part) + static_cast<size_t>(row) * ld;
+  const float c1 = a.c1;
+  float z[PIECES][4];
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    const int c = (p * THREADS + tid) * 4;
+    f32x4_t v = {};
+    if (c < ld) v = *reinterpret_cast<const f32x4_t*>(z_row + c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[p][i] = c + i < a.V ? v[i] : -__builtin_inff();
+  }
+  // (as in the other kernel; of 0 and -0 either may be called the larger, the order in 64 bits knows no difference)
+  const auto key_of = [&](int p, int i) __attribute__((always_inline)) -> uint64_t {
+    const uint32_t bits = __float_as_uint(z[p][i]);
+    return bits == NONE ? 0 : static_cast<uint64_t>(ordered_u32(bits)) << 32 | ~static_cast<uint32_t>((p * THREADS + tid) * 4 + i);
+  };
+  uint64_t best = 0;
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { const uint64_t k = key_of(p, i); best = k > best ? k : best; }
+  if (tid == 0) { s_top = s_least = 0; s_found = 0; }
+  const uint64_t of_group = group_most<SIZE>(best);
+  if (tid % SIZE == 0) keys[tid / SIZE] = of_group;
+  __syncthreads();
+  ranked<THREADS>(GROUPS, [&](int k, int i) __attribute__((always_inline)) { return keys[k] > keys[i]; }, [&](int i, int above) __attribute__((always_inline)) {
+    if (above == 0 && keys[i] != 0) s_top = keys[i];
+    if (above == wanted - 1 && keys[i] != 0) s_least = keys[i];
+  });
+  __syncthreads();
+  const uint64_t top_key = s_top, least = s_least;
+  const int top_col = static_cast<int>(~static_cast<uint32_t>(top_key));
+  const float most = from_ordered(static_cast<uint32_t>(top_key >> 32)), e = ceilf(most * c1);
+  float sum = 0.f, moment = 0.f;
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int col = (p * THREADS + tid) * 4 + i;
+      const float x = __builtin_elementwise_maximum(__builtin_fmaf(z[p][i], c1, -e), -1000.f), s = col == top_col ? 0.f : __builtin_amdgcn_exp2f(x);
+      sum += s;
+      moment = __builtin_fmaf(s, x, moment);
+      const uint64_t key = key_of(p, i);
+      if (key >= least && key != 0) {
+        const int at = atomicAdd(&s_found, 1);
+        if (at < CANDIDATES) found[at] = key;
+      }
+    }
+  sum = group_sum<MOE_WAVE>(sum);
+  moment = group_sum<MOE_WAVE>(moment);
+  if (lane == 0) { part[wave][0] = sum; part[wave][1] = moment; }
+  __syncthreads();
+  int m = s_found;
+  if (m <= CANDIDATES) {
+    ranked<THREADS>(m, [&](int k, int i) __attribute__((always_inline)) { return found[k] > found[i]; }, [&](int i, int above) __attribute__((always_inline)) {
+      if (above < wanted) columns[above] = static_cast<int>(~static_cast<uint32_t>(found[i]));
+    });
+    m = m < wanted ? m : wanted;
+  } else {
+    // (large logits in few threads: one after the other)
+    m = 0;
+    for (uint64_t last = ~0ull; m < wanted; ++m) {
+      uint64_t next = 0;
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const uint64_t k = key_of(p, i); next = k < last && k > next ? k : next; }
+      next = group_most<MOE_WAVE>(next);
+      __syncthreads();
+      if (lane == 0) keys[wave] = next;
+      __syncthreads();
+      uint64_t whole = 0;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) whole = keys[w] > whole ? keys[w] : whole;
+      if (whole == 0) break;
+      if (tid == 0) columns[m] = static_cast<int>(~static_cast<uint32_t>(whole));
+      last = whole;
+    }
+  }
+  if (tid == 0) columns[m] = y;
+  __syncthreads();
+  form_exact<THREADS>(a.x + static_cast<size_t>(t) * a.d, a.W, a.d, columns, exact, m);
+  __syncthreads();
+  ScoreSum all;
+  all.e = e;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) { all.sum += part[w][0]; all.moment += part[w][1]; }
+  const double z_top = exact[0];                                           // (columns[0] is top_col)
+  const ScoreResult r = result_of(all, top_key != 0, z_top, c1);
+  if (tid == 0) put_scores(a, t, r, y == top_col, exact[m], z_top);
+  put_alternatives<THREADS>(a, t, r, columns, exact, m, top_col, z_top);
+}
+
 // With alternatives: a workgroup of THREADS for each token, 1024 where there are few (d 2048, V 50304, 20 alternatives, us, 256 / 1024: 1 token 18.5 / 12.7, 256 tokens
 // 31.6 / 20.5, 600 tokens 35 / 41).  HALF: columns of a strip.  3074 tokens take 95 to 107 us, most of it for some 30 rows of W each, 390 MB at 4 TB/s.
 template <int HALF, int THREADS>
@@ -383,25 +535,7 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
     if (tid == 0) columns[m] = y;
     __syncthreads();
   }
-  // Sixteen lanes take a row of W, or, where there are few tokens and long rows, a wave: one latency then instead of several.
-  const moe_bf16* const x_row = a.x + static_cast<size_t>(t) * a.d;
-  const auto form = [&](auto lanes, auto at_once, auto ahead) __attribute__((always_inline)) {
-    constexpr int LANES = decltype(lanes)::value, N = decltype(at_once)::value, SETS = THREADS / LANES;
-    const int set = tid / LANES;
-    for (int i = 0; i + wave * (MOE_WAVE / LANES) <= m; i += SETS * N) {
-      int col[N];
-      double z[N];
-#pragma unroll
-      for (int k = 0; k < N; ++k) col[k] = columns[i + k * SETS + set < m ? i + k * SETS + set : m];
-      exact_logits<LANES, N, decltype(ahead)::value>(x_row, a.W, a.d, col, z);
-#pragma unroll
-      for (int k = 0; k < N; ++k)
-        if (tid % LANES == 0 && i + k * SETS + set <= m) exact[i + k * SETS + set] = z[k];
-    }
-  };
-  constexpr bool FEW = THREADS > 256;
-  if (FEW && a.d > 512) form(std::integral_constant<int, MOE_WAVE>{}, std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
-  else form(std::integral_constant<int, 16>{}, std::integral_constant<int, FEW ? 1 : 2>{}, std::integral_constant<int, 4>{});
+  form_exact<THREADS>(a.x + static_cast<size_t>(t) * a.d, a.W, a.d, columns, exact, m);
   __syncthreads();
   ScoreSum all;
 #pragma unroll
@@ -411,18 +545,7 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
   const double z_top = exact[s_top_at];
   const ScoreResult r = result_of(all, top_key != 0, z_top, c1);
   if (tid == 0) put_scores(a, t, r, y == top_col, exact[m], z_top);
-  for (int k = m + tid; k < K; k += THREADS) {                       // (logits of -infinity)
-    a.ids[static_cast<size_t>(t) * K + k] = -1;
-    a.top[static_cast<size_t>(t) * K + k] = __builtin_nanf("");
-  }
-  ranked<THREADS>(m, [&](int k, int i) __attribute__((always_inline)) {
-    const int64_t one = ordered_i64(exact[k]), two = ordered_i64(exact[i]);
-    return one > two || (one == two && columns[k] < columns[i]);
-  }, [&](int i, int above) __attribute__((always_inline)) {
-    if (above >= K) return;
-    a.ids[static_cast<size_t>(t) * K + above] = columns[i];
-    a.top[static_cast<size_t>(t) * K + above] = columns[i] == top_col ? -static_cast<float>(r.log_1R) : static_cast<float>((exact[i] - z_top) * a.over_tau - r.log_1R);
-  });
+  put_alternatives<THREADS>(a, t, r, columns, exact, m, top_col, z_top);
 }
 
 template <int HALF> void launch_join(const ScoreJoinArgs& a, hipStream_t s) {
@@ -432,6 +555,12 @@ template <int HALF> void launch_join(const ScoreJoinArgs& a, hipStream_t s) {
     else MOE_LAUNCH("head_score", (head_score_kernel<HALF, false>), rows((a.T + 3) / 4), dim3(256), 0, s, a);
     return;
   }
+  if (score_whole(a.d, a.V, a.K)) {
+    if (a.T <= SCORE_FEW) MOE_LAUNCH("head_score_whole", (head_score_whole_kernel<1024, SCORE_WHOLE_V / 4096>), rows(a.T), dim3(1024), 0, s, a);
+    else if (a.V <= SCORE_WHOLE_V / 4 && score_wanted(a.K) <= 64) MOE_LAUNCH("head_score_whole", (head_score_whole_kernel<64, SCORE_WHOLE_V / 1024>), rows(a.T), dim3(64), 0, s, a);
+    else MOE_LAUNCH("head_score_whole", (head_score_whole_kernel<256, SCORE_WHOLE_V / 1024>), rows(a.T), dim3(256), 0, s, a);
+    return;
+  }
   const int lds = (score_wanted(a.K) * (HALF / 4) + 1) * 12;
   const dim3 grid = rows(a.T);
   if (a.T <= SCORE_FEW) MOE_LAUNCH("head_score_join", (head_score_join_kernel<HALF, 1024>), grid, dim3(1024), lds, s, a);
@@ -439,6 +568,8 @@ template <int HALF> void launch_join(const ScoreJoinArgs& a, hipStream_t s) {
 }
 
 }  // namespace
+
+bool score_whole(int, int V, int K) { return K > 0 && V <= SCORE_WHOLE_V; }
 
 int moe_head_score_join(const ScoreJoinArgs& a, int edge, hipStream_t s) {
   if (edge == 128) launch_join<64>(a, s);
