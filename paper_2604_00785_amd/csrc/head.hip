@@ -675,12 +675,12 @@ BwdShape head_bwd_shape(int T, int d, int cols, bool whole) {
 // so narrow rows take 128 (more: what the epilogue of a tile of 256 costs beside that of a plain product, 3.0 at 128; K steps of 1.4 us).  256 / 128 in us,
 // sums (gradient): 3799 tokens, d 256, V 50524 169 / 160 (215 / 191); 1597, 64, 25439 34 / 29 (48 / 37); 3372, 576, 43471 202 / 197 (239 / 217);
 // 1420, 3968, 58453 516 / 728 (541 / 749); 8192, 2048, 50304 1201 / 1535 (1331 / 1736).
-int logits_edge(int rows, int cols, int d, double more) {
+int logits_edge(int rows, int cols, int d, double more, double behind128 = 0.0, double behind256 = 0.0) {
   const auto time = [&](auto edge, double fixed) {
     constexpr int S = decltype(edge)::value;
     return head_time<S>(static_cast<double>(ceil_div(rows, S)) * ceil_div(cols, S), ceil_div(d, BK), fixed);
   };
-  return time(IC<128>{}, TileCost<128>::FIXED + 3.0) < time(IC<256>{}, TileCost<256>::FIXED + more) ? 128 : 256;
+  return time(IC<128>{}, TileCost<128>::FIXED + 3.0) + behind128 < time(IC<256>{}, TileCost<256>::FIXED + more) + behind256 ? 128 : 256;
 }
 
 // What the workspace holds, by offset.
@@ -838,10 +838,28 @@ int run_head_fwd(const HeadCall& c, int* edges) {
   return moe_check_launch();
 }
 
-size_t score_part_bytes(int T, int d, int V, int K) {
-  return static_cast<size_t>((T + 15) & ~15) * (score_whole(d, V, K) ? score_ld(V) * sizeof(float) : static_cast<size_t>((V + 63) / 64) * sizeof(HeadStrip));
+// Whether the product leaves its logits instead of what it makes of them: where vocabularies are small, or so many alternatives are wanted of so few columns that many
+// lanes of the product have two of them, and all of their columns (an eighth of the tile's edge) would have to be looked at.  us, strips / logits: 16000 tokens, d 128, V 2000, 4
+// alternatives 164 / 115, 20 248 / 141, 64 1213 / 287; V 4000 186 / 188, 241 / 219, 966 / 343; V 8000 228 / 335, 269 / 357, 861 / 492; 2000 tokens, d 2048 (tiles of 256),
+// V 8000 106 / 112, 154 / 117, 563 / 173; V 16000 153 / 174, 186 / 192, 453 / 242; 8192, d 512, V 16000 265 / 412, 305 / 434, 904 / 529; 8 tokens, d 1024, V 5010, 20 31 / 26.
+bool score_whole(int T, int d, int V, int K) {
+  if (K <= 0 || V > SCORE_WHOLE_V) return false;
+  const double pairs = 10.0 * score_wanted(K) * (logits_edge(T, V, d, 9.5) / 8);
+  return static_cast<double>(V) * V <= 1.6e7 + pairs * pairs;
 }
-int run_score_fwd(const HeadCall& c, int* edges) {
+// The edge of the tiles that leave strips: with alternatives the columns that are looked at behind the product count too, (wanted columns of a lane)^2 / 2 V a token as pairs
+// go, each a row of W (0.6 us for a thousand of 2048, units of 1.4 us).  256 / 128, us: 3000 tokens, d 512, V 32003, 64 alternatives 369 / 283; 3071, 2048, 50304, 20 591 / 690.
+int score_edge(int T, int d, int V, int K, bool whole) {
+  const auto behind = [&](int columns) {
+    const double pairs = static_cast<double>(score_wanted(K)) * columns;
+    return K == 0 || whole ? 0.0 : T * (pairs * pairs / (2.0 * V)) * (0.12e-3 + 0.00025e-3 * d) / 1.4;
+  };
+  return logits_edge(T, V, d, 9.5, behind(16), behind(32));
+}
+size_t score_part_bytes(int T, int V, bool whole) {
+  return static_cast<size_t>((T + 15) & ~15) * (whole ? score_ld(V) * sizeof(float) : static_cast<size_t>((V + 63) / 64) * sizeof(HeadStrip));
+}
+int run_score_fwd(const HeadCall& c, bool whole, int* edges) {
   const HeadLayout l = head_layout(c.T, c.d, c.V, 0, false);
   GemmArgs a{};
   HeadArgs h{};
@@ -854,14 +872,14 @@ int run_score_fwd(const HeadCall& c, int* edges) {
   } else if ((rc = run_prep(c, l, BwdRule{}, 0)) != MOE_OK) {
     return rc;
   }
-  const int edge = settle_edge(edges, logits_edge(c.T, c.V, c.d, 9.5));
+  const int edge = settle_edge(edges, score_edge(c.T, c.d, c.V, c.K, whole));
   h.strips = ceil_div(c.V, edge / 2);
-  h.two = c.K == 0 ? 0 : score_whole(c.d, c.V, c.K) ? 2 : 1;
+  h.two = c.K == 0 ? 0 : whole ? 2 : 1;
   h.slots = score_ld(c.V);
   h.part = reinterpret_cast<float*>(c.ws + l.big);
   if ((rc = launch_logits<HEAD_TOP>(a, h, edge, c.T, "gemm_head_top", c.s)) != MOE_OK) return rc;
   const ScoreJoinArgs j{h.part, all ? nullptr : reinterpret_cast<const int32_t*>(c.ws + l.control),
-                        reinterpret_cast<const int32_t*>(c.ws + l.token_row), c.target, c.x, c.W, c.T, c.d, c.V, c.K, h.strips, h.c1, 1.0 / c.tau,
+                        reinterpret_cast<const int32_t*>(c.ws + l.token_row), c.target, c.x, c.W, c.T, c.d, c.V, c.K, h.strips, whole, h.c1, 1.0 / c.tau,
                         c.loss, c.entropy, c.lse, c.ids, c.top};
   return moe_head_score_join(j, edge, c.s);
 }
@@ -1000,13 +1018,13 @@ extern "C" int moe_head_distill_bwd(const moe_bf16* x, const moe_bf16* W, const 
   return moe_head_bwd(x, W, target, ids, teacher, temperature, loss, lse, lse_t, dloss, dkd, T, d, V, K, v_piece, dx, dW, ws, ws_bytes, stream, nullptr);
 }
 
-// Log probabilities, entropies and alternatives.  edges, for tests: as above.
+// Log probabilities, entropies and alternatives.  edges, for tests: as above; forward edges[1]: 1 from the logits, 2 from strips, 0 by the rule.
 namespace {
 bool bad_score(int T, int d, int V, int K) { return bad_head_dims(T, d, V, 0) || K < 0 || K > SCORE_MAX_K || K > V; }
 }  // namespace
 extern "C" size_t moe_head_score_fwd_workspace_bytes(int T, int d, int V, int K) {
   if (bad_score(T, d, V, K)) return 0;
-  return head_layout(T, d, V, 0, false).big + score_part_bytes(T, d, V, K);
+  return head_layout(T, d, V, 0, false).big + score_part_bytes(T, V, score_whole(T, d, V, K));
 }
 extern "C" size_t moe_head_score_bwd_workspace_bytes(int T, int d, int V, int v_piece) { return moe_head_bwd_workspace_bytes(T, d, V, 0, v_piece); }
 
@@ -1015,13 +1033,16 @@ extern "C" int moe_head_score_fwd_edges(const moe_bf16* x, const moe_bf16* W, co
                                         int* edges) {
   if (bad_score(T, d, V, K) || bad_temperature(temperature) || bad_edge_list(edges, 1)) return MOE_ERR_INVALID;
   if (bad_ptrs({x, W, target, logp, entropy, lse, ws}) || (K > 0 && bad_ptrs({ids, top}))) return MOE_ERR_INVALID;
-  if (ws_bytes < moe_head_score_fwd_workspace_bytes(T, d, V, K)) return MOE_ERR_WORKSPACE;
+  bool whole = score_whole(T, d, V, K);
+  if (edges != nullptr && edges[1] != 0) whole = edges[1] == 1;
+  if (whole && (K == 0 || V > SCORE_WHOLE_V)) return MOE_ERR_INVALID;
+  if (ws_bytes < head_layout(T, d, V, 0, false).big + score_part_bytes(T, V, whole)) return MOE_ERR_WORKSPACE;
   HeadCall c{};
   c.x = x; c.W = W; c.target = target; c.t.temperature = 1.f; c.T = T; c.d = d; c.V = V;
   c.score = true; c.tau = temperature; c.K = K;
   c.loss = logp; c.entropy = entropy; c.lse = lse; c.ids = ids; c.top = top;
   c.ws = static_cast<char*>(ws); c.s = static_cast<hipStream_t>(stream);
-  return run_score_fwd(c, edges);
+  return run_score_fwd(c, whole, edges);
 }
 extern "C" int moe_head_score_bwd_edges(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, const float* logp,
                                         const float* entropy, const float* lse, const float* dlogp, const float* dentropy, int T, int d, int V, int v_piece,

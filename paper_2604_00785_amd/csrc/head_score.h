@@ -18,7 +18,7 @@ struct ScoreJoinArgs {
   const void* part;                                // HeadStrip, or (K 0) HeadBest [row][strips], or (whole) the logits [row][score_ld(V)]
   const int32_t *control, *token_row, *target;     // control null: rows are tokens
   const moe_bf16 *x, *W;
-  int T, d, V, K, strips;
+  int T, d, V, K, strips, whole;
   float c1;                                        // log2(e) over the temperature
   double over_tau;
   float *logp, *entropy, *lse;
@@ -26,10 +26,7 @@ struct ScoreJoinArgs {
   float* top;
 };
 
-constexpr int SCORE_WHOLE_V = 8192;
-// Whether the product leaves its logits instead of what it makes of them: where so many alternatives are wanted of so few columns that nearly every lane of the product
-// has two of them, and all of its columns would have to be looked at.
-bool score_whole(int d, int V, int K);
+constexpr int SCORE_WHOLE_V = 16384;
 constexpr int score_ld(int V) { return (V + 3) & ~3; }
 // edge: of the tiles that the strips are from (HALF = edge / 2)
 int moe_head_score_join(const ScoreJoinArgs& a, int edge, hipStream_t s);

@@ -245,8 +245,9 @@ __device__ __forceinline__ void put_alternatives(const ScoreJoinArgs& a, int t, 
 
 // With alternatives, from the logits themselves: a thread has PIECES times four of them in registers.
 template <int THREADS, int PIECES> __global__ __launch_bounds__(THREADS) void head_score_whole_kernel(ScoreJoinArgs a) {
-  // Groups of threads have 4, 8 or 16 columns side by side, and there are at least as many groups as logits are wanted; where fewer of them have any, all columns are candidates.
-  constexpr int WAVES = THREADS / MOE_WAVE, SIZE = THREADS == 64 ? 1 : THREADS == 256 ? 2 : 4, GROUPS = THREADS / SIZE, WANTED = score_wanted(SCORE_MAX_K);
+  // Groups of threads have 4, 8 or 16 columns side by side, and there are at least as many groups as logits are wanted; where fewer of them have any, all columns are
+  // candidates.
+  constexpr int WAVES = THREADS / MOE_WAVE, SIZE = THREADS <= 128 ? 1 : THREADS == 256 ? 2 : 4, GROUPS = THREADS / SIZE, WANTED = score_wanted(SCORE_MAX_K);
   constexpr int CANDIDATES = WANTED * SIZE * 4;
   __shared__ uint64_t keys[GROUPS], found[CANDIDATES], s_top, s_least;
   __shared__ double exact[WANTED + 1];
@@ -548,6 +549,19 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
   put_alternatives<THREADS>(a, t, r, columns, exact, m, top_col, z_top);
 }
 
+// Threads for a token whose logits are all looked at: each has 32 of them at most.
+void launch_whole(const ScoreJoinArgs& a, dim3 grid, hipStream_t s) {
+  const auto launch = [&](auto threads, auto pieces) {
+    constexpr int THREADS = decltype(threads)::value, PIECES = decltype(pieces)::value;
+    MOE_LAUNCH("head_score_whole", (head_score_whole_kernel<THREADS, PIECES>), grid, dim3(THREADS), 0, s, a);
+  };
+  using std::integral_constant;
+  if (a.T <= SCORE_FEW) launch(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+  else if (a.V <= 2048 && score_wanted(a.K) <= 64) launch(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+  else if (a.V <= 4096) launch(integral_constant<int, 128>{}, integral_constant<int, 8>{});
+  else if (a.V <= 8192) launch(integral_constant<int, 256>{}, integral_constant<int, 8>{});
+  else launch(integral_constant<int, 512>{}, integral_constant<int, 8>{});
+}
 template <int HALF> void launch_join(const ScoreJoinArgs& a, hipStream_t s) {
   const auto rows = [](int n) { return dim3(n < SCORE_ROW ? n : SCORE_ROW, (n + SCORE_ROW - 1) / SCORE_ROW); };
   if (a.K == 0) {
@@ -555,10 +569,8 @@ template <int HALF> void launch_join(const ScoreJoinArgs& a, hipStream_t s) {
     else MOE_LAUNCH("head_score", (head_score_kernel<HALF, false>), rows((a.T + 3) / 4), dim3(256), 0, s, a);
     return;
   }
-  if (score_whole(a.d, a.V, a.K)) {
-    if (a.T <= SCORE_FEW) MOE_LAUNCH("head_score_whole", (head_score_whole_kernel<1024, SCORE_WHOLE_V / 4096>), rows(a.T), dim3(1024), 0, s, a);
-    else if (a.V <= SCORE_WHOLE_V / 4 && score_wanted(a.K) <= 64) MOE_LAUNCH("head_score_whole", (head_score_whole_kernel<64, SCORE_WHOLE_V / 1024>), rows(a.T), dim3(64), 0, s, a);
-    else MOE_LAUNCH("head_score_whole", (head_score_whole_kernel<256, SCORE_WHOLE_V / 1024>), rows(a.T), dim3(256), 0, s, a);
+  if (a.whole) {
+    launch_whole(a, rows(a.T), s);
     return;
   }
   const int lds = (score_wanted(a.K) * (HALF / 4) + 1) * 12;
@@ -568,8 +580,6 @@ template <int HALF> void launch_join(const ScoreJoinArgs& a, hipStream_t s) {
 }
 
 }  // namespace
-
-bool score_whole(int, int V, int K) { return K > 0 && V <= SCORE_WHOLE_V; }
 
 int moe_head_score_join(const ScoreJoinArgs& a, int edge, hipStream_t s) {
   if (edge == 128) launch_join<64>(a, s);

@@ -28,20 +28,22 @@ def junk(*shape, dtype=torch.float32):
     return torch.full(shape, -77, dtype=dtype, device=DEV) if dtype == torch.int32 else torch.full(shape, float("nan"), dtype=dtype, device=DEV)
 
 
-def forward(x, W, target, K=0, tau=1.0, edge=0):
+def forward(x, W, target, K=0, tau=1.0, edge=0, path=0):
+    """path 1: alternatives from the logits, 2: from strips of them, 0: as the rule has it."""
     x, W, target = x.to(DEV), W.to(DEV), target.to(DEV)
     (T, d), V = x.shape, W.shape[0]
     out = {"logp": junk(T), "entropy": junk(T), "lse": junk(T)}
     ids, top = (junk(T, K, dtype=torch.int32), junk(T, K)) if K else (None, None)
-    ws = torch.full((B.moe_head_score_fwd_workspace_bytes(T, d, V, K),), 255, dtype=torch.uint8, device=DEV)
-    if edge == 0:
+    n = B.moe_head_score_fwd_workspace_bytes(T, d, V, K)
+    ws = torch.full((n if path == 0 else n + (T + 15) * (V + 64) * 4,), 255, dtype=torch.uint8, device=DEV)
+    if edge == 0 and path == 0:
         B.moe_head_score_fwd(x, W, target, tau, out["logp"], out["entropy"], out["lse"], ids, top, ws)
     else:
         p = lambda t: None if t is None else ctypes.c_void_p(t.data_ptr())  # noqa: E731
-        edges = (ctypes.c_int * 1)(edge)
+        edges = (ctypes.c_int * 2)(edge, path)
         rc = B.load().moe_head_score_fwd_edges(p(x), p(W), p(target), ctypes.c_float(tau), T, d, V, K, p(out["logp"]), p(out["entropy"]), p(out["lse"]), p(ids), p(top),
                                                p(ws), ctypes.c_size_t(ws.numel()), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream), edges)
-        assert rc == 0 and edges[0] == edge
+        assert rc == 0 and edge in (0, edges[0])
     if K:
         out.update(ids=ids, top=top)
     return out
@@ -73,7 +75,18 @@ SHAPES = [(1, 64, 1, 1, 1.0), (2, 64, 7, 7, 1.0), (1, 64, 200, 64, 1.3), (1, 204
 def test_forward(T, d, V, K, tau, edge):
     x, W, target, _, _ = inputs(T, d, V, seed=T)
     want, bound = R.score(x, W, target, K, tau)
-    R.check_all(forward(x, W, target, K, tau, edge), want, bound)
+    for path in (0, 1, 2) if 0 < K and V <= 16384 else (0,):
+        R.check_all(forward(x, W, target, K, tau, edge, path), want, bound)
+
+
+@pytest.mark.parametrize("path", [1, 2])
+@pytest.mark.parametrize("T,V,K", [(3, 16384, 64), (300, 16384, 64), (260, 2049, 60), (260, 2048, 61), (260, 2048, 60), (300, 4097, 20), (300, 8193, 3), (300, 70, 64), (3, 70, 64), (3, 1087, 64),
+                                   (257, 543, 64), (257, 255, 60)])
+def test_both_ways_to_the_alternatives(T, V, K, path):
+    """At the borders of what a workgroup, a thread and a list of candidates hold."""
+    x, W, target, _, _ = inputs(T, 64, V, seed=V)
+    want, bound = R.score(x, W, target, K)
+    R.check_all(forward(x, W, target, K, path=path), want, bound)
 
 
 @pytest.mark.parametrize("edge", [128, 256, 0])
@@ -152,8 +165,9 @@ def test_sure_tokens_keep_their_digits(T):
     assert float(((got["entropy"].cpu().double() - want["entropy"]) / want["entropy"]).abs().max()) < 1e-3
 
 
+@pytest.mark.parametrize("path", [1, 2])
 @pytest.mark.parametrize("edge", [128, 256])
-def test_equal_logits(edge):
+def test_equal_logits(edge, path):
     """All equal, some equal, and the lower column first."""
     T, d, V, K = 6, 64, 3001, 64
     x, W, target, _, _ = inputs(T, d, V, masked=0.0, seed=8)
@@ -164,14 +178,15 @@ def test_equal_logits(edge):
     W[2000:2100] = W[100:200]                            # rows twice
     W[2900:] = W[100:201]
     want, bound = R.score(x, W, target, K)
-    got = forward(x, W, target, K, 1.0, edge)
+    got = forward(x, W, target, K, 1.0, edge, path)
     assert want["ids"][0].tolist() == list(range(K)) and want["ids"][1].tolist() == list(range(0, 3 * K, 3))
     R.check_all(got, want, bound)
     assert abs(float(got["entropy"][0]) - math.log(V)) < 1e-5
 
 
+@pytest.mark.parametrize("path", [1, 2])
 @pytest.mark.parametrize("edge", [128, 256])
-def test_the_largest_side_by_side(edge):
+def test_the_largest_side_by_side(edge, path):
     """Alternatives that all lie in the columns of one lane, of neighbouring lanes, of one strip, and at the ends of the vocabulary."""
     d, V, K = 64, 5003, 40
     g = torch.Generator().manual_seed(9)
@@ -183,7 +198,7 @@ def test_the_largest_side_by_side(edge):
         W[columns] = (W[columns].float() + 0.02 * torch.rand(len(columns), 1, generator=g) * x[:1].float() + 0.2 * x[:1].float()).bfloat16()
         target = torch.tensor([int(columns[0]), 0, V - 1, 17]).int()
         want, bound = R.score(x, W, target, K)
-        R.check_all(forward(x, W, target, K, 1.0, edge), want, bound)
+        R.check_all(forward(x, W, target, K, 1.0, edge, path), want, bound)
 
 
 def test_more_candidates_than_there_is_room_for():
@@ -201,6 +216,18 @@ def test_more_candidates_than_there_is_room_for():
         R.check_all(forward(x, W2, target, K, 1.0, edge), want, bound)
 
 
+@pytest.mark.parametrize("T,V,few", [(2, 16384, lambda c: c // 16 % 256 < 2), (300, 2000, lambda c: c // 4 % 64 < 3), (300, 4000, lambda c: c // 4 % 128 < 3),
+                                     (300, 8000, lambda c: c // 8 % 128 < 2), (300, 16384, lambda c: c // 16 % 128 < 2)])
+def test_more_candidates_among_the_logits_themselves(T, V, few):
+    """The same where all logits are looked at: large ones in the columns of few threads, and all equal."""
+    d, K = 64, 60
+    x, W, target, _, _ = inputs(T, d, V, masked=0.0, seed=16)
+    W[few(torch.arange(V))] += (0.05 * x[1].float()).bfloat16()
+    x[0] = 0
+    want, bound = R.score(x, W, target, K)
+    R.check_all(forward(x, W, target, K, path=1), want, bound)
+
+
 def test_nothing_but_masked_tokens():
     for T in (5, 300):
         x, W, target, dlogp, dentropy = inputs(T, 64, 100, seed=11)
@@ -211,20 +238,21 @@ def test_nothing_but_masked_tokens():
         assert bool((g["dx"] == 0).all()) and bool((g["dW"] == 0).all())
 
 
+@pytest.mark.parametrize("path", [0, 2])
 @pytest.mark.parametrize("T", [20, 400])
-def test_what_is_not_a_number_stays_where_it_is(T):
+def test_what_is_not_a_number_stays_where_it_is(T, path):
     x, W, target, dlogp, dentropy = inputs(T, 64, 300, masked=0.0, seed=12)
-    clean = forward(x, W, target, 4)
+    clean = forward(x, W, target, 4, path=path)
     target[3] = -100
     x2, dl2, de2 = x.clone(), dlogp.clone(), dentropy.clone()
     x2[3], dl2[3], de2[3] = float("nan"), float("nan"), float("inf")              # a masked token: leaves no trace
-    want = forward(x, W, target, 4)
-    got = forward(x2, W, target, 4)
+    want = forward(x, W, target, 4, path=path)
+    got = forward(x2, W, target, 4, path=path)
     assert all(torch.equal(got[n], want[n]) for n in got)
     a, b = backward(x, W, target, 1.0, want, dlogp, dentropy), backward(x2, W, target, 1.0, got, dl2, de2)
     assert all(torch.equal(a[n], b[n]) for n in a)
     x2[5, 7], x2[9] = float("nan"), float("inf")                                  # tokens that count: NaN for themselves alone
-    got = forward(x2, W, target, 4)
+    got = forward(x2, W, target, 4, path=path)
     keep = torch.ones(T, dtype=torch.bool)
     keep[[5, 9]] = False
     for n in ("logp", "entropy", "lse", "top"):
@@ -233,7 +261,7 @@ def test_what_is_not_a_number_stays_where_it_is(T):
     assert torch.equal(got["ids"].cpu()[keep], want["ids"].cpu()[keep]) and int(got["ids"].max()) < 300 and int(got["ids"].min()) >= -1
     W2 = W.clone()
     W2[100, 3] = float("nan")                                                     # a column: NaN for every token
-    got = forward(x, W2, target, 4)
+    got = forward(x, W2, target, 4, path=path)
     on = target >= 0
     assert all(bool(torch.isnan(got[n].cpu()[on]).all()) for n in ("logp", "entropy", "lse"))
     assert all(torch.equal(clean[n].cpu()[keep & on], want[n].cpu()[keep & on]) for n in clean)
