@@ -14,7 +14,7 @@
 
 namespace {
 
-constexpr int SCORE_CANDIDATES = 512, SCORE_FEW = 256;
+constexpr int SCORE_CANDIDATES = 512, SCORE_FEW = 256, SCORE_SOME = 1024;
 constexpr int SCORE_ROW = 1 << 20;                 // workgroups of a row of the grid (a launch may have 2^32 threads in a row)
 
 __device__ __forceinline__ float from_ordered(uint32_t k) { return __uint_as_float(k ^ ((k >> 31) != 0 ? 0x80000000u : 0xFFFFFFFFu)); }
@@ -549,16 +549,18 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
   put_alternatives<THREADS>(a, t, r, columns, exact, m, top_col, z_top);
 }
 
-// Threads for a token whose logits are all looked at: each has 32 of them at most.
+// Threads for a token whose logits are all looked at, each with 32 of them at most: many where there are few tokens, few where there are many (d 832, us of the whole call,
+// 64 / 128 / 256 threads: V 697, 8 alternatives, 500 tokens 36 / 35 / 32, 2000 42 / 44 / 53, 8000 84 / 102 / 145; V 4000, 20 alternatives, 128 / 256: 500 44 / 40, 8000 188 / 214).
+// (64 threads are 64 groups: with as many alternatives wanted nearly every column would be a candidate.)
 void launch_whole(const ScoreJoinArgs& a, dim3 grid, hipStream_t s) {
   const auto launch = [&](auto threads, auto pieces) {
     constexpr int THREADS = decltype(threads)::value, PIECES = decltype(pieces)::value;
     MOE_LAUNCH("head_score_whole", (head_score_whole_kernel<THREADS, PIECES>), grid, dim3(THREADS), 0, s, a);
   };
   using std::integral_constant;
-  if (a.T <= SCORE_FEW) launch(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
-  else if (a.V <= 2048 && score_wanted(a.K) <= 64) launch(integral_constant<int, 64>{}, integral_constant<int, 8>{});
-  else if (a.V <= 4096) launch(integral_constant<int, 128>{}, integral_constant<int, 8>{});
+  const bool few = a.T <= SCORE_SOME;
+  if (!few && a.V <= 2048 && score_wanted(a.K) <= 32) launch(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+  else if (!few && a.V <= 4096) launch(integral_constant<int, 128>{}, integral_constant<int, 8>{});
   else if (a.V <= 8192) launch(integral_constant<int, 256>{}, integral_constant<int, 8>{});
   else launch(integral_constant<int, 512>{}, integral_constant<int, 8>{});
 }
