@@ -48,6 +48,7 @@ SETS = {
     "a table and one": [(300 + 7 * i, F32 if i % 2 else BF) for i in range(121)],
     "many tables": [(1 + 13 * i % 999, BF if i % 2 else F32) for i in range(700)],
     "large": [(30_000_001, BF), (5, F32), (9_999_999, F32), (12345, BF)],
+    "more sums than a workgroup adds up": [(150_001, BF if i % 2 else F32) for i in range(500)],
     "large and many": [(400_003, BF if i % 2 else F32) for i in range(130)],
 }
 

@@ -59,7 +59,7 @@ def test_gradients():
 
 def test_scores():
     T, d, V, K = 4, 64, 100, 5
-    ws = torch.zeros(B.moe_head_score_bwd_workspace_bytes(T, d, V), dtype=torch.uint8, device=DEV)
+    ws = torch.zeros(max(B.moe_head_score_fwd_workspace_bytes(T, d, V, K), B.moe_head_score_bwd_workspace_bytes(T, d, V)), dtype=torch.uint8, device=DEV)
     args = dict(x=bf(T, d), W=bf(V, d), target=i32(T), temperature=1.0, logp=f32(T), entropy=f32(T), lse=f32(T), ids=i32(T, K), top=f32(T, K), ws=ws)
     refused(args, B.moe_head_score_fwd, [
         ("x", f32(T, d), "x"), ("W", bf(V, d + 64), "W"), ("W", bf(V, 2 * d)[:, :d], "W"), ("target", i32(T).long(), "target"), ("logp", f32(T + 1), "logp"),

@@ -144,3 +144,16 @@ def test_scores_in_the_binding():
     ]:
         with pytest.raises(B.MoeError, match=what):
             call()
+
+
+def test_score_buffers():
+    x, W, y, r = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(100, 64, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32), torch.zeros(4)
+    for kw in (dict(K=65), dict(K=101), dict(K=-1), dict(v_piece=100)):
+        with pytest.raises(B.MoeError, match="no scores"):
+            B.ScoreBuffers(4, 64, 100, device="cpu", **kw)
+    with pytest.raises(B.MoeError, match="train"):
+        B.ScoreBuffers(4, 64, 100, train=False, device="cpu").run_bwd(x, W, y, r)
+    for call in (lambda b: b.run_fwd(x, W, y), lambda b: b.run_bwd(x, W, y, r)):
+        with pytest.raises(B.MoeError, match="device"):
+            call(B.ScoreBuffers(4, 64, 100, 5, device="cpu"))
+    assert B.ScoreBuffers(4, 64, 100, 0, train=False, device="cpu").ids is None
