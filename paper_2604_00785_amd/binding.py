@@ -670,6 +670,13 @@ _GRAD_TYPES = {BF16: 0, torch.float32: 1}
 _dtype, _numel, _device = torch.Tensor.dtype.__get__, torch.Tensor.numel, torch.Tensor.get_device
 
 
+def _types_and_sizes(ts, name):
+    try:
+        return [*map(_dtype, ts)], [*map(_numel, ts)]
+    except TypeError:
+        raise MoeError(f"{name}: expected tensors, got {({*map(type, ts)})}") from None
+
+
 def _grad_table(grads, outs):
     """(struct moe_grad of each tensor, their device); the table is read before the call returns.  (Looked at attribute by attribute, all tensors at once: half the time
     of tensor by tensor.)"""
@@ -677,12 +684,12 @@ def _grad_table(grads, outs):
     if n == 0:
         raise MoeError("grads: no tensors")
     dev = _device_of(grads[0], "grads[0]")
-    types, counts = [*map(_dtype, grads)], [*map(_numel, grads)]
+    given = types, counts = _types_and_sizes(grads, "grads")
     kinds = [*map(_GRAD_TYPES.get, types)]
     if None in kinds:
         raise MoeError(f"grads[{kinds.index(None)}]: expected bfloat16 or float32, got {types[kinds.index(None)]}")
     same = outs is grads
-    if not same and ([*map(_dtype, outs)] != types or [*map(_numel, outs)] != counts):
+    if not same and _types_and_sizes(outs, "outs") != given:
         for i, o in enumerate(outs):
             if o.dtype is not types[i] or o.numel() != counts[i]:
                 raise MoeError(f"outs[{i}]: expected {counts[i]} elements of {types[i]}, got {o.numel()} of {o.dtype}")

@@ -49,9 +49,9 @@ def test_gradients():
     g, h = bf(10), f32(4, 4)
     refused(dict(grads=[g, h], norm=f32(1), ws=ws), B.moe_grad_norm, [
         ("grads", [g, h.double()], r"grads.1."), ("grads", [g, h.t()[1:]], "grads"), ("grads", [g, h.cpu()], "grads"), ("norm", f32(2), "norm"), ("norm", None, "norm"),
-        ("ws", None, "ws"), ("ws", ws[:8], "WORKSPACE")])
+        ("ws", None, "ws"), ("ws", ws[:8], "WORKSPACE"), ("grads", [g, None], "grads"), ("grads", [None, g], "grads")])
     refused(dict(grads=[g, h], largest=1.0, norm=f32(1), outs=[bf(10), f32(4, 4)], ws=ws), B.moe_grad_clip, [
-        ("grads", [g, g], "outs"), ("outs", [g], "outs"), ("outs", [bf(9), h], r"outs.0."), ("outs", [bf(10), bf(4, 4)], r"outs.1."), ("largest", 0.0, "INVALID"),
+        ("grads", [g, g], "outs"), ("outs", [g], "outs"), ("outs", [g, None], "outs"), ("outs", [bf(9), h], r"outs.0."), ("outs", [bf(10), bf(4, 4)], r"outs.1."), ("largest", 0.0, "INVALID"),
         ("outs", [bf(10), f32(4, 8)[:, ::2]], "outs")])
     both = bf(20)
     refused(dict(grads=[g, h], largest=1.0, norm=f32(1), outs=None, ws=ws), B.moe_grad_clip, [("grads", [g, g], "INVALID"), ("grads", [both[:12], both[11:]], "INVALID")])

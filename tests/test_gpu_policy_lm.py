@@ -75,6 +75,8 @@ def test_teachers_logits_and_limited_gradients():
     order = (z * 2.0 ** 36).round().sort(dim=1, descending=True, stable=True).indices[:, :16]
     assert torch.equal(ids.long(), order)
     assert float((logits.double() - z.gather(1, order)).abs().max()) < 1e-5 * float(z.abs().max())
+    ids, logits = model.top_logits(tokens, 100)                          # more than the scores have
+    assert ids.shape == logits.shape == (T, 100) and float((logits.double() - z.gather(1, ids.long())).abs().max()) < 1e-5 * float(z.abs().max())
     grads = model.train_step(tokens, target, torch.ones(T, device=DEV) / T)
     before = {k: v.double() for k, v in grads.items()}
     size = math.sqrt(sum(float(v.square().sum()) for v in before.values()))

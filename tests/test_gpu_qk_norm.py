@@ -133,6 +133,25 @@ def test_rows_of_zeros_and_what_is_not_a_number():
     assert bool(torch.isnan(dwq).any()) and bool(torch.isnan(dwk).any())
 
 
+def test_no_epsilon_and_the_largest_numbers():
+    """Squares past what 32 bits hold count as infinite; without an epsilon a head of zeros has no norm, and its neighbours are what they are."""
+    q, k, wq, wk, pos, freq, dqo, dko = inputs(4, 3, 2, 64, 64, seed=6)
+    q[1, 1], k[2, 0] = 0, 0
+    q[3, 2] = 3e19
+    args = [dev(t) for t in (q, k, wq, wk, pos, freq)]
+    qo, ko = run(*args, True, eps=0.0)
+    assert bool(torch.isnan(qo[1, 1]).all()) and bool(torch.isnan(ko[2, 0]).all()) and bool((qo[3, 2] == 0).all())
+    dq, dk, _, _ = run_bwd(dev(dqo), dev(dko), *args, True, eps=0.0)
+    assert bool((dq[3, 2] == 0).all())
+    keep_q, keep_k = torch.ones(4, 3, dtype=torch.bool), torch.ones(4, 2, dtype=torch.bool)
+    keep_q[1, 1], keep_q[3, 2], keep_k[2, 0] = False, False, False
+    alone = [t.clone() for t in (q, k)]
+    alone[0][~keep_q], alone[1][~keep_k] = 1, 1
+    args[:2] = [dev(t) for t in alone]
+    for got, want, keep in zip((qo, ko, dq, dk), (*run(*args, True, eps=0.0), *run_bwd(dev(dqo), dev(dko), *args, True, eps=0.0)[:2]), (keep_q, keep_k) * 2):
+        assert bool(torch.isfinite(got[keep.to(DEV)]).all()) and torch.equal(got[keep.to(DEV)], want[keep.to(DEV)])
+
+
 def test_gradients_against_differences():
     """The 64-bit derivative against differences of the 64-bit result, along random directions."""
     q, _, wq, _, pos, freq, dqo, _ = inputs(6, 3, 1, 32, 16, seed=5)
