@@ -416,7 +416,8 @@ int moe_head_distill_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* ta
  * Logits are compared in 64 bits among the K + 4 that are largest by the matrix product in 32 (its error is about 1e-6 of |x| |W row|).
  * Log probabilities and entropies are sums of positive terms: they keep their digits next to zero.  Logits that are NaN or infinite, or 2^30 and more over the
  * temperature, give NaN.  ws at least moe_head_score_fwd_workspace_bytes(T, d, V, K): about T d * 2 + T V * 5 / 8 bytes; with
- * alternatives from a small vocabulary (up to 4000 columns, and up to 16384 if many are wanted) the logits themselves, T d * 2 + T V * 4.
+ * alternatives from a small vocabulary (up to 4000 columns, and up to 16384 if many are wanted) the logits themselves, T d * 2 + T V * 4; and up to eight times
+ * T V * 4 where few tokens and columns (up to 16384) have long rows, whose products go in parts.
  */
 size_t moe_head_score_fwd_workspace_bytes(int T, int d, int V, int K);
 int moe_head_score_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, int T, int d, int V, int K,
@@ -425,7 +426,7 @@ int moe_head_score_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* targ
 /*
  * Its derivative for given dlogp and dentropy [T] fp32 (NULL: zeros), with logp, entropy and lse as the forward call left them:
  *   dz[t, v] = (dlogp ([v == target] - p) - dentropy p (log p + entropy)) / temperature;  dx = dz . W;  dW = dz^T . x
- * Sizes, pieces of the vocabulary, workspace and rounding as moe_head_ce_bwd.
+ * Sizes, pieces of the vocabulary and rounding as moe_head_ce_bwd, and the workspace too, unless the product goes in parts as above (not in pieces of the vocabulary).
  */
 size_t moe_head_score_bwd_workspace_bytes(int T, int d, int V, int v_piece);
 int moe_head_score_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, const float* logp, const float* entropy,

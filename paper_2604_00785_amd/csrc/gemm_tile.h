@@ -111,7 +111,7 @@ enum GemmMode { GATE_UP = 0, DOWN = 1, DGRAD_H = 2, DGRAD_X = 3, WGRAD = 4, WGRA
 // epilogue makes a row's maximum and sums over the wave's columns, or the logits' gradient (row length M).  HEAD_DX: A0 (row length K) times
 // B0 in row_token[0] parts of the reduction over its M rows, each part's sums in 32 bits.  HEAD_DW: WGRAD with rows of M elements, K of them
 // wanted, in E parts of the reduction; with more than one O1 takes each part's sums in 32 bits.  HEAD_TOP: HEAD_STATS of all logits, which leaves the largest of every
-// few columns apart.  HEAD_SCORE_DZ: HEAD_DZ with the gradient of the entropy.
+// few columns apart, or the logits themselves in E parts of the reduction, M rows of each.  HEAD_SCORE_DZ: HEAD_DZ with the gradient of the entropy.
 constexpr bool is_logits(int mode) { return mode == HEAD_STATS || mode == HEAD_DZ || mode == HEAD_TOP || mode == HEAD_SCORE_DZ; }
 constexpr bool is_head_dz(int mode) { return mode == HEAD_DZ || mode == HEAD_SCORE_DZ; }
 constexpr bool is_head_fwd(int mode) { return mode == HEAD_STATS || mode == HEAD_TOP; }
@@ -150,7 +150,7 @@ struct GemmArgs {
 // by strips of 64 columns.
 struct HeadItem { uint32_t at, slot; };   // at: row in the block | column << 4
 struct HeadArgs {
-  float* part;                // HEAD_TOP: HeadStrip, or (two 0) HeadBest, [row][strips of HALF columns], or (two 2) the logits, [row][slots].  HEAD_STATS: [row block][strips of HALF columns][2 or (two) 3][16 rows]: maximum, sum and sum at the temperature, without the items
+  float* part;                // HEAD_TOP: HeadStrip, or (two 0) HeadBest, [row][strips of HALF columns], or (two 2) the logits, [part][M rows][slots].  HEAD_STATS: [row block][strips of HALF columns][2 or (two) 3][16 rows]: maximum, sum and sum at the temperature, without the items
   const f32x4_t* row;         // HEAD_DZ: per row log2(e) lse, factor, and the same at the temperature.  HEAD_SCORE_DZ: l, u, v of 2^t (u + v t), t = c1 z - l
   const int32_t* target;      // [row]
   const int32_t* list_start;  // [row block][list_ld]: first item of each strip; null: no teacher
@@ -424,7 +424,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
   if constexpr (is_wgrad(MODE)) {
     total = a.E * a.m_tiles_cap * a.n_tiles * wpair;
   } else if constexpr (is_logits(MODE) || MODE == HEAD_DX) {
-    total = (head_rows + S - 1) / S * a.n_tiles * (MODE == HEAD_DX ? head_flag : 1);
+    total = (head_rows + S - 1) / S * a.n_tiles * (MODE == HEAD_DX ? head_flag : MODE == HEAD_TOP ? a.E : 1);
   } else {
     total = count_row_tiles<S>(a.offsets, a.E, tid0 & 63) * a.n_tiles;
     if constexpr (MODE == GATE_UP || MODE == DOWN) {
@@ -470,11 +470,15 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
     // rows and 4 (or 8) of columns; all rows of a column tile in a run would have every XCD fetch all rows in every round.
     m_end = head_rows;
     rt = (m_end + S - 1) / S;
+    e = 0;
+    if constexpr (MODE == HEAD_TOP) {
+      e = tile / (rt * a.n_tiles);      // part of the reduction
+      tile -= e * rt * a.n_tiles;
+    }
     const int band = tile / (8 * a.n_tiles), in = tile - band * 8 * a.n_tiles;
     const int high = rt - band * 8 < 8 ? rt - band * 8 : 8;
     nt = in / high;
     m0 = (band * 8 + in - nt * high) * S;
-    e = 0;
     nt = __builtin_amdgcn_readfirstlane(nt);
   } else if constexpr (MODE == HEAD_DX) {
     m_end = head_rows;
@@ -608,6 +612,13 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
       abase += static_cast<size_t>(k_lo) * 2;
     }
     const size_t wsz = static_cast<size_t>(a.N) * a.K;
+    size_t b_from = static_cast<size_t>(e) * wsz;
+    if constexpr (MODE == HEAD_TOP) {
+      const int from = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<long long>(nk) * e / a.E));
+      nk = nk_phase = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<long long>(nk) * (e + 1) / a.E)) - from;
+      abase += static_cast<size_t>(from) * BK * 2;
+      b_from = static_cast<size_t>(from) * BK;
+    }
     if constexpr (!B_KN) {
       // GATE_UP: with Q = S / 4 a wave's 2 Q tile rows are Q rows of Wg and the same Q rows of Wu: tile rows
       // [0,Q) Wg n0.., [Q,2Q) Wu n0.., [2Q,3Q) Wg n0+Q.., [3Q,4Q) Wu n0+Q.. (wave w fills rows Q w .. of them)
@@ -617,7 +628,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
         if (wave & 1) w = a.B1;
         first_col = (wave >> 1) * (S / 4);
       }
-      bbase = reinterpret_cast<const char*>(w + static_cast<size_t>(e) * wsz + static_cast<size_t>(n0) * a.K);
+      bbase = reinterpret_cast<const char*>(w + b_from + static_cast<size_t>(n0) * a.K);
       b_step = BK * 2;
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
@@ -629,7 +640,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
       }
     } else {  // DGRAD_H / DGRAD_X: weights stored [K][N]
       if constexpr (MODE == HEAD_DX) bbase = reinterpret_cast<const char*>(a.B0 + static_cast<size_t>(k_lo) * a.N + n0);
-      else bbase = reinterpret_cast<const char*>(a.B0 + static_cast<size_t>(e) * wsz + n0);
+      else bbase = reinterpret_cast<const char*>(a.B0 + b_from + n0);
       b_step = static_cast<size_t>(BK) * a.N * 2;
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
@@ -1597,7 +1608,7 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
           f32x4_t v[NB];
           static_for<NB>([&](auto j) { v[decltype(j)::value] = accq(i_tag, j); });
           if (he->two == 2) {
-            float* const o = he->part + static_cast<size_t>(grow0 + i * 16 + l16) * he->slots + gcol0 + 4 * lq;
+            float* const o = he->part + (static_cast<size_t>(t.e) * ae->M + (grow0 + i * 16 + l16)) * he->slots + gcol0 + 4 * lq;
             if (i * 16 + l16 < rows) {
               static_for<NB>([&](auto j) {
                 if (16 * decltype(j)::value + 4 * lq < left) *reinterpret_cast<f32x4_t*>(o + 16 * decltype(j)::value) = v[decltype(j)::value];

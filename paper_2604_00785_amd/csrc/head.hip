@@ -800,7 +800,7 @@ void fill_head(const HeadCall& c, const HeadLayout& l, GemmArgs& a, HeadArgs& h)
 bool too_many(long long tiles) { return tiles > 0x7FFFFFFFll / 2; }
 template <int MODE> int launch_logits(GemmArgs& a, const HeadArgs& h, int edge, int rows, const char* name, hipStream_t s) {
   a.n_tiles = ceil_div(a.N, edge);
-  const long long tiles = static_cast<long long>(a.n_tiles) * ceil_div(rows, edge);
+  const long long tiles = static_cast<long long>(a.n_tiles) * ceil_div(rows, edge) * a.E;
   if (too_many(tiles)) return MOE_ERR_INVALID;
   return edge == 128 ? launch_gemm_head<MODE, 128>(a, h, tiles, s, name) : launch_gemm_head<MODE, 256>(a, h, tiles, s, name);
 }
@@ -856,10 +856,45 @@ int score_edge(int T, int d, int V, int K, bool whole) {
   };
   return logits_edge(T, V, d, 9.5, behind(16), behind(32));
 }
-size_t score_part_bytes(int T, int V, bool whole) {
-  return static_cast<size_t>((T + 15) & ~15) * (whole ? score_ld(V) * sizeof(float) : static_cast<size_t>((V + 63) / 64) * sizeof(HeadStrip));
+// Parts of the reduction over d that the logits' product goes in, with tiles of 128, where these are few: a step takes 0.33 us, more where a compute unit has two tiles, and
+// a part's sums are written and read again (1.4 us a million, and 0.4).  one: the logits are written in one part too; else what follows takes `behind` us more.
+// us, from a graph (15 us of them are its own), whole / in the parts of the rule: forward without alternatives, 1 token, d 4096, V 256 42 / 29; 16, 4096, 5000 44 / 34; 500, 2048,
+// 1031 37 / 33; with 20 alternatives 8, 2112, 610 36 / 30; 1 token 50 / 31; 64, 2048, 16000 43 / 38 (strips / 2 parts); 500, 2048, 1031 47 / 39; 1500, 3584, 1000 100 / 89; 2000,
+// 4096, 1500 120 / 116 (8 parts: 135); backward 8, 2112, 610 41 / 34; 16, 4096, 5000 70 / 56; 500, 2048, 1031 59 / 53; 2000, 2048, 256 61 / 54 (256, 1024, 8000 in 2: 56 / 60).
+int score_parts(int T, int d, int V, int edge, bool one, double behind) {
+  if (V > SCORE_WHOLE_V || edge != 128) return 1;
+  const int steps = ceil_div(d, BK);
+  const double tiles = static_cast<double>(ceil_div(T, 128)) * ceil_div(V, 128);
+  const auto time = [&](int p, bool sums) {
+    const double more = tiles * p / HEAD_CUS - 1.0;
+    return ceil_div(steps, p) * (0.33 + 0.25 * (more > 0.0 ? more : 0.0)) + (sums ? p * (1.4e-6 * T * V + 0.4) : 0.0);
+  };
+  double best = time(1, one) - (one ? 0.0 : behind);
+  int parts = 1;
+  for (int p : {2, 3, 4, 6, 8}) {
+    if (steps / p < 4 || tiles * p > 2 * HEAD_CUS) break;
+    const double t = time(p, true);
+    if (t < best) { best = t; parts = p; }
+  }
+  return parts;
 }
-int run_score_fwd(const HeadCall& c, bool whole, int* edges) {
+// What the product leaves, the edge of its tiles and the parts of its reduction.  path, for tests: 1 logits, 2 strips, 100 + p logits in p parts, 0 by the rules.
+struct ScoreShape { bool whole; int edge, parts; };
+ScoreShape score_shape(int T, int d, int V, int K, int path) {
+  if (path > 100) return {true, 128, path - 100};
+  const bool whole = path == 0 ? score_whole(T, d, V, K) : path == 1;
+  const ScoreShape s{whole, score_edge(T, d, V, K, whole), 1};
+  const int parts = path == 0 ? score_parts(T, d, V, s.edge, whole, K > 0 ? -4.0 : 0.5 + 1.8e-6 * T * V) : 1;
+  return parts > 1 ? ScoreShape{true, 128, parts} : s;
+}
+size_t score_part_bytes(int T, int V, const ScoreShape& s) {
+  return static_cast<size_t>((T + 15) & ~15) * (s.whole ? static_cast<size_t>(s.parts) * score_ld(V) * sizeof(float) : static_cast<size_t>((V + 63) / 64) * sizeof(HeadStrip));
+}
+// The same of the backward pass, whose gradient is formed by a launch of its own then.  (Not in pieces of the vocabulary.)
+int score_dz_parts(int T, int d, int V, int piece, int wanted) {
+  return piece < V ? 1 : wanted > 0 ? wanted : score_parts(T, d, V, logits_edge(T, V, d, 10.8), false, 1.0);
+}
+int run_score_fwd(const HeadCall& c, const ScoreShape& shape, int* edges) {
   const HeadLayout l = head_layout(c.T, c.d, c.V, 0, false);
   GemmArgs a{};
   HeadArgs h{};
@@ -868,23 +903,25 @@ int run_score_fwd(const HeadCall& c, bool whole, int* edges) {
   const bool all = c.T <= ALL_TOKENS;
   int rc = MOE_OK;
   if (all) {
-    a.offsets = nullptr; a.row_token = nullptr; a.A0 = c.x; a.M = c.T;
+    a.offsets = nullptr; a.row_token = nullptr; a.A0 = c.x;
   } else if ((rc = run_prep(c, l, BwdRule{}, 0)) != MOE_OK) {
     return rc;
   }
-  const int edge = settle_edge(edges, score_edge(c.T, c.d, c.V, c.K, whole));
+  const int edge = settle_edge(edges, shape.edge);
+  a.M = c.T;
+  a.E = shape.parts;
   h.strips = ceil_div(c.V, edge / 2);
-  h.two = c.K == 0 ? 0 : whole ? 2 : 1;
+  h.two = shape.whole ? 2 : c.K > 0;
   h.slots = score_ld(c.V);
   h.part = reinterpret_cast<float*>(c.ws + l.big);
   if ((rc = launch_logits<HEAD_TOP>(a, h, edge, c.T, "gemm_head_top", c.s)) != MOE_OK) return rc;
   const ScoreJoinArgs j{h.part, all ? nullptr : reinterpret_cast<const int32_t*>(c.ws + l.control),
-                        reinterpret_cast<const int32_t*>(c.ws + l.token_row), c.target, c.x, c.W, c.T, c.d, c.V, c.K, h.strips, whole, h.c1, 1.0 / c.tau,
+                        reinterpret_cast<const int32_t*>(c.ws + l.token_row), c.target, c.x, c.W, c.T, c.d, c.V, c.K, h.strips, shape.whole, shape.parts, h.c1, 1.0 / c.tau,
                         c.loss, c.entropy, c.lse, c.ids, c.top};
   return moe_head_score_join(j, edge, c.s);
 }
 
-int run_head_bwd(const HeadCall& c, int v_piece, int* edges) {
+int run_head_bwd(const HeadCall& c, int v_piece, int dz_parts, int* edges) {
   const HeadLayout l = head_layout(c.T, c.d, c.V, c.t.K, true);
   const int piece = head_piece(c.T, c.V, v_piece), wanted = edges != nullptr ? edges[1] : 0;
   uint16_t* dz = reinterpret_cast<uint16_t*>(c.ws + l.big);
@@ -913,7 +950,15 @@ int run_head_bwd(const HeadCall& c, int v_piece, int* edges) {
     const uint16_t* W = c.W + static_cast<size_t>(v0) * c.d;
     a.A0 = reinterpret_cast<const uint16_t*>(c.ws + l.xc); a.A1 = c.x; a.B0 = W; a.O0 = dz; a.K = c.d; a.N = cols; a.M = ld;
     const int edge = settle_edge(edges, logits_edge(c.T, cols, c.d, 10.8));
-    rc = c.score ? launch_logits<HEAD_SCORE_DZ>(a, h, edge, c.T, "gemm_head_score_dz", c.s) : launch_logits<HEAD_DZ>(a, h, edge, c.T, "gemm_head_dz", c.s);
+    if (c.score && dz_parts > 1) {
+      GemmArgs z = a;
+      HeadArgs zh = h;
+      z.E = dz_parts; z.M = c.T;
+      zh.two = 2; zh.slots = score_ld(cols); zh.part = part;               // (the products below take this place later)
+      if ((rc = launch_logits<HEAD_TOP>(z, zh, 128, c.T, "gemm_head_top", c.s)) != MOE_OK) return rc;
+      const ScoreDzArgs g{part, control, h.target, h.row, h.terms, h.item, dz, c.T, cols, ld, dz_parts, l.low, h.c1};
+      rc = moe_head_score_dz(g, c.s);
+    } else rc = c.score ? launch_logits<HEAD_SCORE_DZ>(a, h, edge, c.T, "gemm_head_score_dz", c.s) : launch_logits<HEAD_DZ>(a, h, edge, c.T, "gemm_head_dz", c.s);
     if (rc != MOE_OK) return rc;
     GemmArgs b{};
     b.offsets = a.offsets; b.row_token = control + DX_PARTS; b.stream_rows = v0 > 0;
@@ -989,7 +1034,7 @@ extern "C" int moe_head_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t*
   c.x = x; c.W = W; c.target = target; c.t = {ids, teacher, temperature, K}; c.T = T; c.d = d; c.V = V;
   c.in_loss = loss; c.in_lse = lse; c.in_lse_t = lse_t; c.dloss = dloss; c.dkd = dkd; c.dx = dx; c.dW = dW;
   c.ws = static_cast<char*>(ws); c.s = static_cast<hipStream_t>(stream);
-  return run_head_bwd(c, v_piece, edges);
+  return run_head_bwd(c, v_piece, 1, edges);
 }
 
 extern "C" int moe_head_ce_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, int T, int d, int V, float* loss, float* lse,
@@ -1018,44 +1063,53 @@ extern "C" int moe_head_distill_bwd(const moe_bf16* x, const moe_bf16* W, const 
   return moe_head_bwd(x, W, target, ids, teacher, temperature, loss, lse, lse_t, dloss, dkd, T, d, V, K, v_piece, dx, dW, ws, ws_bytes, stream, nullptr);
 }
 
-// Log probabilities, entropies and alternatives.  edges, for tests: as above; forward edges[1]: 1 from the logits, 2 from strips, 0 by the rule.
+// Log probabilities, entropies and alternatives.  edges, for tests: as above; forward edges[1]: what score_shape calls path; backward edges[0]: 1000 p + edge for
+// logits in p parts.
 namespace {
+size_t score_bwd_bytes(int T, int d, int V, int v_piece, int wanted) {
+  const size_t all = moe_head_bwd_workspace_bytes(T, d, V, 0, v_piece);
+  if (all == 0) return 0;
+  const int piece = head_piece(T, V, v_piece), parts = score_dz_parts(T, d, V, piece, wanted);
+  const size_t least = head_layout(T, d, V, 0, true).big + head_dz_bytes(T, piece) + (parts > 1 ? score_part_bytes(T, V, {true, 128, parts}) : 0);
+  return all > least ? all : least;
+}
 bool bad_score(int T, int d, int V, int K) { return bad_head_dims(T, d, V, 0) || K < 0 || K > SCORE_MAX_K || K > V; }
 }  // namespace
 extern "C" size_t moe_head_score_fwd_workspace_bytes(int T, int d, int V, int K) {
   if (bad_score(T, d, V, K)) return 0;
-  return head_layout(T, d, V, 0, false).big + score_part_bytes(T, V, score_whole(T, d, V, K));
+  return head_layout(T, d, V, 0, false).big + score_part_bytes(T, V, score_shape(T, d, V, K, 0));
 }
-extern "C" size_t moe_head_score_bwd_workspace_bytes(int T, int d, int V, int v_piece) { return moe_head_bwd_workspace_bytes(T, d, V, 0, v_piece); }
+extern "C" size_t moe_head_score_bwd_workspace_bytes(int T, int d, int V, int v_piece) { return score_bwd_bytes(T, d, V, v_piece, 0); }
 
 extern "C" int moe_head_score_fwd_edges(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, int T, int d, int V, int K,
                                         float* logp, float* entropy, float* lse, int32_t* ids, float* top, void* ws, size_t ws_bytes, void* stream,
                                         int* edges) {
   if (bad_score(T, d, V, K) || bad_temperature(temperature) || bad_edge_list(edges, 1)) return MOE_ERR_INVALID;
   if (bad_ptrs({x, W, target, logp, entropy, lse, ws}) || (K > 0 && bad_ptrs({ids, top}))) return MOE_ERR_INVALID;
-  bool whole = score_whole(T, d, V, K);
-  if (edges != nullptr && edges[1] != 0) whole = edges[1] == 1;
-  if (whole && (K == 0 || V > SCORE_WHOLE_V)) return MOE_ERR_INVALID;
-  if (ws_bytes < head_layout(T, d, V, 0, false).big + score_part_bytes(T, V, whole)) return MOE_ERR_WORKSPACE;
+  const ScoreShape shape = score_shape(T, d, V, K, edges != nullptr ? edges[1] : 0);
+  if ((shape.whole && V > SCORE_WHOLE_V) || shape.parts > d / BK) return MOE_ERR_INVALID;
+  if (ws_bytes < head_layout(T, d, V, 0, false).big + score_part_bytes(T, V, shape)) return MOE_ERR_WORKSPACE;
   HeadCall c{};
   c.x = x; c.W = W; c.target = target; c.t.temperature = 1.f; c.T = T; c.d = d; c.V = V;
   c.score = true; c.tau = temperature; c.K = K;
   c.loss = logp; c.entropy = entropy; c.lse = lse; c.ids = ids; c.top = top;
   c.ws = static_cast<char*>(ws); c.s = static_cast<hipStream_t>(stream);
-  return run_score_fwd(c, whole, edges);
+  return run_score_fwd(c, shape, edges);
 }
 extern "C" int moe_head_score_bwd_edges(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, const float* logp,
                                         const float* entropy, const float* lse, const float* dlogp, const float* dentropy, int T, int d, int V, int v_piece,
                                         moe_bf16* dx, moe_bf16* dW, void* ws, size_t ws_bytes, void* stream, int* edges) {
-  if (bad_head_dims(T, d, V, 0) || bad_temperature(temperature) || v_piece < 0 || v_piece % 256 != 0 || bad_edge_list(edges, 2)) return MOE_ERR_INVALID;
+  const int wanted = edges != nullptr ? edges[0] / 1000 : 0;
+  if (wanted > 0) edges[0] %= 1000;
+  if (bad_head_dims(T, d, V, 0) || bad_temperature(temperature) || v_piece < 0 || v_piece % 256 != 0 || bad_edge_list(edges, 2) || wanted > d / BK) return MOE_ERR_INVALID;
   if (bad_ptrs({x, W, target, logp, entropy, lse, dlogp, dx, dW, ws}) || !moe_aligned16(dentropy)) return MOE_ERR_INVALID;
-  if (ws_bytes < moe_head_score_bwd_workspace_bytes(T, d, V, v_piece)) return MOE_ERR_WORKSPACE;
+  if (ws_bytes < score_bwd_bytes(T, d, V, v_piece, wanted)) return MOE_ERR_WORKSPACE;
   HeadCall c{};
   c.x = x; c.W = W; c.target = target; c.t.temperature = 1.f; c.T = T; c.d = d; c.V = V;
   c.score = true; c.tau = temperature;
   c.in_loss = logp; c.in_lse = lse; c.in_entropy = entropy; c.dloss = dlogp; c.dentropy = dentropy; c.dx = dx; c.dW = dW;
   c.ws = static_cast<char*>(ws); c.s = static_cast<hipStream_t>(stream);
-  return run_head_bwd(c, v_piece, edges);
+  return run_head_bwd(c, v_piece, score_dz_parts(T, d, V, head_piece(T, V, v_piece), wanted), edges);
 }
 extern "C" int moe_head_score_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, int T, int d, int V, int K, float* logp,
                                   float* entropy, float* lse, int32_t* ids, float* top, void* ws, size_t ws_bytes, void* stream) {

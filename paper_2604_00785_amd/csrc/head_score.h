@@ -15,10 +15,10 @@ constexpr int SCORE_MAX_K = 64, SCORE_SPARE = 4;
 constexpr int score_wanted(int K) { return K > 0 ? K + SCORE_SPARE : 1; }       // logits that are formed anew
 
 struct ScoreJoinArgs {
-  const void* part;                                // HeadStrip, or (K 0) HeadBest [row][strips], or (whole) the logits [row][score_ld(V)]
+  const void* part;                                // HeadStrip, or (K 0) HeadBest [row][strips], or (whole) the logits' `parts` summands [part][T][score_ld(V)]
   const int32_t *control, *token_row, *target;     // control null: rows are tokens
   const moe_bf16 *x, *W;
-  int T, d, V, K, strips, whole;
+  int T, d, V, K, strips, whole, parts;
   float c1;                                        // log2(e) over the temperature
   double over_tau;
   float *logp, *entropy, *lse;
@@ -30,3 +30,15 @@ constexpr int SCORE_WHOLE_V = 16384;
 constexpr int score_ld(int V) { return (V + 3) & ~3; }
 // edge: of the tiles that the strips are from (HALF = edge / 2)
 int moe_head_score_join(const ScoreJoinArgs& a, int edge, hipStream_t s);
+
+// The logits' gradient from their summands, as HEAD_SCORE_DZ has it: dz [rows][ld], and behind it (up to `low` rows) what rounding it loses; item [row]: that of the target's.
+struct ScoreDzArgs {
+  const float* part;                               // [part][T][score_ld(V)]
+  const int32_t *control, *target;                 // control[1]: rows
+  const f32x4_t *row, *terms;
+  float* item;
+  uint16_t* dz;
+  int T, V, ld, parts, low;
+  float c1;
+};
+int moe_head_score_dz(const ScoreDzArgs& a, hipStream_t s);

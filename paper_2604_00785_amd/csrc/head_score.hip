@@ -243,8 +243,8 @@ __device__ __forceinline__ void put_alternatives(const ScoreJoinArgs& a, int t, 
   });
 }
 
-// With alternatives, from the logits themselves: a thread has PIECES times four of them in registers.
-template <int THREADS, int PIECES> __global__ __launch_bounds__(THREADS) void head_score_whole_kernel(ScoreJoinArgs a) {
+// From the logits themselves: a thread has PIECES times four of them in registers.  LISTS: with alternatives.
+template <int THREADS, int PIECES, bool LISTS> __global__ __launch_bounds__(THREADS) void head_score_whole_kernel(ScoreJoinArgs a) {
   // Groups of threads have 4, 8 or 16 columns side by side, and there are at least as many groups as logits are wanted; where fewer of them have any, all columns are
   // candidates.
   constexpr int WAVES = THREADS / MOE_WAVE, SIZE = THREADS <= 128 ? 1 : THREADS == 256 ? 2 : 4, GROUPS = THREADS / SIZE, WANTED = score_wanted(SCORE_MAX_K);
@@ -275,6 +275,17 @@ template <int THREADS, int PIECES> __global__ __launch_bounds__(THREADS) void he
 #pragma unroll
     for (int i = 0; i < 4; ++i) z[p][i] = c + i < a.V ? v[i] : -__builtin_inff();
   }
+  for (int part = 1; part < a.parts; ++part) {
+    const float* const more = z_row + static_cast<size_t>(part) * a.T * ld;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      const int c = (p * THREADS + tid) * 4;
+      f32x4_t v = {};
+      if (c < ld) v = *reinterpret_cast<const f32x4_t*>(more + c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) if (c + i < a.V) z[p][i] += v[i];
+    }
+  }
   // (as in the other kernel; of 0 and -0 either may be called the larger, the order in 64 bits knows no difference)
   const auto key_of = [&](int p, int i) __attribute__((always_inline)) -> uint64_t {
     const uint32_t bits = __float_as_uint(z[p][i]);
@@ -286,15 +297,24 @@ template <int THREADS, int PIECES> __global__ __launch_bounds__(THREADS) void he
 #pragma unroll
     for (int i = 0; i < 4; ++i) { const uint64_t k = key_of(p, i); best = k > best ? k : best; }
   if (tid == 0) { s_top = s_least = 0; s_found = 0; }
-  const uint64_t of_group = group_most<SIZE>(best);
-  if (tid % SIZE == 0) keys[tid / SIZE] = of_group;
-  __syncthreads();
-  ranked<THREADS>(GROUPS, [&](int k, int i) __attribute__((always_inline)) { return keys[k] > keys[i]; }, [&](int i, int above) __attribute__((always_inline)) {
-    if (above == 0 && keys[i] != 0) s_top = keys[i];
-    if (above == wanted - 1 && keys[i] != 0) s_least = keys[i];
-  });
-  __syncthreads();
-  const uint64_t top_key = s_top, least = s_least;
+  const uint64_t of_group = group_most<LISTS ? SIZE : MOE_WAVE>(best);
+  uint64_t top_key = 0, least = 0;
+  if constexpr (LISTS) {
+    if (tid % SIZE == 0) keys[tid / SIZE] = of_group;
+    __syncthreads();
+    ranked<THREADS>(GROUPS, [&](int k, int i) __attribute__((always_inline)) { return keys[k] > keys[i]; }, [&](int i, int above) __attribute__((always_inline)) {
+      if (above == 0 && keys[i] != 0) s_top = keys[i];
+      if (above == wanted - 1 && keys[i] != 0) s_least = keys[i];
+    });
+    __syncthreads();
+    top_key = s_top;
+    least = s_least;
+  } else {
+    if (lane == 0) keys[wave] = of_group;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) top_key = keys[w] > top_key ? keys[w] : top_key;
+  }
   const int top_col = static_cast<int>(~static_cast<uint32_t>(top_key));
   const float most = from_ordered(static_cast<uint32_t>(top_key >> 32)), e = ceilf(most * c1);
   float sum = 0.f, moment = 0.f;
@@ -306,18 +326,22 @@ template <int THREADS, int PIECES> __global__ __launch_bounds__(THREADS) void he
       const float x = __builtin_elementwise_maximum(__builtin_fmaf(z[p][i], c1, -e), -1000.f), s = col == top_col ? 0.f : __builtin_amdgcn_exp2f(x);
       sum += s;
       moment = __builtin_fmaf(s, x, moment);
-      const uint64_t key = key_of(p, i);
-      if (key >= least && key != 0) {
-        const int at = atomicAdd(&s_found, 1);
-        if (at < CANDIDATES) found[at] = key;
+      if constexpr (LISTS) {
+        const uint64_t key = key_of(p, i);
+        if (key >= least && key != 0) {
+          const int at = atomicAdd(&s_found, 1);
+          if (at < CANDIDATES) found[at] = key;
+        }
       }
     }
   sum = group_sum<MOE_WAVE>(sum);
   moment = group_sum<MOE_WAVE>(moment);
   if (lane == 0) { part[wave][0] = sum; part[wave][1] = moment; }
   __syncthreads();
-  int m = s_found;
-  if (m <= CANDIDATES) {
+  int m = LISTS ? s_found : top_key != 0;
+  if (!LISTS) {
+    if (tid == 0) columns[0] = top_col;
+  } else if (m <= CANDIDATES) {
     ranked<THREADS>(m, [&](int k, int i) __attribute__((always_inline)) { return found[k] > found[i]; }, [&](int i, int above) __attribute__((always_inline)) {
       if (above < wanted) columns[above] = static_cast<int>(~static_cast<uint32_t>(found[i]));
     });
@@ -354,7 +378,7 @@ template <int THREADS, int PIECES> __global__ __launch_bounds__(THREADS) void he
   const double z_top = exact[0];                                           // (columns[0] is top_col)
   const ScoreResult r = result_of(all, top_key != 0, z_top, c1);
   if (tid == 0) put_scores(a, t, r, y == top_col, exact[m], z_top);
-  put_alternatives<THREADS>(a, t, r, columns, exact, m, top_col, z_top);
+  if constexpr (LISTS) put_alternatives<THREADS>(a, t, r, columns, exact, m, top_col, z_top);
 }
 
 // With alternatives: a workgroup of THREADS for each token, 1024 where there are few (d 2048, V 50304, 20 alternatives, us, 256 / 1024: 1 token 18.5 / 12.7, 256 tokens
@@ -549,24 +573,63 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
   put_alternatives<THREADS>(a, t, r, columns, exact, m, top_col, z_top);
 }
 
+// The logits' gradient from their summands: what the epilogue of the product of HEAD_SCORE_DZ does with whole logits, eight columns a thread.
+__global__ __launch_bounds__(256) void head_score_dz_kernel(ScoreDzArgs a) {
+  typedef __attribute__((ext_vector_type(4))) uint32_t u4;
+  const int pieces = a.ld / 8, rows = a.control[1];
+  const size_t at = static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x;
+  const int row = static_cast<int>(at / pieces), c = static_cast<int>(at - static_cast<size_t>(row) * pieces) * 8;
+  if (row >= rows) return;
+  const int z_ld = score_ld(a.V), y = a.target[row] - c;
+  const f32x4_t p = a.row[row];
+  const float at_target = a.terms[row][0];
+  float g[8] = {};
+#pragma unroll
+  for (int h = 0; h < 8; h += 4) {
+    if (c + h >= z_ld) continue;
+    const float* z_at = a.part + static_cast<size_t>(row) * z_ld + c + h;
+    f32x4_t z = *reinterpret_cast<const f32x4_t*>(z_at);
+    for (int part = 1; part < a.parts; ++part) z += *reinterpret_cast<const f32x4_t*>(z_at += static_cast<size_t>(a.T) * z_ld);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float t = __builtin_fmaf(z[i], a.c1, -p[0]);
+      const float other = __builtin_amdgcn_exp2f(t) * __builtin_fmaf(p[2], t, p[1]);
+      g[h + i] = c + h + i >= a.V ? 0.f : h + i == y ? at_target : other;
+      if (h + i == y) a.item[row] = at_target - bf16_to_f32(f32_to_bf16(at_target));
+    }
+  }
+  const auto put = [&](int r) __attribute__((always_inline)) {
+    *reinterpret_cast<u4*>(a.dz + static_cast<size_t>(r) * a.ld + c) = u4{pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]), pack_bf16(g[4], g[5]), pack_bf16(g[6], g[7])};
+  };
+  put(row);
+  if (rows > a.low) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) g[i] -= bf16_to_f32(f32_to_bf16(g[i]));
+  put(rows + row);
+}
+
 // Threads for a token whose logits are all looked at, each with 32 of them at most: many where there are few tokens, few where there are many (d 832, us of the whole call,
 // 64 / 128 / 256 threads: V 697, 8 alternatives, 500 tokens 36 / 35 / 32, 2000 42 / 44 / 53, 8000 84 / 102 / 145; V 4000, 20 alternatives, 128 / 256: 500 44 / 40, 8000 188 / 214).
+// Short rows in registers for them alone: 8192 tokens, d 2048, V 256, 20 alternatives, with 8 / 2 pieces a thread 146 / 131; 300, 704, 697 33 / 31.
 // (64 threads are 64 groups: with as many alternatives wanted nearly every column would be a candidate.)
 void launch_whole(const ScoreJoinArgs& a, dim3 grid, hipStream_t s) {
   const auto launch = [&](auto threads, auto pieces) {
     constexpr int THREADS = decltype(threads)::value, PIECES = decltype(pieces)::value;
-    MOE_LAUNCH("head_score_whole", (head_score_whole_kernel<THREADS, PIECES>), grid, dim3(THREADS), 0, s, a);
+    if (a.K > 0) MOE_LAUNCH("head_score_whole", (head_score_whole_kernel<THREADS, PIECES, true>), grid, dim3(THREADS), 0, s, a);
+    else MOE_LAUNCH("head_score_whole", (head_score_whole_kernel<THREADS, PIECES, false>), grid, dim3(THREADS), 0, s, a);
   };
   using std::integral_constant;
   const bool few = a.T <= SCORE_SOME;
-  if (!few && a.V <= 2048 && score_wanted(a.K) <= 32) launch(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+  if (!few && a.V <= 512 && score_wanted(a.K) <= 32) launch(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  else if (!few && a.V <= 2048 && score_wanted(a.K) <= 32) launch(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+  else if (few && a.V <= 2048) launch(integral_constant<int, 256>{}, integral_constant<int, 2>{});
   else if (!few && a.V <= 4096) launch(integral_constant<int, 128>{}, integral_constant<int, 8>{});
   else if (a.V <= 8192) launch(integral_constant<int, 256>{}, integral_constant<int, 8>{});
   else launch(integral_constant<int, 512>{}, integral_constant<int, 8>{});
 }
 template <int HALF> void launch_join(const ScoreJoinArgs& a, hipStream_t s) {
   const auto rows = [](int n) { return dim3(n < SCORE_ROW ? n : SCORE_ROW, (n + SCORE_ROW - 1) / SCORE_ROW); };
-  if (a.K == 0) {
+  if (a.K == 0 && !a.whole) {
     if (a.T <= SCORE_FEW) MOE_LAUNCH("head_score", (head_score_kernel<HALF, true>), dim3(a.T), dim3(256), 0, s, a);
     else MOE_LAUNCH("head_score", (head_score_kernel<HALF, false>), rows((a.T + 3) / 4), dim3(256), 0, s, a);
     return;
@@ -583,6 +646,11 @@ template <int HALF> void launch_join(const ScoreJoinArgs& a, hipStream_t s) {
 
 }  // namespace
 
+int moe_head_score_dz(const ScoreDzArgs& a, hipStream_t s) {
+  const size_t pieces = static_cast<size_t>(a.T) * (a.ld / 8);
+  MOE_LAUNCH("head_score_dz", head_score_dz_kernel, dim3(static_cast<unsigned>((pieces + 255) / 256)), dim3(256), 0, s, a);
+  return moe_check_launch();
+}
 int moe_head_score_join(const ScoreJoinArgs& a, int edge, hipStream_t s) {
   if (edge == 128) launch_join<64>(a, s);
   else launch_join<128>(a, s);

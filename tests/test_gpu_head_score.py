@@ -29,13 +29,13 @@ def junk(*shape, dtype=torch.float32):
 
 
 def forward(x, W, target, K=0, tau=1.0, edge=0, path=0):
-    """path 1: alternatives from the logits, 2: from strips of them, 0: as the rule has it."""
+    """path 1: alternatives from the logits, 2: from strips of them, 100 + p: from logits in p parts of the reduction, 0: as the rule has it."""
     x, W, target = x.to(DEV), W.to(DEV), target.to(DEV)
     (T, d), V = x.shape, W.shape[0]
     out = {"logp": junk(T), "entropy": junk(T), "lse": junk(T)}
     ids, top = (junk(T, K, dtype=torch.int32), junk(T, K)) if K else (None, None)
     n = B.moe_head_score_fwd_workspace_bytes(T, d, V, K)
-    ws = torch.full((n if path == 0 else n + (T + 15) * (V + 64) * 4,), 255, dtype=torch.uint8, device=DEV)
+    ws = torch.full((n if path == 0 else n + max(1, path - 100) * (T + 15) * (V + 64) * 4,), 255, dtype=torch.uint8, device=DEV)
     if edge == 0 and path == 0:
         B.moe_head_score_fwd(x, W, target, tau, out["logp"], out["entropy"], out["lse"], ids, top, ws)
     else:
@@ -49,20 +49,20 @@ def forward(x, W, target, K=0, tau=1.0, edge=0, path=0):
     return out
 
 
-def backward(x, W, target, tau, f, dlogp, dentropy, v_piece=0, edge=0):
+def backward(x, W, target, tau, f, dlogp, dentropy, v_piece=0, edge=0, parts=0):
     x, W, target = x.to(DEV), W.to(DEV), target.to(DEV)
     (T, d), V = x.shape, W.shape[0]
     dx, dW = junk(T, d, dtype=torch.bfloat16), junk(V, d, dtype=torch.bfloat16)
-    ws = torch.full((B.moe_head_score_bwd_workspace_bytes(T, d, V, v_piece),), 255, dtype=torch.uint8, device=DEV)
+    ws = torch.full((B.moe_head_score_bwd_workspace_bytes(T, d, V, v_piece) + parts * (T + 15) * (V + 64) * 4,), 255, dtype=torch.uint8, device=DEV)
     dlogp, dentropy = dlogp.to(DEV), None if dentropy is None else dentropy.to(DEV)
-    if edge == 0:
+    if edge == 0 and parts == 0:
         B.moe_head_score_bwd(x, W, target, tau, f["logp"], f["entropy"], f["lse"], dlogp, dentropy, v_piece, dx, dW, ws)
     else:
         p = lambda t: None if t is None else ctypes.c_void_p(t.data_ptr())  # noqa: E731
-        edges = (ctypes.c_int * 2)(edge, 0)
+        edges = (ctypes.c_int * 2)(edge + 1000 * parts, 0)
         rc = B.load().moe_head_score_bwd_edges(p(x), p(W), p(target), ctypes.c_float(tau), p(f["logp"]), p(f["entropy"]), p(f["lse"]), p(dlogp), p(dentropy), T, d, V,
                                                v_piece, p(dx), p(dW), p(ws), ctypes.c_size_t(ws.numel()), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream), edges)
-        assert rc == 0 and edges[0] == edge
+        assert rc == 0 and edge in (0, edges[0])
     return {"dx": dx, "dW": dW}
 
 
@@ -101,6 +101,84 @@ def test_backward(T, d, V, tau, edge):
             R.check(got[n], want[n], bound[n], n)
     off = target.cpu() < 0
     assert bool((got["dx"].cpu()[off] == 0).all())
+
+
+@pytest.mark.parametrize("T,d,V,K,tau,parts", [(1, 512, 300, 5, 1.0, 8), (1, 512, 1, 0, 1.0, 8), (7, 2112, 610, 0, 0.7, 8), (7, 2112, 610, 20, 0.7, 0), (40, 320, 257, 64, 1.0, 5),
+                                               (65, 576, 130, 2, 1.0, 2), (100, 704, 3001, 20, 1.0, 3), (129, 192, 515, 64, 1.0, 2), (130, 256, 2049, 0, 1.3, 4), (200, 1024, 999, 0, 1.0, 0),
+                                               (257, 512, 70, 64, 1.0, 2), (300, 1024, 1031, 0, 1.0, 4), (300, 1024, 1031, 7, 1.0, 0), (2000, 512, 257, 3, 1.0, 2), (3, 256, 16384, 64, 1.0, 2),
+                                               (1, 4096, 256, 1, 1.0, 0), (1030, 2048, 256, 0, 1.0, 0)])
+def test_parts_of_the_reduction(T, d, V, K, tau, parts):
+    """Few tiles with long reductions: the logits' summands apart, forward and backward."""
+    x, W, target, dlogp, dentropy = inputs(T, d, V, seed=T + d)
+    want, bound = R.score(x, W, target, K, tau, dlogp, dentropy)
+    f = forward(x, W, target, K, tau, path=100 + parts if parts else 0)
+    R.check_all(f, {n: want[n] for n in f}, bound)
+    again = forward(x, W, target, K, tau, path=100 + parts if parts else 0)
+    got = backward(x, W, target, tau, f, dlogp, dentropy, parts=parts)
+    for n in f:
+        assert torch.equal(f[n], again[n]), n
+    for n in ("dx", "dW"):
+        R.check(got[n], want[n], bound[n], n)
+
+
+@pytest.mark.parametrize("K", [0, 3])
+@pytest.mark.parametrize("T", [3, 1030])
+@pytest.mark.parametrize("V", [3, 511, 513, 2048, 2050, 4096, 4099, 8192, 8193, 16384])
+def test_logits_themselves_at_the_borders_of_a_workgroup(T, V, K):
+    x, W, target, _, _ = inputs(T, 128, V, masked=0.9 if T > 100 else 0.0, seed=V + 1)
+    x[0], W[V - 1] = 0, W[0]                             # equal logits
+    want, bound = R.score(x, W, target, K)
+    R.check_all(forward(x, W, target, K, path=102), want, bound)
+
+
+@pytest.mark.parametrize("T", [20, 400])
+def test_what_is_not_a_number_in_parts(T):
+    x, W, target, dlogp, dentropy = inputs(T, 256, 300, masked=0.0, seed=17)
+    target[3] = -100
+    x[3] = float("nan")                                  # a masked token: leaves no trace
+    for K in (0, 4):
+        want = forward(x, W, target, K, path=103)
+        grads = backward(x, W, target, 1.0, want, dlogp, dentropy, parts=3)
+        assert all(bool(torch.isfinite(t).all()) for t in (*want.values(), *grads.values()))
+        assert all(bool((want[n][3] == (-1 if n == "ids" else 0)).all()) for n in want) and bool((grads["dx"][3] == 0).all())
+        x2 = x.clone()
+        x2[5, 200], x2[9], W2 = float("nan"), float("inf"), W.clone()
+        got = forward(x2, W, target, K, path=103)
+        keep = torch.ones(T, dtype=torch.bool)
+        keep[[5, 9]] = False
+        for n in want:
+            assert torch.equal(got[n].cpu()[keep], want[n].cpu()[keep]), n
+            assert n == "ids" or bool(torch.isnan(got[n].cpu()[~keep]).all()), n
+        back = backward(x2, W, target, 1.0, got, dlogp, dentropy, parts=3)
+        assert torch.equal(back["dx"].cpu()[keep], grads["dx"].cpu()[keep]) and bool(torch.isnan(back["dx"].cpu()[~keep]).any(1).all())
+        W2[100, 3] = float("nan")
+        got = forward(x, W2, target, K, path=103)
+        assert all(bool(torch.isnan(got[n].cpu()[target >= 0]).all()) for n in ("logp", "entropy", "lse"))
+
+
+def test_parts_in_a_graph():
+    """The rule's own choice for a few tokens of long rows, masks that change between the replays, a workspace that others write to."""
+    for T, K in ((7, 5), (300, 0)):
+        d, V = 2048, 610
+        x, W, target, dlogp, dentropy = inputs(T, d, V, seed=18)
+        assert B.moe_head_score_fwd_workspace_bytes(T, d, V, K) > B.moe_head_score_fwd_workspace_bytes(T, 64, V, K) + T * V * 4
+        s = B.ScoreBuffers(T, d, V, K, device=DEV)
+        xg, Wg, yg, dl, de = (t.to(DEV) for t in (x, W, target, dlogp, dentropy))
+        s.run_fwd(xg, Wg, yg, 0.9)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            s.run_fwd(xg, Wg, yg, 0.9)
+            s.run_bwd(xg, Wg, yg, dl, de, 0.9)
+        for shift in (0, 1, 2):
+            y2 = target.roll(shift)
+            yg.copy_(y2)
+            s.ws.fill_(255)
+            graph.replay()
+            want = forward(x, W, y2, K, 0.9)
+            want.update(backward(x, W, y2, 0.9, want, dlogp, dentropy))
+            torch.cuda.synchronize()
+            assert all(torch.equal(getattr(s, n), want[n]) for n in want), shift
 
 
 def test_backward_in_pieces_of_the_vocabulary():
