@@ -426,7 +426,8 @@ int moe_head_score_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* targ
 /*
  * Its derivative for given dlogp and dentropy [T] fp32 (NULL: zeros), with logp, entropy and lse as the forward call left them:
  *   dz[t, v] = (dlogp ([v == target] - p) - dentropy p (log p + entropy)) / temperature;  dx = dz . W;  dW = dz^T . x
- * Sizes, pieces of the vocabulary and rounding as moe_head_ce_bwd, and the workspace too, unless the product goes in parts as above (not in pieces of the vocabulary).
+ * Sizes, pieces of the vocabulary and rounding as moe_head_ce_bwd; dW takes what rounding dz loses for up to 256 tokens that count.  ws at least
+ * moe_head_score_bwd_workspace_bytes(T, d, V, v_piece).
  */
 size_t moe_head_score_bwd_workspace_bytes(int T, int d, int V, int v_piece);
 int moe_head_score_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, const float* logp, const float* entropy,

@@ -36,6 +36,10 @@ constexpr int ALL_TOKENS = 256, ALL_TAUGHT = 128;
 // Training steps without / with, us: 100 tokens of d 2048, V 50304 216 / 222; 128, 1088, 32003 99 / 105; 90, 320, 500 37 / 39; up to 32 the same, as the
 // reduction is padded to 64 rows.
 constexpr int LOW_TOKENS = 128;
+// Scores: gradients of log probabilities differ in size, so that fewer tokens make up most of dW (256 tokens of d 128, V 1847, 40 draws: 1.4 times the error of a product in 32 bits at the
+// median, over 1.5 in one draw of ten; the same as it with this).  Backward without / with, us: 256 tokens of d 128, V 1031 33 / 35; 200, 704, 5000 45 / 48; 256, 1024, 32003
+// 93 / 108; 256, 2048, 50304 200 / 246; 512 of these tokens would take 330 / 435 and average better.
+constexpr int SCORE_LOW_TOKENS = 256;
 constexpr float LOG2E = 1.4426950408889634f;
 
 struct Teacher { const int32_t* ids; const float* logits; float temperature; int K; };
@@ -661,10 +665,10 @@ template <int S> void weigh_bwd(int T, int d, int cols, int depth, bool whole, d
     if (time < best) { best = time; shape = {S, p, q}; }
   }
 }
-BwdShape head_bwd_shape(int T, int d, int cols, bool whole) {
+BwdShape head_bwd_shape(int T, int d, int cols, bool whole, int low = LOW_TOKENS) {
   BwdShape shape{128, 1, 1};
   double best = 1e300;
-  const int depth = T <= LOW_TOKENS ? 2 * T : T;
+  const int depth = T <= low ? 2 * T : T;
   // One reduction step of dW, all of it waiting for memory: two workgroups on a compute unit wait better.  256 / 128 in us: 10 tokens, d 2048, V 50304 110 / 94;
   // 8, 2880, 35317 117 / 96; 1, 832, 61930 62 / 50; 22, 1216, 178071 248 / 257.  (100, 2048, 50304: 119 / 118, as the model has it.)
   if (depth > 64) weigh_bwd<256>(T, d, cols, depth, whole, best, shape);
@@ -689,8 +693,8 @@ struct HeadLayout {
   int strips64, blocks, slots, low;
 };
 // Rows of dz, and of x beside it: those of all tokens, or twice as many as take what rounding loses.
-int head_dz_rows(int T) { return T <= LOW_TOKENS ? 2 * T : T < 2 * LOW_TOKENS ? 2 * LOW_TOKENS : T; }
-HeadLayout head_layout(int T, int d, int V, int K, bool backward) {
+int head_dz_rows(int T, int low) { return T <= low ? 2 * T : T < 2 * low ? 2 * low : T; }
+HeadLayout head_layout(int T, int d, int V, int K, bool backward, int low = LOW_TOKENS) {
   HeadLayout l{};
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t p = at; at += (bytes + 255) & ~static_cast<size_t>(255); return p; };
@@ -698,14 +702,14 @@ HeadLayout head_layout(int T, int d, int V, int K, bool backward) {
   l.strips64 = (V + 63) / 64;
   l.blocks = (T + 15) / 16;
   l.slots = K + 1;
-  l.low = backward ? LOW_TOKENS : 0;
+  l.low = backward ? low : 0;
   l.control = take(CONTROL_INTS * 4);
   l.mask = take((n + 63) / 64 * 8);
   l.row_token = take(4 * n);
   l.token_row = take(4 * n);
   l.target_row = take(4 * n);
   l.target_slot = take(4 * n);
-  l.xc = take(2 * static_cast<size_t>(backward ? head_dz_rows(T) : T) * d);
+  l.xc = take(2 * static_cast<size_t>(backward ? head_dz_rows(T, low) : T) * d);
   const size_t items = static_cast<size_t>(l.blocks) * 16 * l.slots;
   if (K > 0) {
     l.list_start = take(static_cast<size_t>(l.blocks) * (l.strips64 + 1) * 4);
@@ -720,7 +724,7 @@ HeadLayout head_layout(int T, int d, int V, int K, bool backward) {
   return l;
 }
 size_t head_part_bytes(int T, int V) { return static_cast<size_t>(3) * ((V + 63) / 64) * ((T + 15) & ~15) * sizeof(float); }
-size_t head_dz_bytes(int T, int piece) { return (static_cast<size_t>(head_dz_rows(T)) * ((piece + 63) & ~63) * 2 + 255) & ~static_cast<size_t>(255); }
+size_t head_dz_bytes(int T, int piece, int low = LOW_TOKENS) { return (static_cast<size_t>(head_dz_rows(T, low)) * ((piece + 63) & ~63) * 2 + 255) & ~static_cast<size_t>(255); }
 
 struct HeadCall {
   const moe_bf16 *x, *W;
@@ -922,11 +926,12 @@ int run_score_fwd(const HeadCall& c, const ScoreShape& shape, int* edges) {
 }
 
 int run_head_bwd(const HeadCall& c, int v_piece, int dz_parts, int* edges) {
-  const HeadLayout l = head_layout(c.T, c.d, c.V, c.t.K, true);
+  const int low = c.score ? SCORE_LOW_TOKENS : LOW_TOKENS;
+  const HeadLayout l = head_layout(c.T, c.d, c.V, c.t.K, true, low);
   const int piece = head_piece(c.T, c.V, v_piece), wanted = edges != nullptr ? edges[1] : 0;
   uint16_t* dz = reinterpret_cast<uint16_t*>(c.ws + l.big);
-  float* part = reinterpret_cast<float*>(c.ws + l.big + head_dz_bytes(c.T, piece));
-  BwdShape shape = head_bwd_shape(c.T, c.d, piece, piece >= c.V);
+  float* part = reinterpret_cast<float*>(c.ws + l.big + head_dz_bytes(c.T, piece, low));
+  BwdShape shape = head_bwd_shape(c.T, c.d, piece, piece >= c.V, low);
   float* dw_part = part + static_cast<size_t>(shape.dx_parts) * c.T * c.d;
   if (wanted != 0) shape.edge = wanted;
   if (edges != nullptr) edges[1] = shape.edge;
@@ -996,13 +1001,16 @@ extern "C" size_t moe_head_fwd_workspace_bytes(int T, int d, int V, int K) {
   return head_layout(T, d, V, K, false).big + head_part_bytes(T, V);
 }
 
-extern "C" size_t moe_head_bwd_workspace_bytes(int T, int d, int V, int K, int v_piece) {
+namespace {
+size_t head_bwd_bytes(int T, int d, int V, int K, int v_piece, int low) {
   if (bad_head_dims(T, d, V, K) || v_piece < 0 || v_piece % 256 != 0) return 0;
   const int piece = head_piece(T, V, v_piece);
-  const BwdShape shape = head_bwd_shape(T, d, piece, piece >= V);
-  return head_layout(T, d, V, K, true).big + head_dz_bytes(T, piece) +
+  const BwdShape shape = head_bwd_shape(T, d, piece, piece >= V, low);
+  return head_layout(T, d, V, K, true, low).big + head_dz_bytes(T, piece, low) +
          (static_cast<size_t>(shape.dx_parts) * T + (shape.dw_parts > 1 ? static_cast<size_t>(shape.dw_parts) * V : 0)) * d * sizeof(float);
 }
+}  // namespace
+extern "C" size_t moe_head_bwd_workspace_bytes(int T, int d, int V, int K, int v_piece) { return head_bwd_bytes(T, d, V, K, v_piece, LOW_TOKENS); }
 
 // Both losses, or (ids null, K 0) the cross entropy alone: what the calls of moe_hotpath.h come to.  edges, for tests: as in gemm.h, of the
 // logits' launch, then (backward) of dx and dW together.
@@ -1067,10 +1075,10 @@ extern "C" int moe_head_distill_bwd(const moe_bf16* x, const moe_bf16* W, const 
 // logits in p parts.
 namespace {
 size_t score_bwd_bytes(int T, int d, int V, int v_piece, int wanted) {
-  const size_t all = moe_head_bwd_workspace_bytes(T, d, V, 0, v_piece);
+  const size_t all = head_bwd_bytes(T, d, V, 0, v_piece, SCORE_LOW_TOKENS);
   if (all == 0) return 0;
   const int piece = head_piece(T, V, v_piece), parts = score_dz_parts(T, d, V, piece, wanted);
-  const size_t least = head_layout(T, d, V, 0, true).big + head_dz_bytes(T, piece) + (parts > 1 ? score_part_bytes(T, V, {true, 128, parts}) : 0);
+  const size_t least = head_layout(T, d, V, 0, true, SCORE_LOW_TOKENS).big + head_dz_bytes(T, piece, SCORE_LOW_TOKENS) + (parts > 1 ? score_part_bytes(T, V, {true, 128, parts}) : 0);
   return all > least ? all : least;
 }
 bool bad_score(int T, int d, int V, int K) { return bad_head_dims(T, d, V, 0) || K < 0 || K > SCORE_MAX_K || K > V; }

@@ -6,8 +6,8 @@ HALF16 = torch.finfo(torch.bfloat16).eps / 2
 HALF32 = torch.finfo(torch.float32).eps / 2
 
 
-def score(x, W, target, K=0, tau=1.0, dlogp=None, dentropy=None):
-    """Results in 64 bits, straight from their definitions, and for each a bound on the kernel's error."""
+def score(x, W, target, K=0, tau=1.0, dlogp=None, dentropy=None, low=False):
+    """Results in 64 bits, straight from their definitions, and for each a bound on the kernel's error.  low: dW takes what rounding dz loses, rounded once more."""
     T, d = x.shape
     V = W.shape[0]
     xd, Wd = x.to(F64), W.to(F64)
@@ -51,6 +51,8 @@ def score(x, W, target, K=0, tau=1.0, dlogp=None, dentropy=None):
         err = HALF16 * dz.abs() + 8 * (tol + 8 * HALF32) * big
         out["dx"], out["dW"] = dz @ Wd, dz.t() @ xd
         bound["dx"] = HALF16 * out["dx"].abs() + err @ Wd.abs() + V * HALF32 * (dz.abs() @ Wd.abs()) + 1e-38
+        if low:
+            err = err - (HALF16 - HALF16 ** 2) * dz.abs()
         bound["dW"] = HALF16 * out["dW"].abs() + err.t() @ xd.abs() + T * HALF32 * (dz.abs().t() @ xd.abs()) + 1e-38
     return out, bound
 
