@@ -204,8 +204,8 @@ template <int THREADS, typename Above, typename Put> __device__ __forceinline__ 
   }
 }
 
-// The logits of columns[0 .. m], in 64 bits.  Sixteen lanes take a row of W, or, where there are few tokens and long rows, a wave: one latency then instead of several.
-template <int THREADS> __device__ __forceinline__ void form_exact(const moe_bf16* x, const moe_bf16* W, int d, const int32_t* columns, double* exact, int m) {
+// The logits of columns[0 .. m], in 64 bits.  Sixteen lanes take a row of W, or, where there are few tokens or (TWO) rows and these are long, a wave: one latency then instead of several.
+template <int THREADS, bool TWO> __device__ __forceinline__ void form_exact(const moe_bf16* x, const moe_bf16* W, int d, const int32_t* columns, double* exact, int m) {
   const int tid = threadIdx.x, wave = tid / MOE_WAVE;
   const auto form = [&](auto lanes, auto at_once, auto ahead) __attribute__((always_inline)) {
     constexpr int LANES = decltype(lanes)::value, N = decltype(at_once)::value, SETS = THREADS / LANES;
@@ -222,7 +222,7 @@ template <int THREADS> __device__ __forceinline__ void form_exact(const moe_bf16
     }
   };
   constexpr bool FEW = THREADS > 256;
-  if (FEW && d > 512) form(std::integral_constant<int, MOE_WAVE>{}, std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
+  if ((FEW || TWO) && d > 512) form(std::integral_constant<int, MOE_WAVE>{}, std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
   else form(std::integral_constant<int, 16>{}, std::integral_constant<int, FEW ? 1 : 2>{}, std::integral_constant<int, 4>{});
 }
 // The K largest of m of these, in the order of their logits, of equal ones the lower column first.
@@ -369,7 +369,7 @@ template <int THREADS, int PIECES, bool LISTS> __global__ __launch_bounds__(THRE
   }
   if (tid == 0) columns[m] = y;
   __syncthreads();
-  form_exact<THREADS>(a.x + static_cast<size_t>(t) * a.d, a.W, a.d, columns, exact, m);
+  form_exact<THREADS, !LISTS>(a.x + static_cast<size_t>(t) * a.d, a.W, a.d, columns, exact, m);
   __syncthreads();
   ScoreSum all;
   all.e = e;
@@ -560,7 +560,7 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
     if (tid == 0) columns[m] = y;
     __syncthreads();
   }
-  form_exact<THREADS>(a.x + static_cast<size_t>(t) * a.d, a.W, a.d, columns, exact, m);
+  form_exact<THREADS, false>(a.x + static_cast<size_t>(t) * a.d, a.W, a.d, columns, exact, m);
   __syncthreads();
   ScoreSum all;
 #pragma unroll
