@@ -862,8 +862,8 @@ int score_edge(int T, int d, int V, int K, bool whole) {
 }
 // Parts of the reduction over d that the logits' product goes in, with tiles of 128, where these are few: a step takes 0.33 us, more where a compute unit has two tiles, and
 // a part's sums are written and read again (1.4 us a million, and 0.4).  one: the logits are written in one part too; else what follows takes `behind` us more.
-// us, from a graph (15 us of them are its own), whole / in the parts of the rule: forward without alternatives, 1 token, d 4096, V 256 42 / 29; 16, 4096, 5000 44 / 34; 500, 2048,
-// 1031 37 / 33; with 20 alternatives 8, 2112, 610 36 / 30; 1 token 50 / 31; 64, 2048, 16000 43 / 38 (strips / 2 parts); 500, 2048, 1031 47 / 39; 1500, 3584, 1000 100 / 89; 2000,
+// us, from a graph (15 us of them are its own), whole / in the parts of the rule: forward without alternatives, 1 token, d 4096, V 256 42 / 24; 16, 4096, 5000 44 / 29; 500, 2048,
+// 1031 37 / 31; with 20 alternatives 8, 2112, 610 36 / 27; 1 token 50 / 31; 64, 2048, 16000 43 / 38 (strips / 2 parts); 500, 2048, 1031 47 / 39; 1500, 3584, 1000 100 / 89; 2000,
 // 4096, 1500 120 / 116 (8 parts: 135); backward 8, 2112, 610 41 / 34; 16, 4096, 5000 70 / 56; 500, 2048, 1031 59 / 53; 2000, 2048, 256 61 / 54 (256, 1024, 8000 in 2: 56 / 60).
 int score_parts(int T, int d, int V, int edge, bool one, double behind) {
   if (V > SCORE_WHOLE_V || edge != 128) return 1;

@@ -611,6 +611,7 @@ __global__ __launch_bounds__(256) void head_score_dz_kernel(ScoreDzArgs a) {
 // Threads for a token whose logits are all looked at, each with 32 of them at most: many where there are few tokens, few where there are many (d 832, us of the whole call,
 // 64 / 128 / 256 threads: V 697, 8 alternatives, 500 tokens 36 / 35 / 32, 2000 42 / 44 / 53, 8000 84 / 102 / 145; V 4000, 20 alternatives, 128 / 256: 500 44 / 40, 8000 188 / 214).
 // Short rows in registers for them alone: 8192 tokens, d 2048, V 256, 20 alternatives, with 8 / 2 pieces a thread 146 / 131; 300, 704, 697 33 / 31.
+// A few tokens, their rows formed anew by waves, 256 / 1024 threads: 16, 4096, 5000 39 / 35.5; 200, 2048, 3001 36 / 34; 1, 4096, 256 29.5 / 35.
 // (64 threads are 64 groups: with as many alternatives wanted nearly every column would be a candidate.)
 void launch_whole(const ScoreJoinArgs& a, dim3 grid, hipStream_t s) {
   const auto launch = [&](auto threads, auto pieces) {
@@ -620,7 +621,8 @@ void launch_whole(const ScoreJoinArgs& a, dim3 grid, hipStream_t s) {
   };
   using std::integral_constant;
   const bool few = a.T <= SCORE_SOME;
-  if (!few && a.V <= 512 && score_wanted(a.K) <= 32) launch(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  if (a.K > 0 && a.T <= SCORE_FEW && a.V > 2048 && a.V <= 8192) launch(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+  else if (!few && a.V <= 512 && score_wanted(a.K) <= 32) launch(integral_constant<int, 64>{}, integral_constant<int, 2>{});
   else if (!few && a.V <= 2048 && score_wanted(a.K) <= 32) launch(integral_constant<int, 64>{}, integral_constant<int, 8>{});
   else if (few && a.V <= 2048) launch(integral_constant<int, 256>{}, integral_constant<int, 2>{});
   else if (!few && a.V <= 4096) launch(integral_constant<int, 128>{}, integral_constant<int, 8>{});
