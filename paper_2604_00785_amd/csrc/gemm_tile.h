@@ -151,7 +151,7 @@ struct GemmArgs {
 struct HeadItem { uint32_t at, slot; };   // at: row in the block | column << 4
 struct HeadArgs {
   float* part;                // HEAD_TOP: HeadStrip, or (two 0) HeadBest, [row][strips of HALF columns], or (two 2) the logits, [part][M rows][slots].  HEAD_STATS: [row block][strips of HALF columns][2 or (two) 3][16 rows]: maximum, sum and sum at the temperature, without the items
-  const f32x4_t* row;         // HEAD_DZ: per row log2(e) lse, factor, and the same at the temperature.  HEAD_SCORE_DZ: l, u, v of 2^t (u + v t), t = c1 z - l
+  const f32x4_t* row;         // HEAD_DZ: per row log2(e) lse, factor, and the same at the temperature.  HEAD_SCORE_DZ: l, u, v of 2^t (u + v t), t = c1 z - l, and what score_apart looks at
   const int32_t* target;      // [row]
   const int32_t* list_start;  // [row block][list_ld]: first item of each strip; null: no teacher
   const HeadItem* items;      // [row block][16 slots]
@@ -1709,6 +1709,17 @@ __device__ __forceinline__ int gemm_tile_list(const GemmArgs& a, int first_tile,
             const float g = __builtin_amdgcn_exp2f(t) * p[1];
             return two ? __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(z, c2, -p[2])), p[3], g) : g;
           };
+          if constexpr (MODE == HEAD_SCORE_DZ) {
+            // A column that another kernel has to look after is marked here, one of a row's in all tiles.  (With the comparison at every element instead of the largest of a
+            // lane's: 8192 rows of d 2048, V 50304 1340 -> 1460 us.)
+            float m = v[0][0];
+#pragma unroll
+            for (int k = 1; k < 4 * NB; ++k) m = __builtin_elementwise_maximum(m, v[k / 4][k % 4]);
+            if (__ballot(score_apart(m, c1, p)) != 0) {
+#pragma unroll
+              for (int k = 0; k < 4 * NB; ++k) v[k / 4][k % 4] = score_apart(v[k / 4][k % 4], c1, p) ? __builtin_nanf("") : v[k / 4][k % 4];
+            }
+          }
           if (has_items(i_tag)) {
             // the gradient at the items replaces their logits; a lane knows it by its bits, which are made to differ from the logit's
             put_logits(v);

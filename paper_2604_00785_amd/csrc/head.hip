@@ -47,13 +47,25 @@ struct Teacher { const int32_t* ids; const float* logits; float temperature; int
 __device__ __forceinline__ bool entry_there(int id, float l, int V) { return id >= 0 && id < V && l > -__builtin_inff(); }
 __device__ __forceinline__ bool target_there(int y, int V) { return y >= 0 && y < V; }
 
-// Which tokens have a loss, a bit each: a target, or (K > 0) an entry.  A workgroup takes 16 tokens, sixteen threads each.
-__global__ __launch_bounds__(256) void head_mask_kernel(const int32_t* __restrict__ target, Teacher t, int T, int V, uint16_t* __restrict__ mask) {
-  __shared__ uint32_t bits[4];
+// The gradient of a token's entropy, -p (log p + entropy) at a column, is small beside either summand where the model is sure of one column, and 32 bits of lse leave an error
+// of 2^-24 of the logits' size in log p: of the gradient of an entropy of 1e-5 nothing would be left.  If that column is the target its log p is known.  Otherwise, from this
+// entropy down (a column has a p of 0.77 at least then, all others together 0.23), the row is SURE, and its likeliest column's gradient is what those of the others, which
+// lose nothing, leave of zero: head_sure_kernel adds these up.  In pieces of the vocabulary a piece does not know the others': there the rows' sums are formed again as in
+// the forward call, and log p with them.  Above this entropy the summands are 1/4 and more.
+constexpr float SURE_ENTROPY = 0.25f, LOG_HALF = -0.693147180559945309f;
+__device__ __forceinline__ bool sure_there(float logp, float entropy, float dentropy) { return entropy < SURE_ENTROPY && logp < LOG_HALF && dentropy != 0.f; }
+struct SureArgs { const float *logp, *entropy, *dentropy; };
+__device__ __forceinline__ bool sure_there(const SureArgs& s, int t) { return sure_there(s.logp[t], s.entropy[t], s.dentropy[t]); }
+
+// Which tokens have a loss, a bit each: a target, or (K > 0) an entry; and (sure not null) which of them are SURE.  A workgroup takes 16 tokens, sixteen threads each.
+__global__ __launch_bounds__(256) void head_mask_kernel(const int32_t* __restrict__ target, Teacher t, int T, int V, SureArgs s, uint16_t* __restrict__ mask,
+                                                        uint16_t* __restrict__ sure) {
+  __shared__ uint32_t bits[4], of_sure[4];
   const int tid = threadIdx.x, l16 = tid & 15, token = blockIdx.x * 16 + (tid >> 4);
-  bool some = false;
+  bool some = false, is_sure = false;
   if (token < T) {
     some = l16 == 0 && target_there(target[token], V);
+    is_sure = sure != nullptr && some && sure_there(s, token);
     const size_t at = static_cast<size_t>(token) * t.K;
 #pragma unroll 4
     for (int j = l16; j < t.K; j += 16) {
@@ -62,18 +74,24 @@ __global__ __launch_bounds__(256) void head_mask_kernel(const int32_t* __restric
       some = some || entry_there(id, l, V);
     }
   }
-  const uint64_t any = __ballot(some);
-  uint32_t four = 0;
+  const uint64_t any = __ballot(some), any_sure = __ballot(is_sure);
+  uint32_t four = 0, four_sure = 0;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) four |= (any >> (16 * k) & 0xFFFFu) != 0 ? 1u << k : 0u;
-  if (tid % MOE_WAVE == 0) bits[tid / MOE_WAVE] = four;
+  for (int k = 0; k < 4; ++k) {
+    four |= (any >> (16 * k) & 0xFFFFu) != 0 ? 1u << k : 0u;
+    four_sure |= (any_sure >> (16 * k) & 0xFFFFu) != 0 ? 1u << k : 0u;
+  }
+  if (tid % MOE_WAVE == 0) { bits[tid / MOE_WAVE] = four; of_sure[tid / MOE_WAVE] = four_sure; }
   __syncthreads();
-  if (tid == 0) mask[blockIdx.x] = static_cast<uint16_t>(bits[0] | bits[1] << 4 | bits[2] << 8 | bits[3] << 12);
+  if (tid == 0) {
+    mask[blockIdx.x] = static_cast<uint16_t>(bits[0] | bits[1] << 4 | bits[2] << 8 | bits[3] << 12);
+    if (sure != nullptr) sure[blockIdx.x] = static_cast<uint16_t>(of_sure[0] | of_sure[1] << 4 | of_sure[2] << 8 | of_sure[3] << 12);
+  }
 }
 
 // What head_prep leaves for the kernels behind it, as integers: rows of the products from 0 to LIVE; those of dW, with the low parts, from 0
-// to DW_ROWS; whether x itself holds the rows.
-enum { ROWS = 0, LIVE = 1, DW_ROWS = 3, DIRECT = 4, DX_PARTS = 5, CONTROL_INTS = 6 };
+// to DW_ROWS; whether x itself holds the rows; SURE rows from 0 to SURE.
+enum { ROWS = 0, LIVE = 1, DW_ROWS = 3, DIRECT = 4, DX_PARTS = 5, SURE = 7, CONTROL_INTS = 8 };
 
 // Parts of dx's reduction for `rows` rows, at most `most`: the number with which dx and dW together take least time (head_bwd_time), each part's sums
 // being written and read besides (8 bytes an element, 7 MB in the model's unit of time).  Lane p - 1 of a wave weighs p parts.
@@ -94,7 +112,7 @@ struct HeadPrepArgs {
   const moe_bf16* x;
   const int32_t* target;
   Teacher t;
-  const uint64_t* mask;            // null: found here (no teacher), or all
+  const uint64_t *mask, *sure;     // mask null: found here (no teacher), or all
   int all;                         // every token is a row (with a teacher); rows without a loss are zeros
   int T, d, V, strips;             // strips: of 64 columns
   int low;                         // up to so many rows: rows of x twice
@@ -115,17 +133,17 @@ struct HeadPrepArgs {
   float over_tau;
 };
 
-// Workgroup (b, 0): rows 16 b to 16 b + 15 of those with a loss, in the order of their tokens; and tokens 16 b to 16 b + 15, if they have none.
+// Workgroup (b, 0): rows 16 b to 16 b + 15 of those with a loss, in the order of their tokens (SORTED: SURE ones first); and tokens 16 b to 16 b + 15, if they have none.
 // Workgroups (b, 1 ..) help with the rows of x.  Sixteen threads share a row and its entries.  A workgroup behind those of the rows writes down what is
 // found for all.  (The kernel is one chain of a few us, and short code is part of that: it is fetched cold.)
-__global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
+template <bool SORTED> __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   extern __shared__ int count[];                     // [strips + 1]
-  __shared__ uint64_t own[SELF_MASK_TOKENS / 64];
-  __shared__ int wave_sum[4], s_token[16], s_slot[16], s_zero[16];
+  __shared__ uint64_t own[SELF_MASK_TOKENS / 64], own_sure[SORTED ? SELF_MASK_TOKENS / 64 : 1];
+  __shared__ int wave_sum[4], wave_sure[4], s_token[16], s_slot[16], s_zero[16];
   const int tid = threadIdx.x, lane = tid % MOE_WAVE, wave = tid / MOE_WAVE;
-  const int words = (a.T + 63) / 64, per = (words + 255) / 256, K = a.t.K, V = a.V, slots = K + 1;
+  const int words = (a.T + 63) / 64, all_words = SORTED ? 2 * words : words, per = (all_words + 255) / 256, K = a.t.K, V = a.V, slots = K + 1;
   const bool lists = blockIdx.y == 0;
-  const uint64_t* mask = a.mask;
+  const uint64_t *mask = a.mask, *sure = a.sure;
   if (mask == nullptr && !a.all) {
     constexpr int WORDS = SELF_MASK_TOKENS / 256;        // of a wave, requested together
     int y[WORDS];
@@ -140,24 +158,44 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
       if (lane == 0) own[wave + 4 * i] = bits;
     }
     mask = own;
+    if constexpr (SORTED) {
+      const SureArgs s{a.in_loss, a.in_entropy, a.dentropy};
+#pragma unroll 4
+      for (int i = 0; (wave + 4 * i) * 64 < a.T; ++i) {
+        const int t = (wave + 4 * i) * 64 + lane;
+        const uint64_t bits = __ballot(t < a.T && target_there(a.target[t], V) && sure_there(s, t));
+        if (lane == 0) own_sure[wave + 4 * i] = bits;
+      }
+      sure = own_sure;
+    }
   }
+  // (SORTED: the words of SURE tokens, then those of the others)
+  const auto word = [&](int w) __attribute__((always_inline)) -> uint64_t { return !SORTED ? mask[w] : w < words ? sure[w] : mask[w - words] & ~sure[w - words]; };
   if (tid < 16) { s_token[tid] = a.all && static_cast<int>(blockIdx.x) * 16 + tid < a.T ? blockIdx.x * 16 + tid : -1; s_slot[tid] = K; }
   if (lists && K > 0) for (int i = tid; i <= a.strips; i += 256) count[i] = 0;
   __syncthreads();
   // rank of each thread's first token among those with a loss
-  const int w0 = tid * per < words ? tid * per : words, w1 = w0 + per < words ? w0 + per : words;
-  int mine = 0;
-  if (!a.all) for (int w = w0; w < w1; ++w) mine += __builtin_popcountll(mask[w]);
+  const int w0 = tid * per < all_words ? tid * per : all_words, w1 = w0 + per < all_words ? w0 + per : all_words;
+  int mine = 0, mine_sure = 0;
+  if (!a.all) for (int w = w0; w < w1; ++w) {
+    const int n = __builtin_popcountll(word(w));
+    mine += n;
+    if (SORTED && w < words) mine_sure += n;
+  }
   int rank = wave_incl_scan(mine);
   if (lane == 63) wave_sum[wave] = rank;
+  if constexpr (SORTED) {
+    mine_sure = wave_incl_scan(mine_sure);
+    if (lane == 63) wave_sure[wave] = mine_sure;
+  }
   __syncthreads();
-  int live = 0;
+  int live = 0, sures = 0;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) { rank += w < wave ? wave_sum[w] : 0; live += wave_sum[w]; }
+  for (int w = 0; w < 4; ++w) { rank += w < wave ? wave_sum[w] : 0; live += wave_sum[w]; sures += SORTED ? wave_sure[w] : 0; }
   rank -= mine;
   if (a.all) live = a.T;
   const int first = blockIdx.x * 16;
-  const bool low = live <= a.low, direct = a.all ? a.row == nullptr : live == a.T && !low;
+  const bool low = live <= a.low, direct = a.all ? a.row == nullptr : live == a.T && !low && sures == 0;
   if (blockIdx.x == gridDim.x - 1) {
     if (!lists || wave != 0) return;
     int parts = 1;
@@ -173,6 +211,7 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
       a.control[DW_ROWS - 1] = 0; a.control[DW_ROWS] = low ? 2 * live : live;
       a.control[DIRECT] = direct;
       a.control[DX_PARTS] = parts;
+      if constexpr (SORTED) { a.control[SURE - 1] = 0; a.control[SURE] = sures; }
     }
     return;
   }
@@ -190,12 +229,12 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
   if (first >= live || (direct && !lists)) return;
   // the words that hold ranks first to first + 15, a bit a lane
   for (uint64_t hit = __ballot(mine > 0 && rank < first + 16 && rank + mine > first); hit != 0; hit &= hit - 1) {
-    const int l = __builtin_ctzll(hit), from = (wave * MOE_WAVE + l) * per, to = from + per < words ? from + per : words;
+    const int l = __builtin_ctzll(hit), from = (wave * MOE_WAVE + l) * per, to = from + per < all_words ? from + per : all_words;
     int at = wave_lane(rank, l);
     for (int w = from; w < to; ++w) {
-      const uint64_t bits = mask[w];
+      const uint64_t bits = word(w);
       const int rk = at + __builtin_popcountll(bits & ((1ull << lane) - 1));
-      if ((bits >> lane & 1) != 0 && rk >= first && rk < first + 16) s_token[rk - first] = w * 64 + lane;
+      if ((bits >> lane & 1) != 0 && rk >= first && rk < first + 16) s_token[rk - first] = (SORTED && w >= words ? w - words : w) * 64 + lane;
       at += __builtin_popcountll(bits);
     }
   }
@@ -258,9 +297,10 @@ __global__ __launch_bounds__(256) void head_prep_kernel(HeadPrepArgs a) {
     if (l16 == 0 && r < n) {
       a.target_row[first + r] = y;
       if (a.in_entropy != nullptr) {
-        // dz = -p (u + v (log p + entropy)) / temperature, and at the target u (1 - p) in place of -u p
+        // dz = -p (u + v (log p + entropy)) / temperature, and at the target u (1 - p) in place of -u p.  The last term of a SURE row is not above 0 (SORTED: log2 p at its
+        // likeliest column, as the join puts it there), of another it is 1.
         const float entropy = a.in_entropy[t], u = gl * a.over_tau, v = a.dentropy != nullptr ? a.dentropy[t] * a.over_tau : 0.f;
-        a.row[first + r] = f32x4_t{in_lse * LOG2E, -__builtin_fmaf(v, entropy, u), v * -0.693147180559945309f, 0.f};
+        a.row[first + r] = f32x4_t{in_lse * LOG2E, -__builtin_fmaf(v, entropy, u), v * -0.693147180559945309f, sure_there(in_loss, entropy, v) ? -1.f : 1.f};
         a.terms[first + r] = f32x4_t{-__builtin_fmaf(expm1f(in_loss), u, expf(in_loss) * v * (in_loss + entropy)), 0.f, 0.f, 0.f};
       } else if (a.row != nullptr) {
         a.row[first + r] = f32x4_t{in_lse * LOG2E, gl, 0.f, 0.f};
@@ -542,6 +582,55 @@ __device__ __forceinline__ void store8(moe_bf16* to, const f32x4_t (&v)[2]) {
   *reinterpret_cast<u4*>(to) = u4{pack_bf16(v[0][0], v[0][1]), pack_bf16(v[0][2], v[0][3]), pack_bf16(v[1][0], v[1][1]), pack_bf16(v[1][2], v[1][3])};
 }
 
+// The gradient of a SURE row's likeliest column, the one that is NaN: from its log2 p (formed), or such that all of the row's are zero together.  What a row has of NaN
+// otherwise it keeps.  A workgroup takes `each` rows, one after the other; with low parts (of rows up to `low`) gradients are the sums of both.
+// (8192 tokens of V 50304, 7 in 100 SURE: 17 us; none: 4.)
+constexpr int SURE_GROUPS = 4096;
+__global__ __launch_bounds__(256) void head_sure_kernel(const int32_t* __restrict__ control, const f32x4_t* __restrict__ row, uint16_t* __restrict__ dz, int T, int ld, int each, int low,
+                                                        int formed) {
+  typedef __attribute__((ext_vector_type(4))) uint32_t u4;
+  __shared__ float sums[4];
+  const int tid = threadIdx.x, lane = tid % MOE_WAVE, first = blockIdx.x * each, last = first + each < T ? first + each : T;
+  for (int r0 = first; r0 < last; r0 += MOE_WAVE) {
+    const float mark = row[r0 + lane < last ? r0 + lane : r0][3];        // (requested together with the number of rows)
+    const int rows = control[LIVE];
+    const bool lows = rows <= low;
+    for (uint64_t left = __ballot(r0 + lane < last && r0 + lane < rows && mark <= 0.f); left != 0; left &= left - 1) {
+      const int r = r0 + __builtin_ctzll(left);
+      uint16_t *const high = dz + static_cast<size_t>(r) * ld, *const rest = dz + static_cast<size_t>(rows + r) * ld;
+      float sum = 0.f;
+      int found = 0, at = 0;
+      for (int c0 = tid * 8; c0 < ld; c0 += 4 * 256 * 8) {
+        u4 v[4], w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int c = c0 + k * 256 * 8;
+          v[k] = w[k] = u4{0, 0, 0, 0};
+          if (c < ld) v[k] = *reinterpret_cast<const u4*>(high + c);
+          if (lows && c < ld) w[k] = *reinterpret_cast<const u4*>(rest + c);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float g = i & 1 ? bf16hi(v[k][i >> 1]) : bf16lo(v[k][i >> 1]), l = i & 1 ? bf16hi(w[k][i >> 1]) : bf16lo(w[k][i >> 1]);
+            if (g != g) { ++found; at = c0 + k * 256 * 8 + i; }
+            else sum += g + l;
+          }
+      }
+      sum = wave_sum_of(sum);
+      if (lane == 0) sums[tid / MOE_WAVE] = sum;
+      if (__syncthreads_count(found) == 1 && found == 1) {
+        const f32x4_t p = row[r];
+        const float g = formed ? __builtin_amdgcn_exp2f(p[3]) * __builtin_fmaf(p[2], p[3], p[1]) : -((sums[0] + sums[1]) + (sums[2] + sums[3]));
+        high[at] = f32_to_bf16(g);
+        if (lows) rest[at] = f32_to_bf16(g - bf16_to_f32(f32_to_bf16(g)));
+      }
+      __syncthreads();
+    }
+  }
+}
+
 struct HeadDxArgs {
   const float* part;
   const int32_t* control;
@@ -689,7 +778,7 @@ int logits_edge(int rows, int cols, int d, double more, double behind128 = 0.0, 
 
 // What the workspace holds, by offset.
 struct HeadLayout {
-  size_t control, mask, row_token, token_row, target_row, target_slot, xc, list_start, items, terms, item, row, big;   // terms, row: of the backward pass
+  size_t control, mask, sure, row_token, token_row, target_row, target_slot, xc, list_start, items, terms, item, row, big;   // terms, row: of the backward pass
   int strips64, blocks, slots, low;
 };
 // Rows of dz, and of x beside it: those of all tokens, or twice as many as take what rounding loses.
@@ -705,6 +794,7 @@ HeadLayout head_layout(int T, int d, int V, int K, bool backward, int low = LOW_
   l.low = backward ? low : 0;
   l.control = take(CONTROL_INTS * 4);
   l.mask = take((n + 63) / 64 * 8);
+  l.sure = take((n + 63) / 64 * 8);
   l.row_token = take(4 * n);
   l.token_row = take(4 * n);
   l.target_row = take(4 * n);
@@ -745,16 +835,17 @@ struct HeadCall {
   const float *in_entropy, *dentropy;
 };
 
-int run_prep(const HeadCall& c, const HeadLayout& l, const BwdRule& dx, long long dx_room) {
-  uint64_t* mask = nullptr;
+int run_prep(const HeadCall& c, const HeadLayout& l, const BwdRule& dx, long long dx_room, bool sorted = false) {
+  uint64_t *mask = nullptr, *sure = nullptr;
   const bool all = c.t.K > 0 && c.T <= ALL_TAUGHT;
   if (!all && (c.t.K > 0 || c.T > SELF_MASK_TOKENS)) {
     mask = reinterpret_cast<uint64_t*>(c.ws + l.mask);
-    MOE_LAUNCH("head_mask", head_mask_kernel, dim3((c.T + 63) / 64 * 4), dim3(256), 0, c.s, c.target, c.t, c.T, c.V,
-               reinterpret_cast<uint16_t*>(mask));
+    if (sorted) sure = reinterpret_cast<uint64_t*>(c.ws + l.sure);
+    MOE_LAUNCH("head_mask", head_mask_kernel, dim3((c.T + 63) / 64 * 4), dim3(256), 0, c.s, c.target, c.t, c.T, c.V, SureArgs{c.in_loss, c.in_entropy, c.dentropy},
+               reinterpret_cast<uint16_t*>(mask), reinterpret_cast<uint16_t*>(sure));
   }
   HeadPrepArgs p{};
-  p.x = c.x; p.target = c.target; p.t = c.t; p.mask = mask; p.T = c.T; p.d = c.d; p.V = c.V; p.strips = l.strips64;
+  p.x = c.x; p.target = c.target; p.t = c.t; p.mask = mask; p.sure = sure; p.T = c.T; p.d = c.d; p.V = c.V; p.strips = l.strips64;
   p.low = l.low;
   p.all = all;
   p.dx = dx; p.dx_room = dx_room;
@@ -777,10 +868,13 @@ int run_prep(const HeadCall& c, const HeadLayout& l, const BwdRule& dx, long lon
     p.row = reinterpret_cast<f32x4_t*>(c.ws + l.row);
   }
   const int lds = (l.strips64 + 1) * 4;
-  static bool configured[MAX_DEVICES] = {};
-  if (configure_lds(&head_prep_kernel, (HEAD_MAX_V / 64 + 1) * 4, configured) != MOE_OK) return MOE_ERR_LAUNCH;
-  MOE_LAUNCH("head_prep", head_prep_kernel, dim3(l.blocks + 1, (c.d + 1023) / 1024), dim3(256), lds, c.s, p);
-  return moe_check_launch();
+  const auto launch = [&](auto kernel, bool (&configured)[MAX_DEVICES]) {
+    if (configure_lds(kernel, (HEAD_MAX_V / 64 + 1) * 4, configured) != MOE_OK) return static_cast<int>(MOE_ERR_LAUNCH);
+    MOE_LAUNCH("head_prep", kernel, dim3(l.blocks + 1, (c.d + 1023) / 1024), dim3(256), lds, c.s, p);
+    return moe_check_launch();
+  };
+  static bool of_sorted[MAX_DEVICES] = {}, of_others[MAX_DEVICES] = {};
+  return sorted ? launch(&head_prep_kernel<true>, of_sorted) : launch(&head_prep_kernel<false>, of_others);
 }
 
 void fill_head(const HeadCall& c, const HeadLayout& l, GemmArgs& a, HeadArgs& h) {
@@ -921,10 +1015,15 @@ int run_score_fwd(const HeadCall& c, const ScoreShape& shape, int* edges) {
   if ((rc = launch_logits<HEAD_TOP>(a, h, edge, c.T, "gemm_head_top", c.s)) != MOE_OK) return rc;
   const ScoreJoinArgs j{h.part, all ? nullptr : reinterpret_cast<const int32_t*>(c.ws + l.control),
                         reinterpret_cast<const int32_t*>(c.ws + l.token_row), c.target, c.x, c.W, c.T, c.d, c.V, c.K, h.strips, shape.whole, shape.parts, h.c1, 1.0 / c.tau,
-                        c.loss, c.entropy, c.lse, c.ids, c.top};
+                        c.loss, c.entropy, c.lse, c.ids, c.top, nullptr, nullptr, nullptr};
   return moe_head_score_join(j, edge, c.s);
 }
 
+// The edge of the tiles that the sums of SURE rows come from, and what they take of the workspace.
+int sure_edge(int T, int d, int V, const int* edges) { return edges != nullptr && edges[0] != 0 ? edges[0] : logits_edge(T, V, d, 9.5); }
+size_t sure_part_bytes(int T, int d, int V, const int* edges) {
+  return static_cast<size_t>((T + 15) & ~15) * ceil_div(V, sure_edge(T, d, V, edges) / 2) * sizeof(HeadBest);
+}
 int run_head_bwd(const HeadCall& c, int v_piece, int dz_parts, int* edges) {
   const int low = c.score ? SCORE_LOW_TOKENS : LOW_TOKENS;
   const HeadLayout l = head_layout(c.T, c.d, c.V, c.t.K, true, low);
@@ -942,9 +1041,25 @@ int run_head_bwd(const HeadCall& c, int v_piece, int dz_parts, int* edges) {
                      static_cast<float>(shape.edge == 256 ? TileCost<256>::FIXED : TileCost<128>::FIXED),
                      static_cast<float>(shape.edge == 256 ? TileCost<256>::WGRAD : TileCost<128>::WGRAD),
                      static_cast<float>(shape.edge == 256 ? TileCost<256>::STEP : TileCost<128>::STEP)};
-  int rc = run_prep(c, l, rule, static_cast<long long>(shape.dx_parts) * c.T);
+  const bool sures = c.score && c.dentropy != nullptr, sorted = sures && piece < c.V;
+  int rc = run_prep(c, l, rule, static_cast<long long>(shape.dx_parts) * c.T, sorted);
   if (rc != MOE_OK) return rc;
   const int32_t* control = reinterpret_cast<const int32_t*>(c.ws + l.control);
+  if (sorted) {                                            // before the gradients take their place
+    GemmArgs a{};
+    HeadArgs h{};
+    fill_head(c, l, a, h);
+    const int edge = sure_edge(c.T, c.d, c.V, edges);
+    a.offsets = control + SURE - 1;
+    a.A0 = reinterpret_cast<const uint16_t*>(c.ws + l.xc); a.A1 = c.x; a.B0 = c.W; a.K = c.d; a.N = c.V; a.M = c.T;
+    h.strips = ceil_div(c.V, edge / 2);
+    h.two = 0;
+    h.part = reinterpret_cast<float*>(c.ws + l.big);
+    if ((rc = launch_logits<HEAD_TOP>(a, h, edge, c.T, "gemm_head_top", c.s)) != MOE_OK) return rc;
+    const ScoreJoinArgs j{h.part, control, nullptr, c.target, c.x, c.W, c.T, c.d, c.V, 0, h.strips, 0, 1, h.c1, 1.0 / c.tau, nullptr, nullptr, nullptr, nullptr, nullptr,
+                          control + SURE, reinterpret_cast<const int32_t*>(c.ws + l.row_token), reinterpret_cast<f32x4_t*>(c.ws + l.row)};
+    if ((rc = moe_head_score_join(j, edge, c.s)) != MOE_OK) return rc;
+  }
   for (int v0 = 0; v0 < c.V; v0 += piece) {
     const int cols = c.V - v0 < piece ? c.V - v0 : piece, ld = (cols + 63) & ~63;
     GemmArgs a{};
@@ -965,6 +1080,11 @@ int run_head_bwd(const HeadCall& c, int v_piece, int dz_parts, int* edges) {
       rc = moe_head_score_dz(g, c.s);
     } else rc = c.score ? launch_logits<HEAD_SCORE_DZ>(a, h, edge, c.T, "gemm_head_score_dz", c.s) : launch_logits<HEAD_DZ>(a, h, edge, c.T, "gemm_head_dz", c.s);
     if (rc != MOE_OK) return rc;
+    if (sures) {
+      const int each = ceil_div(c.T, SURE_GROUPS);
+      MOE_LAUNCH("head_sure", head_sure_kernel, dim3(ceil_div(c.T, each)), dim3(256), 0, c.s, control, h.row, dz, c.T, ld, each, l.low, sorted);
+      if ((rc = moe_check_launch()) != MOE_OK) return rc;
+    }
     GemmArgs b{};
     b.offsets = a.offsets; b.row_token = control + DX_PARTS; b.stream_rows = v0 > 0;
     b.A0 = dz; b.B0 = W; b.O0 = reinterpret_cast<uint16_t*>(part); b.K = ld; b.M = cols; b.N = c.d;
@@ -1074,11 +1194,12 @@ extern "C" int moe_head_distill_bwd(const moe_bf16* x, const moe_bf16* W, const 
 // Log probabilities, entropies and alternatives.  edges, for tests: as above; forward edges[1]: what score_shape calls path; backward edges[0]: 1000 p + edge for
 // logits in p parts.
 namespace {
-size_t score_bwd_bytes(int T, int d, int V, int v_piece, int wanted) {
+size_t score_bwd_bytes(int T, int d, int V, int v_piece, int wanted, const int* edges) {
   const size_t all = head_bwd_bytes(T, d, V, 0, v_piece, SCORE_LOW_TOKENS);
   if (all == 0) return 0;
   const int piece = head_piece(T, V, v_piece), parts = score_dz_parts(T, d, V, piece, wanted);
-  const size_t least = head_layout(T, d, V, 0, true, SCORE_LOW_TOKENS).big + head_dz_bytes(T, piece, SCORE_LOW_TOKENS) + (parts > 1 ? score_part_bytes(T, V, {true, 128, parts}) : 0);
+  const size_t least = head_layout(T, d, V, 0, true, SCORE_LOW_TOKENS).big +
+                       (piece < V ? sure_part_bytes(T, d, V, edges) : head_dz_bytes(T, piece, SCORE_LOW_TOKENS) + (parts > 1 ? score_part_bytes(T, V, {true, 128, parts}) : 0));
   return all > least ? all : least;
 }
 bool bad_score(int T, int d, int V, int K) { return bad_head_dims(T, d, V, 0) || K < 0 || K > SCORE_MAX_K || K > V; }
@@ -1087,7 +1208,7 @@ extern "C" size_t moe_head_score_fwd_workspace_bytes(int T, int d, int V, int K)
   if (bad_score(T, d, V, K)) return 0;
   return head_layout(T, d, V, 0, false).big + score_part_bytes(T, V, score_shape(T, d, V, K, 0));
 }
-extern "C" size_t moe_head_score_bwd_workspace_bytes(int T, int d, int V, int v_piece) { return score_bwd_bytes(T, d, V, v_piece, 0); }
+extern "C" size_t moe_head_score_bwd_workspace_bytes(int T, int d, int V, int v_piece) { return score_bwd_bytes(T, d, V, v_piece, 0, nullptr); }
 
 extern "C" int moe_head_score_fwd_edges(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, int T, int d, int V, int K,
                                         float* logp, float* entropy, float* lse, int32_t* ids, float* top, void* ws, size_t ws_bytes, void* stream,
@@ -1111,7 +1232,7 @@ extern "C" int moe_head_score_bwd_edges(const moe_bf16* x, const moe_bf16* W, co
   if (wanted > 0) edges[0] %= 1000;
   if (bad_head_dims(T, d, V, 0) || bad_temperature(temperature) || v_piece < 0 || v_piece % 256 != 0 || bad_edge_list(edges, 2) || wanted > d / BK) return MOE_ERR_INVALID;
   if (bad_ptrs({x, W, target, logp, entropy, lse, dlogp, dx, dW, ws}) || !moe_aligned16(dentropy)) return MOE_ERR_INVALID;
-  if (ws_bytes < score_bwd_bytes(T, d, V, v_piece, wanted)) return MOE_ERR_WORKSPACE;
+  if (ws_bytes < score_bwd_bytes(T, d, V, v_piece, wanted, edges)) return MOE_ERR_WORKSPACE;
   HeadCall c{};
   c.x = x; c.W = W; c.target = target; c.t.temperature = 1.f; c.T = T; c.d = d; c.V = V;
   c.score = true; c.tau = temperature;

@@ -24,7 +24,14 @@ struct ScoreJoinArgs {
   float *logp, *entropy, *lse;
   int32_t* ids;
   float* top;
+  // of the backward pass (K 0, strips; else null): the first sure_rows[0] rows alone, of which it leaves log2 p of the likeliest column, of_row[row][3]
+  const int32_t *sure_rows, *row_token;
+  f32x4_t* of_row;
 };
+
+// Whether a logit's gradient is formed apart, with the terms of its row: if that is a SURE one (the last term is 0 or less) and the column has more than half of p.  The
+// products leave NaN there.
+__device__ __forceinline__ bool score_apart(float z, float c1, const f32x4_t& row) { return row[3] <= 0.f && __builtin_fmaf(z, c1, -row[0]) > -1.f; }
 
 constexpr int SCORE_WHOLE_V = 16384;
 constexpr int score_ld(int V) { return (V + 3) & ~3; }

@@ -122,20 +122,21 @@ __device__ __forceinline__ void put_scores(const ScoreJoinArgs& a, int t, const 
 }
 
 // Without alternatives: a wave for each token, or (FEW) four (V 50304, us, one / four: 256 tokens 6.4 / 5.5, 1000 8.0 / 8.1, 4000 15 / 21; 8192 23).  HALF: columns of a strip.
-template <int HALF, bool FEW> __global__ __launch_bounds__(256) void head_score_kernel(ScoreJoinArgs a) {
+// SURES: for rows of the backward pass.
+template <int HALF, bool FEW, bool SURES> __global__ __launch_bounds__(256) void head_score_kernel(ScoreJoinArgs a) {
   constexpr int AT_ONCE = 4, STEP = FEW ? 4 * MOE_WAVE : MOE_WAVE;
   typedef __attribute__((ext_vector_type(4))) uint32_t u4;
   __shared__ uint64_t tops[FEW ? 4 : 1];
   __shared__ float parts[FEW ? 4 : 1][3];
   const int lane = threadIdx.x % MOE_WAVE, wave = threadIdx.x / MOE_WAVE, group = blockIdx.y * SCORE_ROW + blockIdx.x;
-  const int t = __builtin_amdgcn_readfirstlane(FEW ? group : group * 4 + wave);
-  if (t >= a.T) return;
-  const int y = a.target[t];
+  const int at = __builtin_amdgcn_readfirstlane(FEW ? group : group * 4 + wave);
+  if (at >= a.T || (SURES && at >= a.sure_rows[0])) return;
+  const int t = SURES ? a.row_token[at] : at, y = a.target[t];
   if (y < 0 || y >= a.V) {
     if (lane == 0) { a.logp[t] = 0.f; a.entropy[t] = 0.f; a.lse[t] = 0.f; }
     return;
   }
-  const int row = a.control != nullptr ? a.token_row[t] : t;
+  const int row = !SURES && a.control != nullptr ? a.token_row[t] : at;
   const u4* const strip = static_cast<const u4*>(a.part) + static_cast<size_t>(row) * a.strips;
   const float c1 = a.c1;
   uint64_t best = 0;
@@ -190,7 +191,10 @@ template <int HALF, bool FEW> __global__ __launch_bounds__(256) void head_score_
   const int col[2] = {top_col, y};
   double z[2];
   exact_logits<MOE_WAVE, 2, 4>(a.x + static_cast<size_t>(t) * a.d, a.W, a.d, col, z);
-  if (lane == 0) put_scores(a, t, result_of(total, top_key != 0, z[0], c1), y == top_col, z[1], z[0]);
+  if (lane != 0) return;
+  const ScoreResult r = result_of(total, top_key != 0, z[0], c1);
+  if constexpr (SURES) reinterpret_cast<float*>(a.of_row + row)[3] = static_cast<float>(r.log_1R * -1.4426950408889634);
+  else put_scores(a, t, r, y == top_col, z[1], z[0]);
 }
 
 // put(i, number of k with above(k, i)) for i and k below n, sixteen threads to an i.
@@ -593,7 +597,7 @@ __global__ __launch_bounds__(256) void head_score_dz_kernel(ScoreDzArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float t = __builtin_fmaf(z[i], a.c1, -p[0]);
-      const float other = __builtin_amdgcn_exp2f(t) * __builtin_fmaf(p[2], t, p[1]);
+      const float other = score_apart(z[i], a.c1, p) ? __builtin_nanf("") : __builtin_amdgcn_exp2f(t) * __builtin_fmaf(p[2], t, p[1]);
       g[h + i] = c + h + i >= a.V ? 0.f : h + i == y ? at_target : other;
       if (h + i == y) a.item[row] = at_target - bf16_to_f32(f32_to_bf16(at_target));
     }
@@ -632,8 +636,13 @@ void launch_whole(const ScoreJoinArgs& a, dim3 grid, hipStream_t s) {
 template <int HALF> void launch_join(const ScoreJoinArgs& a, hipStream_t s) {
   const auto rows = [](int n) { return dim3(n < SCORE_ROW ? n : SCORE_ROW, (n + SCORE_ROW - 1) / SCORE_ROW); };
   if (a.K == 0 && !a.whole) {
-    if (a.T <= SCORE_FEW) MOE_LAUNCH("head_score", (head_score_kernel<HALF, true>), dim3(a.T), dim3(256), 0, s, a);
-    else MOE_LAUNCH("head_score", (head_score_kernel<HALF, false>), rows((a.T + 3) / 4), dim3(256), 0, s, a);
+    const bool few = a.T <= SCORE_FEW;
+    const dim3 grid = few ? dim3(a.T) : rows((a.T + 3) / 4);
+    if (a.of_row != nullptr) {
+      if (few) MOE_LAUNCH("head_score_sure", (head_score_kernel<HALF, true, true>), grid, dim3(256), 0, s, a);
+      else MOE_LAUNCH("head_score_sure", (head_score_kernel<HALF, false, true>), grid, dim3(256), 0, s, a);
+    } else if (few) MOE_LAUNCH("head_score", (head_score_kernel<HALF, true, false>), grid, dim3(256), 0, s, a);
+    else MOE_LAUNCH("head_score", (head_score_kernel<HALF, false, false>), grid, dim3(256), 0, s, a);
     return;
   }
   if (a.whole) {
