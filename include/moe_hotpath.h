@@ -467,7 +467,8 @@ int moe_qk_norm_rope_bwd(const moe_bf16* dqo, long long dqo_ld, const moe_bf16* 
  *   of NaN makes all of them NaN.
  * `grads` is a HOST array of n <= 2^20 tensors; it is read before the call returns, so a captured call keeps the addresses that it was given.  A tensor is dense, at any
  * multiple of its elements' size, and may have no elements (its pointers are then not looked at).  out may be in: nothing is written where the norm is no
- * larger than `largest`.  An output that overlaps another tensor's input or output, the norm or the workspace is refused.  moe_grad_norm does not look at `out`.
+ * larger than `largest`.  An output that overlaps another tensor's input or output, the norm or the workspace is refused, and so is a norm or a workspace over an
+ * input or over each other.  moe_grad_norm does not look at `out`.
  *   norm [1] fp32; 0 < largest < infinity.  ws at least moe_grad_norm_workspace_bytes(n).
  */
 enum { MOE_TYPE_BF16 = 0, MOE_TYPE_F32 = 1 };

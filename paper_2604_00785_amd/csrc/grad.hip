@@ -209,6 +209,17 @@ bool bad_grads(const moe_grad* g, int n, bool clip) {
 }
 // Whether some output lies over an input other than its own, or over another output (the norm and the workspace are such): what is there would depend on who comes first.
 struct Range { uintptr_t from, to; bool out; };
+// The norm alone: its inputs are read while the workgroups' sums are written.
+bool norm_overlaps(const moe_grad* g, int n, const float* norm, const void* ws, size_t ws_bytes) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(norm), sums = reinterpret_cast<uintptr_t>(ws);
+  const auto meet = [](uintptr_t a, uintptr_t a_bytes, uintptr_t b, uintptr_t b_bytes) { return a < b + b_bytes && b < a + a_bytes; };
+  bool some = meet(at, sizeof(float), sums, ws_bytes);
+  for (int i = 0; i < n; ++i) {
+    const uintptr_t in = reinterpret_cast<uintptr_t>(g[i].in), bytes = static_cast<uintptr_t>(g[i].count) * bytes_of(g[i]);
+    some |= g[i].count > 0 && (meet(in, bytes, at, sizeof(float)) || meet(in, bytes, sums, ws_bytes));
+  }
+  return some;
+}
 int overlap(const moe_grad* g, int n, const float* norm, const void* ws, size_t ws_bytes) {
   Range few[2 * 256 + 2];
   Range* r = n <= 256 ? few : new (std::nothrow) Range[2 * static_cast<size_t>(n) + 2];
@@ -293,7 +304,8 @@ int run_grads(const moe_grad* g, int n, bool clip, double largest, float* norm, 
   unsigned long long pieces = 0;
   for (int i = 0; i < n; ++i) pieces += static_cast<unsigned long long>(g[i].count) / (16 / bytes_of(g[i])) + 1;
   if (pieces > 1ull << 40) return MOE_ERR_INVALID;   // chunks are counted in 32 bits
-  if (clip && overlap(g, n, norm, ws, moe_grad_norm_workspace_bytes(n)) != MOE_OK) return MOE_ERR_INVALID;
+  const size_t used = moe_grad_norm_workspace_bytes(n);
+  if (clip ? overlap(g, n, norm, ws, used) != MOE_OK : norm_overlaps(g, n, norm, ws, used)) return MOE_ERR_INVALID;
   const bool wide = pieces >= FEW_PIECES, few = n <= FEW_TENSORS;
   GradCall c{g, n, static_cast<double*>(ws), largest, norm, s};
   int parts = 0;
