@@ -683,8 +683,8 @@ def _grad_table(grads, outs):
     n = len(grads)
     if n == 0:
         raise MoeError("grads: no tensors")
-    dev = _device_of(grads[0], "grads[0]")
     given = types, counts = _types_and_sizes(grads, "grads")
+    dev = _device_of(grads[0], "grads[0]")
     kinds = [*map(_GRAD_TYPES.get, types)]
     if None in kinds:
         raise MoeError(f"grads[{kinds.index(None)}]: expected bfloat16 or float32, got {types[kinds.index(None)]}")

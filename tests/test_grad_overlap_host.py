@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 from paper_2604_00785_amd import binding as B
 from test_more_operators_host import INVALID, WORKSPACE, N, table
@@ -24,3 +25,11 @@ def test_norm_refuses_a_workspace_over_its_inputs(more):
         assert call((1 << 50, 0, 10, BF16), norm, ws, n) == INVALID, norm
     # side by side they do not overlap, and what lies behind the bytes that it uses is not the call's: nothing of this is refused before the workspace's size is
     assert call((ws, 0, 10, BF16), far, ws, n - 1) == WORKSPACE
+
+
+def test_first_entry_that_is_no_tensor_is_refused_by_name():
+    g, one, ws = torch.zeros(10), torch.zeros(1), torch.zeros(1 << 20, dtype=torch.uint8)
+    for call in (lambda grads: B.moe_grad_norm(grads, one, ws), lambda grads: B.moe_grad_clip(grads, 1.0, one, None, ws), lambda grads: B.moe_grad_clip(grads, 1.0, one, [g, g], ws)):
+        for grads in ([1.0, g], [None, g], ["g", g], [[1.0], g], [g, 1.0]):
+            with pytest.raises(B.MoeError, match="grads"):
+                call(grads)
