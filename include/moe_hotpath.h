@@ -427,7 +427,8 @@ int moe_head_score_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* targ
  * Its derivative for given dlogp and dentropy [T] fp32 (NULL: zeros), with logp, entropy and lse as the forward call left them:
  *   dz[t, v] = (dlogp ([v == target] - p) - dentropy p (log p + entropy)) / temperature;  dx = dz . W;  dW = dz^T . x
  * Sizes, pieces of the vocabulary and rounding as moe_head_ce_bwd; dW takes what rounding dz loses for up to 256 tokens that count.  ws at least
- * moe_head_score_bwd_workspace_bytes(T, d, V, v_piece).
+ * moe_head_score_bwd_workspace_bytes(T, d, V, v_piece).  (A workspace of that size for T tokens serves fewer tokens as well, here and in the forward call, as it does in
+ * moe_head_ce_* and moe_head_distill_*; where the reductions have room for fewer parts than the rules take, sums are added up in another order.)
  * p is off by about 1e-6 of the logits' size over the temperature times itself, and log p + entropy by as much, but for the likeliest column of a token with an entropy below
  * 1/4: that is formed apart, so that the gradient of an entropy next to zero has the digits of any other.
  */

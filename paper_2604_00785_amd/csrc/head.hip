@@ -740,28 +740,32 @@ template <int S> double head_time(double tiles, double steps, double fixed) {
 // The backward products of `cols` columns: their tiles' edge and the parts of either reduction, dW's in more than one only where its tiles do not fill the
 // chip, and not in pieces of the vocabulary (`whole`), whose sums would have to be rounded one by one.  The parts of dx are those for all T
 // tokens; they are chosen again for the tokens that have a loss, in the room that these leave.
+// Parts are no more than their sums have `room` for, in bytes: a workspace may be one for more tokens, whose rule wants fewer.
 struct BwdShape { int edge, dx_parts, dw_parts; };
-template <int S> void weigh_bwd(int T, int d, int cols, int depth, bool whole, double& best, BwdShape& shape) {
+size_t bwd_part_bytes(int T, int d, int cols, int dx_parts, int dw_parts) {
+  return (static_cast<size_t>(dx_parts) * T + (dw_parts > 1 ? static_cast<size_t>(dw_parts) * cols : 0)) * d * sizeof(float);
+}
+template <int S> void weigh_bwd(int T, int d, int cols, int depth, bool whole, size_t room, double& best, BwdShape& shape) {
   const int places = HEAD_CUS * Tile<S>::PER_CU, wide = ceil_div(d, S), steps = ceil_div(cols, BK), dw_steps = ceil_div(depth, BK);
   const long long dx_tiles = static_cast<long long>(ceil_div(T, S)) * wide, dw_tiles = static_cast<long long>(ceil_div(cols, S)) * wide;
   int q = 1;
-  if (whole) while (dw_tiles * (q + 1) <= places && dw_steps / (q + 1) >= 4) ++q;
+  if (whole) while (dw_tiles * (q + 1) <= places && dw_steps / (q + 1) >= 4 && bwd_part_bytes(T, d, cols, 1, q + 1) <= room) ++q;
   constexpr int some[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 56, 64};
   for (int p : some) {
-    if (p > 1 && (steps / p < 4 || dx_tiles * p > 8ll * places)) break;
+    if (p > 1 && (steps / p < 4 || dx_tiles * p > 8ll * places || bwd_part_bytes(T, d, cols, p, q) > room)) break;
     const double time = head_bwd_time(static_cast<int>(dx_tiles * p), head_dx_each<S>(steps, p), static_cast<int>(dw_tiles * q), head_dw_each<S>(dw_steps, q), places) +
                         (static_cast<double>(p) * T + (q > 1 ? static_cast<double>(q) * cols : 0.0)) * d / 1.0e6;
     if (time < best) { best = time; shape = {S, p, q}; }
   }
 }
-BwdShape head_bwd_shape(int T, int d, int cols, bool whole, int low = LOW_TOKENS) {
+BwdShape head_bwd_shape(int T, int d, int cols, bool whole, int low, size_t room = ~static_cast<size_t>(0)) {
   BwdShape shape{128, 1, 1};
   double best = 1e300;
   const int depth = T <= low ? 2 * T : T;
   // One reduction step of dW, all of it waiting for memory: two workgroups on a compute unit wait better.  256 / 128 in us: 10 tokens, d 2048, V 50304 110 / 94;
   // 8, 2880, 35317 117 / 96; 1, 832, 61930 62 / 50; 22, 1216, 178071 248 / 257.  (100, 2048, 50304: 119 / 118, as the model has it.)
-  if (depth > 64) weigh_bwd<256>(T, d, cols, depth, whole, best, shape);
-  weigh_bwd<128>(T, d, cols, depth, whole, best, shape);
+  if (depth > 64) weigh_bwd<256>(T, d, cols, depth, whole, room, best, shape);
+  weigh_bwd<128>(T, d, cols, depth, whole, room, best, shape);
   return shape;
 }
 // The logits' products.  Their epilogues take the vector unit, which a tile of 256 leaves idle matrix cores beside and two of 128 share a compute unit for:
@@ -1019,18 +1023,15 @@ int run_score_fwd(const HeadCall& c, const ScoreShape& shape, int* edges) {
   return moe_head_score_join(j, edge, c.s);
 }
 
-// The edge of the tiles that the sums of SURE rows come from, and what they take of the workspace.
-int sure_edge(int T, int d, int V, const int* edges) { return edges != nullptr && edges[0] != 0 ? edges[0] : logits_edge(T, V, d, 9.5); }
-size_t sure_part_bytes(int T, int d, int V, const int* edges) {
-  return static_cast<size_t>((T + 15) & ~15) * ceil_div(V, sure_edge(T, d, V, edges) / 2) * sizeof(HeadBest);
-}
-int run_head_bwd(const HeadCall& c, int v_piece, int dz_parts, int* edges) {
+// What the sums of SURE rows take of the workspace, in strips of 64 columns (tiles of 256 leave half of them).
+size_t sure_part_bytes(int T, int V) { return static_cast<size_t>((T + 15) & ~15) * ((V + 63) / 64) * sizeof(HeadBest); }
+int run_head_bwd(const HeadCall& c, size_t ws_bytes, int v_piece, int dz_parts, int* edges) {
   const int low = c.score ? SCORE_LOW_TOKENS : LOW_TOKENS;
   const HeadLayout l = head_layout(c.T, c.d, c.V, c.t.K, true, low);
   const int piece = head_piece(c.T, c.V, v_piece), wanted = edges != nullptr ? edges[1] : 0;
   uint16_t* dz = reinterpret_cast<uint16_t*>(c.ws + l.big);
   float* part = reinterpret_cast<float*>(c.ws + l.big + head_dz_bytes(c.T, piece, low));
-  BwdShape shape = head_bwd_shape(c.T, c.d, piece, piece >= c.V, low);
+  BwdShape shape = head_bwd_shape(c.T, c.d, piece, piece >= c.V, low, ws_bytes - l.big - head_dz_bytes(c.T, piece, low));
   float* dw_part = part + static_cast<size_t>(shape.dx_parts) * c.T * c.d;
   if (wanted != 0) shape.edge = wanted;
   if (edges != nullptr) edges[1] = shape.edge;
@@ -1049,7 +1050,7 @@ int run_head_bwd(const HeadCall& c, int v_piece, int dz_parts, int* edges) {
     GemmArgs a{};
     HeadArgs h{};
     fill_head(c, l, a, h);
-    const int edge = sure_edge(c.T, c.d, c.V, edges);
+    const int edge = edges != nullptr && edges[0] != 0 ? edges[0] : logits_edge(c.T, c.V, c.d, 9.5);
     a.offsets = control + SURE - 1;
     a.A0 = reinterpret_cast<const uint16_t*>(c.ws + l.xc); a.A1 = c.x; a.B0 = c.W; a.K = c.d; a.N = c.V; a.M = c.T;
     h.strips = ceil_div(c.V, edge / 2);
@@ -1122,12 +1123,18 @@ extern "C" size_t moe_head_fwd_workspace_bytes(int T, int d, int V, int K) {
 }
 
 namespace {
+bool bad_piece(int v_piece) { return v_piece < 0 || v_piece % 256 != 0; }
+// What a backward pass cannot do without: each reduction in one part.
+size_t head_bwd_least(int T, int d, int V, int K, int v_piece, int low) {
+  return head_layout(T, d, V, K, true, low).big + head_dz_bytes(T, head_piece(T, V, v_piece), low) + bwd_part_bytes(T, d, V, 1, 1);
+}
+// What it is laid out for, which is the least of fewer tokens as well: these may have all columns in one piece, of 2 GiB at most, where T have somewhat less.
 size_t head_bwd_bytes(int T, int d, int V, int K, int v_piece, int low) {
-  if (bad_head_dims(T, d, V, K) || v_piece < 0 || v_piece % 256 != 0) return 0;
+  if (bad_head_dims(T, d, V, K) || bad_piece(v_piece)) return 0;
   const int piece = head_piece(T, V, v_piece);
   const BwdShape shape = head_bwd_shape(T, d, piece, piece >= V, low);
-  return head_layout(T, d, V, K, true, low).big + head_dz_bytes(T, piece, low) +
-         (static_cast<size_t>(shape.dx_parts) * T + (shape.dw_parts > 1 ? static_cast<size_t>(shape.dw_parts) * V : 0)) * d * sizeof(float);
+  const size_t dz = head_dz_bytes(T, piece, low), one = static_cast<size_t>(1) << 31;
+  return head_layout(T, d, V, K, true, low).big + (v_piece == 0 && piece < V && dz < one ? one : dz) + bwd_part_bytes(T, d, V, shape.dx_parts, shape.dw_parts);
 }
 }  // namespace
 extern "C" size_t moe_head_bwd_workspace_bytes(int T, int d, int V, int K, int v_piece) { return head_bwd_bytes(T, d, V, K, v_piece, LOW_TOKENS); }
@@ -1157,12 +1164,12 @@ extern "C" int moe_head_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t*
                             int v_piece, moe_bf16* dx, moe_bf16* dW, void* ws, size_t ws_bytes, void* stream, int* edges) {
   if (bad_head_dims(T, d, V, K) || bad_temperature(temperature) || v_piece < 0 || v_piece % 256 != 0 || bad_edge_list(edges, 2)) return MOE_ERR_INVALID;
   if (bad_ptrs({x, W, target, loss, lse, dloss, dx, dW, ws}) || (K > 0 && bad_ptrs({ids, teacher, lse_t, dkd}))) return MOE_ERR_INVALID;
-  if (ws_bytes < moe_head_bwd_workspace_bytes(T, d, V, K, v_piece)) return MOE_ERR_WORKSPACE;
+  if (ws_bytes < head_bwd_least(T, d, V, K, v_piece, LOW_TOKENS)) return MOE_ERR_WORKSPACE;
   HeadCall c{};
   c.x = x; c.W = W; c.target = target; c.t = {ids, teacher, temperature, K}; c.T = T; c.d = d; c.V = V;
   c.in_loss = loss; c.in_lse = lse; c.in_lse_t = lse_t; c.dloss = dloss; c.dkd = dkd; c.dx = dx; c.dW = dW;
   c.ws = static_cast<char*>(ws); c.s = static_cast<hipStream_t>(stream);
-  return run_head_bwd(c, v_piece, 1, edges);
+  return run_head_bwd(c, ws_bytes, v_piece, 1, edges);
 }
 
 extern "C" int moe_head_ce_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, int T, int d, int V, float* loss, float* lse,
@@ -1194,30 +1201,52 @@ extern "C" int moe_head_distill_bwd(const moe_bf16* x, const moe_bf16* W, const 
 // Log probabilities, entropies and alternatives.  edges, for tests: as above; forward edges[1]: what score_shape calls path; backward edges[0]: 1000 p + edge for
 // logits in p parts.
 namespace {
-size_t score_bwd_bytes(int T, int d, int V, int v_piece, int wanted, const int* edges) {
-  const size_t all = head_bwd_bytes(T, d, V, 0, v_piece, SCORE_LOW_TOKENS);
-  if (all == 0) return 0;
-  const int piece = head_piece(T, V, v_piece), parts = score_dz_parts(T, d, V, piece, wanted);
-  const size_t least = head_layout(T, d, V, 0, true, SCORE_LOW_TOKENS).big +
-                       (piece < V ? sure_part_bytes(T, d, V, edges) : head_dz_bytes(T, piece, SCORE_LOW_TOKENS) + (parts > 1 ? score_part_bytes(T, V, {true, 128, parts}) : 0));
-  return all > least ? all : least;
+// The rules take other ways for fewer tokens, some of which need more.  A call takes the one that its workspace has room for, and workspaces are laid out for what fewer
+// tokens want too, so that one for the largest batch serves them all: the largest of the sizes of T and of the tokens that f is called with.
+template <typename F> size_t over_fewer(int T, int every16, F&& f) {
+  size_t most = f(T);
+  const auto look = [&](int t) { const size_t n = f(t); most = n > most ? n : most; };
+  for (int t = 17; t < T && t <= every16; t += 16) look(t);       // (the first of the 16 rows that are laid out together wants the most parts)
+  for (int t = 1; t < T; t *= 2) look(t);
+  return most;
+}
+size_t score_fwd_need(int T, int d, int V, int K, const ScoreShape& s) { return head_layout(T, d, V, 0, false).big + score_part_bytes(T, V, s); }
+// Strips, which need no more for fewer tokens.
+ScoreShape score_strips(int T, int d, int V, int K) { return {false, score_edge(T, d, V, K, false), 1}; }
+size_t score_bwd_need(int T, int d, int V, int v_piece, int dz_parts) {
+  const int piece = head_piece(T, V, v_piece);
+  return head_layout(T, d, V, 0, true, SCORE_LOW_TOKENS).big +
+         (piece < V ? sure_part_bytes(T, V) : head_dz_bytes(T, piece, SCORE_LOW_TOKENS) + (dz_parts > 1 ? score_part_bytes(T, V, {true, 128, dz_parts}) : 0));
 }
 bool bad_score(int T, int d, int V, int K) { return bad_head_dims(T, d, V, 0) || K < 0 || K > SCORE_MAX_K || K > V; }
 }  // namespace
 extern "C" size_t moe_head_score_fwd_workspace_bytes(int T, int d, int V, int K) {
   if (bad_score(T, d, V, K)) return 0;
-  return head_layout(T, d, V, 0, false).big + score_part_bytes(T, V, score_shape(T, d, V, K, 0));
+  const auto most = [](size_t a, size_t b) { return a > b ? a : b; };
+  // (the reduction in parts, what fewer tokens may want more for, takes 512 tiles at most)
+  const int in_parts = V <= SCORE_WHOLE_V && d >= 8 * BK ? HEAD_CUS * 128 / ceil_div(V, 128) : 0;
+  return over_fewer(T, in_parts, [&](int t) {
+    return most(score_fwd_need(t, d, V, K, score_strips(t, d, V, K)), score_fwd_need(t, d, V, K, score_shape(t, d, V, K, 0)));
+  });
 }
-extern "C" size_t moe_head_score_bwd_workspace_bytes(int T, int d, int V, int v_piece) { return score_bwd_bytes(T, d, V, v_piece, 0, nullptr); }
+extern "C" size_t moe_head_score_bwd_workspace_bytes(int T, int d, int V, int v_piece) {
+  if (bad_head_dims(T, d, V, 0) || bad_piece(v_piece)) return 0;
+  return over_fewer(T, 2 * SCORE_LOW_TOKENS, [&](int t) {
+    const size_t all = head_bwd_bytes(t, d, V, 0, v_piece, SCORE_LOW_TOKENS), need = score_bwd_need(t, d, V, v_piece, score_dz_parts(t, d, V, head_piece(t, V, v_piece), 0));
+    return all > need ? all : need;
+  });
+}
 
 extern "C" int moe_head_score_fwd_edges(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, int T, int d, int V, int K,
                                         float* logp, float* entropy, float* lse, int32_t* ids, float* top, void* ws, size_t ws_bytes, void* stream,
                                         int* edges) {
   if (bad_score(T, d, V, K) || bad_temperature(temperature) || bad_edge_list(edges, 1)) return MOE_ERR_INVALID;
   if (bad_ptrs({x, W, target, logp, entropy, lse, ws}) || (K > 0 && bad_ptrs({ids, top}))) return MOE_ERR_INVALID;
-  const ScoreShape shape = score_shape(T, d, V, K, edges != nullptr ? edges[1] : 0);
+  const int path = edges != nullptr ? edges[1] : 0;
+  ScoreShape shape = score_shape(T, d, V, K, path);
   if ((shape.whole && V > SCORE_WHOLE_V) || shape.parts > d / BK) return MOE_ERR_INVALID;
-  if (ws_bytes < head_layout(T, d, V, 0, false).big + score_part_bytes(T, V, shape)) return MOE_ERR_WORKSPACE;
+  if (path == 0 && ws_bytes < score_fwd_need(T, d, V, K, shape)) shape = score_strips(T, d, V, K);
+  if (ws_bytes < score_fwd_need(T, d, V, K, shape)) return MOE_ERR_WORKSPACE;
   HeadCall c{};
   c.x = x; c.W = W; c.target = target; c.t.temperature = 1.f; c.T = T; c.d = d; c.V = V;
   c.score = true; c.tau = temperature; c.K = K;
@@ -1230,15 +1259,17 @@ extern "C" int moe_head_score_bwd_edges(const moe_bf16* x, const moe_bf16* W, co
                                         moe_bf16* dx, moe_bf16* dW, void* ws, size_t ws_bytes, void* stream, int* edges) {
   const int wanted = edges != nullptr ? edges[0] / 1000 : 0;
   if (wanted > 0) edges[0] %= 1000;
-  if (bad_head_dims(T, d, V, 0) || bad_temperature(temperature) || v_piece < 0 || v_piece % 256 != 0 || bad_edge_list(edges, 2) || wanted > d / BK) return MOE_ERR_INVALID;
+  if (bad_head_dims(T, d, V, 0) || bad_temperature(temperature) || bad_piece(v_piece) || bad_edge_list(edges, 2) || wanted > d / BK) return MOE_ERR_INVALID;
   if (bad_ptrs({x, W, target, logp, entropy, lse, dlogp, dx, dW, ws}) || !moe_aligned16(dentropy)) return MOE_ERR_INVALID;
-  if (ws_bytes < score_bwd_bytes(T, d, V, v_piece, wanted, edges)) return MOE_ERR_WORKSPACE;
+  int dz_parts = score_dz_parts(T, d, V, head_piece(T, V, v_piece), wanted);
+  if (wanted == 0 && ws_bytes < score_bwd_need(T, d, V, v_piece, dz_parts)) dz_parts = 1;
+  if (ws_bytes < score_bwd_need(T, d, V, v_piece, dz_parts) || ws_bytes < head_bwd_least(T, d, V, 0, v_piece, SCORE_LOW_TOKENS)) return MOE_ERR_WORKSPACE;
   HeadCall c{};
   c.x = x; c.W = W; c.target = target; c.t.temperature = 1.f; c.T = T; c.d = d; c.V = V;
   c.score = true; c.tau = temperature;
   c.in_loss = logp; c.in_lse = lse; c.in_entropy = entropy; c.dloss = dlogp; c.dentropy = dentropy; c.dx = dx; c.dW = dW;
   c.ws = static_cast<char*>(ws); c.s = static_cast<hipStream_t>(stream);
-  return run_head_bwd(c, v_piece, score_dz_parts(T, d, V, head_piece(T, V, v_piece), wanted), edges);
+  return run_head_bwd(c, ws_bytes, v_piece, dz_parts, edges);
 }
 extern "C" int moe_head_score_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, int T, int d, int V, int K, float* logp,
                                   float* entropy, float* lse, int32_t* ids, float* top, void* ws, size_t ws_bytes, void* stream) {
