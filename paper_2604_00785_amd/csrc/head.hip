@@ -989,8 +989,9 @@ ScoreShape score_shape(int T, int d, int V, int K, int path) {
   const int parts = path == 0 ? score_parts(T, d, V, s.edge, whole, K > 0 ? -4.0 : 0.5 + 1.8e-6 * T * V) : 1;
   return parts > 1 ? ScoreShape{true, 128, parts} : s;
 }
-size_t score_part_bytes(int T, int V, const ScoreShape& s) {
-  return static_cast<size_t>((T + 15) & ~15) * (s.whole ? static_cast<size_t>(s.parts) * score_ld(V) * sizeof(float) : static_cast<size_t>((V + 63) / 64) * sizeof(HeadStrip));
+size_t score_part_bytes(int T, int V, int K, const ScoreShape& s) {
+  const size_t strip = K > 0 ? sizeof(HeadStrip) : sizeof(HeadBest);     // (strips of 64 columns; tiles of 256 leave half as many)
+  return static_cast<size_t>((T + 15) & ~15) * (s.whole ? static_cast<size_t>(s.parts) * score_ld(V) * sizeof(float) : static_cast<size_t>((V + 63) / 64) * strip);
 }
 // The same of the backward pass, whose gradient is formed by a launch of its own then.  (Not in pieces of the vocabulary.)
 int score_dz_parts(int T, int d, int V, int piece, int wanted) {
@@ -1023,8 +1024,8 @@ int run_score_fwd(const HeadCall& c, const ScoreShape& shape, int* edges) {
   return moe_head_score_join(j, edge, c.s);
 }
 
-// What the sums of SURE rows take of the workspace, in strips of 64 columns (tiles of 256 leave half of them).
-size_t sure_part_bytes(int T, int V) { return static_cast<size_t>((T + 15) & ~15) * ((V + 63) / 64) * sizeof(HeadBest); }
+// What the sums of SURE rows take of the workspace.
+size_t sure_part_bytes(int T, int V) { return score_part_bytes(T, V, 0, {false, 128, 1}); }
 int run_head_bwd(const HeadCall& c, size_t ws_bytes, int v_piece, int dz_parts, int* edges) {
   const int low = c.score ? SCORE_LOW_TOKENS : LOW_TOKENS;
   const HeadLayout l = head_layout(c.T, c.d, c.V, c.t.K, true, low);
@@ -1210,13 +1211,13 @@ template <typename F> size_t over_fewer(int T, int every16, F&& f) {
   for (int t = 1; t < T; t *= 2) look(t);
   return most;
 }
-size_t score_fwd_need(int T, int d, int V, int K, const ScoreShape& s) { return head_layout(T, d, V, 0, false).big + score_part_bytes(T, V, s); }
+size_t score_fwd_need(int T, int d, int V, int K, const ScoreShape& s) { return head_layout(T, d, V, 0, false).big + score_part_bytes(T, V, K, s); }
 // Strips, which need no more for fewer tokens.
 ScoreShape score_strips(int T, int d, int V, int K) { return {false, score_edge(T, d, V, K, false), 1}; }
 size_t score_bwd_need(int T, int d, int V, int v_piece, int dz_parts) {
   const int piece = head_piece(T, V, v_piece);
   return head_layout(T, d, V, 0, true, SCORE_LOW_TOKENS).big +
-         (piece < V ? sure_part_bytes(T, V) : head_dz_bytes(T, piece, SCORE_LOW_TOKENS) + (dz_parts > 1 ? score_part_bytes(T, V, {true, 128, dz_parts}) : 0));
+         (piece < V ? sure_part_bytes(T, V) : head_dz_bytes(T, piece, SCORE_LOW_TOKENS) + (dz_parts > 1 ? score_part_bytes(T, V, 0, {true, 128, dz_parts}) : 0));
 }
 bool bad_score(int T, int d, int V, int K) { return bad_head_dims(T, d, V, 0) || K < 0 || K > SCORE_MAX_K || K > V; }
 }  // namespace

@@ -16,3 +16,10 @@ def test_sizes_of_the_scores_grow_with_the_tokens(d, V):
         # (with many tokens, which serve any fewer in whatever room there is, the parts of a reduction may take less than some tokens before)
         sizes = [B.moe_head_score_bwd_workspace_bytes(T, d, V, piece) for T in TOKENS if T <= 512]
         assert sizes[0] > 0 and sizes == sorted(sizes), piece
+
+
+def test_scores_without_alternatives_ask_for_what_they_leave():
+    """16 bytes for each 64 columns of a token beside its row (tokens by sixteens)."""
+    for T, d, V in ((8192, 2048, 50304), (1000, 64, 131072), (16384, 128, 40000)):
+        n = B.moe_head_score_fwd_workspace_bytes(T, d, V, 0)
+        assert T * (2 * d + 16 * (V // 64)) <= n <= (T + 15) * (2 * d + 16 * (V // 64 + 1) + 32) + 4096
