@@ -620,7 +620,9 @@ __global__ __launch_bounds__(256) void head_score_dz_kernel(ScoreDzArgs a) {
 void launch_whole(const ScoreJoinArgs& a, dim3 grid, hipStream_t s) {
   const auto launch = [&](auto threads, auto pieces) {
     constexpr int THREADS = decltype(threads)::value, PIECES = decltype(pieces)::value;
-    if (a.K > 0) MOE_LAUNCH("head_score_whole", (head_score_whole_kernel<THREADS, PIECES, true>), grid, dim3(THREADS), 0, s, a);
+    // (1024 threads are for alternatives)
+    if constexpr (THREADS > 512) MOE_LAUNCH("head_score_whole", (head_score_whole_kernel<THREADS, PIECES, true>), grid, dim3(THREADS), 0, s, a);
+    else if (a.K > 0) MOE_LAUNCH("head_score_whole", (head_score_whole_kernel<THREADS, PIECES, true>), grid, dim3(THREADS), 0, s, a);
     else MOE_LAUNCH("head_score_whole", (head_score_whole_kernel<THREADS, PIECES, false>), grid, dim3(THREADS), 0, s, a);
   };
   using std::integral_constant;

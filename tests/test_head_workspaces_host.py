@@ -23,3 +23,11 @@ def test_scores_without_alternatives_ask_for_what_they_leave():
     for T, d, V in ((8192, 2048, 50304), (1000, 64, 131072), (16384, 128, 40000)):
         n = B.moe_head_score_fwd_workspace_bytes(T, d, V, 0)
         assert T * (2 * d + 16 * (V // 64)) <= n <= (T + 15) * (2 * d + 16 * (V // 64 + 1) + 32) + 4096
+
+
+def test_no_kernel_that_nothing_launches():
+    """1024 threads to a token's logits are for alternatives alone; each other number of threads is there with and without them."""
+    names = open(B.LIB_PATH, "rb").read()
+    kernel = lambda threads, pieces, lists: b"head_score_whole_kernelILi%dELi%dELb%dE" % (threads, pieces, lists) in names  # noqa: E731
+    assert kernel(1024, 2, 1) and not kernel(1024, 2, 0)
+    assert all(kernel(t, p, k) for t, p in ((64, 2), (64, 8), (128, 8), (256, 2), (256, 8), (512, 8)) for k in (0, 1))
