@@ -464,11 +464,11 @@ int moe_qk_norm_rope_bwd(const moe_bf16* dqo, long long dqo_ld, const moe_bf16* 
 /*
  * Behind a backward pass: the norm of all gradients of a model together, and their scaling to a largest norm.
  *   norm[0] = sqrt(sum over all tensors of g^2)  (summed in 64 bits in a fixed order, then rounded to fp32)
- *   moe_grad_clip: out = g min(1, largest / (norm + 1e-6)), rounded once; the norm is that of the 64-bit sum.  A norm of infinity makes finite gradients 0, one
+ *   moe_grad_clip: out = g min(1, largest / (norm + 1e-6)), the scale and the product rounded to fp32, then to the type; the norm is that of the 64-bit sum.  A norm of infinity makes finite gradients 0, one
  *   of NaN makes all of them NaN.
  * `grads` is a HOST array of n <= 2^20 tensors; it is read before the call returns, so a captured call keeps the addresses that it was given.  A tensor is dense, at any
- * multiple of its elements' size, and may have no elements (its pointers are then not looked at).  out may be in: nothing is written where the norm is no
- * larger than `largest`.  An output that overlaps another tensor's input or output, the norm or the workspace is refused, and so is a norm or a workspace over an
+ * multiple of its elements' size, and may have no elements (its pointers are then not looked at).  out may be in: nothing is written where the scale is
+ * 1, as where norm + 1e-6 is no larger than `largest`.  An output that overlaps another tensor's input or output, the norm or the workspace is refused, and so is a norm or a workspace over an
  * input or over each other.  moe_grad_norm does not look at `out`.
  *   norm [1] fp32; 0 < largest < infinity.  ws at least moe_grad_norm_workspace_bytes(n).
  */
