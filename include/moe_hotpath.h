@@ -444,7 +444,7 @@ int moe_head_score_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* targ
  *   q, qo [T, Hq, D], k, ko [T, Hk, D] bf16, each with its own distance `ld` from a token to the next in elements (a multiple of 8, at least H D: queries and
  *   keys may be columns of a wider matrix); wq, wk [D] fp32; pos [T] int32 of any value; freq [R / 2] fp32 (may be NULL for R = 0).
  *   D % 8 == 0, D <= 512; R % 16 == 0, 0 <= R <= D; Hq, Hk <= 4096; T <= 2^30.  qo may be q and ko may be k (with the same ld); no other overlap.
- *   eps >= 0 (0: a head of zeros has no norm, its columns are NaN).  A head whose squares sum up to more than fp32 holds (values of 1e19) counts as infinite: zeros.
+ *   eps >= 0 (0: a head of zeros has no norm, its columns are NaN, and one whose mean square is below 2^-126, values of 1e-19, loses digits).  A head whose squares sum up to more than fp32 holds (values of 1e19) counts as infinite: zeros.
  */
 int moe_qk_norm_rope(const moe_bf16* q, long long q_ld, const moe_bf16* k, long long k_ld, const float* wq, const float* wk, const int32_t* pos,
                      const float* freq, int pairs, float eps, int T, int Hq, int Hk, int D, int R, moe_bf16* qo, long long qo_ld,
