@@ -233,7 +233,7 @@ template <int THREADS, bool TWO> __device__ __forceinline__ void form_exact(cons
 template <int THREADS>
 __device__ __forceinline__ void put_alternatives(const ScoreJoinArgs& a, int t, const ScoreResult& r, const int32_t* columns, const double* exact, int m, int top_col, double z_top) {
   const size_t out = static_cast<size_t>(t) * a.K;
-  for (int k = m + threadIdx.x; k < a.K; k += THREADS) {                   // (logits of -infinity)
+  for (int k = m + threadIdx.x; k < a.K; k += THREADS) {                   // (logits of -infinity: columns that are not there)
     a.ids[out + k] = -1;
     a.top[out + k] = __builtin_nanf("");
   }
@@ -242,8 +242,9 @@ __device__ __forceinline__ void put_alternatives(const ScoreJoinArgs& a, int t, 
     return one > two || (one == two && columns[k] < columns[i]);
   }, [&](int i, int above) __attribute__((always_inline)) {
     if (above >= a.K) return;
-    a.ids[out + above] = columns[i];
-    a.top[out + above] = columns[i] == top_col ? -static_cast<float>(r.log_1R) : static_cast<float>((exact[i] - z_top) * a.over_tau - r.log_1R);
+    const bool there = exact[i] != -static_cast<double>(__builtin_inff());
+    a.ids[out + above] = there ? columns[i] : -1;
+    a.top[out + above] = !there ? __builtin_nanf("") : columns[i] == top_col ? -static_cast<float>(r.log_1R) : static_cast<float>((exact[i] - z_top) * a.over_tau - r.log_1R);
   });
 }
 
