@@ -414,7 +414,7 @@ int moe_head_distill_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* ta
  * A token whose target lies outside [0, V) counts for nothing: zeros, and ids of -1; beyond 256 tokens it takes no time in the products.
  *   x [T, d], W [V, d] bf16; target, ids int32; the rest fp32.  d % 64 == 0; V <= 2^20; 0 <= K <= 64 and K <= V (0: ids, top may be NULL); 0 < temperature < infinity.
  * Logits are compared in 64 bits among the K + 4 that are largest by the matrix product in 32 (its error is about 1e-6 of |x| |W row|).
- * Log probabilities and entropies are sums of positive terms: they keep their digits next to zero.  Logits that are NaN or +infinite, or 2^30 and more over the
+ * Log probabilities and entropies are sums of positive terms: they keep their digits next to zero (down to 1e-35; what is smaller may be 0).  Logits that are NaN or +infinite, or 2^30 and more over the
  * temperature, give NaN; one of -infinity is a column that is not there (its log p is -infinity; with fewer columns than K ids are -1 and top NaN), for the forward call.  ws at least moe_head_score_fwd_workspace_bytes(T, d, V, K): about T d * 2 + T V * 5 / 8 bytes, T d * 2 + T V / 4 without alternatives; with
  * alternatives from a small vocabulary (up to 4000 columns, and up to 16384 if many are wanted) the logits themselves, T d * 2 + T V * 4; and up to eight times
  * T V * 4 where few tokens and columns (up to 16384) have long rows, whose products go in parts.

@@ -56,7 +56,9 @@ def gradients(x, W, target, tau, dlogp, dentropy):
     of_top = p * (v.abs() * (near + of_H) + 16 * R.HALF32 * (u.abs() * of_u + v.abs() * (H + log_top.abs())))
     # Where it is another column than the target its gradient may be what the others', of which each is rounded, leave of zero; their sum is one of 32 bits.
     # (An entropy of half of 1/4 at most: the likeliest column is looked after by itself.)
-    others = (err + (R.HALF16 + (V / 2048 + 16) * R.HALF32) * dz.abs()).scatter(1, best, 0.0).sum(1, keepdim=True)
+    # (What rounding the target's loses is known, and goes into the sum as it goes into dx.)
+    rounded = torch.full_like(dz, R.HALF16).scatter(1, y, 2 * R.HALF16 ** 2)
+    others = (err + (rounded + (V / 2048 + 16) * R.HALF32) * dz.abs()).scatter(1, best, 0.0).sum(1, keepdim=True)
     sure = (H < 0.125) | (best == y)
     err.scatter_(1, best, torch.where(sure, of_top + torch.where(best == y, 0.0, others), err).gather(1, best))
     err = err + R.HALF16 * dz.abs()
@@ -73,7 +75,8 @@ def check(got, want, bound, counts, what):
 
 
 CASES = [(1, 64, 200, 1.0, 12, 12), (3, 128, 700, 1.0, 4, 40), (40, 128, 515, 1.0, 8, 60), (40, 128, 515, 0.1, 8, 30), (130, 64, 2049, 0.7, 3, 30), (256, 128, 1031, 1.0, 3, 25),
-         (300, 192, 999, 1.0, 6, 16), (700, 64, 515, 1.5, 3, 60), (4200, 64, 300, 1.0, 4, 30)]
+         (300, 192, 999, 1.0, 6, 16), (700, 64, 515, 1.5, 3, 60), (4200, 64, 300, 1.0, 4, 30),
+         (2383, 192, 145, 1.0, 2, 20), (1400, 64, 3, 1.0, 2, 9), (1030, 128, 6, 0.5, 2, 12), (400, 64, 47, 0.9, 3, 9)]
 
 
 @pytest.mark.parametrize("edge", [128, 256, 0])
@@ -81,7 +84,7 @@ CASES = [(1, 64, 200, 1.0, 12, 12), (3, 128, 700, 1.0, 4, 40), (40, 128, 515, 1.
 def test_sure_of_another_column(T, d, V, tau, least, most, edge):
     x, W, target, dlogp, dentropy = inputs(T, d, V, tau, least, most, seed=T)
     f = forward(x, W, target, 0, tau)
-    for dl in (dlogp, torch.zeros(T)):
+    for dl in (dlogp, torch.zeros(T), 3.0 * dentropy.roll(1)):
         want, bound, counts = gradients(x, W, target, tau, dl, dentropy)
         got = backward(x, W, target, tau, f, dl, dentropy, edge=edge)
         check(got, want, bound, counts, (T, edge))
