@@ -387,7 +387,7 @@ template <int THREADS, int PIECES, bool LISTS> __global__ __launch_bounds__(THRE
 }
 
 // With alternatives: a workgroup of THREADS for each token, 1024 where there are few (d 2048, V 50304, 20 alternatives, us, 256 / 1024: 1 token 18.5 / 12.7, 256 tokens
-// 31.6 / 20.5, 600 tokens 35 / 41).  HALF: columns of a strip.  3074 tokens take 95 to 107 us, most of it for some 30 rows of W each, 390 MB at 4 TB/s.
+// 31.6 / 20.5, 600 tokens 35 / 41; the whole call 257 to 512 tokens 111 / 112.5 to 142 / 140.5; 300 tokens, d 128, V 20000, 4 alternatives 24 / 29, d 512, V 32003, 64 83 / 65).  HALF: columns of a strip.  3074 tokens take 95 to 107 us, most of it for some 30 rows of W each, 390 MB at 4 TB/s.
 template <int HALF, int THREADS>
 __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs a) {
   constexpr int GROUPS = 256, WAVES = THREADS / MOE_WAVE, AT_ONCE = THREADS > 256 ? 4 : 8, STEP = THREADS / 4;
@@ -616,7 +616,9 @@ __global__ __launch_bounds__(256) void head_score_dz_kernel(ScoreDzArgs a) {
 // Threads for a token whose logits are all looked at, each with 32 of them at most: many where there are few tokens, few where there are many (d 832, us of the whole call,
 // 64 / 128 / 256 threads: V 697, 8 alternatives, 500 tokens 36 / 35 / 32, 2000 42 / 44 / 53, 8000 84 / 102 / 145; V 4000, 20 alternatives, 128 / 256: 500 44 / 40, 8000 188 / 214).
 // Short rows in registers for them alone: 8192 tokens, d 2048, V 256, 20 alternatives, with 8 / 2 pieces a thread 146 / 131; 300, 704, 697 33 / 31.
-// A few tokens, their rows formed anew by waves, 256 / 1024 threads: 16, 4096, 5000 39 / 35.5; 200, 2048, 3001 36 / 34; 1, 4096, 256 29.5 / 35.
+// A few tokens, their rows formed anew by waves, 256 / 1024 threads: 16, 4096, 5000 39 / 35.5; 200, 2048, 3001 36 / 34; 1, 4096, 256 29.5 / 35.  At the borders (from a graph):
+// 256, 2048, 8192 33.6 / 32.6; 256, 256, 2049 17.7 / 17.4; 256, 512, 8192 20.1 / 20.2; 1, 512, 2049, one alternative 14.4 / 14.7; 64 alternatives 256, 512, 4096 28.9 / 23.3;
+// 64, 2048, 5000 38 / 28; past 256 tokens 300, 256, 5000 25.5 / 32, 500, 2048, 3000 36.5 / 45.
 // (64 threads are 64 groups: with as many alternatives wanted nearly every column would be a candidate.)
 void launch_whole(const ScoreJoinArgs& a, dim3 grid, hipStream_t s) {
   const auto launch = [&](auto threads, auto pieces) {
