@@ -742,7 +742,6 @@ template <int S> double head_time(double tiles, double steps, double fixed) {
 // The backward products of `cols` columns: their tiles' edge and the parts of either reduction, dW's in more than one only where its tiles do not fill the
 // chip, and not in pieces of the vocabulary (`whole`), whose sums would have to be rounded one by one.  The parts of dx are those for all T
 // tokens; they are chosen again for the tokens that have a loss, in the room that these leave.
-// Parts are no more than their sums have `room` for, in bytes: a workspace may be one for more tokens, whose rule wants fewer.
 struct BwdShape { int edge, dx_parts, dw_parts; };
 size_t bwd_part_bytes(int T, int d, int cols, int dx_parts, int dw_parts) {
   return (static_cast<size_t>(dx_parts) * T + (dw_parts > 1 ? static_cast<size_t>(dw_parts) * cols : 0)) * d * sizeof(float);
@@ -760,7 +759,8 @@ template <int S> void weigh_bwd(int T, int d, int cols, int depth, bool whole, s
     if (time < best) { best = time; shape = {S, p, q}; }
   }
 }
-BwdShape head_bwd_shape(int T, int d, int cols, bool whole, int low, size_t room = ~static_cast<size_t>(0)) {
+constexpr size_t ANY_ROOM = ~static_cast<size_t>(0);
+BwdShape head_bwd_shape(int T, int d, int cols, bool whole, int low, size_t room = ANY_ROOM) {
   BwdShape shape{128, 1, 1};
   double best = 1e300;
   const int depth = T <= low ? 2 * T : T;
@@ -769,6 +769,11 @@ BwdShape head_bwd_shape(int T, int d, int cols, bool whole, int low, size_t room
   if (depth > 64) weigh_bwd<256>(T, d, cols, depth, whole, room, best, shape);
   weigh_bwd<128>(T, d, cols, depth, whole, room, best, shape);
   return shape;
+}
+// The rule's, or, where its parts' sums have not enough room (a workspace may be one for more tokens, whose rule wants fewer), the best that has.
+BwdShape head_bwd_shape_in(int T, int d, int V, int piece, int low, size_t room) {
+  const BwdShape shape = head_bwd_shape(T, d, piece, piece >= V, low);
+  return bwd_part_bytes(T, d, V, shape.dx_parts, shape.dw_parts) <= room ? shape : head_bwd_shape(T, d, piece, piece >= V, low, room);
 }
 // The logits' products.  Their epilogues take the vector unit, which a tile of 256 leaves idle matrix cores beside and two of 128 share a compute unit for:
 // so narrow rows take 128 (more: what the epilogue of a tile of 256 costs beside that of a plain product, 3.0 at 128; K steps of 1.4 us).  256 / 128 in us,
@@ -1034,7 +1039,7 @@ int run_head_bwd(const HeadCall& c, size_t ws_bytes, int v_piece, int dz_parts, 
   const int piece = head_piece(c.T, c.V, v_piece), wanted = edges != nullptr ? edges[1] : 0;
   uint16_t* dz = reinterpret_cast<uint16_t*>(c.ws + l.big);
   float* part = reinterpret_cast<float*>(c.ws + l.big + head_dz_bytes(c.T, piece, low));
-  BwdShape shape = head_bwd_shape(c.T, c.d, piece, piece >= c.V, low, ws_bytes - l.big - head_dz_bytes(c.T, piece, low));
+  BwdShape shape = head_bwd_shape_in(c.T, c.d, c.V, piece, low, ws_bytes - l.big - head_dz_bytes(c.T, piece, low));
   float* dw_part = part + static_cast<size_t>(shape.dx_parts) * c.T * c.d;
   if (wanted != 0) shape.edge = wanted;
   if (edges != nullptr) edges[1] = shape.edge;

@@ -81,3 +81,22 @@ def test_cross_entropy(most, fewer):
         # the same sums, perhaps in another order: what differs is rounded the other way
         for a, b in ((dx, h.dx), (dW, h.dW)):
             assert float((a.double() - b.double()).norm() / b.double().norm()) < R.HALF16 / 8
+
+
+@pytest.mark.parametrize("T,d,V", [(500, 2048, 1031), (256, 1024, 8000), (500, 2048, 3000), (16, 4096, 5000), (200, 704, 5001)])
+def test_a_call_takes_the_same_way_in_its_own_size_as_in_more(T, d, V):
+    """The same bits: its size is all that its rule wants."""
+    fwd, bwd = B.moe_head_score_fwd_workspace_bytes(T, d, V, 3), B.moe_head_score_bwd_workspace_bytes(T, d, V)
+    more = 2 * max(fwd, bwd) + (1 << 28)
+    c = Calls(T, d, V, 3, more)
+    f, g = c.run(fwd, False), c.run(more, False)
+    assert all(torch.equal(f[n], g[n]) for n in f)
+    a, b = c.run(bwd, True, f), c.run(more, True, f)
+    assert all(torch.equal(a[n], b[n]) for n in a)
+    h = B.HeadBuffers(T, d, V)
+    h.run_fwd(c.x, c.W, c.y)
+    for n in (B.moe_head_bwd_workspace_bytes(T, d, V), more):
+        dx, dW = junk(T, d, dtype=torch.bfloat16), junk(V, d, dtype=torch.bfloat16)
+        B.moe_head_ce_bwd(c.x, c.W, c.y, h.loss, h.lse, c.dl, 0, dx, dW, c.ws[:n])
+        a = (dx, dW) if n < more else a
+    assert torch.equal(a[0], dx) and torch.equal(a[1], dW)
