@@ -1000,9 +1000,16 @@ size_t score_part_bytes(int T, int V, int K, const ScoreShape& s) {
   const size_t strip = K > 0 ? sizeof(HeadStrip) : sizeof(HeadBest);     // (strips of 64 columns; tiles of 256 leave half as many)
   return static_cast<size_t>((T + 15) & ~15) * (s.whole ? static_cast<size_t>(s.parts) * score_ld(V) * sizeof(float) : static_cast<size_t>((V + 63) / 64) * strip);
 }
-// The same of the backward pass, whose gradient is formed by a launch of its own then.  (Not in pieces of the vocabulary.)
+// The same of the backward pass, whose gradient is formed by a launch of its own then; 0: in the product's epilogue.  (So it is in pieces of the vocabulary, and without a
+// gradient of the entropy if the reduction is in one part: head_sure_kernel is not needed then.)  One part for few logits of short rows, which that launch and head_sure_kernel take
+// longer for together.  us, from a graph, epilogue / launch of its own: 1 token, d 64, V 300 17.7 / 17.1; 256, 64, 300 27.1 / 22.6; 256, 128, 1031 30.5 / 26.9; 1000, 128, 1031
+// 35.8 / 34.3; 2000, 64, 1000 35.2 / 35.1; 3000, 64, 300 33.5 / 30.8; 300, 192, 3500 35.6 / 35.6; 200, 256, 5000 39.7 / 39.2; 100, 128, 8000 29.8 / 32.1.
+constexpr long long DZ_WHOLE = 1 << 20;
+constexpr int DZ_WHOLE_V = 4096;
 int score_dz_parts(int T, int d, int V, int piece, int wanted) {
-  return piece < V ? 1 : wanted > 0 ? wanted : score_parts(T, d, V, logits_edge(T, V, d, 10.8), false, 1.0);
+  if (piece < V || wanted > 0) return piece < V ? 0 : wanted;
+  const int edge = logits_edge(T, V, d, 10.8), parts = score_parts(T, d, V, edge, false, 1.0);
+  return parts > 1 ? parts : edge == 128 && V <= DZ_WHOLE_V && static_cast<long long>(T) * V <= DZ_WHOLE ? 1 : 0;
 }
 int run_score_fwd(const HeadCall& c, const ScoreShape& shape, int* edges) {
   const HeadLayout l = head_layout(c.T, c.d, c.V, 0, false);
@@ -1079,7 +1086,7 @@ int run_head_bwd(const HeadCall& c, size_t ws_bytes, int v_piece, int dz_parts, 
     const uint16_t* W = c.W + static_cast<size_t>(v0) * c.d;
     a.A0 = reinterpret_cast<const uint16_t*>(c.ws + l.xc); a.A1 = c.x; a.B0 = W; a.O0 = dz; a.K = c.d; a.N = cols; a.M = ld;
     const int edge = settle_edge(edges, logits_edge(c.T, cols, c.d, 10.8));
-    if (c.score && dz_parts > 1) {
+    if (dz_parts > 0) {
       GemmArgs z = a;
       HeadArgs zh = h;
       z.E = dz_parts; z.M = c.T;
@@ -1089,7 +1096,7 @@ int run_head_bwd(const HeadCall& c, size_t ws_bytes, int v_piece, int dz_parts, 
       rc = moe_head_score_dz(g, c.s);
     } else rc = c.score ? launch_logits<HEAD_SCORE_DZ>(a, h, edge, c.T, "gemm_head_score_dz", c.s) : launch_logits<HEAD_DZ>(a, h, edge, c.T, "gemm_head_dz", c.s);
     if (rc != MOE_OK) return rc;
-    if (sures) {
+    if (sures && dz_parts == 0) {
       const int each = ceil_div(c.T, SURE_GROUPS);
       MOE_LAUNCH("head_sure", head_sure_kernel, dim3(ceil_div(c.T, each)), dim3(256), 0, c.s, control, h.row, h.item, dz, c.T, ld, each, l.low, sorted);
       if ((rc = moe_check_launch()) != MOE_OK) return rc;
@@ -1177,7 +1184,7 @@ extern "C" int moe_head_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t*
   c.x = x; c.W = W; c.target = target; c.t = {ids, teacher, temperature, K}; c.T = T; c.d = d; c.V = V;
   c.in_loss = loss; c.in_lse = lse; c.in_lse_t = lse_t; c.dloss = dloss; c.dkd = dkd; c.dx = dx; c.dW = dW;
   c.ws = static_cast<char*>(ws); c.s = static_cast<hipStream_t>(stream);
-  return run_head_bwd(c, ws_bytes, v_piece, 1, edges);
+  return run_head_bwd(c, ws_bytes, v_piece, 0, edges);
 }
 
 extern "C" int moe_head_ce_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, int T, int d, int V, float* loss, float* lse,
@@ -1224,7 +1231,7 @@ ScoreShape score_strips(int T, int d, int V, int K) { return {false, score_edge(
 size_t score_bwd_need(int T, int d, int V, int v_piece, int dz_parts) {
   const int piece = head_piece(T, V, v_piece);
   return head_layout(T, d, V, 0, true, SCORE_LOW_TOKENS).big +
-         (piece < V ? sure_part_bytes(T, V) : head_dz_bytes(T, piece, SCORE_LOW_TOKENS) + (dz_parts > 1 ? score_part_bytes(T, V, 0, {true, 128, dz_parts}) : 0));
+         (piece < V ? sure_part_bytes(T, V) : head_dz_bytes(T, piece, SCORE_LOW_TOKENS) + (dz_parts > 0 ? score_part_bytes(T, V, 0, {true, 128, dz_parts}) : 0));
 }
 bool bad_score(int T, int d, int V, int K) { return bad_head_dims(T, d, V, 0) || K < 0 || K > SCORE_MAX_K || K > V; }
 }  // namespace
@@ -1270,7 +1277,7 @@ extern "C" int moe_head_score_bwd_edges(const moe_bf16* x, const moe_bf16* W, co
   if (bad_head_dims(T, d, V, 0) || bad_temperature(temperature) || bad_piece(v_piece) || bad_edge_list(edges, 2) || wanted > d / BK) return MOE_ERR_INVALID;
   if (bad_ptrs({x, W, target, logp, entropy, lse, dlogp, dx, dW, ws}) || !moe_aligned16(dentropy)) return MOE_ERR_INVALID;
   int dz_parts = score_dz_parts(T, d, V, head_piece(T, V, v_piece), wanted);
-  if (wanted == 0 && ws_bytes < score_bwd_need(T, d, V, v_piece, dz_parts)) dz_parts = 1;
+  if (wanted == 0 && ((edges != nullptr && edges[0] != 0) || (dz_parts == 1 && dentropy == nullptr) || ws_bytes < score_bwd_need(T, d, V, v_piece, dz_parts))) dz_parts = 0;
   if (ws_bytes < score_bwd_need(T, d, V, v_piece, dz_parts) || ws_bytes < head_bwd_least(T, d, V, 0, v_piece, SCORE_LOW_TOKENS)) return MOE_ERR_WORKSPACE;
   HeadCall c{};
   c.x = x; c.W = W; c.target = target; c.t.temperature = 1.f; c.T = T; c.d = d; c.V = V;

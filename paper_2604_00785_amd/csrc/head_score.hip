@@ -578,39 +578,65 @@ __global__ __launch_bounds__(THREADS) void head_score_join_kernel(ScoreJoinArgs 
   put_alternatives<THREADS>(a, t, r, columns, exact, m, top_col, z_top);
 }
 
-// The logits' gradient from their summands: what the epilogue of the product of HEAD_SCORE_DZ does with whole logits, eight columns a thread.
-__global__ __launch_bounds__(256) void head_score_dz_kernel(ScoreDzArgs a) {
+// The logits' gradient from their summands: what the epilogue of the product of HEAD_SCORE_DZ does with whole logits, and, as all of a row is at hand, what head_sure_kernel does
+// behind it.  THREADS to a row, eight columns each at a time.
+template <int THREADS> __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void head_score_dz_kernel(ScoreDzArgs a) {
   typedef __attribute__((ext_vector_type(4))) uint32_t u4;
-  const int pieces = a.ld / 8, rows = a.control[1];
-  const size_t at = static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x;
-  const int row = static_cast<int>(at / pieces), c = static_cast<int>(at - static_cast<size_t>(row) * pieces) * 8;
+  constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1, WAVES = THREADS / MOE_WAVE;
+  __shared__ float part[WAVES];
+  const int tid = threadIdx.x % THREADS, row = blockIdx.x * ROWS + threadIdx.x / THREADS, rows = a.control[1];
   if (row >= rows) return;
-  const int z_ld = score_ld(a.V), y = a.target[row] - c;
+  const int z_ld = score_ld(a.V), y = a.target[row];
   const f32x4_t p = a.row[row];
   const float at_target = a.terms[row][0];
-  float g[8] = {};
+  const float* const z_row = a.part + static_cast<size_t>(row) * z_ld;
+  const auto rounded = [](float x) __attribute__((always_inline)) { return bf16_to_f32(f32_to_bf16(x)); };
+  float sum = 0.f;
+  int found = 0, top = 0;
+  for (int c = tid * 8; c < a.ld; c += THREADS * 8) {
+    float g[8] = {};
 #pragma unroll
-  for (int h = 0; h < 8; h += 4) {
-    if (c + h >= z_ld) continue;
-    const float* z_at = a.part + static_cast<size_t>(row) * z_ld + c + h;
-    f32x4_t z = *reinterpret_cast<const f32x4_t*>(z_at);
-    for (int part = 1; part < a.parts; ++part) z += *reinterpret_cast<const f32x4_t*>(z_at += static_cast<size_t>(a.T) * z_ld);
+    for (int h = 0; h < 8; h += 4) {
+      if (c + h >= z_ld) continue;
+      const float* z_at = z_row + c + h;
+      f32x4_t z = *reinterpret_cast<const f32x4_t*>(z_at);
+      for (int part = 1; part < a.parts; ++part) z += *reinterpret_cast<const f32x4_t*>(z_at += static_cast<size_t>(a.T) * z_ld);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float t = __builtin_fmaf(z[i], a.c1, -p[0]);
-      const float other = score_apart(z[i], a.c1, p) ? __builtin_nanf("") : __builtin_amdgcn_exp2f(t) * __builtin_fmaf(p[2], t, p[1]);
-      g[h + i] = c + h + i >= a.V ? 0.f : h + i == y ? at_target : other;
-      if (h + i == y) a.item[row] = at_target - bf16_to_f32(f32_to_bf16(at_target));
+      for (int i = 0; i < 4; ++i) {
+        const int col = c + h + i;
+        const float t = __builtin_fmaf(z[i], a.c1, -p[0]);
+        float v = __builtin_amdgcn_exp2f(t) * __builtin_fmaf(p[2], t, p[1]);
+        if (col >= a.V) v = 0.f;
+        else if (col == y) v = at_target;
+        else if (score_apart(z[i], a.c1, p)) { ++found; top = col; v = __builtin_nanf(""); }
+        g[h + i] = v;
+        if (v == v) sum += v;
+      }
+    }
+    const auto put = [&](int r) __attribute__((always_inline)) {
+      *reinterpret_cast<u4*>(a.dz + static_cast<size_t>(r) * a.ld + c) = u4{pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]), pack_bf16(g[4], g[5]), pack_bf16(g[6], g[7])};
+    };
+    put(row);
+    if (rows <= a.low) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[i] -= rounded(g[i]);
+      put(rows + row);
     }
   }
-  const auto put = [&](int r) __attribute__((always_inline)) {
-    *reinterpret_cast<u4*>(a.dz + static_cast<size_t>(r) * a.ld + c) = u4{pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]), pack_bf16(g[4], g[5]), pack_bf16(g[6], g[7])};
-  };
-  put(row);
-  if (rows > a.low) return;
+  if (tid == 0) a.item[row] = at_target - rounded(at_target);
+  if (!(p[3] <= 0.f)) return;                                             // (the same for all threads of a row)
+  sum = group_sum<MOE_WAVE>(sum);
+  bool one = __popcll(__ballot(found == 1)) == 1 && __ballot(found > 1) == 0;
+  if constexpr (WAVES > 1) {
+    if (threadIdx.x % MOE_WAVE == 0) part[threadIdx.x / MOE_WAVE] = sum;
+    one = __syncthreads_count(found != 0) == 1;
+    sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) g[i] -= bf16_to_f32(f32_to_bf16(g[i]));
-  put(rows + row);
+    for (int w = 0; w < WAVES; ++w) sum += part[w];
+  }
+  if (!one || found != 1) return;                                         // (NaN for a row that has more of it)
+  a.dz[static_cast<size_t>(row) * a.ld + top] = f32_to_bf16(-sum);
+  if (rows <= a.low) a.dz[static_cast<size_t>(rows + row) * a.ld + top] = f32_to_bf16(-sum - rounded(-sum));
 }
 
 // Threads for a token whose logits are all looked at, each with 32 of them at most: many where there are few tokens, few where there are many (d 832, us of the whole call,
@@ -663,8 +689,9 @@ template <int HALF> void launch_join(const ScoreJoinArgs& a, hipStream_t s) {
 }  // namespace
 
 int moe_head_score_dz(const ScoreDzArgs& a, hipStream_t s) {
-  const size_t pieces = static_cast<size_t>(a.T) * (a.ld / 8);
-  MOE_LAUNCH("head_score_dz", head_score_dz_kernel, dim3(static_cast<unsigned>((pieces + 255) / 256)), dim3(256), 0, s, a);
+  if (a.ld <= 8 * MOE_WAVE) MOE_LAUNCH("head_score_dz", head_score_dz_kernel<MOE_WAVE>, dim3((a.T + 3) / 4), dim3(256), 0, s, a);
+  else if (a.ld <= 4096) MOE_LAUNCH("head_score_dz", head_score_dz_kernel<256>, dim3(a.T), dim3(256), 0, s, a);
+  else MOE_LAUNCH("head_score_dz", head_score_dz_kernel<1024>, dim3(a.T), dim3(1024), 0, s, a);
   return moe_check_launch();
 }
 int moe_head_score_join(const ScoreJoinArgs& a, int edge, hipStream_t s) {
