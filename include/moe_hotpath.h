@@ -430,7 +430,8 @@ int moe_head_score_fwd(const moe_bf16* x, const moe_bf16* W, const int32_t* targ
  * moe_head_score_bwd_workspace_bytes(T, d, V, v_piece).  (A workspace of that size for T tokens serves fewer tokens as well, here and in the forward call, as it does in
  * moe_head_ce_* and moe_head_distill_*; where the reductions have room for fewer parts than the rules take, sums are added up in another order.)
  * p is off by about 1e-6 of the logits' size over the temperature times itself, and log p + entropy by as much, but for the likeliest column of a token with an entropy below
- * 1/4: that is formed apart, so that the gradient of an entropy next to zero has the digits of any other.
+ * 1/4: that is formed apart, so that the gradient of an entropy next to zero has the digits of any other.  Logits of 10^6 and more over the temperature leave p no digits, and
+ * their tokens' gradients may be NaN.
  */
 size_t moe_head_score_bwd_workspace_bytes(int T, int d, int V, int v_piece);
 int moe_head_score_bwd(const moe_bf16* x, const moe_bf16* W, const int32_t* target, float temperature, const float* logp, const float* entropy,
